@@ -506,6 +506,144 @@ as2d_status as2d_budget_select(const double* cost_us, const int32_t* refs,
                                int32_t n_commit, int32_t window, int32_t b_max,
                                double* tok_s, int32_t* calls, int32_t* best_b);
 
+/* ---- Operators on caches and logits ------------------------------------------
+   What a decoder around this library needs beside the chain of greedy
+   candidates: attention of a tree of drafted tokens over a cache, the weight
+   that attention gives each cache entry and eviction by it, probabilities at a
+   temperature, and the acceptance of drafted tokens from given random numbers.
+   They work on the caller's tensors.
+
+   Each call is enqueued on `stream` without a host synchronisation and can be
+   captured into a graph; nothing is kept from one call to the next.  A
+   workspace needs no initial contents, 256-byte alignment, and may serve any
+   number of calls that run one after another: calls (or captured graphs) that
+   may overlap on the GPU need one each. */
+
+/* A caller's cache: device bf16 [n_layers][batch][n_kv][capacity][head_dim],
+   16-byte aligned; head_dim 64 or 128, capacity <= 65536, batch <=
+   AS2D_MAX_BATCH. */
+typedef struct as2d_cache {
+  void* k;
+  void* v;
+  int32_t n_layers, batch, n_kv, capacity, head_dim;
+} as2d_cache;
+
+#define AS2D_TYPE_BF16 0
+#define AS2D_TYPE_F32 1
+/* Most rows of one request in a call of as2d_tree_attention or
+   as2d_attention_weights. */
+#define AS2D_MAX_TREE 64
+
+/* The query rows of a call.  Request b has rows[b] of them (0 .. AS2D_MAX_TREE),
+   packed request by request; its cache holds kv_len[b] entries of the prefix
+   and, right behind them, at [kv_len[b], kv_len[b] + rows[b]), the entries of
+   these rows in row order.  Row i sees the whole prefix and those of its
+   request's rows j whose bit j is set in visible[row] (itself only if bit i is;
+   bits from rows[b] on are ignored): a tree of drafted tokens gives each row
+   its ancestors and itself.  A row that sees nothing is allowed.
+   q: device [sum rows][n_q][head_dim] of q_type, row r at element r q_stride
+   (q_stride >= n_q head_dim); q and q_stride in bytes are multiples of 16.
+   Query head h reads kv head h / (n_q / n_kv).  kv_len: device int32 [batch].
+   max_len: host bound of the lengths, by which the launch is sized (0: the
+   capacity); results do not depend on it beyond the order of sums.  rows: host
+   int32 [batch].  visible: device uint64 [sum rows], or NULL for a chain (row i
+   sees rows 0 .. i).  scale: the factor of q k (finite, > 0), usually 1 /
+   sqrt(head_dim). */
+typedef struct as2d_tree_rows {
+  const void* q;
+  int32_t q_type, n_q;
+  int64_t q_stride;
+  const int32_t* kv_len;
+  int32_t max_len;
+  const int32_t* rows;
+  const uint64_t* visible;
+  float scale;
+} as2d_tree_rows;
+
+/* Bytes of as2d_tree_attention's workspace on the current device, whatever the
+   call. */
+as2d_status as2d_tree_attention_workspace(const as2d_cache* cache, int64_t* bytes);
+
+/* Softmax attention of the rows over one layer of a cache:
+     out = sum_t p_t v_t,  p = softmax over the visible t of scale q k_t,
+   and, unless lse is NULL, lse = ln sum_t e^(scale q k_t).  out: device [sum
+   rows][n_q][head_dim] of q_type, 16-byte aligned; lse: device float [sum
+   rows][n_q].  Scores, maxima and sums are held in 32 bits.  A row that sees
+   nothing gets out = 0 and lse = -inf.  What a row does not see does not reach
+   its result, whatever it holds (NaN and infinities among it).
+   A request whose kv_len[b] is negative or leaves no room for its rows in the
+   capacity is skipped: its rows of out and lse stay as they were and
+   AS2D_DEVERR_CAPACITY is ORed into error_bits (device int32 [1], set to 0 by
+   the caller beforehand, or NULL), as is AS2D_DEVERR_TIMEOUT where a bounded
+   wait gave up (the outputs are then undefined).  out may not overlap q. */
+as2d_status as2d_tree_attention(const as2d_cache* cache, int32_t layer,
+                                const as2d_tree_rows* rows, void* out, float* lse,
+                                void* workspace, int64_t workspace_bytes,
+                                int32_t* error_bits, void* stream);
+
+/* The weight that the rows' attention gives each entry of one layer's cache,
+   added to what the entries have gathered: with lse as as2d_tree_attention
+   leaves it, over the request's rows i and the query heads h of kv head g,
+     weights[layer][b][g][t] += sum e^(scale q_ih k_t - lse_ih)   t < kv_len[b]
+     weights[layer][b][g][t]  = the same sum       t in the rows' own entries
+   (an entry starts with the weight its own call gives it).  What a row does
+   not see adds 0.  weights: device float [n_layers][batch][n_kv][capacity];
+   entries past the rows' own, and requests without rows, stay as they were.
+   Requests are skipped and flagged as by as2d_tree_attention. */
+as2d_status as2d_attention_weights(const as2d_cache* cache, int32_t layer,
+                                   const as2d_tree_rows* rows, const float* lse,
+                                   float* weights, int32_t* error_bits, void* stream);
+
+/* Bytes of as2d_cache_evict's workspace. */
+as2d_status as2d_cache_evict_workspace(const as2d_cache* cache, int64_t* bytes);
+
+/* Evict entries by gathered weight, in place.  Of every (layer, request, kv
+   head), each by itself, of a request with kv_len[b] > keep[b]: the latest
+   min(recent, keep[b]) entries stay and, of the older ones, those of largest
+   weight, keep[b] in all.  Equal weights: the lower position stays; -0 equals
+   0, and NaN counts as less than every number.  The entries that stay keep
+   their order and move, with their weights, to positions 0 .. keep[b] - 1;
+   what lies behind stays as it was.  kv_len[b] becomes keep[b].  Other
+   requests are left alone.  Keys keep the rotation of their old positions.
+   weights: device float [n_layers][batch][n_kv][capacity]; kv_len: device int32
+   [batch], in and out; keep: host int32 [batch], >= 0; recent >= 0.  A kv_len[b]
+   outside [0, capacity] leaves that request alone. */
+as2d_status as2d_cache_evict(const as2d_cache* cache, float* weights, int32_t* kv_len,
+                             const int32_t* keep, int32_t recent, void* workspace,
+                             int64_t workspace_bytes, void* stream);
+
+/* Probabilities of rows of logits: probs = softmax(logits / temperature) over
+   each row, sums in 32 bits or more.  logits, probs: device float [n_rows][vocab],
+   4-byte aligned; probs may be logits.  temperature: finite, > 0.  Logits of -inf
+   get 0; a row that holds nothing else gets all zeros; NaN or +inf in a row
+   makes the row NaN. */
+as2d_status as2d_token_probs(const float* logits, int32_t n_rows, int32_t vocab,
+                             float temperature, float* probs, void* stream);
+
+/* Accept drafted tokens against the target's probabilities with given random
+   numbers.  Request b drafted k[b] >= 0 candidates (packed in candidates, device
+   int32 [sum k]) and owns k[b] + 1 rows of probs (device float [sum (k + 1)][vocab],
+   row i the target's probabilities after the first i candidates) and of u
+   (device float [sum (k + 1)], in [0, 1)).  draft_probs: device float [sum
+   k][vocab], the drafter's probabilities that each candidate was drawn from, or
+   NULL for candidates that the drafter gave with certainty.
+     Candidate c at place i stands if u_i q_i(c) < p_i(c) (q_i(c) = 1 without
+   draft_probs), exactly; n is the number of candidates before the first that
+   does not.  The token after them is drawn, by u_k, from max(p_n - q_n, 0) if n <
+   k (without draft_probs: p_n without candidate n) and from p_k otherwise: the
+   lowest v at which the sum of the weights up to v exceeds u_k times their total
+   (sums to some 48 bits).  With u uniform the tokens follow the target's
+   distribution.  Weights need not sum to 1; negative and NaN ones count as 0.  If max(p_n -
+   q_n, 0) is 0 throughout the token is drawn from p_n; if that is too, token
+   is -1.  A candidate outside [0, vocab) does not stand and takes nothing from
+   p_n (with draft_probs its row is used as it is).
+   k: host int32 [batch], 1 <= batch <= AS2D_MAX_BATCH, each <= AS2D_MAX_K;
+   candidates may be NULL if all are 0.  n_accepted, token: device int32 [batch]. */
+as2d_status as2d_accept_sampled(const float* probs, const float* draft_probs,
+                                const int32_t* candidates, const int32_t* k, int32_t batch,
+                                int32_t vocab, const float* u, int32_t* n_accepted,
+                                int32_t* token, void* stream);
+
 /* Thread-local description of the last error ("" if none). */
 const char* as2d_last_error(void);
 

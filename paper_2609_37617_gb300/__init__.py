@@ -34,6 +34,9 @@ AS2D_CBUF_BATCH = 8
 CBUF_MODES = {0: "normal", 1: "realign", 2: "alone"}
 AS2D_MAX_K = 16
 AS2D_MAX_BATCH = 64
+AS2D_MAX_TREE = 64
+AS2D_TYPE_BF16 = 0
+AS2D_TYPE_F32 = 1
 
 EXPORTED = ("as2d_model_load", "as2d_kv_init_prefilled", "as2d_verify_block",
             "as2d_decode_step", "as2d_kv_rollback", "as2d_kv_read_state",
@@ -45,7 +48,10 @@ EXPORTED = ("as2d_model_load", "as2d_kv_init_prefilled", "as2d_verify_block",
             "as2d_verify_from_buffers", "as2d_interval_accounting", "as2d_session_run",
             "as2d_budget_select", "as2d_prefill", "as2d_model_set_sm_budget",
             "as2d_cpu_decoder_create", "as2d_cpu_decoder_step", "as2d_cpu_decoder_logits",
-            "as2d_cpu_decoder_reset", "as2d_cpu_decoder_free")
+            "as2d_cpu_decoder_reset", "as2d_cpu_decoder_free",
+            "as2d_tree_attention_workspace", "as2d_tree_attention", "as2d_attention_weights",
+            "as2d_cache_evict_workspace", "as2d_cache_evict", "as2d_token_probs",
+            "as2d_accept_sampled")
 KERNEL_CLASSES = {"qkv": 0, "attention": 1, "o": 2, "gate_up": 3, "down": 4,
                   "lm_head": 5, "other": 6}
 
@@ -74,6 +80,18 @@ class as2d_source_record(ctypes.Structure):
                 ("producer", ctypes.c_int32), ("offset", ctypes.c_int32),
                 ("time", ctypes.c_double), ("confidence", ctypes.c_float),
                 ("has_confidence", ctypes.c_int32)]
+
+
+class as2d_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int32) for n in ("n_layers", "batch", "n_kv", "capacity", "head_dim")]
+
+
+class as2d_tree_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_type", ctypes.c_int32), ("n_q", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("kv_len", ctypes.c_void_p),
+                ("max_len", ctypes.c_int32), ("rows", ctypes.c_void_p),
+                ("visible", ctypes.c_void_p), ("scale", ctypes.c_float)]
 
 
 class as2d_session_spec(ctypes.Structure):
@@ -161,6 +179,18 @@ _lib.as2d_cpu_decoder_free.argtypes = [_P]
 _lib.as2d_cpu_decoder_free.restype = None
 for _n in ("as2d_cpu_decoder_create", "as2d_cpu_decoder_step", "as2d_cpu_decoder_logits",
            "as2d_cpu_decoder_reset"):
+    getattr(_lib, _n).restype = _S
+_CACHE, _ROWS, _I64 = ctypes.POINTER(as2d_cache), ctypes.POINTER(as2d_tree_rows), ctypes.c_int64
+_lib.as2d_tree_attention_workspace.argtypes = [_CACHE, ctypes.POINTER(_I64)]
+_lib.as2d_tree_attention.argtypes = [_CACHE, _S, _ROWS, _P, _P, _P, _I64, _P, _P]
+_lib.as2d_attention_weights.argtypes = [_CACHE, _S, _ROWS, _P, _P, _P, _P]
+_lib.as2d_cache_evict_workspace.argtypes = [_CACHE, ctypes.POINTER(_I64)]
+_lib.as2d_cache_evict.argtypes = [_CACHE, _P, _P, _P, _S, _P, _I64, _P]
+_lib.as2d_token_probs.argtypes = [_P, _S, _S, ctypes.c_float, _P, _P]
+_lib.as2d_accept_sampled.argtypes = [_P, _P, _P, _P, _S, _S, _P, _P, _P, _P]
+for _n in ("as2d_tree_attention_workspace", "as2d_tree_attention", "as2d_attention_weights",
+           "as2d_cache_evict_workspace", "as2d_cache_evict", "as2d_token_probs",
+           "as2d_accept_sampled"):
     getattr(_lib, _n).restype = _S
 _lib.as2d_last_error.argtypes = []
 _lib.as2d_last_error.restype = ctypes.c_char_p
@@ -611,3 +641,137 @@ class State:
             self.close()
         except Exception:
             pass
+
+
+# ---- operators on tensors ------------------------------------------------------
+
+def _tensor(t, name, dtypes, shape=None, contiguous=True):
+    """Checks a CUDA tensor argument and returns its device address."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise TypeError(f"{name} must be a tensor of {' or '.join(map(str, dtypes))}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+class Cache:
+    """A key/value cache of the caller's (two bf16 tensors [n_layers][batch][n_kv]
+    [capacity][head_dim], kept alive here) with the workspace of the operators
+    on it; see include/as2d.h, "Operators on caches and logits".  Calls on one
+    Cache share the workspace, so calls that may overlap on the GPU (several
+    streams, captured graphs) need a Cache each."""
+
+    def __init__(self, k, v):
+        import torch
+        if k.dim() != 5:
+            raise ValueError("k must have shape [n_layers, batch, n_kv, capacity, head_dim]")
+        kp = _tensor(k, "k", (torch.bfloat16,))
+        vp = _tensor(v, "v", (torch.bfloat16,), k.shape)
+        self.k, self.v, self.shape = k, v, tuple(k.shape)
+        self._c = as2d_cache(kp, vp, *self.shape)
+        self._ref = ctypes.byref(self._c)
+        need = _I64()
+        _check(_lib.as2d_tree_attention_workspace(self._ref, ctypes.byref(need)),
+               "as2d_tree_attention_workspace")
+        most = need.value
+        _check(_lib.as2d_cache_evict_workspace(self._ref, ctypes.byref(need)),
+               "as2d_cache_evict_workspace")
+        self._workspace = torch.empty(max(most, need.value), dtype=torch.uint8, device=k.device)
+
+    def _rows(self, q, kv_len, rows, visible, scale, max_len):
+        import torch
+        _, batch, _, _, d = self.shape
+        if len(rows) != batch:
+            raise ValueError(f"rows must name {batch} requests")
+        _tensor(q, "q", (torch.bfloat16, torch.float32), contiguous=False)
+        if q.dim() != 3 or q.shape[2] != d or q.stride(2) != 1 or q.stride(1) != d:
+            raise ValueError(f"q must be [rows, n_q, {d}] with contiguous rows")
+        n = q.shape[0]
+        if n != sum(rows):
+            raise ValueError("q must have as many rows as the requests together")
+        # the stride of a single row is not looked at
+        stride = q.stride(0) if n > 1 else q.shape[1] * d
+        host_rows = _i32_array(rows)
+        r = as2d_tree_rows(
+            q.data_ptr(), AS2D_TYPE_F32 if q.dtype == torch.float32 else AS2D_TYPE_BF16, q.shape[1],
+            stride, _tensor(kv_len, "kv_len", (torch.int32,), (batch,)), int(max_len),
+            ctypes.addressof(host_rows),
+            None if visible is None else _tensor(visible, "visible", (torch.int64, torch.uint64), (n,)),
+            d ** -0.5 if scale is None else float(scale))
+        r.keep = host_rows  # alive as long as the descriptor
+        return r
+
+    def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
+                       lse=None, error_bits=None, stream=0):
+        """as2d_tree_attention; returns out (made like q unless given)."""
+        import torch
+        r = self._rows(q, kv_len, rows, visible, scale, max_len)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _check(_lib.as2d_tree_attention(
+            self._ref, layer, ctypes.byref(r), _tensor(out, "out", (q.dtype,), q.shape),
+            None if lse is None else _tensor(lse, "lse", (torch.float32,), q.shape[:2]),
+            self._workspace.data_ptr(), self._workspace.numel(),
+            None if error_bits is None else _tensor(error_bits, "error_bits", (torch.int32,)),
+            stream), "as2d_tree_attention")
+        return out
+
+    def attention_weights(self, q, lse, weights, kv_len, rows, visible=None, layer=0, scale=None,
+                          max_len=0, error_bits=None, stream=0):
+        """as2d_attention_weights: adds to weights in place."""
+        import torch
+        r = self._rows(q, kv_len, rows, visible, scale, max_len)
+        _check(_lib.as2d_attention_weights(
+            self._ref, layer, ctypes.byref(r), _tensor(lse, "lse", (torch.float32,), q.shape[:2]),
+            _tensor(weights, "weights", (torch.float32,), self.shape[:4]),
+            None if error_bits is None else _tensor(error_bits, "error_bits", (torch.int32,)),
+            stream), "as2d_attention_weights")
+
+    def evict(self, weights, kv_len, keep, recent=0, stream=0):
+        """as2d_cache_evict: cuts the cache, weights and kv_len in place."""
+        import torch
+        batch = self.shape[1]
+        if len(keep) != batch:
+            raise ValueError(f"keep must name {batch} requests")
+        _check(_lib.as2d_cache_evict(
+            self._ref, _tensor(weights, "weights", (torch.float32,), self.shape[:4]),
+            _tensor(kv_len, "kv_len", (torch.int32,), (batch,)), _i32_array(keep), int(recent),
+            self._workspace.data_ptr(), self._workspace.numel(), stream), "as2d_cache_evict")
+
+
+def token_probs(logits, temperature, out=None, stream=0):
+    """as2d_token_probs of logits [rows, vocab]; returns out (made like logits
+    unless given; may be logits)."""
+    import torch
+    lp = _tensor(logits, "logits", (torch.float32,))
+    if logits.dim() != 2:
+        raise ValueError("logits must be [rows, vocab]")
+    if out is None:
+        out = torch.empty_like(logits)
+    _check(_lib.as2d_token_probs(lp, *logits.shape, float(temperature),
+                                 _tensor(out, "out", (torch.float32,), logits.shape), stream),
+           "as2d_token_probs")
+    return out
+
+
+def accept_sampled(probs, candidates, k, u, n_accepted, token, draft_probs=None, stream=0):
+    """as2d_accept_sampled: probs [sum (k + 1), vocab], candidates [sum k] (or
+    None), k a list, u [sum (k + 1)], n_accepted and token [batch]."""
+    import torch
+    total, batch = sum(k), len(k)
+    pp = _tensor(probs, "probs", (torch.float32,))
+    if probs.dim() != 2 or probs.shape[0] != total + batch:
+        raise ValueError("probs must be [sum (k + 1), vocab]")
+    _check(_lib.as2d_accept_sampled(
+        pp, None if draft_probs is None or total == 0 else
+        _tensor(draft_probs, "draft_probs", (torch.float32,), (total, probs.shape[1])),
+        None if candidates is None or total == 0 else
+        _tensor(candidates, "candidates", (torch.int32,), (total,)), _i32_array(k), batch,
+        probs.shape[1], _tensor(u, "u", (torch.float32,), (total + batch,)),
+        _tensor(n_accepted, "n_accepted", (torch.int32,), (batch,)),
+        _tensor(token, "token", (torch.int32,), (batch,)), stream), "as2d_accept_sampled")

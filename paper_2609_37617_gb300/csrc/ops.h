@@ -1,0 +1,63 @@
+// ops.h -- launchers of the operators on caches and logits (include/as2d.h,
+// "Operators on caches and logits"), shared by their entry points (ops_api.cu)
+// and the state's calls (as2d_api.cu).
+#pragma once
+
+#include "as2d_internal.h"
+
+namespace as2d {
+
+constexpr int kMaxTree = AS2D_MAX_TREE;
+
+// The rows of a call (as2d_tree_rows) over one layer of a cache.
+struct TreeArgs {
+  RowMap rm;                // rows of each request; may be none
+  const int32_t* len;       // device [batch]
+  int cap, nq, nkv;
+  const void* q;            // [rows][nq][d], rows q_stride elements apart
+  int q_f32;
+  int64_t q_stride;
+  const uint64_t* visible;  // device [rows], or null: a chain
+  float scale_log2;         // scale log2(e)
+  const bf16* k;            // the layer's [batch][nkv][cap][d]
+  const bf16* v;
+  void* out;                // [rows][nq][d] of the queries' type
+  float* lse;               // [rows][nq], nullable
+  int32_t* err;             // error bits, nullable
+};
+
+struct WeightArgs {
+  TreeArgs t;               // out and v unused; lse is read
+  float* w;                 // the layer's [batch][nkv][cap]
+};
+
+struct EvictArgs {
+  bf16 *k, *v;              // [units][cap][d], unit = (layer batch + b) nkv + g
+  float* w;                 // [units][cap]
+  int32_t* len;             // device [batch]
+  int n_layers, batch, nkv, cap, recent;
+  int32_t keep[kMaxBatch];
+  uint16_t* at;             // [units][cap] old position of each entry that stays
+  int32_t* first;           // [units] entries before it stay where they are; -1: nothing moves
+};
+
+struct SampledArgs {
+  const float *probs, *draft, *u;
+  const int32_t* cand;
+  int batch, vocab;
+  int32_t start[kMaxBatch + 1];  // rows before request b (k + 1 each)
+  int32_t *n_out, *token_out;
+};
+
+cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
+                                  cudaStream_t st);
+size_t tree_attention_workspace(int head_dim);
+cudaError_t launch_attention_weights(const WeightArgs& a, int head_dim, int64_t max_keys, cudaStream_t st);
+cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, cudaStream_t st);
+size_t cache_evict_workspace(int64_t units, int cap);
+void cache_evict_carve(EvictArgs& a, int64_t units, void* workspace);
+cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float temperature, float* probs,
+                               cudaStream_t st);
+cudaError_t launch_accept_sampled(const SampledArgs& a, cudaStream_t st);
+
+}  // namespace as2d
