@@ -5,85 +5,669 @@
 // at L_b + j, whose bit j its mask has.  With s_t = scale q k_t over what it sees:
 //   m = max s_t, l = sum e^(s_t - m), out = sum e^(s_t - m) v_t / l, lse = m + ln l.
 //
-// One CTA per (row, query head); its four warps take every fourth key, a lane
-// holding D / 32 dims, with a running maximum and sum each, joined at the end.
+// All G = n_q / n_kv query heads of a kv head, for all rows of a request, form
+// one query matrix of rows G queries, cut into query tiles of 128 (the MMA's M),
+// so each key and value is read from memory once per call (by further query
+// tiles from L2).  An item is one (request, kv head, query tile), a unit one tile of
+// 128 keys of an item.  The units of all items, in order, are split evenly over
+// one CTA per SM (UnitPlan), from the lengths on the device: whatever the
+// requests' lengths, every SM streams the same number of bytes.  An item cut
+// between CTAs leaves partial results, which tree_combine_kernel joins in CTA order;
+// so results repeat bit for bit.
+//
+// Per CTA (12 warps, TMEM full: two score buffers, two accumulators):
+//   warp 0     loads key and value tiles by TMA (3D map over the layer, 128-byte
+//              swizzle) through a ring of shared-memory stages;
+//   warp 1     issues the products: S = Q K^T (M = 128 queries, N = 128 keys),
+//              O += P V (A = P from TMEM, V read MN-major);
+//   warps 2-3  bring in the queries, and prepare the value tiles that hold
+//              entries of the call's own rows (clean_tile);
+//   warps 4-7 and 8-11  take the item's key tiles in turn, a query per thread:
+//              S from TMEM, mask, running maximum, P = 2^(S - m) back into TMEM
+//              over S as bf16 hi and lo parts (P to 2^-17), both multiplied by V;
+//              each group has its own accumulator, maximum and sum, and O is
+//              rescaled only where the maximum grew by more than 2^8 (P stays
+//              below 2^8, in 32-bit sums).
+// 32-bit queries are bf16 hi and lo parts too (two products with K), 16-bit
+// ones are exact.
 #include "ops.h"
 #include "ptx_sm100.cuh"
 #include "small_dev.cuh"
+#include "tree_plan.cuh"
 
 namespace as2d {
 namespace {
 
+constexpr uint32_t kRegion = 128 * 128;  // 64 columns of 128 rows, bytes
+constexpr int kThreads = 384;
+// P may grow to 2^kLazy before the accumulator is rescaled.
+constexpr float kLazy = 8.f;
+
+struct TreeWork {
+  float* o;    // [2 CTAs][128][D] partial accumulators: slot 0 an item that began in an
+               // earlier CTA, slot 1 one that began in this
+  float2* ml;  // [2 CTAs][128] (maximum base 2, sum)
+};
+
+template <int D, bool F32>
+struct Shape {
+  static constexpr uint32_t STAGE = 128 * D * 2;            // one K or V tile
+  static constexpr uint32_t Q = (F32 ? 2 : 1) * 128 * D * 2;  // hi (and lo) image
+  static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
+  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 2 * 128 * 8 + (3 * NST + 11) * 8 + sizeof(UnitPlan) + 64;
+  static_assert(SMEM <= 232448, "shared memory of one CTA");
+};
+
+// Byte offset of the 16-byte chunk j (of a row's D / 8) of row r in a 128-row
+// operand image of 128-byte-swizzled K-major bf16.
+__device__ __forceinline__ uint32_t chunk_off(int r, int j) {
+  return (uint32_t)(j >> 3) * kRegion + (uint32_t)r * 128u + (uint32_t)(((j & 7) ^ (r & 7)) << 4);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The weight of a part (maximum m) beside a maximum M: 0 where the part holds
+// nothing that the row sees.
+__device__ __forceinline__ float part_weight(float m, float M) {
+  return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+// hi = bf16(x), lo = bf16(x - hi) of two numbers.
+__device__ __forceinline__ void hi_lo(float a, float b, uint32_t& h, uint32_t& l) {
+  h = pack2(a, b);
+  l = pack2(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xFFFF0000u));
+}
+
+// The visible rows of row r of a request, as a mask of its `rows` rows.
+__device__ __forceinline__ uint64_t visible_rows(const TreeArgs& a, int r, int i, int rows) {
+  const uint64_t all = ~0ull >> (64 - rows);
+  return (a.visible ? a.visible[r] : ~0ull >> (63 - i)) & all;
+}
+
+// Which of keys [p0, p0 + 32) a row sees.
+__device__ __forceinline__ uint32_t key_bits(int p0, int L, uint64_t vis) {
+  const int off = L - p0;  // prefix entries in the word
+  if (off >= 32) return ~0u;
+  if (off >= 0) return ((1u << off) - 1) | (uint32_t)(vis << off);
+  return off > -64 ? (uint32_t)(vis >> -off) : 0u;
+}
+
+__device__ __forceinline__ void mask_scores(uint32_t (&v)[32], uint32_t bits) {
+#pragma unroll
+  for (int e = 0; e < 32; ++e)
+    if (!((bits >> e) & 1)) v[e] = 0xFF800000u;  // -inf
+}
+
+// The queries of an item into the operand image(s), by 64 threads; rows past the
+// item's queries are left as they are (what they hold reaches no other row).
+template <int D, bool F32>
+__device__ __forceinline__ void load_queries(const TreeArgs& a, const Unit& it, int tid, uint8_t* img) {
+  constexpr int C = D / 8, B = 8;  // chunks of a row, loads in flight
+  const int G = a.nq / a.nkv, n0 = it.qt * 128;
+  const int n = min(128, it.rows * G - n0) * C;
+  for (int c0 = tid; c0 < n; c0 += 64 * B) {
+    uint4 v[B][F32 ? 2 : 1];
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int c = c0 + 64 * u;
+      if (c < n) {
+        const int q = n0 + c / C, i = q / G, h = it.g * G + (q - i * G);
+        const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + 8 * (c % C);
+        if (F32) {
+          const uint4* s = reinterpret_cast<const uint4*>((const float*)a.q + at);
+          v[u][0] = s[0];
+          v[u][F32 ? 1 : 0] = s[1];
+        } else {
+          v[u][0] = *reinterpret_cast<const uint4*>((const bf16*)a.q + at);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int c = c0 + 64 * u;
+      if (c < n) {
+        uint8_t* to = img + chunk_off(c / C, c % C);
+        if (F32) {
+          const float* x = reinterpret_cast<const float*>(&v[u][0]);
+          uint32_t h[4], l[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) hi_lo(x[2 * e], x[2 * e + 1], h[e], l[e]);
+          *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(to + 128 * D * 2) = make_uint4(l[0], l[1], l[2], l[3]);
+        } else {
+          *reinterpret_cast<uint4*>(to) = v[u][0];
+        }
+      }
+    }
+  }
+}
+
+// A value tile that holds entries from L on, before it is multiplied: entries
+// past the request's last are zeroed (a stale NaN would reach O through 0 V), and
+// in the entries of the call's own rows, which not every row sees, values that
+// are not finite are zeroed too and their rows noted in bad: the epilogue adds
+// them to the rows that do see them.
 template <int D>
-__global__ void __launch_bounds__(128) tree_attn_kernel(const __grid_constant__ TreeArgs a) {
-  constexpr int E = D / 32, W = 4;
-  __shared__ float s_m[W], s_l[W], s_o[W][D];
+__device__ __forceinline__ void clean_tile(uint8_t* v, int p0, int L, int kend, int tid, unsigned long long* bad) {
+  constexpr int C = D / 8;
+  const int z = max(L - p0, 0);
+  for (int c = tid; c < (128 - z) * C; c += 64) {
+    const int r = z + c / C;
+    uint4* at = reinterpret_cast<uint4*>(v + chunk_off(r, c % C));
+    if (p0 + r >= kend) {
+      *at = make_uint4(0, 0, 0, 0);
+      continue;
+    }
+    uint4 x = *at;
+    uint32_t* w = reinterpret_cast<uint32_t*>(&x);
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u, any = true;
+      if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu, any = true;
+    }
+    if (any) {
+      *at = x;
+      atomicOr(bad, 1ull << (p0 + r - L));
+    }
+  }
+}
+
+// N consecutive results x inv at element `at` of the output.
+template <int N>
+__device__ __forceinline__ void write_out(const TreeArgs& a, const float* x, float inv, size_t at) {
+  if (a.q_f32) {
+    float* out = (float*)a.out + at;
+#pragma unroll
+    for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(out + e) = make_float2(x[e] * inv, x[e + 1] * inv);
+  } else {
+    bf16* out = (bf16*)a.out + at;
+#pragma unroll
+    for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(out + e) = pack2(x[e] * inv, x[e + 1] * inv);
+  }
+}
+
+template <int D, bool F32>
+__global__ void __launch_bounds__(kThreads, 1)
+    tree_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const __grid_constant__ TreeArgs a, TreeWork ws, int whole) {
+  using S = Shape<D, F32>;
+  constexpr int NST = S::NST, NR = D / 64;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* qimg = sm;
+  uint8_t* ring = sm + S::Q;
+  float2* s_ml = reinterpret_cast<float2*>(ring + NST * S::STAGE);  // [2][128]
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_ml + 256);
+  uint64_t* empty = full + NST;
+  uint64_t* tail_full = empty + NST;  // in full's place for value tiles that clean_tile prepares
+  uint64_t* q_full = tail_full + NST;
+  uint64_t* q_empty = q_full + 1;
+  uint64_t* s_full = q_empty + 1;   // [2]
+  uint64_t* p_full = s_full + 2;    // [2]
+  uint64_t* v_clean = p_full + 2;   // [2]
+  uint64_t* o_full = v_clean + 2;
+  uint64_t* o_empty = o_full + 1;
+  uint64_t* drain = o_empty + 1;
+  UnitPlan* plan = reinterpret_cast<UnitPlan*>(drain + 1);
+  unsigned long long* s_bad = reinterpret_cast<unsigned long long*>(plan + 1);
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(s_bad + 1);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < NST; ++i) {
+      ptx::mbar_init(&full[i], 1);
+      ptx::mbar_init(&empty[i], 1);
+      ptx::mbar_init(&tail_full[i], 1);
+    }
+    ptx::mbar_init(q_full, 64);
+    ptx::mbar_init(q_empty, 1);
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&s_full[i], 1);
+      ptx::mbar_init(&p_full[i], 4);
+      ptx::mbar_init(&v_clean[i], 64);
+    }
+    ptx::mbar_init(o_full, 1);
+    ptx::mbar_init(o_empty, 8);
+    ptx::mbar_init(drain, 1);
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) ptx::tmem_alloc(tslot, 512);
+  if (warp == 0 && lane == 0) {
+    ptx::prefetch_tmap(&tmK);
+    ptx::prefetch_tmap(&tmV);
+  }
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  const int r = blockIdx.x, h = blockIdx.y, w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int b = row_request(a.rm, r), r0 = a.rm.start[b], i = r - r0, rows = a.rm.start[b + 1] - r0;
-  const int L = a.len[b];
-  if (!rows_fit(L, rows, a.cap)) {
-    if (threadIdx.x == 0 && a.err) atomicOr(a.err, kErrCapacity);
-    return;
-  }
-  const uint64_t vis = a.visible ? a.visible[r] : ~0ull >> (63 - i);
-  float q[E], o[E], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int64_t at = r * a.q_stride + (int64_t)h * D + lane * E + e;
-    q[e] = a.q_f32 ? ((const float*)a.q)[at] : __bfloat162float(((const bf16*)a.q)[at]);
-    o[e] = 0.f;
-  }
-  const size_t base = ((size_t)b * a.nkv + h / (a.nq / a.nkv)) * a.cap * D;
-  for (int t = w; t < L + rows; t += W) {
-    if (t >= L && !((vis >> (t - L)) & 1)) continue;
-    const bf16 *k = a.k + base + (size_t)t * D + lane * E, *v = a.v + base + (size_t)t * D + lane * E;
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s = fmaf(q[e], __bfloat162float(k[e]), s);
-    s = warp_sum(s) * a.scale_log2;
-    const float mn = fmaxf(m, s);
-    const float c = m == -INFINITY ? 0.f : exp2f(m - mn), p = exp2f(s - mn);
-    l = fmaf(l, c, p);
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], c, p * __bfloat162float(v[e]));
-    m = mn;
-  }
-  if (lane == 0) s_m[w] = m, s_l[w] = l;
-#pragma unroll
-  for (int e = 0; e < E; ++e) s_o[w][lane * E + e] = o[e];
+  if (warp == 0) make_plan(a, 128, lane, *plan, blockIdx.x == 0);
+  ptx::tc_fence_before();
   __syncthreads();
-  float M = -INFINITY, l_all = 0.f;
-  for (int j = 0; j < W; ++j) M = fmaxf(M, s_m[j]);
-  float wt[W];
-  for (int j = 0; j < W; ++j) {
-    wt[j] = s_l[j] == 0.f ? 0.f : exp2f(s_m[j] - M);
-    l_all += s_l[j] * wt[j];
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tslot;
+  long long u0, u1;
+  unit_range(*plan, a, blockIdx.x, gridDim.x, whole, u0, u1);
+  // every wait is bounded; a role that gives up flags the call and waits for
+  // nothing more, so that all of them come to the end
+  const unsigned long long limit = a.timeout_ns;
+  bool ok = true;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (ok && !ptx::mbar_wait(bar, parity, limit)) {
+      ok = false;
+      if (a.err) atomicOr(a.err, kErrTimeout);
+    }
+    return ok;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint64_t pol = ptx::policy_evict_first();
+      uint32_t n = 0, tail = 0, turn = 0;  // slots whose last tile is on tail_full, its parity
+      for (long long u = u0; u < u1;) {
+        const Unit it = unit_at(*plan, a, u, u1);
+        const int z = it.b * a.nkv + it.g;
+        for (int t = it.t0; t < it.t1 && ok; ++t)
+          for (int kv = 0; kv < 2; ++kv, ++n) {
+            const uint32_t s = n % NST, bit = 1u << s;
+            if (n >= NST && !wait(&empty[s], (n / NST - 1) & 1)) break;
+            uint64_t* bar = &full[s];
+            tail &= ~bit;
+            if (kv && t >= it.L / 128) {
+              ptx::mbar_arrive(bar);  // (this tile's phase of it)
+              bar = &tail_full[s];
+              tail |= bit;
+              turn ^= bit;
+            }
+            ptx::mbar_arrive_expect_tx(bar, S::STAGE);
+#pragma unroll
+            for (int h = 0; h < NR; ++h)
+              ptx::tma_load_3d(ring + s * S::STAGE + h * kRegion, kv ? &tmV : &tmK, bar, 64 * h, t * 128, z, pol);
+          }
+        u += it.t1 - it.t0;
+      }
+      // no copy is in flight when the CTA ends
+      for (uint32_t i = n > NST ? n - NST : 0; i < n; ++i) {
+        const uint32_t s = i % NST;
+        if ((tail >> s) & 1)
+          ptx::mbar_wait(&tail_full[s], ((turn >> s) & 1) ^ 1, ptx::kDrainNs);
+        else
+          ptx::mbar_wait(&full[s], (i / NST) & 1, ptx::kDrainNs);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t IDESC1 = ptx::idesc_bf16_f32(128, 128);
+      constexpr uint32_t IDESC2 = ptx::idesc_bf16_f32(128, D, true);
+      uint32_t n = 0, items = 0, np[2] = {0, 0}, nc[2] = {0, 0};
+      uint32_t slot_v[2] = {0, 0};
+      bool used[2] = {false, false};
+      int tile_v[2] = {0, 0};
+      for (long long u = u0; u < u1 && ok; ++items) {
+        const Unit it = unit_at(*plan, a, u, u1);
+        const int cnt = it.t1 - it.t0;
+        wait(q_full, items & 1);
+        for (int j = 0; j <= cnt && ok; ++j) {
+          if (j < cnt) {
+            const uint32_t s = n % NST;
+            if (!wait(&full[s], (n / NST) & 1)) break;
+            // the last P that stood where these scores go has been read: its
+            // product released the stage of its values
+            if (used[j & 1] && !wait(&empty[slot_v[j & 1] % NST], (slot_v[j & 1] / NST) & 1)) break;
+            ptx::tc_fence_after();
+            const uint32_t kt = ptx::smem_u32(ring + s * S::STAGE), qt = ptx::smem_u32(qimg);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint64_t ad = ptx::sdesc_sw128(qt + (kk >> 2) * kRegion) + 2 * (kk & 3);
+              const uint64_t bd = ptx::sdesc_sw128(kt + (kk >> 2) * kRegion) + 2 * (kk & 3);
+              ptx::mma_bf16(tmem + 128 * (j & 1), ad, bd, IDESC1, kk > 0 ? 1u : 0u);
+            }
+            if (F32) {
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk) {
+                const uint64_t ad = ptx::sdesc_sw128(qt + 128 * D * 2 + (kk >> 2) * kRegion) + 2 * (kk & 3);
+                const uint64_t bd = ptx::sdesc_sw128(kt + (kk >> 2) * kRegion) + 2 * (kk & 3);
+                ptx::mma_bf16(tmem + 128 * (j & 1), ad, bd, IDESC1, 1u);
+              }
+            }
+            ptx::mma_commit(&empty[s]);
+            ptx::mma_commit(&s_full[j & 1]);
+            if (j == cnt - 1) ptx::mma_commit(q_empty);
+            slot_v[j & 1] = n + 1;
+            used[j & 1] = true;
+            tile_v[j & 1] = it.t0 + j;
+            n += 2;
+          }
+          if (j > 0) {
+            const int i = (j - 1) & 1, t = tile_v[i];
+            const uint32_t s = slot_v[i] % NST;
+            if (!wait(&p_full[i], np[i]++ & 1)) break;
+            if (j <= 2 && items > 0 && !wait(o_empty, (items - 1) & 1)) break;
+            const int tail = t - it.L / 128;  // the tiles that hold entries from L on
+            if (tail >= 0 ? !wait(&v_clean[tail], nc[tail]++ & 1) : !wait(&full[s], (slot_v[i] / NST) & 1)) break;
+            ptx::tc_fence_after();
+            const uint32_t vt = ptx::smem_u32(ring + s * S::STAGE);
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk) {
+                const uint64_t bd = ptx::sdesc_sw128_mn(vt + kk * 2048u, kRegion, 1024u);
+                ptx::mma_bf16_ta(tmem + 256 + 128 * i, tmem + 128 * i + 16 * part + 32u * (kk >> 1) + 8u * (kk & 1), bd, IDESC2,
+                                 j > 2 || part > 0 || kk > 0 ? 1u : 0u);
+              }
+            ptx::mma_commit(&empty[s]);
+            if (j == cnt) ptx::mma_commit(o_full);
+          }
+        }
+        u += cnt;
+      }
+      // no product is running when TMEM is freed
+      ptx::mma_commit(drain);
+      ptx::mbar_wait(drain, 0, ptx::kDrainNs);
+    }
+  } else if (warp < 4) {
+    const int t64 = tid - 64;
+    uint32_t n = 0, items = 0, turn = 0;
+    for (long long u = u0; u < u1; ++items) {
+      const Unit it = unit_at(*plan, a, u, u1);
+      if (items > 0) wait(q_empty, (items - 1) & 1);
+      if (ok) load_queries<D, F32>(a, it, t64, qimg);
+      ptx::fence_proxy_async_smem();
+      ptx::mbar_arrive(q_full);
+      const int first = it.L / 128;
+      // the epilogue of the item before has read what was noted for it
+      if (items > 0) wait(o_empty, (items - 1) & 1);
+      if (it.t1 > first) {
+        if (t64 == 0) *s_bad = 0;
+        ptx::named_bar_sync(2, 64);
+        for (int t = max(first, it.t0); t < it.t1; ++t) {
+          const uint32_t s = (n + 2 * (t - it.t0) + 1) % NST;
+          const bool here = wait(&tail_full[s], (turn >> s) & 1);
+          turn ^= 1u << s;
+          if (here)
+            clean_tile<D>(ring + s * S::STAGE, t * 128, it.L, it.L + it.rows, t64, s_bad);
+          ptx::fence_proxy_async_smem();
+          ptx::mbar_arrive(&v_clean[t - first]);
+        }
+      }
+      n += 2 * (it.t1 - it.t0);
+      u += it.t1 - it.t0;
+    }
+  } else {
+    const int wg = (warp - 4) >> 2;              // takes the item's tiles of this parity
+    const int row = 32 * (warp & 3) + lane;      // query of the tile, TMEM lane
+    const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+    const uint32_t ts = tl + 128 * wg, to = tl + 256 + 128 * wg;
+    const int G = a.nq / a.nkv;
+    const float c = a.scale_log2;
+    uint32_t ns = 0, items = 0, nc[2] = {0, 0};
+    for (long long u = u0; u < u1; ++items) {
+      const Unit it = unit_at(*plan, a, u, u1);
+      const int cnt = it.t1 - it.t0, nqs = it.rows * G;
+      const int q = it.qt * 128 + row, i = q / G;
+      const bool live = q < nqs;
+      const bool warp_live = it.qt * 128 + 32 * (warp & 3) < nqs;  // a query of the warp is
+      const int h = it.g * G + (q - i * G);
+      const uint64_t vis = live ? visible_rows(a, it.r0 + i, i, it.rows) : 0ull;
+      float m = -INFINITY, l = 0.f;
+      for (int j = wg; j < cnt; j += 2, ++ns) {
+        wait(&s_full[wg], ns & 1);
+        ok = __all_sync(~0u, ok);
+        if (ok && warp_live) {
+          ptx::tc_fence_after();
+          const int p0 = (it.t0 + j) * 128;
+          const bool tail = p0 + 128 > it.L;
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          uint32_t sv[2][32];
+          // 32 scores at a time, the next 32 on their way, -inf where the row does not see
+          ptx::tmem_ld32(ts, sv[0]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            ptx::tmem_ld_wait();
+            ptx::tmem_ld32(ts + 32 * ((x + 1) & 3), sv[(x + 1) & 1]);
+            if (tail) mask_scores(sv[x & 1], key_bits(p0 + 32 * x, it.L, vis));
+#pragma unroll
+            for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(sv[x & 1][e]));
+          }
+          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+          // (NaN scores pass the maximum by, and reach the sums)
+          const bool grow = mt > m + kLazy || (m == -INFINITY && mt > m);
+          if (__any_sync(~0u, grow)) {
+            const float m_new = grow ? mt : m;
+            const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
+            l = grow ? l * f : l;
+            if (j >= 2) {
+#pragma unroll 1
+              for (int x = 0; x < D; x += 32) {
+                uint32_t o[32];
+                ptx::tmem_ld32(to + x, o);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = grow ? __float_as_uint(__uint_as_float(o[e]) * f) : o[e];
+                ptx::tmem_st16(to + x, o);
+                ptx::tmem_st16(to + x + 16, o + 16);
+              }
+            }
+            m = m_new;
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          float ls[4] = {0.f, 0.f, 0.f, 0.f};
+          // again, now for P (its parts take the place of the scores they come from)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            uint32_t hi[16], lo[16];
+            uint32_t(&v)[32] = sv[x & 1];
+            ptx::tmem_ld_wait();
+            if (x < 3) ptx::tmem_ld32(ts + 32 * (x + 1), sv[(x + 1) & 1]);
+            if (tail) mask_scores(v, key_bits(p0 + 32 * x, it.L, vis));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float p0_ = ex2(fmaf(__uint_as_float(v[2 * e]), c, -ref));
+              const float p1_ = ex2(fmaf(__uint_as_float(v[2 * e + 1]), c, -ref));
+              ls[2 * (e & 1)] += p0_;
+              ls[2 * (e & 1) + 1] += p1_;
+              hi_lo(p0_, p1_, hi[e], lo[e]);
+            }
+            ptx::tmem_st16(ts + 32 * x, hi);
+            ptx::tmem_st16(ts + 32 * x + 16, lo);
+          }
+          l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+          ptx::tmem_st_wait();
+          ptx::tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&p_full[wg]);
+      }
+      // ---- the item's end: both groups' parts, each group half of the dims ----
+      const bool tails = it.t1 > it.L / 128;
+      wait(o_full, items & 1);
+      if (tails)
+        for (int t = max(it.L / 128, it.t0); t < it.t1; ++t) {
+          const int x = t - it.L / 128;
+          wait(&v_clean[x], nc[x]++ & 1);
+        }
+      ok = __all_sync(~0u, ok);
+      ptx::tc_fence_after();
+      s_ml[wg * 128 + row] = make_float2(m, l);
+      ptx::named_bar_sync(1, 256);
+      const float2 ml0 = s_ml[row], ml1 = s_ml[128 + row];
+      const float M = fmaxf(ml0.x, ml1.x);
+      const float w0 = part_weight(ml0.x, M), w1 = cnt > 1 ? part_weight(ml1.x, M) : 0.f;
+      const float lt = ml0.y * w0 + (cnt > 1 ? ml1.y * w1 : 0.f);
+      const unsigned long long bad = tails ? *s_bad & vis : 0ull;
+      if (ok && warp_live) {
+        const bool done = it.t0 == 0 && it.t1 == it.tiles;
+        const float inv = lt == 0.f ? 0.f : 1.f / lt;
+        const size_t part = ((size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1)) * 128 + row;
+#pragma unroll 1
+        for (int x = 0; x < D / 2; x += 32) {
+          const int d0 = wg * (D / 2) + x;
+          uint32_t o0[32], o1[32];
+          ptx::tmem_ld32(tl + 256 + d0, o0);
+          if (cnt > 1) ptx::tmem_ld32(tl + 384 + d0, o1);
+          ptx::tmem_ld_wait();
+          float o[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            o[e] = w0 != 0.f ? __uint_as_float(o0[e]) * w0 : 0.f;
+            if (cnt > 1 && w1 != 0.f) o[e] = fmaf(__uint_as_float(o1[e]), w1, o[e]);
+          }
+          for (unsigned long long left = bad; left; left &= left - 1) {
+            const int r = __ffsll((long long)left) - 1;
+            const bf16* v = a.v + (((size_t)it.b * a.nkv + it.g) * a.cap + it.L + r) * D + d0;
+            if (it.L + r >= it.t0 * 128 && it.L + r < it.t1 * 128)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const float y = __bfloat162float(v[e]);
+                if (!(fabsf(y) <= 3.4e38f)) o[e] += y;
+              }
+          }
+          if (live && !done) {
+            float4* dst = reinterpret_cast<float4*>(ws.o + part * D + d0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          } else if (live) {
+            write_out<32>(a, o, inv, ((size_t)(it.r0 + i) * a.nq + h) * D + d0);
+          }
+          __syncwarp();
+        }
+        if (live && wg == 0) {
+          if (!done)
+            ws.ml[part] = make_float2(M, lt);
+          else if (a.lse)
+            a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, lt);
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(o_empty);
+      u += cnt;
+    }
   }
-  if ((int)threadIdx.x < D) {
-    float x = 0.f;
-    for (int j = 0; j < W; ++j)
-      if (wt[j] != 0.f) x += s_o[j][threadIdx.x] * wt[j];
-    x = l_all == 0.f ? 0.f : x / l_all;
-    const size_t at = ((size_t)r * a.nq + h) * D + threadIdx.x;
-    if (a.q_f32)
-      ((float*)a.out)[at] = x;
-    else
-      ((bf16*)a.out)[at] = __float2bfloat16_rn(x);
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 1) ptx::tmem_dealloc(tmem, 512);
+}
+
+// The parts of items cut between CTAs, joined in CTA order: a warp per query, a
+// lane D / 32 dims; every part's maximum first, then eight parts' rows in flight.
+template <int D>
+__global__ void __launch_bounds__(256) tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas) {
+  constexpr int E = D / 32, U = 8;
+  __shared__ UnitPlan plan;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  if (warp == 0) make_plan(a, 128, lane, plan, false);
+  __syncthreads();
+  long long us;
+  if (!item_at(plan, a, blockIdx.x, us)) return;
+  const Unit it = unit_at(plan, a, us, us + (1ll << 40));
+  const int G = a.nq / a.nkv, row = 8 * blockIdx.y + warp, q = it.qt * 128 + row;
+  if (q >= it.rows * G) return;
+  const int c0 = unit_owner(plan, us, ctas), c1 = unit_owner(plan, us + it.tiles - 1, ctas);
+  if (c0 == c1) return;  // written by its CTA
+  const int n = c1 - c0 + 1;
+  auto part = [&](int k) { return ((size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0)) * 128 + row; };
+  float M = -INFINITY;
+  for (int k = lane; k < n; k += 32) M = fmaxf(M, __ldcg(&ws.ml[part(k)]).x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(~0u, M, o));
+  float l = 0.f, x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  for (int k0 = 0; k0 < n; k0 += U) {
+    float2 ml[U];
+    float v[U][E];
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (k0 + k < n) {
+        ml[k] = __ldcg(&ws.ml[part(k0 + k)]);
+        const float* s = ws.o + part(k0 + k) * D + E * lane;
+        if constexpr (E == 4) {
+          const float4 t = __ldcg(reinterpret_cast<const float4*>(s));
+          v[k][0] = t.x, v[k][1] = t.y, v[k][2] = t.z, v[k][3] = t.w;
+        } else {
+          const float2 t = __ldcg(reinterpret_cast<const float2*>(s));
+          v[k][0] = t.x, v[k][1] = t.y;
+        }
+      }
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (k0 + k < n) {
+        const float w = part_weight(ml[k].x, M);
+        if (w != 0.f) {
+          l = fmaf(ml[k].y, w, l);
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = fmaf(v[k][e], w, x[e]);
+        }
+      }
   }
-  if (threadIdx.x == 0 && a.lse)
-    a.lse[(size_t)r * a.nq + h] = l_all == 0.f ? -INFINITY : (M + log2f(l_all)) * 0.69314718055994531f;
+  const int i = q / G, h = it.g * G + (q - i * G);
+  write_out<E>(a, x, l == 0.f ? 0.f : 1.f / l, ((size_t)(it.r0 + i) * a.nq + h) * D + E * lane);
+  if (lane == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, l);
+}
+
+// Items of at most this many key tiles are each done by one CTA, without the
+// second kernel.
+constexpr int kWholeTiles = 2;
+
+template <int D, bool F32>
+cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs& a, const TreeWork& ws,
+                   int64_t items, int64_t most_tiles, int sms, cudaStream_t st) {
+  using S = Shape<D, F32>;
+  static const cudaError_t attr = cudaFuncSetAttribute(
+      tree_attn_kernel<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
+  if (attr != cudaSuccess) return attr;
+  const bool whole = most_tiles <= kWholeTiles;
+  const int64_t units = items * most_tiles;
+  const int ctas = (int)(whole ? items : units < sms ? units : sms);
+  const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
+                                   (int)whole);
+  if (e != cudaSuccess || whole) return e;
+  return launch_pdl(tree_combine_kernel<D>, dim3((unsigned)items, 16), dim3(256), 0, st, 1, a, ws, ctas);
+}
+
+int device_sms() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1)
+    return 1;
+  return n;
 }
 
 }  // namespace
 
-size_t tree_attention_workspace(int) { return 256; }
+size_t tree_attention_workspace(int head_dim) {
+  return (size_t)device_sms() * 2 * 128 * (head_dim * 4 + 8);
+}
 
-cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t, void*, cudaStream_t st) {
-  const dim3 grid(a.rm.rows, a.nq);
-  return head_dim == 128 ? launch_pdl(tree_attn_kernel<128>, grid, dim3(128), 0, st, 1, a)
-                         : launch_pdl(tree_attn_kernel<64>, grid, dim3(128), 0, st, 1, a);
+cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
+                                  cudaStream_t st) {
+  const int sms = device_sms(), G = a.nq / a.nkv;
+  int64_t items = 0;
+  for (int b = 0; b < a.rm.batch; ++b)
+    items += (int64_t)((a.rm.start[b + 1] - a.rm.start[b]) * G + 127) / 128 * a.nkv;
+  TreeWork ws;
+  ws.o = (float*)workspace;
+  ws.ml = (float2*)(ws.o + (size_t)sms * 2 * 128 * head_dim);
+  CUtensorMap tk, tv;
+  if (!encode_cache_map(&tk, a.k, head_dim, a.cap, (int64_t)a.rm.batch * a.nkv) ||
+      !encode_cache_map(&tv, a.v, head_dim, a.cap, (int64_t)a.rm.batch * a.nkv))
+    return cudaErrorInvalidValue;
+  const int64_t tiles = (max_keys + 127) / 128;
+  if (head_dim == 128)
+    return a.q_f32 ? launch<128, true>(tk, tv, a, ws, items, tiles, sms, st)
+                   : launch<128, false>(tk, tv, a, ws, items, tiles, sms, st);
+  return a.q_f32 ? launch<64, true>(tk, tv, a, ws, items, tiles, sms, st)
+                 : launch<64, false>(tk, tv, a, ws, items, tiles, sms, st);
 }
 
 }  // namespace as2d

@@ -24,6 +24,7 @@ struct TreeArgs {
   void* out;                // [rows][nq][d] of the queries' type
   float* lse;               // [rows][nq], nullable
   int32_t* err;             // error bits, nullable
+  unsigned long long timeout_ns = 2000000000ull;  // limit of the kernel's waits
 };
 
 struct WeightArgs {

@@ -1,0 +1,129 @@
+// tree_plan.cuh -- how the rows of a call over a cache are cut into items and
+// units and spread over CTAs, from the lengths on the device (k_tree_attn.cu,
+// k_attn_weights.cu).
+//
+// An item is one (request, kv head, query tile), a unit one tile of 128 keys of
+// an item.  Items and their units are numbered request by request, kv head by kv
+// head, query tile by query tile (the query tiles of a head read its keys one
+// after another, from L2).
+#pragma once
+
+#include "ops.h"
+
+namespace as2d {
+
+struct UnitPlan {
+  long long unit[kMaxBatch + 1];  // units before each request
+  int len[kMaxBatch];
+  int tiles[kMaxBatch];           // key tiles of a request's items
+  int qts[kMaxBatch];             // query tiles of a request
+};
+
+// What a CTA does of one item: key tiles [t0, t1) of it.
+struct Unit {
+  int b, g, qt, tiles, t0, t1;
+  int L, rows, r0;
+};
+
+// Filled by one warp; requests without rows, or whose length leaves no room for
+// theirs, have no units.
+__device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int lane, UnitPlan& p, bool flag) {
+  const int G = a.nq / a.nkv;
+  long long before = 0;
+  bool over = false;
+#pragma unroll
+  for (int h = 0; h < kMaxBatch / 32; ++h) {
+    const int b = 32 * h + lane;
+    int L = 0, tiles = 0, qts = 0;
+    if (b < a.rm.batch) {
+      const int rows = a.rm.start[b + 1] - a.rm.start[b];
+      L = a.len[b];
+      qts = (rows * G + q_tile - 1) / q_tile;
+      if (rows > 0 && rows_fit(L, rows, a.cap))
+        tiles = (L + rows + 127) / 128;
+      else
+        over = over || rows > 0;
+    }
+    long long n = (long long)a.nkv * qts * tiles, at = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long t = __shfl_up_sync(~0u, at, o);
+      if (lane >= o) at += t;
+    }
+    p.unit[b] = before + at - n;
+    p.len[b] = L;
+    p.tiles[b] = tiles;
+    p.qts[b] = qts;
+    before += __shfl_sync(~0u, at, 31);
+  }
+  if (lane == 0) p.unit[kMaxBatch] = before;
+  if (flag && __any_sync(~0u, over) && lane == 0 && a.err) atomicOr(a.err, kErrCapacity);
+}
+
+// First unit of item n; false past the last one.
+__device__ __forceinline__ bool item_at(const UnitPlan& p, const TreeArgs& a, long long n, long long& u) {
+  for (int b = 0; b < a.rm.batch; ++b) {
+    const long long items = p.tiles[b] > 0 ? (long long)a.nkv * p.qts[b] : 0;
+    if (n < items) {
+      u = p.unit[b] + n * p.tiles[b];
+      return true;
+    }
+    n -= items;
+  }
+  return false;
+}
+
+// Units of CTA c: even shares of all of them, or (whole) those of item c.
+__device__ __forceinline__ void unit_range(const UnitPlan& p, const TreeArgs& a, int c, int ctas, int whole,
+                                           long long& u0, long long& u1) {
+  if (whole) {
+    u0 = u1 = 0;
+    if (item_at(p, a, c, u0)) {
+      int b = 0;
+      while (p.unit[b + 1] <= u0) ++b;
+      u1 = u0 + p.tiles[b];
+    }
+    return;
+  }
+  const long long n = p.unit[kMaxBatch], of = min((long long)ctas, n);  // no CTA among them without units
+  u0 = c < of ? c * n / of : 0;
+  u1 = c < of ? (c + 1) * n / of : 0;
+}
+// The CTA that does unit u.
+__device__ __forceinline__ int unit_owner(const UnitPlan& p, long long u, int ctas) {
+  const long long n = p.unit[kMaxBatch];
+  return (int)(((u + 1) * min((long long)ctas, n) - 1) / n);
+}
+
+// What is done of unit u's item from u on, up to unit u1 at most.
+__device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, long long u, long long u1) {
+  Unit it;
+  int lo = 0, hi = kMaxBatch - 1;  // the last request whose first unit is at or before u
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (p.unit[mid] <= u)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  it.b = lo;
+  it.tiles = p.tiles[lo];
+  it.L = p.len[lo];
+  it.r0 = a.rm.start[lo];
+  it.rows = a.rm.start[lo + 1] - it.r0;
+  const long long rel = u - p.unit[lo];
+  const long long item = rel / it.tiles;
+  it.t0 = (int)(rel - item * it.tiles);
+  it.g = (int)(item / p.qts[lo]);
+  it.qt = (int)(item - (long long)it.g * p.qts[lo]);
+  const long long left = u1 - u;
+  it.t1 = left < it.tiles - it.t0 ? it.t0 + (int)left : it.tiles;
+  return it;
+}
+
+// ln of a sum l of powers of two relative to 2^M; -inf of nothing.
+__device__ __forceinline__ float row_lse(float M, float l) {
+  return l == 0.f ? -INFINITY : (M + log2f(l)) * 0.69314718055994531f;
+}
+
+}  // namespace as2d
