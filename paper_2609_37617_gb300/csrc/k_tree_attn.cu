@@ -15,19 +15,20 @@
 // between CTAs leaves partial results, which tree_combine_kernel joins in CTA order;
 // so results repeat bit for bit.
 //
-// Per CTA (12 warps, TMEM full: two score buffers, two accumulators):
+// Per CTA (20 warps, TMEM full: two score buffers, two accumulators):
 //   warp 0     loads key and value tiles by TMA (3D map over the layer, 128-byte
 //              swizzle) through a ring of shared-memory stages;
 //   warp 1     issues the products: S = Q K^T (M = 128 queries, N = 128 keys),
 //              O += P V (A = P from TMEM, V read MN-major);
 //   warps 2-3  bring in the queries, and prepare the value tiles that hold
 //              entries of the call's own rows (clean_tile);
-//   warps 4-7 and 8-11  take the item's key tiles in turn, a query per thread:
-//              S from TMEM, mask, running maximum, P = 2^(S - m) back into TMEM
-//              over S as bf16 hi and lo parts (P to 2^-17), both multiplied by V;
-//              each group has its own accumulator, maximum and sum, and O is
-//              rescaled only where the maximum grew by more than 2^8 (P stays
-//              below 2^8, in 32-bit sums).
+//   warps 4-19 two sets of eight that take the item's key tiles in turn, half of
+//              a query's keys per thread: S from TMEM, mask, running maximum (of
+//              both halves, exchanged through shared memory), P = 2^(S - m) back
+//              into TMEM over S as bf16 hi and lo parts (P to 2^-17), both
+//              multiplied by V.  Each set has its own accumulator, maximum and sum,
+//              and O is rescaled only where the maximum grew by more than 2^8 (P
+//              stays below 2^8, in 32-bit sums).
 // 32-bit queries are bf16 hi and lo parts too (two products with K), 16-bit
 // ones are exact.
 #include "ops.h"
@@ -39,13 +40,14 @@ namespace as2d {
 namespace {
 
 constexpr uint32_t kRegion = 128 * 128;  // 64 columns of 128 rows, bytes
-constexpr int kThreads = 384;
+constexpr int kThreads = 640;
 // P may grow to 2^kLazy before the accumulator is rescaled.
 constexpr float kLazy = 8.f;
 
 struct TreeWork {
-  float* o;    // [2 CTAs][128][D] partial accumulators: slot 0 an item that began in an
-               // earlier CTA, slot 1 one that began in this
+  float4* o;   // [2 CTAs][D / 4][128] partial accumulators, four dims of a query
+               // together: slot 0 an item that began in an earlier CTA, slot 1 one
+               // that began in this
   float2* ml;  // [2 CTAs][128] (maximum base 2, sum)
 };
 
@@ -54,8 +56,8 @@ struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;            // one K or V tile
   static constexpr uint32_t Q = (F32 ? 2 : 1) * 128 * D * 2;  // hi (and lo) image
   static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
-  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 2 * 128 * 8 + (3 * NST + 11) * 8 + sizeof(UnitPlan) + 64;
-  static_assert(SMEM <= 232448, "shared memory of one CTA");
+  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 11) * 8 + 8 + 16;
+  static_assert(SMEM + sizeof(UnitPlan) <= 232448, "shared memory of one CTA");
 };
 
 // Byte offset of the 16-byte chunk j (of a row's D / 8) of row r in a 128-row
@@ -100,11 +102,25 @@ __device__ __forceinline__ uint32_t key_bits(int p0, int L, uint64_t vis) {
   return off > -64 ? (uint32_t)(vis >> -off) : 0u;
 }
 
-__device__ __forceinline__ void mask_scores(uint32_t (&v)[32], uint32_t bits) {
+template <int N>
+__device__ __forceinline__ void mask_scores(uint32_t (&v)[N], uint32_t bits) {
 #pragma unroll
-  for (int e = 0; e < 32; ++e)
+  for (int e = 0; e < N; ++e)
     if (!((bits >> e) & 1)) v[e] = 0xFF800000u;  // -inf
 }
+
+// The ring's next stage and its parity, as slot | parity << 8.
+struct Stage {
+  uint32_t x = 0;
+  template <int NST>
+  __device__ __forceinline__ uint32_t next() {
+    const uint32_t now = x;
+    x = (now & 255u) + 1 == NST ? (now & 256u) ^ 256u : now + 1;
+    return now;
+  }
+  static __device__ __forceinline__ uint32_t slot(uint32_t x) { return x & 255u; }
+  static __device__ __forceinline__ uint32_t parity(uint32_t x) { return x >> 8; }
+};
 
 // The queries of an item into the operand image(s), by 64 threads; rows past the
 // item's queries are left as they are (what they hold reaches no other row).
@@ -206,8 +222,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* qimg = sm;
   uint8_t* ring = sm + S::Q;
-  float2* s_ml = reinterpret_cast<float2*>(ring + NST * S::STAGE);  // [2][128]
-  uint64_t* full = reinterpret_cast<uint64_t*>(s_ml + 256);
+  float2* s_ml = reinterpret_cast<float2*>(ring + NST * S::STAGE);  // [4 groups][128] (maximum, sum)
+  float* s_mx = reinterpret_cast<float*>(s_ml + 4 * 128);           // [4 groups][128] a tile's maxima
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_mx + 4 * 128);
   uint64_t* empty = full + NST;
   uint64_t* tail_full = empty + NST;  // in full's place for value tiles that clean_tile prepares
   uint64_t* q_full = tail_full + NST;
@@ -218,9 +235,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* o_full = v_clean + 2;
   uint64_t* o_empty = o_full + 1;
   uint64_t* drain = o_empty + 1;
-  UnitPlan* plan = reinterpret_cast<UnitPlan*>(drain + 1);
-  unsigned long long* s_bad = reinterpret_cast<unsigned long long*>(plan + 1);
+  unsigned long long* s_bad = reinterpret_cast<unsigned long long*>(drain + 1);
   uint32_t* tslot = reinterpret_cast<uint32_t*>(s_bad + 1);
+  __shared__ UnitPlan s_plan;
+  const UnitPlan* plan = &s_plan;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -233,11 +251,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&s_full[i], 1);
-      ptx::mbar_init(&p_full[i], 4);
+      ptx::mbar_init(&p_full[i], 8);
       ptx::mbar_init(&v_clean[i], 64);
     }
     ptx::mbar_init(o_full, 1);
-    ptx::mbar_init(o_empty, 8);
+    ptx::mbar_init(o_empty, 16);
     ptx::mbar_init(drain, 1);
     ptx::fence_mbar_init();
   }
@@ -248,19 +266,19 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  if (warp == 0) make_plan(a, 128, lane, *plan, blockIdx.x == 0);
+  if (warp == 0) make_plan(a, 128, lane, s_plan, blockIdx.x == 0);
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tslot;
-  long long u0, u1;
+  int u0, u1;
   unit_range(*plan, a, blockIdx.x, gridDim.x, whole, u0, u1);
   // every wait is bounded; a role that gives up flags the call and waits for
   // nothing more, so that all of them come to the end
   const unsigned long long limit = a.timeout_ns;
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok && !ptx::mbar_wait(bar, parity, limit)) {
+    if (ok && !ptx::mbar_spin(bar, parity, limit)) {
       ok = false;
       if (a.err) atomicOr(a.err, kErrTimeout);
     }
@@ -271,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       const uint64_t pol = ptx::policy_evict_first();
       uint32_t n = 0, tail = 0, turn = 0;  // slots whose last tile is on tail_full, its parity
-      for (long long u = u0; u < u1;) {
+      for (int u = u0; u < u1;) {
         const Unit it = unit_at(*plan, a, u, u1);
         const int z = it.b * a.nkv + it.g;
         for (int t = it.t0; t < it.t1 && ok; ++t)
@@ -306,63 +324,65 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       constexpr uint32_t IDESC1 = ptx::idesc_bf16_f32(128, 128);
       constexpr uint32_t IDESC2 = ptx::idesc_bf16_f32(128, D, true);
-      uint32_t n = 0, items = 0, np[2] = {0, 0}, nc[2] = {0, 0};
-      uint32_t slot_v[2] = {0, 0};
-      bool used[2] = {false, false};
-      int tile_v[2] = {0, 0};
-      for (long long u = u0; u < u1 && ok; ++items) {
+      const uint32_t q_lo = ptx::desc_lo(ptx::smem_u32(qimg), 16u);
+      constexpr uint32_t kNone = ~0u;
+      Stage at;
+      uint32_t items = 0, p_turn = 0, c_turn = 0;    // parities of p_full and v_clean
+      uint32_t last0 = kNone, last1 = kNone, v = 0;  // value stages of the sets' last tiles, of the last tile
+      for (int u = u0; u < u1 && ok; ++items) {
         const Unit it = unit_at(*plan, a, u, u1);
-        const int cnt = it.t1 - it.t0;
+        const int cnt = it.t1 - it.t0, first_tail = it.L / 128 - it.t0;
         wait(q_full, items & 1);
         for (int j = 0; j <= cnt && ok; ++j) {
+          const uint32_t v_before = v;
           if (j < cnt) {
-            const uint32_t s = n % NST;
-            if (!wait(&full[s], (n / NST) & 1)) break;
+            const uint32_t k = at.next<NST>(), last = j & 1 ? last1 : last0;
+            v = at.next<NST>();
+            if (!wait(&full[Stage::slot(k)], Stage::parity(k))) break;
             // the last P that stood where these scores go has been read: its
             // product released the stage of its values
-            if (used[j & 1] && !wait(&empty[slot_v[j & 1] % NST], (slot_v[j & 1] / NST) & 1)) break;
+            if (last != kNone && !wait(&empty[Stage::slot(last)], Stage::parity(last))) break;
             ptx::tc_fence_after();
-            const uint32_t kt = ptx::smem_u32(ring + s * S::STAGE), qt = ptx::smem_u32(qimg);
+            const uint32_t kt = ptx::desc_lo(ptx::smem_u32(ring + Stage::slot(k) * S::STAGE), 16u);
+            const uint32_t ds = tmem + 128 * (j & 1);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-              const uint64_t ad = ptx::sdesc_sw128(qt + (kk >> 2) * kRegion) + 2 * (kk & 3);
-              const uint64_t bd = ptx::sdesc_sw128(kt + (kk >> 2) * kRegion) + 2 * (kk & 3);
-              ptx::mma_bf16(tmem + 128 * (j & 1), ad, bd, IDESC1, kk > 0 ? 1u : 0u);
+              const uint32_t to = ((kk >> 2) * kRegion + 32u * (kk & 3)) >> 4;
+              if (kk == 0)
+                ptx::mma_bf16_lo<false>(ds, q_lo, kt, IDESC1);
+              else
+                ptx::mma_bf16_lo<true>(ds, q_lo + to, kt + to, IDESC1);
+              if (F32) ptx::mma_bf16_lo<true>(ds, q_lo + to + (128u * D * 2 >> 4), kt + to, IDESC1);
             }
-            if (F32) {
-#pragma unroll
-              for (int kk = 0; kk < D / 16; ++kk) {
-                const uint64_t ad = ptx::sdesc_sw128(qt + 128 * D * 2 + (kk >> 2) * kRegion) + 2 * (kk & 3);
-                const uint64_t bd = ptx::sdesc_sw128(kt + (kk >> 2) * kRegion) + 2 * (kk & 3);
-                ptx::mma_bf16(tmem + 128 * (j & 1), ad, bd, IDESC1, 1u);
-              }
-            }
-            ptx::mma_commit(&empty[s]);
             ptx::mma_commit(&s_full[j & 1]);
+            ptx::mma_commit(&empty[Stage::slot(k)]);
             if (j == cnt - 1) ptx::mma_commit(q_empty);
-            slot_v[j & 1] = n + 1;
-            used[j & 1] = true;
-            tile_v[j & 1] = it.t0 + j;
-            n += 2;
+            if (j & 1)
+              last1 = v;
+            else
+              last0 = v;
           }
           if (j > 0) {
-            const int i = (j - 1) & 1, t = tile_v[i];
-            const uint32_t s = slot_v[i] % NST;
-            if (!wait(&p_full[i], np[i]++ & 1)) break;
+            const uint32_t i = (j - 1) & 1;
+            if (!wait(&p_full[i], (p_turn >> i) & 1)) break;
+            p_turn ^= 1u << i;
             if (j <= 2 && items > 0 && !wait(o_empty, (items - 1) & 1)) break;
-            const int tail = t - it.L / 128;  // the tiles that hold entries from L on
-            if (tail >= 0 ? !wait(&v_clean[tail], nc[tail]++ & 1) : !wait(&full[s], (slot_v[i] / NST) & 1)) break;
+            const int tail = j - 1 - first_tail;  // the tiles that hold entries from L on
+            if (tail < 0) {
+              if (!wait(&full[Stage::slot(v_before)], Stage::parity(v_before))) break;
+            } else {
+              if (!wait(&v_clean[tail], (c_turn >> tail) & 1)) break;
+              c_turn ^= 1u << tail;
+            }
             ptx::tc_fence_after();
-            const uint32_t vt = ptx::smem_u32(ring + s * S::STAGE);
+            const uint32_t vt = ptx::desc_lo(ptx::smem_u32(ring + Stage::slot(v_before) * S::STAGE), kRegion);
+            const uint32_t ds = tmem + 256 + 128 * i, ps = tmem + 128 * i;
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
-#pragma unroll
-              for (int kk = 0; kk < 8; ++kk) {
-                const uint64_t bd = ptx::sdesc_sw128_mn(vt + kk * 2048u, kRegion, 1024u);
-                ptx::mma_bf16_ta(tmem + 256 + 128 * i, tmem + 128 * i + 16 * part + 32u * (kk >> 1) + 8u * (kk & 1), bd, IDESC2,
-                                 j > 2 || part > 0 || kk > 0 ? 1u : 0u);
-              }
-            ptx::mma_commit(&empty[s]);
+            for (int kk = 0; kk < 8; ++kk) {
+              ptx::mma_bf16_ta_lo(ds, ps + 16u * kk, vt + 128u * kk, IDESC2, j > 2 || kk > 0 ? 1u : 0u);
+              ptx::mma_bf16_ta_lo(ds, ps + 16u * kk + 8, vt + 128u * kk, IDESC2, 1u);
+            }
+            ptx::mma_commit(&empty[Stage::slot(v_before)]);
             if (j == cnt) ptx::mma_commit(o_full);
           }
         }
@@ -375,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp < 4) {
     const int t64 = tid - 64;
     uint32_t n = 0, items = 0, turn = 0;
-    for (long long u = u0; u < u1; ++items) {
+    for (int u = u0; u < u1; ++items) {
       const Unit it = unit_at(*plan, a, u, u1);
       if (items > 0) wait(q_empty, (items - 1) & 1);
       if (ok) load_queries<D, F32>(a, it, t64, qimg);
@@ -401,42 +421,55 @@ __global__ void __launch_bounds__(kThreads, 1)
       u += it.t1 - it.t0;
     }
   } else {
-    const int wg = (warp - 4) >> 2;              // takes the item's tiles of this parity
-    const int row = 32 * (warp & 3) + lane;      // query of the tile, TMEM lane
-    const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    const uint32_t ts = tl + 128 * wg, to = tl + 256 + 128 * wg;
+    const int group = (warp - 4) >> 2;           // of four warps
+    const int set = group & 1, half = group >> 1;  // tiles of this parity, keys of this half of them
+    const int quad = warp & 3, row = 32 * quad + lane;  // query of the tile, TMEM lane
+    const uint32_t tl = tmem + ((uint32_t)(32 * quad) << 16);
+    const uint32_t ts = tl + 128 * set + 64 * half, to = tl + 256 + 128 * set + half * (D / 2);
     const int G = a.nq / a.nkv;
     const float c = a.scale_log2;
-    uint32_t ns = 0, items = 0, nc[2] = {0, 0};
-    for (long long u = u0; u < u1; ++items) {
+    uint32_t ns = 0, items = 0, c_turn = 0;
+    for (int u = u0; u < u1; ++items) {
       const Unit it = unit_at(*plan, a, u, u1);
       const int cnt = it.t1 - it.t0, nqs = it.rows * G;
       const int q = it.qt * 128 + row, i = q / G;
       const bool live = q < nqs;
-      const bool warp_live = it.qt * 128 + 32 * (warp & 3) < nqs;  // a query of the warp is
+      const bool warp_live = it.qt * 128 + 32 * quad < nqs;  // a query of the warp is
       const int h = it.g * G + (q - i * G);
-      const uint64_t vis = live ? visible_rows(a, it.r0 + i, i, it.rows) : 0ull;
+      const uint64_t vis = live && it.t1 > it.L / 128 ? visible_rows(a, it.r0 + i, i, it.rows) : 0ull;
       float m = -INFINITY, l = 0.f;
-      for (int j = wg; j < cnt; j += 2, ++ns) {
-        wait(&s_full[wg], ns & 1);
+      for (int j = set; j < cnt; j += 2, ++ns) {
+        wait(&s_full[set], ns & 1);
         ok = __all_sync(~0u, ok);
-        if (ok && warp_live) {
+        // (a warp without a query leaves what it has in the place of P: it reaches
+        // the accumulators of rows that are not read)
+        if (warp_live) {
           ptx::tc_fence_after();
-          const int p0 = (it.t0 + j) * 128;
-          const bool tail = p0 + 128 > it.L;
+          const int p0 = (it.t0 + j) * 128 + 64 * half;
+          const bool tail = p0 + 64 > it.L;
+          uint32_t bits[2] = {~0u, ~0u};
+          if (tail) bits[0] = key_bits(p0, it.L, vis), bits[1] = key_bits(p0 + 32, it.L, vis);
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          uint32_t sv[2][32];
-          // 32 scores at a time, the next 32 on their way, -inf where the row does not see
-          ptx::tmem_ld32(ts, sv[0]);
+          {
+            uint32_t all[2][32];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
+            for (int x = 0; x < 2; ++x) ptx::tmem_ld32(ts + 32 * x, all[x]);
             ptx::tmem_ld_wait();
-            ptx::tmem_ld32(ts + 32 * ((x + 1) & 3), sv[(x + 1) & 1]);
-            if (tail) mask_scores(sv[x & 1], key_bits(p0 + 32 * x, it.L, vis));
 #pragma unroll
-            for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(sv[x & 1][e]));
+            for (int x = 0; x < 2; ++x) {
+              if (tail) mask_scores<32>(all[x], bits[x]);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(all[x][e]));
+            }
           }
-          const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+          // the scores are read again below, 16 at a time: kept from here on they
+          // would not fit the registers
+          uint32_t sv[2][16];
+          ptx::tmem_ld16(ts, sv[0]);
+          const float mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          s_mx[group * 128 + row] = mine;
+          ptx::named_bar_sync(3 + 4 * set + quad, 64);
+          const float mt = fmaxf(mine, s_mx[(group ^ 2) * 128 + row]) * c;
           // (NaN scores pass the maximum by, and reach the sums)
           const bool grow = mt > m + kLazy || (m == -INFINITY && mt > m);
           if (__any_sync(~0u, grow)) {
@@ -444,78 +477,79 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
             l = grow ? l * f : l;
             if (j >= 2) {
+              ptx::tmem_ld_wait();
 #pragma unroll 1
-              for (int x = 0; x < D; x += 32) {
-                uint32_t o[32];
-                ptx::tmem_ld32(to + x, o);
+              for (int x = 0; x < D / 2; x += 16) {
+                uint32_t o[16];
+                ptx::tmem_ld16(to + x, o);
                 ptx::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = grow ? __float_as_uint(__uint_as_float(o[e]) * f) : o[e];
+                for (int e = 0; e < 16; ++e) o[e] = grow ? __float_as_uint(__uint_as_float(o[e]) * f) : o[e];
                 ptx::tmem_st16(to + x, o);
-                ptx::tmem_st16(to + x + 16, o + 16);
               }
             }
             m = m_new;
           }
           const float ref = m == -INFINITY ? 0.f : m;
           float ls[4] = {0.f, 0.f, 0.f, 0.f};
-          // again, now for P (its parts take the place of the scores they come from)
-#pragma unroll
+          // P: of each 16 keys the hi parts, then the lo parts, in the place of
+          // their scores
+#pragma unroll 2
           for (int x = 0; x < 4; ++x) {
-            uint32_t hi[16], lo[16];
-            uint32_t(&v)[32] = sv[x & 1];
+            uint32_t p[16];
+            uint32_t(&v)[16] = sv[x & 1];
             ptx::tmem_ld_wait();
-            if (x < 3) ptx::tmem_ld32(ts + 32 * (x + 1), sv[(x + 1) & 1]);
-            if (tail) mask_scores(v, key_bits(p0 + 32 * x, it.L, vis));
+            if (x < 3) ptx::tmem_ld16(ts + 16 * (x + 1), sv[(x + 1) & 1]);
+            if (tail) mask_scores<16>(v, (x < 2 ? bits[0] : bits[1]) >> (16 * (x & 1)));
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float p0_ = ex2(fmaf(__uint_as_float(v[2 * e]), c, -ref));
-              const float p1_ = ex2(fmaf(__uint_as_float(v[2 * e + 1]), c, -ref));
-              ls[2 * (e & 1)] += p0_;
-              ls[2 * (e & 1) + 1] += p1_;
-              hi_lo(p0_, p1_, hi[e], lo[e]);
+            for (int e = 0; e < 8; ++e) {
+              const float a0 = ex2(fmaf(__uint_as_float(v[2 * e]), c, -ref));
+              const float a1 = ex2(fmaf(__uint_as_float(v[2 * e + 1]), c, -ref));
+              ls[2 * (e & 1)] += a0;
+              ls[2 * (e & 1) + 1] += a1;
+              hi_lo(a0, a1, p[e], p[8 + e]);
             }
-            ptx::tmem_st16(ts + 32 * x, hi);
-            ptx::tmem_st16(ts + 32 * x + 16, lo);
+            ptx::tmem_st16(ts + 16 * x, p);
           }
           l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
           ptx::tmem_st_wait();
           ptx::tc_fence_before();
         }
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&p_full[wg]);
+        if (lane == 0) ptx::mbar_arrive(&p_full[set]);
       }
-      // ---- the item's end: both groups' parts, each group half of the dims ----
+      // ---- the item's end: the two sets' parts, each group a quarter of the dims ----
       const bool tails = it.t1 > it.L / 128;
       wait(o_full, items & 1);
       if (tails)
         for (int t = max(it.L / 128, it.t0); t < it.t1; ++t) {
           const int x = t - it.L / 128;
-          wait(&v_clean[x], nc[x]++ & 1);
+          wait(&v_clean[x], (c_turn >> x) & 1);
+          c_turn ^= 1u << x;
         }
       ok = __all_sync(~0u, ok);
       ptx::tc_fence_after();
-      s_ml[wg * 128 + row] = make_float2(m, l);
-      ptx::named_bar_sync(1, 256);
-      const float2 ml0 = s_ml[row], ml1 = s_ml[128 + row];
-      const float M = fmaxf(ml0.x, ml1.x);
-      const float w0 = part_weight(ml0.x, M), w1 = cnt > 1 ? part_weight(ml1.x, M) : 0.f;
-      const float lt = ml0.y * w0 + (cnt > 1 ? ml1.y * w1 : 0.f);
+      s_ml[group * 128 + row] = make_float2(m, l);
+      ptx::named_bar_sync(1, 512);
+      const float m0 = s_ml[row].x, m1 = s_ml[128 + row].x;
+      const float l0 = s_ml[row].y + s_ml[256 + row].y, l1 = s_ml[128 + row].y + s_ml[384 + row].y;
+      const float M = fmaxf(m0, m1);
+      const float w0 = part_weight(m0, M), w1 = cnt > 1 ? part_weight(m1, M) : 0.f;
+      const float lt = l0 * w0 + (cnt > 1 ? l1 * w1 : 0.f);
       const unsigned long long bad = tails ? *s_bad & vis : 0ull;
       if (ok && warp_live) {
         const bool done = it.t0 == 0 && it.t1 == it.tiles;
+        const size_t part = (size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1);
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
-        const size_t part = ((size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1)) * 128 + row;
 #pragma unroll 1
-        for (int x = 0; x < D / 2; x += 32) {
-          const int d0 = wg * (D / 2) + x;
-          uint32_t o0[32], o1[32];
-          ptx::tmem_ld32(tl + 256 + d0, o0);
-          if (cnt > 1) ptx::tmem_ld32(tl + 384 + d0, o1);
+        for (int d0 = group * (D / 4); d0 < (group + 1) * (D / 4); d0 += 16) {
+          uint32_t o0[16], o1[16];
+          ptx::tmem_ld16(tl + 256 + d0, o0);
+          if (cnt > 1) ptx::tmem_ld16(tl + 384 + d0, o1);
           ptx::tmem_ld_wait();
-          float o[32];
+          float o[16];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
+          for (int e = 0; e < 16; ++e) {
             o[e] = w0 != 0.f ? __uint_as_float(o0[e]) * w0 : 0.f;
             if (cnt > 1 && w1 != 0.f) o[e] = fmaf(__uint_as_float(o1[e]), w1, o[e]);
           }
@@ -524,23 +558,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bf16* v = a.v + (((size_t)it.b * a.nkv + it.g) * a.cap + it.L + r) * D + d0;
             if (it.L + r >= it.t0 * 128 && it.L + r < it.t1 * 128)
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
+              for (int e = 0; e < 16; ++e) {
                 const float y = __bfloat162float(v[e]);
                 if (!(fabsf(y) <= 3.4e38f)) o[e] += y;
               }
           }
           if (live && !done) {
-            float4* dst = reinterpret_cast<float4*>(ws.o + part * D + d0);
+            float4* dst = ws.o + (part * (D / 4) + d0 / 4) * 128 + row;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int e = 0; e < 4; ++e) dst[e * 128] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           } else if (live) {
-            write_out<32>(a, o, inv, ((size_t)(it.r0 + i) * a.nq + h) * D + d0);
+            write_out<16>(a, o, inv, ((size_t)(it.r0 + i) * a.nq + h) * D + d0);
           }
           __syncwarp();
         }
-        if (live && wg == 0) {
+        if (live && group == 0) {
           if (!done)
-            ws.ml[part] = make_float2(M, lt);
+            ws.ml[part * 128 + row] = make_float2(M, lt);
           else if (a.lse)
             a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, lt);
         }
@@ -556,63 +590,61 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 1) ptx::tmem_dealloc(tmem, 512);
 }
 
-// The parts of items cut between CTAs, joined in CTA order: a warp per query, a
-// lane D / 32 dims; every part's maximum first, then eight parts' rows in flight.
+// The parts of items cut between CTAs, joined in CTA order: a thread per query and
+// four dims, a warp over 32 queries (16 bytes each side by side in a part), eight
+// parts in flight.
+constexpr int kCombineQuads = 8;  // of a CTA: its warps
 template <int D>
-__global__ void __launch_bounds__(256) tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas) {
-  constexpr int E = D / 32, U = 8;
+__global__ void __launch_bounds__(32 * kCombineQuads)
+    tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas) {
+  constexpr int U = 8;
   __shared__ UnitPlan plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   if (warp == 0) make_plan(a, 128, lane, plan, false);
   __syncthreads();
-  long long us;
+  int us;
   if (!item_at(plan, a, blockIdx.x, us)) return;
-  const Unit it = unit_at(plan, a, us, us + (1ll << 40));
-  const int G = a.nq / a.nkv, row = 8 * blockIdx.y + warp, q = it.qt * 128 + row;
-  if (q >= it.rows * G) return;
+  const Unit it = unit_at(plan, a, us, 0x7fffffff);
   const int c0 = unit_owner(plan, us, ctas), c1 = unit_owner(plan, us + it.tiles - 1, ctas);
   if (c0 == c1) return;  // written by its CTA
-  const int n = c1 - c0 + 1;
-  auto part = [&](int k) { return ((size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0)) * 128 + row; };
-  float M = -INFINITY;
-  for (int k = lane; k < n; k += 32) M = fmaxf(M, __ldcg(&ws.ml[part(k)]).x);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(~0u, M, o));
-  float l = 0.f, x[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  const int G = a.nq / a.nkv, row = 32 * blockIdx.y + lane, q = it.qt * 128 + row;
+  if (q >= it.rows * G) return;
+  const int n = c1 - c0 + 1, quad = kCombineQuads * blockIdx.z + warp;
+  auto part = [&](int k) { return (size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0); };
+  float M = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int k = U; k < n; ++k) M = fmaxf(M, __ldcg(&ws.ml[part(k) * 128 + row]).x);
   for (int k0 = 0; k0 < n; k0 += U) {
     float2 ml[U];
-    float v[U][E];
+    float4 v[U];
 #pragma unroll
     for (int k = 0; k < U; ++k)
       if (k0 + k < n) {
-        ml[k] = __ldcg(&ws.ml[part(k0 + k)]);
-        const float* s = ws.o + part(k0 + k) * D + E * lane;
-        if constexpr (E == 4) {
-          const float4 t = __ldcg(reinterpret_cast<const float4*>(s));
-          v[k][0] = t.x, v[k][1] = t.y, v[k][2] = t.z, v[k][3] = t.w;
-        } else {
-          const float2 t = __ldcg(reinterpret_cast<const float2*>(s));
-          v[k][0] = t.x, v[k][1] = t.y;
-        }
+        ml[k] = __ldcg(&ws.ml[part(k0 + k) * 128 + row]);
+        v[k] = __ldcg(&ws.o[(part(k0 + k) * (D / 4) + quad) * 128 + row]);
       }
+    if (k0 == 0) {
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (k < n) M = fmaxf(M, ml[k].x);
+    }
 #pragma unroll
     for (int k = 0; k < U; ++k)
       if (k0 + k < n) {
         const float w = part_weight(ml[k].x, M);
         if (w != 0.f) {
           l = fmaf(ml[k].y, w, l);
-#pragma unroll
-          for (int e = 0; e < E; ++e) x[e] = fmaf(v[k][e], w, x[e]);
+          x[0] = fmaf(v[k].x, w, x[0]);
+          x[1] = fmaf(v[k].y, w, x[1]);
+          x[2] = fmaf(v[k].z, w, x[2]);
+          x[3] = fmaf(v[k].w, w, x[3]);
         }
       }
   }
   const int i = q / G, h = it.g * G + (q - i * G);
-  write_out<E>(a, x, l == 0.f ? 0.f : 1.f / l, ((size_t)(it.r0 + i) * a.nq + h) * D + E * lane);
-  if (lane == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, l);
+  write_out<4>(a, x, l == 0.f ? 0.f : 1.f / l, ((size_t)(it.r0 + i) * a.nq + h) * D + 4 * quad);
+  if (quad == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, l);
 }
 
 // Items of at most this many key tiles are each done by one CTA, without the
@@ -621,7 +653,7 @@ constexpr int kWholeTiles = 2;
 
 template <int D, bool F32>
 cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs& a, const TreeWork& ws,
-                   int64_t items, int64_t most_tiles, int sms, cudaStream_t st) {
+                   int64_t items, int most_queries, int64_t most_tiles, int sms, cudaStream_t st) {
   using S = Shape<D, F32>;
   static const cudaError_t attr = cudaFuncSetAttribute(
       tree_attn_kernel<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
@@ -632,7 +664,8 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                                    (int)whole);
   if (e != cudaSuccess || whole) return e;
-  return launch_pdl(tree_combine_kernel<D>, dim3((unsigned)items, 16), dim3(256), 0, st, 1, a, ws, ctas);
+  return launch_pdl(tree_combine_kernel<D>, dim3((unsigned)items, (most_queries + 31) / 32, D / 4 / kCombineQuads),
+                    dim3(32 * kCombineQuads), 0, st, 1, a, ws, ctas);
 }
 
 int device_sms() {
@@ -653,21 +686,25 @@ cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_k
                                   cudaStream_t st) {
   const int sms = device_sms(), G = a.nq / a.nkv;
   int64_t items = 0;
-  for (int b = 0; b < a.rm.batch; ++b)
-    items += (int64_t)((a.rm.start[b + 1] - a.rm.start[b]) * G + 127) / 128 * a.nkv;
+  int most = 0;  // queries of an item
+  for (int b = 0; b < a.rm.batch; ++b) {
+    const int n = (a.rm.start[b + 1] - a.rm.start[b]) * G;
+    items += (int64_t)(n + 127) / 128 * a.nkv;
+    if (n > most) most = n < 128 ? n : 128;
+  }
   TreeWork ws;
-  ws.o = (float*)workspace;
-  ws.ml = (float2*)(ws.o + (size_t)sms * 2 * 128 * head_dim);
+  ws.o = (float4*)workspace;
+  ws.ml = (float2*)(ws.o + (size_t)sms * 2 * 128 * head_dim / 4);
   CUtensorMap tk, tv;
   if (!encode_cache_map(&tk, a.k, head_dim, a.cap, (int64_t)a.rm.batch * a.nkv) ||
       !encode_cache_map(&tv, a.v, head_dim, a.cap, (int64_t)a.rm.batch * a.nkv))
     return cudaErrorInvalidValue;
   const int64_t tiles = (max_keys + 127) / 128;
   if (head_dim == 128)
-    return a.q_f32 ? launch<128, true>(tk, tv, a, ws, items, tiles, sms, st)
-                   : launch<128, false>(tk, tv, a, ws, items, tiles, sms, st);
-  return a.q_f32 ? launch<64, true>(tk, tv, a, ws, items, tiles, sms, st)
-                 : launch<64, false>(tk, tv, a, ws, items, tiles, sms, st);
+    return a.q_f32 ? launch<128, true>(tk, tv, a, ws, items, most, tiles, sms, st)
+                   : launch<128, false>(tk, tv, a, ws, items, most, tiles, sms, st);
+  return a.q_f32 ? launch<64, true>(tk, tv, a, ws, items, most, tiles, sms, st)
+                 : launch<64, false>(tk, tv, a, ws, items, most, tiles, sms, st);
 }
 
 }  // namespace as2d

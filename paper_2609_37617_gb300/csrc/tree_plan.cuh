@@ -12,8 +12,8 @@
 
 namespace as2d {
 
-struct UnitPlan {
-  long long unit[kMaxBatch + 1];  // units before each request
+struct alignas(16) UnitPlan {
+  int unit[kMaxBatch + 1];  // units before each request (the host refuses calls of 2^31)
   int len[kMaxBatch];
   int tiles[kMaxBatch];           // key tiles of a request's items
   int qts[kMaxBatch];             // query tiles of a request
@@ -29,7 +29,7 @@ struct Unit {
 // theirs, have no units.
 __device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int lane, UnitPlan& p, bool flag) {
   const int G = a.nq / a.nkv;
-  long long before = 0;
+  int before = 0;
   bool over = false;
 #pragma unroll
   for (int h = 0; h < kMaxBatch / 32; ++h) {
@@ -44,10 +44,11 @@ __device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int lan
       else
         over = over || rows > 0;
     }
-    long long n = (long long)a.nkv * qts * tiles, at = n;
+    const int n = a.nkv * qts * tiles;
+    int at = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long t = __shfl_up_sync(~0u, at, o);
+      const int t = __shfl_up_sync(~0u, at, o);
       if (lane >= o) at += t;
     }
     p.unit[b] = before + at - n;
@@ -61,9 +62,9 @@ __device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int lan
 }
 
 // First unit of item n; false past the last one.
-__device__ __forceinline__ bool item_at(const UnitPlan& p, const TreeArgs& a, long long n, long long& u) {
+__device__ __forceinline__ bool item_at(const UnitPlan& p, const TreeArgs& a, int n, int& u) {
   for (int b = 0; b < a.rm.batch; ++b) {
-    const long long items = p.tiles[b] > 0 ? (long long)a.nkv * p.qts[b] : 0;
+    const int items = p.tiles[b] > 0 ? a.nkv * p.qts[b] : 0;
     if (n < items) {
       u = p.unit[b] + n * p.tiles[b];
       return true;
@@ -73,9 +74,10 @@ __device__ __forceinline__ bool item_at(const UnitPlan& p, const TreeArgs& a, lo
   return false;
 }
 
-// Units of CTA c: even shares of all of them, or (whole) those of item c.
+// Units [u0, u1) of CTA c: even shares of all of them (one more for the first
+// CTAs, and no more CTAs than units), or (whole) those of item c.
 __device__ __forceinline__ void unit_range(const UnitPlan& p, const TreeArgs& a, int c, int ctas, int whole,
-                                           long long& u0, long long& u1) {
+                                           int& u0, int& u1) {
   if (whole) {
     u0 = u1 = 0;
     if (item_at(p, a, c, u0)) {
@@ -85,18 +87,22 @@ __device__ __forceinline__ void unit_range(const UnitPlan& p, const TreeArgs& a,
     }
     return;
   }
-  const long long n = p.unit[kMaxBatch], of = min((long long)ctas, n);  // no CTA among them without units
-  u0 = c < of ? c * n / of : 0;
-  u1 = c < of ? (c + 1) * n / of : 0;
+  const int n = p.unit[kMaxBatch], of = min(ctas, n);
+  u0 = u1 = 0;
+  if (c >= of) return;
+  const int each = n / of, more = n - each * of;
+  u0 = c * each + min(c, more);
+  u1 = u0 + each + (c < more ? 1 : 0);
 }
 // The CTA that does unit u.
-__device__ __forceinline__ int unit_owner(const UnitPlan& p, long long u, int ctas) {
-  const long long n = p.unit[kMaxBatch];
-  return (int)(((u + 1) * min((long long)ctas, n) - 1) / n);
+__device__ __forceinline__ int unit_owner(const UnitPlan& p, int u, int ctas) {
+  const int n = p.unit[kMaxBatch], of = min(ctas, n);
+  const int each = n / of, more = n - each * of, wide = more * (each + 1);
+  return u < wide ? u / (each + 1) : more + (u - wide) / each;
 }
 
 // What is done of unit u's item from u on, up to unit u1 at most.
-__device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, long long u, long long u1) {
+__device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, int u, int u1) {
   Unit it;
   int lo = 0, hi = kMaxBatch - 1;  // the last request whose first unit is at or before u
   while (lo < hi) {
@@ -111,13 +117,11 @@ __device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, lo
   it.L = p.len[lo];
   it.r0 = a.rm.start[lo];
   it.rows = a.rm.start[lo + 1] - it.r0;
-  const long long rel = u - p.unit[lo];
-  const long long item = rel / it.tiles;
-  it.t0 = (int)(rel - item * it.tiles);
-  it.g = (int)(item / p.qts[lo]);
-  it.qt = (int)(item - (long long)it.g * p.qts[lo]);
-  const long long left = u1 - u;
-  it.t1 = left < it.tiles - it.t0 ? it.t0 + (int)left : it.tiles;
+  const int rel = u - p.unit[lo], item = rel / it.tiles;
+  it.t0 = rel - item * it.tiles;
+  it.g = item / p.qts[lo];
+  it.qt = item - it.g * p.qts[lo];
+  it.t1 = min(it.tiles, it.t0 + u1 - u);
   return it;
 }
 
