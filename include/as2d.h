@@ -616,7 +616,7 @@ as2d_status as2d_cache_evict(const as2d_cache* cache, float* weights, int32_t* k
    each row, sums in 32 bits or more.  logits, probs: device float [n_rows][vocab],
    4-byte aligned; probs may be logits.  temperature: finite, > 0.  Logits of -inf
    get 0; a row that holds nothing else gets all zeros; NaN or +inf in a row
-   makes the row NaN. */
+   makes the row NaN.  vocab <= 2^24. */
 as2d_status as2d_token_probs(const float* logits, int32_t n_rows, int32_t vocab,
                              float temperature, float* probs, void* stream);
 
@@ -633,12 +633,13 @@ as2d_status as2d_token_probs(const float* logits, int32_t n_rows, int32_t vocab,
    k (without draft_probs: p_n without candidate n) and from p_k otherwise: the
    lowest v at which the sum of the weights up to v exceeds u_k times their total
    (sums to some 48 bits).  With u uniform the tokens follow the target's
-   distribution.  Weights need not sum to 1; negative and NaN ones count as 0.  If max(p_n -
+   distribution.  Weights need not sum to 1; negative, infinite
+   and NaN ones count as 0.  If max(p_n -
    q_n, 0) is 0 throughout the token is drawn from p_n; if that is too, token
    is -1.  A candidate outside [0, vocab) does not stand and takes nothing from
    p_n (with draft_probs its row is used as it is).
    k: host int32 [batch], 1 <= batch <= AS2D_MAX_BATCH, each <= AS2D_MAX_K;
-   candidates may be NULL if all are 0.  n_accepted, token: device int32 [batch]. */
+   vocab <= 2^24; candidates may be NULL if all are 0.  n_accepted, token: device int32 [batch]. */
 as2d_status as2d_accept_sampled(const float* probs, const float* draft_probs,
                                 const int32_t* candidates, const int32_t* k, int32_t batch,
                                 int32_t vocab, const float* u, int32_t* n_accepted,

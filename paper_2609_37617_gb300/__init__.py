@@ -645,14 +645,22 @@ class State:
 
 # ---- operators on tensors ------------------------------------------------------
 
-def _tensor(t, name, dtypes, shape=None, contiguous=True):
-    """Checks a CUDA tensor argument and returns its device address."""
+def _device():
     import torch
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+    return torch.cuda.current_device()
+
+
+def _tensor(t, name, device, dtypes, shape=None, contiguous=True):
+    """Checks a CUDA tensor argument and returns its device address."""
+    try:
+        good = t.dtype in dtypes
+    except AttributeError:
+        good = False
+    if not good:
         raise TypeError(f"{name} must be a tensor of {' or '.join(map(str, dtypes))}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != device:
         raise ValueError(f"{name} must be on the current CUDA device")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -670,11 +678,14 @@ class Cache:
         import torch
         if k.dim() != 5:
             raise ValueError("k must have shape [n_layers, batch, n_kv, capacity, head_dim]")
-        kp = _tensor(k, "k", (torch.bfloat16,))
-        vp = _tensor(v, "v", (torch.bfloat16,), k.shape)
+        kp = _tensor(k, "k", _device(), (torch.bfloat16,))
+        vp = _tensor(v, "v", _device(), (torch.bfloat16,), k.shape)
         self.k, self.v, self.shape = k, v, tuple(k.shape)
         self._c = as2d_cache(kp, vp, *self.shape)
         self._ref = ctypes.byref(self._c)
+        self._i32s = ctypes.c_int32 * self.shape[1]
+        self._f32, self._i32, self._q = (torch.float32,), (torch.int32,), (torch.bfloat16, torch.float32)
+        self._mask = (torch.int64, torch.uint64)
         need = _I64()
         _check(_lib.as2d_tree_attention_workspace(self._ref, ctypes.byref(need)),
                "as2d_tree_attention_workspace")
@@ -682,79 +693,80 @@ class Cache:
         _check(_lib.as2d_cache_evict_workspace(self._ref, ctypes.byref(need)),
                "as2d_cache_evict_workspace")
         self._workspace = torch.empty(max(most, need.value), dtype=torch.uint8, device=k.device)
+        self._workspace_at = self._workspace.data_ptr(), self._workspace.numel()
 
-    def _rows(self, q, kv_len, rows, visible, scale, max_len):
-        import torch
-        _, batch, _, _, d = self.shape
-        if len(rows) != batch:
-            raise ValueError(f"rows must name {batch} requests")
-        _tensor(q, "q", (torch.bfloat16, torch.float32), contiguous=False)
-        if q.dim() != 3 or q.shape[2] != d or q.stride(2) != 1 or q.stride(1) != d:
+    def _counts(self, values, name):
+        if len(values) != self.shape[1]:
+            raise ValueError(f"{name} must name {self.shape[1]} requests")
+        return self._i32s(*values)
+
+    def _rows(self, device, q, kv_len, rows, visible, scale, max_len):
+        d = self.shape[4]
+        at = _tensor(q, "q", device, self._q, None, False)
+        shape = q.shape
+        if len(shape) != 3 or shape[2] != d or q.stride(2) != 1 or q.stride(1) != d:
             raise ValueError(f"q must be [rows, n_q, {d}] with contiguous rows")
-        n = q.shape[0]
+        n = shape[0]
+        host_rows = self._counts(rows, "rows")
         if n != sum(rows):
             raise ValueError("q must have as many rows as the requests together")
-        # the stride of a single row is not looked at
-        stride = q.stride(0) if n > 1 else q.shape[1] * d
-        host_rows = _i32_array(rows)
         r = as2d_tree_rows(
-            q.data_ptr(), AS2D_TYPE_F32 if q.dtype == torch.float32 else AS2D_TYPE_BF16, q.shape[1],
-            stride, _tensor(kv_len, "kv_len", (torch.int32,), (batch,)), int(max_len),
+            at, AS2D_TYPE_BF16 if q.dtype is self._q[0] else AS2D_TYPE_F32, shape[1],
+            q.stride(0) if n > 1 else shape[1] * d,  # (the stride of a single row is not looked at)
+            _tensor(kv_len, "kv_len", device, self._i32, self.shape[1:2]), max_len,
             ctypes.addressof(host_rows),
-            None if visible is None else _tensor(visible, "visible", (torch.int64, torch.uint64), (n,)),
-            d ** -0.5 if scale is None else float(scale))
+            None if visible is None else _tensor(visible, "visible", device, self._mask, shape[:1]),
+            d ** -0.5 if scale is None else scale)
         r.keep = host_rows  # alive as long as the descriptor
         return r
 
     def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
                        lse=None, error_bits=None, stream=0):
         """as2d_tree_attention; returns out (made like q unless given)."""
-        import torch
-        r = self._rows(q, kv_len, rows, visible, scale, max_len)
+        device = _device()
+        r = self._rows(device, q, kv_len, rows, visible, scale, max_len)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         _check(_lib.as2d_tree_attention(
-            self._ref, layer, ctypes.byref(r), _tensor(out, "out", (q.dtype,), q.shape),
-            None if lse is None else _tensor(lse, "lse", (torch.float32,), q.shape[:2]),
-            self._workspace.data_ptr(), self._workspace.numel(),
-            None if error_bits is None else _tensor(error_bits, "error_bits", (torch.int32,)),
+            self._ref, layer, ctypes.byref(r), _tensor(out, "out", device, (q.dtype,), q.shape),
+            None if lse is None else _tensor(lse, "lse", device, self._f32, q.shape[:2]),
+            *self._workspace_at,
+            None if error_bits is None else _tensor(error_bits, "error_bits", device, self._i32),
             stream), "as2d_tree_attention")
         return out
 
     def attention_weights(self, q, lse, weights, kv_len, rows, visible=None, layer=0, scale=None,
                           max_len=0, error_bits=None, stream=0):
         """as2d_attention_weights: adds to weights in place."""
-        import torch
-        r = self._rows(q, kv_len, rows, visible, scale, max_len)
+        device = _device()
+        r = self._rows(device, q, kv_len, rows, visible, scale, max_len)
         _check(_lib.as2d_attention_weights(
-            self._ref, layer, ctypes.byref(r), _tensor(lse, "lse", (torch.float32,), q.shape[:2]),
-            _tensor(weights, "weights", (torch.float32,), self.shape[:4]),
-            None if error_bits is None else _tensor(error_bits, "error_bits", (torch.int32,)),
+            self._ref, layer, ctypes.byref(r), _tensor(lse, "lse", device, self._f32, q.shape[:2]),
+            _tensor(weights, "weights", device, self._f32, self.shape[:4]),
+            None if error_bits is None else _tensor(error_bits, "error_bits", device, self._i32),
             stream), "as2d_attention_weights")
 
     def evict(self, weights, kv_len, keep, recent=0, stream=0):
         """as2d_cache_evict: cuts the cache, weights and kv_len in place."""
-        import torch
-        batch = self.shape[1]
-        if len(keep) != batch:
-            raise ValueError(f"keep must name {batch} requests")
+        device = _device()
         _check(_lib.as2d_cache_evict(
-            self._ref, _tensor(weights, "weights", (torch.float32,), self.shape[:4]),
-            _tensor(kv_len, "kv_len", (torch.int32,), (batch,)), _i32_array(keep), int(recent),
-            self._workspace.data_ptr(), self._workspace.numel(), stream), "as2d_cache_evict")
+            self._ref, _tensor(weights, "weights", device, self._f32, self.shape[:4]),
+            _tensor(kv_len, "kv_len", device, self._i32, self.shape[1:2]),
+            self._counts(keep, "keep"), recent, *self._workspace_at, stream), "as2d_cache_evict")
 
 
 def token_probs(logits, temperature, out=None, stream=0):
     """as2d_token_probs of logits [rows, vocab]; returns out (made like logits
     unless given; may be logits)."""
     import torch
-    lp = _tensor(logits, "logits", (torch.float32,))
+    device, kind = _device(), (torch.float32,)
+    at = _tensor(logits, "logits", device, kind)
     if logits.dim() != 2:
         raise ValueError("logits must be [rows, vocab]")
     if out is None:
         out = torch.empty_like(logits)
-    _check(_lib.as2d_token_probs(lp, *logits.shape, float(temperature),
-                                 _tensor(out, "out", (torch.float32,), logits.shape), stream),
+    _check(_lib.as2d_token_probs(at, *logits.shape, temperature,
+                                 _tensor(out, "out", device, kind, logits.shape), stream),
            "as2d_token_probs")
     return out
 
@@ -763,15 +775,17 @@ def accept_sampled(probs, candidates, k, u, n_accepted, token, draft_probs=None,
     """as2d_accept_sampled: probs [sum (k + 1), vocab], candidates [sum k] (or
     None), k a list, u [sum (k + 1)], n_accepted and token [batch]."""
     import torch
+    device, f32, i32 = _device(), (torch.float32,), (torch.int32,)
     total, batch = sum(k), len(k)
-    pp = _tensor(probs, "probs", (torch.float32,))
+    at = _tensor(probs, "probs", device, f32)
     if probs.dim() != 2 or probs.shape[0] != total + batch:
         raise ValueError("probs must be [sum (k + 1), vocab]")
+    vocab = probs.shape[1]
     _check(_lib.as2d_accept_sampled(
-        pp, None if draft_probs is None or total == 0 else
-        _tensor(draft_probs, "draft_probs", (torch.float32,), (total, probs.shape[1])),
+        at, None if draft_probs is None or total == 0 else
+        _tensor(draft_probs, "draft_probs", device, f32, (total, vocab)),
         None if candidates is None or total == 0 else
-        _tensor(candidates, "candidates", (torch.int32,), (total,)), _i32_array(k), batch,
-        probs.shape[1], _tensor(u, "u", (torch.float32,), (total + batch,)),
-        _tensor(n_accepted, "n_accepted", (torch.int32,), (batch,)),
-        _tensor(token, "token", (torch.int32,), (batch,)), stream), "as2d_accept_sampled")
+        _tensor(candidates, "candidates", device, i32, (total,)), (ctypes.c_int32 * batch)(*k),
+        batch, vocab, _tensor(u, "u", device, f32, (total + batch,)),
+        _tensor(n_accepted, "n_accepted", device, i32, (batch,)),
+        _tensor(token, "token", device, i32, (batch,)), stream), "as2d_accept_sampled")

@@ -2,60 +2,343 @@
 // (as2d_attention_weights): over a request's rows i and the query heads h of a
 // kv head, w_t (+)= sum e^(scale q_ih k_t - lse_ih).
 //
-// A thread per key, which goes through the queries one after another.
+// The product is taken with the keys as the MMA's rows, S^T = K Q^T (M = 128 keys,
+// N = the queries, padded to 16): a thread owns a key and adds the exponentials
+// of its row of TMEM, so that no sum crosses threads, the order of every sum is
+// fixed, and each weight is read and written once by one thread.  32-bit queries
+// are bf16 hi and lo parts, two products.
+//
+// Work is cut as in k_tree_attn.cu: the key tiles of every (request, kv head),
+// weighted by the tiles of 128 queries that go over them, in even shares over one
+// CTA per SM; a tile belongs to the CTA in whose share its first unit falls.
+// Per CTA: warp 0 loads key tiles by TMA through a ring, warp 1 issues the
+// products into four TMEM buffers, warps 2-3 bring in the queries and their sums,
+// warps 4-7 and 8-11 take the tiles in turn.  More than 128 queries: one pass
+// over the CTA's tiles for each 128 (the keys then come from L2).
+#include <type_traits>
+
 #include "ops.h"
 #include "ptx_sm100.cuh"
+#include "tree_dev.cuh"
 
 namespace as2d {
 namespace {
 
-template <int D>
-__global__ void __launch_bounds__(128) attn_weights_kernel(const __grid_constant__ WeightArgs wa) {
+constexpr int kThreads = 384;
+
+template <int D, bool F32>
+struct Shape {
+  static constexpr uint32_t STAGE = 128 * D * 2;
+  static constexpr uint32_t Q = (F32 ? 2 : 1) * 128 * D * 2;
+  static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
+  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 128 * 4 + 128 * 8 + (2 * NST + 13) * 8 + 16;
+  static_assert(SMEM + sizeof(UnitPlan) <= 232448, "shared memory of one CTA");
+};
+
+// The tiles of one (request, kv head) in units [u, u1): [t0, t1); units done.
+struct Segment {
+  Unit it;
+  int units, passes;
+};
+__device__ __forceinline__ Segment segment_at(const UnitPlan& p, const TreeArgs& a, int u, int u1) {
+  Segment s;
+  s.it = unit_at(p, a, u, u1);  // (for the request; the rest is in another order here)
+  const int b = s.it.b, per = p.tiles[b] * p.qts[b], rel = u - p.unit[b];
+  s.passes = p.qts[b];
+  s.it.g = rel / per;
+  const int r0 = rel - s.it.g * per, r1 = min(per, r0 + (u1 - u));
+  s.units = r1 - r0;
+  s.it.t0 = (r0 + s.passes - 1) / s.passes;
+  s.it.t1 = (r1 + s.passes - 1) / s.passes;
+  s.it.qt = 0;
+  return s;
+}
+
+// Sum of the exponentials of 16 queries from column q0 on; masked: of those that
+// see key j of the rows' own, q < n.
+template <bool MASKED>
+__device__ __forceinline__ void add_weights(const uint32_t (&v)[16], float c, const float* lse, const uint64_t* vis,
+                                            int q0, int n, int j, float (&sum)[4]) {
+#pragma unroll
+  for (int e = 0; e < 16; e += 4) {
+    const float4 l = *reinterpret_cast<const float4*>(lse + q0 + e);
+    const float ls[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float p = ex2(fmaf(__uint_as_float(v[e + k]), c, -ls[k]));
+      if (MASKED) {
+        const int q = q0 + e + k;
+        if (q < n && (j < 0 || ((vis[q] >> j) & 1))) sum[k] += p;
+      } else {
+        sum[k] += p;
+      }
+    }
+  }
+}
+
+template <int D, bool F32>
+__global__ void __launch_bounds__(kThreads, 1)
+    attn_weights_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ WeightArgs wa) {
+  using S = Shape<D, F32>;
+  constexpr int NST = S::NST, NR = D / 64;
   const TreeArgs& a = wa.t;
-  __shared__ float s_q[D];
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint8_t* qimg = sm;
+  uint8_t* ring = sm + S::Q;
+  float* s_lse = reinterpret_cast<float*>(ring + NST * S::STAGE);  // [128] base 2
+  uint64_t* s_vis = reinterpret_cast<uint64_t*>(s_lse + 128);      // [128]
+  uint64_t* full = s_vis + 128;
+  uint64_t* empty = full + NST;
+  uint64_t* s_full = empty + NST;   // [4]
+  uint64_t* s_empty = s_full + 4;   // [4]
+  uint64_t* q_first = s_empty + 4;
+  uint64_t* q_full = q_first + 1;
+  uint64_t* q_empty = q_full + 1;
+  uint64_t* e_empty = q_empty + 1;
+  uint64_t* drain = e_empty + 1;
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(drain + 1);
+  __shared__ UnitPlan plan;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < NST; ++i) {
+      ptx::mbar_init(&full[i], 1);
+      ptx::mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      ptx::mbar_init(&s_full[i], 1);
+      ptx::mbar_init(&s_empty[i], 4);
+    }
+    ptx::mbar_init(q_first, kThreads / 32 - 2);
+    ptx::mbar_init(q_full, 2);
+    ptx::mbar_init(q_empty, 1);
+    ptx::mbar_init(e_empty, 8);
+    ptx::mbar_init(drain, 1);
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) ptx::tmem_alloc(tslot, 512);
+  if (warp == 0 && lane == 0) ptx::prefetch_tmap(&tmK);
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  const int g = blockIdx.y, b = blockIdx.z, G = a.nq / a.nkv;
-  const int r0 = a.rm.start[b], rows = a.rm.start[b + 1] - r0;
-  if (rows == 0) return;
-  const int L = a.len[b];
-  if (!rows_fit(L, rows, a.cap)) {
-    if (threadIdx.x == 0 && a.err) atomicOr(a.err, kErrCapacity);
-    return;
-  }
-  for (int t0 = blockIdx.x * 128; t0 < L + rows; t0 += gridDim.x * 128) {
-    const int t = t0 + threadIdx.x;
-    const bool live = t < L + rows;
-    float k[D], sum = 0.f;
-    const size_t head = (size_t)b * a.nkv + g;
-    for (int e = 0; e < D; ++e) k[e] = live ? __bfloat162float(a.k[(head * a.cap + t) * D + e]) : 0.f;
-    for (int n = 0; n < rows * G; ++n) {
-      const int r = r0 + n / G, h = g * G + n % G;
-      __syncthreads();
-      for (int e = threadIdx.x; e < D; e += 128) {
-        const int64_t at = r * a.q_stride + (int64_t)h * D + e;
-        s_q[e] = a.q_f32 ? ((const float*)a.q)[at] : __bfloat162float(((const bf16*)a.q)[at]);
+  if (warp == 0) make_plan(a, 128, lane, plan, blockIdx.x == 0);
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tslot;
+  const int G = a.nq / a.nkv;
+  int u0, u1;
+  unit_range(plan, a, blockIdx.x, gridDim.x, 0, u0, u1);
+  const unsigned long long limit = a.timeout_ns;
+  bool ok = true;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (ok && !ptx::mbar_spin(bar, parity, limit)) {
+      ok = false;
+      if (a.err) atomicOr(a.err, kErrTimeout);
+    }
+    return ok;
+  };
+  // queries of a pass (zeros up to the next 16th), their sums and masks, by N
+  // threads from t on
+  auto bring = [&](const Unit& it, int t, auto n_threads) {
+    constexpr int N = decltype(n_threads)::value;
+    load_queries<D, F32, N, 4>(a, it, t, qimg);
+    const int n0 = it.qt * 128, n = min(128, it.rows * G - n0), pad = (n + 15) & ~15;
+    for (int c = t; c < (pad - n) * (D / 8); c += N) {
+      uint8_t* to = qimg + chunk_off(n + c / (D / 8), c % (D / 8));
+      *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
+      if (F32) *reinterpret_cast<uint4*>(to + 128 * D * 2) = make_uint4(0, 0, 0, 0);
+    }
+    ptx::fence_proxy_async_smem();
+  };
+  auto bring_sums = [&](const Unit& it, int t, int n_threads) {
+    const int n0 = it.qt * 128, n = min(128, it.rows * G - n0);
+    for (int q = t; q < 128; q += n_threads) {
+      float l = 0.f;
+      uint64_t vis = 0;
+      if (q < n) {
+        const int i = (n0 + q) / G, h = it.g * G + (n0 + q - i * G);
+        l = a.lse[(size_t)(it.r0 + i) * a.nq + h] * 1.4426950408889634f;
+        vis = visible_rows(a, it.r0 + i, i, it.rows);
       }
-      __syncthreads();
-      const uint64_t vis = a.visible ? a.visible[r] : ~0ull >> (63 - (r - r0));
-      if (!live || (t >= L && !((vis >> (t - L)) & 1))) continue;
-      float s = 0.f;
-      for (int e = 0; e < D; ++e) s = fmaf(s_q[e], k[e], s);
-      sum += exp2f(s * a.scale_log2 - a.lse[(size_t)r * a.nq + h] * 1.4426950408889634f);
+      s_lse[q] = l;
+      s_vis[q] = vis;
     }
-    if (live) {
-      float* w = wa.w + head * a.cap + t;
-      *w = t < L ? *w + sum : sum;
+  };
+  // (the first pass that has tiles: by every warp that has nothing to do yet)
+  int uf = u0;
+  while (uf < u1) {
+    const Segment s = segment_at(plan, a, uf, u1);
+    if (s.it.t0 < s.it.t1) {
+      if (warp >= 2) {
+        bring(s.it, tid - 64, std::integral_constant<int, kThreads - 64>{});
+        bring_sums(s.it, tid - 64, kThreads - 64);
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(q_first);
+      }
+      break;
+    }
+    uf += s.units;
+  }
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint64_t pol = ptx::policy_evict_first();
+      Stage at;
+      uint32_t n = 0;
+      for (int u = uf; u < u1;) {
+        const Segment s = segment_at(plan, a, u, u1);
+        const int z = s.it.b * a.nkv + s.it.g;
+        for (int qt = 0; qt < s.passes; ++qt)
+          for (int t = s.it.t0; t < s.it.t1 && ok; ++t, ++n) {
+            const uint32_t k = at.next<NST>(), i = Stage::slot(k);
+            if (n >= NST && !wait(&empty[i], Stage::parity(k) ^ 1)) break;
+            ptx::mbar_arrive_expect_tx(&full[i], S::STAGE);
+#pragma unroll
+            for (int h = 0; h < NR; ++h)
+              ptx::tma_load_3d(ring + i * S::STAGE + h * kRegion, &tmK, &full[i], 64 * h, t * 128, z, pol);
+          }
+        u += s.units;
+      }
+      // no copy is in flight when the CTA ends
+      for (uint32_t i = n > NST ? n - NST : 0; i < n; ++i)
+        ptx::mbar_wait(&full[i % NST], (i / NST) & 1, ptx::kDrainNs);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t q_lo = ptx::desc_lo(ptx::smem_u32(qimg), 16u);
+      Stage at;
+      uint32_t done[2] = {0, 0}, pass = 0;  // tiles of each group so far
+      for (int u = uf; u < u1 && ok;) {
+        const Segment s = segment_at(plan, a, u, u1);
+        for (int qt = 0; qt < s.passes && s.it.t0 < s.it.t1 && ok; ++qt, ++pass) {
+          pass == 0 ? wait(q_first, 0) : wait(q_full, (pass - 1) & 1);
+          const int n = min(128, s.it.rows * G - qt * 128);
+          const uint32_t idesc = ptx::idesc_bf16_f32(128, (n + 15) & ~15);
+          for (int t = s.it.t0; t < s.it.t1 && ok; ++t) {
+            const int odd = (t - s.it.t0) & 1;
+            const uint32_t d = odd ? done[1] : done[0], buf = odd + 2 * (d & 1);
+            const uint32_t k = at.next<NST>(), i = Stage::slot(k);
+            if (!wait(&full[i], Stage::parity(k))) break;
+            if (d >= 2 && !wait(&s_empty[buf], ((d >> 1) - 1) & 1)) break;
+            ptx::tc_fence_after();
+            const uint32_t kt = ptx::desc_lo(ptx::smem_u32(ring + i * S::STAGE), 16u), ds = tmem + 128 * buf;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint32_t to = ((kk >> 2) * kRegion + 32u * (kk & 3)) >> 4;
+              if (kk == 0)
+                ptx::mma_bf16_lo<false>(ds, kt, q_lo, idesc);
+              else
+                ptx::mma_bf16_lo<true>(ds, kt + to, q_lo + to, idesc);
+              if (F32) ptx::mma_bf16_lo<true>(ds, kt + to, q_lo + to + (128u * D * 2 >> 4), idesc);
+            }
+            ptx::mma_commit(&s_full[buf]);
+            ptx::mma_commit(&empty[i]);
+            if (t == s.it.t1 - 1) ptx::mma_commit(q_empty);
+            if (odd)
+              ++done[1];
+            else
+              ++done[0];
+          }
+        }
+        u += s.units;
+      }
+      // no product is running when TMEM is freed
+      ptx::mma_commit(drain);
+      ptx::mbar_wait(drain, 0, ptx::kDrainNs);
+    }
+  } else if (warp < 4) {
+    uint32_t pass = 0;
+    for (int u = uf; u < u1;) {
+      Segment s = segment_at(plan, a, u, u1);
+      for (int qt = 0; qt < s.passes && s.it.t0 < s.it.t1; ++qt, ++pass) {
+        if (pass == 0) continue;
+        s.it.qt = qt;
+        wait(q_empty, (pass - 1) & 1);
+        if (ok) bring(s.it, tid - 64, std::integral_constant<int, 64>{});
+        wait(e_empty, (pass - 1) & 1);  // the last pass's sums have been read
+        if (ok) bring_sums(s.it, tid - 64, 64);
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(q_full);
+      }
+      u += s.units;
+    }
+  } else {
+    const int group = (warp - 4) >> 2, row = 32 * (warp & 3) + lane;  // key of the tile, TMEM lane
+    const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+    const float c = a.scale_log2;
+    uint32_t d = 0, pass = 0;
+    for (int u = uf; u < u1;) {
+      const Segment s = segment_at(plan, a, u, u1);
+      float* w = wa.w + ((size_t)s.it.b * a.nkv + s.it.g) * a.cap;
+      for (int qt = 0; qt < s.passes && s.it.t0 < s.it.t1; ++qt, ++pass) {
+        const int n = min(128, s.it.rows * G - qt * 128);
+        // the queries' sums are there (the products wait for them too)
+        pass == 0 ? wait(q_first, 0) : wait(q_full, (pass - 1) & 1);
+        for (int t = s.it.t0 + group; t < s.it.t1; t += 2, ++d) {
+          const int key = t * 128 + row, j = key - s.it.L;
+          const bool live = j < s.it.rows;
+          // its weight so far, on its way while the product runs
+          const float before = live && (j < 0 || qt > 0) ? w[key] : 0.f;
+          const uint32_t buf = group + 2 * (d & 1);
+          wait(&s_full[buf], (d >> 1) & 1);
+          ok = __all_sync(~0u, ok);
+          ptx::tc_fence_after();
+          const bool tail = t * 128 + 128 > s.it.L;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          uint32_t v[2][16];
+          ptx::tmem_ld16(tl + 128 * buf, v[0]);
+#pragma unroll 1
+          for (int q0 = 0; q0 < n; q0 += 32) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int q = q0 + 16 * x;
+              ptx::tmem_ld_wait();
+              if (q + 16 < n) ptx::tmem_ld16(tl + 128 * buf + q + 16, v[x ^ 1]);
+              if (q < n) {
+                if (tail || q + 16 > n)
+                  add_weights<true>(v[x], c, s_lse, s_vis, q, n, j, sum);
+                else
+                  add_weights<false>(v[x], c, s_lse, s_vis, q, n, j, sum);
+              }
+            }
+          }
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&s_empty[buf]);
+          if (live && ok) w[key] = before + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(e_empty);
+      }
+      u += s.units;
     }
   }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 1) ptx::tmem_dealloc(tmem, 512);
+}
+
+template <int D, bool F32>
+cudaError_t launch(const CUtensorMap& tk, const WeightArgs& a, int ctas, cudaStream_t st) {
+  using S = Shape<D, F32>;
+  static const cudaError_t attr = cudaFuncSetAttribute(
+      attn_weights_kernel<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
+  if (attr != cudaSuccess) return attr;
+  return launch_pdl(attn_weights_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, a);
 }
 
 }  // namespace
 
 cudaError_t launch_attention_weights(const WeightArgs& a, int head_dim, int64_t max_keys, cudaStream_t st) {
-  const dim3 grid((unsigned)((max_keys + 127) / 128), a.t.nkv, a.t.rm.batch);
-  return head_dim == 128 ? launch_pdl(attn_weights_kernel<128>, grid, dim3(128), 0, st, 1, a)
-                         : launch_pdl(attn_weights_kernel<64>, grid, dim3(128), 0, st, 1, a);
+  const int sms = device_sms();
+  CUtensorMap tk;
+  if (!encode_cache_map(&tk, a.t.k, head_dim, a.t.cap, (int64_t)a.t.rm.batch * a.t.nkv)) return cudaErrorInvalidValue;
+  const int64_t units = (max_keys + 127) / 128 * tree_items(a.t);
+  const int ctas = (int)(units < sms ? units : sms);
+  if (head_dim == 128) return a.t.q_f32 ? launch<128, true>(tk, a, ctas, st) : launch<128, false>(tk, a, ctas, st);
+  return a.t.q_f32 ? launch<64, true>(tk, a, ctas, st) : launch<64, false>(tk, a, ctas, st);
 }
 
 }  // namespace as2d

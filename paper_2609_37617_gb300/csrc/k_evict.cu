@@ -3,21 +3,28 @@
 //
 // evict_select_kernel, one CTA per unit (layer, request, kv head): the threshold
 // among the older entries' weights by radix selection (order keys of 32 bits,
-// 8 bits a pass, counted in shared memory), then the entries that stay, in
+// counted in shared memory), then the entries that stay, in
 // order: those above it, those equal to it from the lowest position up to the
 // number wanted, the latest `recent`.  It writes their old positions and moves
-// their weights.
-// evict_move_kernel, one CTA per unit and cache: entry j comes from position
-// at[j] >= j.  Tiles of entries in order, a tile read before it is written: what
-// a tile's writes cover, [j0, j0 + T), no later tile reads, as its entries
-// come from their own positions or later.
+// their weights.  The weights stay in registers over all passes.
+// evict_move_kernel, one CTA per unit, cache and 128 bytes of an entry: entry j comes
+// from position at[j] >= j.  Tiles of entries in order, a tile read wholly before
+// it is written: what its writes cover, [j0, j0 + T), no later tile reads, as
+// those entries come from their own positions or later; so the next tile's
+// reads are on their way while a tile is written.  Bound by memory: each entry that
+// moves is read and written once.
 #include "ops.h"
 #include "ptx_sm100.cuh"
 
 namespace as2d {
 namespace {
 
-constexpr int kSel = 1024;  // threads of the selection
+constexpr int kSel = 1024;   // threads of the selection
+// Digits of the radix selection, 11 + 11 + 10 bits from the top: the first takes
+// in the exponent and two bits of the mantissa, so that weights of one size still
+// fall into several bins (8-bit digits put them into one or two, whose counts
+// are then added one after another).
+constexpr int kPasses = 3, kBins = 2048;
 
 // An unsigned key in the order of the float values; NaN below all, -0 as 0.
 __device__ __forceinline__ uint32_t evict_key(float w) {
@@ -42,9 +49,13 @@ __device__ __forceinline__ int warp_prefix(int v, int* s, int* total) {
   return before;
 }
 
+// E: entries of a thread (a warp's are consecutive, 32 at a time), kept in
+// registers as keys.
+template <int E>
 __global__ void __launch_bounds__(kSel) evict_select_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ int hist[256], s_w[32], s_pick[2];
+  __shared__ int hist[kPasses * kBins], s_w[32], s_pick[2];
   ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
   const int unit = blockIdx.x, b = (unit / a.nkv) % a.batch;
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
   const int L = a.len[b], keep = a.keep[b];
@@ -56,95 +67,136 @@ __global__ void __launch_bounds__(kSel) evict_select_kernel(const __grid_constan
   uint16_t* at = a.at + (size_t)unit * a.cap;
   const int late = min(a.recent, keep), old = L - late;  // [old, L) stay
   int want = keep - late;                                // of [0, old)
+  const int t0 = w * 32 * E + lane;
+  float x[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) x[i] = t0 + 32 * i < L ? wt[t0 + 32 * i] : 0.f;
+  for (int i = tid; i < kPasses * kBins; i += kSel) hist[i] = 0;
+  __syncthreads();
   uint32_t prefix = 0, mask = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kSel) hist[i] = 0;
-    __syncthreads();
-    for (int t = tid; t < old; t += kSel) {
-      const uint32_t key = evict_key(wt[t]);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255], 1);
+#pragma unroll 1
+  for (int pass = 0; pass < kPasses; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t digit = pass < 2 ? kBins - 1 : kBins / 2 - 1;
+    int* h = hist + pass * kBins;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const uint32_t key = evict_key(x[i]);
+      if (t0 + 32 * i < old && (key & mask) == prefix) atomicAdd(&h[(key >> shift) & digit], 1);
     }
     __syncthreads();
-    if (tid == 0) {
-      int n = 0, bin = 255;
-      while (bin > 0 && n + hist[bin] < want) n += hist[bin--];
-      s_pick[0] = bin;
-      s_pick[1] = n;
+    // the bin in which the count from above reaches `want`: two bins a thread,
+    // the highest first
+    const int bin = kBins - 1 - 2 * tid, c0 = h[bin], c1 = h[bin - 1];
+    int upto = c0 + c1, all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(~0u, upto, o);
+      if (lane >= o) upto += t;
+    }
+    const int before = warp_prefix(__shfl_sync(~0u, upto, 31), s_w, &all) + upto - c0 - c1;
+    if (before < want && want <= before + c0 + c1) {
+      const bool lower = before + c0 < want;
+      s_pick[0] = bin - (lower ? 1 : 0);
+      s_pick[1] = before + (lower ? c0 : 0);
+    } else if (want == 0 && tid == 0) {  // none of them: nothing is above the highest key
+      s_pick[0] = digit;
+      s_pick[1] = 0;
     }
     __syncthreads();
     prefix |= (uint32_t)s_pick[0] << shift;
-    mask |= 255u << shift;
+    mask |= digit << shift;
     want -= s_pick[1];
-    __syncthreads();
   }
   // entries above the threshold stay, and the first `want` equal to it
-  const int per = (L + kSel - 1) / kSel * 32, t0 = w * per, t1 = min(t0 + per, L);
-  int ties = 0;
-  for (int c = t0; c < t1; c += 32)
-    ties += __popc(__ballot_sync(~0u, c + lane < min(t1, old) && evict_key(wt[c + lane]) == prefix));
-  int all;
+  const unsigned below = (1u << lane) - 1;
+  int ties = 0, all;
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    ties += __popc(__ballot_sync(~0u, t0 + 32 * i < old && evict_key(x[i]) == prefix));
   int tie = warp_prefix(ties, s_w, &all);
-  const int tie0 = tie;
-  auto stays = [&](int t, float x, int& tie_at) {
-    const uint32_t key = evict_key(x);
-    const bool in = t < t1 && t < old, eq = in && key == prefix;
-    const unsigned m = __ballot_sync(~0u, eq);
-    const bool yes = (in && key > prefix) || (eq && tie_at + __popc(m & ((1u << lane) - 1)) < want) ||
-                     (t < t1 && t >= old);
-    tie_at += __popc(m);
-    return yes;
-  };
+  uint32_t stay[(E + 31) / 32] = {};
   int n = 0;
-  for (int c = t0; c < t1; c += 32)
-    n += __popc(__ballot_sync(~0u, stays(c + lane, c + lane < t1 ? wt[c + lane] : 0.f, tie)));
-  int j = warp_prefix(n, s_w, &all);
-  // old positions first, then the weights by them: a weight is read before its
-  // place is written
-  tie = tie0;
-  for (int c = t0; c < t1; c += 32) {
-    const bool yes = stays(c + lane, c + lane < t1 ? wt[c + lane] : 0.f, tie);
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int t = t0 + 32 * i;
+    const uint32_t key = evict_key(x[i]);
+    const bool eq = t < old && key == prefix;
+    const unsigned m = __ballot_sync(~0u, eq);
+    const bool yes = t < L && (t >= old || key > prefix || (eq && tie + __popc(m & below) < want));
+    tie += __popc(m);
+    if (yes) stay[i / 32] |= 1u << (i % 32);
+    n += __popc(__ballot_sync(~0u, yes));
+  }
+  int j = warp_prefix(n, s_w, &all), first = keep;
+  // (every weight is in a register by now: their places can be written)
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const bool yes = (stay[i / 32] >> (i % 32)) & 1;
     const unsigned m = __ballot_sync(~0u, yes);
-    if (yes) at[j + __popc(m & ((1u << lane) - 1))] = (uint16_t)(c + lane);
+    const int to = j + __popc(m & below);
+    if (yes) {
+      at[to] = (uint16_t)(t0 + 32 * i);
+      wt[to] = x[i];
+      if (to != t0 + 32 * i) first = min(first, to);
+    }
     j += __popc(m);
   }
-  __syncthreads();
   if (tid == 0) s_pick[0] = keep;
   __syncthreads();
-  for (int c = 0; c < keep; c += kSel) {
-    const bool in = c + tid < keep;
-    const int from = in ? at[c + tid] : 0;
-    const float x = in ? wt[from] : 0.f;
-    __syncthreads();
-    if (in) wt[c + tid] = x;
-    if (in && from != c + tid) atomicMin(&s_pick[0], c + tid);
-    __syncthreads();
-  }
+  if (first < keep) atomicMin(&s_pick[0], first);
+  __syncthreads();
   if (tid == 0) a.first[unit] = s_pick[0] < keep ? s_pick[0] : -1;
 }
 
+// (and the new lengths: nothing after the selection reads the old ones)
+constexpr int kMove = 256, kSteps = 8;  // threads, entries of a thread in a tile
 template <int D>
-__global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ EvictArgs a) {
-  constexpr int C = D / 8, T = 256 / C;  // 16-byte pieces of an entry, entries of a tile
+__global__ void __launch_bounds__(kMove) evict_move_kernel(const __grid_constant__ EvictArgs a) {
+  constexpr int P = 8, E = kMove / P, T = E * kSteps;  // 16-byte pieces, entries of a step, of a tile
   ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
   const int unit = blockIdx.x, b = (unit / a.nkv) % a.batch, keep = a.keep[b];
-  bf16* x = (blockIdx.y ? a.v : a.k) + (size_t)unit * a.cap * D;
-  const uint16_t* at = a.at + (size_t)unit * a.cap;
-  const int first = a.first[unit], c = threadIdx.x % C;
-  if (first < 0) return;
-  for (int j0 = first; j0 < keep; j0 += T) {
-    const int j = j0 + threadIdx.x / C;
-    uint4 v;
-    if (j < keep) v = *reinterpret_cast<const uint4*>(x + (size_t)at[j] * D + 8 * c);
-    __syncthreads();
-    if (j < keep) *reinterpret_cast<uint4*>(x + (size_t)j * D + 8 * c) = v;
-    __syncthreads();
+  if (threadIdx.x == 0 && blockIdx.y == 0 && unit < a.batch * a.nkv && unit % a.nkv == 0) {
+    const int L = a.len[b];
+    if (L > keep && L <= a.cap) a.len[b] = keep;
   }
-}
-
-__global__ void evict_len_kernel(const __grid_constant__ EvictArgs a) {
-  ptx::griddep_wait();
-  const int b = threadIdx.x;
-  if (b < a.batch && a.len[b] > a.keep[b] && a.len[b] <= a.cap) a.len[b] = a.keep[b];
+  const int first = a.first[unit];
+  if (first < 0) return;
+  constexpr int kSlices = D / 64;
+  bf16* x = (blockIdx.y >= kSlices ? a.v : a.k) + (size_t)unit * a.cap * D + (blockIdx.y % kSlices) * 64 +
+            (threadIdx.x % P) * 8;
+  const uint16_t* at = a.at + (size_t)unit * a.cap;
+  const int e0 = threadIdx.x / P;
+  uint4 v[kSteps];
+  int from[kSteps];
+  auto places = [&](int j0) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int j = j0 + s * E + e0;
+      from[s] = j < keep ? at[j] : -1;
+    }
+  };
+  auto read = [&]() {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      if (from[s] >= 0) v[s] = *reinterpret_cast<const uint4*>(x + (size_t)from[s] * D);
+  };
+  places(first);
+  read();
+  for (int j0 = first; j0 < keep; j0 += T) {
+    uint4 w[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) w[s] = v[s];
+    places(j0 + T);
+    read();
+    __syncthreads();  // every thread has read this tile
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int j = j0 + s * E + e0;
+      if (j < keep) *reinterpret_cast<uint4*>(x + (size_t)j * D) = w[s];
+    }
+  }
 }
 
 }  // namespace
@@ -160,12 +212,13 @@ void cache_evict_carve(EvictArgs& a, int64_t units, void* workspace) {
 
 cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, cudaStream_t st) {
   const unsigned units = (unsigned)(a.n_layers * a.batch * a.nkv);
-  cudaError_t e = launch_pdl(evict_select_kernel, dim3(units), dim3(kSel), 0, st, 1, a);
+  const cudaError_t e =
+      a.cap <= 4 * kSel    ? launch_pdl(evict_select_kernel<4>, dim3(units), dim3(kSel), 0, st, 1, a)
+      : a.cap <= 16 * kSel ? launch_pdl(evict_select_kernel<16>, dim3(units), dim3(kSel), 0, st, 1, a)
+                           : launch_pdl(evict_select_kernel<64>, dim3(units), dim3(kSel), 0, st, 1, a);
   if (e != cudaSuccess) return e;
-  e = head_dim == 128 ? launch_pdl(evict_move_kernel<128>, dim3(units, 2), dim3(256), 0, st, 1, a)
-                      : launch_pdl(evict_move_kernel<64>, dim3(units, 2), dim3(256), 0, st, 1, a);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(evict_len_kernel, dim3(1), dim3(kMaxBatch), 0, st, 1, a);
+  return head_dim == 128 ? launch_pdl(evict_move_kernel<128>, dim3(units, 4), dim3(kMove), 0, st, 1, a)
+                         : launch_pdl(evict_move_kernel<64>, dim3(units, 2), dim3(kMove), 0, st, 1, a);
 }
 
 }  // namespace as2d

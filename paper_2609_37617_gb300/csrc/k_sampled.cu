@@ -1,11 +1,5 @@
 // k_sampled.cu -- probabilities at a temperature (as2d_token_probs) and the
 // acceptance of drafted tokens from given random numbers (as2d_accept_sampled).
-//
-// probs_kernel, one CTA per row: p_v = e^((x_v - max x) / T) / sum, in three
-// passes over the row.
-// accept_kernel, one CTA per request: the candidates' tests, then the sum of the
-// weights max(p_n - q_n, 0) in chunks of a thread each, the chunk that holds the
-// border u_k total, and the token within it.
 #include "ops.h"
 #include "ptx_sm100.cuh"
 #include "small_dev.cuh"
@@ -13,126 +7,378 @@
 namespace as2d {
 namespace {
 
-template <int N>
-__device__ __forceinline__ float block_max(float v, float* s) {
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-  __syncthreads();
-  for (int i = 0; i < N / 32; ++i) v = fmaxf(v, s[i]);
-  return v;
-}
-template <int N>
-__device__ __forceinline__ float block_sum(float v, float* s) {
-  v = warp_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = 0.f;
-  for (int i = 0; i < N / 32; ++i) v += s[i];
-  return v;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-__global__ void __launch_bounds__(1024) probs_kernel(const float* logits, int vocab, float c, float* probs) {
-  __shared__ float s[32];
+// ---- probabilities -----------------------------------------------------------
+//
+// p_v = e^((x_v - max x) / T) / sum: bound by memory, each value read and written
+// once.  A cluster of CTAs per row, a slice of it in the registers of each: the
+// slice's maximum m_c, e^((x - m_c) / T) and their sum, then one exchange of
+// (m_c, sum) through distributed shared memory and the factor that is left.
+// Slices that the registers do not hold (kHeld values a thread) are read again.
+// VEC: rows in pieces of 16 bytes.
+
+constexpr int kHeld = 24;
+
+__device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
+  // (maximum, sum relative to it); -inf: nothing there
+  const float M = fmaxf(a.x, b.x);
+  const float wa = a.x == -INFINITY ? 0.f : ex2((a.x - M) * c), wb = b.x == -INFINITY ? 0.f : ex2((b.x - M) * c);
+  return make_float2(M, a.y * wa + b.y * wb);
+}
+
+template <bool VEC>
+__global__ void __launch_bounds__(kThreads) probs_kernel(const float* logits, int vocab, int slice, float c,
+                                                         float* probs) {
+  constexpr int W = VEC ? 4 : 1, R = kHeld / W;
+  __shared__ float s_red[kWarps];
+  __shared__ float2 s_part[16];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = ptx::cluster_rank(), ranks = gridDim.x;
+  const int v0 = min((int)rank * slice, vocab), n = (min(v0 + slice, vocab) - v0) / W;  // pieces
+  const float* x = logits + (size_t)blockIdx.y * vocab + v0;
+  float* p = probs + (size_t)blockIdx.y * vocab + v0;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  const float* x = logits + (size_t)blockIdx.x * vocab;
-  float* p = probs + (size_t)blockIdx.x * vocab;
-  float m = -INFINITY, bad = 0.f;
-  for (int v = threadIdx.x; v < vocab; v += 1024) {
-    m = fmaxf(m, x[v]);
-    if (x[v] != x[v]) bad = 1.f;
+  float v[R][W];
+  auto load = [&](int i, float (&to)[W]) {
+    if constexpr (VEC) {
+      const float4 t = __ldcs(reinterpret_cast<const float4*>(x) + i);
+      to[0] = t.x, to[1] = t.y, to[2] = t.z, to[3] = t.w;
+    } else {
+      to[0] = __ldcs(x + i);
+    }
+  };
+  auto store = [&](int i, const float (&from)[W]) {
+    if constexpr (VEC)
+      __stcs(reinterpret_cast<float4*>(p) + i, make_float4(from[0], from[1], from[2], from[3]));
+    else
+      __stcs(p + i, from[0]);
+  };
+  float m = -INFINITY;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int i = r * kThreads + tid;
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[r][e] = -INFINITY;
+    if (i < n) load(i, v[r]);
   }
-  m = block_max<1024>(m, s);
-  if (block_max<1024>(bad, s) != 0.f) m = NAN;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int e = 0; e < W; ++e) m = fmaxf(m, v[r][e]);
+  for (int i = R * kThreads + tid; i < n; i += kThreads) {
+    float t[W];
+    load(i, t);
+#pragma unroll
+    for (int e = 0; e < W; ++e) m = fmaxf(m, t[e]);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+  if (lane == 0) s_red[warp] = m;
+  __syncthreads();
+  m = s_red[lane % kWarps];
+#pragma unroll
+  for (int o = kWarps / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+  const float ref = m == -INFINITY ? 0.f : m;  // (e^-inf = 0; NaN passes the maximum by and reaches the sum)
   float l = 0.f;
-  const float ref = m == -INFINITY ? 0.f : m;
-  for (int v = threadIdx.x; v < vocab; v += 1024) l += exp2f((x[v] - ref) * c);
-  l = block_sum<1024>(l, s);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int v = threadIdx.x; v < vocab; v += 1024) p[v] = exp2f((x[v] - ref) * c) * inv;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      v[r][e] = ex2((v[r][e] - ref) * c);
+      l += v[r][e];
+    }
+  for (int i = R * kThreads + tid; i < n; i += kThreads) {
+    float t[W];
+    load(i, t);
+#pragma unroll
+    for (int e = 0; e < W; ++e) l += ex2((t[e] - ref) * c);
+  }
+  l = warp_sum(l);
+  __syncthreads();
+  if (lane == 0) s_red[warp] = l;
+  __syncthreads();
+  l = s_red[lane % kWarps];
+#pragma unroll
+  for (int o = kWarps / 2; o > 0; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
+  float2 all = make_float2(m, l);
+  if (ranks > 1) {
+    if (tid < (int)ranks) {
+      const uint32_t to = ptx::dsmem_map(ptx::smem_u32(&s_part[rank]), tid);
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m), "f"(l) : "memory");
+    }
+    ptx::cluster_sync();
+    all = s_part[0];
+    for (uint32_t r = 1; r < ranks; ++r) all = join(all, s_part[r], c);
+  }
+  const float f = m == -INFINITY && all.y == 0.f ? 0.f : (m == -INFINITY ? 1.f : ex2((m - all.x) * c)) / all.y;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int i = r * kThreads + tid;
+#pragma unroll
+    for (int e = 0; e < W; ++e) v[r][e] *= f;
+    if (i < n) store(i, v[r]);
+  }
+  for (int i = R * kThreads + tid; i < n; i += kThreads) {
+    float t[W];
+    load(i, t);
+#pragma unroll
+    for (int e = 0; e < W; ++e) t[e] = ex2((t[e] - ref) * c) * f;
+    store(i, t);
+  }
 }
 
-__global__ void __launch_bounds__(1024) accept_sampled_kernel(const __grid_constant__ SampledArgs a) {
-  __shared__ double s_sum[1024];
-  __shared__ int s_n, s_chunk, s_any;
+// ---- acceptance ------------------------------------------------------------------
+//
+// A cluster of CTAs per request.  Each finds n from the candidates' tests (one
+// gather), then sums its slice of row n's weights w_v = max(p_v - q_v, 0): the
+// slice lies in shared memory and a thread adds a contiguous chunk of it, each
+// difference exactly (as the sum of two floats, Knuth's two-sum) and the sum in
+// two floats, so that the border u total falls between the same two tokens as in
+// 64 bits but for differences of some 2^-48.  The first warp adds the threads' sums
+// in 64 bits (the whole block's additions in 64 bits would take 3 us), the CTAs
+// exchange their totals, and the first warp of the one that holds the border
+// finds the chunk and the token within it.  Bound by latency for a few requests
+// (three dependent round trips to memory), by memory for many.
+
+// a + b = s + e exactly.
+__device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {
+  s = a + b;
+  const float t = s - a;
+  e = (a - (s - t)) + (b - t);
+}
+
+constexpr int kMostChunk = 53;   // values of a thread's chunk at most: two rows of a slice fit shared memory
+constexpr int kMostPieces = 128; // pieces of a slice that shared memory holds one after another
+
+__global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_constant__ SampledArgs a, int chunk,
+                                                                  int pieces) {
+  extern __shared__ float s_row[];  // [512 chunks] p, then q
+  __shared__ float2 s_sum[kThreads];
+  __shared__ double s_part[2][16], s_piece[kMostPieces];
+  __shared__ int s_n;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int b = blockIdx.y, ranks = gridDim.x, rank = (int)ptx::cluster_rank();
+  const int r0 = a.start[b], k = a.start[b + 1] - r0 - 1, c0 = r0 - b;
+  const size_t V = a.vocab;
+  const int piece = chunk * kThreads;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  const int b = blockIdx.x, r0 = a.start[b], k = a.start[b + 1] - r0 - 1, c0 = r0 - b, tid = threadIdx.x;
-  const size_t V = a.vocab;
-  if (tid < 32) {
+  if (warp == 0) {
     bool stands = false;
-    if (tid < k) {
-      const int c = a.cand[c0 + tid];
+    if (lane < k) {
+      const int c = a.cand[c0 + lane];
       if (c >= 0 && c < a.vocab) {
-        const double q = a.draft ? (double)a.draft[(size_t)(c0 + tid) * V + c] : 1.0;
-        stands = (double)a.u[r0 + tid] * q < (double)a.probs[(size_t)(r0 + tid) * V + c];
+        const double q = a.draft ? (double)a.draft[(size_t)(c0 + lane) * V + c] : 1.0;
+        stands = (double)a.u[r0 + lane] * q < (double)a.probs[(size_t)(r0 + lane) * V + c];
       }
     }
     const unsigned m = __ballot_sync(~0u, stands);
-    if (tid == 0) s_n = __ffs(~m) - 1;
+    if (lane == 0) s_n = __ffs(~m) - 1;
   }
   __syncthreads();
   const int n = s_n, gone = n < k && !a.draft ? a.cand[c0 + n] : -1;
   const float* p = a.probs + (size_t)(r0 + n) * V;
   const float* q = n < k && a.draft ? a.draft + (size_t)(c0 + n) * V : nullptr;
-  const int per = (a.vocab + 1023) / 1024;
-  const double u = a.u[r0 + k];
-  int token = -1;
-  for (int plain = n < k ? 0 : 1; plain < 2 && token < 0; ++plain) {
-    auto weight = [&](int v) -> double {
-      double x = p[v];
-      if (!plain) x = q ? x - (double)q[v] : (v == gone ? 0.0 : x);
-      return x > 0.0 ? x : 0.0;
-    };
-    const int v0 = min(tid * per, a.vocab), v1 = min(v0 + per, a.vocab);
-    double sum = 0.0;
-    for (int v = v0; v < v1; ++v) sum += weight(v);
+  // (within [0, 1): the border is below the total)
+  const double u = fminf(fmaxf(a.u[r0 + k], 0.f), 0x1.fffffep-1f);
+  float *sp = s_row, *sq = s_row + piece;
+
+  auto weight = [&](int j, bool less, float& hi, float& lo) {
+    hi = sp[j], lo = 0.f;
+    if (less) two_sum(hi, -sq[j], hi, lo);
+    if (!(hi > 0.f && hi < INFINITY)) hi = lo = 0.f;
+  };
+  // Piece i of the slice into shared memory and the threads' sums into s_sum;
+  // returns its first token.
+  auto stage = [&](int i, bool plain) {
+    const int v0 = (int)min((long long)(rank * pieces + i) * piece, (long long)a.vocab), len = min(piece, a.vocab - v0);
+    const bool less = q && !plain;
+    constexpr int U = 10;
     __syncthreads();
-    s_sum[tid] = sum;
-    if (tid == 0) s_chunk = -1;
-    __syncthreads();
-    if (tid == 0) {
-      double total = 0.0, at = 0.0;
-      for (int i = 0; i < 1024; ++i) total += s_sum[i];
-      const double border = u * total;
-      int pick = -1;
-      for (int i = 0; i < 1024; ++i) {
-        if (s_sum[i] > 0.0) pick = i;
-        if (at + s_sum[i] > border) break;
-        at += s_sum[i];
-      }
-      if (pick >= 0) {
-        at = 0.0;
-        for (int i = 0; i < pick; ++i) at += s_sum[i];
-        for (int v = pick * per; v < min((pick + 1) * per, a.vocab); ++v) {
-          const double x = weight(v);
-          if (x > 0.0) s_chunk = v;
-          if (at + x > border) break;
-          at += x;
+    for (int j0 = tid; j0 < len; j0 += U * kThreads) {
+      float x[U], y[U];
+#pragma unroll
+      for (int t = 0; t < U; ++t)
+        if (j0 + t * kThreads < len) {
+          x[t] = __ldcs(p + v0 + j0 + t * kThreads);
+          if (less) y[t] = __ldcs(q + v0 + j0 + t * kThreads);
+        }
+#pragma unroll
+      for (int t = 0; t < U; ++t) {
+        const int j = j0 + t * kThreads;
+        if (j < len) {
+          sp[j] = !plain && v0 + j == gone ? 0.f : x[t];
+          if (less) sq[j] = y[t];
         }
       }
     }
     __syncthreads();
-    token = s_chunk;
-  }
-  if (tid == 0) {
+    float s = 0.f, e = 0.f;
+    for (int j = tid * chunk; j < min((tid + 1) * chunk, len); ++j) {
+      float hi, lo, t;
+      weight(j, less, hi, lo);
+      two_sum(s, hi, s, t);
+      e += t + lo;
+    }
+    s_sum[tid] = make_float2(s, e);
+    __syncthreads();
+    return v0;
+  };
+  // First warp: the sum of a lane's 16 threads and of those before them.
+  constexpr int kPer = kThreads / 32;
+  auto lane_sums = [&](double& sum, double& upto) {
+    sum = 0.0;
+    for (int i = 0; i < kPer; ++i) sum += (double)s_sum[lane * kPer + i].x + (double)s_sum[lane * kPer + i].y;
+    upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double t = __shfl_up_sync(~0u, upto, o);
+      if (lane >= o) upto += t;
+    }
+  };
+  for (int plain = n < k ? 0 : 1; plain < 2; ++plain) {
+    const bool less = q && !plain;
+    double mine = 0.0, sum = 0.0, upto = 0.0;
+    int v0 = 0;
+    for (int i = 0; i < pieces; ++i) {
+      v0 = stage(i, plain);
+      if (warp == 0) {
+        lane_sums(sum, upto);
+        const double t = __shfl_sync(~0u, upto, 31);
+        if (lane == 0) s_piece[i] = t;
+        mine += t;
+      }
+    }
+    if (tid < ranks) {
+      const uint32_t to = ptx::dsmem_map(ptx::smem_u32(&s_part[plain][rank]), tid);
+      asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(mine) : "memory");
+    }
+    ptx::cluster_sync();
+    double total = 0.0, before = 0.0, next = 0.0;
+    int last = -1;  // the last slice that holds anything
+    for (int r = 0; r < ranks; ++r) {
+      const double t = s_part[plain][r];
+      if (r == rank) before = total;
+      total += t;
+      if (r == rank) next = total;
+      if (t > 0.0) last = r;
+    }
+    if (last < 0) continue;  // nothing: once more without q
+    const double border = u * total;
+    // the slice whose sums the border lies between (the last one that holds
+    // anything, beyond rounding)
+    if (rank == last ? border < before : !(before <= border && border < next)) return;
+    double base = before;
+    if (pieces > 1) {
+      int pick = -1;
+      double at = before, t = before;
+      for (int i = 0; i < pieces; ++i) {
+        if (s_piece[i] > 0.0) {
+          pick = i, at = t;
+          if (border < t + s_piece[i]) break;
+        }
+        t += s_piece[i];
+      }
+      base = at;
+      v0 = stage(pick, plain);
+      if (warp == 0) lane_sums(sum, upto);
+    }
+    if (warp != 0) return;
+    // the first lane, of its chunks the first, of that chunk's values the first
+    // whose sums pass the border; else the last that holds anything
+    const unsigned over = __ballot_sync(~0u, sum > 0.0 && border < base + upto), any = __ballot_sync(~0u, sum > 0.0);
+    if (lane != (over ? __ffs(over) - 1 : 31 - __clz(any))) return;
+    double at = base + (upto - sum), t = at;
+    int pick = 0;
+    for (int i = 0; i < kPer; ++i) {
+      const double w = (double)s_sum[lane * kPer + i].x + (double)s_sum[lane * kPer + i].y;
+      if (w > 0.0) {
+        pick = lane * kPer + i, at = t;
+        if (border < t + w) break;
+      }
+      t += w;
+    }
+    int token = -1;
+    const int end = min((pick + 1) * chunk, a.vocab - v0);
+    for (int j = pick * chunk; j < end; ++j) {
+      float hi, lo;
+      weight(j, less, hi, lo);
+      if (hi > 0.f) {
+        token = v0 + j;
+        at += (double)hi + (double)lo;
+        if (border < at) break;
+      }
+    }
     a.n_out[b] = n;
     a.token_out[b] = token;
+    return;
   }
+  if (rank == 0 && tid == 0) {
+    a.n_out[b] = n;
+    a.token_out[b] = -1;
+  }
+}
+
+cudaError_t cluster_attrs(const void* kernel, int smem) {
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  return e != cudaSuccess || smem == 0
+             ? e
+             : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
 }
 
 }  // namespace
 
 cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float temperature, float* probs,
                                cudaStream_t st) {
-  return launch_pdl(probs_kernel, dim3(rows), dim3(1024), 0, st, 1, logits, vocab,
-                    (float)(1.4426950408889634 / temperature), probs);
+  static const cudaError_t attr = [] {
+    const cudaError_t e = cluster_attrs((const void*)probs_kernel<true>, 0);
+    return e != cudaSuccess ? e : cluster_attrs((const void*)probs_kernel<false>, 0);
+  }();
+  if (attr != cudaSuccess) return attr;
+  // CTAs per row: as many as hold it in registers, twice as many (up to 16) while
+  // all of them run at once and a slice is no smaller than 2048 values
+  int ranks = 1;
+  while (ranks < 16 && (ranks * kThreads * kHeld < vocab ||
+                        (ranks * 4096 <= vocab && (int64_t)rows * 2 * ranks <= device_sms())))
+    ranks *= 2;
+  const bool vec = vocab % 4 == 0 && ((uintptr_t)logits | (uintptr_t)probs) % 16 == 0;
+  const int slice = ((vocab + ranks - 1) / ranks + 3) / 4 * 4;
+  const float c = (float)(1.4426950408889634 / temperature);
+  for (int r0 = 0; r0 < rows; r0 += 65535) {  // (a grid's rows)
+    const int n = rows - r0 < 65535 ? rows - r0 : 65535;
+    const float* x = logits + (size_t)r0 * vocab;
+    float* p = probs + (size_t)r0 * vocab;
+    const cudaError_t e =
+        vec ? launch_pdl(probs_kernel<true>, dim3(ranks, n), dim3(kThreads), 0, st, ranks, x, vocab, slice, c, p)
+            : launch_pdl(probs_kernel<false>, dim3(ranks, n), dim3(kThreads), 0, st, ranks, x, vocab, slice, c, p);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 cudaError_t launch_accept_sampled(const SampledArgs& a, cudaStream_t st) {
-  return launch_pdl(accept_sampled_kernel, dim3(a.batch), dim3(1024), 0, st, 1, a);
+  constexpr int kSmem = 2 * kMostChunk * kThreads * 4;
+  static const cudaError_t attr = cluster_attrs((const void*)accept_sampled_kernel, kSmem);
+  if (attr != cudaSuccess) return attr;
+  // 16 CTAs a request while all of them run at once, else 8
+  const int ranks = a.batch * 16 <= device_sms() ? 16 : 8;
+  const int slice = (a.vocab + ranks - 1) / ranks;
+  // (odd chunks: the threads' chunks start in different banks)
+  int chunk = (slice + kThreads - 1) / kThreads | 1, pieces = 1;
+  if (chunk > kMostChunk) {
+    chunk = kMostChunk;
+    pieces = (slice + chunk * kThreads - 1) / (chunk * kThreads);
+  }
+  const size_t smem = (size_t)(a.draft ? 2 : 1) * chunk * kThreads * 4;
+  return launch_pdl(accept_sampled_kernel, dim3(ranks, a.batch), dim3(kThreads), smem, st, ranks, a, chunk, pieces);
 }
 
 }  // namespace as2d

@@ -34,12 +34,11 @@
 #include "ops.h"
 #include "ptx_sm100.cuh"
 #include "small_dev.cuh"
-#include "tree_plan.cuh"
+#include "tree_dev.cuh"
 
 namespace as2d {
 namespace {
 
-constexpr uint32_t kRegion = 128 * 128;  // 64 columns of 128 rows, bytes
 constexpr int kThreads = 640;
 // P may grow to 2^kLazy before the accumulator is rescaled.
 constexpr float kLazy = 8.f;
@@ -56,42 +55,14 @@ struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;            // one K or V tile
   static constexpr uint32_t Q = (F32 ? 2 : 1) * 128 * D * 2;  // hi (and lo) image
   static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
-  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 11) * 8 + 8 + 16;
+  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16;
   static_assert(SMEM + sizeof(UnitPlan) <= 232448, "shared memory of one CTA");
 };
-
-// Byte offset of the 16-byte chunk j (of a row's D / 8) of row r in a 128-row
-// operand image of 128-byte-swizzled K-major bf16.
-__device__ __forceinline__ uint32_t chunk_off(int r, int j) {
-  return (uint32_t)(j >> 3) * kRegion + (uint32_t)r * 128u + (uint32_t)(((j & 7) ^ (r & 7)) << 4);
-}
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 // The weight of a part (maximum m) beside a maximum M: 0 where the part holds
 // nothing that the row sees.
 __device__ __forceinline__ float part_weight(float m, float M) {
   return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
-}
-
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&t);
-}
-// hi = bf16(x), lo = bf16(x - hi) of two numbers.
-__device__ __forceinline__ void hi_lo(float a, float b, uint32_t& h, uint32_t& l) {
-  h = pack2(a, b);
-  l = pack2(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xFFFF0000u));
-}
-
-// The visible rows of row r of a request, as a mask of its `rows` rows.
-__device__ __forceinline__ uint64_t visible_rows(const TreeArgs& a, int r, int i, int rows) {
-  const uint64_t all = ~0ull >> (64 - rows);
-  return (a.visible ? a.visible[r] : ~0ull >> (63 - i)) & all;
 }
 
 // Which of keys [p0, p0 + 32) a row sees.
@@ -107,63 +78,6 @@ __device__ __forceinline__ void mask_scores(uint32_t (&v)[N], uint32_t bits) {
 #pragma unroll
   for (int e = 0; e < N; ++e)
     if (!((bits >> e) & 1)) v[e] = 0xFF800000u;  // -inf
-}
-
-// The ring's next stage and its parity, as slot | parity << 8.
-struct Stage {
-  uint32_t x = 0;
-  template <int NST>
-  __device__ __forceinline__ uint32_t next() {
-    const uint32_t now = x;
-    x = (now & 255u) + 1 == NST ? (now & 256u) ^ 256u : now + 1;
-    return now;
-  }
-  static __device__ __forceinline__ uint32_t slot(uint32_t x) { return x & 255u; }
-  static __device__ __forceinline__ uint32_t parity(uint32_t x) { return x >> 8; }
-};
-
-// The queries of an item into the operand image(s), by 64 threads; rows past the
-// item's queries are left as they are (what they hold reaches no other row).
-template <int D, bool F32>
-__device__ __forceinline__ void load_queries(const TreeArgs& a, const Unit& it, int tid, uint8_t* img) {
-  constexpr int C = D / 8, B = 8;  // chunks of a row, loads in flight
-  const int G = a.nq / a.nkv, n0 = it.qt * 128;
-  const int n = min(128, it.rows * G - n0) * C;
-  for (int c0 = tid; c0 < n; c0 += 64 * B) {
-    uint4 v[B][F32 ? 2 : 1];
-#pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const int c = c0 + 64 * u;
-      if (c < n) {
-        const int q = n0 + c / C, i = q / G, h = it.g * G + (q - i * G);
-        const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + 8 * (c % C);
-        if (F32) {
-          const uint4* s = reinterpret_cast<const uint4*>((const float*)a.q + at);
-          v[u][0] = s[0];
-          v[u][F32 ? 1 : 0] = s[1];
-        } else {
-          v[u][0] = *reinterpret_cast<const uint4*>((const bf16*)a.q + at);
-        }
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const int c = c0 + 64 * u;
-      if (c < n) {
-        uint8_t* to = img + chunk_off(c / C, c % C);
-        if (F32) {
-          const float* x = reinterpret_cast<const float*>(&v[u][0]);
-          uint32_t h[4], l[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) hi_lo(x[2 * e], x[2 * e + 1], h[e], l[e]);
-          *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(to + 128 * D * 2) = make_uint4(l[0], l[1], l[2], l[3]);
-        } else {
-          *reinterpret_cast<uint4*>(to) = v[u][0];
-        }
-      }
-    }
-  }
 }
 
 // A value tile that holds entries from L on, before it is multiplied: entries
@@ -198,9 +112,9 @@ __device__ __forceinline__ void clean_tile(uint8_t* v, int p0, int L, int kend, 
 }
 
 // N consecutive results x inv at element `at` of the output.
-template <int N>
+template <int N, bool F32>
 __device__ __forceinline__ void write_out(const TreeArgs& a, const float* x, float inv, size_t at) {
-  if (a.q_f32) {
+  if (F32) {
     float* out = (float*)a.out + at;
 #pragma unroll
     for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(out + e) = make_float2(x[e] * inv, x[e + 1] * inv);
@@ -235,7 +149,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* o_full = v_clean + 2;
   uint64_t* o_empty = o_full + 1;
   uint64_t* drain = o_empty + 1;
-  unsigned long long* s_bad = reinterpret_cast<unsigned long long*>(drain + 1);
+  uint64_t* q_first = drain + 1;  // in q_full's place for the CTA's first item
+  unsigned long long* s_bad = reinterpret_cast<unsigned long long*>(q_first + 1);
   uint32_t* tslot = reinterpret_cast<uint32_t*>(s_bad + 1);
   __shared__ UnitPlan s_plan;
   const UnitPlan* plan = &s_plan;
@@ -247,7 +162,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(&empty[i], 1);
       ptx::mbar_init(&tail_full[i], 1);
     }
-    ptx::mbar_init(q_full, 64);
+    ptx::mbar_init(q_first, (kThreads - 64) / 32);
+    ptx::mbar_init(q_full, 2);
     ptx::mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&s_full[i], 1);
@@ -273,6 +189,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tslot;
   int u0, u1;
   unit_range(*plan, a, blockIdx.x, gridDim.x, whole, u0, u1);
+  if (warp >= 2 && u0 < u1) {
+    // the first item's queries, by every warp that has nothing to do yet (by two
+    // warps 32-bit queries of 119 rows took 5 us)
+    load_queries<D, F32, kThreads - 64, 4>(a, unit_at(*plan, a, u0, u1), tid - 64, qimg);
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(q_first);
+  }
   // every wait is bounded; a role that gives up flags the call and waits for
   // nothing more, so that all of them come to the end
   const unsigned long long limit = a.timeout_ns;
@@ -332,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int u = u0; u < u1 && ok; ++items) {
         const Unit it = unit_at(*plan, a, u, u1);
         const int cnt = it.t1 - it.t0, first_tail = it.L / 128 - it.t0;
-        wait(q_full, items & 1);
+        items == 0 ? wait(q_first, 0) : wait(q_full, (items - 1) & 1);
         for (int j = 0; j <= cnt && ok; ++j) {
           const uint32_t v_before = v;
           if (j < cnt) {
@@ -397,10 +321,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t n = 0, items = 0, turn = 0;
     for (int u = u0; u < u1; ++items) {
       const Unit it = unit_at(*plan, a, u, u1);
-      if (items > 0) wait(q_empty, (items - 1) & 1);
-      if (ok) load_queries<D, F32>(a, it, t64, qimg);
-      ptx::fence_proxy_async_smem();
-      ptx::mbar_arrive(q_full);
+      if (items > 0) {
+        wait(q_empty, (items - 1) & 1);
+        if (ok) load_queries<D, F32, 64, 8>(a, it, t64, qimg);
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(q_full);
+      }
       const int first = it.L / 128;
       // the epilogue of the item before has read what was noted for it
       if (items > 0) wait(o_empty, (items - 1) & 1);
@@ -568,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e) dst[e * 128] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           } else if (live) {
-            write_out<16>(a, o, inv, ((size_t)(it.r0 + i) * a.nq + h) * D + d0);
+            write_out<16, F32>(a, o, inv, ((size_t)(it.r0 + i) * a.nq + h) * D + d0);
           }
           __syncwarp();
         }
@@ -594,13 +521,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 // four dims, a warp over 32 queries (16 bytes each side by side in a part), eight
 // parts in flight.
 constexpr int kCombineQuads = 8;  // of a CTA: its warps
-template <int D>
+template <int D, bool F32>
 __global__ void __launch_bounds__(32 * kCombineQuads)
     tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas) {
   constexpr int U = 8;
   __shared__ UnitPlan plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  ptx::griddep_wait();
+  // The lengths before the wait: the products' kernel let this one start after
+  // its own wait, so what ran before that kernel is done, and it writes none.
   ptx::griddep_launch_dependents();
   if (warp == 0) make_plan(a, 128, lane, plan, false);
   __syncthreads();
@@ -612,6 +540,7 @@ __global__ void __launch_bounds__(32 * kCombineQuads)
   const int G = a.nq / a.nkv, row = 32 * blockIdx.y + lane, q = it.qt * 128 + row;
   if (q >= it.rows * G) return;
   const int n = c1 - c0 + 1, quad = kCombineQuads * blockIdx.z + warp;
+  ptx::griddep_wait();
   auto part = [&](int k) { return (size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0); };
   float M = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
   for (int k = U; k < n; ++k) M = fmaxf(M, __ldcg(&ws.ml[part(k) * 128 + row]).x);
@@ -643,7 +572,7 @@ __global__ void __launch_bounds__(32 * kCombineQuads)
       }
   }
   const int i = q / G, h = it.g * G + (q - i * G);
-  write_out<4>(a, x, l == 0.f ? 0.f : 1.f / l, ((size_t)(it.r0 + i) * a.nq + h) * D + 4 * quad);
+  write_out<4, F32>(a, x, l == 0.f ? 0.f : 1.f / l, ((size_t)(it.r0 + i) * a.nq + h) * D + 4 * quad);
   if (quad == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, l);
 }
 
@@ -664,9 +593,11 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                                    (int)whole);
   if (e != cudaSuccess || whole) return e;
-  return launch_pdl(tree_combine_kernel<D>, dim3((unsigned)items, (most_queries + 31) / 32, D / 4 / kCombineQuads),
+  return launch_pdl(tree_combine_kernel<D, F32>, dim3((unsigned)items, (most_queries + 31) / 32, D / 4 / kCombineQuads),
                     dim3(32 * kCombineQuads), 0, st, 1, a, ws, ctas);
 }
+
+}  // namespace
 
 int device_sms() {
   int dev = 0, n = 0;
@@ -676,7 +607,13 @@ int device_sms() {
   return n;
 }
 
-}  // namespace
+int64_t tree_items(const TreeArgs& a) {
+  const int G = a.nq / a.nkv;
+  int64_t items = 0;
+  for (int b = 0; b < a.rm.batch; ++b)
+    items += (int64_t)((a.rm.start[b + 1] - a.rm.start[b]) * G + 127) / 128 * a.nkv;
+  return items;
+}
 
 size_t tree_attention_workspace(int head_dim) {
   return (size_t)device_sms() * 2 * 128 * (head_dim * 4 + 8);
@@ -685,11 +622,10 @@ size_t tree_attention_workspace(int head_dim) {
 cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
                                   cudaStream_t st) {
   const int sms = device_sms(), G = a.nq / a.nkv;
-  int64_t items = 0;
+  const int64_t items = tree_items(a);
   int most = 0;  // queries of an item
   for (int b = 0; b < a.rm.batch; ++b) {
     const int n = (a.rm.start[b + 1] - a.rm.start[b]) * G;
-    items += (int64_t)(n + 127) / 128 * a.nkv;
     if (n > most) most = n < 128 ? n : 128;
   }
   TreeWork ws;

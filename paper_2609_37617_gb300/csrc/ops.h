@@ -50,6 +50,9 @@ struct SampledArgs {
   int32_t *n_out, *token_out;
 };
 
+// SMs of the current device; (request, kv head, tile of 128 queries) items of a call.
+int device_sms();
+int64_t tree_items(const TreeArgs& a);
 cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
                                   cudaStream_t st);
 size_t tree_attention_workspace(int head_dim);

@@ -10,6 +10,8 @@ namespace {
 
 as2d_status invalid(const char* msg) { return report_error(AS2D_ERR_INVALID_ARG, msg); }
 
+constexpr int kMaxOpVocab = 1 << 24;
+
 bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 as2d_status launched(cudaError_t e, const char* what) {
@@ -179,6 +181,7 @@ extern "C" as2d_status as2d_token_probs(const float* logits, int32_t n_rows, int
   clear_error();
   if (n_rows < 0 || vocab < 1) return invalid("n_rows must be >= 0 and vocab >= 1");
   if (!(temperature > 0.f) || !std::isfinite(temperature)) return invalid("temperature must be finite and > 0");
+  if (vocab > kMaxOpVocab) return report_error(AS2D_ERR_UNSUPPORTED, "vocab above 2^24 is not supported");
   if (n_rows == 0) return AS2D_OK;
   if (!logits || !probs) return invalid("logits and probs are required");
   if (!aligned(logits, 4) || !aligned(probs, 4)) return invalid("logits and probs must be 4-byte aligned");
@@ -195,6 +198,7 @@ extern "C" as2d_status as2d_accept_sampled(const float* probs, const float* draf
     return invalid("probs, k, u, n_accepted and token are required");
   if (batch < 1 || batch > kMaxBatch) return invalid("batch must be in [1, AS2D_MAX_BATCH]");
   if (vocab < 1) return invalid("vocab must be >= 1");
+  if (vocab > kMaxOpVocab) return report_error(AS2D_ERR_UNSUPPORTED, "vocab above 2^24 is not supported");
   SampledArgs a{};
   a.start[0] = 0;
   for (int b = 0; b < batch; ++b) {
