@@ -52,11 +52,16 @@ typedef int32_t as2d_status;
 /* Device-side error bits (as2d_kv_check's message names them; the static
    decode step returns them through its error_bits output). */
 #define AS2D_DEVERR_BAD_TOKEN 1  /* a root or candidate id outside [0, vocab)  */
-#define AS2D_DEVERR_ROLLBACK 2   /* a rollback beyond the committed length     */
+#define AS2D_DEVERR_ROLLBACK 2   /* a rollback beyond the committed length, or
+                                    below what an eviction left               */
 #define AS2D_DEVERR_TIMEOUT 4    /* a kernel's bounded wait gave up            */
 #define AS2D_DEVERR_CAPACITY 8   /* a device-side length left no room for the
                                     call's rows (length < 0 or length + rows >
                                     capacity): that request was skipped       */
+#define AS2D_DEVERR_BAD_TREE 16  /* a candidate's parent is no earlier row of
+                                    its request                               */
+#define AS2D_DEVERR_NO_TOKEN 32  /* a row's probabilities gave no token (NaN
+                                    logits, or none above -inf)               */
 
 /* Largest number of candidates per request in one call (the budget b of
    App. A.2; physical width K = k + 1 <= 17). */
@@ -196,8 +201,9 @@ as2d_status as2d_decode_step(as2d_kv* kv, const as2d_verify_out* out,
 /* Restore each request's state to an earlier committed prefix (App. C.4,
    requirement 2): length new_len[b] and pending root new_root[b] (host int32
    [batch]).  Entries [0, new_len[b]) must be ones this state holds; a
-   new_len above the device-side length is a device error that leaves that
-   request unchanged.  Asynchronous on `stream`. */
+   new_len above the device-side length, or below the number of entries that the
+   last as2d_kv_evict left, is a device error that leaves that request
+   unchanged.  Asynchronous on `stream`. */
 as2d_status as2d_kv_rollback(as2d_kv* kv, const int32_t* new_len,
                              const int32_t* new_root, void* stream);
 
@@ -511,7 +517,8 @@ as2d_status as2d_budget_select(const double* cost_us, const int32_t* refs,
    candidates: attention of a tree of drafted tokens over a cache, the weight
    that attention gives each cache entry and eviction by it, probabilities at a
    temperature, and the acceptance of drafted tokens from given random numbers.
-   They work on the caller's tensors.
+   They work on the caller's tensors; as2d_verify_tree, as2d_verify_sampled,
+   as2d_kv_track_weights and as2d_kv_evict, further below, run them on a state.
 
    Each call is enqueued on `stream` without a host synchronisation and can be
    captured into a graph; nothing is kept from one call to the next.  A
@@ -644,6 +651,61 @@ as2d_status as2d_accept_sampled(const float* probs, const float* draft_probs,
                                 const int32_t* candidates, const int32_t* k, int32_t batch,
                                 int32_t vocab, const float* u, int32_t* n_accepted,
                                 int32_t* token, void* stream);
+
+/* ---- The same on a verification state ------------------------------------------ */
+
+/* Verify a tree of candidates per request in one pass: as as2d_verify_block, but
+   parents (device int32, packed as candidates) gives each candidate the row it
+   follows, 0 for the root and j for the request's candidate j (1 .. k_b), which
+   must be an earlier one.  A candidate stands at position L_b + its depth and
+   sees the prefix, its ancestors and itself.  From the root down, the candidate
+   that follows the last one accepted and equals the greedy token there is
+   accepted (the first, if several do); the greedy token after the last one
+   is the correction.  Afterwards the cache holds the root's and the accepted
+   candidates' entries at L_b .. L_b + n_b, as if they had been a chain.
+   out: as for as2d_verify_block, n_accepted the accepted path's length, greedy
+   and logits by row.  path: device int32 [batch][AS2D_MAX_K] or NULL: the
+   accepted candidates' numbers in order, then -1.  A parent that is no earlier
+   row is a device error (as2d_kv_check) that leaves that request unchanged with
+   n_accepted = correction = -1, its path -1.  A row's logits depend on the other rows and
+   requests of the call by the order of 32-bit sums only.  The first call
+   allocates working memory, kept until as2d_kv_free. */
+as2d_status as2d_verify_tree(as2d_kv* kv, const int32_t* candidates,
+                             const int32_t* parents, const int32_t* k,
+                             const as2d_verify_out* out, int32_t* path, void* stream);
+
+/* as2d_verify_block with sampling in the place of the greedy rule: the rows'
+   logits become probabilities at `temperature` (as2d_token_probs) and the
+   candidates are accepted and the correction drawn by as2d_accept_sampled from
+   them, draft_probs (device float [sum k][vocab] or NULL) and u (device float
+   [sum (k + 1)] in [0, 1)).  probs: device float [rows][vocab], receives the
+   probabilities.  out: as for as2d_verify_block, with logits NULL; greedy still
+   holds each row's greedy token.  A row that gives no token is a device error
+   that leaves that request unchanged with n_accepted = correction = -1. */
+as2d_status as2d_verify_sampled(as2d_kv* kv, const int32_t* candidates, const int32_t* k,
+                                const float* draft_probs, const float* u, float temperature,
+                                const as2d_verify_out* out, float* probs, void* stream);
+
+/* From now on every verification call of this state (as2d_verify_block,
+   as2d_decode_step, as2d_verify_tree, as2d_verify_sampled and what calls them)
+   adds the weight that its rows' attention gives each entry to `weights`
+   (device float [n_layers][batch][n_kv][capacity], the caller's, who fills in
+   what the entries of the prefix start with and keeps it alive), as
+   as2d_attention_weights does, over all rows of the call whether accepted or
+   not; NULL ends it.  The weights of accepted entries move with them.  These calls take the
+   attention of as2d_verify_tree, so that their logits differ from those of
+   other calls by the order of 32-bit sums.  as2d_prefill is refused meanwhile
+   (AS2D_ERR_UNSUPPORTED).  Allocates device memory on first use. */
+as2d_status as2d_kv_track_weights(as2d_kv* kv, float* weights);
+
+/* Cut every layer and kv head of each request b to the keep[b] entries
+   (host int32 [batch], >= 0) that as2d_cache_evict chooses by the tracked weights,
+   the latest `recent` among them; requests that hold no more are left alone.  The
+   length becomes keep[b]; the pending root stays, and later rows take their
+   positions as if nothing had been evicted.  Needs tracked weights
+   (AS2D_ERR_INVALID_ARG).  as2d_kv_rollback cannot go below keep[b] afterwards.
+   Asynchronous on `stream`. */
+as2d_status as2d_kv_evict(as2d_kv* kv, const int32_t* keep, int32_t recent, void* stream);
 
 /* Thread-local description of the last error ("" if none). */
 const char* as2d_last_error(void);

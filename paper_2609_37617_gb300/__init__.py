@@ -30,6 +30,8 @@ AS2D_DEVERR_BAD_TOKEN = 1
 AS2D_DEVERR_ROLLBACK = 2
 AS2D_DEVERR_TIMEOUT = 4
 AS2D_DEVERR_CAPACITY = 8
+AS2D_DEVERR_BAD_TREE = 16
+AS2D_DEVERR_NO_TOKEN = 32
 AS2D_CBUF_BATCH = 8
 CBUF_MODES = {0: "normal", 1: "realign", 2: "alone"}
 AS2D_MAX_K = 16
@@ -51,7 +53,8 @@ EXPORTED = ("as2d_model_load", "as2d_kv_init_prefilled", "as2d_verify_block",
             "as2d_cpu_decoder_reset", "as2d_cpu_decoder_free",
             "as2d_tree_attention_workspace", "as2d_tree_attention", "as2d_attention_weights",
             "as2d_cache_evict_workspace", "as2d_cache_evict", "as2d_token_probs",
-            "as2d_accept_sampled")
+            "as2d_accept_sampled", "as2d_verify_tree", "as2d_verify_sampled",
+            "as2d_kv_track_weights", "as2d_kv_evict")
 KERNEL_CLASSES = {"qkv": 0, "attention": 1, "o": 2, "gate_up": 3, "down": 4,
                   "lm_head": 5, "other": 6}
 
@@ -188,7 +191,13 @@ _lib.as2d_cache_evict_workspace.argtypes = [_CACHE, ctypes.POINTER(_I64)]
 _lib.as2d_cache_evict.argtypes = [_CACHE, _P, _P, _P, _S, _P, _I64, _P]
 _lib.as2d_token_probs.argtypes = [_P, _S, _S, ctypes.c_float, _P, _P]
 _lib.as2d_accept_sampled.argtypes = [_P, _P, _P, _P, _S, _S, _P, _P, _P, _P]
-for _n in ("as2d_tree_attention_workspace", "as2d_tree_attention", "as2d_attention_weights",
+_lib.as2d_verify_tree.argtypes = [_P, _P, _P, _P, ctypes.POINTER(as2d_verify_out), _P, _P]
+_lib.as2d_verify_sampled.argtypes = [_P, _P, _P, _P, _P, ctypes.c_float,
+                                     ctypes.POINTER(as2d_verify_out), _P, _P]
+_lib.as2d_kv_track_weights.argtypes = [_P, _P]
+_lib.as2d_kv_evict.argtypes = [_P, _P, _S, _P]
+for _n in ("as2d_verify_tree", "as2d_verify_sampled", "as2d_kv_track_weights", "as2d_kv_evict",
+           "as2d_tree_attention_workspace", "as2d_tree_attention", "as2d_attention_weights",
            "as2d_cache_evict_workspace", "as2d_cache_evict", "as2d_token_probs",
            "as2d_accept_sampled"):
     getattr(_lib, _n).restype = _S
@@ -588,6 +597,40 @@ class State:
                               greedy.data_ptr() if greedy is not None else 0,
                               logits.data_ptr() if logits is not None else 0)
         _check(as2d_decode_step(self.handle, out, stream), "as2d_decode_step")
+
+    def verify_tree(self, candidates, parents, k, n_accepted, correction, greedy=None, logits=None,
+                    path=None, stream=0):
+        """as2d_verify_tree: device int32 candidates and parents, packed."""
+        out = make_verify_out(n_accepted.data_ptr(), correction.data_ptr(),
+                              greedy.data_ptr() if greedy is not None else 0,
+                              logits.data_ptr() if logits is not None else 0)
+        some = candidates is not None and candidates.numel()
+        _check(_lib.as2d_verify_tree(
+            self.handle, candidates.data_ptr() if some else None, parents.data_ptr() if some else None,
+            _i32_array(k), ctypes.byref(out), path.data_ptr() if path is not None else None, stream),
+            "as2d_verify_tree")
+
+    def verify_sampled(self, candidates, k, u, temperature, probs, n_accepted, correction,
+                       draft_probs=None, greedy=None, stream=0):
+        """as2d_verify_sampled: u [rows] and probs [rows, vocab] device float."""
+        out = make_verify_out(n_accepted.data_ptr(), correction.data_ptr(),
+                              greedy.data_ptr() if greedy is not None else 0)
+        some = candidates is not None and candidates.numel()
+        _check(_lib.as2d_verify_sampled(
+            self.handle, candidates.data_ptr() if some else None, _i32_array(k),
+            draft_probs.data_ptr() if draft_probs is not None and some else None, u.data_ptr(),
+            temperature, ctypes.byref(out), probs.data_ptr(), stream), "as2d_verify_sampled")
+
+    def track_weights(self, weights):
+        """as2d_kv_track_weights: a device float tensor (kept alive here) or None."""
+        _check(_lib.as2d_kv_track_weights(
+            self.handle, weights.data_ptr() if weights is not None else None), "as2d_kv_track_weights")
+        self._weights = weights
+
+    def evict(self, keep, recent=0, stream=0):
+        if len(keep) != self.batch:
+            raise ValueError(f"keep must name {self.batch} requests")
+        _check(_lib.as2d_kv_evict(self.handle, _i32_array(keep), recent, stream), "as2d_kv_evict")
 
     def verify_from_buffers(self, bufs, b, stream=0):
         """One verification call with candidates from CandidateBuffer objects

@@ -1,12 +1,14 @@
 // as2d_api.cu -- the C-ABI of include/as2d.h: argument checking, ownership,
 // weight re-layout at load time, and the per-call launch sequence of the
 // verification pass (Section 3.2; App. C.2).
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
 #include <string>
 
 #include "as2d_internal.h"
+#include "ops.h"
 
 using namespace as2d;
 
@@ -292,7 +294,7 @@ as2d_status alloc_work(KvState& s, const Model& m, int batch, int capacity,
   const size_t R = s.rows_alloc, H = m.cfg.hidden, F = m.cfg.ffn;
   const size_t ws_ctas = m.sm_count > 2 ? m.sm_count : 2;  // a projection's grid is even
   const size_t max_tiles = ((size_t)(m.cfg.vocab > 2 * F ? m.cfg.vocab : 2 * F) + 127) / 128 + 64;
-  size_t bytes = 4096 + 3 * align_up((size_t)(batch + 1) * 4, 256);
+  size_t bytes = 4096 + 5 * align_up((size_t)(batch + 1) * 4, 256);
   bytes += align_up(R * H * 4, 256) + align_up(2 * R * H * 2, 256) +
            align_up(2 * R * m.q_dim * 2, 256) + align_up(2 * R * F * 2, 256) + align_up(R * 8, 256) +
            align_up(R * (m.cfg.head_dim / 2) * 8, 256) + align_up(R * (H / 128) * 4, 256) +
@@ -318,6 +320,8 @@ as2d_status alloc_work(KvState& s, const Model& m, int batch, int capacity,
   s.d_len = cv.take<int32_t>(batch);
   s.d_root = cv.take<int32_t>(batch);
   s.d_err = cv.take<int32_t>(batch + 1);
+  s.d_off = cv.take<int32_t>(batch);
+  s.d_floor = cv.take<int32_t>(batch);
   s.h = cv.take<float>(R * H);
   s.xn = cv.take<bf16>(2 * R * H);
   s.ao = cv.take<bf16>(2 * R * m.q_dim);
@@ -415,6 +419,8 @@ extern "C" void as2d_kv_free(as2d_kv* kh) {
   cudaFree(kh->s.rope_full);
   cudaFree(kh->s.cb_dev);
   cudaFree(kh->s.pf_out);
+  cudaFree(kh->s.tree_work);
+  cudaFree(kh->s.evict_ws);
   for (KvState* w = kh->s.pf; w;) {
     // the prefill states' lengths, roots, flags and rotary table are this state's
     KvState* next = w->pf;
@@ -561,14 +567,56 @@ cudaError_t tc_project(int epi, const Model& m, KvState& s, const RowMap& rm, co
   return cudaSuccess;
 }
 
+// The attention of a layer by as2d_tree_attention's kernels: along trees, or where
+// the entries' weights are gathered (then for chains too).
+cudaError_t launch_masked_attention(const RowMap& rm, const Model& m, KvState& s, int layer, bool tree,
+                                    cudaStream_t st) {
+  const as2d_config& c = m.cfg;
+  cudaError_t e = launch_attention_split(rm, m, s, layer, st, s.tree_q);
+  if (e != cudaSuccess) return e;
+  const size_t at = (size_t)layer * s.batch * c.n_kv_heads * s.capacity;
+  WeightArgs w{};
+  TreeArgs& a = w.t;
+  a.rm = rm;
+  a.len = s.d_len;
+  a.cap = s.capacity;
+  a.nq = c.n_q_heads;
+  a.nkv = c.n_kv_heads;
+  a.q = s.tree_q;
+  a.q_f32 = 1;
+  a.q_stride = m.q_dim;
+  a.visible = tree ? s.tree_visible : nullptr;
+  a.scale_log2 = 1.4426950408889634f / sqrtf((float)c.head_dim);
+  a.k = s.k_cache + at * c.head_dim;
+  a.v = s.v_cache + at * c.head_dim;
+  a.out = s.ao;
+  a.out_lo = s.ao + (size_t)s.rows_alloc * m.q_dim;
+  a.lse = s.track ? s.tree_lse : nullptr;
+  a.err = s.d_err;
+  a.timeout_ns = s.wait_ns;
+  int64_t keys = 1;
+  for (int b = 0; b < s.batch; ++b) {
+    const int64_t n = s.len_upper[b] + rm.start[b + 1] - rm.start[b];
+    if (n > keys) keys = n;
+  }
+  s.launches += 2;
+  e = launch_tree_attention(a, c.head_dim, keys, s.tree_ws, st);
+  if (e != cudaSuccess || !s.track) return e;
+  w.w = s.track + at;
+  ++s.launches;
+  return launch_attention_weights(w, c.head_dim, keys, st);
+}
+
 // One verification pass.  mode: kAcceptVerify, or for a prefill's passes
 // (batch 1) every row kept and the LM head run over the pass's last row
 // (kAcceptAll) or not at all (kAcceptAllNoRoot); root_override: device int32
 // [batch], the tokens forwarded in place of the pending roots; keep: the
-// pass's part in a prefill of several.
+// pass's part in a prefill of several; tree: the candidates are trees; sampled:
+// tokens are accepted and drawn by given random numbers (out->logits null).
 as2d_status run_block(KvState& s, const int32_t* cand, const int32_t* k,
                       const as2d_verify_out* out, cudaStream_t st, AcceptMode mode = kAcceptVerify,
-                      const int32_t* root_override = nullptr, KeepRow keep = kKeepNone) {
+                      const int32_t* root_override = nullptr, KeepRow keep = kKeepNone,
+                      const TreeCall* tree = nullptr, const SampledCall* sampled = nullptr) {
   if (!out || !out->n_accepted || !out->correction_token)
     return fail(AS2D_ERR_INVALID_ARG, "out, out->n_accepted and out->correction_token are required");
   RowMap rm;
@@ -595,11 +643,12 @@ as2d_status run_block(KvState& s, const int32_t* cand, const int32_t* k,
   // gather, n_layers x {QKV (split-K sums), RoPE + KV append + attention, O + residual,
   // gate/up + SwiGLU, down + residual}, LM head + argmax, accept scan, as a
   // sequence of kernels chained by programmatic dependent launch.
-  LAUNCH(AS2D_KERNEL_OTHER, launch_embed(rm, m, s, cand, st, root_override));
+  if (tree) LAUNCH(AS2D_KERNEL_OTHER, launch_tree_plan(rm, m, s, tree->parents, st));
+  LAUNCH(AS2D_KERNEL_OTHER, launch_embed(rm, m, s, cand, st, root_override, tree ? s.tree_depth : nullptr));
   TcParams tp{};
   tp.h = s.h;
   tp.u = s.u;
-  tp.logits = out->logits;
+  tp.logits = sampled ? sampled->probs : out->logits;
   tp.best = s.best;
   tp.xn = s.xn;
   tp.ss = s.ss;
@@ -612,7 +661,10 @@ as2d_status run_block(KvState& s, const int32_t* cand, const int32_t* k,
   const Operand xn{s.tm_xn, s.tm_xn_pair}, ao{s.tm_ao, s.tm_ao_pair}, u{s.tm_u, s.tm_u_pair};
   for (int l = 0; l < c.n_layers; ++l) {
     LAUNCH(AS2D_KERNEL_QKV, tc_project(TC_PART, m, s, rm, m.w_qkv[l], m.tm_qkv[l], xn, m.qkv_rows, H, tp, st));
-    LAUNCH(AS2D_KERNEL_ATTENTION, launch_attention_split(rm, m, s, l, st));
+    if (tree || s.track)
+      LAUNCH(AS2D_KERNEL_ATTENTION, launch_masked_attention(rm, m, s, l, tree != nullptr, st));
+    else
+      LAUNCH(AS2D_KERNEL_ATTENTION, launch_attention_split(rm, m, s, l, st));
     tp.g_next = m.mlp_norm[l];
     LAUNCH(AS2D_KERNEL_O, tc_project(TC_RESID, m, s, rm, m.w_o[l], m.tm_o[l], ao, H, m.q_dim, tp, st));
     LAUNCH(AS2D_KERNEL_GATE_UP, tc_project(TC_SWIGLU, m, s, rm, m.w_gu[l], m.tm_gu[l], xn, 2 * F, H, tp, st));
@@ -624,7 +676,27 @@ as2d_status run_block(KvState& s, const int32_t* cand, const int32_t* k,
   if (mode != kAcceptAllNoRoot)
     LAUNCH(AS2D_KERNEL_LM_HEAD, tc_project(TC_LOGITS, m, s, rm, m.lm_head, m.tm_lm_head, xn, c.vocab, H, tp,
                                            st, mode == kAcceptAll ? rm.rows - 1 : 0));
-  LAUNCH(AS2D_KERNEL_OTHER, launch_accept(rm, m, s, cand, *out, st, mode, keep == kKeepRestore));
+  if (tree) {
+    LAUNCH(AS2D_KERNEL_OTHER, launch_accept_tree(rm, m, s, cand, *tree, *out, st));
+  } else if (sampled) {
+    SampledArgs a{};
+    a.probs = sampled->probs;
+    a.draft = sampled->draft;
+    a.u = sampled->u;
+    a.cand = cand;
+    a.batch = s.batch;
+    a.vocab = c.vocab;
+    for (int b = 0; b <= s.batch; ++b) a.start[b] = rm.start[b];
+    a.n_out = out->n_accepted;
+    a.token_out = out->correction_token;
+    s.launches += 2;
+    LAUNCH(AS2D_KERNEL_OTHER, launch_token_probs(sampled->probs, rm.rows, c.vocab, sampled->temperature,
+                                                 sampled->probs, st));
+    LAUNCH(AS2D_KERNEL_OTHER, launch_accept_sampled(a, st));
+    LAUNCH(AS2D_KERNEL_OTHER, launch_commit_sampled(rm, s, *out, st));
+  } else {
+    LAUNCH(AS2D_KERNEL_OTHER, launch_accept(rm, m, s, cand, *out, st, mode, keep == kKeepRestore));
+  }
   for (int b = 0; b < s.batch; ++b) s.len_upper[b] += (k ? k[b] : 0) + 1;
   return AS2D_OK;
 }
@@ -684,6 +756,8 @@ as2d_status make_prefill_state(KvState& s, int rows, cudaStream_t st, bool captu
   a->d_len = s.d_len;
   a->d_root = s.d_root;
   a->d_err = s.d_err;
+  a->d_off = s.d_off;
+  a->d_floor = s.d_floor;
   a->rope_full = s.rope_full;
   a->kept = s.kept;
   a->kept_x = s.kept_x;
@@ -732,6 +806,7 @@ extern "C" as2d_status as2d_prefill(as2d_kv* kh, const int32_t* tokens, int32_t 
   if (!kh || !tokens || n < 1) return fail(AS2D_ERR_INVALID_ARG, "kv, tokens and n >= 1 are required");
   KvState& s = kh->s;
   if (s.batch != 1) return fail(AS2D_ERR_UNSUPPORTED, "prefill runs batch-1 states");
+  if (s.track) return fail(AS2D_ERR_UNSUPPORTED, "prefill does not track weights");
   if (s.len_upper[0] + n > s.capacity)
     return fail(AS2D_ERR_CAPACITY, "length bound + n exceeds the cache capacity");
   const int want = prefill_rows(n);
@@ -782,6 +857,121 @@ extern "C" as2d_status as2d_decode_step(as2d_kv* kh, const as2d_verify_out* out,
   g_err.clear();
   if (!kh) return fail(AS2D_ERR_INVALID_ARG, "kv is NULL");
   return run_block(kh->s, nullptr, nullptr, out, (cudaStream_t)stream);
+}
+
+namespace {
+
+// Working memory of calls along trees and of calls with tracked weights, kept
+// until as2d_kv_free; it needs no initial contents, so a call under stream
+// capture can make it.
+as2d_status ensure_tree_work(KvState& s) {
+  if (s.tree_work) return AS2D_OK;
+  const Model& m = *s.model;
+  const RelaxedCapture relaxed;
+  const size_t R = s.max_rows, B = s.batch, ws = tree_attention_workspace(m.cfg.head_dim);
+  const size_t bytes = align_up(R * m.q_dim * 4, 256) + align_up(R * m.cfg.n_q_heads * 4, 256) + align_up(R * 8, 256) +
+                       align_up(R * 4, 256) + align_up(B * kMaxK * 4, 256) + align_up(B * 4, 256) +
+                       align_up(ws, 256) + 256;
+  const cudaError_t e = cudaMalloc(&s.tree_work, bytes);
+  if (e != cudaSuccess) {
+    s.tree_work = nullptr;
+    (void)cudaGetLastError();
+    return fail(AS2D_ERR_CUDA, std::string("cudaMalloc of the tree's working memory: ") + cudaGetErrorString(e));
+  }
+  Carver cv{(char*)s.tree_work};
+  s.tree_q = cv.take<float>(R * m.q_dim);
+  s.tree_lse = cv.take<float>(R * m.cfg.n_q_heads);
+  s.tree_visible = cv.take<uint64_t>(R);
+  s.tree_depth = cv.take<int32_t>(R);
+  s.tree_path = cv.take<int32_t>(B * kMaxK);
+  s.tree_from = cv.take<int32_t>(B);
+  s.tree_ws = cv.take<char>(ws);
+  return AS2D_OK;
+}
+
+}  // namespace
+
+extern "C" as2d_status as2d_verify_tree(as2d_kv* kh, const int32_t* candidates, const int32_t* parents,
+                                        const int32_t* k, const as2d_verify_out* out, int32_t* path,
+                                        void* stream) {
+  g_err.clear();
+  if (!kh || !k) return fail(AS2D_ERR_INVALID_ARG, "kv and k are required");
+  KvState& s = kh->s;
+  for (int b = 0; b < s.batch; ++b)
+    if (k[b] > 0 && !parents) return fail(AS2D_ERR_INVALID_ARG, "parents is NULL");
+  const as2d_status st = ensure_tree_work(s);
+  if (st != AS2D_OK) return st;
+  const TreeCall tree{parents, path};
+  return run_block(s, candidates, k, out, (cudaStream_t)stream, kAcceptVerify, nullptr, kKeepNone, &tree);
+}
+
+extern "C" as2d_status as2d_verify_sampled(as2d_kv* kh, const int32_t* candidates, const int32_t* k,
+                                           const float* draft_probs, const float* u, float temperature,
+                                           const as2d_verify_out* out, float* probs, void* stream) {
+  g_err.clear();
+  if (!kh || !k || !u || !probs) return fail(AS2D_ERR_INVALID_ARG, "kv, k, u and probs are required");
+  if (!(temperature > 0.f) || !std::isfinite(temperature))
+    return fail(AS2D_ERR_INVALID_ARG, "temperature must be finite and > 0");
+  if (out && out->logits) return fail(AS2D_ERR_INVALID_ARG, "out->logits must be NULL: the rows become probabilities");
+  if (kh->s.model->cfg.vocab > 1 << 24)
+    return fail(AS2D_ERR_UNSUPPORTED, "vocab above 2^24 is not supported");
+  const SampledCall sampled{draft_probs, u, temperature, probs};
+  return run_block(kh->s, candidates, k, out, (cudaStream_t)stream, kAcceptVerify, nullptr, kKeepNone, nullptr,
+                   &sampled);
+}
+
+extern "C" as2d_status as2d_kv_track_weights(as2d_kv* kh, float* weights) {
+  g_err.clear();
+  if (!kh) return fail(AS2D_ERR_INVALID_ARG, "kv is NULL");
+  KvState& s = kh->s;
+  if (weights) {
+    const as2d_status st = ensure_tree_work(s);
+    if (st != AS2D_OK) return st;
+    if (!s.evict_ws) {
+      const RelaxedCapture relaxed;
+      const as2d_config& c = s.model->cfg;
+      const cudaError_t e =
+          cudaMalloc(&s.evict_ws, cache_evict_workspace((int64_t)c.n_layers * s.batch * c.n_kv_heads, s.capacity));
+      if (e != cudaSuccess) {
+        s.evict_ws = nullptr;
+        (void)cudaGetLastError();
+        return fail(AS2D_ERR_CUDA, std::string("cudaMalloc of the eviction's workspace: ") + cudaGetErrorString(e));
+      }
+    }
+  }
+  s.track = weights;
+  return AS2D_OK;
+}
+
+extern "C" as2d_status as2d_kv_evict(as2d_kv* kh, const int32_t* keep, int32_t recent, void* stream) {
+  g_err.clear();
+  if (!kh || !keep) return fail(AS2D_ERR_INVALID_ARG, "kv and keep are required");
+  KvState& s = kh->s;
+  if (!s.track) return fail(AS2D_ERR_INVALID_ARG, "no weights are tracked (as2d_kv_track_weights)");
+  if (recent < 0) return fail(AS2D_ERR_INVALID_ARG, "recent must be >= 0");
+  const as2d_config& c = s.model->cfg;
+  EvictArgs a{};
+  a.k = s.k_cache;
+  a.v = s.v_cache;
+  a.w = s.track;
+  a.len = s.d_len;
+  a.n_layers = c.n_layers;
+  a.batch = s.batch;
+  a.nkv = c.n_kv_heads;
+  a.cap = s.capacity;
+  a.recent = recent;
+  for (int b = 0; b < s.batch; ++b) {
+    if (keep[b] < 0) return fail(AS2D_ERR_INVALID_ARG, "keep must be >= 0");
+    a.keep[b] = keep[b];
+  }
+  cache_evict_carve(a, (int64_t)c.n_layers * s.batch * c.n_kv_heads, s.evict_ws);
+  cudaStream_t st = (cudaStream_t)stream;
+  s.launches += 3;
+  LAUNCH(AS2D_KERNEL_OTHER, launch_note_evict(s, keep, st));
+  LAUNCH(AS2D_KERNEL_OTHER, launch_cache_evict(a, c.head_dim, st));
+  for (int b = 0; b < s.batch; ++b)
+    if (s.len_upper[b] > keep[b]) s.len_upper[b] = keep[b];
+  return AS2D_OK;
 }
 
 extern "C" as2d_status as2d_kv_rollback(as2d_kv* kh, const int32_t* new_len,
@@ -846,8 +1036,10 @@ extern "C" as2d_status as2d_kv_check(as2d_kv* kh, void* stream) {
     }
     std::string msg = "device error:";
     if (err & kErrBadToken) msg += " candidate or root token outside [0, vocab);";
-    if (err & kErrRollback) msg += " rollback beyond the committed length;";
+    if (err & kErrRollback) msg += " rollback beyond the committed length or below an eviction;";
     if (err & kErrTimeout) msg += " a kernel wait timed out;";
+    if (err & kErrBadTree) msg += " a candidate's parent is no earlier row of its request;";
+    if (err & kErrNoToken) msg += " a row's probabilities gave no token;";
     if (err & kErrCapacity) msg += " a device-side length left no room for the call's rows;";
     return fail(AS2D_ERR_DEVICE, msg);
   }

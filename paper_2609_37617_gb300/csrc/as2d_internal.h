@@ -62,6 +62,8 @@ enum : int32_t {
   kErrRollback = AS2D_DEVERR_ROLLBACK,
   kErrTimeout = AS2D_DEVERR_TIMEOUT,
   kErrCapacity = AS2D_DEVERR_CAPACITY,
+  kErrBadTree = AS2D_DEVERR_BAD_TREE,
+  kErrNoToken = AS2D_DEVERR_NO_TOKEN,
 };
 
 // Whether a request of device-side length `len` has room for `rows` more
@@ -192,6 +194,8 @@ struct KvState {
   int32_t* d_len = nullptr;   // [batch]
   int32_t* d_root = nullptr;  // [batch]
   int32_t* d_err = nullptr;   // [1]
+  int32_t* d_off = nullptr;   // [batch] a new row's position minus its cache index: entries evicted so far
+  int32_t* d_floor = nullptr; // [batch] entries that the last eviction left: no rollback goes below
   // working memory, sized for batch * (max_k + 1) rows
   int max_k = kMaxK;         // most candidates (rows - 1) of one request in a call
   int max_rows = 0;
@@ -251,6 +255,31 @@ struct KvState {
   // its own pf; shares this state's cache, lengths, roots, error flags and
   // rotary table
   KvState* pf = nullptr;
+  // as2d_verify_tree and calls with tracked weights (tree_work, allocated on
+  // first use: nothing in it outlives a call)
+  void* tree_work = nullptr;
+  float* tree_q = nullptr;         // [max_rows][nq][d] rotated queries
+  float* tree_lse = nullptr;       // [max_rows][nq]
+  uint64_t* tree_visible = nullptr;  // [max_rows]
+  int32_t* tree_depth = nullptr;   // [max_rows] of each row below its request's root
+  int32_t* tree_path = nullptr;    // [batch][kMaxK] accepted candidates, then -1
+  int32_t* tree_from = nullptr;    // [batch] length before the call, -1: nothing moves
+  void* tree_ws = nullptr;         // tree_attention_workspace
+  float* track = nullptr;          // caller's [layers][batch][n_kv][cap] weights (as2d_kv_track_weights)
+  void* evict_ws = nullptr;        // cache_evict_workspace, own allocation
+};
+
+// A call of as2d_verify_tree: its parents (device, packed as the candidates) and
+// the caller's copy of the accepted paths.
+struct TreeCall {
+  const int32_t* parents;
+  int32_t* path;  // [batch][kMaxK], nullable
+};
+// A call of as2d_verify_sampled.
+struct SampledCall {
+  const float *draft, *u;
+  float temperature;
+  float* probs;
 };
 
 // Error reporting shared by the translation units of the C-ABI: records the
@@ -261,12 +290,24 @@ void clear_error();
 // Launchers (k_basic.cu).  All enqueue on `st` and return cudaGetLastError().
 cudaError_t launch_embed(const RowMap& m, const Model& md, KvState& kv,
                          const int32_t* cand, cudaStream_t st,
-                         const int32_t* root_override = nullptr);
+                         const int32_t* root_override = nullptr,
+                         const int32_t* depth = nullptr);
 cudaError_t launch_accept(const RowMap& m, const Model& md, KvState& kv,
                           const int32_t* cand, const as2d_verify_out& out,
                           cudaStream_t st, AcceptMode mode = kAcceptVerify,
                           bool kept_root = false);
 cudaError_t launch_keep_row(const Model& md, KvState& kv, KeepRow op, int row, cudaStream_t st);
+// Each request's tree: rows' masks and depths (k_basic.cu).
+cudaError_t launch_tree_plan(const RowMap& m, const Model& md, KvState& kv, const int32_t* parents,
+                             cudaStream_t st);
+// Accept scan along a tree, and the accepted entries (with their tracked weights)
+// moved up to one after another.
+cudaError_t launch_accept_tree(const RowMap& m, const Model& md, KvState& kv, const int32_t* cand,
+                               const TreeCall& t, const as2d_verify_out& out, cudaStream_t st);
+// State update after as2d_accept_sampled wrote out's n_accepted and correction.
+cudaError_t launch_commit_sampled(const RowMap& m, KvState& kv, const as2d_verify_out& out, cudaStream_t st);
+// Position offsets and floors before an eviction down to keep[b] entries.
+cudaError_t launch_note_evict(KvState& kv, const int32_t* keep, cudaStream_t st);
 cudaError_t launch_rollback(KvState& kv, const int32_t* new_len,
                             const int32_t* new_root, cudaStream_t st);
 // Fills kv.rope_full for positions [0, capacity).
@@ -285,8 +326,10 @@ size_t attn_qimg_bytes(int head_dim);
 // map the attention kernel loads key/value tiles through.
 bool encode_cache_map(CUtensorMap* map, const void* cache, int head_dim, int capacity,
                       int64_t heads);
+// With q32 only the QKV projection is finished: keys and values appended, rotated
+// queries to q32 ([rows][nq][d]).
 cudaError_t launch_attention_split(const RowMap& m, const Model& md, KvState& kv, int layer,
-                                   cudaStream_t st);
+                                   cudaStream_t st, float* q32 = nullptr);
 
 // Tensor-core GEMM launchers (k_tc_*.cu), one per fused epilogue.
 int qkv_split_for(const Model& m);

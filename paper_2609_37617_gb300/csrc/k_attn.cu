@@ -111,6 +111,7 @@ struct AttnArgs {
   bf16* kc;
   bf16* vc;
   uint8_t* qimg;          // [batch][nkv][qt_max] operand images, 256 d bytes each
+  float* q32;             // not null: queries go here instead, unscaled, [rows][nq][d]
   int qt_max;
   float* ws_o;            // [batch][nkv][qt_max][chunks_max][64][d] chunk partials
   float2* ws_ml;          // [batch][nkv][qt_max][chunks_max][64] (max, sum), base 2
@@ -237,7 +238,11 @@ __global__ void __launch_bounds__(32 * kQkvWarps) qkv_finish_kernel(const __grid
     else
       *reinterpret_cast<uint32_t*>(to) = w[0];
   };
-  if (is_q) {
+  if (is_q && a.q32) {
+    float* to = a.q32 + ((size_t)gm * a.nq + head) * D + e;
+#pragma unroll
+    for (int u = 0; u < V; ++u) to[u] = y0[u], to[u + H2] = y1[u];
+  } else if (is_q) {
     // hi parts, and what they leave (exact) as lo parts
     float l0[V], l1[V];
 #pragma unroll
@@ -1333,7 +1338,7 @@ int attn_chunks(int capacity) { return (capacity + kChunk - 1) / kChunk; }
 size_t attn_qimg_bytes(int head_dim) { return (size_t)256 * head_dim; }
 
 cudaError_t launch_attention_split(const RowMap& m, const Model& md, KvState& kv, int layer,
-                                   cudaStream_t st) {
+                                   cudaStream_t st, float* q32) {
   const as2d_config& c = md.cfg;
   AttnArgs a;
   a.rm = m;
@@ -1352,6 +1357,7 @@ cudaError_t launch_attention_split(const RowMap& m, const Model& md, KvState& kv
   a.kc = kv.k_cache;
   a.vc = kv.v_cache;
   a.qimg = kv.qimg;
+  a.q32 = q32;
   a.qt_max = kv.attn_qt;
   a.ws_o = kv.attn_o;
   a.ws_ml = kv.attn_ml;
@@ -1361,6 +1367,13 @@ cudaError_t launch_attention_split(const RowMap& m, const Model& md, KvState& kv
   a.lo_row = kv.rows_alloc;
   a.err = kv.d_err;
   a.timeout_ns = kv.wait_ns;
+  const dim3 gf(m.rows, (c.n_q_heads + 2 * c.n_kv_heads + 2 * kQkvWarps - 1) / (2 * kQkvWarps));
+  const dim3 bf(32, kQkvWarps);
+  if (q32) {
+    ++kv.launches;
+    return c.head_dim == 128 ? launch_pdl(qkv_finish_kernel<128>, gf, bf, 0, st, 1, a)
+                             : launch_pdl(qkv_finish_kernel<64>, gf, bf, 0, st, 1, a);
+  }
   const int G = c.n_q_heads / c.n_kv_heads;
   int clusters8 = 0, max_nch = 0;
   for (int b = 0; b < kv.batch; ++b) {
@@ -1403,8 +1416,6 @@ cudaError_t launch_attention_split(const RowMap& m, const Model& md, KvState& kv
   a.fold_later = fold ? 1 : 0;
   int q_tiles = 0;
   for (int b = 0; b < kv.batch; ++b) q_tiles += attn_q_tiles(m.start[b + 1] - m.start[b], G);
-  const dim3 gf(m.rows, (c.n_q_heads + 2 * c.n_kv_heads + 2 * kQkvWarps - 1) / (2 * kQkvWarps));
-  const dim3 bf(32, kQkvWarps);
   cudaError_t e;
   kv.launches += fold ? 3 : 2;
   if (c.head_dim == 128) {

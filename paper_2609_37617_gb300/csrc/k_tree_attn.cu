@@ -40,6 +40,10 @@ namespace as2d {
 namespace {
 
 constexpr int kThreads = 640;
+// What turning to another item costs a CTA, in tiles (where a CTA has several): its
+// queries, its epilogue.  16 ragged requests of 60 items take 77 us with 0, 60 / 55 /
+// 51 / 55 with 3 / 4 / 5 / 6, a tree of 64 rows (16 items) 45 / 42 / 40 with 3 / 5 / 6.
+constexpr int kTurn = 5;
 // P may grow to 2^kLazy before the accumulator is rescaled.
 constexpr float kLazy = 8.f;
 
@@ -111,10 +115,17 @@ __device__ __forceinline__ void clean_tile(uint8_t* v, int p0, int L, int kend, 
   }
 }
 
-// N consecutive results x inv at element `at` of the output.
+// N consecutive results x inv at element `at` of the output: 32-bit (F32), bf16, or
+// bf16 hi and lo parts (F32 with out_lo).
 template <int N, bool F32>
 __device__ __forceinline__ void write_out(const TreeArgs& a, const float* x, float inv, size_t at) {
-  if (F32) {
+  if (F32 && a.out_lo) {
+    bf16* out = (bf16*)a.out + at;
+    bf16* lo = a.out_lo + at;
+#pragma unroll
+    for (int e = 0; e < N; e += 2)
+      hi_lo(x[e] * inv, x[e + 1] * inv, *reinterpret_cast<uint32_t*>(out + e), *reinterpret_cast<uint32_t*>(lo + e));
+  } else if (F32) {
     float* out = (float*)a.out + at;
 #pragma unroll
     for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(out + e) = make_float2(x[e] * inv, x[e + 1] * inv);
@@ -128,7 +139,7 @@ __device__ __forceinline__ void write_out(const TreeArgs& a, const float* x, flo
 template <int D, bool F32>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                     const __grid_constant__ TreeArgs a, TreeWork ws, int whole) {
+                     const __grid_constant__ TreeArgs a, TreeWork ws, int whole, int turn) {
   using S = Shape<D, F32>;
   constexpr int NST = S::NST, NR = D / 64;
   extern __shared__ uint8_t smem_raw[];
@@ -182,17 +193,18 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  if (warp == 0) make_plan(a, 128, lane, s_plan, blockIdx.x == 0);
+  if (warp == 0) make_plan(a, 128, turn, lane, s_plan, blockIdx.x == 0);
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tslot;
   int u0, u1;
   unit_range(*plan, a, blockIdx.x, gridDim.x, whole, u0, u1);
-  if (warp >= 2 && u0 < u1) {
+  Unit one;
+  if (int u = u0; warp >= 2 && next_item(*plan, a, u, u1, one)) {
     // the first item's queries, by every warp that has nothing to do yet (by two
     // warps 32-bit queries of 119 rows took 5 us)
-    load_queries<D, F32, kThreads - 64, 4>(a, unit_at(*plan, a, u0, u1), tid - 64, qimg);
+    load_queries<D, F32, kThreads - 64, 4>(a, one, tid - 64, qimg);
     ptx::fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(q_first);
@@ -213,8 +225,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       const uint64_t pol = ptx::policy_evict_first();
       uint32_t n = 0, tail = 0, turn = 0;  // slots whose last tile is on tail_full, its parity
-      for (int u = u0; u < u1;) {
-        const Unit it = unit_at(*plan, a, u, u1);
+      Unit it;
+      for (int u = u0; next_item(*plan, a, u, u1, it);) {
         const int z = it.b * a.nkv + it.g;
         for (int t = it.t0; t < it.t1 && ok; ++t)
           for (int kv = 0; kv < 2; ++kv, ++n) {
@@ -233,7 +245,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int h = 0; h < NR; ++h)
               ptx::tma_load_3d(ring + s * S::STAGE + h * kRegion, kv ? &tmV : &tmK, bar, 64 * h, t * 128, z, pol);
           }
-        u += it.t1 - it.t0;
       }
       // no copy is in flight when the CTA ends
       for (uint32_t i = n > NST ? n - NST : 0; i < n; ++i) {
@@ -253,8 +264,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       Stage at;
       uint32_t items = 0, p_turn = 0, c_turn = 0;    // parities of p_full and v_clean
       uint32_t last0 = kNone, last1 = kNone, v = 0;  // value stages of the sets' last tiles, of the last tile
-      for (int u = u0; u < u1 && ok; ++items) {
-        const Unit it = unit_at(*plan, a, u, u1);
+      Unit it;
+      for (int u = u0; ok && next_item(*plan, a, u, u1, it); ++items) {
         const int cnt = it.t1 - it.t0, first_tail = it.L / 128 - it.t0;
         items == 0 ? wait(q_first, 0) : wait(q_full, (items - 1) & 1);
         for (int j = 0; j <= cnt && ok; ++j) {
@@ -310,7 +321,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (j == cnt) ptx::mma_commit(o_full);
           }
         }
-        u += cnt;
       }
       // no product is running when TMEM is freed
       ptx::mma_commit(drain);
@@ -319,11 +329,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp < 4) {
     const int t64 = tid - 64;
     uint32_t n = 0, items = 0, turn = 0;
-    for (int u = u0; u < u1; ++items) {
-      const Unit it = unit_at(*plan, a, u, u1);
+    Unit it;
+    for (int u = u0; next_item(*plan, a, u, u1, it); ++items) {
       if (items > 0) {
         wait(q_empty, (items - 1) & 1);
-        if (ok) load_queries<D, F32, 64, 8>(a, it, t64, qimg);
+        if (ok) load_queries<D, F32, 64, F32 ? 8 : 16>(a, it, t64, qimg);
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(q_full);
@@ -345,7 +355,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       n += 2 * (it.t1 - it.t0);
-      u += it.t1 - it.t0;
     }
   } else {
     const int group = (warp - 4) >> 2;           // of four warps
@@ -356,8 +365,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int G = a.nq / a.nkv;
     const float c = a.scale_log2;
     uint32_t ns = 0, items = 0, c_turn = 0;
-    for (int u = u0; u < u1; ++items) {
-      const Unit it = unit_at(*plan, a, u, u1);
+    Unit it;
+    for (int u = u0; next_item(*plan, a, u, u1, it); ++items) {
       const int cnt = it.t1 - it.t0, nqs = it.rows * G;
       const int q = it.qt * 128 + row, i = q / G;
       const bool live = q < nqs;
@@ -509,7 +518,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(o_empty);
-      u += cnt;
     }
   }
   ptx::tc_fence_before();
@@ -523,19 +531,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 constexpr int kCombineQuads = 8;  // of a CTA: its warps
 template <int D, bool F32>
 __global__ void __launch_bounds__(32 * kCombineQuads)
-    tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas) {
+    tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas, int turn) {
   constexpr int U = 8;
   __shared__ UnitPlan plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // The lengths before the wait: the products' kernel let this one start after
   // its own wait, so what ran before that kernel is done, and it writes none.
   ptx::griddep_launch_dependents();
-  if (warp == 0) make_plan(a, 128, lane, plan, false);
+  if (warp == 0) make_plan(a, 128, turn, lane, plan, false);
   __syncthreads();
   int us;
   if (!item_at(plan, a, blockIdx.x, us)) return;
   const Unit it = unit_at(plan, a, us, 0x7fffffff);
-  const int c0 = unit_owner(plan, us, ctas), c1 = unit_owner(plan, us + it.tiles - 1, ctas);
+  const int c0 = unit_owner(plan, us + turn, ctas), c1 = unit_owner(plan, us + turn + it.tiles - 1, ctas);
   if (c0 == c1) return;  // written by its CTA
   const int G = a.nq / a.nkv, row = 32 * blockIdx.y + lane, q = it.qt * 128 + row;
   if (q >= it.rows * G) return;
@@ -589,12 +597,12 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   if (attr != cudaSuccess) return attr;
   const bool whole = most_tiles <= kWholeTiles;
   const int64_t units = items * most_tiles;
-  const int ctas = (int)(whole ? items : units < sms ? units : sms);
+  const int ctas = (int)(whole ? items : units < sms ? units : sms), turn = !whole && units > sms ? kTurn : 0;
   const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
-                                   (int)whole);
+                                   (int)whole, turn);
   if (e != cudaSuccess || whole) return e;
   return launch_pdl(tree_combine_kernel<D, F32>, dim3((unsigned)items, (most_queries + 31) / 32, D / 4 / kCombineQuads),
-                    dim3(32 * kCombineQuads), 0, st, 1, a, ws, ctas);
+                    dim3(32 * kCombineQuads), 0, st, 1, a, ws, ctas, turn);
 }
 
 }  // namespace

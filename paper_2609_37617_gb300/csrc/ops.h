@@ -22,6 +22,7 @@ struct TreeArgs {
   const bf16* k;            // the layer's [batch][nkv][cap][d]
   const bf16* v;
   void* out;                // [rows][nq][d] of the queries' type
+  bf16* out_lo;             // not null (32-bit queries): out takes bf16 hi parts, this the lo parts
   float* lse;               // [rows][nq], nullable
   int32_t* err;             // error bits, nullable
   unsigned long long timeout_ns = 2000000000ull;  // limit of the kernel's waits

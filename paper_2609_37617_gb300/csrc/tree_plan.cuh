@@ -3,7 +3,9 @@
 // k_attn_weights.cu).
 //
 // An item is one (request, kv head, query tile), a unit one tile of 128 keys of
-// an item.  Items and their units are numbered request by request, kv head by kv
+// an item or, at its head, one of `extra` units that stand for what a CTA spends on
+// turning to another item (its queries, its epilogue): a CTA that ends one item
+// and begins another gets fewer tiles.  Items and their units are numbered request by request, kv head by kv
 // head, query tile by query tile (the query tiles of a head read its keys one
 // after another, from L2).
 #pragma once
@@ -13,6 +15,7 @@
 namespace as2d {
 
 struct alignas(16) UnitPlan {
+  int extra;                      // units of an item that are no tiles
   int unit[kMaxBatch + 1];  // units before each request (the host refuses calls of 2^31)
   int len[kMaxBatch];
   int tiles[kMaxBatch];           // key tiles of a request's items
@@ -23,11 +26,12 @@ struct alignas(16) UnitPlan {
 struct Unit {
   int b, g, qt, tiles, t0, t1;
   int L, rows, r0;
+  int next;
 };
 
 // Filled by one warp; requests without rows, or whose length leaves no room for
 // theirs, have no units.
-__device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int lane, UnitPlan& p, bool flag) {
+__device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int extra, int lane, UnitPlan& p, bool flag) {
   const int G = a.nq / a.nkv;
   int before = 0;
   bool over = false;
@@ -44,7 +48,7 @@ __device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int lan
       else
         over = over || rows > 0;
     }
-    const int n = a.nkv * qts * tiles;
+    const int n = tiles > 0 ? a.nkv * qts * (tiles + extra) : 0;
     int at = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -57,7 +61,7 @@ __device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int lan
     p.qts[b] = qts;
     before += __shfl_sync(~0u, at, 31);
   }
-  if (lane == 0) p.unit[kMaxBatch] = before;
+  if (lane == 0) p.unit[kMaxBatch] = before, p.extra = extra;
   if (flag && __any_sync(~0u, over) && lane == 0 && a.err) atomicOr(a.err, kErrCapacity);
 }
 
@@ -66,7 +70,7 @@ __device__ __forceinline__ bool item_at(const UnitPlan& p, const TreeArgs& a, in
   for (int b = 0; b < a.rm.batch; ++b) {
     const int items = p.tiles[b] > 0 ? a.nkv * p.qts[b] : 0;
     if (n < items) {
-      u = p.unit[b] + n * p.tiles[b];
+      u = p.unit[b] + n * (p.tiles[b] + p.extra);
       return true;
     }
     n -= items;
@@ -83,7 +87,7 @@ __device__ __forceinline__ void unit_range(const UnitPlan& p, const TreeArgs& a,
     if (item_at(p, a, c, u0)) {
       int b = 0;
       while (p.unit[b + 1] <= u0) ++b;
-      u1 = u0 + p.tiles[b];
+      u1 = u0 + p.tiles[b] + p.extra;
     }
     return;
   }
@@ -101,7 +105,8 @@ __device__ __forceinline__ int unit_owner(const UnitPlan& p, int u, int ctas) {
   return u < wide ? u / (each + 1) : more + (u - wide) / each;
 }
 
-// What is done of unit u's item from u on, up to unit u1 at most.
+// What is done of unit u's item from u on, up to unit u1 at most; `next`: the
+// first unit after that.  May hold no tile.
 __device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, int u, int u1) {
   Unit it;
   int lo = 0, hi = kMaxBatch - 1;  // the last request whose first unit is at or before u
@@ -117,12 +122,25 @@ __device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, in
   it.L = p.len[lo];
   it.r0 = a.rm.start[lo];
   it.rows = a.rm.start[lo + 1] - it.r0;
-  const int rel = u - p.unit[lo], item = rel / it.tiles;
-  it.t0 = rel - item * it.tiles;
+  const int per = it.tiles + p.extra, rel = u - p.unit[lo], item = rel / per, at = rel - item * per;
   it.g = item / p.qts[lo];
   it.qt = item - it.g * p.qts[lo];
-  it.t1 = min(it.tiles, it.t0 + u1 - u);
+  const int end = min(per, at + u1 - u);
+  it.next = u + end - at;
+  it.t0 = max(at - p.extra, 0);
+  it.t1 = max(end - p.extra, 0);
   return it;
+}
+
+// The same of the first item from u on of which there is a tile to do; u: the first
+// unit after it.  False past unit u1.
+__device__ __forceinline__ bool next_item(const UnitPlan& p, const TreeArgs& a, int& u, int u1, Unit& it) {
+  while (u < u1) {
+    it = unit_at(p, a, u, u1);
+    u = it.next;
+    if (it.t0 < it.t1) return true;
+  }
+  return false;
 }
 
 // ln of a sum l of powers of two relative to 2^M; -inf of nothing.
