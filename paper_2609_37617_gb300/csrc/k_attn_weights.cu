@@ -25,6 +25,8 @@ namespace as2d {
 namespace {
 
 constexpr int kThreads = 384;
+// What turning to another head costs a CTA, in tiles (where a CTA has several).
+constexpr int kTurn = 5;
 
 template <int D, bool F32>
 struct Shape {
@@ -35,23 +37,35 @@ struct Shape {
   static_assert(SMEM + sizeof(UnitPlan) <= 232448, "shared memory of one CTA");
 };
 
-// The tiles of one (request, kv head) in units [u, u1): [t0, t1); units done.
+// The tiles of one (request, kv head) in units [u, u1): [t0, t1); the first unit
+// after them.  A head's units: what its passes' turns count (UnitPlan::extra), then
+// its tiles one after another, `passes` units each.
 struct Segment {
   Unit it;
-  int units, passes;
+  int next, passes;
 };
 __device__ __forceinline__ Segment segment_at(const UnitPlan& p, const TreeArgs& a, int u, int u1) {
   Segment s;
   s.it = unit_at(p, a, u, u1);  // (for the request; the rest is in another order here)
-  const int b = s.it.b, per = p.tiles[b] * p.qts[b], rel = u - p.unit[b];
+  const int b = s.it.b, extra = p.qts[b] * p.extra, per = p.tiles[b] * p.qts[b] + extra, rel = u - p.unit[b];
   s.passes = p.qts[b];
   s.it.g = rel / per;
   const int r0 = rel - s.it.g * per, r1 = min(per, r0 + (u1 - u));
-  s.units = r1 - r0;
-  s.it.t0 = (r0 + s.passes - 1) / s.passes;
-  s.it.t1 = (r1 + s.passes - 1) / s.passes;
+  s.next = u + r1 - r0;
+  s.it.t0 = (max(r0 - extra, 0) + s.passes - 1) / s.passes;
+  s.it.t1 = (max(r1 - extra, 0) + s.passes - 1) / s.passes;
   s.it.qt = 0;
   return s;
+}
+// The same of the first head from u on of which there is a tile to do; u: the first
+// unit after it.
+__device__ __forceinline__ bool next_segment(const UnitPlan& p, const TreeArgs& a, int& u, int u1, Segment& s) {
+  while (u < u1) {
+    s = segment_at(p, a, u, u1);
+    u = s.next;
+    if (s.it.t0 < s.it.t1) return true;
+  }
+  return false;
 }
 
 // Sum of the exponentials of 16 queries from column q0 on; masked: of those that
@@ -78,7 +92,7 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[16], float c, co
 
 template <int D, bool F32>
 __global__ void __launch_bounds__(kThreads, 1)
-    attn_weights_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ WeightArgs wa) {
+    attn_weights_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ WeightArgs wa, int turn) {
   using S = Shape<D, F32>;
   constexpr int NST = S::NST, NR = D / 64;
   const TreeArgs& a = wa.t;
@@ -122,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0 && lane == 0) ptx::prefetch_tmap(&tmK);
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  if (warp == 0) make_plan(a, 128, 0, lane, plan, blockIdx.x == 0);
+  if (warp == 0) make_plan(a, 128, turn, lane, plan, blockIdx.x == 0);
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
@@ -141,9 +155,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   };
   // queries of a pass (zeros up to the next 16th), their sums and masks, by N
   // threads from t on
-  auto bring = [&](const Unit& it, int t, auto n_threads) {
+  auto bring = [&](const Unit& it, int t, auto n_threads, auto in_flight) {
     constexpr int N = decltype(n_threads)::value;
-    load_queries<D, F32, N, 4>(a, it, t, qimg);
+    load_queries<D, F32, N, decltype(in_flight)::value>(a, it, t, qimg);
     const int n0 = it.qt * 128, n = min(128, it.rows * G - n0), pad = (n + 15) & ~15;
     for (int c = t; c < (pad - n) * (D / 8); c += N) {
       uint8_t* to = qimg + chunk_off(n + c / (D / 8), c % (D / 8));
@@ -166,20 +180,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       s_vis[q] = vis;
     }
   };
-  // (the first pass that has tiles: by every warp that has nothing to do yet)
-  int uf = u0;
-  while (uf < u1) {
-    const Segment s = segment_at(plan, a, uf, u1);
-    if (s.it.t0 < s.it.t1) {
-      if (warp >= 2) {
-        bring(s.it, tid - 64, std::integral_constant<int, kThreads - 64>{});
-        bring_sums(s.it, tid - 64, kThreads - 64);
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(q_first);
-      }
-      break;
-    }
-    uf += s.units;
+  Segment s;
+  if (int u = u0; warp >= 2 && next_segment(plan, a, u, u1, s)) {
+    // the first pass, by every warp that has nothing to do yet
+    bring(s.it, tid - 64, std::integral_constant<int, kThreads - 64>{}, std::integral_constant<int, 8>{});
+    bring_sums(s.it, tid - 64, kThreads - 64);
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(q_first);
   }
 
   if (warp == 0) {
@@ -187,8 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t pol = ptx::policy_evict_first();
       Stage at;
       uint32_t n = 0;
-      for (int u = uf; u < u1;) {
-        const Segment s = segment_at(plan, a, u, u1);
+      for (int u = u0; next_segment(plan, a, u, u1, s);) {
         const int z = s.it.b * a.nkv + s.it.g;
         for (int qt = 0; qt < s.passes; ++qt)
           for (int t = s.it.t0; t < s.it.t1 && ok; ++t, ++n) {
@@ -199,7 +205,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int h = 0; h < NR; ++h)
               ptx::tma_load_3d(ring + i * S::STAGE + h * kRegion, &tmK, &full[i], 64 * h, t * 128, z, pol);
           }
-        u += s.units;
       }
       // no copy is in flight when the CTA ends
       for (uint32_t i = n > NST ? n - NST : 0; i < n; ++i)
@@ -210,9 +215,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t q_lo = ptx::desc_lo(ptx::smem_u32(qimg), 16u);
       Stage at;
       uint32_t done[2] = {0, 0}, pass = 0;  // tiles of each group so far
-      for (int u = uf; u < u1 && ok;) {
-        const Segment s = segment_at(plan, a, u, u1);
-        for (int qt = 0; qt < s.passes && s.it.t0 < s.it.t1 && ok; ++qt, ++pass) {
+      for (int u = u0; ok && next_segment(plan, a, u, u1, s);) {
+        for (int qt = 0; qt < s.passes && ok; ++qt, ++pass) {
           pass == 0 ? wait(q_first, 0) : wait(q_full, (pass - 1) & 1);
           const int n = min(128, s.it.rows * G - qt * 128);
           const uint32_t idesc = ptx::idesc_bf16_f32(128, (n + 15) & ~15);
@@ -242,7 +246,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               ++done[0];
           }
         }
-        u += s.units;
       }
       // no product is running when TMEM is freed
       ptx::mma_commit(drain);
@@ -250,29 +253,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp < 4) {
     uint32_t pass = 0;
-    for (int u = uf; u < u1;) {
-      Segment s = segment_at(plan, a, u, u1);
-      for (int qt = 0; qt < s.passes && s.it.t0 < s.it.t1; ++qt, ++pass) {
+    for (int u = u0; next_segment(plan, a, u, u1, s);) {
+      for (int qt = 0; qt < s.passes; ++qt, ++pass) {
         if (pass == 0) continue;
         s.it.qt = qt;
         wait(q_empty, (pass - 1) & 1);
-        if (ok) bring(s.it, tid - 64, std::integral_constant<int, 64>{});
+        if (ok) bring(s.it, tid - 64, std::integral_constant<int, 64>{}, std::integral_constant<int, 16>{});
         wait(e_empty, (pass - 1) & 1);  // the last pass's sums have been read
         if (ok) bring_sums(s.it, tid - 64, 64);
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(q_full);
       }
-      u += s.units;
     }
   } else {
     const int group = (warp - 4) >> 2, row = 32 * (warp & 3) + lane;  // key of the tile, TMEM lane
     const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
     const float c = a.scale_log2;
     uint32_t d = 0, pass = 0;
-    for (int u = uf; u < u1;) {
-      const Segment s = segment_at(plan, a, u, u1);
+    for (int u = u0; next_segment(plan, a, u, u1, s);) {
       float* w = wa.w + ((size_t)s.it.b * a.nkv + s.it.g) * a.cap;
-      for (int qt = 0; qt < s.passes && s.it.t0 < s.it.t1; ++qt, ++pass) {
+      for (int qt = 0; qt < s.passes; ++qt, ++pass) {
         const int n = min(128, s.it.rows * G - qt * 128);
         // the queries' sums are there (the products wait for them too)
         pass == 0 ? wait(q_first, 0) : wait(q_full, (pass - 1) & 1);
@@ -312,7 +312,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(e_empty);
       }
-      u += s.units;
     }
   }
   ptx::tc_fence_before();
@@ -321,12 +320,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 template <int D, bool F32>
-cudaError_t launch(const CUtensorMap& tk, const WeightArgs& a, int ctas, cudaStream_t st) {
+cudaError_t launch(const CUtensorMap& tk, const WeightArgs& a, int ctas, int turn, cudaStream_t st) {
   using S = Shape<D, F32>;
   static const cudaError_t attr = cudaFuncSetAttribute(
       attn_weights_kernel<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
   if (attr != cudaSuccess) return attr;
-  return launch_pdl(attn_weights_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, a);
+  return launch_pdl(attn_weights_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, a, turn);
 }
 
 }  // namespace
@@ -336,9 +335,9 @@ cudaError_t launch_attention_weights(const WeightArgs& a, int head_dim, int64_t 
   CUtensorMap tk;
   if (!encode_cache_map(&tk, a.t.k, head_dim, a.t.cap, (int64_t)a.t.rm.batch * a.t.nkv)) return cudaErrorInvalidValue;
   const int64_t units = (max_keys + 127) / 128 * tree_items(a.t);
-  const int ctas = (int)(units < sms ? units : sms);
-  if (head_dim == 128) return a.t.q_f32 ? launch<128, true>(tk, a, ctas, st) : launch<128, false>(tk, a, ctas, st);
-  return a.t.q_f32 ? launch<64, true>(tk, a, ctas, st) : launch<64, false>(tk, a, ctas, st);
+  const int ctas = (int)(units < sms ? units : sms), turn = units > sms ? kTurn : 0;
+  if (head_dim == 128) return a.t.q_f32 ? launch<128, true>(tk, a, ctas, turn, st) : launch<128, false>(tk, a, ctas, turn, st);
+  return a.t.q_f32 ? launch<64, true>(tk, a, ctas, turn, st) : launch<64, false>(tk, a, ctas, turn, st);
 }
 
 }  // namespace as2d

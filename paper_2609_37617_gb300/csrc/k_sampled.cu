@@ -24,7 +24,7 @@ __device__ __forceinline__ float ex2(float x) {
 // Slices that the registers do not hold (kHeld values a thread) are read again.
 // VEC: rows in pieces of 16 bytes.
 
-constexpr int kHeld = 24;
+constexpr int kHeld = 40;
 
 __device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
   // (maximum, sum relative to it); -inf: nothing there
@@ -34,7 +34,7 @@ __device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
 }
 
 template <bool VEC>
-__global__ void __launch_bounds__(kThreads) probs_kernel(const float* logits, int vocab, int slice, float c,
+__global__ void __launch_bounds__(kThreads, 2) probs_kernel(const float* logits, int vocab, int slice, float c,
                                                          float* probs) {
   constexpr int W = VEC ? 4 : 1, R = kHeld / W;
   __shared__ float s_red[kWarps];
@@ -142,11 +142,12 @@ __global__ void __launch_bounds__(kThreads) probs_kernel(const float* logits, in
 // slice lies in shared memory and a thread adds a contiguous chunk of it, each
 // difference exactly (as the sum of two floats, Knuth's two-sum) and the sum in
 // two floats, so that the border u total falls between the same two tokens as in
-// 64 bits but for differences of some 2^-48.  The first warp adds the threads' sums
-// in 64 bits (the whole block's additions in 64 bits would take 3 us), the CTAs
-// exchange their totals, and the first warp of the one that holds the border
-// finds the chunk and the token within it.  Bound by latency for a few requests
-// (three dependent round trips to memory), by memory for many.
+// 64 bits but for differences of some 2^-46.  The threads' sums are
+// scanned by shuffles, the CTAs exchange their totals, and the thread whose sums
+// the border lies between finds the token in its chunk.  All of it in pairs of
+// floats: in 64 bits, at this card's rate and latency for them, the additions of
+// one request took 9 of 22 us.  Bound by latency for a few requests (three
+// dependent round trips to memory), by memory for many.
 
 // a + b = s + e exactly.
 __device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {
@@ -155,15 +156,40 @@ __device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {
   e = (a - (s - t)) + (b - t);
 }
 
-constexpr int kMostChunk = 53;   // values of a thread's chunk at most: two rows of a slice fit shared memory
-constexpr int kMostPieces = 128; // pieces of a slice that shared memory holds one after another
+// A number as the sum of two floats, |y| at most half a step of x.
+__device__ __forceinline__ float2 pair_of(float x, float y) {
+  const float s = x + y;
+  return make_float2(s, y - (s - x));
+}
+__device__ __forceinline__ float2 add(float2 a, float2 b) {
+  float s, e;
+  two_sum(a.x, b.x, s, e);
+  return pair_of(s, e + (a.y + b.y));
+}
+__device__ __forceinline__ bool less(float2 a, float2 b) { return a.x < b.x || (a.x == b.x && a.y < b.y); }
+// Inclusive sums over the first N lanes of each N.
+template <int N>
+__device__ __forceinline__ float2 scan(float2 v, int lane) {
+#pragma unroll
+  for (int o = 1; o < N; o <<= 1) {
+    const float2 t = make_float2(__shfl_up_sync(~0u, v.x, o, N), __shfl_up_sync(~0u, v.y, o, N));
+    if ((lane & (N - 1)) >= o) v = add(t, v);
+  }
+  return v;
+}
+__device__ __forceinline__ float2 from_lane(float2 v, int lane) {
+  return make_float2(__shfl_sync(~0u, v.x, lane), __shfl_sync(~0u, v.y, lane));
+}
+
+constexpr int kMostChunk = 53;    // values of a thread's chunk at most: two rows of a slice fit shared memory
+constexpr int kMostPieces = 128;  // pieces of a slice that shared memory holds one after another
+static_assert(kWarps == 16, "the warps' sums and the CTAs' are scanned by 16 lanes");
 
 __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_constant__ SampledArgs a, int chunk,
                                                                   int pieces) {
   extern __shared__ float s_row[];  // [512 chunks] p, then q
-  __shared__ float2 s_sum[kThreads];
-  __shared__ double s_part[2][16], s_piece[kMostPieces];
-  __shared__ int s_n;
+  __shared__ float2 s_part[2][16], s_warp[kWarps], s_piece[kMostPieces];
+  __shared__ int s_n, s_pick, s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int b = blockIdx.y, ranks = gridDim.x, rank = (int)ptx::cluster_rank();
   const int r0 = a.start[b], k = a.start[b + 1] - r0 - 1, c0 = r0 - b;
@@ -176,6 +202,7 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
     if (lane < k) {
       const int c = a.cand[c0 + lane];
       if (c >= 0 && c < a.vocab) {
+        // (products of two floats and their comparison are exact in 64 bits)
         const double q = a.draft ? (double)a.draft[(size_t)(c0 + lane) * V + c] : 1.0;
         stands = (double)a.u[r0 + lane] * q < (double)a.probs[(size_t)(r0 + lane) * V + c];
       }
@@ -188,35 +215,37 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
   const float* p = a.probs + (size_t)(r0 + n) * V;
   const float* q = n < k && a.draft ? a.draft + (size_t)(c0 + n) * V : nullptr;
   // (within [0, 1): the border is below the total)
-  const double u = fminf(fmaxf(a.u[r0 + k], 0.f), 0x1.fffffep-1f);
+  const float u = fminf(fmaxf(a.u[r0 + k], 0.f), 0x1.fffffep-1f);
   float *sp = s_row, *sq = s_row + piece;
 
-  auto weight = [&](int j, bool less, float& hi, float& lo) {
+  auto weight = [&](int j, bool minus, float& hi, float& lo) {
     hi = sp[j], lo = 0.f;
-    if (less) two_sum(hi, -sq[j], hi, lo);
+    if (minus) two_sum(hi, -sq[j], hi, lo);
     if (!(hi > 0.f && hi < INFINITY)) hi = lo = 0.f;
   };
-  // Piece i of the slice into shared memory and the threads' sums into s_sum;
-  // returns its first token.
+  // Piece i of the slice into shared memory: its first token, the thread's sum
+  // and the sum up to and with it, and of all threads.
+  float2 mine, upto, all;
   auto stage = [&](int i, bool plain) {
     const int v0 = (int)min((long long)(rank * pieces + i) * piece, (long long)a.vocab), len = min(piece, a.vocab - v0);
-    const bool less = q && !plain;
+    const bool minus = q && !plain;
     constexpr int U = 10;
     __syncthreads();
+    if (tid == 0) s_pick = 0x7fffffff, s_last = -1;
     for (int j0 = tid; j0 < len; j0 += U * kThreads) {
       float x[U], y[U];
 #pragma unroll
       for (int t = 0; t < U; ++t)
         if (j0 + t * kThreads < len) {
           x[t] = __ldcs(p + v0 + j0 + t * kThreads);
-          if (less) y[t] = __ldcs(q + v0 + j0 + t * kThreads);
+          if (minus) y[t] = __ldcs(q + v0 + j0 + t * kThreads);
         }
 #pragma unroll
       for (int t = 0; t < U; ++t) {
         const int j = j0 + t * kThreads;
         if (j < len) {
           sp[j] = !plain && v0 + j == gone ? 0.f : x[t];
-          if (less) sq[j] = y[t];
+          if (minus) sq[j] = y[t];
         }
       }
     }
@@ -224,97 +253,74 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
     float s = 0.f, e = 0.f;
     for (int j = tid * chunk; j < min((tid + 1) * chunk, len); ++j) {
       float hi, lo, t;
-      weight(j, less, hi, lo);
+      weight(j, minus, hi, lo);
       two_sum(s, hi, s, t);
       e += t + lo;
     }
-    s_sum[tid] = make_float2(s, e);
+    mine = pair_of(s, e);
+    upto = scan<32>(mine, lane);
+    if (lane == 31) s_warp[warp] = upto;
     __syncthreads();
+    const float2 w = scan<16>(s_warp[lane & 15], lane);
+    all = from_lane(w, 15);
+    if (warp > 0) upto = add(from_lane(w, warp - 1), upto);
     return v0;
   };
-  // First warp: the sum of a lane's 16 threads and of those before them.
-  constexpr int kPer = kThreads / 32;
-  auto lane_sums = [&](double& sum, double& upto) {
-    sum = 0.0;
-    for (int i = 0; i < kPer; ++i) sum += (double)s_sum[lane * kPer + i].x + (double)s_sum[lane * kPer + i].y;
-    upto = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const double t = __shfl_up_sync(~0u, upto, o);
-      if (lane >= o) upto += t;
-    }
-  };
   for (int plain = n < k ? 0 : 1; plain < 2; ++plain) {
-    const bool less = q && !plain;
-    double mine = 0.0, sum = 0.0, upto = 0.0;
+    float2 sum = make_float2(0.f, 0.f);
     int v0 = 0;
     for (int i = 0; i < pieces; ++i) {
       v0 = stage(i, plain);
-      if (warp == 0) {
-        lane_sums(sum, upto);
-        const double t = __shfl_sync(~0u, upto, 31);
-        if (lane == 0) s_piece[i] = t;
-        mine += t;
-      }
+      if (tid == 0) s_piece[i] = all;
+      sum = add(sum, all);
     }
     if (tid < ranks) {
       const uint32_t to = ptx::dsmem_map(ptx::smem_u32(&s_part[plain][rank]), tid);
-      asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(mine) : "memory");
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(sum.x), "f"(sum.y) : "memory");
     }
     ptx::cluster_sync();
-    double total = 0.0, before = 0.0, next = 0.0;
-    int last = -1;  // the last slice that holds anything
-    for (int r = 0; r < ranks; ++r) {
-      const double t = s_part[plain][r];
-      if (r == rank) before = total;
-      total += t;
-      if (r == rank) next = total;
-      if (t > 0.0) last = r;
-    }
-    if (last < 0) continue;  // nothing: once more without q
-    const double border = u * total;
-    // the slice whose sums the border lies between (the last one that holds
-    // anything, beyond rounding)
-    if (rank == last ? border < before : !(before <= border && border < next)) return;
-    double base = before;
+    const bool part = (lane & 15) < ranks;
+    const float2 own = part ? s_part[plain][lane & 15] : make_float2(0.f, 0.f), ends = scan<16>(own, lane);
+    const float2 total = from_lane(ends, 15);
+    if (!(total.x > 0.f)) continue;  // nothing: once more without q
+    // border = u total
+    const float h = u * total.x;
+    const float2 border = pair_of(h, fmaf(u, total.x, -h) + u * total.y);
+    // the first slice that ends above the border, else the last that holds
+    // anything; of it the first piece, of that the first thread, and so on
+    const unsigned over = __ballot_sync(~0u, own.x > 0.f && less(border, ends)) & 0xFFFFu;
+    const unsigned any = __ballot_sync(~0u, own.x > 0.f) & 0xFFFFu;
+    if (rank != (over ? __ffs(over) - 1 : 31 - __clz(any))) return;
+    float2 base = rank > 0 ? from_lane(ends, rank - 1) : make_float2(0.f, 0.f);
     if (pieces > 1) {
-      int pick = -1;
-      double at = before, t = before;
+      int pick = 0;
+      float2 at = base, t = base;
       for (int i = 0; i < pieces; ++i) {
-        if (s_piece[i] > 0.0) {
+        const float2 end = add(t, s_piece[i]);
+        if (s_piece[i].x > 0.f) {
           pick = i, at = t;
-          if (border < t + s_piece[i]) break;
+          if (less(border, end)) break;
         }
-        t += s_piece[i];
+        t = end;
       }
       base = at;
       v0 = stage(pick, plain);
-      if (warp == 0) lane_sums(sum, upto);
     }
-    if (warp != 0) return;
-    // the first lane, of its chunks the first, of that chunk's values the first
-    // whose sums pass the border; else the last that holds anything
-    const unsigned over = __ballot_sync(~0u, sum > 0.0 && border < base + upto), any = __ballot_sync(~0u, sum > 0.0);
-    if (lane != (over ? __ffs(over) - 1 : 31 - __clz(any))) return;
-    double at = base + (upto - sum), t = at;
-    int pick = 0;
-    for (int i = 0; i < kPer; ++i) {
-      const double w = (double)s_sum[lane * kPer + i].x + (double)s_sum[lane * kPer + i].y;
-      if (w > 0.0) {
-        pick = lane * kPer + i, at = t;
-        if (border < t + w) break;
-      }
-      t += w;
+    if (mine.x > 0.f) {
+      if (less(border, add(base, upto))) atomicMin(&s_pick, tid);
+      atomicMax(&s_last, tid);
     }
+    __syncthreads();
+    if (tid != (s_pick < kThreads ? s_pick : s_last)) return;
+    float2 at = add(base, add(upto, make_float2(-mine.x, -mine.y)));
     int token = -1;
-    const int end = min((pick + 1) * chunk, a.vocab - v0);
-    for (int j = pick * chunk; j < end; ++j) {
+    for (int j = tid * chunk; j < min((tid + 1) * chunk, a.vocab - v0); ++j) {
       float hi, lo;
-      weight(j, less, hi, lo);
+      weight(j, q && !plain, hi, lo);
       if (hi > 0.f) {
         token = v0 + j;
-        at += (double)hi + (double)lo;
-        if (border < at) break;
+        at = add(at, make_float2(hi, lo));
+        if (less(border, at)) break;
       }
     }
     a.n_out[b] = n;
