@@ -18,27 +18,30 @@ __device__ __forceinline__ float ex2(float x) {
 // ---- probabilities -----------------------------------------------------------
 //
 // p_v = e^((x_v - max x) / T) / sum: bound by memory, each value read and written
-// once.  A cluster of CTAs per row, a slice of it in the registers of each: the
-// slice's maximum m_c, e^((x - m_c) / T) and their sum, then one exchange of
-// (m_c, sum) through distributed shared memory and the factor that is left.
-// Slices that the registers do not hold (kHeld values a thread) are read again.
-// VEC: rows in pieces of 16 bytes.
+// once.  A cluster of CTAs per row, a slice of it in the registers of each: a
+// thread's maximum m_t, e^((x - m_t) / T) and their sum, then one reduction of
+// (maximum, sum) over the block and, through distributed shared memory, the
+// cluster, and the factor that is left to each thread.  Slices that the registers
+// do not hold (kHeld values a thread) are read again.  VEC: rows in pieces of 16
+// bytes.
 
-constexpr int kHeld = 40;
+// Threads, values a thread holds, CTAs per SM.  145 rows of 152064 values, us: 512 /
+// 40 / 2 39, 256 / 40 / 4 42, 256 / 48 / 3 41, 128 / 40 / 8 45, 1024 / 24 / 1 55
+// (the copy peak takes 26).
+constexpr int kProbs = 512, kHeld = 40, kProbsCtas = 2, kProbsWarps = kProbs / 32;
 
+// (maximum, sum relative to it) of two parts; -inf: nothing there.
 __device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
-  // (maximum, sum relative to it); -inf: nothing there
   const float M = fmaxf(a.x, b.x);
   const float wa = a.x == -INFINITY ? 0.f : ex2((a.x - M) * c), wb = b.x == -INFINITY ? 0.f : ex2((b.x - M) * c);
-  return make_float2(M, a.y * wa + b.y * wb);
+  return make_float2(M, (a.x == -INFINITY ? a.y : a.y * wa) + (b.x == -INFINITY ? b.y : b.y * wb));
 }
 
 template <bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) probs_kernel(const float* logits, int vocab, int slice, float c,
-                                                         float* probs) {
+__global__ void __launch_bounds__(kProbs, kProbsCtas) probs_kernel(const float* logits, int vocab, int slice, float c,
+                                                          float* probs) {
   constexpr int W = VEC ? 4 : 1, R = kHeld / W;
-  __shared__ float s_red[kWarps];
-  __shared__ float2 s_part[16];
+  __shared__ float2 s_warp[kProbsWarps], s_part[16];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = ptx::cluster_rank(), ranks = gridDim.x;
   const int v0 = min((int)rank * slice, vocab), n = (min(v0 + slice, vocab) - v0) / W;  // pieces
@@ -64,7 +67,7 @@ __global__ void __launch_bounds__(kThreads, 2) probs_kernel(const float* logits,
   float m = -INFINITY;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int i = r * kThreads + tid;
+    const int i = r * kProbs + tid;
 #pragma unroll
     for (int e = 0; e < W; ++e) v[r][e] = -INFINITY;
     if (i < n) load(i, v[r]);
@@ -73,19 +76,12 @@ __global__ void __launch_bounds__(kThreads, 2) probs_kernel(const float* logits,
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int e = 0; e < W; ++e) m = fmaxf(m, v[r][e]);
-  for (int i = R * kThreads + tid; i < n; i += kThreads) {
+  for (int i = R * kProbs + tid; i < n; i += kProbs) {
     float t[W];
     load(i, t);
 #pragma unroll
     for (int e = 0; e < W; ++e) m = fmaxf(m, t[e]);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-  if (lane == 0) s_red[warp] = m;
-  __syncthreads();
-  m = s_red[lane % kWarps];
-#pragma unroll
-  for (int o = kWarps / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
   const float ref = m == -INFINITY ? 0.f : m;  // (e^-inf = 0; NaN passes the maximum by and reaches the sum)
   float l = 0.f;
 #pragma unroll
@@ -95,38 +91,42 @@ __global__ void __launch_bounds__(kThreads, 2) probs_kernel(const float* logits,
       v[r][e] = ex2((v[r][e] - ref) * c);
       l += v[r][e];
     }
-  for (int i = R * kThreads + tid; i < n; i += kThreads) {
+  for (int i = R * kProbs + tid; i < n; i += kProbs) {
     float t[W];
     load(i, t);
 #pragma unroll
     for (int e = 0; e < W; ++e) l += ex2((t[e] - ref) * c);
   }
-  l = warp_sum(l);
-  __syncthreads();
-  if (lane == 0) s_red[warp] = l;
-  __syncthreads();
-  l = s_red[lane % kWarps];
-#pragma unroll
-  for (int o = kWarps / 2; o > 0; o >>= 1) l += __shfl_xor_sync(~0u, l, o);
   float2 all = make_float2(m, l);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
+  if (lane == 0) s_warp[warp] = all;
+  __syncthreads();
+  all = s_warp[lane % kProbsWarps];
+#pragma unroll
+  for (int o = kProbsWarps / 2; o > 0; o >>= 1)
+    all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
   if (ranks > 1) {
     if (tid < (int)ranks) {
       const uint32_t to = ptx::dsmem_map(ptx::smem_u32(&s_part[rank]), tid);
-      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m), "f"(l) : "memory");
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(all.x), "f"(all.y) : "memory");
     }
     ptx::cluster_sync();
-    all = s_part[0];
-    for (uint32_t r = 1; r < ranks; ++r) all = join(all, s_part[r], c);
+    all = s_part[lane % ranks];
+    for (int o = ranks / 2; o > 0; o >>= 1)
+      all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
   }
-  const float f = m == -INFINITY && all.y == 0.f ? 0.f : (m == -INFINITY ? 1.f : ex2((m - all.x) * c)) / all.y;
+  // (a thread that holds nothing has zeros, a row that holds nothing gets them)
+  const float f = all.y == 0.f ? 0.f : (m == -INFINITY ? 1.f : ex2((m - all.x) * c)) / all.y;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int i = r * kThreads + tid;
+    const int i = r * kProbs + tid;
 #pragma unroll
     for (int e = 0; e < W; ++e) v[r][e] *= f;
     if (i < n) store(i, v[r]);
   }
-  for (int i = R * kThreads + tid; i < n; i += kThreads) {
+  for (int i = R * kProbs + tid; i < n; i += kProbs) {
     float t[W];
     load(i, t);
 #pragma unroll
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
   auto stage = [&](int i, bool plain) {
     const int v0 = (int)min((long long)(rank * pieces + i) * piece, (long long)a.vocab), len = min(piece, a.vocab - v0);
     const bool minus = q && !plain;
-    constexpr int U = 10;
+    constexpr int U = 20;
     __syncthreads();
     if (tid == 0) s_pick = 0x7fffffff, s_last = -1;
     for (int j0 = tid; j0 < len; j0 += U * kThreads) {
@@ -352,7 +352,7 @@ cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float t
   // CTAs per row: as many as hold it in registers, twice as many (up to 16) while
   // all of them run at once and a slice is no smaller than 2048 values
   int ranks = 1;
-  while (ranks < 16 && (ranks * kThreads * kHeld < vocab ||
+  while (ranks < 16 && (ranks * kProbs * kHeld < vocab ||
                         (ranks * 4096 <= vocab && (int64_t)rows * 2 * ranks <= device_sms())))
     ranks *= 2;
   const bool vec = vocab % 4 == 0 && ((uintptr_t)logits | (uintptr_t)probs) % 16 == 0;
@@ -363,8 +363,8 @@ cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float t
     const float* x = logits + (size_t)r0 * vocab;
     float* p = probs + (size_t)r0 * vocab;
     const cudaError_t e =
-        vec ? launch_pdl(probs_kernel<true>, dim3(ranks, n), dim3(kThreads), 0, st, ranks, x, vocab, slice, c, p)
-            : launch_pdl(probs_kernel<false>, dim3(ranks, n), dim3(kThreads), 0, st, ranks, x, vocab, slice, c, p);
+        vec ? launch_pdl(probs_kernel<true>, dim3(ranks, n), dim3(kProbs), 0, st, ranks, x, vocab, slice, c, p)
+            : launch_pdl(probs_kernel<false>, dim3(ranks, n), dim3(kProbs), 0, st, ranks, x, vocab, slice, c, p);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -374,8 +374,10 @@ cudaError_t launch_accept_sampled(const SampledArgs& a, cudaStream_t st) {
   constexpr int kSmem = 2 * kMostChunk * kThreads * 4;
   static const cudaError_t attr = cluster_attrs((const void*)accept_sampled_kernel, kSmem);
   if (attr != cudaSuccess) return attr;
-  // 16 CTAs a request while all of them run at once, else 8
-  const int ranks = a.batch * 16 <= device_sms() ? 16 : 8;
+  // 16 CTAs a request, but 8 for many requests without a draft's rows.  us, 8 / 16,
+  // vocab 152064: 4 requests 12.9 / 8.7, 16 with draft 22.3 / 17.0, 64 with draft
+  // 58 / 48, 24 without 18.8 / 19.4, 64 without 33 / 43.
+  const int ranks = a.draft || a.batch * 16 <= 2 * device_sms() ? 16 : 8;
   const int slice = (a.vocab + ranks - 1) / ranks;
   // (odd chunks: the threads' chunks start in different banks)
   int chunk = (slice + kThreads - 1) / kThreads | 1, pieces = 1;
