@@ -1,5 +1,7 @@
 // k_sampled.cu -- probabilities at a temperature (as2d_token_probs) and the
 // acceptance of drafted tokens from given random numbers (as2d_accept_sampled).
+#include <type_traits>
+
 #include "ops.h"
 #include "ptx_sm100.cuh"
 #include "small_dev.cuh"
@@ -185,9 +187,11 @@ constexpr int kMostChunk = 53;    // values of a thread's chunk at most: two row
 constexpr int kMostPieces = 128;  // pieces of a slice that shared memory holds one after another
 static_assert(kWarps == 16, "the warps' sums and the CTAs' are scanned by 16 lanes");
 
+// VEC: rows in pieces of 16 bytes.
+template <bool VEC>
 __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_constant__ SampledArgs a, int chunk,
                                                                   int pieces) {
-  extern __shared__ float s_row[];  // [512 chunks] p, then q
+  extern __shared__ __align__(16) float s_row[];  // [512 chunks] p, then q
   __shared__ float2 s_part[2][16], s_warp[kWarps], s_piece[kMostPieces];
   __shared__ int s_n, s_pick, s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -229,27 +233,33 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
   auto stage = [&](int i, bool plain) {
     const int v0 = (int)min((long long)(rank * pieces + i) * piece, (long long)a.vocab), len = min(piece, a.vocab - v0);
     const bool minus = q && !plain;
-    constexpr int U = 20;
+    using T = std::conditional_t<VEC, float4, float>;
+    constexpr int W = VEC ? 4 : 1, U = VEC ? 5 : 20;
+    const T *pv = reinterpret_cast<const T*>(p + v0), *qv = reinterpret_cast<const T*>(q + v0);
     __syncthreads();
     if (tid == 0) s_pick = 0x7fffffff, s_last = -1;
-    for (int j0 = tid; j0 < len; j0 += U * kThreads) {
-      float x[U], y[U];
+    for (int j0 = tid; j0 < len / W; j0 += U * kThreads) {
+      T x[U], y[U];
 #pragma unroll
       for (int t = 0; t < U; ++t)
-        if (j0 + t * kThreads < len) {
-          x[t] = __ldcs(p + v0 + j0 + t * kThreads);
-          if (minus) y[t] = __ldcs(q + v0 + j0 + t * kThreads);
+        if (j0 + t * kThreads < len / W) {
+          x[t] = __ldcs(pv + j0 + t * kThreads);
+          if (minus) y[t] = __ldcs(qv + j0 + t * kThreads);
         }
 #pragma unroll
       for (int t = 0; t < U; ++t) {
         const int j = j0 + t * kThreads;
-        if (j < len) {
-          sp[j] = !plain && v0 + j == gone ? 0.f : x[t];
-          if (minus) sq[j] = y[t];
+        if (j < len / W) {
+          reinterpret_cast<T*>(sp)[j] = x[t];
+          if (minus) reinterpret_cast<T*>(sq)[j] = y[t];
         }
       }
     }
     __syncthreads();
+    if (!plain && gone >= v0 && gone < v0 + len) {
+      if (tid == 0) sp[gone - v0] = 0.f;
+      __syncthreads();
+    }
     float s = 0.f, e = 0.f;
     for (int j = tid * chunk; j < min((tid + 1) * chunk, len); ++j) {
       float hi, lo, t;
@@ -372,7 +382,10 @@ cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float t
 
 cudaError_t launch_accept_sampled(const SampledArgs& a, cudaStream_t st) {
   constexpr int kSmem = 2 * kMostChunk * kThreads * 4;
-  static const cudaError_t attr = cluster_attrs((const void*)accept_sampled_kernel, kSmem);
+  static const cudaError_t attr = [] {
+    const cudaError_t e = cluster_attrs((const void*)accept_sampled_kernel<true>, kSmem);
+    return e != cudaSuccess ? e : cluster_attrs((const void*)accept_sampled_kernel<false>, kSmem);
+  }();
   if (attr != cudaSuccess) return attr;
   // 16 CTAs a request, but 8 for many requests without a draft's rows.  us, 8 / 16,
   // vocab 152064: 4 requests 12.9 / 8.7, 16 with draft 22.3 / 17.0, 64 with draft
@@ -386,7 +399,9 @@ cudaError_t launch_accept_sampled(const SampledArgs& a, cudaStream_t st) {
     pieces = (slice + chunk * kThreads - 1) / (chunk * kThreads);
   }
   const size_t smem = (size_t)(a.draft ? 2 : 1) * chunk * kThreads * 4;
-  return launch_pdl(accept_sampled_kernel, dim3(ranks, a.batch), dim3(kThreads), smem, st, ranks, a, chunk, pieces);
+  const bool vec = a.vocab % 4 == 0 && ((uintptr_t)a.probs | (uintptr_t)a.draft) % 16 == 0;
+  return launch_pdl(vec ? accept_sampled_kernel<true> : accept_sampled_kernel<false>, dim3(ranks, a.batch),
+                    dim3(kThreads), smem, st, ranks, a, chunk, pieces);
 }
 
 }  // namespace as2d
