@@ -582,6 +582,7 @@ cudaError_t launch_masked_attention(const RowMap& rm, const Model& m, KvState& s
   a.cap = s.capacity;
   a.nq = c.n_q_heads;
   a.nkv = c.n_kv_heads;
+  a.group_inv = group_inverse(a.nq, a.nkv);
   a.q = s.tree_q;
   a.q_f32 = 1;
   a.q_stride = m.q_dim;

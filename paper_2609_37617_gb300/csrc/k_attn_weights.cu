@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tslot;
   const int G = a.nq / a.nkv;
   int u0, u1;
-  unit_range(plan, a, blockIdx.x, gridDim.x, 0, u0, u1);
+  unit_range(plan, blockIdx.x, gridDim.x, u0, u1);
   const unsigned long long limit = a.timeout_ns;
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float l = 0.f;
       uint64_t vis = 0;
       if (q < n) {
-        const int i = (n0 + q) / G, h = it.g * G + (n0 + q - i * G);
+        const int i = divide_group(a, n0 + q), h = it.g * G + (n0 + q - i * G);
         l = a.lse[(size_t)(it.r0 + i) * a.nq + h] * 1.4426950408889634f;
         vis = visible_rows(a, it.r0 + i, i, it.rows);
       }

@@ -13,7 +13,9 @@
 // one CTA per SM (UnitPlan), from the lengths on the device: whatever the
 // requests' lengths, every SM streams the same number of bytes.  An item cut
 // between CTAs leaves partial results, which tree_combine_kernel joins in CTA order;
-// so results repeat bit for bit.
+// so results repeat bit for bit.  Small calls go other ways, without the second
+// kernel (Mode): one CTA to an item of up to two tiles, or a cluster of eight, which
+// joins its parts through distributed shared memory.
 //
 // Per CTA (20 warps, TMEM full: two score buffers, two accumulators):
 //   warp 0     loads key and value tiles by TMA (3D map over the layer, 128-byte
@@ -31,6 +33,8 @@
 //              stays below 2^8, in 32-bit sums).
 // 32-bit queries are bf16 hi and lo parts too (two products with K), 16-bit
 // ones are exact.
+#include <algorithm>
+
 #include "ops.h"
 #include "ptx_sm100.cuh"
 #include "small_dev.cuh"
@@ -46,6 +50,14 @@ constexpr int kThreads = 640;
 constexpr int kTurn = 5;
 // P may grow to 2^kLazy before the accumulator is rescaled.
 constexpr float kLazy = 8.f;
+
+// How the items go over the CTAs.
+enum Mode : int {
+  kShares = 0,   // even shares of all units
+  kWhole = 1,    // an item to a CTA
+  kCluster = 2,  // an item to a cluster of kRanks CTAs
+};
+constexpr int kRanks = 8;
 
 struct TreeWork {
   float4* o;   // [2 CTAs][D / 4][128] partial accumulators, four dims of a query
@@ -69,6 +81,26 @@ __device__ __forceinline__ float part_weight(float m, float M) {
   return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
 }
 
+// Adds a part's sum and four of its dims to those of maximum M.
+__device__ __forceinline__ void add_part(float2 ml, float4 v, float M, float& l, float (&x)[4]) {
+  const float w = part_weight(ml.x, M);
+  if (w != 0.f) {
+    l = fmaf(ml.y, w, l);
+    x[0] = fmaf(v.x, w, x[0]);
+    x[1] = fmaf(v.y, w, x[1]);
+    x[2] = fmaf(v.z, w, x[2]);
+    x[3] = fmaf(v.w, w, x[3]);
+  }
+}
+
+__device__ __forceinline__ void dsmem_st4(uint32_t addr, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+               : "memory");
+}
+__device__ __forceinline__ void dsmem_st2(uint32_t addr, float2 v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
+}
+
 // Which of keys [p0, p0 + 32) a row sees.
 __device__ __forceinline__ uint32_t key_bits(int p0, int L, uint64_t vis) {
   const int off = L - p0;  // prefix entries in the word
@@ -77,10 +109,9 @@ __device__ __forceinline__ uint32_t key_bits(int p0, int L, uint64_t vis) {
   return off > -64 ? (uint32_t)(vis >> -off) : 0u;
 }
 
-template <int N>
-__device__ __forceinline__ void mask_scores(uint32_t (&v)[N], uint32_t bits) {
+__device__ __forceinline__ void mask_scores(uint32_t (&v)[32], uint32_t bits) {
 #pragma unroll
-  for (int e = 0; e < N; ++e)
+  for (int e = 0; e < 32; ++e)
     if (!((bits >> e) & 1)) v[e] = 0xFF800000u;  // -inf
 }
 
@@ -139,7 +170,7 @@ __device__ __forceinline__ void write_out(const TreeArgs& a, const float* x, flo
 template <int D, bool F32>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                     const __grid_constant__ TreeArgs a, TreeWork ws, int whole, int turn) {
+                     const __grid_constant__ TreeArgs a, TreeWork ws, int mode, int turn) {
   using S = Shape<D, F32>;
   constexpr int NST = S::NST, NR = D / 64;
   extern __shared__ uint8_t smem_raw[];
@@ -147,6 +178,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* qimg = sm;
   uint8_t* ring = sm + S::Q;
+  // kCluster, over the ring once it is read: each rank's part of this CTA's dims,
+  // four of a query together, and its (maximum, sum)
+  constexpr int kQuads = D / kRanks / 4;
+  static_assert(kRanks * 128 * (kQuads * 16 + 8) <= NST * S::STAGE, "the parts fit the ring");
+  float4* recv = reinterpret_cast<float4*>(ring);                          // [rank][quad][128]
+  float2* recv_ml = reinterpret_cast<float2*>(recv + kRanks * kQuads * 128);  // [rank][128]
   float2* s_ml = reinterpret_cast<float2*>(ring + NST * S::STAGE);  // [4 groups][128] (maximum, sum)
   float* s_mx = reinterpret_cast<float*>(s_ml + 4 * 128);           // [4 groups][128] a tile's maxima
   uint64_t* full = reinterpret_cast<uint64_t*>(s_mx + 4 * 128);
@@ -193,15 +230,40 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  if (warp == 0) make_plan(a, 128, turn, lane, s_plan, blockIdx.x == 0);
+  int u0 = 0, u1 = 0;
+  Unit item{};  // kWhole, kCluster: the item, this CTA's tiles of it
+  if (mode == kShares) {
+    if (warp == 0) make_plan(a, 128, turn, lane, s_plan, blockIdx.x == 0);
+  } else {
+    // grid: (query tile and rank, kv head, request)
+    item.b = blockIdx.z;
+    item.g = blockIdx.y;
+    item.qt = mode == kCluster ? blockIdx.x / kRanks : blockIdx.x;
+    item.r0 = a.rm.start[item.b];
+    item.rows = a.rm.start[item.b + 1] - item.r0;
+    item.L = a.len[item.b];
+    const bool some = item.qt * 128 < item.rows * (a.nq / a.nkv);
+    if (some && rows_fit(item.L, item.rows, a.cap))
+      item.tiles = (item.L + item.rows + 127) / 128;
+    else if (some && tid == 0 && a.err)
+      atomicOr(a.err, kErrCapacity);
+    const int per = mode == kCluster ? (item.tiles + kRanks - 1) / kRanks : item.tiles;
+    item.t0 = mode == kCluster ? min((int)ptx::cluster_rank() * per, item.tiles) : 0;
+    item.t1 = min(item.t0 + per, item.tiles);
+    u1 = item.t0 < item.t1 ? 1 : 0;
+  }
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tslot;
-  int u0, u1;
-  unit_range(*plan, a, blockIdx.x, gridDim.x, whole, u0, u1);
+  if (mode == kShares) unit_range(*plan, blockIdx.x, gridDim.x, u0, u1);
+  auto next = [&](int& u, Unit& it) {
+    if (mode == kShares) return next_item(*plan, a, u, u1, it);
+    it = item;
+    return u++ < u1;
+  };
   Unit one;
-  if (int u = u0; warp >= 2 && next_item(*plan, a, u, u1, one)) {
+  if (int u = u0; warp >= 2 && next(u, one)) {
     // the first item's queries, by every warp that has nothing to do yet (by two
     // warps 32-bit queries of 119 rows took 5 us)
     load_queries<D, F32, kThreads - 64, 4>(a, one, tid - 64, qimg);
@@ -226,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t pol = ptx::policy_evict_first();
       uint32_t n = 0, tail = 0, turn = 0;  // slots whose last tile is on tail_full, its parity
       Unit it;
-      for (int u = u0; next_item(*plan, a, u, u1, it);) {
+      for (int u = u0; next(u, it);) {
         const int z = it.b * a.nkv + it.g;
         for (int t = it.t0; t < it.t1 && ok; ++t)
           for (int kv = 0; kv < 2; ++kv, ++n) {
@@ -265,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t items = 0, p_turn = 0, c_turn = 0;    // parities of p_full and v_clean
       uint32_t last0 = kNone, last1 = kNone, v = 0;  // value stages of the sets' last tiles, of the last tile
       Unit it;
-      for (int u = u0; ok && next_item(*plan, a, u, u1, it); ++items) {
+      for (int u = u0; ok && next(u, it); ++items) {
         const int cnt = it.t1 - it.t0, first_tail = it.L / 128 - it.t0;
         items == 0 ? wait(q_first, 0) : wait(q_full, (items - 1) & 1);
         for (int j = 0; j <= cnt && ok; ++j) {
@@ -330,10 +392,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int t64 = tid - 64;
     uint32_t n = 0, items = 0, turn = 0;
     Unit it;
-    for (int u = u0; next_item(*plan, a, u, u1, it); ++items) {
+    for (int u = u0; next(u, it); ++items) {
       if (items > 0) {
         wait(q_empty, (items - 1) & 1);
-        if (ok) load_queries<D, F32, 64, F32 ? 8 : 16>(a, it, t64, qimg);
+        if (ok) load_queries<D, F32, 64, 8>(a, it, t64, qimg);
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(q_full);
@@ -366,9 +428,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const float c = a.scale_log2;
     uint32_t ns = 0, items = 0, c_turn = 0;
     Unit it;
-    for (int u = u0; next_item(*plan, a, u, u1, it); ++items) {
+    for (int u = u0; next(u, it); ++items) {
       const int cnt = it.t1 - it.t0, nqs = it.rows * G;
-      const int q = it.qt * 128 + row, i = q / G;
+      const int q = it.qt * 128 + row, i = divide_group(a, q);
       const bool live = q < nqs;
       const bool warp_live = it.qt * 128 + 32 * quad < nqs;  // a query of the warp is
       const int h = it.g * G + (q - i * G);
@@ -383,26 +445,26 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::tc_fence_after();
           const int p0 = (it.t0 + j) * 128 + 64 * half;
           const bool tail = p0 + 64 > it.L;
-          uint32_t bits[2] = {~0u, ~0u};
-          if (tail) bits[0] = key_bits(p0, it.L, vis), bits[1] = key_bits(p0 + 32, it.L, vis);
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          {
-            uint32_t all[2][32];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) ptx::tmem_ld32(ts + 32 * x, all[x]);
+          float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int x = 0; x < 64; x += 32) {
+            uint32_t v[32];
+            ptx::tmem_ld32(ts + x, v);
             ptx::tmem_ld_wait();
+            if (tail) {
+              // -inf where the row does not see, for the second reading too
+              mask_scores(v, key_bits(p0 + x, it.L, vis));
+              ptx::tmem_st16(ts + x, v);
+              ptx::tmem_st16(ts + x + 16, v + 16);
+            }
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              if (tail) mask_scores<32>(all[x], bits[x]);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(all[x][e]));
+            for (int e = 0; e < 32; e += 4) {
+              mx[0] = max3(mx[0], __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+              mx[1] = max3(mx[1], __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
             }
           }
-          // the scores are read again below, 16 at a time: kept from here on they
-          // would not fit the registers
-          uint32_t sv[2][16];
-          ptx::tmem_ld16(ts, sv[0]);
-          const float mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          if (tail) ptx::tmem_st_wait();
+          const float mine = fmaxf(mx[0], mx[1]);
           s_mx[group * 128 + row] = mine;
           ptx::named_bar_sync(3 + 4 * set + quad, 64);
           const float mt = fmaxf(mine, s_mx[(group ^ 2) * 128 + row]) * c;
@@ -413,7 +475,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
             l = grow ? l * f : l;
             if (j >= 2) {
-              ptx::tmem_ld_wait();
 #pragma unroll 1
               for (int x = 0; x < D / 2; x += 16) {
                 uint32_t o[16];
@@ -427,27 +488,31 @@ __global__ void __launch_bounds__(kThreads, 1)
             m = m_new;
           }
           const float ref = m == -INFINITY ? 0.f : m;
-          float ls[4] = {0.f, 0.f, 0.f, 0.f};
+          const uint64_t c2 = two(c, c), ref2 = two(-ref, -ref), less = two(-1.f, -1.f);
+          uint64_t ls[2] = {0, 0};
           // P: of each 16 keys the hi parts, then the lo parts, in the place of
-          // their scores
-#pragma unroll 2
-          for (int x = 0; x < 4; ++x) {
-            uint32_t p[16];
-            uint32_t(&v)[16] = sv[x & 1];
+          // their scores (which are read a second time: they do not fit the
+          // registers)
+#pragma unroll 1
+          for (int x = 0; x < 64; x += 16) {
+            uint32_t v[16], p[16];
+            ptx::tmem_ld16(ts + x, v);
             ptx::tmem_ld_wait();
-            if (x < 3) ptx::tmem_ld16(ts + 16 * (x + 1), sv[(x + 1) & 1]);
-            if (tail) mask_scores<16>(v, (x < 2 ? bits[0] : bits[1]) >> (16 * (x & 1)));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float a0 = ex2(fmaf(__uint_as_float(v[2 * e]), c, -ref));
-              const float a1 = ex2(fmaf(__uint_as_float(v[2 * e + 1]), c, -ref));
-              ls[2 * (e & 1)] += a0;
-              ls[2 * (e & 1) + 1] += a1;
-              hi_lo(a0, a1, p[e], p[8 + e]);
+              const float2 y = of_two(fma2(two(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), c2, ref2));
+              const uint64_t w = two(ex2(y.x), ex2(y.y));
+              ls[e & 1] = add2(ls[e & 1], w);
+              const float2 f = of_two(w);
+              p[e] = pack2(f.x, f.y);
+              const float2 r = of_two(
+                  fma2(two(__uint_as_float(p[e] << 16), __uint_as_float(p[e] & 0xFFFF0000u)), less, w));
+              p[8 + e] = pack2(r.x, r.y);
             }
-            ptx::tmem_st16(ts + 16 * x, p);
+            ptx::tmem_st16(ts + x, p);
           }
-          l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+          const float2 sums = of_two(add2(ls[0], ls[1]));
+          l += sums.x + sums.y;
           ptx::tmem_st_wait();
           ptx::tc_fence_before();
         }
@@ -473,8 +538,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float w0 = part_weight(m0, M), w1 = cnt > 1 ? part_weight(m1, M) : 0.f;
       const float lt = l0 * w0 + (cnt > 1 ? l1 * w1 : 0.f);
       const unsigned long long bad = tails ? *s_bad & vis : 0ull;
+      // every CTA of the cluster has read its ring: the parts go there
+      if (mode == kCluster) ptx::cluster_sync();
       if (ok && warp_live) {
-        const bool done = it.t0 == 0 && it.t1 == it.tiles;
+        const bool done = mode == kWhole || (it.t0 == 0 && it.t1 == it.tiles && mode == kShares);
         const size_t part = (size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1);
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
 #pragma unroll 1
@@ -499,7 +566,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!(fabsf(y) <= 3.4e38f)) o[e] += y;
               }
           }
-          if (live && !done) {
+          if (live && mode == kCluster) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int quad = d0 / 4 + e;
+              dsmem_st4(ptx::dsmem_map(ptx::smem_u32(recv + (ptx::cluster_rank() * kQuads + quad % kQuads) * 128 + row),
+                                       quad / kQuads),
+                        make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]));
+            }
+          } else if (live && !done) {
             float4* dst = ws.o + (part * (D / 4) + d0 / 4) * 128 + row;
 #pragma unroll
             for (int e = 0; e < 4; ++e) dst[e * 128] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
@@ -508,7 +583,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
         }
-        if (live && group == 0) {
+        if (live && mode == kCluster) {
+          for (int r = 2 * group; r < 2 * group + 2; ++r)
+            dsmem_st2(ptx::dsmem_map(ptx::smem_u32(recv_ml + ptx::cluster_rank() * 128 + row), r), make_float2(M, lt));
+        } else if (live && group == 0) {
           if (!done)
             ws.ml[part * 128 + row] = make_float2(M, lt);
           else if (a.lse)
@@ -518,6 +596,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(o_empty);
+    }
+  }
+  if (mode == kCluster) {
+    // (the groups of a CTA with tiles have passed the first barrier above)
+    __syncwarp();
+    if (warp < 4 || u0 == u1) ptx::cluster_sync();
+    ptx::cluster_sync();
+    // the parts of four dims of a query, in rank order
+    const int t = tid - 128, quad = t >> 7, row = t & 127, q = item.qt * 128 + row, G = a.nq / a.nkv;
+    if (t >= 0 && quad < kQuads && q < item.rows * G && item.tiles > 0) {
+      const int per = (item.tiles + kRanks - 1) / kRanks, n = (item.tiles + per - 1) / per;
+      float M = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int r = 0; r < n; ++r) M = fmaxf(M, recv_ml[r * 128 + row].x);
+#pragma unroll 1
+      for (int r = 0; r < n; ++r) add_part(recv_ml[r * 128 + row], recv[(r * kQuads + quad) * 128 + row], M, l, x);
+      const int i = divide_group(a, q), h = item.g * G + (q - i * G);
+      write_out<4, F32>(a, x, l == 0.f ? 0.f : 1.f / l,
+                        ((size_t)(item.r0 + i) * a.nq + h) * D + ptx::cluster_rank() * (D / kRanks) + 4 * quad);
+      if (quad == 0 && ptx::cluster_rank() == 0 && a.lse) a.lse[(size_t)(item.r0 + i) * a.nq + h] = row_lse(M, l);
     }
   }
   ptx::tc_fence_before();
@@ -569,38 +667,44 @@ __global__ void __launch_bounds__(32 * kCombineQuads)
 #pragma unroll
     for (int k = 0; k < U; ++k)
       if (k0 + k < n) {
-        const float w = part_weight(ml[k].x, M);
-        if (w != 0.f) {
-          l = fmaf(ml[k].y, w, l);
-          x[0] = fmaf(v[k].x, w, x[0]);
-          x[1] = fmaf(v[k].y, w, x[1]);
-          x[2] = fmaf(v[k].z, w, x[2]);
-          x[3] = fmaf(v[k].w, w, x[3]);
-        }
+        add_part(ml[k], v[k], M, l, x);
       }
   }
-  const int i = q / G, h = it.g * G + (q - i * G);
+  const int i = divide_group(a, q), h = it.g * G + (q - i * G);
   write_out<4, F32>(a, x, l == 0.f ? 0.f : 1.f / l, ((size_t)(it.r0 + i) * a.nq + h) * D + 4 * quad);
   if (quad == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, l);
 }
 
-// Items of at most this many key tiles are each done by one CTA, without the
-// second kernel.
+// Items of at most this many key tiles are each done by one CTA.
 constexpr int kWholeTiles = 2;
+// A call whose clusters all run at once is done by clusters, unless its items are
+// longer than this.
+#ifndef KCT
+#define KCT 4
+#define MAXC 152
+#endif
+constexpr int kClusterTiles = KCT * kRanks;
 
 template <int D, bool F32>
 cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs& a, const TreeWork& ws,
-                   int64_t items, int most_queries, int64_t most_tiles, int sms, cudaStream_t st) {
+                   int64_t items, int most_rows, int64_t most_tiles, int sms, cudaStream_t st) {
   using S = Shape<D, F32>;
   static const cudaError_t attr = cudaFuncSetAttribute(
       tree_attn_kernel<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
   if (attr != cudaSuccess) return attr;
-  const bool whole = most_tiles <= kWholeTiles;
   const int64_t units = items * most_tiles;
-  const int ctas = (int)(whole ? items : units < sms ? units : sms), turn = !whole && units > sms ? kTurn : 0;
+  const int group = a.nq / a.nkv, most_queries = most_rows * group < 128 ? most_rows * group : 128;
+  const dim3 direct((most_rows * (a.nq / a.nkv) + 127) / 128, a.nkv, a.rm.batch);
+  if (most_tiles <= kWholeTiles)
+    return launch_pdl(tree_attn_kernel<D, F32>, direct, dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
+                      (int)kWhole, 0);
+  if (most_tiles <= kClusterTiles && items * kRanks <= MAXC)
+    return launch_pdl(tree_attn_kernel<D, F32>, dim3(direct.x * kRanks, direct.y, direct.z), dim3(kThreads), S::SMEM, st, kRanks, tk,
+                      tv, a, ws, (int)kCluster, 0);
+  const int ctas = (int)(units < sms ? units : sms), turn = units > sms ? kTurn : 0;
   const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
-                                   (int)whole, turn);
-  if (e != cudaSuccess || whole) return e;
+                                   (int)kShares, turn);
+  if (e != cudaSuccess) return e;
   return launch_pdl(tree_combine_kernel<D, F32>, dim3((unsigned)items, (most_queries + 31) / 32, D / 4 / kCombineQuads),
                     dim3(32 * kCombineQuads), 0, st, 1, a, ws, ctas, turn);
 }
@@ -629,13 +733,10 @@ size_t tree_attention_workspace(int head_dim) {
 
 cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
                                   cudaStream_t st) {
-  const int sms = device_sms(), G = a.nq / a.nkv;
+  const int sms = device_sms();
   const int64_t items = tree_items(a);
-  int most = 0;  // queries of an item
-  for (int b = 0; b < a.rm.batch; ++b) {
-    const int n = (a.rm.start[b + 1] - a.rm.start[b]) * G;
-    if (n > most) most = n < 128 ? n : 128;
-  }
+  int most = 0;  // rows of a request
+  for (int b = 0; b < a.rm.batch; ++b) most = std::max(most, a.rm.start[b + 1] - a.rm.start[b]);
   TreeWork ws;
   ws.o = (float4*)workspace;
   ws.ml = (float2*)(ws.o + (size_t)sms * 2 * 128 * head_dim / 4);

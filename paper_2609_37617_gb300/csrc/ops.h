@@ -14,6 +14,7 @@ struct TreeArgs {
   RowMap rm;                // rows of each request; may be none
   const int32_t* len;       // device [batch]
   int cap, nq, nkv;
+  uint32_t group_inv;       // 2^32 / (nq / nkv), rounded up (divide_group)
   const void* q;            // [rows][nq][d], rows q_stride elements apart
   int q_f32;
   int64_t q_stride;
@@ -27,6 +28,11 @@ struct TreeArgs {
   int32_t* err;             // error bits, nullable
   unsigned long long timeout_ns = 2000000000ull;  // limit of the kernel's waits
 };
+
+inline uint32_t group_inverse(int nq, int nkv) {
+  const uint32_t g = (uint32_t)(nq / nkv);
+  return (uint32_t)(((1ull << 32) + g - 1) / g);  // (0 for 1)
+}
 
 struct WeightArgs {
   TreeArgs t;               // out and v unused; lse is read

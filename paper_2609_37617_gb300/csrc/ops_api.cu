@@ -67,6 +67,7 @@ as2d_status check_rows(const as2d_cache* c, int32_t layer, const as2d_tree_rows*
   a.cap = c->capacity;
   a.nq = r->n_q;
   a.nkv = c->n_kv;
+  a.group_inv = group_inverse(a.nq, a.nkv);
   a.q = r->q;
   a.q_f32 = r->q_type == AS2D_TYPE_F32;
   a.q_stride = r->q_stride;

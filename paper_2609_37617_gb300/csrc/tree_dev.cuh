@@ -22,6 +22,34 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// Two floats side by side, and arithmetic on both at once.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 of_two(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// The larger of three (NaN is passed by).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&t);
@@ -51,45 +79,48 @@ struct Stage {
   static __device__ __forceinline__ uint32_t parity(uint32_t x) { return x >> 8; }
 };
 
-// The queries of an item into the operand image(s), by N threads; rows past the
-// item's queries are left as they are (what they hold reaches no other row).
+// The queries of an item into the operand image(s), by N threads (a multiple of a
+// row's chunks of 16 bytes), B chunks of a thread in flight (32-bit queries); rows
+// past the item's queries are left as they are (what they hold reaches no other row).
 template <int D, bool F32, int N, int B>
 __device__ __forceinline__ void load_queries(const TreeArgs& a, const Unit& it, int tid, uint8_t* img) {
-  constexpr int C = D / 8;  // chunks of a row (B: of a thread, loads in flight)
-  const int G = a.nq / a.nkv, n0 = it.qt * 128;
-  const int n = min(128, it.rows * G - n0) * C;
-  for (int c0 = tid; c0 < n; c0 += N * B) {
-    uint4 v[B][F32 ? 2 : 1];
+  constexpr int C = D / 8, R = N / C;  // chunks of a row, rows of a step
+  static_assert(N % C == 0, "a thread keeps its chunk");
+  const int G = a.nq / a.nkv, n0 = it.qt * 128, n = min(128, it.rows * G - n0), c = tid % C;
+  if constexpr (!F32) {
+    // straight into shared memory, every copy on its way at once
+#pragma unroll 1
+    for (int r = tid / C; r < n; r += R) {
+      const int i = divide_group(a, n0 + r), h = it.g * G + (n0 + r - i * G);
+      ptx::cp_async16(img + chunk_off(r, c), (const bf16*)a.q + (it.r0 + i) * a.q_stride + (int64_t)h * D + 8 * c);
+    }
+    ptx::cp_async_wait_all();
+  }
+#pragma unroll 1
+  for (int r0 = F32 ? tid / C : n; r0 < n; r0 += R * B) {
+    uint4 v[B][2];
 #pragma unroll
     for (int u = 0; u < B; ++u) {
-      const int c = c0 + N * u;
-      if (c < n) {
-        const int q = n0 + c / C, i = q / G, h = it.g * G + (q - i * G);
-        const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + 8 * (c % C);
-        if (F32) {
-          const uint4* s = reinterpret_cast<const uint4*>((const float*)a.q + at);
-          v[u][0] = s[0];
-          v[u][F32 ? 1 : 0] = s[1];
-        } else {
-          v[u][0] = *reinterpret_cast<const uint4*>((const bf16*)a.q + at);
-        }
+      const int r = r0 + R * u;
+      if (r < n) {
+        const int i = divide_group(a, n0 + r), h = it.g * G + (n0 + r - i * G);
+        const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + 8 * c;
+        const uint4* s = reinterpret_cast<const uint4*>((const float*)a.q + at);
+        v[u][0] = s[0];
+        v[u][1] = s[1];
       }
     }
 #pragma unroll
     for (int u = 0; u < B; ++u) {
-      const int c = c0 + N * u;
-      if (c < n) {
-        uint8_t* to = img + chunk_off(c / C, c % C);
-        if (F32) {
-          const float* x = reinterpret_cast<const float*>(&v[u][0]);
-          uint32_t h[4], l[4];
+      const int r = r0 + R * u;
+      if (r < n) {
+        uint8_t* to = img + chunk_off(r, c);
+        const float* x = reinterpret_cast<const float*>(&v[u][0]);
+        uint32_t h[4], l[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) hi_lo(x[2 * e], x[2 * e + 1], h[e], l[e]);
-          *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
-          *reinterpret_cast<uint4*>(to + 128 * D * 2) = make_uint4(l[0], l[1], l[2], l[3]);
-        } else {
-          *reinterpret_cast<uint4*>(to) = v[u][0];
-        }
+        for (int e = 0; e < 4; ++e) hi_lo(x[2 * e], x[2 * e + 1], h[e], l[e]);
+        *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(to + 128 * D * 2) = make_uint4(l[0], l[1], l[2], l[3]);
       }
     }
   }

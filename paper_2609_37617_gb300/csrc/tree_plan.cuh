@@ -22,6 +22,12 @@ struct alignas(16) UnitPlan {
   int qts[kMaxBatch];             // query tiles of a request
 };
 
+// q / G for the G query heads of a kv head: exact for q < 2^16, G <= 2^10 (the
+// inverse is off by less than 1, q times that by less than 2^32 / G).
+__device__ __forceinline__ int divide_group(const TreeArgs& a, int q) {
+  return a.group_inv == 0 ? q : (int)__umulhi((uint32_t)q, a.group_inv);
+}
+
 // What a CTA does of one item: key tiles [t0, t1) of it.
 struct Unit {
   int b, g, qt, tiles, t0, t1;
@@ -79,18 +85,8 @@ __device__ __forceinline__ bool item_at(const UnitPlan& p, const TreeArgs& a, in
 }
 
 // Units [u0, u1) of CTA c: even shares of all of them (one more for the first
-// CTAs, and no more CTAs than units), or (whole) those of item c.
-__device__ __forceinline__ void unit_range(const UnitPlan& p, const TreeArgs& a, int c, int ctas, int whole,
-                                           int& u0, int& u1) {
-  if (whole) {
-    u0 = u1 = 0;
-    if (item_at(p, a, c, u0)) {
-      int b = 0;
-      while (p.unit[b + 1] <= u0) ++b;
-      u1 = u0 + p.tiles[b] + p.extra;
-    }
-    return;
-  }
+// CTAs, and no more CTAs than units).
+__device__ __forceinline__ void unit_range(const UnitPlan& p, int c, int ctas, int& u0, int& u1) {
   const int n = p.unit[kMaxBatch], of = min(ctas, n);
   u0 = u1 = 0;
   if (c >= of) return;
@@ -133,8 +129,9 @@ __device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, in
 }
 
 // The same of the first item from u on of which there is a tile to do; u: the first
-// unit after it.  False past unit u1.
-__device__ __forceinline__ bool next_item(const UnitPlan& p, const TreeArgs& a, int& u, int u1, Unit& it) {
+// unit after it.  False past unit u1.  (Not inlined: the kernels' roles run it once
+// an item each, and are short of instruction cache.)
+static __device__ __noinline__ bool next_item(const UnitPlan& p, const TreeArgs& a, int& u, int u1, Unit& it) {
   while (u < u1) {
     it = unit_at(p, a, u, u1);
     u = it.next;
