@@ -167,7 +167,8 @@ __device__ __forceinline__ void write_out(const TreeArgs& a, const float* x, flo
   }
 }
 
-template <int D, bool F32>
+// DIRECT: kWhole, kCluster; else kShares.
+template <int D, bool F32, bool DIRECT>
 __global__ void __launch_bounds__(kThreads, 1)
     tree_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                      const __grid_constant__ TreeArgs a, TreeWork ws, int mode, int turn) {
@@ -201,7 +202,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   unsigned long long* s_bad = reinterpret_cast<unsigned long long*>(q_first + 1);
   uint32_t* tslot = reinterpret_cast<uint32_t*>(s_bad + 1);
   __shared__ UnitPlan s_plan;
-  const UnitPlan* plan = &s_plan;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -231,42 +231,44 @@ __global__ void __launch_bounds__(kThreads, 1)
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   int u0 = 0, u1 = 0;
-  Unit item{};  // kWhole, kCluster: the item, this CTA's tiles of it
-  if (mode == kShares) {
-    if (warp == 0) make_plan(a, 128, turn, lane, s_plan, blockIdx.x == 0);
-  } else {
+  Unit it;
+  if constexpr (DIRECT) {
     // grid: (query tile and rank, kv head, request)
-    item.b = blockIdx.z;
-    item.g = blockIdx.y;
-    item.qt = mode == kCluster ? blockIdx.x / kRanks : blockIdx.x;
-    item.r0 = a.rm.start[item.b];
-    item.rows = a.rm.start[item.b + 1] - item.r0;
-    item.L = a.len[item.b];
-    const bool some = item.qt * 128 < item.rows * (a.nq / a.nkv);
-    if (some && rows_fit(item.L, item.rows, a.cap))
-      item.tiles = (item.L + item.rows + 127) / 128;
+    it.b = blockIdx.z;
+    it.g = blockIdx.y;
+    it.qt = mode == kCluster ? blockIdx.x / kRanks : blockIdx.x;
+    it.r0 = a.rm.start[it.b];
+    it.rows = a.rm.start[it.b + 1] - it.r0;
+    it.L = a.len[it.b];
+    it.tiles = 0;
+    const bool some = it.qt * 128 < it.rows * (a.nq / a.nkv);
+    if (some && rows_fit(it.L, it.rows, a.cap))
+      it.tiles = (it.L + it.rows + 127) / 128;
     else if (some && tid == 0 && a.err)
       atomicOr(a.err, kErrCapacity);
-    const int per = mode == kCluster ? (item.tiles + kRanks - 1) / kRanks : item.tiles;
-    item.t0 = mode == kCluster ? min((int)ptx::cluster_rank() * per, item.tiles) : 0;
-    item.t1 = min(item.t0 + per, item.tiles);
-    u1 = item.t0 < item.t1 ? 1 : 0;
+    const int per = mode == kCluster ? (it.tiles + kRanks - 1) / kRanks : it.tiles;
+    it.t0 = mode == kCluster ? min((int)ptx::cluster_rank() * per, it.tiles) : 0;
+    it.t1 = min(it.t0 + per, it.tiles);
+    u1 = it.t0 < it.t1 ? 1 : 0;
+  } else {
+    if (warp == 0) make_plan(a, 128, turn, lane, s_plan, blockIdx.x == 0);
   }
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tslot;
-  if (mode == kShares) unit_range(*plan, blockIdx.x, gridDim.x, u0, u1);
-  auto next = [&](int& u, Unit& it) {
-    if (mode == kShares) return next_item(*plan, a, u, u1, it);
-    it = item;
-    return u++ < u1;
+  if constexpr (!DIRECT) unit_range(s_plan, blockIdx.x, gridDim.x, u0, u1);
+  // The CTA's items one after another, each with its tiles, in `it`.
+  auto next = [&](int& u) {
+    if constexpr (DIRECT)
+      return u++ < u1;
+    else
+      return next_item(s_plan, a, u, u1, it);
   };
-  Unit one;
-  if (int u = u0; warp >= 2 && next(u, one)) {
+  if (int u = u0; warp >= 2 && next(u)) {
     // the first item's queries, by every warp that has nothing to do yet (by two
     // warps 32-bit queries of 119 rows took 5 us)
-    load_queries<D, F32, kThreads - 64, 4>(a, one, tid - 64, qimg);
+    load_queries<D, F32, kThreads - 64, 4>(a, it, tid - 64, qimg);
     ptx::fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(q_first);
@@ -287,8 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       const uint64_t pol = ptx::policy_evict_first();
       uint32_t n = 0, tail = 0, turn = 0;  // slots whose last tile is on tail_full, its parity
-      Unit it;
-      for (int u = u0; next(u, it);) {
+      for (int u = u0; next(u);) {
         const int z = it.b * a.nkv + it.g;
         for (int t = it.t0; t < it.t1 && ok; ++t)
           for (int kv = 0; kv < 2; ++kv, ++n) {
@@ -326,8 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       Stage at;
       uint32_t items = 0, p_turn = 0, c_turn = 0;    // parities of p_full and v_clean
       uint32_t last0 = kNone, last1 = kNone, v = 0;  // value stages of the sets' last tiles, of the last tile
-      Unit it;
-      for (int u = u0; ok && next(u, it); ++items) {
+      for (int u = u0; ok && next(u); ++items) {
         const int cnt = it.t1 - it.t0, first_tail = it.L / 128 - it.t0;
         items == 0 ? wait(q_first, 0) : wait(q_full, (items - 1) & 1);
         for (int j = 0; j <= cnt && ok; ++j) {
@@ -391,8 +391,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp < 4) {
     const int t64 = tid - 64;
     uint32_t n = 0, items = 0, turn = 0;
-    Unit it;
-    for (int u = u0; next(u, it); ++items) {
+    for (int u = u0; next(u); ++items) {
       if (items > 0) {
         wait(q_empty, (items - 1) & 1);
         if (ok) load_queries<D, F32, 64, 8>(a, it, t64, qimg);
@@ -427,8 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int G = a.nq / a.nkv;
     const float c = a.scale_log2;
     uint32_t ns = 0, items = 0, c_turn = 0;
-    Unit it;
-    for (int u = u0; next(u, it); ++items) {
+    for (int u = u0; next(u); ++items) {
       const int cnt = it.t1 - it.t0, nqs = it.rows * G;
       const int q = it.qt * 128 + row, i = divide_group(a, q);
       const bool live = q < nqs;
@@ -539,9 +537,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float lt = l0 * w0 + (cnt > 1 ? l1 * w1 : 0.f);
       const unsigned long long bad = tails ? *s_bad & vis : 0ull;
       // every CTA of the cluster has read its ring: the parts go there
-      if (mode == kCluster) ptx::cluster_sync();
+      if (DIRECT && mode == kCluster) ptx::cluster_sync();
       if (ok && warp_live) {
-        const bool done = mode == kWhole || (it.t0 == 0 && it.t1 == it.tiles && mode == kShares);
+        const bool done = DIRECT || (it.t0 == 0 && it.t1 == it.tiles);
         const size_t part = (size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1);
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
 #pragma unroll 1
@@ -566,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!(fabsf(y) <= 3.4e38f)) o[e] += y;
               }
           }
-          if (live && mode == kCluster) {
+          if (DIRECT && live && mode == kCluster) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int quad = d0 / 4 + e;
@@ -574,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                        quad / kQuads),
                         make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]));
             }
-          } else if (live && !done) {
+          } else if (!DIRECT && live && !done) {
             float4* dst = ws.o + (part * (D / 4) + d0 / 4) * 128 + row;
 #pragma unroll
             for (int e = 0; e < 4; ++e) dst[e * 128] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
@@ -583,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
         }
-        if (live && mode == kCluster) {
+        if (DIRECT && live && mode == kCluster) {
           for (int r = 2 * group; r < 2 * group + 2; ++r)
             dsmem_st2(ptx::dsmem_map(ptx::smem_u32(recv_ml + ptx::cluster_rank() * 128 + row), r), make_float2(M, lt));
         } else if (live && group == 0) {
@@ -598,24 +596,24 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) ptx::mbar_arrive(o_empty);
     }
   }
-  if (mode == kCluster) {
+  if (DIRECT && mode == kCluster) {
     // (the groups of a CTA with tiles have passed the first barrier above)
     __syncwarp();
     if (warp < 4 || u0 == u1) ptx::cluster_sync();
     ptx::cluster_sync();
     // the parts of four dims of a query, in rank order
-    const int t = tid - 128, quad = t >> 7, row = t & 127, q = item.qt * 128 + row, G = a.nq / a.nkv;
-    if (t >= 0 && quad < kQuads && q < item.rows * G && item.tiles > 0) {
-      const int per = (item.tiles + kRanks - 1) / kRanks, n = (item.tiles + per - 1) / per;
+    const int t = tid - 128, quad = t >> 7, row = t & 127, q = it.qt * 128 + row, G = a.nq / a.nkv;
+    if (t >= 0 && quad < kQuads && q < it.rows * G && it.tiles > 0) {
+      const int per = (it.tiles + kRanks - 1) / kRanks, n = (it.tiles + per - 1) / per;
       float M = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
       for (int r = 0; r < n; ++r) M = fmaxf(M, recv_ml[r * 128 + row].x);
 #pragma unroll 1
       for (int r = 0; r < n; ++r) add_part(recv_ml[r * 128 + row], recv[(r * kQuads + quad) * 128 + row], M, l, x);
-      const int i = divide_group(a, q), h = item.g * G + (q - i * G);
+      const int i = divide_group(a, q), h = it.g * G + (q - i * G);
       write_out<4, F32>(a, x, l == 0.f ? 0.f : 1.f / l,
-                        ((size_t)(item.r0 + i) * a.nq + h) * D + ptx::cluster_rank() * (D / kRanks) + 4 * quad);
-      if (quad == 0 && ptx::cluster_rank() == 0 && a.lse) a.lse[(size_t)(item.r0 + i) * a.nq + h] = row_lse(M, l);
+                        ((size_t)(it.r0 + i) * a.nq + h) * D + ptx::cluster_rank() * (D / kRanks) + 4 * quad);
+      if (quad == 0 && ptx::cluster_rank() == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, l);
     }
   }
   ptx::tc_fence_before();
@@ -689,20 +687,25 @@ template <int D, bool F32>
 cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs& a, const TreeWork& ws,
                    int64_t items, int most_rows, int64_t most_tiles, int sms, cudaStream_t st) {
   using S = Shape<D, F32>;
-  static const cudaError_t attr = cudaFuncSetAttribute(
-      tree_attn_kernel<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
+  static const cudaError_t attr = [] {
+    const cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<D, F32, true>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
+    return e != cudaSuccess ? e
+                            : cudaFuncSetAttribute(tree_attn_kernel<D, F32, false>,
+                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
+  }();
   if (attr != cudaSuccess) return attr;
   const int64_t units = items * most_tiles;
   const int group = a.nq / a.nkv, most_queries = most_rows * group < 128 ? most_rows * group : 128;
   const dim3 direct((most_rows * (a.nq / a.nkv) + 127) / 128, a.nkv, a.rm.batch);
   if (most_tiles <= kWholeTiles)
-    return launch_pdl(tree_attn_kernel<D, F32>, direct, dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
+    return launch_pdl(tree_attn_kernel<D, F32, true>, direct, dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                       (int)kWhole, 0);
   if (most_tiles <= kClusterTiles && items * kRanks <= MAXC)
-    return launch_pdl(tree_attn_kernel<D, F32>, dim3(direct.x * kRanks, direct.y, direct.z), dim3(kThreads), S::SMEM, st, kRanks, tk,
+    return launch_pdl(tree_attn_kernel<D, F32, true>, dim3(direct.x * kRanks, direct.y, direct.z), dim3(kThreads), S::SMEM, st, kRanks, tk,
                       tv, a, ws, (int)kCluster, 0);
   const int ctas = (int)(units < sms ? units : sms), turn = units > sms ? kTurn : 0;
-  const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
+  const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                                    (int)kShares, turn);
   if (e != cudaSuccess) return e;
   return launch_pdl(tree_combine_kernel<D, F32>, dim3((unsigned)items, (most_queries + 31) / 32, D / 4 / kCombineQuads),
