@@ -68,24 +68,25 @@ __device__ __forceinline__ bool next_segment(const UnitPlan& p, const TreeArgs& 
   return false;
 }
 
-// Sum of the exponentials of 16 queries from column q0 on; masked: of those that
-// see key j of the rows' own, q < n.
+// Adds the exponentials of 16 queries from column q0 on; masked: of those that see
+// key j of the rows' own (j < 0: of all), q < n.
 template <bool MASKED>
-__device__ __forceinline__ void add_weights(const uint32_t (&v)[16], float c, const float* lse, const uint64_t* vis,
-                                            int q0, int n, int j, float (&sum)[4]) {
+__device__ __forceinline__ void add_weights(const uint32_t (&v)[16], uint64_t c2, const float* lse, const uint64_t* vis,
+                                            int q0, int n, int j, uint64_t (&sum)[2]) {
 #pragma unroll
   for (int e = 0; e < 16; e += 4) {
-    const float4 l = *reinterpret_cast<const float4*>(lse + q0 + e);
-    const float ls[4] = {l.x, l.y, l.z, l.w};
+    const float4 l = *reinterpret_cast<const float4*>(lse + q0 + e);  // (negated)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float p = ex2(fmaf(__uint_as_float(v[e + k]), c, -ls[k]));
+    for (int k = 0; k < 4; k += 2) {
+      const uint64_t less = k == 0 ? two(l.x, l.y) : two(l.z, l.w);
+      const float2 y = of_two(fma2(two(__uint_as_float(v[e + k]), __uint_as_float(v[e + k + 1])), c2, less));
+      float p0 = ex2(y.x), p1 = ex2(y.y);
       if (MASKED) {
         const int q = q0 + e + k;
-        if (q < n && (j < 0 || ((vis[q] >> j) & 1))) sum[k] += p;
-      } else {
-        sum[k] += p;
+        if (q >= n || (j >= 0 && !((vis[q] >> j) & 1))) p0 = 0.f;
+        if (q + 1 >= n || (j >= 0 && !((vis[q + 1] >> j) & 1))) p1 = 0.f;
       }
+      sum[k >> 1] = add2(sum[k >> 1], two(p0, p1));
     }
   }
 }
@@ -101,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* qimg = sm;
   uint8_t* ring = sm + S::Q;
-  float* s_lse = reinterpret_cast<float*>(ring + NST * S::STAGE);  // [128] base 2
+  float* s_lse = reinterpret_cast<float*>(ring + NST * S::STAGE);  // [128] base 2, negated
   uint64_t* s_vis = reinterpret_cast<uint64_t*>(s_lse + 128);      // [128]
   uint64_t* full = s_vis + 128;
   uint64_t* empty = full + NST;
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint64_t vis = 0;
       if (q < n) {
         const int i = divide_group(a, n0 + q), h = it.g * G + (n0 + q - i * G);
-        l = a.lse[(size_t)(it.r0 + i) * a.nq + h] * 1.4426950408889634f;
+        l = a.lse[(size_t)(it.r0 + i) * a.nq + h] * -1.4426950408889634f;
         vis = visible_rows(a, it.r0 + i, i, it.rows);
       }
       s_lse[q] = l;
@@ -183,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   Segment s;
   if (int u = u0; warp >= 2 && next_segment(plan, a, u, u1, s)) {
     // the first pass, by every warp that has nothing to do yet
-    bring(s.it, tid - 64, std::integral_constant<int, kThreads - 64>{}, std::integral_constant<int, 8>{});
+    bring(s.it, tid - 64, std::integral_constant<int, kThreads - 64>{}, std::integral_constant<int, 4>{});
     bring_sums(s.it, tid - 64, kThreads - 64);
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(q_first);
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (pass == 0) continue;
         s.it.qt = qt;
         wait(q_empty, (pass - 1) & 1);
-        if (ok) bring(s.it, tid - 64, std::integral_constant<int, 64>{}, std::integral_constant<int, 16>{});
+        if (ok) bring(s.it, tid - 64, std::integral_constant<int, 64>{}, std::integral_constant<int, 8>{});
         wait(e_empty, (pass - 1) & 1);  // the last pass's sums have been read
         if (ok) bring_sums(s.it, tid - 64, 64);
         __syncwarp();
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     const int group = (warp - 4) >> 2, row = 32 * (warp & 3) + lane;  // key of the tile, TMEM lane
     const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    const float c = a.scale_log2;
+    const uint64_t c2 = two(a.scale_log2, a.scale_log2);
     uint32_t d = 0, pass = 0;
     for (int u = u0; next_segment(plan, a, u, u1, s);) {
       float* w = wa.w + ((size_t)s.it.b * a.nkv + s.it.g) * a.cap;
@@ -286,28 +287,22 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = __all_sync(~0u, ok);
           ptx::tc_fence_after();
           const bool tail = t * 128 + 128 > s.it.L;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          uint32_t v[2][16];
-          ptx::tmem_ld16(tl + 128 * buf, v[0]);
+          uint64_t sum[2] = {0, 0};
 #pragma unroll 1
-          for (int q0 = 0; q0 < n; q0 += 32) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int q = q0 + 16 * x;
-              ptx::tmem_ld_wait();
-              if (q + 16 < n) ptx::tmem_ld16(tl + 128 * buf + q + 16, v[x ^ 1]);
-              if (q < n) {
-                if (tail || q + 16 > n)
-                  add_weights<true>(v[x], c, s_lse, s_vis, q, n, j, sum);
-                else
-                  add_weights<false>(v[x], c, s_lse, s_vis, q, n, j, sum);
-              }
-            }
+          for (int q = 0; q < n; q += 16) {
+            uint32_t v[16];
+            ptx::tmem_ld16(tl + 128 * buf + q, v);
+            ptx::tmem_ld_wait();
+            if (tail || q + 16 > n)
+              add_weights<true>(v, c2, s_lse, s_vis, q, n, j, sum);
+            else
+              add_weights<false>(v, c2, s_lse, s_vis, q, n, j, sum);
           }
+          const float2 sums = of_two(add2(sum[0], sum[1]));
           ptx::tc_fence_before();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(&s_empty[buf]);
-          if (live && ok) w[key] = before + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+          if (live && ok) w[key] = before + (sums.x + sums.y);
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(e_empty);
