@@ -688,18 +688,9 @@ class State:
 
 # ---- operators on tensors ------------------------------------------------------
 
-def _device():
-    import torch
-    return torch.cuda.current_device()
-
-
 def _tensor(t, name, device, dtypes, shape=None, contiguous=True):
     """Checks a CUDA tensor argument and returns its device address."""
-    try:
-        good = t.dtype in dtypes
-    except AttributeError:
-        good = False
-    if not good:
+    if getattr(t, "dtype", None) not in dtypes:
         raise TypeError(f"{name} must be a tensor of {' or '.join(map(str, dtypes))}")
     if t.get_device() != device:
         raise ValueError(f"{name} must be on the current CUDA device")
@@ -708,6 +699,17 @@ def _tensor(t, name, device, dtypes, shape=None, contiguous=True):
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+def _address(t, name, device, dtype, shape):
+    """The same of a contiguous tensor of one type and shape: the common case in one
+    expression, as a small call's time is the host's."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _tensor(t, name, device, (dtype,), shape)
 
 
 class Cache:
@@ -719,15 +721,17 @@ class Cache:
 
     def __init__(self, k, v):
         import torch
+        self._device = torch.cuda.current_device
+        device = self._device()
+        kp = _tensor(k, "k", device, (torch.bfloat16,))
         if k.dim() != 5:
             raise ValueError("k must have shape [n_layers, batch, n_kv, capacity, head_dim]")
-        kp = _tensor(k, "k", _device(), (torch.bfloat16,))
-        vp = _tensor(v, "v", _device(), (torch.bfloat16,), k.shape)
+        vp = _tensor(v, "v", device, (torch.bfloat16,), k.shape)
         self.k, self.v, self.shape = k, v, tuple(k.shape)
         self._c = as2d_cache(kp, vp, *self.shape)
         self._ref = ctypes.byref(self._c)
-        self._i32s = ctypes.c_int32 * self.shape[1]
-        self._f32, self._i32, self._q = (torch.float32,), (torch.int32,), (torch.bfloat16, torch.float32)
+        self._i32s, self._per_request = ctypes.c_int32 * self.shape[1], self.shape[1:2]
+        self._bf16, self._f32, self._i32, self._i64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
         self._mask = (torch.int64, torch.uint64)
         need = _I64()
         _check(_lib.as2d_tree_attention_workspace(self._ref, ctypes.byref(need)),
@@ -745,72 +749,84 @@ class Cache:
 
     def _rows(self, device, q, kv_len, rows, visible, scale, max_len):
         d = self.shape[4]
-        at = _tensor(q, "q", device, self._q, None, False)
+        at = _tensor(q, "q", device, (self._bf16, self._f32), None, False)
         shape = q.shape
-        if len(shape) != 3 or shape[2] != d or q.stride(2) != 1 or q.stride(1) != d:
+        n_q = shape[1] if len(shape) == 3 else 0
+        if n_q == 0 or shape[2] != d or q.stride()[1:] != (d, 1):
             raise ValueError(f"q must be [rows, n_q, {d}] with contiguous rows")
         n = shape[0]
         host_rows = self._counts(rows, "rows")
         if n != sum(rows):
             raise ValueError("q must have as many rows as the requests together")
+        if visible is not None:
+            if visible.dtype is self._i64:
+                visible = _address(visible, "visible", device, self._i64, shape[:1])
+            else:
+                visible = _tensor(visible, "visible", device, self._mask, shape[:1])
         r = as2d_tree_rows(
-            at, AS2D_TYPE_BF16 if q.dtype is self._q[0] else AS2D_TYPE_F32, shape[1],
-            q.stride(0) if n > 1 else shape[1] * d,  # (the stride of a single row is not looked at)
-            _tensor(kv_len, "kv_len", device, self._i32, self.shape[1:2]), max_len,
-            ctypes.addressof(host_rows),
-            None if visible is None else _tensor(visible, "visible", device, self._mask, shape[:1]),
-            d ** -0.5 if scale is None else scale)
+            at, AS2D_TYPE_BF16 if q.dtype is self._bf16 else AS2D_TYPE_F32, n_q,
+            q.stride(0) if n > 1 else n_q * d,  # (the stride of a single row is not looked at)
+            _address(kv_len, "kv_len", device, self._i32, self._per_request), max_len,
+            ctypes.addressof(host_rows), visible, d ** -0.5 if scale is None else scale)
         r.keep = host_rows  # alive as long as the descriptor
         return r
 
     def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
                        lse=None, error_bits=None, stream=0):
         """as2d_tree_attention; returns out (made like q unless given)."""
-        device = _device()
+        device = self._device()
         r = self._rows(device, q, kv_len, rows, visible, scale, max_len)
+        shape = q.shape
         if out is None:
-            out = q.new_empty(q.shape)
-        _check(_lib.as2d_tree_attention(
-            self._ref, layer, ctypes.byref(r), _tensor(out, "out", device, (q.dtype,), q.shape),
-            None if lse is None else _tensor(lse, "lse", device, self._f32, q.shape[:2]),
+            out = q.new_empty(shape)
+        st = _lib.as2d_tree_attention(
+            self._ref, layer, ctypes.byref(r), _address(out, "out", device, q.dtype, shape),
+            None if lse is None else _address(lse, "lse", device, self._f32, shape[:2]),
             *self._workspace_at,
-            None if error_bits is None else _tensor(error_bits, "error_bits", device, self._i32),
-            stream), "as2d_tree_attention")
+            None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)),
+            stream)
+        if st:
+            _check(st, "as2d_tree_attention")
         return out
 
     def attention_weights(self, q, lse, weights, kv_len, rows, visible=None, layer=0, scale=None,
                           max_len=0, error_bits=None, stream=0):
         """as2d_attention_weights: adds to weights in place."""
-        device = _device()
+        device = self._device()
         r = self._rows(device, q, kv_len, rows, visible, scale, max_len)
-        _check(_lib.as2d_attention_weights(
-            self._ref, layer, ctypes.byref(r), _tensor(lse, "lse", device, self._f32, q.shape[:2]),
-            _tensor(weights, "weights", device, self._f32, self.shape[:4]),
-            None if error_bits is None else _tensor(error_bits, "error_bits", device, self._i32),
-            stream), "as2d_attention_weights")
+        st = _lib.as2d_attention_weights(
+            self._ref, layer, ctypes.byref(r), _address(lse, "lse", device, self._f32, q.shape[:2]),
+            _address(weights, "weights", device, self._f32, self.shape[:4]),
+            None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)),
+            stream)
+        if st:
+            _check(st, "as2d_attention_weights")
 
     def evict(self, weights, kv_len, keep, recent=0, stream=0):
         """as2d_cache_evict: cuts the cache, weights and kv_len in place."""
-        device = _device()
-        _check(_lib.as2d_cache_evict(
-            self._ref, _tensor(weights, "weights", device, self._f32, self.shape[:4]),
-            _tensor(kv_len, "kv_len", device, self._i32, self.shape[1:2]),
-            self._counts(keep, "keep"), recent, *self._workspace_at, stream), "as2d_cache_evict")
+        device = self._device()
+        st = _lib.as2d_cache_evict(
+            self._ref, _address(weights, "weights", device, self._f32, self.shape[:4]),
+            _address(kv_len, "kv_len", device, self._i32, self._per_request),
+            self._counts(keep, "keep"), recent, *self._workspace_at, stream)
+        if st:
+            _check(st, "as2d_cache_evict")
 
 
 def token_probs(logits, temperature, out=None, stream=0):
     """as2d_token_probs of logits [rows, vocab]; returns out (made like logits
     unless given; may be logits)."""
     import torch
-    device, kind = _device(), (torch.float32,)
-    at = _tensor(logits, "logits", device, kind)
-    if logits.dim() != 2:
+    device, shape = torch.cuda.current_device(), logits.shape
+    at = _address(logits, "logits", device, torch.float32, shape)
+    if len(shape) != 2:
         raise ValueError("logits must be [rows, vocab]")
     if out is None:
         out = torch.empty_like(logits)
-    _check(_lib.as2d_token_probs(at, *logits.shape, temperature,
-                                 _tensor(out, "out", device, kind, logits.shape), stream),
-           "as2d_token_probs")
+    st = _lib.as2d_token_probs(at, shape[0], shape[1], temperature,
+                               _address(out, "out", device, torch.float32, shape), stream)
+    if st:
+        _check(st, "as2d_token_probs")
     return out
 
 
@@ -818,17 +834,18 @@ def accept_sampled(probs, candidates, k, u, n_accepted, token, draft_probs=None,
     """as2d_accept_sampled: probs [sum (k + 1), vocab], candidates [sum k] (or
     None), k a list, u [sum (k + 1)], n_accepted and token [batch]."""
     import torch
-    device, f32, i32 = _device(), (torch.float32,), (torch.int32,)
-    total, batch = sum(k), len(k)
-    at = _tensor(probs, "probs", device, f32)
-    if probs.dim() != 2 or probs.shape[0] != total + batch:
+    f32, i32 = torch.float32, torch.int32
+    device, total, batch, shape = torch.cuda.current_device(), sum(k), len(k), probs.shape
+    at = _address(probs, "probs", device, f32, shape)
+    if len(shape) != 2 or shape[0] != total + batch:
         raise ValueError("probs must be [sum (k + 1), vocab]")
-    vocab = probs.shape[1]
-    _check(_lib.as2d_accept_sampled(
+    st = _lib.as2d_accept_sampled(
         at, None if draft_probs is None or total == 0 else
-        _tensor(draft_probs, "draft_probs", device, f32, (total, vocab)),
+        _address(draft_probs, "draft_probs", device, f32, (total, shape[1])),
         None if candidates is None or total == 0 else
-        _tensor(candidates, "candidates", device, i32, (total,)), (ctypes.c_int32 * batch)(*k),
-        batch, vocab, _tensor(u, "u", device, f32, (total + batch,)),
-        _tensor(n_accepted, "n_accepted", device, i32, (batch,)),
-        _tensor(token, "token", device, i32, (batch,)), stream), "as2d_accept_sampled")
+        _address(candidates, "candidates", device, i32, (total,)), (ctypes.c_int32 * batch)(*k),
+        batch, shape[1], _address(u, "u", device, f32, shape[:1]),
+        _address(n_accepted, "n_accepted", device, i32, (batch,)),
+        _address(token, "token", device, i32, (batch,)), stream)
+    if st:
+        _check(st, "as2d_accept_sampled")

@@ -34,6 +34,7 @@
 // 32-bit queries are bf16 hi and lo parts too (two products with K), 16-bit
 // ones are exact.
 #include <algorithm>
+#include <atomic>
 
 #include "ops.h"
 #include "ptx_sm100.cuh"
@@ -715,10 +716,12 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
 }  // namespace
 
 int device_sms() {
+  static std::atomic<int> known[64];  // by device; 0: not asked yet
   int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1)
-    return 1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+  if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 1;
+  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 
