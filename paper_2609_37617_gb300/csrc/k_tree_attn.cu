@@ -622,56 +622,58 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 1) ptx::tmem_dealloc(tmem, 512);
 }
 
-// The parts of items cut between CTAs, joined in CTA order: a thread per query and
-// four dims, a warp over 32 queries (16 bytes each side by side in a part), eight
-// parts in flight.
-constexpr int kCombineQuads = 8;  // of a CTA: its warps
+// The parts of items cut between CTAs, joined in CTA order: a CTA per 32 queries and
+// 32 dims of an item, a lane per query (16 bytes each side by side in a part), a
+// warp per four dims, eight parts in flight.  (One CTA for all dims, a quarter of
+// the CTAs: a tree of 64 rows 50 us, now 35.)
+constexpr int kCombineWarps = 8;
 template <int D, bool F32>
-__global__ void __launch_bounds__(32 * kCombineQuads)
+__global__ void __launch_bounds__(32 * kCombineWarps)
     tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas, int turn) {
-  constexpr int U = 8;
+  constexpr int Z = D / 4 / kCombineWarps, U = 8;
   __shared__ UnitPlan plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int b = blockIdx.z, g = blockIdx.y, quad = blockIdx.x % Z * kCombineWarps + warp;
+  const int qt = blockIdx.x / Z >> 2, row = 32 * (blockIdx.x / Z & 3) + lane, q = qt * 128 + row;
+  const int r0 = a.rm.start[b], rows = a.rm.start[b + 1] - r0, G = a.nq / a.nkv;
   // The lengths before the wait: the products' kernel let this one start after
   // its own wait, so what ran before that kernel is done, and it writes none.
   ptx::griddep_launch_dependents();
+  if (q - lane >= rows * G) return;
   if (warp == 0) make_plan(a, 128, turn, lane, plan, false);
   __syncthreads();
-  int us;
-  if (!item_at(plan, a, blockIdx.x, us)) return;
-  const Unit it = unit_at(plan, a, us, 0x7fffffff);
-  const int c0 = unit_owner(plan, us + turn, ctas), c1 = unit_owner(plan, us + turn + it.tiles - 1, ctas);
-  if (c0 == c1) return;  // written by its CTA
-  const int G = a.nq / a.nkv, row = 32 * blockIdx.y + lane, q = it.qt * 128 + row;
-  if (q >= it.rows * G) return;
-  const int n = c1 - c0 + 1, quad = kCombineQuads * blockIdx.z + warp;
+  const int tiles = plan.tiles[b];
+  if (tiles == 0) return;  // skipped
+  const int first = plan.unit[b] + (g * plan.qts[b] + qt) * (tiles + turn) + turn;
+  const int c0 = unit_owner(plan, first, ctas), n = unit_owner(plan, first + tiles - 1, ctas) - c0 + 1;
+  if (n == 1 || q >= rows * G) return;  // written by its CTA
   ptx::griddep_wait();
   auto part = [&](int k) { return (size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0); };
   float M = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
   for (int k = U; k < n; ++k) M = fmaxf(M, __ldcg(&ws.ml[part(k) * 128 + row]).x);
+#pragma unroll 1
   for (int k0 = 0; k0 < n; k0 += U) {
     float2 ml[U];
     float4 v[U];
 #pragma unroll
-    for (int k = 0; k < U; ++k)
+    for (int k = 0; k < U; ++k) {
+      ml[k] = make_float2(-INFINITY, 0.f);
       if (k0 + k < n) {
         ml[k] = __ldcg(&ws.ml[part(k0 + k) * 128 + row]);
         v[k] = __ldcg(&ws.o[(part(k0 + k) * (D / 4) + quad) * 128 + row]);
       }
+    }
     if (k0 == 0) {
 #pragma unroll
-      for (int k = 0; k < U; ++k)
-        if (k < n) M = fmaxf(M, ml[k].x);
+      for (int k = 0; k < U; ++k) M = fmaxf(M, ml[k].x);
     }
 #pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (k0 + k < n) {
-        add_part(ml[k], v[k], M, l, x);
-      }
+    for (int k = 0; k < U; ++k) add_part(ml[k], v[k], M, l, x);
   }
-  const int i = divide_group(a, q), h = it.g * G + (q - i * G);
-  write_out<4, F32>(a, x, l == 0.f ? 0.f : 1.f / l, ((size_t)(it.r0 + i) * a.nq + h) * D + 4 * quad);
-  if (quad == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, l);
+  const int i = divide_group(a, q), h = g * G + (q - i * G);
+  write_out<4, F32>(a, x, l == 0.f ? 0.f : 1.f / l, ((size_t)(r0 + i) * a.nq + h) * D + 4 * quad);
+  if (quad == 0 && a.lse) a.lse[(size_t)(r0 + i) * a.nq + h] = row_lse(M, l);
 }
 
 // Items of at most this many key tiles are each done by one CTA.
@@ -697,7 +699,6 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   }();
   if (attr != cudaSuccess) return attr;
   const int64_t units = items * most_tiles;
-  const int group = a.nq / a.nkv, most_queries = most_rows * group < 128 ? most_rows * group : 128;
   const dim3 direct((most_rows * (a.nq / a.nkv) + 127) / 128, a.nkv, a.rm.batch);
   if (most_tiles <= kWholeTiles)
     return launch_pdl(tree_attn_kernel<D, F32, true>, direct, dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
@@ -709,8 +710,8 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                                    (int)kShares, turn);
   if (e != cudaSuccess) return e;
-  return launch_pdl(tree_combine_kernel<D, F32>, dim3((unsigned)items, (most_queries + 31) / 32, D / 4 / kCombineQuads),
-                    dim3(32 * kCombineQuads), 0, st, 1, a, ws, ctas, turn);
+  return launch_pdl(tree_combine_kernel<D, F32>, dim3(direct.x * 4 * (D / 4 / kCombineWarps), direct.y, direct.z),
+                    dim3(32 * kCombineWarps), 0, st, 1, a, ws, ctas, turn);
 }
 
 }  // namespace

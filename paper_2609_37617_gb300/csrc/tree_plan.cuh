@@ -71,19 +71,6 @@ __device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int ext
   if (flag && __any_sync(~0u, over) && lane == 0 && a.err) atomicOr(a.err, kErrCapacity);
 }
 
-// First unit of item n; false past the last one.
-__device__ __forceinline__ bool item_at(const UnitPlan& p, const TreeArgs& a, int n, int& u) {
-  for (int b = 0; b < a.rm.batch; ++b) {
-    const int items = p.tiles[b] > 0 ? a.nkv * p.qts[b] : 0;
-    if (n < items) {
-      u = p.unit[b] + n * (p.tiles[b] + p.extra);
-      return true;
-    }
-    n -= items;
-  }
-  return false;
-}
-
 // Units [u0, u1) of CTA c: even shares of all of them (one more for the first
 // CTAs, and no more CTAs than units).
 __device__ __forceinline__ void unit_range(const UnitPlan& p, int c, int ctas, int& u0, int& u1) {
