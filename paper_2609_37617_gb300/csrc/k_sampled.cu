@@ -39,12 +39,38 @@ __device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
   return make_float2(M, (a.x == -INFINITY ? a.y : a.y * wa) + (b.x == -INFINITY ? b.y : b.y * wb));
 }
 
+// (maximum, sum) of the row from each thread's, over the block and the cluster.
+__device__ __forceinline__ float2 join_row(float2 all, float c, uint32_t rank, uint32_t ranks, float2* s_warp,
+                                           float2* s_part) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
+  if (lane == 0) s_warp[warp] = all;
+  __syncthreads();
+  all = s_warp[lane % kProbsWarps];
+#pragma unroll
+  for (int o = kProbsWarps / 2; o > 0; o >>= 1)
+    all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
+  if (ranks > 1) {
+    if (tid < (int)ranks) {
+      const uint32_t to = ptx::dsmem_map(ptx::smem_u32(&s_part[rank]), tid);
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(all.x), "f"(all.y) : "memory");
+    }
+    ptx::cluster_sync();
+    all = s_part[lane % ranks];
+    for (int o = ranks / 2; o > 0; o >>= 1)
+      all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
+  }
+  return all;
+}
+
 template <bool VEC>
 __global__ void __launch_bounds__(kProbs, kProbsCtas) probs_kernel(const float* logits, int vocab, int slice, float c,
                                                           float* probs) {
   constexpr int W = VEC ? 4 : 1, R = kHeld / W;
   __shared__ float2 s_warp[kProbsWarps], s_part[16];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x;
   const uint32_t rank = ptx::cluster_rank(), ranks = gridDim.x;
   const int v0 = min((int)rank * slice, vocab), n = (min(v0 + slice, vocab) - v0) / W;  // pieces
   const float* x = logits + (size_t)blockIdx.y * vocab + v0;
@@ -99,26 +125,7 @@ __global__ void __launch_bounds__(kProbs, kProbsCtas) probs_kernel(const float* 
 #pragma unroll
     for (int e = 0; e < W; ++e) l += ex2((t[e] - ref) * c);
   }
-  float2 all = make_float2(m, l);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-    all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
-  if (lane == 0) s_warp[warp] = all;
-  __syncthreads();
-  all = s_warp[lane % kProbsWarps];
-#pragma unroll
-  for (int o = kProbsWarps / 2; o > 0; o >>= 1)
-    all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
-  if (ranks > 1) {
-    if (tid < (int)ranks) {
-      const uint32_t to = ptx::dsmem_map(ptx::smem_u32(&s_part[rank]), tid);
-      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(all.x), "f"(all.y) : "memory");
-    }
-    ptx::cluster_sync();
-    all = s_part[lane % ranks];
-    for (int o = ranks / 2; o > 0; o >>= 1)
-      all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
-  }
+  const float2 all = join_row(make_float2(m, l), c, rank, ranks, s_warp, s_part);
   // (a thread that holds nothing has zeros, a row that holds nothing gets them)
   const float f = all.y == 0.f ? 0.f : (m == -INFINITY ? 1.f : ex2((m - all.x) * c)) / all.y;
 #pragma unroll
@@ -134,6 +141,56 @@ __global__ void __launch_bounds__(kProbs, kProbsCtas) probs_kernel(const float* 
 #pragma unroll
     for (int e = 0; e < W; ++e) t[e] = ex2((t[e] - ref) * c) * f;
     store(i, t);
+  }
+}
+
+// The same for more rows than clusters run at once (rows in pieces of 16 bytes,
+// slices that the registers hold): the clusters stay, each goes from row to row,
+// and while a row is worked on and written the next one is on its way into shared
+// memory (each thread's own pieces, so that only the sums are waited for).
+__global__ void __launch_bounds__(kProbs, kProbsCtas) probs_rows_kernel(const float* logits, int rows, int vocab,
+                                                                       int slice, float c, float* probs) {
+  constexpr int R = kHeld / 4;
+  extern __shared__ float4 s_next[];  // [R][kProbs]
+  __shared__ float2 s_warp[2][kProbsWarps], s_part[2][16];
+  const int tid = threadIdx.x;
+  const uint32_t rank = ptx::cluster_rank(), ranks = gridDim.x;
+  const int v0 = min((int)rank * slice, vocab), n = (min(v0 + slice, vocab) - v0) / 4;  // pieces
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  auto fetch = [&](int row) {
+    const float4* x = reinterpret_cast<const float4*>(logits + (size_t)row * vocab + v0);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r * kProbs + tid < n) ptx::cp_async16(&s_next[r * kProbs + tid], x + r * kProbs + tid);
+  };
+  if ((int)blockIdx.y < rows) fetch(blockIdx.y);
+  for (int row = blockIdx.y, turn = 0; row < rows; row += gridDim.y, turn ^= 1) {
+    float4 v[R];
+    float m = -INFINITY;
+    ptx::cp_async_wait_all();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      v[r] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      if (r * kProbs + tid < n) v[r] = s_next[r * kProbs + tid];
+      m = fmaxf(m, fmaxf(fmaxf(v[r].x, v[r].y), fmaxf(v[r].z, v[r].w)));
+    }
+    if (row + (int)gridDim.y < rows) fetch(row + gridDim.y);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      v[r] = make_float4(ex2((v[r].x - ref) * c), ex2((v[r].y - ref) * c), ex2((v[r].z - ref) * c),
+                         ex2((v[r].w - ref) * c));
+      l += (v[r].x + v[r].y) + (v[r].z + v[r].w);
+    }
+    const float2 all = join_row(make_float2(m, l), c, rank, ranks, s_warp[turn], s_part[turn]);
+    const float f = all.y == 0.f ? 0.f : (m == -INFINITY ? 1.f : ex2((m - all.x) * c)) / all.y;
+    float4* p = reinterpret_cast<float4*>(probs + (size_t)row * vocab + v0);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r * kProbs + tid < n)
+        __stcs(p + r * kProbs + tid, make_float4(v[r].x * f, v[r].y * f, v[r].z * f, v[r].w * f));
   }
 }
 
@@ -368,6 +425,36 @@ cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float t
   const bool vec = vocab % 4 == 0 && ((uintptr_t)logits | (uintptr_t)probs) % 16 == 0;
   const int slice = ((vocab + ranks - 1) / ranks + 3) / 4 * 4;
   const float c = (float)(1.4426950408889634 / temperature);
+  constexpr int kNext = kHeld * kProbs * 4;
+  static const int resident = [] {
+    // clusters of eight that run at once, by the occupancy calculator less two (0: not
+    // found out): with all of them, 36, some started late (250 rows 67 us, not 56)
+    if (cluster_attrs((const void*)probs_rows_kernel, kNext) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(8, 256);
+    cfg.blockDim = dim3(kProbs);
+    cfg.dynamicSmemBytes = kNext;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 8;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, probs_rows_kernel, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return 0;
+    }
+    return n > 2 ? n - 2 : 0;
+  }();
+  // us, a cluster to a row / this, vocab 152064: 73 rows 22.7 / 21.9, 100 27.1 / 25.6,
+  // 145 38.5 / 35.4, 300 73 / 66, 400 96 / 86; 72 rows in two rounds 19.8 / 23.3, which
+  // stay with the first.
+  if (vec && ranks == 8 && rows > 2 * resident && resident > 0 && slice <= kHeld * kProbs) {
+    const int rounds = (rows + resident - 1) / resident;
+    return launch_pdl(probs_rows_kernel, dim3(8, (rows + rounds - 1) / rounds), dim3(kProbs), kNext, st, 8, logits,
+                      rows, vocab, slice, c, probs);
+  }
   for (int r0 = 0; r0 < rows; r0 += 65535) {  // (a grid's rows)
     const int n = rows - r0 < 65535 ? rows - r0 : 65535;
     const float* x = logits + (size_t)r0 * vocab;

@@ -320,7 +320,8 @@ def test_evict_equal_high_bits(lib):
 
 @pytest.mark.parametrize("rows,vocab,temperature", [
     (1, 1, 1.0), (3, 2, 0.5), (2, 31, 2.0), (5, 4096, 0.7), (2, 4097, 1.0), (1, 50001, 0.3), (9, 152064, 0.7),
-    (3, 151936, 1.3), (1, 400003, 1.0), (300, 129, 1.0)])
+    (3, 151936, 1.3), (1, 400003, 1.0), (300, 129, 1.0),
+    (75, 152064, 0.7), (103, 90004, 1.0)])
 def test_probs(lib, rows, vocab, temperature):
     g = torch.Generator(device="cuda").manual_seed(vocab)
     x = torch.randn((rows, vocab), generator=g, device="cuda") * 5
