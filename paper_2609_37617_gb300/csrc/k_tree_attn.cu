@@ -651,8 +651,6 @@ __global__ void __launch_bounds__(32 * kCombineWarps)
   auto part = [&](int k) { return (size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0); };
   float M = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-  for (int k = U; k < n; ++k) M = fmaxf(M, __ldcg(&ws.ml[part(k) * 128 + row]).x);
-#pragma unroll 1
   for (int k0 = 0; k0 < n; k0 += U) {
     float2 ml[U];
     float4 v[U];
@@ -664,10 +662,13 @@ __global__ void __launch_bounds__(32 * kCombineWarps)
         v[k] = __ldcg(&ws.o[(part(k0 + k) * (D / 4) + quad) * 128 + row]);
       }
     }
-    if (k0 == 0) {
+    const float before = M;
 #pragma unroll
-      for (int k = 0; k < U; ++k) M = fmaxf(M, ml[k].x);
-    }
+    for (int k = 0; k < U; ++k) M = fmaxf(M, ml[k].x);
+    const float w = part_weight(before, M);
+    l *= w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = w != 0.f ? x[e] * w : 0.f;
 #pragma unroll
     for (int k = 0; k < U; ++k) add_part(ml[k], v[k], M, l, x);
   }
@@ -679,12 +680,34 @@ __global__ void __launch_bounds__(32 * kCombineWarps)
 // Items of at most this many key tiles are each done by one CTA.
 constexpr int kWholeTiles = 2;
 // A call whose clusters all run at once is done by clusters, unless its items are
-// longer than this.
-#ifndef KCT
-#define KCT 4
-#define MAXC 152
-#endif
-constexpr int kClusterTiles = KCT * kRanks;
+// longer than this.  us, even shares / clusters, rows of seven queries: 4 items of
+// 1564 entries 14.0 / 9.8, 15 14.6 / 10.9, 16 (one more than run at once) 14.6 / 17.9;
+// one of 8100 14.9 / 17.3, 4 17.4 / 17.5, 15 20.7 / 18.3; 4 of 15128 19.8 / 25.5.
+constexpr int kClusterTiles = 6 * kRanks;
+
+// Clusters of the direct kernel that run at once (0: not found out).
+template <int D, bool F32>
+int resident_clusters() {
+  static const int n = [] {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kRanks * 64);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Shape<D, F32>::SMEM;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = kRanks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int most = 0;
+    if (cudaOccupancyMaxActiveClusters(&most, tree_attn_kernel<D, F32, true>, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return 0;
+    }
+    return most;
+  }();
+  return n;
+}
 
 template <int D, bool F32>
 cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs& a, const TreeWork& ws,
@@ -703,10 +726,14 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   if (most_tiles <= kWholeTiles)
     return launch_pdl(tree_attn_kernel<D, F32, true>, direct, dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                       (int)kWhole, 0);
-  if (most_tiles <= kClusterTiles && items * kRanks <= MAXC)
+  if (most_tiles <= kClusterTiles && items <= resident_clusters<D, F32>())
     return launch_pdl(tree_attn_kernel<D, F32, true>, dim3(direct.x * kRanks, direct.y, direct.z), dim3(kThreads), S::SMEM, st, kRanks, tk,
                       tv, a, ws, (int)kCluster, 0);
-  const int ctas = (int)(units < sms ? units : sms), turn = units > sms ? kTurn : 0;
+  // No more CTAs to an item than pay for the joining of their parts.  us, one item
+  // of 8100 / 15128 / 60000 entries: at most 16 15.7 / 20.2 / 46.5, 32 14.9 / 17.8 / 30.7,
+  // 64 18.4 / 19.0 / 26.5, as many as there are SMs 18.4 / 25.5 / 38.8.
+  const int64_t most_ctas = items * (16 + most_tiles / 8);
+  const int ctas = (int)std::min(std::min<int64_t>(units, sms), most_ctas), turn = units > sms ? kTurn : 0;
   const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                                    (int)kShares, turn);
   if (e != cudaSuccess) return e;
