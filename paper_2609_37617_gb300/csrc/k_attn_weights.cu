@@ -317,9 +317,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <int D, bool F32>
 cudaError_t launch(const CUtensorMap& tk, const WeightArgs& a, int ctas, int turn, cudaStream_t st) {
   using S = Shape<D, F32>;
-  static const cudaError_t attr = cudaFuncSetAttribute(
-      attn_weights_kernel<D, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
-  if (attr != cudaSuccess) return attr;
+  static PerDevice opted;
+  const cudaError_t e = opt_in(opted, attn_weights_kernel<D, F32>, S::SMEM);
+  if (e != cudaSuccess) return e;
   return launch_pdl(attn_weights_kernel<D, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, a, turn);
 }
 

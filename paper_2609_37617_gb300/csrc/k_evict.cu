@@ -19,7 +19,6 @@
 namespace as2d {
 namespace {
 
-constexpr int kSel = 1024;   // threads of the selection
 // Digits of the radix selection, 11 + 11 + 10 bits from the top: the first takes
 // in the exponent and two bits of the mantissa, so that weights of one size still
 // fall into several bins (8-bit digits put them into one or two, whose counts
@@ -33,27 +32,30 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Exclusive prefix of v over the block (warps in order, every thread of a warp
-// passing the warp's value); total: the sum.
-__device__ __forceinline__ int warp_prefix(int v, int* s, int* total) {
+// Exclusive prefix of v over the block's W warps in order (every thread of a warp
+// passing the warp's value).
+template <int W>
+__device__ __forceinline__ int warp_prefix(int v, int* s) {
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
   __syncthreads();
   if (lane == 0) s[w] = v;
   __syncthreads();
-  int before = 0, all = 0;
-  for (int i = 0; i < kSel / 32; ++i) {
-    before += i < w ? s[i] : 0;
-    all += s[i];
+  const int mine = lane < W ? s[lane] : 0;
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < W; o <<= 1) {
+    const int t = __shfl_up_sync(~0u, upto, o);
+    if (lane >= o) upto += t;
   }
-  *total = all;
-  return before;
+  return __shfl_sync(~0u, upto - mine, w);
 }
 
-// E: entries of a thread (a warp's are consecutive, 32 at a time), kept in
-// registers as keys.
-template <int E>
-__global__ void __launch_bounds__(kSel) evict_select_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ int hist[kPasses * kBins], s_w[32], s_pick[2];
+// T threads, E entries of a thread (a warp's are consecutive, 32 at a time), which
+// stay in registers.
+template <int T, int E>
+__global__ void __launch_bounds__(T) evict_select_kernel(const __grid_constant__ EvictArgs a) {
+  constexpr int W = T / 32, B = kBins / T;  // warps, bins of a thread
+  __shared__ int hist[kPasses * kBins], s_w[W], s_pick[2];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int unit = blockIdx.x, b = (unit / a.nkv) % a.batch;
@@ -71,7 +73,7 @@ __global__ void __launch_bounds__(kSel) evict_select_kernel(const __grid_constan
   float x[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) x[i] = t0 + 32 * i < L ? wt[t0 + 32 * i] : 0.f;
-  for (int i = tid; i < kPasses * kBins; i += kSel) hist[i] = 0;
+  for (int i = tid; i < kPasses * kBins; i += T) hist[i] = 0;
   __syncthreads();
   uint32_t prefix = 0, mask = 0;
 #pragma unroll 1
@@ -85,20 +87,26 @@ __global__ void __launch_bounds__(kSel) evict_select_kernel(const __grid_constan
       if (t0 + 32 * i < old && (key & mask) == prefix) atomicAdd(&h[(key >> shift) & digit], 1);
     }
     __syncthreads();
-    // the bin in which the count from above reaches `want`: two bins a thread,
-    // the highest first
-    const int bin = kBins - 1 - 2 * tid, c0 = h[bin], c1 = h[bin - 1];
-    int upto = c0 + c1, all;
+    // the bin in which the count from above reaches `want`: B bins a thread, the
+    // highest first
+    const int bin = kBins - 1 - B * tid;
+    int c[B], sum = 0;
+#pragma unroll
+    for (int i = 0; i < B; ++i) sum += c[i] = h[bin - i];
+    int upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int t = __shfl_up_sync(~0u, upto, o);
       if (lane >= o) upto += t;
     }
-    const int before = warp_prefix(__shfl_sync(~0u, upto, 31), s_w, &all) + upto - c0 - c1;
-    if (before < want && want <= before + c0 + c1) {
-      const bool lower = before + c0 < want;
-      s_pick[0] = bin - (lower ? 1 : 0);
-      s_pick[1] = before + (lower ? c0 : 0);
+    int n = warp_prefix<W>(__shfl_sync(~0u, upto, 31), s_w) + upto - sum;
+    if (n < want && want <= n + sum) {
+      int i = 0;
+#pragma unroll
+      for (int k = 0; k < B - 1; ++k)
+        if (i == k && n + c[k] < want) n += c[k], ++i;
+      s_pick[0] = bin - i;
+      s_pick[1] = n;
     } else if (want == 0 && tid == 0) {  // none of them: nothing is above the highest key
       s_pick[0] = digit;
       s_pick[1] = 0;
@@ -110,11 +118,11 @@ __global__ void __launch_bounds__(kSel) evict_select_kernel(const __grid_constan
   }
   // entries above the threshold stay, and the first `want` equal to it
   const unsigned below = (1u << lane) - 1;
-  int ties = 0, all;
+  int ties = 0;
 #pragma unroll
   for (int i = 0; i < E; ++i)
     ties += __popc(__ballot_sync(~0u, t0 + 32 * i < old && evict_key(x[i]) == prefix));
-  int tie = warp_prefix(ties, s_w, &all);
+  int tie = warp_prefix<W>(ties, s_w);
   uint32_t stay[(E + 31) / 32] = {};
   int n = 0;
 #pragma unroll
@@ -128,7 +136,7 @@ __global__ void __launch_bounds__(kSel) evict_select_kernel(const __grid_constan
     if (yes) stay[i / 32] |= 1u << (i % 32);
     n += __popc(__ballot_sync(~0u, yes));
   }
-  int j = warp_prefix(n, s_w, &all), first = keep;
+  int j = warp_prefix<W>(n, s_w), first = keep;
   // (every weight is in a register by now: their places can be written)
 #pragma unroll
   for (int i = 0; i < E; ++i) {
@@ -212,10 +220,12 @@ void cache_evict_carve(EvictArgs& a, int64_t units, void* workspace) {
 
 cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, cudaStream_t st) {
   const unsigned units = (unsigned)(a.n_layers * a.batch * a.nkv);
+  // (an eviction of 200 entries of the tiny decoder takes 17.0 us with 1024 threads,
+  // 13.5 with 256: fewer warps wait for one another)
   const cudaError_t e =
-      a.cap <= 4 * kSel    ? launch_pdl(evict_select_kernel<4>, dim3(units), dim3(kSel), 0, st, 1, a)
-      : a.cap <= 16 * kSel ? launch_pdl(evict_select_kernel<16>, dim3(units), dim3(kSel), 0, st, 1, a)
-                           : launch_pdl(evict_select_kernel<64>, dim3(units), dim3(kSel), 0, st, 1, a);
+      a.cap <= 4096    ? launch_pdl(evict_select_kernel<256, 16>, dim3(units), dim3(256), 0, st, 1, a)
+      : a.cap <= 16384 ? launch_pdl(evict_select_kernel<1024, 16>, dim3(units), dim3(1024), 0, st, 1, a)
+                       : launch_pdl(evict_select_kernel<1024, 64>, dim3(units), dim3(1024), 0, st, 1, a);
   if (e != cudaSuccess) return e;
   return head_dim == 128 ? launch_pdl(evict_move_kernel<128>, dim3(units, 4), dim3(kMove), 0, st, 1, a)
                          : launch_pdl(evict_move_kernel<64>, dim3(units, 2), dim3(kMove), 0, st, 1, a);

@@ -400,22 +400,16 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
   }
 }
 
-cudaError_t cluster_attrs(const void* kernel, int smem) {
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  return e != cudaSuccess || smem == 0
-             ? e
-             : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-}
-
 }  // namespace
 
 cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float temperature, float* probs,
                                cudaStream_t st) {
-  static const cudaError_t attr = [] {
-    const cudaError_t e = cluster_attrs((const void*)probs_kernel<true>, 0);
-    return e != cudaSuccess ? e : cluster_attrs((const void*)probs_kernel<false>, 0);
-  }();
-  if (attr != cudaSuccess) return attr;
+  constexpr int kNext = kHeld * kProbs * 4;
+  static PerDevice opted[3], clusters;
+  cudaError_t e = opt_in(opted[0], probs_kernel<true>, 0, true);
+  if (e == cudaSuccess) e = opt_in(opted[1], probs_kernel<false>, 0, true);
+  if (e == cudaSuccess) e = opt_in(opted[2], probs_rows_kernel, kNext);
+  if (e != cudaSuccess) return e;
   // CTAs per row: as many as hold it in registers, twice as many (up to 16) while
   // all of them run at once and a slice is no smaller than 2048 values
   int ranks = 1;
@@ -425,28 +419,9 @@ cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float t
   const bool vec = vocab % 4 == 0 && ((uintptr_t)logits | (uintptr_t)probs) % 16 == 0;
   const int slice = ((vocab + ranks - 1) / ranks + 3) / 4 * 4;
   const float c = (float)(1.4426950408889634 / temperature);
-  constexpr int kNext = kHeld * kProbs * 4;
-  static const int resident = [] {
-    // clusters of eight that run at once, by the occupancy calculator less two (0: not
-    // found out): with all of them, 36, some started late (250 rows 67 us, not 56)
-    if (cluster_attrs((const void*)probs_rows_kernel, kNext) != cudaSuccess) return 0;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(8, 256);
-    cfg.blockDim = dim3(kProbs);
-    cfg.dynamicSmemBytes = kNext;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 8;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, probs_rows_kernel, &cfg) != cudaSuccess) {
-      (void)cudaGetLastError();
-      return 0;
-    }
-    return n > 2 ? n - 2 : 0;
-  }();
+  // the clusters of eight that run at once, by the occupancy calculator less two: with
+  // all of them, 36, some started late (250 rows 67 us, not 56)
+  const int resident = resident_clusters(clusters, probs_rows_kernel, kProbs, kNext, 8) - 2;
   // us, a cluster to a row / this, vocab 152064: 73 rows 22.7 / 21.9, 100 27.1 / 25.6,
   // 145 38.5 / 35.4, 300 73 / 66, 400 96 / 86; 72 rows in two rounds 19.8 / 23.3, which
   // stay with the first.
@@ -459,8 +434,7 @@ cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float t
     const int n = rows - r0 < 65535 ? rows - r0 : 65535;
     const float* x = logits + (size_t)r0 * vocab;
     float* p = probs + (size_t)r0 * vocab;
-    const cudaError_t e =
-        vec ? launch_pdl(probs_kernel<true>, dim3(ranks, n), dim3(kProbs), 0, st, ranks, x, vocab, slice, c, p)
+    e = vec ? launch_pdl(probs_kernel<true>, dim3(ranks, n), dim3(kProbs), 0, st, ranks, x, vocab, slice, c, p)
             : launch_pdl(probs_kernel<false>, dim3(ranks, n), dim3(kProbs), 0, st, ranks, x, vocab, slice, c, p);
     if (e != cudaSuccess) return e;
   }
@@ -469,11 +443,10 @@ cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float t
 
 cudaError_t launch_accept_sampled(const SampledArgs& a, cudaStream_t st) {
   constexpr int kSmem = 2 * kMostChunk * kThreads * 4;
-  static const cudaError_t attr = [] {
-    const cudaError_t e = cluster_attrs((const void*)accept_sampled_kernel<true>, kSmem);
-    return e != cudaSuccess ? e : cluster_attrs((const void*)accept_sampled_kernel<false>, kSmem);
-  }();
-  if (attr != cudaSuccess) return attr;
+  static PerDevice opted[2];
+  cudaError_t e = opt_in(opted[0], accept_sampled_kernel<true>, kSmem, true);
+  if (e == cudaSuccess) e = opt_in(opted[1], accept_sampled_kernel<false>, kSmem, true);
+  if (e != cudaSuccess) return e;
   // 16 CTAs a request, but 8 for many requests without a draft's rows.  us, 8 / 16,
   // vocab 152064: 4 requests 12.9 / 8.7, 16 with draft 22.3 / 17.0, 64 with draft
   // 58 / 48, 24 without 18.8 / 19.4, 64 without 33 / 43.

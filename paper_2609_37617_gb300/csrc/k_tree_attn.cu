@@ -34,7 +34,6 @@
 // 32-bit queries are bf16 hi and lo parts too (two products with K), 16-bit
 // ones are exact.
 #include <algorithm>
-#include <atomic>
 
 #include "ops.h"
 #include "ptx_sm100.cuh"
@@ -638,16 +637,16 @@ __global__ void __launch_bounds__(32 * kCombineWarps)
   const int r0 = a.rm.start[b], rows = a.rm.start[b + 1] - r0, G = a.nq / a.nkv;
   // The lengths before the wait: the products' kernel let this one start after
   // its own wait, so what ran before that kernel is done, and it writes none.
+  // (No CTA ends before it: what follows in the stream waits for this kernel.)
   ptx::griddep_launch_dependents();
-  if (q - lane >= rows * G) return;
   if (warp == 0) make_plan(a, 128, turn, lane, plan, false);
   __syncthreads();
   const int tiles = plan.tiles[b];
-  if (tiles == 0) return;  // skipped
   const int first = plan.unit[b] + (g * plan.qts[b] + qt) * (tiles + turn) + turn;
-  const int c0 = unit_owner(plan, first, ctas), n = unit_owner(plan, first + tiles - 1, ctas) - c0 + 1;
-  if (n == 1 || q >= rows * G) return;  // written by its CTA
+  const int c0 = tiles > 0 ? unit_owner(plan, first, ctas) : 0;
+  const int n = tiles > 0 ? unit_owner(plan, first + tiles - 1, ctas) - c0 + 1 : 0;
   ptx::griddep_wait();
+  if (n <= 1 || q >= rows * G) return;  // skipped, or written by its CTA
   auto part = [&](int k) { return (size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0); };
   float M = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
@@ -685,48 +684,21 @@ constexpr int kWholeTiles = 2;
 // one of 8100 14.9 / 17.3, 4 17.4 / 17.5, 15 20.7 / 18.3; 4 of 15128 19.8 / 25.5.
 constexpr int kClusterTiles = 6 * kRanks;
 
-// Clusters of the direct kernel that run at once (0: not found out).
-template <int D, bool F32>
-int resident_clusters() {
-  static const int n = [] {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kRanks * 64);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Shape<D, F32>::SMEM;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = kRanks;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    int most = 0;
-    if (cudaOccupancyMaxActiveClusters(&most, tree_attn_kernel<D, F32, true>, &cfg) != cudaSuccess) {
-      (void)cudaGetLastError();
-      return 0;
-    }
-    return most;
-  }();
-  return n;
-}
-
 template <int D, bool F32>
 cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs& a, const TreeWork& ws,
                    int64_t items, int most_rows, int64_t most_tiles, int sms, cudaStream_t st) {
   using S = Shape<D, F32>;
-  static const cudaError_t attr = [] {
-    const cudaError_t e = cudaFuncSetAttribute(tree_attn_kernel<D, F32, true>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
-    return e != cudaSuccess ? e
-                            : cudaFuncSetAttribute(tree_attn_kernel<D, F32, false>,
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
-  }();
-  if (attr != cudaSuccess) return attr;
+  static PerDevice opted[2], clusters;
+  cudaError_t e = opt_in(opted[0], tree_attn_kernel<D, F32, true>, S::SMEM);
+  if (e == cudaSuccess) e = opt_in(opted[1], tree_attn_kernel<D, F32, false>, S::SMEM);
+  if (e != cudaSuccess) return e;
   const int64_t units = items * most_tiles;
   const dim3 direct((most_rows * (a.nq / a.nkv) + 127) / 128, a.nkv, a.rm.batch);
   if (most_tiles <= kWholeTiles)
     return launch_pdl(tree_attn_kernel<D, F32, true>, direct, dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                       (int)kWhole, 0);
-  if (most_tiles <= kClusterTiles && items <= resident_clusters<D, F32>())
+  if (most_tiles <= kClusterTiles &&
+      items <= resident_clusters(clusters, tree_attn_kernel<D, F32, true>, kThreads, S::SMEM, kRanks))
     return launch_pdl(tree_attn_kernel<D, F32, true>, dim3(direct.x * kRanks, direct.y, direct.z), dim3(kThreads), S::SMEM, st, kRanks, tk,
                       tv, a, ws, (int)kCluster, 0);
   // No more CTAs to an item than pay for the joining of their parts.  us, one item
@@ -734,7 +706,7 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   // 64 18.4 / 19.0 / 26.5, as many as there are SMs 18.4 / 25.5 / 38.8.
   const int64_t most_ctas = items * (16 + most_tiles / 8);
   const int ctas = (int)std::min(std::min<int64_t>(units, sms), most_ctas), turn = units > sms ? kTurn : 0;
-  const cudaError_t e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
+  e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                                    (int)kShares, turn);
   if (e != cudaSuccess) return e;
   return launch_pdl(tree_combine_kernel<D, F32>, dim3(direct.x * 4 * (D / 4 / kCombineWarps), direct.y, direct.z),
@@ -744,13 +716,15 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
 }  // namespace
 
 int device_sms() {
-  static std::atomic<int> known[64];  // by device; 0: not asked yet
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return 1;
-  if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
-  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 1;
-  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
-  return n;
+  static PerDevice sms;
+  const int n = sms.get([] {
+    int dev = 0, count = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+      return -1;
+    return count;
+  });
+  return n > 0 ? n : 1;
 }
 
 int64_t tree_items(const TreeArgs& a) {

@@ -3,9 +3,63 @@
 // and the state's calls (as2d_api.cu).
 #pragma once
 
+#include <atomic>
+
 #include "as2d_internal.h"
 
 namespace as2d {
+
+// What is found out or set once per device (a kernel's attributes, how many of its
+// clusters run at once): `ask` gives a value >= 0, asked again until it does.
+struct PerDevice {
+  std::atomic<int> value[64] = {};  // + 1; 0: not asked yet
+  template <typename F>
+  int get(F ask) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return -1;
+    if (dev < 64)
+      if (const int v = value[dev].load(std::memory_order_acquire)) return v - 1;
+    const int v = ask();
+    if (v >= 0 && dev < 64) value[dev].store(v + 1, std::memory_order_release);
+    return v;
+  }
+};
+
+// Opts a kernel into `smem` bytes of dynamic shared memory on the current device
+// (and, with `big`, into clusters of more than eight).
+template <typename K>
+cudaError_t opt_in(PerDevice& done, K* kernel, int smem, bool big = false) {
+  cudaError_t e = cudaSuccess;
+  done.get([&] {
+    if (smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && big) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e == cudaSuccess ? 0 : -1;
+  });
+  return e;
+}
+
+// Clusters of `ranks` CTAs of a kernel that run at once on the current device (0:
+// not found out).
+template <typename K>
+int resident_clusters(PerDevice& known, K* kernel, int threads, int smem, int ranks) {
+  const int n = known.get([&] {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ranks * 256);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ranks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int most = 0;
+    if (cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) == cudaSuccess) return most;
+    (void)cudaGetLastError();
+    return 0;
+  });
+  return n > 0 ? n : 0;
+}
 
 constexpr int kMaxTree = AS2D_MAX_TREE;
 

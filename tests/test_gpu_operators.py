@@ -98,6 +98,22 @@ def test_attention_ragged(lib, heads, q_type):
     check_attention(x, *run_attention(lib, x, layer=1), layer=1)
     # the bound of the lengths sizes the launch and nothing else
     check_attention(x, *run_attention(lib, x, layer=1, max_len=3333), layer=1)
+    check_attention(x, *run_attention(lib, x, layer=1, max_len=1), layer=1)  # (too low a bound)
+
+
+@pytest.mark.parametrize("requests", [1, 3, 4, 12])
+def test_attention_whole_items_and_clusters(lib, requests):
+    """Lengths on both sides of what one CTA, a cluster of them and even shares do."""
+    rng = np.random.default_rng(requests)
+    for longest in (255, 257, 2000, 5000, 7000):
+        lens = [int(t) for t in rng.integers(0, longest, requests)]
+        lens[0] = longest
+        rows = [int(t) for t in rng.integers(0, 6, requests)]
+        rows[0] = 2
+        for heads in ((28, 4, 128), (4, 2, 64)):
+            for q_type in (torch.bfloat16, torch.float32):
+                x = Inputs(heads, lens, rows, ref.tree_masks(rows, rng), q_type, seed=longest)
+                check_attention(x, *run_attention(lib, x, max_len=longest))
 
 
 @pytest.mark.parametrize("length", [6000, 15128])
@@ -321,7 +337,7 @@ def test_evict_equal_high_bits(lib):
 @pytest.mark.parametrize("rows,vocab,temperature", [
     (1, 1, 1.0), (3, 2, 0.5), (2, 31, 2.0), (5, 4096, 0.7), (2, 4097, 1.0), (1, 50001, 0.3), (9, 152064, 0.7),
     (3, 151936, 1.3), (1, 400003, 1.0), (300, 129, 1.0),
-    (75, 152064, 0.7), (103, 90004, 1.0)])
+    (75, 152064, 0.7), (103, 90004, 1.0), (2, 500000, 1.0), (70000, 5, 1.0)])
 def test_probs(lib, rows, vocab, temperature):
     g = torch.Generator(device="cuda").manual_seed(vocab)
     x = torch.randn((rows, vocab), generator=g, device="cuda") * 5
@@ -378,7 +394,8 @@ def run_accept(lib, probs, draft, cand, ks, u):
 
 
 @pytest.mark.parametrize("with_draft", [False, True])
-@pytest.mark.parametrize("vocab,live", [(1, 1), (2, 2), (33, 20), (1000, 40), (4096, 4096), (152064, 3000), (151937, 500)])
+@pytest.mark.parametrize("vocab,live", [(1, 1), (2, 2), (33, 20), (1000, 40), (4096, 4096), (152064, 3000), (151937, 500),
+                                        (1000004, 5000), (1000003, 5000)])
 def test_accept(lib, vocab, live, with_draft):
     rng = np.random.default_rng(vocab + with_draft)
     for ks in ([0], [1], [16], [0, 3, 16, 1, 8, 0, 5]):
