@@ -320,8 +320,6 @@ as2d_status alloc_work(KvState& s, const Model& m, int batch, int capacity,
   s.d_len = cv.take<int32_t>(batch);
   s.d_root = cv.take<int32_t>(batch);
   s.d_err = cv.take<int32_t>(batch + 1);
-  s.d_off = cv.take<int32_t>(batch);
-  s.d_floor = cv.take<int32_t>(batch);
   s.h = cv.take<float>(R * H);
   s.xn = cv.take<bf16>(2 * R * H);
   s.ao = cv.take<bf16>(2 * R * m.q_dim);
@@ -340,6 +338,8 @@ as2d_status alloc_work(KvState& s, const Model& m, int batch, int capacity,
   s.attn_ml = cv.take<float2>(attn_rows);
   s.attn_cnt = cv.take<int>(attn_items * 8);
   s.n_attn_cnt = (int)attn_items * 8;
+  s.d_off = cv.take<int32_t>(batch);
+  s.d_floor = cv.take<int32_t>(batch);
   bool ok = encode_cache_map(&s.tm_kc, s.k_cache, m.cfg.head_dim, capacity,
                              (int64_t)m.cfg.n_layers * batch * m.cfg.n_kv_heads) &&
             encode_cache_map(&s.tm_vc, s.v_cache, m.cfg.head_dim, capacity,

@@ -111,7 +111,6 @@ struct AttnArgs {
   bf16* kc;
   bf16* vc;
   uint8_t* qimg;          // [batch][nkv][qt_max] operand images, 256 d bytes each
-  float* q32;             // not null: queries go here instead, unscaled, [rows][nq][d]
   int qt_max;
   float* ws_o;            // [batch][nkv][qt_max][chunks_max][64][d] chunk partials
   float2* ws_ml;          // [batch][nkv][qt_max][chunks_max][64] (max, sum), base 2
@@ -127,6 +126,7 @@ struct AttnArgs {
   // query tile (chunks covering the host's bound of the request's keys)
   int32_t cl_start[kMaxBatch + 1];
   int32_t n_ch[kMaxBatch];
+  float* q32;             // Q32: [rows][nq][d] unscaled queries
 };
 
 // ---- finishing the QKV projection from its split-K sums ----------------------
@@ -156,8 +156,9 @@ __device__ __forceinline__ int hi_row(int q) { return (q >> 3) * 16 + (q & 7); }
 // dependent launch is triggered after the wait: attention CTAs that start
 // before it read the requests' lengths (and measured slower: 7B k = 8 2784 ->
 // 2810 us).
+// Q32: queries go to q32 as they are, for as2d_verify_tree's attention.
 constexpr int kQkvWarps = 8;  // warps of one CTA, two heads each
-template <int D>
+template <int D, bool Q32>
 __global__ void __launch_bounds__(32 * kQkvWarps) qkv_finish_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int H2 = D / 2, V = H2 / 16;
   const int gm = blockIdx.x, head = 2 * (blockIdx.y * kQkvWarps + threadIdx.y) + (threadIdx.x >> 4);
@@ -238,7 +239,7 @@ __global__ void __launch_bounds__(32 * kQkvWarps) qkv_finish_kernel(const __grid
     else
       *reinterpret_cast<uint32_t*>(to) = w[0];
   };
-  if (is_q && a.q32) {
+  if (Q32 && is_q) {
     float* to = a.q32 + ((size_t)gm * a.nq + head) * D + e;
 #pragma unroll
     for (int u = 0; u < V; ++u) to[u] = y0[u], to[u + H2] = y1[u];
@@ -1371,8 +1372,8 @@ cudaError_t launch_attention_split(const RowMap& m, const Model& md, KvState& kv
   const dim3 bf(32, kQkvWarps);
   if (q32) {
     ++kv.launches;
-    return c.head_dim == 128 ? launch_pdl(qkv_finish_kernel<128>, gf, bf, 0, st, 1, a)
-                             : launch_pdl(qkv_finish_kernel<64>, gf, bf, 0, st, 1, a);
+    return c.head_dim == 128 ? launch_pdl(qkv_finish_kernel<128, true>, gf, bf, 0, st, 1, a)
+                             : launch_pdl(qkv_finish_kernel<64, true>, gf, bf, 0, st, 1, a);
   }
   const int G = c.n_q_heads / c.n_kv_heads;
   int clusters8 = 0, max_nch = 0;
@@ -1419,14 +1420,14 @@ cudaError_t launch_attention_split(const RowMap& m, const Model& md, KvState& kv
   cudaError_t e;
   kv.launches += fold ? 3 : 2;
   if (c.head_dim == 128) {
-    e = launch_pdl(qkv_finish_kernel<128>, gf, bf, 0, st, 1, a);
+    e = launch_pdl(qkv_finish_kernel<128, false>, gf, bf, 0, st, 1, a);
     if (e == cudaSuccess)
       e = quad     ? launch_attn4<128>(kv.tm_kc, kv.tm_vc, a, clusters, q_tiles, fold, st)
           : narrow ? launch_attn<128, true, false>(kv.tm_kc, kv.tm_vc, a, clusters, st)
           : pair ? launch_attn<128, false, true>(kv.tm_kc, kv.tm_vc, a, clusters, st)
                  : launch_attn<128, false, false>(kv.tm_kc, kv.tm_vc, a, clusters, st);
   } else {
-    e = launch_pdl(qkv_finish_kernel<64>, gf, bf, 0, st, 1, a);
+    e = launch_pdl(qkv_finish_kernel<64, false>, gf, bf, 0, st, 1, a);
     if (e == cudaSuccess)
       e = quad     ? launch_attn4<64>(kv.tm_kc, kv.tm_vc, a, clusters, q_tiles, fold, st)
           : narrow ? launch_attn<64, true, false>(kv.tm_kc, kv.tm_vc, a, clusters, st)
