@@ -11,10 +11,12 @@
 // Work is cut as in k_tree_attn.cu: the key tiles of every (request, kv head),
 // weighted by the tiles of 128 queries that go over them, in even shares over one
 // CTA per SM; a tile belongs to the CTA in whose share its first unit falls.
-// Per CTA: warp 0 loads key tiles by TMA through a ring, warp 1 issues the
-// products into four TMEM buffers, warps 2-3 bring in the queries and their sums,
-// warps 4-7 and 8-11 take the tiles in turn.  More than 128 queries: one pass
-// over the CTA's tiles for each 128 (the keys then come from L2).
+// Per CTA: warp 0 loads key tiles by TMA through a ring (and the next one into L2
+// while the ring is full), warp 1 issues the products into four TMEM buffers, warps
+// 2-9 bring in the queries and their sums (a pass ahead, into registers: with two
+// warps, after the last product of a pass, turning took 6 us), warps 10-13 and
+// 14-17 take the tiles in turn.  More than 128 queries: one pass over the CTA's
+// tiles for each 128 (the keys then come from L2).
 #include <type_traits>
 
 #include "ops.h"
@@ -24,16 +26,18 @@
 namespace as2d {
 namespace {
 
-constexpr int kThreads = 384;
-// What turning to another head costs a CTA, in tiles (where a CTA has several).
-constexpr int kTurn = 5;
+// Threads that bring in queries: those of 128 in registers at once.
+constexpr int kBring = 256, kThreads = 64 + kBring + 256;
+// What turning to another head costs a CTA, in tiles (where a CTA has several): 16
+// ragged requests take 24.1 / 22.5 / 22.2 / 22.4 / 22.6 us with 1 / 2 / 3 / 4 / 5.
+constexpr int kTurn = 3;
 
 template <int D, bool F32>
 struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;
   static constexpr uint32_t Q = (F32 ? 2 : 1) * 128 * D * 2;
   static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
-  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 128 * 4 + 128 * 8 + (2 * NST + 13) * 8 + 16;
+  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 2 * 128 * (4 + 8) + (2 * NST + 16) * 8 + 16;
   static_assert(SMEM + sizeof(UnitPlan) <= 232448, "shared memory of one CTA");
 };
 
@@ -68,11 +72,12 @@ __device__ __forceinline__ bool next_segment(const UnitPlan& p, const TreeArgs& 
   return false;
 }
 
-// Adds the exponentials of 16 queries from column q0 on; masked: of those that see
-// key j of the rows' own (j < 0: of all), q < n.
+// Adds the exponentials of 16 queries from column q0 on; masked: of those, q < n,
+// that see the thread's key.  need: its bit in a word of seen's masks (0: all see it),
+// upper: in their upper words.
 template <bool MASKED>
-__device__ __forceinline__ void add_weights(const uint32_t (&v)[16], uint64_t c2, const float* lse, const uint64_t* vis,
-                                            int q0, int n, int j, uint64_t (&sum)[2]) {
+__device__ __forceinline__ void add_weights(const uint32_t (&v)[16], uint64_t c2, const float* lse, const uint2* seen,
+                                            int q0, int n, uint32_t need, bool upper, uint64_t (&sum)[2]) {
 #pragma unroll
   for (int e = 0; e < 16; e += 4) {
     const float4 l = *reinterpret_cast<const float4*>(lse + q0 + e);  // (negated)
@@ -83,8 +88,10 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[16], uint64_t c2
       float p0 = ex2(y.x), p1 = ex2(y.y);
       if (MASKED) {
         const int q = q0 + e + k;
-        if (q >= n || (j >= 0 && !((vis[q] >> j) & 1))) p0 = 0.f;
-        if (q + 1 >= n || (j >= 0 && !((vis[q + 1] >> j) & 1))) p1 = 0.f;
+        const uint4 m = *reinterpret_cast<const uint4*>(seen + q);
+        const uint32_t w0 = upper ? m.y : m.x, w1 = upper ? m.w : m.z;
+        p0 = q < n && (w0 & need) == need ? p0 : 0.f;
+        p1 = q + 1 < n && (w1 & need) == need ? p1 : 0.f;
       }
       sum[k >> 1] = add2(sum[k >> 1], two(p0, p1));
     }
@@ -96,23 +103,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     attn_weights_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ WeightArgs wa, int turn) {
   using S = Shape<D, F32>;
   constexpr int NST = S::NST, NR = D / 64;
+  constexpr int kInFlight = 128 * (D / 8) / kBring;  // all of 128 queries
   const TreeArgs& a = wa.t;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* qimg = sm;
   uint8_t* ring = sm + S::Q;
-  float* s_lse = reinterpret_cast<float*>(ring + NST * S::STAGE);  // [128] base 2, negated
-  uint64_t* s_vis = reinterpret_cast<uint64_t*>(s_lse + 128);      // [128]
-  uint64_t* full = s_vis + 128;
+  // of a pass, by its parity
+  float* s_lse = reinterpret_cast<float*>(ring + NST * S::STAGE);  // [2][128] base 2, negated
+  uint64_t* s_vis = reinterpret_cast<uint64_t*>(s_lse + 2 * 128);  // [2][128]
+  uint64_t* full = s_vis + 2 * 128;
   uint64_t* empty = full + NST;
   uint64_t* s_full = empty + NST;   // [4]
   uint64_t* s_empty = s_full + 4;   // [4]
   uint64_t* q_first = s_empty + 4;
   uint64_t* q_full = q_first + 1;
   uint64_t* q_empty = q_full + 1;
-  uint64_t* e_empty = q_empty + 1;
-  uint64_t* drain = e_empty + 1;
+  uint64_t* e_empty = q_empty + 1;  // [2]
+  uint64_t* e_full = e_empty + 2;   // [2]
+  uint64_t* drain = e_full + 2;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(drain + 1);
   __shared__ UnitPlan plan;
 
@@ -127,9 +137,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(&s_empty[i], 4);
     }
     ptx::mbar_init(q_first, kThreads / 32 - 2);
-    ptx::mbar_init(q_full, 2);
+    ptx::mbar_init(q_full, kBring / 32);
     ptx::mbar_init(q_empty, 1);
-    ptx::mbar_init(e_empty, 8);
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&e_empty[i], 8);
+      ptx::mbar_init(&e_full[i], 4);
+    }
     ptx::mbar_init(drain, 1);
     ptx::fence_mbar_init();
   }
@@ -154,11 +167,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     return ok;
   };
-  // queries of a pass (zeros up to the next 16th), their sums and masks, by N
-  // threads from t on
-  auto bring = [&](const Unit& it, int t, auto n_threads, auto in_flight) {
+  // queries of a pass (zeros up to the next 16th), by N threads from t on
+  auto bring = [&](const Unit& it, int t, auto n_threads, auto in_flight, auto later, auto ready) {
     constexpr int N = decltype(n_threads)::value;
-    load_queries<D, F32, N, decltype(in_flight)::value>(a, it, t, qimg);
+    load_queries<D, F32, N, decltype(in_flight)::value, decltype(later)::value>(a, it, t, qimg, ready);
     const int n0 = it.qt * 128, n = min(128, it.rows * G - n0), pad = (n + 15) & ~15;
     for (int c = t; c < (pad - n) * (D / 8); c += N) {
       uint8_t* to = qimg + chunk_off(n + c / (D / 8), c % (D / 8));
@@ -167,25 +179,23 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     ptx::fence_proxy_async_smem();
   };
-  auto bring_sums = [&](const Unit& it, int t, int n_threads) {
+  // the sum of query q of a pass and which rows it sees
+  auto sums_of = [&](const Unit& it, int q, float& l, uint64_t& vis) {
     const int n0 = it.qt * 128, n = min(128, it.rows * G - n0);
-    for (int q = t; q < 128; q += n_threads) {
-      float l = 0.f;
-      uint64_t vis = 0;
-      if (q < n) {
-        const int i = divide_group(a, n0 + q), h = it.g * G + (n0 + q - i * G);
-        l = a.lse[(size_t)(it.r0 + i) * a.nq + h] * -1.4426950408889634f;
-        vis = visible_rows(a, it.r0 + i, i, it.rows);
-      }
-      s_lse[q] = l;
-      s_vis[q] = vis;
-    }
+    l = 0.f;
+    vis = 0;
+    if (q >= n) return;
+    const int i = divide_group(a, n0 + q), h = it.g * G + (n0 + q - i * G);
+    l = a.lse[(size_t)(it.r0 + i) * a.nq + h] * -1.4426950408889634f;
+    vis = visible_rows(a, it.r0 + i, i, it.rows);
   };
   Segment s;
   if (int u = u0; warp >= 2 && next_segment(plan, a, u, u1, s)) {
     // the first pass, by every warp that has nothing to do yet
-    bring(s.it, tid - 64, std::integral_constant<int, kThreads - 64>{}, std::integral_constant<int, 4>{});
-    bring_sums(s.it, tid - 64, kThreads - 64);
+    const int q = tid - 64;
+    bring(s.it, q, std::integral_constant<int, kThreads - 64>{}, std::integral_constant<int, 4>{}, std::false_type{}, [&] {
+      if (q < 128) sums_of(s.it, q, s_lse[q], s_vis[q]);
+    });
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(q_first);
   }
@@ -195,18 +205,28 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t pol = ptx::policy_evict_first();
       Stage at;
       uint32_t n = 0;
+      auto load = [&](int t, int z) {
+        const uint32_t k = at.next<NST>(), i = Stage::slot(k);
+        if (n >= NST && !wait(&empty[i], Stage::parity(k) ^ 1)) return;
+        ptx::mbar_arrive_expect_tx(&full[i], S::STAGE);
+#pragma unroll
+        for (int h = 0; h < NR; ++h)
+          ptx::tma_load_3d(ring + i * S::STAGE + h * kRegion, &tmK, &full[i], 64 * h, t * 128, z, pol);
+        ++n;
+      };
+      int before = -1, z_before = 0;  // the tile that is on its way to L2 while the ring is full
       for (int u = u0; next_segment(plan, a, u, u1, s);) {
         const int z = s.it.b * a.nkv + s.it.g;
         for (int qt = 0; qt < s.passes; ++qt)
-          for (int t = s.it.t0; t < s.it.t1 && ok; ++t, ++n) {
-            const uint32_t k = at.next<NST>(), i = Stage::slot(k);
-            if (n >= NST && !wait(&empty[i], Stage::parity(k) ^ 1)) break;
-            ptx::mbar_arrive_expect_tx(&full[i], S::STAGE);
+          for (int t = s.it.t0; t < s.it.t1 && ok; ++t) {
+            if (before >= 0) load(before, z_before);
 #pragma unroll
-            for (int h = 0; h < NR; ++h)
-              ptx::tma_load_3d(ring + i * S::STAGE + h * kRegion, &tmK, &full[i], 64 * h, t * 128, z, pol);
+            for (int h = 0; h < NR; ++h) ptx::tma_prefetch_3d(&tmK, 64 * h, t * 128, z);
+            before = t;
+            z_before = z;
           }
       }
+      if (ok && before >= 0) load(before, z_before);
       // no copy is in flight when the CTA ends
       for (uint32_t i = n > NST ? n - NST : 0; i < n; ++i)
         ptx::mbar_wait(&full[i % NST], (i / NST) & 1, ptx::kDrainNs);
@@ -252,22 +272,32 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mma_commit(drain);
       ptx::mbar_wait(drain, 0, ptx::kDrainNs);
     }
-  } else if (warp < 4) {
+  } else if (warp < 2 + kBring / 32) {
+    const int q = tid - 64;
     uint32_t pass = 0;
     for (int u = u0; next_segment(plan, a, u, u1, s);) {
       for (int qt = 0; qt < s.passes; ++qt, ++pass) {
         if (pass == 0) continue;
         s.it.qt = qt;
-        wait(q_empty, (pass - 1) & 1);
-        if (ok) bring(s.it, tid - 64, std::integral_constant<int, 64>{}, std::integral_constant<int, 8>{});
-        wait(e_empty, (pass - 1) & 1);  // the last pass's sums have been read
-        if (ok) bring_sums(s.it, tid - 64, 64);
+        float l;
+        uint64_t vis;
+        if (q < 128) sums_of(s.it, q, l, vis);
+        bring(s.it, q, std::integral_constant<int, kBring>{}, std::integral_constant<int, kInFlight>{}, std::true_type{},
+              [&] { wait(q_empty, (pass - 1) & 1); });
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(q_full);
+        if (q < 128) {
+          // the sums of the pass before the last have been read
+          if (pass > 1) wait(&e_empty[pass & 1], ((pass >> 1) - 1) & 1);
+          s_lse[128 * (pass & 1) + q] = l;
+          s_vis[128 * (pass & 1) + q] = vis;
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&e_full[pass & 1]);
+        }
       }
     }
   } else {
-    const int group = (warp - 4) >> 2, row = 32 * (warp & 3) + lane;  // key of the tile, TMEM lane
+    const int group = (warp - 2 - kBring / 32) >> 2, row = 32 * (warp & 3) + lane;  // key of the tile, TMEM lane
     const uint32_t tl = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
     const uint64_t c2 = two(a.scale_log2, a.scale_log2);
     uint32_t d = 0, pass = 0;
@@ -275,8 +305,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       float* w = wa.w + ((size_t)s.it.b * a.nkv + s.it.g) * a.cap;
       for (int qt = 0; qt < s.passes; ++qt, ++pass) {
         const int n = min(128, s.it.rows * G - qt * 128);
-        // the queries' sums are there (the products wait for them too)
-        pass == 0 ? wait(q_first, 0) : wait(q_full, (pass - 1) & 1);
+        const float* lse = s_lse + 128 * (pass & 1);
+        const uint2* seen = reinterpret_cast<const uint2*>(s_vis + 128 * (pass & 1));
+        pass == 0 ? wait(q_first, 0) : wait(&e_full[pass & 1], ((pass - 1) >> 1) & 1);
         for (int t = s.it.t0 + group; t < s.it.t1; t += 2, ++d) {
           const int key = t * 128 + row, j = key - s.it.L;
           const bool live = j < s.it.rows;
@@ -286,17 +317,23 @@ __global__ void __launch_bounds__(kThreads, 1)
           wait(&s_full[buf], (d >> 1) & 1);
           ok = __all_sync(~0u, ok);
           ptx::tc_fence_after();
-          const bool tail = t * 128 + 128 > s.it.L;
+          const bool tail = t * 128 + 128 > s.it.L, upper = j >= 32;
+          const uint32_t need = j < 0 ? 0u : 1u << (j & 31);
           uint64_t sum[2] = {0, 0};
 #pragma unroll 1
-          for (int q = 0; q < n; q += 16) {
-            uint32_t v[16];
-            ptx::tmem_ld16(tl + 128 * buf + q, v);
+          for (int q = 0; q < n; q += 32) {
+            uint32_t v[2][16];
+            ptx::tmem_ld16(tl + 128 * buf + q, v[0]);
+            if (q + 16 < n) ptx::tmem_ld16(tl + 128 * buf + q + 16, v[1]);
             ptx::tmem_ld_wait();
-            if (tail || q + 16 > n)
-              add_weights<true>(v, c2, s_lse, s_vis, q, n, j, sum);
-            else
-              add_weights<false>(v, c2, s_lse, s_vis, q, n, j, sum);
+#pragma unroll
+            for (int h = 0; h < 32; h += 16) {
+              if (q + h >= n) break;
+              if (tail || q + h + 16 > n)
+                add_weights<true>(v[h >> 4], c2, lse, seen, q + h, n, need, upper, sum);
+              else
+                add_weights<false>(v[h >> 4], c2, lse, seen, q + h, n, need, upper, sum);
+            }
           }
           const float2 sums = of_two(add2(sum[0], sum[1]));
           ptx::tc_fence_before();
@@ -305,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (live && ok) w[key] = before + (sums.x + sums.y);
         }
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(e_empty);
+        if (lane == 0) ptx::mbar_arrive(&e_empty[pass & 1]);
       }
     }
   }

@@ -22,8 +22,8 @@
 //              swizzle) through a ring of shared-memory stages;
 //   warp 1     issues the products: S = Q K^T (M = 128 queries, N = 128 keys),
 //              O += P V (A = P from TMEM, V read MN-major);
-//   warps 2-3  bring in the queries, and prepare the value tiles that hold
-//              entries of the call's own rows (clean_tile);
+//   warps 2-3  prepare the value tiles that hold entries of the call's own rows
+//              (clean_tile);
 //   warps 4-19 two sets of eight that take the item's key tiles in turn, half of
 //              a query's keys per thread: S from TMEM, mask, running maximum (of
 //              both halves, exchanged through shared memory), P = 2^(S - m) back
@@ -31,6 +31,8 @@
 //              multiplied by V.  Each set has its own accumulator, maximum and sum,
 //              and O is rescaled only where the maximum grew by more than 2^8 (P
 //              stays below 2^8, in 32-bit sums).
+// The first item's queries are brought in by warps 2-19, another's by the set that
+// has no part in the last tile of the item before, while the other has.
 // 32-bit queries are bf16 hi and lo parts too (two products with K), 16-bit
 // ones are exact.
 #include <algorithm>
@@ -45,9 +47,9 @@ namespace {
 
 constexpr int kThreads = 640;
 // What turning to another item costs a CTA, in tiles (where a CTA has several): its
-// queries, its epilogue.  16 ragged requests of 60 items take 77 us with 0, 60 / 55 /
-// 51 / 55 with 3 / 4 / 5 / 6, a tree of 64 rows (16 items) 45 / 42 / 40 with 3 / 5 / 6.
-constexpr int kTurn = 5;
+// queries, its epilogue.  16 ragged requests (60 items) take 43.5 / 43.8 us with 4 / 5
+// (2 / 3: 58 / 52), a tree of 64 rows (16 items) 34.0 / 35.0.
+constexpr int kTurn = 4;
 // P may grow to 2^kLazy before the accumulator is rescaled.
 constexpr float kLazy = 8.f;
 
@@ -71,7 +73,7 @@ struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;            // one K or V tile
   static constexpr uint32_t Q = (F32 ? 2 : 1) * 128 * D * 2;  // hi (and lo) image
   static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
-  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16;
+  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16 + 2 * sizeof(Unit);
   static_assert(SMEM + sizeof(UnitPlan) <= 232448, "shared memory of one CTA");
 };
 
@@ -122,28 +124,38 @@ __device__ __forceinline__ void mask_scores(uint32_t (&v)[32], uint32_t bits) {
 // them to the rows that do see them.
 template <int D>
 __device__ __forceinline__ void clean_tile(uint8_t* v, int p0, int L, int kend, int tid, unsigned long long* bad) {
-  constexpr int C = D / 8;
-  const int z = max(L - p0, 0);
-  for (int c = tid; c < (128 - z) * C; c += 64) {
-    const int r = z + c / C;
-    uint4* at = reinterpret_cast<uint4*>(v + chunk_off(r, c % C));
-    if (p0 + r >= kend) {
-      *at = make_uint4(0, 0, 0, 0);
-      continue;
-    }
-    uint4 x = *at;
-    uint32_t* w = reinterpret_cast<uint32_t*>(&x);
-    bool any = false;
+  constexpr int C = D / 8, B = 4;  // chunks of a row, of a thread at once
+  const int z = max(L - p0, 0), end = min(kend - p0, 128);
+#pragma unroll 1
+  for (int c0 = z * C + tid; c0 < end * C; c0 += 64 * B) {
+    uint4 x[B];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u, any = true;
-      if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu, any = true;
+    for (int u = 0; u < B; ++u) {
+      const int c = c0 + 64 * u;
+      x[u] = make_uint4(0, 0, 0, 0);
+      if (c < end * C) x[u] = *reinterpret_cast<const uint4*>(v + chunk_off(c / C, c % C));
     }
-    if (any) {
-      *at = x;
-      atomicOr(bad, 1ull << (p0 + r - L));
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      uint32_t* w = reinterpret_cast<uint32_t*>(&x[u]);
+      // an exponent of ones, and no other, carries into its value's sign bit
+      uint32_t any = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= (w[e] & 0x7F807F80u) + 0x00800080u;
+      if (!(any & 0x80008000u)) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+        if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
+      }
+      const int c = c0 + 64 * u;
+      *reinterpret_cast<uint4*>(v + chunk_off(c / C, c % C)) = x[u];
+      atomicOr(bad, 1ull << (p0 + c / C - L));
     }
   }
+#pragma unroll 1
+  for (int c = max(end, z) * C + tid; c < 128 * C; c += 64)
+    *reinterpret_cast<uint4*>(v + chunk_off(c / C, c % C)) = make_uint4(0, 0, 0, 0);
 }
 
 // N consecutive results x inv at element `at` of the output: 32-bit (F32), bf16, or
@@ -154,16 +166,24 @@ __device__ __forceinline__ void write_out(const TreeArgs& a, const float* x, flo
     bf16* out = (bf16*)a.out + at;
     bf16* lo = a.out_lo + at;
 #pragma unroll
-    for (int e = 0; e < N; e += 2)
-      hi_lo(x[e] * inv, x[e + 1] * inv, *reinterpret_cast<uint32_t*>(out + e), *reinterpret_cast<uint32_t*>(lo + e));
+    for (int e = 0; e < N; e += 4) {
+      uint2 h, l;
+      hi_lo(x[e] * inv, x[e + 1] * inv, h.x, l.x);
+      hi_lo(x[e + 2] * inv, x[e + 3] * inv, h.y, l.y);
+      *reinterpret_cast<uint2*>(out + e) = h;
+      *reinterpret_cast<uint2*>(lo + e) = l;
+    }
   } else if (F32) {
     float* out = (float*)a.out + at;
 #pragma unroll
-    for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(out + e) = make_float2(x[e] * inv, x[e + 1] * inv);
+    for (int e = 0; e < N; e += 4)
+      *reinterpret_cast<float4*>(out + e) = make_float4(x[e] * inv, x[e + 1] * inv, x[e + 2] * inv, x[e + 3] * inv);
   } else {
     bf16* out = (bf16*)a.out + at;
 #pragma unroll
-    for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(out + e) = pack2(x[e] * inv, x[e + 1] * inv);
+    for (int e = 0; e < N; e += 4)
+      *reinterpret_cast<uint2*>(out + e) =
+          make_uint2(pack2(x[e] * inv, x[e + 1] * inv), pack2(x[e + 2] * inv, x[e + 3] * inv));
   }
 }
 
@@ -201,6 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* q_first = drain + 1;  // in q_full's place for the CTA's first item
   unsigned long long* s_bad = reinterpret_cast<unsigned long long*>(q_first + 1);
   uint32_t* tslot = reinterpret_cast<uint32_t*>(s_bad + 1);
+  Unit* s_next = reinterpret_cast<Unit*>(tslot + 2);  // [2] the item after one of this parity
   __shared__ UnitPlan s_plan;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -211,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(&tail_full[i], 1);
     }
     ptx::mbar_init(q_first, (kThreads - 64) / 32);
-    ptx::mbar_init(q_full, 2);
+    ptx::mbar_init(q_full, 8);
     ptx::mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&s_full[i], 1);
@@ -268,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (int u = u0; warp >= 2 && next(u)) {
     // the first item's queries, by every warp that has nothing to do yet (by two
     // warps 32-bit queries of 119 rows took 5 us)
-    load_queries<D, F32, kThreads - 64, 4>(a, it, tid - 64, qimg);
+    load_queries<D, F32, kThreads - 64, 4, false>(a, it, tid - 64, qimg, [] {});
     ptx::fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(q_first);
@@ -392,13 +413,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int t64 = tid - 64;
     uint32_t n = 0, items = 0, turn = 0;
     for (int u = u0; next(u); ++items) {
-      if (items > 0) {
-        wait(q_empty, (items - 1) & 1);
-        if (ok) load_queries<D, F32, 64, 8>(a, it, t64, qimg);
-        ptx::fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(q_full);
-      }
       const int first = it.L / 128;
       // the epilogue of the item before has read what was noted for it
       if (items > 0) wait(o_empty, (items - 1) & 1);
@@ -426,7 +440,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int G = a.nq / a.nkv;
     const float c = a.scale_log2;
     uint32_t ns = 0, items = 0, c_turn = 0;
-    for (int u = u0; next(u); ++items) {
+    int u = u0;
+    bool more = next(u);
+    while (more) {
       const int cnt = it.t1 - it.t0, nqs = it.rows * G;
       const int q = it.qt * 128 + row, i = divide_group(a, q);
       const bool live = q < nqs;
@@ -517,6 +533,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&p_full[set]);
       }
+      // the next item and its queries, by the set that has no part in the last tile
+      if constexpr (!DIRECT) {
+        if (set == (cnt & 1)) {
+          Unit then;
+          if (int v = it.next; next_item(s_plan, a, v, u1, then)) {
+            load_queries<D, F32, 256, 4, true>(a, then, half * 128 + row, qimg, [&] { wait(q_empty, items & 1); });
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(q_full);
+          } else {
+            then.rows = 0;
+          }
+          if (half == 0 && row == 0) s_next[items & 1] = then;
+        }
+      }
       // ---- the item's end: the two sets' parts, each group a quarter of the dims ----
       const bool tails = it.t1 > it.L / 128;
       wait(o_full, items & 1);
@@ -594,6 +625,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(o_empty);
+      if constexpr (!DIRECT) it = s_next[items & 1];
+      more = !DIRECT && it.rows > 0;
+      ++items;
     }
   }
   if (DIRECT && mode == kCluster) {

@@ -82,47 +82,63 @@ struct Stage {
 // The queries of an item into the operand image(s), by N threads (a multiple of a
 // row's chunks of 16 bytes), B chunks of a thread in flight (32-bit queries); rows
 // past the item's queries are left as they are (what they hold reaches no other row).
-template <int D, bool F32, int N, int B>
-__device__ __forceinline__ void load_queries(const TreeArgs& a, const Unit& it, int tid, uint8_t* img) {
+// LATER: the image is written only after ready() (its last readers), called by every
+// thread once its first loads, and the others' into L2, are on their way.
+template <int D, bool F32, int N, int B, bool LATER, typename F>
+__device__ __forceinline__ void load_queries(const TreeArgs& a, const Unit& it, int tid, uint8_t* img, F ready) {
   constexpr int C = D / 8, R = N / C;  // chunks of a row, rows of a step
   static_assert(N % C == 0, "a thread keeps its chunk");
   const int G = a.nq / a.nkv, n0 = it.qt * 128, n = min(128, it.rows * G - n0), c = tid % C;
+  auto at = [&](int r) {
+    const int i = divide_group(a, n0 + r), h = it.g * G + (n0 + r - i * G);
+    return (it.r0 + i) * a.q_stride + (int64_t)h * D + 8 * c;
+  };
+  // (chunks of 16 bytes of bf16 or 32 of floats, lines of 128)
+  auto to_l2 = [&](int r) {
+    if (LATER && c % (F32 ? 4 : 8) == 0)
+      for (; r < n; r += R) ptx::prefetch_l2((const uint8_t*)a.q + at(r) * (F32 ? 4 : 2));
+  };
   if constexpr (!F32) {
     // straight into shared memory, every copy on its way at once
+    to_l2(tid / C);
+    ready();
 #pragma unroll 1
-    for (int r = tid / C; r < n; r += R) {
-      const int i = divide_group(a, n0 + r), h = it.g * G + (n0 + r - i * G);
-      ptx::cp_async16(img + chunk_off(r, c), (const bf16*)a.q + (it.r0 + i) * a.q_stride + (int64_t)h * D + 8 * c);
-    }
+    for (int r = tid / C; r < n; r += R) ptx::cp_async16(img + chunk_off(r, c), (const bf16*)a.q + at(r));
     ptx::cp_async_wait_all();
-  }
-#pragma unroll 1
-  for (int r0 = F32 ? tid / C : n; r0 < n; r0 += R * B) {
-    uint4 v[B][2];
+  } else {
+    int r0 = tid / C;
+    bool first = true;
+    do {
+      uint4 v[B][2];
 #pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const int r = r0 + R * u;
-      if (r < n) {
-        const int i = divide_group(a, n0 + r), h = it.g * G + (n0 + r - i * G);
-        const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + 8 * c;
-        const uint4* s = reinterpret_cast<const uint4*>((const float*)a.q + at);
-        v[u][0] = s[0];
-        v[u][1] = s[1];
+      for (int u = 0; u < B; ++u) {
+        const int r = r0 + R * u;
+        if (r < n) {
+          const uint4* s = reinterpret_cast<const uint4*>((const float*)a.q + at(r));
+          v[u][0] = s[0];
+          v[u][1] = s[1];
+        }
       }
-    }
-#pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const int r = r0 + R * u;
-      if (r < n) {
-        uint8_t* to = img + chunk_off(r, c);
-        const float* x = reinterpret_cast<const float*>(&v[u][0]);
-        uint32_t h[4], l[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) hi_lo(x[2 * e], x[2 * e + 1], h[e], l[e]);
-        *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
-        *reinterpret_cast<uint4*>(to + 128 * D * 2) = make_uint4(l[0], l[1], l[2], l[3]);
+      if (first) {
+        if (R * B < 128) to_l2(r0 + R * B);
+        ready();
+        first = false;
       }
-    }
+#pragma unroll
+      for (int u = 0; u < B; ++u) {
+        const int r = r0 + R * u;
+        if (r < n) {
+          uint8_t* to = img + chunk_off(r, c);
+          const float* x = reinterpret_cast<const float*>(&v[u][0]);
+          uint32_t h[4], l[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) hi_lo(x[2 * e], x[2 * e + 1], h[e], l[e]);
+          *reinterpret_cast<uint4*>(to) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(to + 128 * D * 2) = make_uint4(l[0], l[1], l[2], l[3]);
+        }
+      }
+      r0 += R * B;
+    } while (r0 < n);
   }
 }
 
