@@ -554,8 +554,8 @@ typedef struct as2d_cache {
    max_len: host bound of the lengths, by which the launch is sized (0: the
    capacity); results do not depend on it beyond the order of sums.  rows: host
    int32 [batch].  visible: device uint64 [sum rows], or NULL for a chain (row i
-   sees rows 0 .. i).  scale: the factor of q k (finite, > 0), usually 1 /
-   sqrt(head_dim). */
+   sees rows 0 .. i).  scale: the factor of q k (> 0, finite in 32 bits as a
+   multiple of log2(e) too), usually 1 / sqrt(head_dim). */
 typedef struct as2d_tree_rows {
   const void* q;
   int32_t q_type, n_q;
@@ -703,7 +703,8 @@ as2d_status as2d_kv_track_weights(as2d_kv* kv, float* weights);
    the latest `recent` among them; requests that hold no more are left alone.  The
    length becomes keep[b]; the pending root stays, and later rows take their
    positions as if nothing had been evicted.  Needs tracked weights
-   (AS2D_ERR_INVALID_ARG).  as2d_kv_rollback cannot go below keep[b] afterwards.
+   (AS2D_ERR_INVALID_ARG).  Under stream capture the host's bound of the lengths
+   stays as it was (as2d_kv_read_state reads them).  as2d_kv_rollback cannot go below keep[b] afterwards.
    Asynchronous on `stream`. */
 as2d_status as2d_kv_evict(as2d_kv* kv, const int32_t* keep, int32_t recent, void* stream);
 

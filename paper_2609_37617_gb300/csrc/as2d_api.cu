@@ -970,7 +970,10 @@ extern "C" as2d_status as2d_kv_evict(as2d_kv* kh, const int32_t* keep, int32_t r
   s.launches += 3;
   LAUNCH(AS2D_KERNEL_OTHER, launch_note_evict(s, keep, st));
   LAUNCH(AS2D_KERNEL_OTHER, launch_cache_evict(a, c.head_dim, st));
-  for (int b = 0; b < s.batch; ++b)
+  // (a captured call may be followed by others before it runs, or never run)
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  const bool eager = cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone;
+  for (int b = 0; b < s.batch && eager; ++b)
     if (s.len_upper[b] > keep[b]) s.len_upper[b] = keep[b];
   return AS2D_OK;
 }

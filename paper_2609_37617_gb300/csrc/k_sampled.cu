@@ -1,5 +1,7 @@
 // k_sampled.cu -- probabilities at a temperature (as2d_token_probs) and the
 // acceptance of drafted tokens from given random numbers (as2d_accept_sampled).
+#include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 #include "ops.h"
@@ -418,7 +420,8 @@ cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float t
     ranks *= 2;
   const bool vec = vocab % 4 == 0 && ((uintptr_t)logits | (uintptr_t)probs) % 16 == 0;
   const int slice = ((vocab + ranks - 1) / ranks + 3) / 4 * 4;
-  const float c = (float)(1.4426950408889634 / temperature);
+  // (finite: at the smallest temperatures the maximum's own 0 c is 0, not NaN)
+  const float c = (float)std::min(1.4426950408889634 / temperature, (double)FLT_MAX);
   // the clusters of eight that run at once, by the occupancy calculator less two: with
   // all of them, 36, some started late (250 rows 67 us, not 56)
   const int resident = resident_clusters(clusters, probs_rows_kernel, kProbs, kNext, 8) - 2;

@@ -45,7 +45,8 @@ as2d_status check_rows(const as2d_cache* c, int32_t layer, const as2d_tree_rows*
   if (r->q_type != AS2D_TYPE_BF16 && r->q_type != AS2D_TYPE_F32) return invalid("q_type is no AS2D_TYPE_*");
   if (r->n_q < 1 || r->n_q % c->n_kv != 0) return invalid("n_q must be a positive multiple of n_kv");
   if (r->n_q / c->n_kv > 1024 || r->n_q > 65535) return report_error(AS2D_ERR_UNSUPPORTED, "too many query heads");
-  if (!(r->scale > 0.f) || !std::isfinite(r->scale)) return invalid("scale must be finite and > 0");
+  if (!(r->scale > 0.f) || !std::isfinite(r->scale * 1.4426950408889634f))
+    return invalid("scale must be > 0 and scale log2(e) finite");
   if (r->max_len < 0 || r->max_len > c->capacity) return invalid("max_len outside [0, capacity]");
   a.rm.batch = c->batch;
   a.rm.start[0] = 0;

@@ -577,3 +577,98 @@ def test_calls_back_to_back(lib):
         check_attention(x, out, lse)
     for i in range(len(xs)):  # bit for bit the same each time
         assert torch.equal(outs[i][1], outs[i + len(xs)][1]) and torch.equal(outs[i][1], outs[i + 2 * len(xs)][1])
+
+
+# ---- calls at the edges of what is allowed ------------------------------------------
+
+def test_smallest_and_largest_temperatures(lib):
+    """At the smallest temperature a row is its maxima, at the largest it is even."""
+    x = torch.zeros((3, 1000), device="cuda")
+    x[0, 17], x[1, 3], x[1, 900] = 1.0, 2.0, 2.0
+    x[2, ::2] = -math.inf
+    p = lib.token_probs(x, 1e-45)
+    assert p[0, 17] == 1 and p[0].sum() == 1
+    assert p[1, 3] == 0.5 and p[1, 900] == 0.5 and p[1].sum() == 1
+    assert (p[2, ::2] == 0).all() and ((p[2, 1::2].double() * 500 - 1).abs() <= 2.0 ** -15).all()
+    p = lib.token_probs(x, 3e38)
+    assert ((p[:2].double() * 1000 - 1).abs() <= 2.0 ** -15).all() and (p[2, ::2] == 0).all()
+
+
+@pytest.mark.parametrize("heads", [(1024, 1, 64), (640, 5, 128)])
+def test_many_heads_to_a_kv_head(lib, heads):
+    """Hundreds of query tiles of one kv head, one after another in a CTA."""
+    rows, lens = [64, 1, 20], [130, 0, 515]
+    masks = ref.tree_masks(rows, np.random.default_rng(7))
+    x = Inputs(heads, lens, rows, masks, torch.float32)
+    out, lse = run_attention(lib, x)
+    check_attention(x, out, lse)
+    check_weights(lib, x)
+
+
+def test_two_streams_at_once(lib):
+    """Calls that overlap, each on a stream, cache and workspace of its own, give
+    what they give alone."""
+    xs = [Inputs((28, 4, 128), [n, 40], [r, 3], ref.tree_masks([r, 3], np.random.default_rng(n)), t, seed=n)
+          for n, r, t in ((9000, 30, torch.float32), (8000, 64, torch.bfloat16))]
+    caches = [lib.Cache(x.k, x.v) for x in xs]
+    logits = [torch.randn((40, 60000), device="cuda") for _ in xs]
+
+    def step(i, stream):
+        x = xs[i]
+        lse = torch.empty((sum(x.rows), 28), device="cuda")
+        w = torch.zeros(x.k.shape[:4], device="cuda")
+        outs = [torch.empty_like(x.q, memory_format=torch.contiguous_format), lse, w, torch.empty_like(logits[i])]
+        torch.cuda.synchronize()
+
+        def run():
+            caches[i].tree_attention(x.q, x.kv_len, x.rows, x.visible, lse=lse, out=outs[0], stream=stream)
+            caches[i].attention_weights(x.q, lse, w, x.kv_len, x.rows, x.visible, stream=stream)
+            lib.token_probs(logits[i], 0.9, out=outs[3], stream=stream)
+        return run, outs
+    streams = [torch.cuda.Stream() for _ in xs]
+    alone = []
+    for i in range(2):
+        run, outs = step(i, streams[i].cuda_stream)
+        for _ in range(4):
+            run()
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in outs])
+    pairs = [step(i, streams[i].cuda_stream) for i in range(2)]
+    for _ in range(4):
+        for run, _ in pairs:
+            run()
+    torch.cuda.synchronize()
+    for (_, outs), want in zip(pairs, alone):
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_accept_the_same_candidate_twice(lib):
+    """One token at several places, each place with its own row; random numbers that
+    are no numbers, or outside [0, 1), take the nearest that is one (NaN: 0)."""
+    V = 2000
+    p = np.zeros((3, V), dtype=np.float32)
+    p[0, [4, 9]], p[1, [4, 9]], p[2, [4, 9]] = [0.75, 0.25], [0.25, 0.75], [0.5, 0.5]
+    assert run_accept(lib, p, None, [4, 4], [2], [0.5, 0.2, 0.1]) == ([2], [4])
+    assert run_accept(lib, p, None, [4, 4], [2], [0.5, 0.5, 0.1]) == ([1], [9])
+    for u, want in ((math.nan, 4), (-1.0, 4), (1.0, 9), (7.0, 9), (math.inf, 9), (-math.inf, 4)):
+        assert run_accept(lib, p[:1], None, [], [0], [u]) == ([0], [want])
+
+
+def test_probs_and_acceptance_off_16_bytes(lib):
+    """Rows whose first value lies 4 bytes behind a 16-byte boundary."""
+    rng = np.random.default_rng(5)
+    x = torch.randn((5, 4096), device="cuda")
+    off = torch.empty(5 * 4096 + 1, device="cuda")[1:].view(5, 4096)
+    off.copy_(x)
+    p = lib.token_probs(off, 0.7, out=torch.empty(5 * 4096 + 1, device="cuda")[1:].view(5, 4096))
+    want = lib.token_probs(x, 0.7)
+    assert ((p - want).abs() <= want * 2.0 ** -14).all()
+    rows = dyadic_rows(rng, 5, 4096, 300)
+    dev = torch.empty(5 * 4096 + 1, device="cuda")[1:].view(5, 4096)
+    dev.copy_(torch.from_numpy(rows))
+    cand = [int(np.flatnonzero(rows[i])[3]) for i in (0, 1, 3)]
+    u = (rng.integers(0, 2 ** 20, 5) / 2.0 ** 20).astype(np.float32)
+    n, tok = (torch.empty(2, dtype=torch.int32, device="cuda") for _ in range(2))
+    lib.accept_sampled(dev, torch.tensor(cand, dtype=torch.int32, device="cuda"), [2, 1],
+                       torch.from_numpy(u).cuda(), n, tok)
+    assert (n.tolist(), tok.tolist()) == ref.accept(rows.astype(np.float64), None, cand, [2, 1], u.astype(np.float64))

@@ -469,6 +469,70 @@ def test_state_graph(sharp, sharp_text):
     st.close()
 
 
+def test_an_eviction_that_is_captured_has_not_run(pair):
+    """Calls between the capture of an eviction and its first replay see every entry."""
+    cfg = pair.cfg
+    st = pair.state([L0], CAP, [5])
+    w = torch.rand(st.kc.shape[:4], device="cuda")
+    st.track_weights(w)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        st.evict([20], recent=4, stream=s.cuda_stream)
+    st.track_weights(None)
+    _, corr, _, logits = run_gpu_block(st, cfg, [[]])
+    want, _ = forward(pair, st.kc[:, 0].double(), st.vc[:, 0].double(), L0, L0, 5)
+    assert (want - torch.from_numpy(logits[0]).cuda()).abs().max() <= LOGIT_TOL
+    g.replay()
+    torch.cuda.synchronize()
+    assert st.read_state() == ([20], list(corr))
+    _, _, _, logits = run_gpu_block(st, cfg, [[]])
+    want, _ = forward(pair, st.kc[:, 0].double(), st.vc[:, 0].double(), 20, L0 + 1, corr[0])
+    assert (want - torch.from_numpy(logits[0]).cuda()).abs().max() <= LOGIT_TOL
+    st.check()
+    st.close()
+
+
+def test_prefill_after_an_eviction(pair):
+    """Tokens prefilled over what an eviction left stand at their true positions: what
+    decode steps over them give."""
+    cfg = pair.cfg
+    tokens = [5, 9, 2, 11, 7, 3, 8]
+    caches = []
+    for whole in (True, False):
+        st = pair.state([L0], CAP, [5])
+        w = torch.linspace(0, 1, CAP, device="cuda").expand(st.kc.shape[:4]).contiguous()
+        st.track_weights(w)
+        st.evict([90], recent=4)
+        st.track_weights(None)
+        first = ints([0])
+        if whole:
+            with pytest.raises(Exception, match="tracked|track|refused|weights"):
+                st.track_weights(w)
+                st.prefill(ints(tokens), first)
+            st.track_weights(None)
+            st.prefill(ints(tokens), first)
+        else:
+            for i, t in enumerate(tokens):
+                st.rollback([90 + i], [t])
+                _, corr, _, logits = run_gpu_block(st, cfg, [[]])
+                want, _ = forward(pair, st.kc[:, 0].double(), st.vc[:, 0].double(), 90 + i, L0 + i, t)
+                assert (want - torch.from_numpy(logits[0]).cuda()).abs().max() <= LOGIT_TOL
+            margin = np.sort(logits[0].ravel())[-1] - np.sort(logits[0].ravel())[-2]
+        st.check()
+        ln, rt = st.read_state()
+        assert ln == [90 + len(tokens)]
+        caches.append((st, st.kc[:, 0, :, 90:ln[0]].float(), st.vc[:, 0, :, 90:ln[0]].float(), rt))
+    (a, ka, va, ra), (b, kb, vb, rb) = caches
+    # (the bar of prefilled entries against the decode steps' elsewhere)
+    assert (ka - kb).abs().max() <= 3e-2 and (va - vb).abs().max() <= 3e-2
+    if margin > MARGIN_SURE:
+        assert ra == rb
+    a.close()
+    b.close()
+
+
 def test_a_state_without_the_operators_is_as_before(pair):
     """Calls before, between and after calls along trees give the same bits."""
     cfg = pair.cfg

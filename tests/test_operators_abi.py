@@ -129,3 +129,10 @@ def test_bad_sampling(lib):
     for bad in (-1, 17):
         k[1] = bad
         assert f(*good, None) == -1
+
+
+def test_scale_beyond_its_base_two_form(lib):
+    """scale itself is finite, scale log2(e) is not: a score of 0 would be 0 inf."""
+    r = rows(lib, scale=3e38)
+    assert attention(lib, r=r) == -1 and "scale" in lib.as2d_last_error()
+    assert weights(lib, r=r) == -1
