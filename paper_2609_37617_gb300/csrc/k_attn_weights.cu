@@ -232,46 +232,45 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::mbar_wait(&full[i % NST], (i / NST) & 1, ptx::kDrainNs);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t q_lo = ptx::desc_lo(ptx::smem_u32(qimg), 16u);
-      Stage at;
-      uint32_t done[2] = {0, 0}, pass = 0;  // tiles of each group so far
-      for (int u = u0; ok && next_segment(plan, a, u, u1, s);) {
-        for (int qt = 0; qt < s.passes && ok; ++qt, ++pass) {
-          pass == 0 ? wait(q_first, 0) : wait(q_full, (pass - 1) & 1);
-          const int n = min(128, s.it.rows * G - qt * 128);
-          const uint32_t idesc = ptx::idesc_bf16_f32(128, (n + 15) & ~15);
-          for (int t = s.it.t0; t < s.it.t1 && ok; ++t) {
-            const int odd = (t - s.it.t0) & 1;
-            const uint32_t d = odd ? done[1] : done[0], buf = odd + 2 * (d & 1);
-            const uint32_t k = at.next<NST>(), i = Stage::slot(k);
-            if (!wait(&full[i], Stage::parity(k))) break;
-            if (d >= 2 && !wait(&s_empty[buf], ((d >> 1) - 1) & 1)) break;
-            ptx::tc_fence_after();
-            const uint32_t kt = ptx::desc_lo(ptx::smem_u32(ring + i * S::STAGE), 16u), ds = tmem + 128 * buf;
+    // the whole warp, for operands in uniform registers; one thread issues
+    const uint32_t lead = ptx::elect_one(), tm = __shfl_sync(~0u, tmem, 0);
+    const uint32_t q_lo = ptx::desc_lo(ptx::smem_u32(qimg), 16u);
+    auto whole = [&](bool) { return ok = __all_sync(~0u, ok); };
+    Stage at;
+    uint32_t done[2] = {0, 0}, pass = 0;  // tiles of each group so far
+    for (int u = u0; ok && next_segment(plan, a, u, u1, s);) {
+      const int tiles = __shfl_sync(~0u, s.it.t1 - s.it.t0, 0), queries = __shfl_sync(~0u, s.it.rows * G, 0);
+      for (int qt = 0; qt * 128 < queries && ok; ++qt, ++pass) {
+        whole(pass == 0 ? wait(q_first, 0) : wait(q_full, (pass - 1) & 1));
+        const uint32_t idesc = ptx::idesc_bf16_f32(128, (min(128, queries - qt * 128) + 15) & ~15);
+        for (int t = 0; t < tiles && ok; ++t) {
+          const int odd = t & 1;
+          const uint32_t d = odd ? done[1] : done[0], buf = odd + 2 * (d & 1);
+          const uint32_t k = at.next<NST>(), i = Stage::slot(k);
+          wait(&full[i], Stage::parity(k));
+          if (d >= 2) wait(&s_empty[buf], ((d >> 1) - 1) & 1);
+          if (!whole(ok)) break;
+          ptx::tc_fence_after();
+          const uint32_t kt = ptx::desc_lo(ptx::smem_u32(ring + i * S::STAGE), 16u), ds = tm + 128 * buf;
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              const uint32_t to = ((kk >> 2) * kRegion + 32u * (kk & 3)) >> 4;
-              if (kk == 0)
-                ptx::mma_bf16_lo<false>(ds, kt, q_lo, idesc);
-              else
-                ptx::mma_bf16_lo<true>(ds, kt + to, q_lo + to, idesc);
-              if (F32) ptx::mma_bf16_lo<true>(ds, kt + to, q_lo + to + (128u * D * 2 >> 4), idesc);
-            }
-            ptx::mma_commit(&s_full[buf]);
-            ptx::mma_commit(&empty[i]);
-            if (t == s.it.t1 - 1) ptx::mma_commit(q_empty);
-            if (odd)
-              ++done[1];
-            else
-              ++done[0];
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t to = ((kk >> 2) * kRegion + 32u * (kk & 3)) >> 4;
+            ptx::mma_bf16_lo(lead, ds, kt + to, q_lo + to, idesc, kk > 0 ? 1u : 0u);
+            if (F32) ptx::mma_bf16_lo(lead, ds, kt + to, q_lo + to + (128u * D * 2 >> 4), idesc, 1u);
           }
+          ptx::mma_commit_if(lead, &s_full[buf]);
+          ptx::mma_commit_if(lead, &empty[i]);
+          if (t == tiles - 1) ptx::mma_commit_if(lead, q_empty);
+          if (odd)
+            ++done[1];
+          else
+            ++done[0];
         }
       }
-      // no product is running when TMEM is freed
-      ptx::mma_commit(drain);
-      ptx::mbar_wait(drain, 0, ptx::kDrainNs);
     }
+    // no product is running when TMEM is freed
+    ptx::mma_commit_if(lead, drain);
+    ptx::mbar_wait(drain, 0, ptx::kDrainNs);
   } else if (warp < 2 + kBring / 32) {
     const int q = tid - 64;
     uint32_t pass = 0;

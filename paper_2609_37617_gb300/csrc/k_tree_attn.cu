@@ -47,9 +47,9 @@ namespace {
 
 constexpr int kThreads = 640;
 // What turning to another item costs a CTA, in tiles (where a CTA has several): its
-// queries, its epilogue.  16 ragged requests (60 items) take 43.5 / 43.8 us with 4 / 5
-// (2 / 3: 58 / 52), a tree of 64 rows (16 items) 34.0 / 35.0.
-constexpr int kTurn = 4;
+// queries, its epilogue.  us with 3 / 4 / 5 / 6: 16 ragged requests (60 items) 46.9 /
+// 42.7 / 41.4 / 42.7, a tree of 64 rows (16 items) 32.1 / 31.4 / 32.1 / 32.6.
+constexpr int kTurn = 5;
 // P may grow to 2^kLazy before the accumulator is rescaled.
 constexpr float kLazy = 8.f;
 
@@ -305,6 +305,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     return ok;
   };
+  // two at once: their first looks overlap
+  auto wait2 = [&](uint64_t* a_bar, uint32_t a_parity, uint64_t* b_bar, uint32_t b_parity) {
+    const bool a_done = ptx::mbar_try_wait(a_bar, a_parity), b_done = ptx::mbar_try_wait(b_bar, b_parity);
+    if (!a_done) wait(a_bar, a_parity);
+    if (!b_done) wait(b_bar, b_parity);
+    return ok;
+  };
 
   if (warp == 0) {
     if (lane == 0) {
@@ -340,75 +347,71 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t IDESC1 = ptx::idesc_bf16_f32(128, 128);
-      constexpr uint32_t IDESC2 = ptx::idesc_bf16_f32(128, D, true);
-      const uint32_t q_lo = ptx::desc_lo(ptx::smem_u32(qimg), 16u);
-      constexpr uint32_t kNone = ~0u;
-      Stage at;
-      uint32_t items = 0, p_turn = 0, c_turn = 0;    // parities of p_full and v_clean
-      uint32_t last0 = kNone, last1 = kNone, v = 0;  // value stages of the sets' last tiles, of the last tile
-      for (int u = u0; ok && next(u); ++items) {
-        const int cnt = it.t1 - it.t0, first_tail = it.L / 128 - it.t0;
-        items == 0 ? wait(q_first, 0) : wait(q_full, (items - 1) & 1);
-        for (int j = 0; j <= cnt && ok; ++j) {
-          const uint32_t v_before = v;
-          if (j < cnt) {
-            const uint32_t k = at.next<NST>(), last = j & 1 ? last1 : last0;
-            v = at.next<NST>();
-            if (!wait(&full[Stage::slot(k)], Stage::parity(k))) break;
-            // the last P that stood where these scores go has been read: its
-            // product released the stage of its values
-            if (last != kNone && !wait(&empty[Stage::slot(last)], Stage::parity(last))) break;
-            ptx::tc_fence_after();
-            const uint32_t kt = ptx::desc_lo(ptx::smem_u32(ring + Stage::slot(k) * S::STAGE), 16u);
-            const uint32_t ds = tmem + 128 * (j & 1);
+    // the whole warp, for operands in uniform registers; one thread issues
+    const uint32_t lead = ptx::elect_one(), tm = __shfl_sync(~0u, tmem, 0);
+    auto whole = [&](bool) { return ok = __all_sync(~0u, ok); };
+    constexpr uint32_t IDESC1 = ptx::idesc_bf16_f32(128, 128);
+    constexpr uint32_t IDESC2 = ptx::idesc_bf16_f32(128, D, true);
+    const uint32_t q_lo = ptx::desc_lo(ptx::smem_u32(qimg), 16u);
+    constexpr uint32_t kNone = ~0u;
+    Stage at;
+    uint32_t items = 0, p_turn = 0, c_turn = 0;    // parities of p_full and v_clean
+    uint32_t last0 = kNone, last1 = kNone, v = 0;  // value stages of the sets' last tiles, of the last tile
+    for (int u = u0; ok && next(u); ++items) {
+      const int cnt = __shfl_sync(~0u, it.t1 - it.t0, 0), first_tail = __shfl_sync(~0u, it.L / 128 - it.t0, 0);
+      whole(items == 0 ? wait(q_first, 0) : wait(q_full, (items - 1) & 1));
+      for (int j = 0; j <= cnt && ok; ++j) {
+        const uint32_t v_before = v;
+        if (j < cnt) {
+          const uint32_t k = at.next<NST>(), last = j & 1 ? last1 : last0;
+          v = at.next<NST>();
+          // the last P that stood where these scores go has been read: its
+          // product released the stage of its values
+          uint64_t* there = &full[Stage::slot(k)];
+          if (!whole(last == kNone ? wait(there, Stage::parity(k))
+                                   : wait2(there, Stage::parity(k), &empty[Stage::slot(last)], Stage::parity(last))))
+            break;
+          ptx::tc_fence_after();
+          const uint32_t kt = ptx::desc_lo(ptx::smem_u32(ring + Stage::slot(k) * S::STAGE), 16u);
+          const uint32_t ds = tm + 128 * (j & 1);
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              const uint32_t to = ((kk >> 2) * kRegion + 32u * (kk & 3)) >> 4;
-              if (kk == 0)
-                ptx::mma_bf16_lo<false>(ds, q_lo, kt, IDESC1);
-              else
-                ptx::mma_bf16_lo<true>(ds, q_lo + to, kt + to, IDESC1);
-              if (F32) ptx::mma_bf16_lo<true>(ds, q_lo + to + (128u * D * 2 >> 4), kt + to, IDESC1);
-            }
-            ptx::mma_commit(&s_full[j & 1]);
-            ptx::mma_commit(&empty[Stage::slot(k)]);
-            if (j == cnt - 1) ptx::mma_commit(q_empty);
-            if (j & 1)
-              last1 = v;
-            else
-              last0 = v;
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t to = ((kk >> 2) * kRegion + 32u * (kk & 3)) >> 4;
+            ptx::mma_bf16_lo(lead, ds, q_lo + to, kt + to, IDESC1, kk > 0 ? 1u : 0u);
+            if (F32) ptx::mma_bf16_lo(lead, ds, q_lo + to + (128u * D * 2 >> 4), kt + to, IDESC1, 1u);
           }
-          if (j > 0) {
-            const uint32_t i = (j - 1) & 1;
-            if (!wait(&p_full[i], (p_turn >> i) & 1)) break;
-            p_turn ^= 1u << i;
-            if (j <= 2 && items > 0 && !wait(o_empty, (items - 1) & 1)) break;
-            const int tail = j - 1 - first_tail;  // the tiles that hold entries from L on
-            if (tail < 0) {
-              if (!wait(&full[Stage::slot(v_before)], Stage::parity(v_before))) break;
-            } else {
-              if (!wait(&v_clean[tail], (c_turn >> tail) & 1)) break;
-              c_turn ^= 1u << tail;
-            }
-            ptx::tc_fence_after();
-            const uint32_t vt = ptx::desc_lo(ptx::smem_u32(ring + Stage::slot(v_before) * S::STAGE), kRegion);
-            const uint32_t ds = tmem + 256 + 128 * i, ps = tmem + 128 * i;
+          ptx::mma_commit_if(lead, &s_full[j & 1]);
+          if (j == cnt - 1) ptx::mma_commit_if(lead, q_empty);
+          if (j & 1)
+            last1 = v;
+          else
+            last0 = v;
+        }
+        if (j > 0) {
+          const uint32_t i = (j - 1) & 1;
+          const int tail = j - 1 - first_tail;  // the tiles that hold entries from L on
+          uint64_t* there = tail < 0 ? &full[Stage::slot(v_before)] : &v_clean[tail];
+          const uint32_t parity = tail < 0 ? Stage::parity(v_before) : (c_turn >> tail) & 1;
+          if (!whole(wait2(there, parity, &p_full[i], (p_turn >> i) & 1))) break;
+          p_turn ^= 1u << i;
+          if (tail >= 0) c_turn ^= 1u << tail;
+          if (j <= 2 && items > 0 && !whole(wait(o_empty, (items - 1) & 1))) break;
+          ptx::tc_fence_after();
+          const uint32_t vt = ptx::desc_lo(ptx::smem_u32(ring + Stage::slot(v_before) * S::STAGE), kRegion);
+          const uint32_t ds = tm + 256 + 128 * i, ps = tm + 128 * i;
 #pragma unroll
-            for (int kk = 0; kk < 8; ++kk) {
-              ptx::mma_bf16_ta_lo(ds, ps + 16u * kk, vt + 128u * kk, IDESC2, j > 2 || kk > 0 ? 1u : 0u);
-              ptx::mma_bf16_ta_lo(ds, ps + 16u * kk + 8, vt + 128u * kk, IDESC2, 1u);
-            }
-            ptx::mma_commit(&empty[Stage::slot(v_before)]);
-            if (j == cnt) ptx::mma_commit(o_full);
+          for (int kk = 0; kk < 8; ++kk) {
+            ptx::mma_bf16_ta_lo(lead, ds, ps + 16u * kk, vt + 128u * kk, IDESC2, j > 2 || kk > 0 ? 1u : 0u);
+            ptx::mma_bf16_ta_lo(lead, ds, ps + 16u * kk + 8, vt + 128u * kk, IDESC2, 1u);
           }
+          ptx::mma_commit_if(lead, &empty[Stage::slot(v_before)]);
+          if (j == cnt) ptx::mma_commit_if(lead, o_full);
         }
       }
-      // no product is running when TMEM is freed
-      ptx::mma_commit(drain);
-      ptx::mbar_wait(drain, 0, ptx::kDrainNs);
     }
+    // no product is running when TMEM is freed
+    ptx::mma_commit_if(lead, drain);
+    ptx::mbar_wait(drain, 0, ptx::kDrainNs);
   } else if (warp < 4) {
     const int t64 = tid - 64;
     uint32_t n = 0, items = 0, turn = 0;
@@ -439,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t ts = tl + 128 * set + 64 * half, to = tl + 256 + 128 * set + half * (D / 2);
     const int G = a.nq / a.nkv;
     const float c = a.scale_log2;
-    uint32_t ns = 0, items = 0, c_turn = 0;
+    uint32_t ns = 0, items = 0, c_turn = 0, before = 0;  // tiles of this CTA before the item
     int u = u0;
     bool more = next(u);
     while (more) {
@@ -452,6 +455,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m = -INFINITY, l = 0.f;
       for (int j = set; j < cnt; j += 2, ++ns) {
         wait(&s_full[set], ns & 1);
+        // (the tile's keys have been read)
+        if (half == 0 && quad == 0 && lane == 0) ptx::mbar_arrive(&empty[2 * (before + j) % NST]);
         ok = __all_sync(~0u, ok);
         // (a warp without a query leaves what it has in the place of P: it reaches
         // the accumulators of rows that are not read)
@@ -626,6 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(o_empty);
       if constexpr (!DIRECT) it = s_next[items & 1];
+      before += cnt;
       more = !DIRECT && it.rows > 0;
       ++items;
     }
@@ -657,13 +663,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // The parts of items cut between CTAs, joined in CTA order: a CTA per 32 queries and
 // 32 dims of an item, a lane per query (16 bytes each side by side in a part), a
-// warp per four dims, eight parts in flight.  (One CTA for all dims, a quarter of
-// the CTAs: a tree of 64 rows 50 us, now 35.)
+// warp per four dims, U parts in flight.  (One CTA for all dims, a quarter of
+// the CTAs: a tree of 64 rows 50 us, now 31.)  U: 8, but 4 where with 8, whose
+// registers let three CTAs run per SM, not all would run at once: 16 ragged requests
+// (1024 CTAs) 41.4 / 39.9 us with 8 / 4, a tree of 64 rows (256) 31.4 / 33.4.
 constexpr int kCombineWarps = 8;
-template <int D, bool F32>
-__global__ void __launch_bounds__(32 * kCombineWarps)
+template <int D, bool F32, int U>
+__global__ void __launch_bounds__(32 * kCombineWarps, U == 8 ? 3 : 5)
     tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas, int turn) {
-  constexpr int Z = D / 4 / kCombineWarps, U = 8;
+  constexpr int Z = D / 4 / kCombineWarps;
   __shared__ UnitPlan plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int b = blockIdx.z, g = blockIdx.y, quad = blockIdx.x % Z * kCombineWarps + warp;
@@ -673,6 +681,10 @@ __global__ void __launch_bounds__(32 * kCombineWarps)
   // its own wait, so what ran before that kernel is done, and it writes none.
   // (No CTA ends before it: what follows in the stream waits for this kernel.)
   ptx::griddep_launch_dependents();
+  if (q - lane >= rows * G) {
+    ptx::griddep_wait();
+    return;
+  }
   if (warp == 0) make_plan(a, 128, turn, lane, plan, false);
   __syncthreads();
   const int tiles = plan.tiles[b];
@@ -743,7 +755,9 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                                    (int)kShares, turn);
   if (e != cudaSuccess) return e;
-  return launch_pdl(tree_combine_kernel<D, F32>, dim3(direct.x * 4 * (D / 4 / kCombineWarps), direct.y, direct.z),
+  const dim3 join(direct.x * 4 * (D / 4 / kCombineWarps), direct.y, direct.z);
+  const bool few = (int64_t)join.x * join.y * join.z <= 3 * sms;
+  return launch_pdl(few ? tree_combine_kernel<D, F32, 8> : tree_combine_kernel<D, F32, 4>, join,
                     dim3(32 * kCombineWarps), 0, st, 1, a, ws, ctas, turn);
 }
 
