@@ -721,8 +721,8 @@ class Cache:
 
     def __init__(self, k, v):
         import torch
-        self._device = torch.cuda.current_device
-        device = self._device()
+        self._current = torch.cuda.current_device
+        device = self._on = self._current()
         kp = _tensor(k, "k", device, (torch.bfloat16,))
         if k.dim() != 5:
             raise ValueError("k must have shape [n_layers, batch, n_kv, capacity, head_dim]")
@@ -741,6 +741,12 @@ class Cache:
                "as2d_cache_evict_workspace")
         self._workspace = torch.empty(max(most, need.value), dtype=torch.uint8, device=k.device)
         self._workspace_at = self._workspace.data_ptr(), self._workspace.numel()
+
+    def _device(self):
+        device = self._current()
+        if device != self._on:
+            raise ValueError("the cache must be on the current CUDA device")
+        return device
 
     def _counts(self, values, name):
         if len(values) != self.shape[1]:

@@ -197,9 +197,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (int u = u0; warp >= 2 && next_segment(plan, a, u, u1, s)) {
     // the first pass, by every warp that has nothing to do yet
     const int q = tid - 64;
-    bring(s.it, q, std::integral_constant<int, kThreads - 64>{}, std::integral_constant<int, 4>{}, std::false_type{}, [&] {
-      if (q < 128) sums_of(s.it, q, s_lse[q], s_vis[q]);
-    });
+    bring(s.it, q, std::integral_constant<int, kThreads - 64>{}, std::integral_constant<int, 4>{}, std::false_type{},
+          [&] {
+            if (q < 128) sums_of(s.it, q, s_lse[q], s_vis[q]);
+          });
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(q_first);
   }
@@ -285,8 +286,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         float l;
         uint64_t vis;
         if (q < 128) sums_of(s.it, q, l, vis);
-        bring(s.it, q, std::integral_constant<int, kBring>{}, std::integral_constant<int, kInFlight>{}, std::true_type{},
-              [&] { wait(q_empty, (pass - 1) & 1); });
+        bring(s.it, q, std::integral_constant<int, kBring>{}, std::integral_constant<int, kInFlight>{},
+              std::true_type{}, [&] { wait(q_empty, (pass - 1) & 1); });
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(q_full);
         if (q < 128) {
@@ -371,7 +372,8 @@ cudaError_t launch_attention_weights(const WeightArgs& a, int head_dim, int64_t 
   if (!encode_cache_map(&tk, a.t.k, head_dim, a.t.cap, (int64_t)a.t.rm.batch * a.t.nkv)) return cudaErrorInvalidValue;
   const int64_t units = (max_keys + 127) / 128 * tree_items(a.t);
   const int ctas = (int)(units < sms ? units : sms), turn = units > sms ? kTurn : 0;
-  if (head_dim == 128) return a.t.q_f32 ? launch<128, true>(tk, a, ctas, turn, st) : launch<128, false>(tk, a, ctas, turn, st);
+  if (head_dim == 128)
+    return a.t.q_f32 ? launch<128, true>(tk, a, ctas, turn, st) : launch<128, false>(tk, a, ctas, turn, st);
   return a.t.q_f32 ? launch<64, true>(tk, a, ctas, turn, st) : launch<64, false>(tk, a, ctas, turn, st);
 }
 

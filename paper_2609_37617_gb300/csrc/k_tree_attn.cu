@@ -37,10 +37,10 @@
 // of |q| |k|), 16-bit ones are exact.
 //
 // Bound by memory for the rows of a chain or a small tree (a key and value are
-// read once: 16 ragged requests, 126 MB, 39.9 us; in the loop 5.3 TB/s of a copy's
+// read once: 16 ragged requests, 126 MB, 39.1 us; in the loop 5.3 TB/s of a copy's
 // 6.8, the rest is start, turns and join), by the products and what stands
 // between them for more than 128 queries to a kv head (64 rows of seven over 15128
-// entries 32.0 us, the tensor pipe 3/4 busy in the loop), by the latency of one
+// entries 31.6 us, the tensor pipe 3/4 busy in the loop), by the latency of one
 // chain of launch, load, products for few entries (9 rows over 1564: 9.5 us).
 #include <algorithm>
 
@@ -80,7 +80,8 @@ struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;            // one K or V tile
   static constexpr uint32_t Q = (F32 ? 2 : 1) * 128 * D * 2;  // hi (and lo) image
   static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
-  static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16 + 2 * sizeof(Unit);
+  static constexpr uint32_t SMEM =
+      1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16 + 2 * sizeof(Unit);
   static_assert(SMEM + sizeof(UnitPlan) <= 232448, "shared memory of one CTA");
 };
 
@@ -293,7 +294,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     else
       return next_item(s_plan, a, u, u1, it);
   };
-  if (int u = u0; warp >= 2 && next(u)) {
+  bool some = false;  // (what `it` then holds, for the warps from 2 on)
+  if (int u = u0; warp >= 2 && (some = next(u))) {
     // the first item's queries, by every warp that has nothing to do yet (by two
     // warps 32-bit queries of 119 rows took 5 us)
     load_queries<D, F32, kThreads - 64, 4, false>(a, it, tid - 64, qimg, [] {});
@@ -422,7 +424,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp < 4) {
     const int t64 = tid - 64;
     uint32_t n = 0, items = 0, turn = 0;
-    for (int u = u0; next(u); ++items) {
+    int u = DIRECT ? u1 : it.next;
+    for (bool more = some; more; more = next(u), ++items) {
       const int first = it.L / 128;
       // the epilogue of the item before has read what was noted for it
       if (items > 0) wait(o_empty, (items - 1) & 1);
@@ -450,9 +453,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int G = a.nq / a.nkv;
     const float c = a.scale_log2;
     uint32_t ns = 0, items = 0, c_turn = 0, before = 0;  // tiles of this CTA before the item
-    int u = u0;
-    bool more = next(u);
-    while (more) {
+    for (bool more = some; more;) {
       const int cnt = it.t1 - it.t0, nqs = it.rows * G;
       const int q = it.qt * 128 + row, i = divide_group(a, q);
       const bool live = q < nqs;
@@ -752,15 +753,15 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
                       (int)kWhole, 0);
   if (most_tiles <= kClusterTiles &&
       items <= resident_clusters(clusters, tree_attn_kernel<D, F32, true>, kThreads, S::SMEM, kRanks))
-    return launch_pdl(tree_attn_kernel<D, F32, true>, dim3(direct.x * kRanks, direct.y, direct.z), dim3(kThreads), S::SMEM, st, kRanks, tk,
-                      tv, a, ws, (int)kCluster, 0);
+    return launch_pdl(tree_attn_kernel<D, F32, true>, dim3(direct.x * kRanks, direct.y, direct.z), dim3(kThreads),
+                      S::SMEM, st, kRanks, tk, tv, a, ws, (int)kCluster, 0);
   // No more CTAs to an item than pay for the joining of their parts.  us, one item
   // of 8100 / 15128 / 60000 entries: at most 16 15.7 / 20.2 / 46.5, 32 14.9 / 17.8 / 30.7,
   // 64 18.4 / 19.0 / 26.5, as many as there are SMs 18.4 / 25.5 / 38.8.
   const int64_t most_ctas = items * (16 + most_tiles / 8);
   const int ctas = (int)std::min(std::min<int64_t>(units, sms), most_ctas), turn = units > sms ? kTurn : 0;
   e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
-                                   (int)kShares, turn);
+                 (int)kShares, turn);
   if (e != cudaSuccess) return e;
   const dim3 join(direct.x * 4 * (D / 4 / kCombineWarps), direct.y, direct.z);
   const bool few = (int64_t)join.x * join.y * join.z <= 3 * sms;

@@ -5,9 +5,9 @@
 // An item is one (request, kv head, query tile), a unit one tile of 128 keys of
 // an item or, at its head, one of `extra` units that stand for what a CTA spends on
 // turning to another item (its queries, its epilogue): a CTA that ends one item
-// and begins another gets fewer tiles.  Items and their units are numbered request by request, kv head by kv
-// head, query tile by query tile (the query tiles of a head read its keys one
-// after another, from L2).
+// and begins another gets fewer tiles.  Items and their units are numbered request
+// by request, kv head by kv head, query tile by query tile (the query tiles of a
+// head read its keys one after another, from L2).
 #pragma once
 
 #include "ops.h"

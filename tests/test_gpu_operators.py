@@ -672,3 +672,16 @@ def test_probs_and_acceptance_off_16_bytes(lib):
     lib.accept_sampled(dev, torch.tensor(cand, dtype=torch.int32, device="cuda"), [2, 1],
                        torch.from_numpy(u).cuda(), n, tok)
     assert (n.tolist(), tok.tolist()) == ref.accept(rows.astype(np.float64), None, cand, [2, 1], u.astype(np.float64))
+
+
+def test_cache_of_another_device(lib, monkeypatch):
+    """A cache made on one device is refused while another is current."""
+    x = Inputs((4, 2, 64), [40], [3], ref.tree_masks([3], np.random.default_rng(1)))
+    cache = lib.Cache(x.k, x.v)
+    monkeypatch.setattr(cache, "_current", lambda: x.k.get_device() + 1)
+    w = torch.zeros(x.k.shape[:4], device="cuda")
+    for call in (lambda: cache.tree_attention(x.q, x.kv_len, x.rows, x.visible),
+                 lambda: cache.attention_weights(x.q, w, w, x.kv_len, x.rows, x.visible),
+                 lambda: cache.evict(w, x.kv_len, [20])):
+        with pytest.raises(ValueError, match="current CUDA device"):
+            call()
