@@ -37,10 +37,10 @@
 // of |q| |k|), 16-bit ones are exact.
 //
 // Bound by memory for the rows of a chain or a small tree (a key and value are
-// read once: 16 ragged requests, 126 MB, 39.1 us; in the loop 5.3 TB/s of a copy's
+// read once: 16 ragged requests, 126 MB, 38.7 us; in the loop 5.3 TB/s of a copy's
 // 6.8, the rest is start, turns and join), by the products and what stands
 // between them for more than 128 queries to a kv head (64 rows of seven over 15128
-// entries 31.6 us, the tensor pipe 3/4 busy in the loop), by the latency of one
+// entries 30.8 us, the tensor pipe 3/4 busy in the loop), by the latency of one
 // chain of launch, load, products for few entries (9 rows over 1564: 9.5 us).
 #include <algorithm>
 
@@ -82,7 +82,7 @@ struct Shape {
   static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
   static constexpr uint32_t SMEM =
       1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16 + 2 * sizeof(Unit);
-  static_assert(SMEM + sizeof(UnitPlan) <= 232448, "shared memory of one CTA");
+  static_assert(SMEM + sizeof(UnitPlan) + sizeof(First) <= 232448, "shared memory of one CTA");
 };
 
 // The weight of a part (maximum m) beside a maximum M: 0 where the part holds
@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t* tslot = reinterpret_cast<uint32_t*>(s_bad + 1);
   Unit* s_next = reinterpret_cast<Unit*>(tslot + 2);  // [2] the item after one of this parity
   __shared__ UnitPlan s_plan;
+  __shared__ First s_first;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -259,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  int u0 = 0, u1 = 0;
+  int u1 = 0;
   Unit it;
   if constexpr (DIRECT) {
     // grid: (query tile and rank, kv head, request)
@@ -280,22 +281,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     it.t1 = min(it.t0 + per, it.tiles);
     u1 = it.t0 < it.t1 ? 1 : 0;
   } else {
-    if (warp == 0) make_plan(a, 128, turn, lane, s_plan, blockIdx.x == 0);
+    if (warp == 0) {
+      make_plan(a, 128, turn, lane, s_plan, blockIdx.x == 0);
+      first_item(s_plan, a, blockIdx.x, gridDim.x, lane, s_first);
+    }
   }
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tslot;
-  if constexpr (!DIRECT) unit_range(s_plan, blockIdx.x, gridDim.x, u0, u1);
-  // The CTA's items one after another, each with its tiles, in `it`.
-  auto next = [&](int& u) {
+  if constexpr (!DIRECT) it = s_first.it, u1 = s_first.u1;
+  const bool some = DIRECT ? u1 > 0 : it.rows > 0;
+  // The CTA's items one after another, each with its tiles, in `it` (the first is there).
+  auto next = [&] {
     if constexpr (DIRECT)
-      return u++ < u1;
-    else
+      return false;
+    else {
+      int u = it.next;
       return next_item(s_plan, a, u, u1, it);
+    }
   };
-  bool some = false;  // (what `it` then holds, for the warps from 2 on)
-  if (int u = u0; warp >= 2 && (some = next(u))) {
+  if (warp >= 2 && some) {
     // the first item's queries, by every warp that has nothing to do yet (by two
     // warps 32-bit queries of 119 rows took 5 us)
     load_queries<D, F32, kThreads - 64, 4, false>(a, it, tid - 64, qimg, [] {});
@@ -326,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) {
       const uint64_t pol = ptx::policy_evict_first();
       uint32_t n = 0, tail = 0, turn = 0;  // slots whose last tile is on tail_full, its parity
-      for (int u = u0; next(u);) {
+      for (bool more = some; more; more = next()) {
         const int z = it.b * a.nkv + it.g;
         for (int t = it.t0; t < it.t1 && ok; ++t)
           for (int kv = 0; kv < 2; ++kv, ++n) {
@@ -366,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     Stage at;
     uint32_t items = 0, p_turn = 0, c_turn = 0;    // parities of p_full and v_clean
     uint32_t last0 = kNone, last1 = kNone, v = 0;  // value stages of the sets' last tiles, of the last tile
-    for (int u = u0; ok && next(u); ++items) {
+    for (bool more = some; ok && more; more = next(), ++items) {
       const int cnt = __shfl_sync(~0u, it.t1 - it.t0, 0), first_tail = __shfl_sync(~0u, it.L / 128 - it.t0, 0);
       whole(items == 0 ? wait(q_first, 0) : wait(q_full, (items - 1) & 1));
       for (int j = 0; j <= cnt && ok; ++j) {
@@ -424,8 +430,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp < 4) {
     const int t64 = tid - 64;
     uint32_t n = 0, items = 0, turn = 0;
-    int u = DIRECT ? u1 : it.next;
-    for (bool more = some; more; more = next(u), ++items) {
+    for (bool more = some; more; more = next(), ++items) {
       const int first = it.L / 128;
       // the epilogue of the item before has read what was noted for it
       if (items > 0) wait(o_empty, (items - 1) & 1);
@@ -647,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (DIRECT && mode == kCluster) {
     // (the groups of a CTA with tiles have passed the first barrier above)
     __syncwarp();
-    if (warp < 4 || u0 == u1) ptx::cluster_sync();
+    if (warp < 4 || !some) ptx::cluster_sync();
     ptx::cluster_sync();
     // the parts of four dims of a query, in rank order
     const int t = tid - 128, quad = t >> 7, row = t & 127, q = it.qt * 128 + row, G = a.nq / a.nkv;

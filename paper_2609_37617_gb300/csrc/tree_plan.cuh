@@ -88,18 +88,10 @@ __device__ __forceinline__ int unit_owner(const UnitPlan& p, int u, int ctas) {
   return u < wide ? u / (each + 1) : more + (u - wide) / each;
 }
 
-// What is done of unit u's item from u on, up to unit u1 at most; `next`: the
-// first unit after that.  May hold no tile.
-__device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, int u, int u1) {
+// What is done of unit u's item (of request lo) from u on, up to unit u1 at most;
+// `next`: the first unit after that.  May hold no tile.
+__device__ __forceinline__ Unit unit_of(const UnitPlan& p, const TreeArgs& a, int lo, int u, int u1) {
   Unit it;
-  int lo = 0, hi = kMaxBatch - 1;  // the last request whose first unit is at or before u
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (p.unit[mid] <= u)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
   it.b = lo;
   it.tiles = p.tiles[lo];
   it.L = p.len[lo];
@@ -115,6 +107,18 @@ __device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, in
   return it;
 }
 
+__device__ __forceinline__ Unit unit_at(const UnitPlan& p, const TreeArgs& a, int u, int u1) {
+  int lo = 0, hi = kMaxBatch - 1;  // the last request whose first unit is at or before u
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (p.unit[mid] <= u)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return unit_of(p, a, lo, u, u1);
+}
+
 // The same of the first item from u on of which there is a tile to do; u: the first
 // unit after it.  False past unit u1.  (Not inlined: the kernels' roles run it once
 // an item each, and are short of instruction cache.)
@@ -125,6 +129,34 @@ static __device__ __noinline__ bool next_item(const UnitPlan& p, const TreeArgs&
     if (it.t0 < it.t1) return true;
   }
   return false;
+}
+
+// By a whole warp: the last request whose first unit is at or before u.
+__device__ __forceinline__ int request_of(const UnitPlan& p, int u, int lane) {
+  int lo = -1;
+#pragma unroll
+  for (int h = 0; h < kMaxBatch / 32; ++h) lo += __popc(__ballot_sync(~0u, p.unit[32 * h + lane] <= u));
+  return lo;
+}
+// A CTA's share and its first item (rows 0: none), found by the warp that made the
+// plan for all of them: each on its own spent 1 us on it.
+struct First {
+  Unit it;
+  int u1;
+};
+__device__ __forceinline__ void first_item(const UnitPlan& p, const TreeArgs& a, int c, int ctas, int lane, First& f) {
+  __syncwarp();
+  int u0, u1;
+  unit_range(p, c, ctas, u0, u1);
+  const int lo = request_of(p, u0, lane);
+  Unit it;
+  it.rows = 0;
+  if (u0 < u1) {
+    it = unit_of(p, a, lo, u0, u1);
+    int u = it.next;
+    if (it.t0 >= it.t1 && !next_item(p, a, u, u1, it)) it.rows = 0;
+  }
+  if (lane == 0) f.it = it, f.u1 = u1;
 }
 
 // ln of a sum l of powers of two relative to 2^M; -inf of nothing.
