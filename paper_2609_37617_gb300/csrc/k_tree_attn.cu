@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // The parts of items cut between CTAs, joined in CTA order: a CTA per 32 queries and
 // 32 dims of an item, a lane per query (16 bytes each side by side in a part), a
 // warp per four dims, U parts in flight.  (One CTA for all dims, a quarter of
-// the CTAs: a tree of 64 rows 50 us, now 31.)  U: 8, but 4 where with 8, whose
+// the CTAs: a tree of 64 rows 50 us, then 35.)  U: 8, but 4 where with 8, whose
 // registers let three CTAs run per SM, not all would run at once: 16 ragged requests
 // (1024 CTAs) 41.4 / 39.9 us with 8 / 4, a tree of 64 rows (256) 31.4 / 33.4.
 constexpr int kCombineWarps = 8;
@@ -735,12 +735,14 @@ __global__ void __launch_bounds__(32 * kCombineWarps, U == 8 ? 3 : 5)
   if (quad == 0 && a.lse) a.lse[(size_t)(r0 + i) * a.nq + h] = row_lse(M, l);
 }
 
-// Items of at most this many key tiles are each done by one CTA.
+// Items of at most this many key tiles are each done by one CTA.  us, in one CTA /
+// by clusters: four items of two tiles 6.7 / 6.9, of three 8.2 / 7.2.
 constexpr int kWholeTiles = 2;
 // A call whose clusters all run at once is done by clusters, unless its items are
 // longer than this.  us, even shares / clusters, rows of seven queries: 4 items of
-// 1564 entries 14.0 / 9.8, 15 14.6 / 10.9, 16 (one more than run at once) 14.6 / 17.9;
-// one of 8100 14.9 / 17.3, 4 17.4 / 17.5, 15 20.7 / 18.3; 4 of 15128 19.8 / 25.5.
+// 1564 entries 10.2 / 8.9, 15 14.0 / 9.6, 16 (one more than run at once) 13.6 / 13.7; 4
+// of 6000 14.9 / 13.9; one of 8100 14.0 / 15.7, 4 15.8 / 16.3, 15 22.0 / 18.5; 4 of
+// 15128 19.6 / 23.2.
 constexpr int kClusterTiles = 6 * kRanks;
 
 template <int D, bool F32>
@@ -761,8 +763,8 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
     return launch_pdl(tree_attn_kernel<D, F32, true>, dim3(direct.x * kRanks, direct.y, direct.z), dim3(kThreads),
                       S::SMEM, st, kRanks, tk, tv, a, ws, (int)kCluster, 0);
   // No more CTAs to an item than pay for the joining of their parts.  us, one item
-  // of 8100 / 15128 / 60000 entries: at most 16 15.7 / 20.2 / 46.5, 32 14.9 / 17.8 / 30.7,
-  // 64 18.4 / 19.0 / 26.5, as many as there are SMs 18.4 / 25.5 / 38.8.
+  // of 8100 / 15128 / 60000 entries: at most 16 14.3 / 18.9 / 46.7, 32 13.4 / 16.3 / 30.4,
+  // 64 16.5 / 17.7 / 26.0, as many as there are SMs 16.5 / 24.0 / 42.5; so 13.8 / 16.1 / 26.7.
   const int64_t most_ctas = items * (16 + most_tiles / 8);
   const int ctas = (int)std::min(std::min<int64_t>(units, sms), most_ctas), turn = units > sms ? kTurn : 0;
   e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
