@@ -2,6 +2,9 @@
 masks where they can go wrong, what they must leave alone, streams, captured
 graphs and a run of them together."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -685,3 +688,50 @@ def test_cache_of_another_device(lib, monkeypatch):
                  lambda: cache.evict(w, x.kv_len, [20])):
         with pytest.raises(ValueError, match="current CUDA device"):
             call()
+
+
+FIRST_USE = """
+import torch
+import paper_2609_37617_gb300 as lib
+g = torch.Generator(device="cuda").manual_seed(3)
+k, v = (torch.randn((1, 2, 4, 2000, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+cache, rows = lib.Cache(k, v), [9, 4]
+q = torch.randn((13, 28, 128), generator=g, device="cuda")
+kv_len = torch.tensor([1900, 333], dtype=torch.int32, device="cuda")
+lse, out = torch.empty((13, 28), device="cuda"), torch.empty_like(q)
+w = torch.rand((1, 2, 4, 2000), generator=g, device="cuda")
+logits = torch.randn((90, 152064), generator=g, device="cuda")
+probs = torch.empty_like(logits)
+cand = torch.zeros(8, dtype=torch.int32, device="cuda")
+u = torch.full((9,), 0.5, device="cuda")
+n, tok = (torch.empty(1, dtype=torch.int32, device="cuda") for _ in range(2))
+state = [t.clone() for t in (k, v, w, kv_len)]
+
+def step(s):
+    cache.tree_attention(q, kv_len, rows, out=out, lse=lse, stream=s)
+    cache.attention_weights(q, lse, w, kv_len, rows, stream=s)
+    cache.evict(w, kv_len, [1000, 300], recent=16, stream=s)
+    lib.token_probs(logits, 0.8, out=probs, stream=s)
+    lib.accept_sampled(probs[:9], cand, [8], u, n, tok, stream=s)
+
+def results():
+    torch.cuda.synchronize()
+    return [t.clone() for t in (out, lse, w, k, v, kv_len, probs, n, tok)]
+torch.cuda.synchronize()
+s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph, stream=s):
+    step(s.cuda_stream)
+graph.replay()
+first = results()
+for t, old in zip((k, v, w, kv_len), state):
+    t.copy_(old)
+torch.cuda.synchronize()
+step(0)
+assert all(torch.equal(a, b) for a, b in zip(results(), first))
+"""
+
+
+def test_first_use_under_capture(lib):
+    """A process whose first call of each operator is captured."""
+    subprocess.run([sys.executable, "-c", FIRST_USE], check=True, timeout=120,
+                   cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
