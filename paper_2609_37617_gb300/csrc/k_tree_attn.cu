@@ -441,8 +441,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t s = (n + 2 * (t - it.t0) + 1) % NST;
           const bool here = wait(&tail_full[s], (turn >> s) & 1);
           turn ^= 1u << s;
-          if (here)
-            clean_tile<D>(ring + s * S::STAGE, t * 128, it.L, it.L + it.rows, t64, s_bad);
+          if (!here) continue;  // (nor is this one let go)
+          clean_tile<D>(ring + s * S::STAGE, t * 128, it.L, it.L + it.rows, t64, s_bad);
           ptx::fence_proxy_async_smem();
           ptx::mbar_arrive(&v_clean[t - first]);
         }
@@ -468,8 +468,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m = -INFINITY, l = 0.f;
       for (int j = set; j < cnt; j += 2, ++ns) {
         wait(&s_full[set], ns & 1);
-        // (the tile's keys have been read)
-        if (half == 0 && quad == 0 && lane == 0) ptx::mbar_arrive(&empty[2 * (before + j) % NST]);
+        // (the tile's keys have been read; after a wait that gave up they may not be there
+        // yet, and their stage is not given back)
+        if (ok && half == 0 && quad == 0 && lane == 0) ptx::mbar_arrive(&empty[2 * (before + j) % NST]);
         ok = __all_sync(~0u, ok);
         // (a warp without a query leaves what it has in the place of P: it reaches
         // the accumulators of rows that are not read)

@@ -533,6 +533,40 @@ def test_prefill_after_an_eviction(pair):
     b.close()
 
 
+@pytest.mark.parametrize("length,cap", [(L0, CAP), (3000, 3100), (8000, 8100)])
+def test_waits_that_run_out(pair, length, cap):
+    """A wait limit of 0 in the attention of trees and the gathered weights: the call
+    comes to an end and is flagged, and with the limit restored the next one gives
+    what it gives on a fresh state.  (One CTA to an item, a cluster, even shares.)"""
+    import paper_2609_37617_gb300 as lib
+    cfg, cand, parents = pair.cfg, [1, 2, 3, 4], [0, 0, 1, 2]
+    fresh, st = (pair.state([length], cap, [5]) for _ in range(2))
+    w0, w1 = (torch.zeros(st.kc.shape[:4], device="cuda") for _ in range(2))
+    fresh.track_weights(w0)
+    want = run_tree(fresh, cfg, [cand], [parents])
+    k0, v0 = st.kc.clone(), st.vc.clone()
+    st.track_weights(w1)
+    st.set_wait_limit(0)
+    for _ in range(3):
+        run_tree(st, cfg, [cand], [parents], want_logits=False)
+        st.rollback([length], [5])
+    torch.cuda.synchronize()
+    with pytest.raises(lib.AS2DError, match="timed out"):
+        st.check()
+    st.check()
+    st.set_wait_limit(2_000_000_000)
+    st.rollback([length], [5])
+    for t, old in ((st.kc, k0), (st.vc, v0)):
+        t.copy_(old)
+    w1.zero_()
+    torch.cuda.synchronize()
+    got = run_tree(st, cfg, [cand], [parents])
+    st.check()
+    assert got[0] == want[0] and got[1] == want[1] and np.array_equal(got[3], want[3]) and torch.equal(w0, w1)
+    st.close()
+    fresh.close()
+
+
 def test_a_state_without_the_operators_is_as_before(pair):
     """Calls before, between and after calls along trees give the same bits."""
     cfg = pair.cfg
