@@ -40,7 +40,7 @@
 // read once: 16 ragged requests, 126 MB, 38.7 us; in the loop 5.3 TB/s of a copy's
 // 6.8, the rest is start, turns and join), by the products and what stands
 // between them for more than 128 queries to a kv head (64 rows of seven over 15128
-// entries 30.8 us, the tensor pipe 3/4 busy in the loop), by the latency of one
+// entries 29.6 us, the tensor pipe 3/4 busy in the loop), by the latency of one
 // chain of launch, load, products for few entries (9 rows over 1564: 9.5 us).
 #include <algorithm>
 
@@ -678,12 +678,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 // The parts of items cut between CTAs, joined in CTA order: a CTA per 32 queries and
 // 32 dims of an item, a lane per query (16 bytes each side by side in a part), a
 // warp per four dims, U parts in flight.  (One CTA for all dims, a quarter of
-// the CTAs: a tree of 64 rows 50 us, then 35.)  U: 8, but 4 where with 8, whose
-// registers let three CTAs run per SM, not all would run at once: 16 ragged requests
-// (1024 CTAs) 41.4 / 39.9 us with 8 / 4, a tree of 64 rows (256) 31.4 / 33.4.
+// the CTAs: a tree of 64 rows 50 us, then 35.)  U: as many of 12, 8 and 4 as let all
+// CTAs run at once, 2, 3 and 5 per SM.  us with 12 / 8, 256 CTAs: a tree of 64 rows
+// 29.3 / 30.4, one item of 60000 entries 25.4 / 26.6; with 4 / 8, 384 CTAs: six requests
+// of 4000 entries 20.4 / 19.3; 1024 CTAs: 16 ragged requests 39.9 / 41.4.
 constexpr int kCombineWarps = 8;
 template <int D, bool F32, int U>
-__global__ void __launch_bounds__(32 * kCombineWarps, U == 8 ? 3 : 5)
+__global__ void __launch_bounds__(32 * kCombineWarps, U == 12 ? 2 : U == 8 ? 3 : 5)
     tree_combine_kernel(const __grid_constant__ TreeArgs a, TreeWork ws, int ctas, int turn) {
   constexpr int Z = D / 4 / kCombineWarps;
   __shared__ UnitPlan plan;
@@ -765,16 +766,19 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
                       S::SMEM, st, kRanks, tk, tv, a, ws, (int)kCluster, 0);
   // No more CTAs to an item than pay for the joining of their parts.  us, one item
   // of 8100 / 15128 / 60000 entries: at most 16 14.3 / 18.9 / 46.7, 32 13.4 / 16.3 / 30.4,
-  // 64 16.5 / 17.7 / 26.0, as many as there are SMs 16.5 / 24.0 / 42.5; so 13.8 / 16.1 / 26.7.
+  // 64 16.5 / 17.7 / 26.0, as many as there are SMs 16.5 / 24.0 / 42.5; so 13.8 / 16.1 / 26.7
+  // (all with eight parts of the join in flight).
   const int64_t most_ctas = items * (16 + most_tiles / 8);
   const int ctas = (int)std::min(std::min<int64_t>(units, sms), most_ctas), turn = units > sms ? kTurn : 0;
   e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                  (int)kShares, turn);
   if (e != cudaSuccess) return e;
   const dim3 join(direct.x * 4 * (D / 4 / kCombineWarps), direct.y, direct.z);
-  const bool few = (int64_t)join.x * join.y * join.z <= 3 * sms;
-  return launch_pdl(few ? tree_combine_kernel<D, F32, 8> : tree_combine_kernel<D, F32, 4>, join,
-                    dim3(32 * kCombineWarps), 0, st, 1, a, ws, ctas, turn);
+  const int64_t joins = (int64_t)join.x * join.y * join.z;
+  return launch_pdl(joins <= 2 * sms   ? tree_combine_kernel<D, F32, 12>
+                    : joins <= 3 * sms ? tree_combine_kernel<D, F32, 8>
+                                       : tree_combine_kernel<D, F32, 4>,
+                    join, dim3(32 * kCombineWarps), 0, st, 1, a, ws, ctas, turn);
 }
 
 }  // namespace
