@@ -79,8 +79,8 @@ as2d_status check_rows(const as2d_cache* c, int32_t layer, const as2d_tree_rows*
   a.v = (const bf16*)c->v + at;
   max_keys = (r->max_len > 0 ? r->max_len : c->capacity) + most;
   if (max_keys > c->capacity) max_keys = c->capacity;
-  // units of work, counted in 32 bits on the device
-  const int64_t tiles = (c->capacity + 127) / 128, G = r->n_q / c->n_kv;
+  // units of work (tiles, and up to eight for each turn), counted in 32 bits on the device
+  const int64_t tiles = (c->capacity + 127) / 128 + 8, G = r->n_q / c->n_kv;
   if ((a.rm.rows * G / 64 + c->batch) * c->n_kv * tiles > 0x7fffffff)
     return report_error(AS2D_ERR_UNSUPPORTED, "too many heads, rows and positions");
   return AS2D_OK;
