@@ -386,6 +386,8 @@ extern "C" as2d_status as2d_kv_init_prefilled(as2d_model* mh, int32_t batch,
   s.k_cache = (bf16*)k_cache;
   s.v_cache = (bf16*)v_cache;
   s.len_upper.assign(kv_len, kv_len + batch);
+  s.floor_upper.assign(batch, 0);
+  s.floor_captured.assign(batch, 0);
   {
     const as2d_status rc = alloc_work(s, m, batch, capacity, kMaxK + 1);
     if (rc != AS2D_OK) {
@@ -973,8 +975,13 @@ extern "C" as2d_status as2d_kv_evict(as2d_kv* kh, const int32_t* keep, int32_t r
   // (a captured call may be followed by others before it runs, or never run)
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
   const bool eager = cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone;
-  for (int b = 0; b < s.batch && eager; ++b)
-    if (s.len_upper[b] > keep[b]) s.len_upper[b] = keep[b];
+  for (int b = 0; b < s.batch; ++b) {
+    const int64_t left = s.len_upper[b] > keep[b] ? keep[b] : s.len_upper[b];
+    if (eager)
+      s.len_upper[b] = s.floor_upper[b] = left;  // (the floor is keep[b], or what it was: no more than the length)
+    else if (keep[b] > s.floor_captured[b])
+      s.floor_captured[b] = keep[b];
+  }
   return AS2D_OK;
 }
 
@@ -991,7 +998,11 @@ extern "C" as2d_status as2d_kv_rollback(as2d_kv* kh, const int32_t* new_len,
       return fail(AS2D_ERR_INVALID_ARG, "new_root outside [0, vocab)");
   }
   CUDA_TRY(launch_rollback(s, new_len, new_root, (cudaStream_t)stream));
-  for (int b = 0; b < s.batch; ++b) s.len_upper[b] = new_len[b];
+  // (one that may be refused for the floor leaves the bound where it was: the entries may all
+  // still be there)
+  for (int b = 0; b < s.batch; ++b)
+    if ((new_len[b] >= s.floor_upper[b] && new_len[b] >= s.floor_captured[b]) || new_len[b] > s.len_upper[b])
+      s.len_upper[b] = new_len[b];
   return AS2D_OK;
 }
 

@@ -190,6 +190,10 @@ struct KvState {
   bf16* k_cache = nullptr;  // [layers][batch][n_kv][cap][d]
   bf16* v_cache = nullptr;
   std::vector<int64_t> len_upper;  // host bound of each request's length
+  // Host bounds of d_floor, from the evictions enqueued and from those captured
+  // (which may run at any later time): a rollback to no less is one that the device
+  // does not refuse for the floor.
+  std::vector<int64_t> floor_upper, floor_captured;
   // device state
   int32_t* d_len = nullptr;   // [batch]
   int32_t* d_root = nullptr;  // [batch]

@@ -578,3 +578,45 @@ def test_a_state_without_the_operators_is_as_before(pair):
     assert all(np.array_equal(x, y) for x, y in zip(one, two))
     a.close()
     b.close()
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_a_rollback_refused_below_an_eviction_changes_nothing(pair, captured):
+    """The calls right after it see every entry that is there (several chunks of the
+    chain's attention), whether the eviction was enqueued or captured and replayed."""
+    import paper_2609_37617_gb300 as lib
+    cfg, length, cap, keep = pair.cfg, 4000, 4200, 2600
+    results = []
+    for refused in (False, True):
+        st = pair.state([length, 30], cap, [5, 6])
+        w = torch.linspace(0, 1, cap, device="cuda").expand(st.kc.shape[:4]).contiguous()
+        st.track_weights(w)
+        if captured:
+            s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(g, stream=s):
+                st.evict([keep, 100], recent=4, stream=s.cuda_stream)
+            g.replay()
+            torch.cuda.synchronize()
+        else:
+            st.evict([keep, 100], recent=4)
+        st.track_weights(None)
+        if refused:
+            st.rollback([100, 30], [7, 6])
+        calls = [run_gpu_block(st, cfg, [[1, 2], [3]]), run_gpu_block(st, cfg, [[], [4]])]
+        if refused:
+            with pytest.raises(lib.AS2DError, match="eviction"):
+                st.check()
+        st.check()
+        ln, rt = st.read_state()
+        # what is left can be rolled back to, and gone on from
+        st.rollback([keep, 30], [8, 9])
+        calls.append(run_gpu_block(st, cfg, [[1], []]))
+        st.check()
+        assert st.read_state()[0] == [keep + 1 + int(calls[-1][0][0]), 31]
+        results.append((ln, rt, calls))
+        st.close()
+    (ln, rt, calls), (ln2, rt2, calls2) = results
+    assert ln == ln2 and rt == rt2 and ln[0] > keep
+    for a, b in zip(calls, calls2):
+        assert all(np.array_equal(x, y) for x, y in zip(a, b))
