@@ -91,11 +91,13 @@ __device__ __forceinline__ float part_weight(float m, float M) {
   return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
 }
 
-// Adds a part's sum and four of its dims to those of maximum M.
+// Adds a part's sum and four of its dims to those of maximum M.  NaN scores pass every
+// maximum by and are in the sum alone, so the sum counts whatever the part's weight (without
+// NaN it is 0 where the maximum is -inf): the row is NaN wherever the work is cut.
 __device__ __forceinline__ void add_part(float2 ml, float4 v, float M, float& l, float (&x)[4]) {
   const float w = part_weight(ml.x, M);
+  l = fmaf(ml.y, w, l);
   if (w != 0.f) {
-    l = fmaf(ml.y, w, l);
     x[0] = fmaf(v.x, w, x[0]);
     x[1] = fmaf(v.y, w, x[1]);
     x[2] = fmaf(v.z, w, x[2]);

@@ -735,3 +735,39 @@ def test_first_use_under_capture(lib):
     """A process whose first call of each operator is captured."""
     subprocess.run([sys.executable, "-c", FIRST_USE], check=True, timeout=120,
                    cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+
+# ---- rows and entries that are not finite --------------------------------------------
+
+# (requests' lengths, rows): an item in one CTA, in a cluster, in even shares; the last also two
+# requests, so that CTAs end one item and begin another
+CUTS = [([200], [3]), ([1564], [3]), ([15128], [3]), ([9000, 8000], [3, 64])]
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cut", range(len(CUTS)))
+def test_nan_reaches_the_row_however_the_work_is_cut(lib, cut, q_type):
+    """A query that holds NaN, keys of NaN over some tiles, a part or all of the prefix:
+    the rows that they enter get NaN in out and lse, all others the same bits as before."""
+    lens, rows = CUTS[cut]
+    masks = ref.tree_masks(rows, np.random.default_rng(cut))
+    x = Inputs((28, 4, 128), lens, rows, masks, q_type, seed=cut)
+    base, base_lse = run_attention(lib, x)
+
+    def check(out, lse, rows_of, heads):
+        hit = torch.zeros(lse.shape, dtype=torch.bool, device="cuda")
+        for r in rows_of:
+            hit[r, heads] = True
+        assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
+        assert torch.equal(out[~hit], base[~hit]) and torch.equal(lse[~hit], base_lse[~hit])
+
+    kept = x.q[1, 9, 100].clone()
+    x.q[1, 9, 100] = math.nan
+    check(*run_attention(lib, x), [1], [9])
+    x.q[1, 9, 100] = kept
+    n = lens[0]
+    for a, b in ((0, 1), (0, 128), (n // 2, n), (0, 7 * n // 8), (n // 3, n // 3 + 700), (0, n)):
+        kept = x.k[0, 0, 2, a:min(b, n)].clone()
+        x.k[0, 0, 2, a:min(b, n)] = math.nan
+        check(*run_attention(lib, x), range(rows[0]), list(range(14, 21)))
+        x.k[0, 0, 2, a:min(b, n)] = kept
