@@ -577,7 +577,9 @@ as2d_status as2d_tree_attention_workspace(const as2d_cache* cache, int64_t* byte
    rows][n_q][head_dim] of q_type, 16-byte aligned; lse: device float [sum
    rows][n_q].  Scores, maxima and sums are held in 32 bits.  A row that sees
    nothing gets out = 0 and lse = -inf.  What a row does not see does not reach
-   its result, whatever it holds (NaN and infinities among it).
+   its result, whatever it holds (NaN and infinities among it).  What it sees
+   does as the formula has it: an infinite value makes its dim that infinity
+   (values of both: NaN), and NaN or a score of +inf makes the row NaN in out and lse.
    A request whose kv_len[b] is negative or leaves no room for its rows in the
    capacity is skipped: its rows of out and lse stay as they were and
    AS2D_DEVERR_CAPACITY is ORed into error_bits (device int32 [1], set to 0 by

@@ -43,6 +43,7 @@
 // entries 29.6 us, the tensor pipe 3/4 busy in the loop), by the latency of one
 // chain of launch, load, products for few entries (9 rows over 1564: 9.5 us).
 #include <algorithm>
+#include <cfloat>
 
 #include "ops.h"
 #include "ptx_sm100.cuh"
@@ -91,23 +92,30 @@ __device__ __forceinline__ float part_weight(float m, float M) {
   return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
 }
 
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= FLT_MAX; }
+
+// An accumulator of weight w; infinities and NaN as they are, as no weight of the
+// formula is 0.
+__device__ __forceinline__ float weighted(float x, float w) { return is_finite(x) ? x * w : x; }
+
 // Adds a part's sum and four of its dims to those of maximum M.  NaN scores pass every
 // maximum by and are in the sum alone, so the sum counts whatever the part's weight (without
 // NaN it is 0 where the maximum is -inf): the row is NaN wherever the work is cut.
 __device__ __forceinline__ void add_part(float2 ml, float4 v, float M, float& l, float (&x)[4]) {
   const float w = part_weight(ml.x, M);
   l = fmaf(ml.y, w, l);
-  if (w != 0.f) {
-    x[0] = fmaf(v.x, w, x[0]);
-    x[1] = fmaf(v.y, w, x[1]);
-    x[2] = fmaf(v.z, w, x[2]);
-    x[3] = fmaf(v.w, w, x[3]);
-  }
+  x[0] += weighted(v.x, w);
+  x[1] += weighted(v.y, w);
+  x[2] += weighted(v.z, w);
+  x[3] += weighted(v.w, w);
 }
 
 __device__ __forceinline__ void dsmem_st4(uint32_t addr, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
                : "memory");
+}
+__device__ __forceinline__ void dsmem_st(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 __device__ __forceinline__ void dsmem_st2(uint32_t addr, float2 v) {
   asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
@@ -166,6 +174,21 @@ __device__ __forceinline__ void clean_tile(uint8_t* v, int p0, int L, int kend, 
 #pragma unroll 1
   for (int c = max(end, z) * C + tid; c < 128 * C; c += 64)
     *reinterpret_cast<uint4*>(v + chunk_off(c / C, c % C)) = make_uint4(0, 0, 0, 0);
+}
+
+// Sum of the infinities and NaN among one dim of prefix entries [t0, t1) (their values from v on, D
+// apart), by a whole warp; 0 if there are none.
+template <int D>
+__device__ __forceinline__ float not_finite_values(const bf16* v, int t0, int t1, int lane) {
+  float sum = 0.f;
+#pragma unroll 4
+  for (int t = t0 + lane; t < t1; t += 32) {
+    const float y = __bfloat162float(v[(size_t)t * D]);
+    if (!is_finite(y)) sum += y;
+  }
+#pragma unroll 1
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+  return sum;
 }
 
 // N consecutive results x inv at element `at` of the output: 32-bit (F32), bf16, or
@@ -462,11 +485,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t ns = 0, items = 0, c_turn = 0, before = 0;  // tiles of this CTA before the item
     for (bool more = some; more;) {
       const int cnt = it.t1 - it.t0, nqs = it.rows * G;
-      const int q = it.qt * 128 + row, i = divide_group(a, q);
-      const bool live = q < nqs;
+      const bool live = it.qt * 128 + row < nqs;
+      // the row and query head of the thread's query (computed where they are needed: they would take
+      // registers over the tiles)
+      auto place = [&](int& i, int& h) {
+        int q = it.qt * 128 + row;
+        asm volatile("" : "+r"(q));
+        i = divide_group(a, q);
+        h = it.g * G + (q - i * G);
+      };
       const bool warp_live = it.qt * 128 + 32 * quad < nqs;  // a query of the warp is
-      const int h = it.g * G + (q - i * G);
-      const uint64_t vis = live && it.t1 > it.L / 128 ? visible_rows(a, it.r0 + i, i, it.rows) : 0ull;
+      uint64_t vis = 0;
+      if (live && it.t1 > it.L / 128) {
+        int i, h;
+        place(i, h);
+        vis = visible_rows(a, it.r0 + i, i, it.rows);
+      }
       float m = -INFINITY, l = 0.f;
       for (int j = set; j < cnt; j += 2, ++ns) {
         wait(&s_full[set], ns & 1);
@@ -588,12 +622,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float w0 = part_weight(m0, M), w1 = cnt > 1 ? part_weight(m1, M) : 0.f;
       const float lt = l0 * w0 + (cnt > 1 ? l1 * w1 : 0.f);
       const unsigned long long bad = tails ? *s_bad & vis : 0ull;
+      int i, h;
+      place(i, h);
       // every CTA of the cluster has read its ring: the parts go there
       if (DIRECT && mode == kCluster) ptx::cluster_sync();
       if (ok && warp_live) {
         const bool done = DIRECT || (it.t0 == 0 && it.t1 == it.tiles);
         const size_t part = (size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1);
         const float inv = lt == 0.f ? 0.f : 1.f / lt;
+        float zero[2] = {0.f, 0.f};  // 0 times each accumulator
 #pragma unroll 1
         for (int d0 = group * (D / 4); d0 < (group + 1) * (D / 4); d0 += 16) {
           uint32_t o0[16], o1[16];
@@ -603,6 +640,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           float o[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
+            zero[e & 1] = fmaf(__uint_as_float(o0[e]), 0.f, zero[e & 1]);
+            if (cnt > 1) zero[e & 1] = fmaf(__uint_as_float(o1[e]), 0.f, zero[e & 1]);
             o[e] = w0 != 0.f ? __uint_as_float(o0[e]) * w0 : 0.f;
             if (cnt > 1 && w1 != 0.f) o[e] = fmaf(__uint_as_float(o1[e]), w1, o[e]);
           }
@@ -630,6 +669,37 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int e = 0; e < 4; ++e) dst[e * 128] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           } else if (live) {
             write_out<16, F32>(a, o, inv, ((size_t)(it.r0 + i) * a.nq + h) * D + d0);
+          }
+          __syncwarp();
+        }
+        // An infinite value of the prefix times hi and lo parts of P, of which lo may be 0 or
+        // negative, or times a P that is 0 in 32 bits, is NaN where the formula has that
+        // infinity; and a set of weight 0 beside the other is left out.  Such dims once more.
+        if (__any_sync(~0u, live && zero[0] + zero[1] != 0.f && lt == lt)) {
+          const bf16* v = a.v + ((size_t)it.b * a.nkv + it.g) * a.cap * D;
+#pragma unroll 1
+          for (int d = group * (D / 4); d < (group + 1) * (D / 4); ++d) {
+            float y = not_finite_values<D>(v + d, it.t0 * 128, min(it.t1 * 128, it.L), lane);
+            if (is_finite(y) || !live || lt != lt) continue;
+#pragma unroll 1
+            for (unsigned long long left = bad; left; left &= left - 1) {
+              const int t = it.L + __ffsll((long long)left) - 1;
+              const float z = __bfloat162float(v[(size_t)t * D + d]);
+              if (t >= it.t0 * 128 && t < it.t1 * 128 && !is_finite(z)) y += z;
+            }
+            if (DIRECT && mode == kCluster) {
+              const float* to = &recv[(ptx::cluster_rank() * kQuads + d / 4 % kQuads) * 128 + row].x + d % 4;
+              dsmem_st(ptx::dsmem_map(ptx::smem_u32(to), d / 4 / kQuads), y);
+            } else if (!DIRECT && !done) {
+              (&ws.o[(part * (D / 4) + d / 4) * 128 + row].x)[d % 4] = y;
+            } else {
+              const size_t at = ((size_t)(it.r0 + i) * a.nq + h) * D + d;
+              if (F32 && !a.out_lo)
+                ((float*)a.out)[at] = y;
+              else
+                ((bf16*)a.out)[at] = __float2bfloat16_rn(y);
+              if (F32 && a.out_lo) a.out_lo[at] = __float2bfloat16_rn(0.f);
+            }
           }
           __syncwarp();
         }
@@ -719,6 +789,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps, U == 12 ? 2 : U == 8 ? 3 :
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       ml[k] = make_float2(-INFINITY, 0.f);
+      v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (k0 + k < n) {
         ml[k] = __ldcg(&ws.ml[part(k0 + k) * 128 + row]);
         v[k] = __ldcg(&ws.o[(part(k0 + k) * (D / 4) + quad) * 128 + row]);
@@ -730,7 +801,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps, U == 12 ? 2 : U == 8 ? 3 :
     const float w = part_weight(before, M);
     l *= w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = w != 0.f ? x[e] * w : 0.f;
+    for (int e = 0; e < 4; ++e) x[e] = weighted(x[e], w);
 #pragma unroll
     for (int k = 0; k < U; ++k) add_part(ml[k], v[k], M, l, x);
   }

@@ -771,3 +771,39 @@ def test_nan_reaches_the_row_however_the_work_is_cut(lib, cut, q_type):
         x.k[0, 0, 2, a:min(b, n)] = math.nan
         check(*run_attention(lib, x), range(rows[0]), list(range(14, 21)))
         x.k[0, 0, 2, a:min(b, n)] = kept
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cut", range(len(CUTS)))
+def test_infinite_values_of_the_prefix(lib, cut, q_type):
+    """out = sum p_t v_t with an infinite v_t of the prefix is that infinity (two of both signs:
+    NaN) in its dim and its kv head's rows, the same bits as before elsewhere; however
+    small p_t is beside the others."""
+    lens, rows = CUTS[cut]
+    masks = ref.tree_masks(rows, np.random.default_rng(cut))
+    x = Inputs((28, 4, 128), lens, rows, masks, q_type, seed=cut)
+    n = lens[0]
+    # scores far apart: weights that are 0 in 32 bits beside others
+    x.k[0, 0, 1, 5] *= 40
+    x.k[0, 0, 1, n - 1] *= 40
+    x.k[0, 0, 1, n // 2] *= 40
+    base, base_lse = run_attention(lib, x)
+    assert torch.isfinite(base).all()
+    mine, heads = list(range(rows[0])), list(range(7, 14))
+    for at, value in ((0, math.inf), (5, -math.inf), (n // 2, math.inf), (n // 2 + 1, math.nan), (n - 1, -math.inf),
+                      (n - 2, math.inf), (n // 3, -math.inf)):
+        kept = x.v[0, 0, 1, at, 70].clone()
+        x.v[0, 0, 1, at, 70] = value
+        out, lse = run_attention(lib, x)
+        got = out[mine][:, heads, 70]
+        assert (torch.isnan(got) if math.isnan(value) else got == value).all(), (at, value)
+        out[mine[0]:mine[-1] + 1, heads[0]:heads[-1] + 1, 70] = base[mine[0]:mine[-1] + 1, heads[0]:heads[-1] + 1, 70]
+        assert torch.equal(out, base) and torch.equal(lse, base_lse), (at, value)
+        x.v[0, 0, 1, at, 70] = kept
+    x.v[0, 0, 1, 3, 70], x.v[0, 0, 1, n - 3, 70] = math.inf, -math.inf
+    x.v[0, 0, 1, 2, 33], x.v[0, 0, 1, 4, 33] = math.inf, math.inf
+    x.v[0, 0, 1, 2] = math.inf  # a whole entry, beside the last two
+    out, _ = run_attention(lib, x)
+    got = out[mine][:, heads]
+    assert torch.isnan(got[..., 70]).all()
+    assert (got[..., [e for e in range(128) if e != 70]] == math.inf).all()
