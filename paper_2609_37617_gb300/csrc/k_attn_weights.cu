@@ -102,6 +102,34 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[16], uint64_t c2
   }
 }
 
+// The weight of one key of 32-bit queries q0 .. q0 + n - 1 of a head, that came out as NaN: if the key
+// holds infinities (and no NaN) once more in 32-bit arithmetic, as in hi and lo parts a score
+// of -inf may be NaN.
+template <int D>
+__device__ __forceinline__ float weight_of(const TreeArgs& a, const Unit& it, int q0, int n, int key, const float* lse,
+                                           const uint2* seen, uint32_t need, bool upper) {
+  const bf16* k = a.k + (((size_t)it.b * a.nkv + it.g) * a.cap + key) * D;
+  const int G = a.nq / a.nkv;
+  bool inf = false, none = true;
+#pragma unroll 1
+  for (int d = 0; d < D; ++d) {
+    const float y = fabsf(__bfloat162float(k[d]));
+    inf = inf || y == INFINITY;
+    none = none && y == y;
+  }
+  if (!inf || !none) return NAN;
+  float sum = 0.f;
+#pragma unroll 1
+  for (int q = 0; q < n; ++q) {
+    const uint32_t w = upper ? seen[q].y : seen[q].x;
+    if ((w & need) != need) continue;
+    const int i = divide_group(a, q0 + q);
+    const float* x = (const float*)a.q + (it.r0 + i) * a.q_stride + (int64_t)(it.g * G + (q0 + q - i * G)) * D;
+    sum += ex2(fmaf(exact_product<D>(x, k), a.scale_log2, lse[q]));
+  }
+  return sum;
+}
+
 template <int D, bool F32>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_weights_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ WeightArgs wa, int turn) {
@@ -343,7 +371,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::tc_fence_before();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(&s_empty[buf]);
-          if (live && ok) w[key] = before + (sums.x + sums.y);
+          float more = sums.x + sums.y;
+          if (F32 && ok && live && more != more) more = weight_of<D>(a, s.it, qt * 128, n, key, lse, seen, need, upper);
+          if (live && ok) w[key] = before + more;
+          __syncwarp();
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&e_empty[pass & 1]);

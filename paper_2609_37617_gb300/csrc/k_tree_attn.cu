@@ -176,6 +176,56 @@ __device__ __forceinline__ void clean_tile(uint8_t* v, int p0, int L, int kend, 
     *reinterpret_cast<uint4*>(v + chunk_off(c / C, c % C)) = make_uint4(0, 0, 0, 0);
 }
 
+// 32-bit queries are hi and lo parts, so a score of -inf (infinite keys) may come out as NaN.
+// The weights P of 64 keys of a head, k the first, by a whole warp whose threads with `mine`
+// found NaN in their sum: those of keys that hold infinities (and no NaN), whose score in 32 bits
+// leaves them nothing beside the reference, are set to 0.  Returns the thread's sum.
+template <int D>
+__device__ __forceinline__ float mend_weights(uint32_t ts, bool mine, const float* q, const bf16* k, float c, float ref,
+                                              float sum) {
+  const int lane = threadIdx.x & 31;
+  float l = 0.f;
+  ptx::tmem_st_wait();
+#pragma unroll 1
+  for (int x = 0; x < 64; x += 16) {
+    uint32_t p[16], nan = 0;  // of each 16 keys the hi parts, two in a word, then the lo parts
+    ptx::tmem_ld16(ts + x, p);
+    ptx::tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float y = __uint_as_float(e & 1 ? p[e / 2] & 0xFFFF0000u : p[e / 2] << 16);
+      nan |= (y != y ? 1u : 0u) << e;
+    }
+    uint32_t gone = 0;  // of them
+    if (!mine) nan = 0;
+#pragma unroll 1
+    for (uint32_t left = __reduce_or_sync(~0u, nan); left; left &= left - 1) {
+      const int e = __ffs(left) - 1;
+      const bf16* key = k + (size_t)(x + e) * D;
+      bool inf = false, none = true;  // infinities, no NaN
+#pragma unroll
+      for (int d = 0; d < D; d += 32) {
+        const float y = fabsf(__bfloat162float(key[d + lane]));
+        inf = inf || y == INFINITY;
+        none = none && y == y;
+      }
+      if (!__any_sync(~0u, inf) || !__all_sync(~0u, none)) continue;
+      if (((nan >> e) & 1) && exact_product<D>(q, key) * c < ref - 160.f) gone |= 1u << e;
+      __syncwarp();
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const uint32_t other = e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+      if ((gone >> e) & 1) p[e / 2] &= other, p[8 + e / 2] &= other;
+      l += __uint_as_float(e & 1 ? p[e / 2] & 0xFFFF0000u : p[e / 2] << 16) +
+           __uint_as_float(e & 1 ? p[8 + e / 2] & 0xFFFF0000u : p[8 + e / 2] << 16);
+    }
+    __syncwarp();
+    ptx::tmem_st16(ts + x, p);
+  }
+  return mine ? l : sum;
+}
+
 // Sum of the infinities and NaN among one dim of prefix entries [t0, t1) (their values from v on, D
 // apart), by a whole warp; 0 if there are none.
 template <int D>
@@ -581,7 +631,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             ptx::tmem_st16(ts + x, p);
           }
           const float2 sums = of_two(add2(ls[0], ls[1]));
-          l += sums.x + sums.y;
+          float more = sums.x + sums.y;
+          if (F32 && ok && __any_sync(~0u, live && more != more)) {
+            int i, h;
+            place(i, h);
+            more = mend_weights<D>(ts, live && more != more,
+                                   (const float*)a.q + (it.r0 + i) * a.q_stride + (int64_t)h * D,
+                                   a.k + (((size_t)it.b * a.nkv + it.g) * a.cap + p0) * D, c, ref, more);
+          }
+          l += more;
           ptx::tmem_st_wait();
           ptx::tc_fence_before();
         }

@@ -60,6 +60,23 @@ __device__ __forceinline__ void hi_lo(float a, float b, uint32_t& h, uint32_t& l
   l = pack2(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xFFFF0000u));
 }
 
+// A 32-bit query's product with a key, in 32-bit arithmetic.
+template <int D>
+__device__ __forceinline__ float exact_product(const float* q, const bf16* k) {
+  float s = 0.f;
+#pragma unroll 1
+  for (int d = 0; d < D && s == s; d += 8) {  // (NaN stays)
+    const uint4 y = *reinterpret_cast<const uint4*>(k + d);
+    const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s = fmaf(q[d + 2 * e], __uint_as_float(w[e] << 16), s);
+      s = fmaf(q[d + 2 * e + 1], __uint_as_float(w[e] & 0xFFFF0000u), s);
+    }
+  }
+  return s;
+}
+
 // The visible rows of row r of a request, as a mask of its `rows` rows.
 __device__ __forceinline__ uint64_t visible_rows(const TreeArgs& a, int r, int i, int rows) {
   const uint64_t all = ~0ull >> (64 - rows);

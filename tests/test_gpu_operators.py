@@ -807,3 +807,45 @@ def test_infinite_values_of_the_prefix(lib, cut, q_type):
     got = out[mine][:, heads]
     assert torch.isnan(got[..., 70]).all()
     assert (got[..., [e for e in range(128) if e != 70]] == math.inf).all()
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("heads", [(28, 4, 128), (4, 2, 64)])
+@pytest.mark.parametrize("cut", range(len(CUTS)))
+def test_infinite_keys(lib, cut, heads, q_type):
+    """A score of -inf is a weight of 0, in the prefix and in the rows' own entries;
+    one of +inf makes its row NaN."""
+    lens, rows = CUTS[cut]
+    nq, nkv, d = heads
+    masks = ref.chain_masks(rows)
+    x = Inputs(heads, lens, rows, masks, q_type, seed=cut)
+    x.q[:, :, 5] = -x.q[:, :, 5].abs() - 2.0 ** -6
+    x.q[:, :, 6] = x.q[:, :, 6].abs() + 2.0 ** -6
+    n, r = lens[0], rows[0]
+    gone = sorted({0, 77, 127, n // 2, n - 1, n})  # (n: the first row's own entry)
+    for t in gone:
+        x.k[0, 0, 0, t, 5] = math.inf
+        x.k[0, 0, 0, t, 6] = -math.inf if t % 2 else x.k[0, 0, 0, t, 6]
+    out, lse = run_attention(lib, x)
+    # the formula without those entries, for kv head 0; the other heads as they are
+    q, k, v, seen = x.request(0)
+    less = seen.clone()
+    less[:, gone] = False
+    G, half_step = nq // nkv, torch.finfo(q_type).eps / 2
+    for g in range(nkv):
+        qg, kg, vg = q[:, g * G:(g + 1) * G], k[g:g + 1], v[g:g + 1]
+        want, tol, want_lse, tol_lse = ref.attention(qg, kg, vg, less if g == 0 else seen, x.scale)
+        got = out[:r, g * G:(g + 1) * G].double()
+        assert ((got - want).abs() <= want.abs() * half_step * (1 + 2.0 ** -6) + tol).all()
+        assert ((lse[:r, g * G:(g + 1) * G].double() - want_lse).abs() <= tol_lse).all()
+    w = torch.zeros(x.k.shape[:4], device="cuda")
+    lib.Cache(x.k, x.v).attention_weights(x.q, lse, w, x.kv_len, x.rows, x.visible)
+    want, tol = ref.weights(q[:, :G], k[:1], less, x.scale, lse[:r, :G].double())
+    got = w[0, 0, :1, :n + r].double()
+    assert ((got - want).abs() <= tol + want.abs() * 2.0 ** -23).all() and (got[0, gone] == 0).all()
+    # +inf: the rows that see it, NaN
+    x.k[0, 0, 0, 9, 6] = math.inf
+    x.k[0, 0, 0, 9, 5] = 0.0
+    out, lse = run_attention(lib, x)
+    assert torch.isnan(out[:r, :G]).all() and torch.isnan(lse[:r, :G]).all()
+    assert torch.isfinite(out[:r, G:]).all() and torch.isfinite(out[r:]).all()
