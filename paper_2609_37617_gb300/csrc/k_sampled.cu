@@ -44,9 +44,11 @@ __device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
   return make_float2(M, (a.x == -INFINITY ? a.y : a.y * wa) + (b.x == -INFINITY ? b.y : b.y * wb));
 }
 
-// (maximum, sum) of the row from each thread's, over the block and the cluster.
+// (maximum, sum) of the row from each thread's, over the block and the cluster.  start: the
+// first row of a cluster whose CTAs have arrived at its barrier; their shared memory is written once
+// all of them have started.
 __device__ __forceinline__ float2 join_row(float2 all, float c, uint32_t rank, uint32_t ranks, float2* s_warp,
-                                           float2* s_part) {
+                                           float2* s_part, bool start) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
@@ -58,6 +60,7 @@ __device__ __forceinline__ float2 join_row(float2 all, float c, uint32_t rank, u
   for (int o = kProbsWarps / 2; o > 0; o >>= 1)
     all = join(all, make_float2(__shfl_xor_sync(~0u, all.x, o), __shfl_xor_sync(~0u, all.y, o)), c);
   if (ranks > 1) {
+    if (start) ptx::cluster_wait();
     if (tid < (int)ranks) {
       const uint32_t to = ptx::dsmem_map(ptx::smem_u32(&s_part[rank]), tid);
       asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(all.x), "f"(all.y) : "memory");
@@ -80,6 +83,7 @@ __global__ void __launch_bounds__(kProbs, kProbsCtas) probs_kernel(const float* 
   const int v0 = min((int)rank * slice, vocab), n = (min(v0 + slice, vocab) - v0) / W;  // pieces
   const float* x = logits + (size_t)blockIdx.y * vocab + v0;
   float* p = probs + (size_t)blockIdx.y * vocab + v0;
+  if (ranks > 1) ptx::cluster_arrive_relaxed();
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   float v[R][W];
@@ -130,7 +134,7 @@ __global__ void __launch_bounds__(kProbs, kProbsCtas) probs_kernel(const float* 
 #pragma unroll
     for (int e = 0; e < W; ++e) l += ex2((t[e] - ref) * c);
   }
-  const float2 all = join_row(make_float2(m, l), c, rank, ranks, s_warp, s_part);
+  const float2 all = join_row(make_float2(m, l), c, rank, ranks, s_warp, s_part, true);
   // (a thread that holds nothing has zeros, a row that holds nothing gets them)
   const float f = all.y == 0.f ? 0.f : (m == -INFINITY ? 1.f : ex2((m - all.x) * c)) / all.y;
 #pragma unroll
@@ -161,6 +165,7 @@ __global__ void __launch_bounds__(kProbs, kProbsCtas) probs_rows_kernel(const fl
   const int tid = threadIdx.x;
   const uint32_t rank = ptx::cluster_rank(), ranks = gridDim.x;
   const int v0 = min((int)rank * slice, vocab), n = (min(v0 + slice, vocab) - v0) / 4;  // pieces
+  if (ranks > 1) ptx::cluster_arrive_relaxed();
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   auto fetch = [&](int row) {
@@ -189,7 +194,8 @@ __global__ void __launch_bounds__(kProbs, kProbsCtas) probs_rows_kernel(const fl
                          ex2((v[r].w - ref) * c));
       l += (v[r].x + v[r].y) + (v[r].z + v[r].w);
     }
-    const float2 all = join_row(make_float2(m, l), c, rank, ranks, s_warp[turn], s_part[turn]);
+    const float2 all =
+        join_row(make_float2(m, l), c, rank, ranks, s_warp[turn], s_part[turn], row == (int)blockIdx.y);
     const float f = all.y == 0.f ? 0.f : (m == -INFINITY ? 1.f : ex2((m - all.x) * c)) / all.y;
     float4* p = reinterpret_cast<float4*>(probs + (size_t)row * vocab + v0);
 #pragma unroll
@@ -262,6 +268,7 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
   const int r0 = a.start[b], k = a.start[b + 1] - r0 - 1, c0 = r0 - b;
   const size_t V = a.vocab;
   const int piece = chunk * kThreads;
+  ptx::cluster_arrive_relaxed();
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   if (warp == 0) {
@@ -339,7 +346,7 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
     if (warp > 0) upto = add(from_lane(w, warp - 1), upto);
     return v0;
   };
-  for (int plain = n < k ? 0 : 1; plain < 2; ++plain) {
+  for (int plain = n < k ? 0 : 1, first = 1; plain < 2; ++plain, first = 0) {
     float2 sum = make_float2(0.f, 0.f);
     int v0 = 0;
     for (int i = 0; i < pieces; ++i) {
@@ -347,6 +354,7 @@ __global__ void __launch_bounds__(kThreads) accept_sampled_kernel(const __grid_c
       if (tid == 0) s_piece[i] = all;
       sum = add(sum, all);
     }
+    if (first) ptx::cluster_wait();  // every CTA has started: its shared memory can be written
     if (tid < ranks) {
       const uint32_t to = ptx::dsmem_map(ptx::smem_u32(&s_part[plain][rank]), tid);
       asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(sum.x), "f"(sum.y) : "memory");

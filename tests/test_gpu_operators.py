@@ -849,3 +849,35 @@ def test_infinite_keys(lib, cut, heads, q_type):
     out, lse = run_attention(lib, x)
     assert torch.isnan(out[:r, :G]).all() and torch.isnan(lse[:r, :G]).all()
     assert torch.isfinite(out[:r, G:]).all() and torch.isfinite(out[r:]).all()
+
+
+def test_clusters_beside_other_work(lib):
+    """Rows and requests whose clusters hold CTAs with nothing to do, call after call while another
+    stream fills the SMs: the same results each time."""
+    rng = np.random.default_rng(11)
+    ks, V = [1, 0, 3, 2], 40
+    probs = dyadic_rows(rng, sum(ks) + len(ks), V, 20)
+    draft = dyadic_rows(rng, sum(ks), V, 20)
+    cand = [int(t) for t in rng.integers(0, V, sum(ks))]
+    u = (rng.integers(0, 2 ** 20, len(probs)) / 2.0 ** 20).astype(np.float32)
+    want = ref.accept(probs.astype(np.float64), draft.astype(np.float64), cand, ks, u.astype(np.float64))
+    dev = lambda a, t: torch.tensor(np.asarray(a), dtype=t, device="cuda")  # noqa: E731
+    p, q, c, r = dev(probs, torch.float32), dev(draft, torch.float32), dev(cand, torch.int32), dev(u, torch.float32)
+    n, tok = (torch.empty((300, 4), dtype=torch.int32, device="cuda") for _ in range(2))
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn((90, 90004), generator=g, device="cuda") * 4  # (clusters that go from row to row)
+    y = torch.randn((3, 20490), generator=g, device="cuda") * 4
+    first = [lib.token_probs(t, 0.9) for t in (x, y)]
+    other = torch.cuda.Stream()
+    big = torch.randn((2048, 2048), device="cuda")
+    torch.cuda.synchronize()
+    for i in range(300):
+        if i % 3 == 0:
+            with torch.cuda.stream(other):
+                big @ big
+        lib.accept_sampled(p, c, ks, r, n[i], tok[i], draft_probs=q)
+        if i % 5 == 0:
+            for t, f in zip((x, y), first):
+                assert torch.equal(lib.token_probs(t, 0.9), f)
+    torch.cuda.synchronize()
+    assert all(a == want[0] for a in n.tolist()) and all(t == want[1] for t in tok.tolist())
