@@ -740,7 +740,6 @@ class Cache:
         _check(_lib.as2d_cache_evict_workspace(self._ref, ctypes.byref(need)),
                "as2d_cache_evict_workspace")
         self._workspace = torch.empty(max(most, need.value), dtype=torch.uint8, device=k.device)
-        self._workspace_at = self._workspace.data_ptr(), self._workspace.numel()
 
     def _device(self):
         device = self._current()
@@ -788,7 +787,7 @@ class Cache:
         st = _lib.as2d_tree_attention(
             self._ref, layer, ctypes.byref(r), _address(out, "out", device, q.dtype, shape),
             None if lse is None else _address(lse, "lse", device, self._f32, shape[:2]),
-            *self._workspace_at,
+            self._workspace.data_ptr(), self._workspace.numel(),
             None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)),
             stream)
         if st:
@@ -814,7 +813,7 @@ class Cache:
         st = _lib.as2d_cache_evict(
             self._ref, _address(weights, "weights", device, self._f32, self.shape[:4]),
             _address(kv_len, "kv_len", device, self._i32, self._per_request),
-            self._counts(keep, "keep"), recent, *self._workspace_at, stream)
+            self._counts(keep, "keep"), recent, self._workspace.data_ptr(), self._workspace.numel(), stream)
         if st:
             _check(st, "as2d_cache_evict")
 

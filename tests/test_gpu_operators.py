@@ -881,3 +881,35 @@ def test_clusters_beside_other_work(lib):
                 assert torch.equal(lib.token_probs(t, 0.9), f)
     torch.cuda.synchronize()
     assert all(a == want[0] for a in n.tolist()) and all(t == want[1] for t in tok.tolist())
+
+
+def test_one_workspace_for_several_caches(lib, monkeypatch):
+    """Calls in even shares, which leave parts in the workspace, an eviction and small calls one
+    after another without a wait, all on one workspace: bit for bit what each gives alone."""
+    sizes = [(15128, 17), (9000, 64), (200, 3), (12000, 1), (8100, 9)]
+    xs = [Inputs((28, 4, 128), [n], [r], ref.tree_masks([r], np.random.default_rng(n)), seed=n) for n, r in sizes]
+    alone = [run_attention(lib, x) for x in xs]
+    caches = [lib.Cache(x.k, x.v) for x in xs]
+    shared = max((c._workspace for c in caches), key=lambda t: t.numel())
+    for c in caches:
+        c._workspace = shared
+    # (a cache of the same shape as the first, to be cut)
+    cut = [torch.randn_like(x, dtype=torch.float32).bfloat16() for x in (xs[2].k, xs[2].v)]
+    evict = lib.Cache(*cut)
+    assert evict._workspace.numel() <= shared.numel()
+    evict._workspace = shared
+    given = []
+    for name, at in (("as2d_tree_attention", 5), ("as2d_cache_evict", 5)):
+        f = getattr(lib._lib, name)
+        monkeypatch.setattr(lib._lib, name, lambda *a, f=f, at=at: (given.append(a[at]), f(*a))[1])
+    outs, w = [], torch.rand(cut[0].shape[:4], device="cuda")
+    for _ in range(4):
+        for i, (x, c) in enumerate(zip(xs, caches)):
+            lse = torch.empty((sum(x.rows), 28), device="cuda")
+            outs.append((i, c.tree_attention(x.q, x.kv_len, x.rows, x.visible, lse=lse), lse))
+            if i % 2:
+                evict.evict(w, torch.tensor([200], dtype=torch.int32, device="cuda"), [150], recent=5)
+    torch.cuda.synchronize()
+    assert len(given) == 28 and set(given) == {shared.data_ptr()}
+    for i, out, lse in outs:
+        assert torch.equal(out, alone[i][0]) and torch.equal(lse, alone[i][1])
