@@ -687,6 +687,24 @@ class State:
 
 
 # ---- operators on tensors ------------------------------------------------------
+#
+# A call is enqueued on `stream` (a cudaStream_t, 0 for the legacy default stream), on torch's
+# current stream unless one is given.  A result that the call makes itself belongs to that
+# stream, as a tensor that torch makes there would.
+
+def _stream_reader(torch):
+    """A function that gives torch's current stream of a device as a cudaStream_t."""
+    return (getattr(torch._C, "_cuda_getCurrentRawStream", None) or
+            (lambda device: torch.cuda.current_stream(device).cuda_stream))
+
+
+def _new_on(stream, device, like, shape):
+    """An uninitialised tensor of like's type that belongs to `stream`."""
+    import torch
+    of = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(of):
+        return like.new_empty(shape)
+
 
 def _tensor(t, name, device, dtypes, shape=None, contiguous=True):
     """Checks a CUDA tensor argument and returns its device address."""
@@ -717,7 +735,9 @@ class Cache:
     [capacity][head_dim], kept alive here) with the workspace of the operators
     on it; see include/as2d.h, "Operators on caches and logits".  Calls on one
     Cache share the workspace, so calls that may overlap on the GPU (several
-    streams, captured graphs) need a Cache each."""
+    streams, captured graphs) need a Cache each.  A Cache outlives the captured
+    graphs that hold its calls, and calls enqueued on a stream that was given by
+    its handle; those on torch's current stream may still run when it goes."""
 
     def __init__(self, k, v):
         import torch
@@ -740,12 +760,19 @@ class Cache:
         _check(_lib.as2d_cache_evict_workspace(self._ref, ctypes.byref(need)),
                "as2d_cache_evict_workspace")
         self._workspace = torch.empty(max(most, need.value), dtype=torch.uint8, device=k.device)
+        self._current_stream = _stream_reader(torch)
+        self._made_on = self._current_stream(device)
 
     def _device(self):
         device = self._current()
         if device != self._on:
             raise ValueError("the cache must be on the current CUDA device")
         return device
+
+    def _used_here(self):
+        """Tells torch's allocator of a use of the workspace on torch's current stream."""
+        import torch
+        self._workspace.record_stream(torch.cuda.current_stream(self._on))
 
     def _counts(self, values, name):
         if len(values) != self.shape[1]:
@@ -777,13 +804,18 @@ class Cache:
         return r
 
     def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
-                       lse=None, error_bits=None, stream=0):
+                       lse=None, error_bits=None, stream=None):
         """as2d_tree_attention; returns out (made like q unless given)."""
         device = self._device()
+        current = self._current_stream(device)
+        if stream is None:
+            stream = current
+            if stream != self._made_on:
+                self._used_here()
         r = self._rows(device, q, kv_len, rows, visible, scale, max_len)
         shape = q.shape
         if out is None:
-            out = q.new_empty(shape)
+            out = q.new_empty(shape) if stream == current else _new_on(stream, device, q, shape)
         st = _lib.as2d_tree_attention(
             self._ref, layer, ctypes.byref(r), _address(out, "out", device, q.dtype, shape),
             None if lse is None else _address(lse, "lse", device, self._f32, shape[:2]),
@@ -795,9 +827,14 @@ class Cache:
         return out
 
     def attention_weights(self, q, lse, weights, kv_len, rows, visible=None, layer=0, scale=None,
-                          max_len=0, error_bits=None, stream=0):
+                          max_len=0, error_bits=None, stream=None):
         """as2d_attention_weights: adds to weights in place."""
         device = self._device()
+        current = self._current_stream(device)
+        if stream is None:
+            stream = current
+            if stream != self._made_on:
+                self._used_here()
         r = self._rows(device, q, kv_len, rows, visible, scale, max_len)
         st = _lib.as2d_attention_weights(
             self._ref, layer, ctypes.byref(r), _address(lse, "lse", device, self._f32, q.shape[:2]),
@@ -807,9 +844,14 @@ class Cache:
         if st:
             _check(st, "as2d_attention_weights")
 
-    def evict(self, weights, kv_len, keep, recent=0, stream=0):
+    def evict(self, weights, kv_len, keep, recent=0, stream=None):
         """as2d_cache_evict: cuts the cache, weights and kv_len in place."""
         device = self._device()
+        current = self._current_stream(device)
+        if stream is None:
+            stream = current
+            if stream != self._made_on:
+                self._used_here()
         st = _lib.as2d_cache_evict(
             self._ref, _address(weights, "weights", device, self._f32, self.shape[:4]),
             _address(kv_len, "kv_len", device, self._i32, self._per_request),
@@ -818,7 +860,7 @@ class Cache:
             _check(st, "as2d_cache_evict")
 
 
-def token_probs(logits, temperature, out=None, stream=0):
+def token_probs(logits, temperature, out=None, stream=None):
     """as2d_token_probs of logits [rows, vocab]; returns out (made like logits
     unless given; may be logits)."""
     import torch
@@ -826,8 +868,11 @@ def token_probs(logits, temperature, out=None, stream=0):
     at = _address(logits, "logits", device, torch.float32, shape)
     if len(shape) != 2:
         raise ValueError("logits must be [rows, vocab]")
+    current = _stream_reader(torch)(device)
+    if stream is None:
+        stream = current
     if out is None:
-        out = torch.empty_like(logits)
+        out = torch.empty_like(logits) if stream == current else _new_on(stream, device, logits, shape)
     st = _lib.as2d_token_probs(at, shape[0], shape[1], temperature,
                                _address(out, "out", device, torch.float32, shape), stream)
     if st:
@@ -835,7 +880,7 @@ def token_probs(logits, temperature, out=None, stream=0):
     return out
 
 
-def accept_sampled(probs, candidates, k, u, n_accepted, token, draft_probs=None, stream=0):
+def accept_sampled(probs, candidates, k, u, n_accepted, token, draft_probs=None, stream=None):
     """as2d_accept_sampled: probs [sum (k + 1), vocab], candidates [sum k] (or
     None), k a list, u [sum (k + 1)], n_accepted and token [batch]."""
     import torch
@@ -844,6 +889,8 @@ def accept_sampled(probs, candidates, k, u, n_accepted, token, draft_probs=None,
     at = _address(probs, "probs", device, f32, shape)
     if len(shape) != 2 or shape[0] != total + batch:
         raise ValueError("probs must be [sum (k + 1), vocab]")
+    if stream is None:
+        stream = _stream_reader(torch)(device)
     st = _lib.as2d_accept_sampled(
         at, None if draft_probs is None or total == 0 else
         _address(draft_probs, "draft_probs", device, f32, (total, shape[1])),

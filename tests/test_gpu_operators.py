@@ -913,3 +913,65 @@ def test_one_workspace_for_several_caches(lib, monkeypatch):
     assert len(given) == 28 and set(given) == {shared.data_ptr()}
     for i, out, lse in outs:
         assert torch.equal(out, alone[i][0]) and torch.equal(lse, alone[i][1])
+
+
+def test_torchs_current_stream(lib):
+    """Without a stream given, a call follows what torch's current stream does before it and
+    precedes what it does next, and its result belongs there."""
+    args = together_inputs(5)
+    step, outs = run_together(lib, *args)
+    first = [t.clone() for t in outs]
+    step(0)
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    x, w, logits, cand, ks, u, keep = args
+    q, lg = x.q.clone(), logits.clone()
+    for t, f in zip(outs, first):
+        t.copy_(f)
+    x.q.zero_()
+    logits.zero_()
+    big = torch.randn((8192, 8192), device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        for _ in range(3):
+            big @ big
+        x.q.copy_(q)  # long after the calls are enqueued
+        logits.copy_(lg)
+        cache = lib.Cache(x.k, x.v)
+        lse = torch.empty(x.q.shape[:2], device="cuda")
+        out = cache.tree_attention(x.q, x.kv_len, x.rows, x.visible, lse=lse)
+        cache.attention_weights(x.q, lse, w, x.kv_len, x.rows, x.visible)
+        cache.evict(w, x.kv_len, keep, recent=4)
+        p = lib.token_probs(logits, 0.9)
+        n, tok = (torch.zeros(len(ks), dtype=torch.int32, device="cuda") for _ in range(2))
+        lib.accept_sampled(p, cand, ks, u, n, tok)
+        got = [t.clone() for t in (out, lse, w, x.k, x.v, x.kv_len, p, n, tok)]
+        del out, p, cache  # may be given away while the calls run
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_results_made_for_a_given_stream(lib):
+    """A result made for a call on another stream than torch's current one is not memory that
+    the current one may still be using, nor given back to it while the call runs."""
+    x = torch.randn((64, 50000), device="cuda")
+    want = lib.token_probs(x, 0.7)
+    at = Inputs((4, 2, 64), [300], [5], ref.tree_masks([5], np.random.default_rng(2)))
+    base, _ = run_attention(lib, at)
+    s = torch.cuda.Stream()
+    cache = lib.Cache(at.k, at.v)
+    torch.cuda.synchronize()
+    for other in (s.cuda_stream, 0):
+        with torch.cuda.stream(s if other == 0 else torch.cuda.default_stream()):
+            p = lib.token_probs(x, 0.7, stream=other)
+            out = cache.tree_attention(at.q, at.kv_len, at.rows, at.visible, stream=other)
+        torch.cuda.synchronize()
+        assert torch.equal(p, want) and torch.equal(out, base)
+    # (memory freed on the current stream is not taken for another one's result)
+    free = torch.empty_like(x)
+    address = free.data_ptr()
+    del free
+    p = lib.token_probs(x, 0.7, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    assert p.data_ptr() != address and torch.equal(p, want)
