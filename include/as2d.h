@@ -695,7 +695,9 @@ as2d_status as2d_verify_sampled(as2d_kv* kv, const int32_t* candidates, const in
    (device float [n_layers][batch][n_kv][capacity], the caller's, who fills in
    what the entries of the prefix start with and keeps it alive), as
    as2d_attention_weights does, over all rows of the call whether accepted or
-   not; NULL ends it.  The weights of accepted entries move with them.  These calls take the
+   not; NULL ends it.  A request that the call drops adds nothing, but for one
+   whose rows give no token (AS2D_DEVERR_NO_TOKEN), which is known at the call's end
+   only.  The weights of accepted entries move with them.  These calls take the
    attention of as2d_verify_tree, so that their logits differ from those of
    other calls by the order of 32-bit sums.  as2d_prefill is refused meanwhile
    (AS2D_ERR_UNSUPPORTED).  Allocates device memory on first use. */

@@ -606,6 +606,7 @@ cudaError_t launch_masked_attention(const RowMap& rm, const Model& m, KvState& s
   e = launch_tree_attention(a, c.head_dim, keys, s.tree_ws, st);
   if (e != cudaSuccess || !s.track) return e;
   w.w = s.track + at;
+  w.skip = s.d_err + 1;  // requests flagged by now are dropped
   ++s.launches;
   return launch_attention_weights(w, c.head_dim, keys, st);
 }

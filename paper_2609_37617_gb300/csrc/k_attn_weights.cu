@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0 && lane == 0) ptx::prefetch_tmap(&tmK);
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  if (warp == 0) make_plan(a, 128, turn, lane, plan, blockIdx.x == 0);
+  if (warp == 0) make_plan(a, 128, turn, lane, plan, blockIdx.x == 0, wa.skip);
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();

@@ -90,6 +90,7 @@ inline uint32_t group_inverse(int nq, int nkv) {
 
 struct WeightArgs {
   TreeArgs t;               // out and v unused; lse is read
+  const int32_t* skip;      // device [batch], nullable: requests (not 0) whose rows add nothing
   float* w;                 // the layer's [batch][nkv][cap]
 };
 

@@ -36,8 +36,9 @@ struct Unit {
 };
 
 // Filled by one warp; requests without rows, or whose length leaves no room for
-// theirs, have no units.
-__device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int extra, int lane, UnitPlan& p, bool flag) {
+// theirs, or that skip (device [batch], nullable) names, have no units.
+__device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int extra, int lane, UnitPlan& p, bool flag,
+                                          const int32_t* skip = nullptr) {
   const int G = a.nq / a.nkv;
   int before = 0;
   bool over = false;
@@ -50,7 +51,7 @@ __device__ __forceinline__ void make_plan(const TreeArgs& a, int q_tile, int ext
       L = a.len[b];
       qts = (rows * G + q_tile - 1) / q_tile;
       if (rows > 0 && rows_fit(L, rows, a.cap))
-        tiles = (L + rows + 127) / 128;
+        tiles = skip && skip[b] ? 0 : (L + rows + 127) / 128;
       else
         over = over || rows > 0;
     }

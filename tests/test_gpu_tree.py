@@ -620,3 +620,30 @@ def test_a_rollback_refused_below_an_eviction_changes_nothing(pair, captured):
     assert ln == ln2 and rt == rt2 and ln[0] > keep
     for a, b in zip(calls, calls2):
         assert all(np.array_equal(x, y) for x, y in zip(a, b))
+
+
+def test_a_dropped_request_leaves_its_tracked_weights(pair):
+    """A bad parent, or a token outside the vocabulary, drops a request before its rows'
+    weights are gathered; the other requests' are those of a call without it."""
+    import paper_2609_37617_gb300 as lib
+    cfg, lens = pair.cfg, [150, 200, 30]
+    w0 = torch.rand((cfg.n_layers, 3, cfg.n_kv, CAP), device="cuda")
+    results = []
+    for cand, parents, match in (([1, 2], [0, 1], None), ([1, 2], [2, 1], "parent"), ([1, cfg.vocab], [0, 1], "vocab"),
+                                 ([-1, 2], [0, 1], "vocab")):
+        st = pair.state(lens, CAP, [5, 6, 7])
+        w = w0.clone()
+        st.track_weights(w)
+        n, _, _, _, _ = run_tree(st, cfg, [cand, [3, 4, 5], []], [parents, [0, 0, 1], []], want_logits=False)
+        if match:
+            with pytest.raises(lib.AS2DError, match=match):
+                st.check()
+            assert n[0] == -1 and torch.equal(w[:, 0], w0[:, 0])
+        else:
+            st.check()
+            assert not torch.equal(w[:, 0, :, :lens[0]], w0[:, 0, :, :lens[0]])
+        results.append(w[:, 1:])
+        st.close()
+    # (the others' sums may come in another order where the work is cut elsewhere)
+    for w in results[1:]:
+        assert ((w - results[0]).abs() <= results[0].abs() * 2.0 ** -9 + 2.0 ** -20).all()
