@@ -602,8 +602,7 @@ cudaError_t launch_masked_attention(const RowMap& rm, const Model& m, KvState& s
     const int64_t n = s.len_upper[b] + rm.start[b + 1] - rm.start[b];
     if (n > keys) keys = n;
   }
-  s.launches += 2;
-  e = launch_tree_attention(a, c.head_dim, keys, s.tree_ws, st);
+  e = launch_tree_attention(a, c.head_dim, keys, s.tree_ws, st, &s.launches);
   if (e != cudaSuccess || !s.track) return e;
   w.w = s.track + at;
   w.skip = s.d_err + 1;  // requests flagged by now are dropped

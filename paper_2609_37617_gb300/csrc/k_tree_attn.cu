@@ -880,13 +880,14 @@ constexpr int kClusterTiles = 6 * kRanks;
 
 template <int D, bool F32>
 cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs& a, const TreeWork& ws,
-                   int64_t items, int most_rows, int64_t most_tiles, int sms, cudaStream_t st) {
+                   int64_t items, int most_rows, int64_t most_tiles, int sms, cudaStream_t st, int64_t& launches) {
   using S = Shape<D, F32>;
   static PerDevice opted[2], clusters;
   cudaError_t e = opt_in(opted[0], tree_attn_kernel<D, F32, true>, S::SMEM);
   if (e == cudaSuccess) e = opt_in(opted[1], tree_attn_kernel<D, F32, false>, S::SMEM);
   if (e != cudaSuccess) return e;
   const int64_t units = items * most_tiles;
+  ++launches;
   const dim3 direct((most_rows * (a.nq / a.nkv) + 127) / 128, a.nkv, a.rm.batch);
   if (most_tiles <= kWholeTiles)
     return launch_pdl(tree_attn_kernel<D, F32, true>, direct, dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
@@ -905,6 +906,7 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
                  (int)kShares, turn);
   if (e != cudaSuccess) return e;
   const dim3 join(direct.x * 4 * (D / 4 / kCombineWarps), direct.y, direct.z);
+  ++launches;
   const int64_t joins = (int64_t)join.x * join.y * join.z;
   return launch_pdl(joins <= 2 * sms   ? tree_combine_kernel<D, F32, 12>
                     : joins <= 3 * sms ? tree_combine_kernel<D, F32, 8>
@@ -939,8 +941,9 @@ size_t tree_attention_workspace(int head_dim) {
 }
 
 cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
-                                  cudaStream_t st) {
+                                  cudaStream_t st, int64_t* launches) {
   const int sms = device_sms();
+  int64_t uncounted = 0, &n = launches ? *launches : uncounted;
   const int64_t items = tree_items(a);
   int most = 0;  // rows of a request
   for (int b = 0; b < a.rm.batch; ++b) most = std::max(most, a.rm.start[b + 1] - a.rm.start[b]);
@@ -953,10 +956,10 @@ cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_k
     return cudaErrorInvalidValue;
   const int64_t tiles = (max_keys + 127) / 128;
   if (head_dim == 128)
-    return a.q_f32 ? launch<128, true>(tk, tv, a, ws, items, most, tiles, sms, st)
-                   : launch<128, false>(tk, tv, a, ws, items, most, tiles, sms, st);
-  return a.q_f32 ? launch<64, true>(tk, tv, a, ws, items, most, tiles, sms, st)
-                 : launch<64, false>(tk, tv, a, ws, items, most, tiles, sms, st);
+    return a.q_f32 ? launch<128, true>(tk, tv, a, ws, items, most, tiles, sms, st, n)
+                   : launch<128, false>(tk, tv, a, ws, items, most, tiles, sms, st, n);
+  return a.q_f32 ? launch<64, true>(tk, tv, a, ws, items, most, tiles, sms, st, n)
+                 : launch<64, false>(tk, tv, a, ws, items, most, tiles, sms, st, n);
 }
 
 }  // namespace as2d

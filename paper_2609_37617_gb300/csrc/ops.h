@@ -115,8 +115,9 @@ struct SampledArgs {
 // SMs of the current device; (request, kv head, tile of 128 queries) items of a call.
 int device_sms();
 int64_t tree_items(const TreeArgs& a);
+// (launches, nullable: counts the kernels enqueued)
 cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
-                                  cudaStream_t st);
+                                  cudaStream_t st, int64_t* launches = nullptr);
 size_t tree_attention_workspace(int head_dim);
 cudaError_t launch_attention_weights(const WeightArgs& a, int head_dim, int64_t max_keys, cudaStream_t st);
 cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, cudaStream_t st);

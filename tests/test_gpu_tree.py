@@ -647,3 +647,18 @@ def test_a_dropped_request_leaves_its_tracked_weights(pair):
     # (the others' sums may come in another order where the work is cut elsewhere)
     for w in results[1:]:
         assert ((w - results[0]).abs() <= results[0].abs() * 2.0 ** -9 + 2.0 ** -20).all()
+
+
+def test_launches_are_counted(pair):
+    """A pass along a tree counts one kernel more a layer where the attention's parts are
+    joined by a second one (long prefixes), none where it is not."""
+    import paper_2609_37617_gb300 as lib
+    cfg, counts = pair.cfg, []
+    for length, cap in ((L0, CAP), (3000, 3100), (8000, 8100)):
+        st = pair.state([length], cap, [5])
+        lib.as2d_kv_profile_read(st.handle)
+        run_tree(st, cfg, [[1, 2, 3]], [[0, 0, 1]], want_logits=False)
+        counts.append(lib.as2d_kv_profile_read(st.handle)[3])
+        st.check()
+        st.close()
+    assert counts[0] == counts[1] == counts[2] - cfg.n_layers
