@@ -521,7 +521,9 @@ as2d_status as2d_budget_select(const double* cost_us, const int32_t* refs,
    as2d_kv_track_weights and as2d_kv_evict, further below, run them on a state.
 
    Each call is enqueued on `stream` without a host synchronisation and can be
-   captured into a graph; nothing is kept from one call to the next.  A
+   captured into a graph; nothing is kept from one call to the next.  Device
+   addresses are multiples of their type's size, and of more where it is said;
+   others are refused.  A
    workspace needs no initial contents, 256-byte alignment, and may serve any
    number of calls that run one after another: calls (or captured graphs) that
    may overlap on the GPU need one each. */

@@ -902,6 +902,8 @@ extern "C" as2d_status as2d_verify_tree(as2d_kv* kh, const int32_t* candidates, 
   KvState& s = kh->s;
   for (int b = 0; b < s.batch; ++b)
     if (k[b] > 0 && !parents) return fail(AS2D_ERR_INVALID_ARG, "parents is NULL");
+  if ((uintptr_t)parents % 4 || (uintptr_t)path % 4)
+    return fail(AS2D_ERR_INVALID_ARG, "parents and path must be 4-byte aligned");
   const as2d_status st = ensure_tree_work(s);
   if (st != AS2D_OK) return st;
   const TreeCall tree{parents, path};
@@ -916,6 +918,8 @@ extern "C" as2d_status as2d_verify_sampled(as2d_kv* kh, const int32_t* candidate
   if (!(temperature > 0.f) || !std::isfinite(temperature))
     return fail(AS2D_ERR_INVALID_ARG, "temperature must be finite and > 0");
   if (out && out->logits) return fail(AS2D_ERR_INVALID_ARG, "out->logits must be NULL: the rows become probabilities");
+  if ((uintptr_t)draft_probs % 4 || (uintptr_t)u % 4 || (uintptr_t)probs % 4)
+    return fail(AS2D_ERR_INVALID_ARG, "draft_probs, u and probs must be 4-byte aligned");
   if (kh->s.model->cfg.vocab > 1 << 24)
     return fail(AS2D_ERR_UNSUPPORTED, "vocab above 2^24 is not supported");
   const SampledCall sampled{draft_probs, u, temperature, probs};
@@ -926,6 +930,7 @@ extern "C" as2d_status as2d_verify_sampled(as2d_kv* kh, const int32_t* candidate
 extern "C" as2d_status as2d_kv_track_weights(as2d_kv* kh, float* weights) {
   g_err.clear();
   if (!kh) return fail(AS2D_ERR_INVALID_ARG, "kv is NULL");
+  if ((uintptr_t)weights % 4) return fail(AS2D_ERR_INVALID_ARG, "weights must be 4-byte aligned");
   KvState& s = kh->s;
   if (weights) {
     const as2d_status st = ensure_tree_work(s);

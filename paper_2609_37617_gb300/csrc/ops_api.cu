@@ -64,6 +64,7 @@ as2d_status check_rows(const as2d_cache* c, int32_t layer, const as2d_tree_rows*
   if (!aligned(r->q, 16) || r->q_stride * size % 16 != 0)
     return invalid("q and q_stride in bytes must be multiples of 16");
   if (!aligned(r->visible, 8)) return invalid("visible must be 8-byte aligned");
+  if (!aligned(r->kv_len, 4)) return invalid("kv_len must be 4-byte aligned");
   a.len = r->kv_len;
   a.cap = c->capacity;
   a.nq = r->n_q;
@@ -116,6 +117,7 @@ extern "C" as2d_status as2d_tree_attention(const as2d_cache* cache, int32_t laye
   if (st != AS2D_OK) return st;
   if (a.rm.rows == 0) return AS2D_OK;
   if (!out || !aligned(out, 16)) return invalid("out must be 16-byte aligned");
+  if (!aligned(lse, 4) || !aligned(error_bits, 4)) return invalid("lse and error_bits must be 4-byte aligned");
   a.out = out;
   a.lse = lse;
   a.err = error_bits;
@@ -133,6 +135,8 @@ extern "C" as2d_status as2d_attention_weights(const as2d_cache* cache, int32_t l
   if (st != AS2D_OK) return st;
   if (a.t.rm.rows == 0) return AS2D_OK;
   if (!lse || !weights) return invalid("lse and weights are required");
+  if (!aligned(lse, 4) || !aligned(weights, 4) || !aligned(error_bits, 4))
+    return invalid("lse, weights and error_bits must be 4-byte aligned");
   a.t.lse = const_cast<float*>(lse);
   a.t.err = error_bits;
   a.w = weights + (size_t)layer * cache->batch * cache->n_kv * cache->capacity;
@@ -156,6 +160,7 @@ extern "C" as2d_status as2d_cache_evict(const as2d_cache* cache, float* weights,
   as2d_status st = check_cache(cache, true);
   if (st != AS2D_OK) return st;
   if (!weights || !kv_len || !keep) return invalid("weights, kv_len and keep are required");
+  if (!aligned(weights, 4) || !aligned(kv_len, 4)) return invalid("weights and kv_len must be 4-byte aligned");
   if (recent < 0) return invalid("recent must be >= 0");
   const int64_t units = (int64_t)cache->n_layers * cache->batch * cache->n_kv;
   st = check_workspace(workspace, workspace_bytes, cache_evict_workspace(units, cache->capacity));
@@ -198,6 +203,9 @@ extern "C" as2d_status as2d_accept_sampled(const float* probs, const float* draf
   clear_error();
   if (!probs || !k || !u || !n_accepted || !token)
     return invalid("probs, k, u, n_accepted and token are required");
+  for (const void* p : {(const void*)probs, (const void*)draft_probs, (const void*)candidates, (const void*)u,
+                        (const void*)n_accepted, (const void*)token})
+    if (!aligned(p, 4)) return invalid("the tensors of an acceptance must be 4-byte aligned");
   if (batch < 1 || batch > kMaxBatch) return invalid("batch must be in [1, AS2D_MAX_BATCH]");
   if (vocab < 1) return invalid("vocab must be >= 1");
   if (vocab > kMaxOpVocab) return report_error(AS2D_ERR_UNSUPPORTED, "vocab above 2^24 is not supported");

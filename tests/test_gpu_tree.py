@@ -662,3 +662,26 @@ def test_launches_are_counted(pair):
         st.check()
         st.close()
     assert counts[0] == counts[1] == counts[2] - cfg.n_layers
+
+
+def test_addresses_off_their_types(pair):
+    """Refused on the host, with nothing enqueued or changed."""
+    import ctypes
+    import paper_2609_37617_gb300 as lib
+    st = pair.state([L0], CAP, [1])
+    n, c = ints([0]), ints([1, 2, 3])
+    f = torch.zeros((4, pair.cfg.vocab), device="cuda")
+    out, k = lib.make_verify_out(n.data_ptr(), n.data_ptr()), lib._i32_array([2])
+    tree = lambda par, path: lib._lib.as2d_verify_tree(  # noqa: E731
+        st.handle, c.data_ptr(), par, k, ctypes.byref(out), path, None)
+    sampled = lambda q, u, p: lib._lib.as2d_verify_sampled(  # noqa: E731
+        st.handle, c.data_ptr(), k, q, u, 1.0, ctypes.byref(out), p, None)
+    at = f.data_ptr()
+    for off in (1, 2, 3):
+        for status in (tree(c.data_ptr() + off, None), tree(c.data_ptr(), n.data_ptr() + off), sampled(at + off, at, at),
+                       sampled(None, at + off, at), sampled(None, at, at + off),
+                       lib._lib.as2d_kv_track_weights(st.handle, at + off)):
+            assert status == lib.AS2D_ERR_INVALID_ARG and "aligned" in lib.as2d_last_error()
+    st.check()
+    assert st.read_state() == ([L0], [1])
+    st.close()

@@ -136,3 +136,25 @@ def test_scale_beyond_its_base_two_form(lib):
     r = rows(lib, scale=3e38)
     assert attention(lib, r=r) == -1 and "scale" in lib.as2d_last_error()
     assert weights(lib, r=r) == -1
+
+
+def test_addresses_off_their_types(lib):
+    """Addresses that are no multiple of their type's size are refused, argument by argument."""
+    for off in (1, 2, 3):
+        r = rows(lib, kv_len=A + off)
+        assert attention(lib, r=r) == -1 and weights(lib, r=r) == -1 and "kv_len" in lib.as2d_last_error()
+        c, r = ctypes.byref(cache(lib)), ctypes.byref(rows(lib))
+        assert lib._lib.as2d_tree_attention(c, 0, r, A, A + off, A, 1 << 40, None, None) == -1
+        assert lib._lib.as2d_tree_attention(c, 0, r, A, None, A, 1 << 40, A + off, None) == -1
+        assert weights(lib, lse=A + off) == -1 and weights(lib, w=A + off) == -1
+        assert lib._lib.as2d_attention_weights(c, 0, r, A, A, A + off, None) == -1
+        keep = (ctypes.c_int32 * 2)(5, 5)
+        assert lib._lib.as2d_cache_evict(c, A + off, A, keep, 0, A, 1 << 40, None) == -1
+        assert lib._lib.as2d_cache_evict(c, A, A + off, keep, 0, A, 1 << 40, None) == -1
+        k = (ctypes.c_int32 * 2)(2, 2)
+        good = [A, A, A, k, 2, 100, A, A, A]
+        for at in (0, 1, 2, 6, 7, 8):
+            args = list(good)
+            args[at] = A + off
+            assert lib._lib.as2d_accept_sampled(*args, None) == -1, at
+            assert "aligned" in lib.as2d_last_error()
