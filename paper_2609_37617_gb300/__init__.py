@@ -598,26 +598,33 @@ class State:
                               logits.data_ptr() if logits is not None else 0)
         _check(as2d_decode_step(self.handle, out, stream), "as2d_decode_step")
 
+    def _counts(self, values, name):
+        if len(values) != self.batch:
+            raise ValueError(f"{name} must name {self.batch} requests")
+        return _int32s(values, name)
+
     def verify_tree(self, candidates, parents, k, n_accepted, correction, greedy=None, logits=None,
                     path=None, stream=0):
         """as2d_verify_tree: device int32 candidates and parents, packed."""
+        counts = self._counts(k, "k")
         out = make_verify_out(n_accepted.data_ptr(), correction.data_ptr(),
                               greedy.data_ptr() if greedy is not None else 0,
                               logits.data_ptr() if logits is not None else 0)
         some = candidates is not None and candidates.numel()
         _check(_lib.as2d_verify_tree(
             self.handle, candidates.data_ptr() if some else None, parents.data_ptr() if some else None,
-            _i32_array(k), ctypes.byref(out), path.data_ptr() if path is not None else None, stream),
+            counts, ctypes.byref(out), path.data_ptr() if path is not None else None, stream),
             "as2d_verify_tree")
 
     def verify_sampled(self, candidates, k, u, temperature, probs, n_accepted, correction,
                        draft_probs=None, greedy=None, stream=0):
         """as2d_verify_sampled: u [rows] and probs [rows, vocab] device float."""
+        counts = self._counts(k, "k")
         out = make_verify_out(n_accepted.data_ptr(), correction.data_ptr(),
                               greedy.data_ptr() if greedy is not None else 0)
         some = candidates is not None and candidates.numel()
         _check(_lib.as2d_verify_sampled(
-            self.handle, candidates.data_ptr() if some else None, _i32_array(k),
+            self.handle, candidates.data_ptr() if some else None, counts,
             draft_probs.data_ptr() if draft_probs is not None and some else None, u.data_ptr(),
             temperature, ctypes.byref(out), probs.data_ptr(), stream), "as2d_verify_sampled")
 
@@ -628,9 +635,8 @@ class State:
         self._weights = weights
 
     def evict(self, keep, recent=0, stream=0):
-        if len(keep) != self.batch:
-            raise ValueError(f"keep must name {self.batch} requests")
-        _check(_lib.as2d_kv_evict(self.handle, _i32_array(keep), recent, stream), "as2d_kv_evict")
+        _check(_lib.as2d_kv_evict(self.handle, self._counts(keep, "keep"), _int32s((recent,), "recent")[0], stream),
+               "as2d_kv_evict")
 
     def verify_from_buffers(self, bufs, b, stream=0):
         """One verification call with candidates from CandidateBuffer objects
@@ -692,6 +698,15 @@ class State:
 # current stream unless one is given.  A result that the call makes itself belongs to that
 # stream, as a tensor that torch makes there would.
 
+def _int32s(values, name):
+    """A C array of Python integers; ctypes itself takes those beyond 32 bits modulo 2^32."""
+    values = list(values)
+    array = (ctypes.c_int32 * len(values))(*values)
+    if array[:] != values:
+        raise ValueError(f"{name} must be of 32 bits")
+    return array
+
+
 def _stream_reader(torch):
     """A function that gives torch's current stream of a device as a cudaStream_t."""
     return (getattr(torch._C, "_cuda_getCurrentRawStream", None) or
@@ -750,7 +765,7 @@ class Cache:
         self.k, self.v, self.shape = k, v, tuple(k.shape)
         self._c = as2d_cache(kp, vp, *self.shape)
         self._ref = ctypes.byref(self._c)
-        self._i32s, self._per_request = ctypes.c_int32 * self.shape[1], self.shape[1:2]
+        self._per_request = self.shape[1:2]
         self._bf16, self._f32, self._i32, self._i64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
         self._mask = (torch.int64, torch.uint64)
         need = _I64()
@@ -777,10 +792,12 @@ class Cache:
     def _counts(self, values, name):
         if len(values) != self.shape[1]:
             raise ValueError(f"{name} must name {self.shape[1]} requests")
-        return self._i32s(*values)
+        return _int32s(values, name)
 
-    def _rows(self, device, q, kv_len, rows, visible, scale, max_len):
+    def _rows(self, device, q, kv_len, rows, visible, scale, layer, max_len):
         d = self.shape[4]
+        if abs(layer) >> 31 or abs(max_len) >> 31:
+            raise ValueError("layer and max_len must be of 32 bits")
         at = _tensor(q, "q", device, (self._bf16, self._f32), None, False)
         shape = q.shape
         n_q = shape[1] if len(shape) == 3 else 0
@@ -812,7 +829,7 @@ class Cache:
             stream = current
             if stream != self._made_on:
                 self._used_here()
-        r = self._rows(device, q, kv_len, rows, visible, scale, max_len)
+        r = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
         shape = q.shape
         if out is None:
             out = q.new_empty(shape) if stream == current else _new_on(stream, device, q, shape)
@@ -835,7 +852,7 @@ class Cache:
             stream = current
             if stream != self._made_on:
                 self._used_here()
-        r = self._rows(device, q, kv_len, rows, visible, scale, max_len)
+        r = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
         st = _lib.as2d_attention_weights(
             self._ref, layer, ctypes.byref(r), _address(lse, "lse", device, self._f32, q.shape[:2]),
             _address(weights, "weights", device, self._f32, self.shape[:4]),
@@ -855,7 +872,7 @@ class Cache:
         st = _lib.as2d_cache_evict(
             self._ref, _address(weights, "weights", device, self._f32, self.shape[:4]),
             _address(kv_len, "kv_len", device, self._i32, self._per_request),
-            self._counts(keep, "keep"), recent, self._workspace.data_ptr(), self._workspace.numel(), stream)
+            self._counts(keep, "keep"), _int32s((recent,), "recent")[0], self._workspace.data_ptr(), self._workspace.numel(), stream)
         if st:
             _check(st, "as2d_cache_evict")
 
@@ -895,7 +912,7 @@ def accept_sampled(probs, candidates, k, u, n_accepted, token, draft_probs=None,
         at, None if draft_probs is None or total == 0 else
         _address(draft_probs, "draft_probs", device, f32, (total, shape[1])),
         None if candidates is None or total == 0 else
-        _address(candidates, "candidates", device, i32, (total,)), (ctypes.c_int32 * batch)(*k),
+        _address(candidates, "candidates", device, i32, (total,)), _int32s(k, "k"),
         batch, shape[1], _address(u, "u", device, f32, shape[:1]),
         _address(n_accepted, "n_accepted", device, i32, (batch,)),
         _address(token, "token", device, i32, (batch,)), stream)

@@ -975,3 +975,25 @@ def test_results_made_for_a_given_stream(lib):
     p = lib.token_probs(x, 0.7, stream=s.cuda_stream)
     torch.cuda.synchronize()
     assert p.data_ptr() != address and torch.equal(p, want)
+
+
+def test_integers_beyond_32_bits(lib):
+    """Counts and indices that 32 bits do not hold are refused, not taken modulo 2^32."""
+    x = Inputs((4, 2, 64), [40], [3], ref.tree_masks([3], np.random.default_rng(1)))
+    cache, w = lib.Cache(x.k, x.v), torch.zeros(x.k.shape[:4], device="cuda")
+    lse = torch.zeros((3, 4), device="cuda")
+    n, tok = (torch.full((2,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    p, u = torch.ones((2, 8), device="cuda"), torch.zeros(2, device="cuda")
+    far = 2 ** 32
+    for call in (lambda: cache.evict(w, x.kv_len, [far + 20]), lambda: cache.evict(w, x.kv_len, [far]),
+                 lambda: cache.evict(w, x.kv_len, [2 ** 63 - 1]), lambda: cache.evict(w, x.kv_len, [20], recent=far),
+                 lambda: cache.tree_attention(x.q, x.kv_len, x.rows, layer=far),
+                 lambda: cache.tree_attention(x.q, x.kv_len, x.rows, max_len=far),
+                 lambda: cache.attention_weights(x.q, lse, w, x.kv_len, x.rows, layer=-far),
+                 lambda: lib.accept_sampled(p, None, [far, -far], u, n, tok)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    torch.cuda.synchronize()
+    assert x.kv_len.tolist() == [40] and (w == 0).all() and n.tolist() == [-7, -7]
+    with pytest.raises(lib.AS2DError):  # (what 32 bits hold goes on to the library's own checks)
+        cache.tree_attention(x.q, x.kv_len, x.rows, layer=1)

@@ -685,3 +685,21 @@ def test_addresses_off_their_types(pair):
     st.check()
     assert st.read_state() == ([L0], [1])
     st.close()
+
+
+def test_counts_of_a_state(pair):
+    """One count to each request, of 32 bits."""
+    st = pair.state([L0, 30], CAP, [1, 2])
+    st.track_weights(torch.zeros(st.kc.shape[:4], device="cuda"))
+    n, c = ints([0, 0]), ints([1, 2, 3])
+    probs, u = torch.empty((4, pair.cfg.vocab), device="cuda"), torch.zeros(4, device="cuda")
+    for k in ([1], [1, 1, 1], [2 ** 32 + 1, 1], [1, 2 ** 32]):
+        for call in (lambda: st.verify_tree(c, ints([0, 0, 0]), k, n, n), lambda: st.evict(k),
+                     lambda: st.verify_sampled(c, k, u, 1.0, probs, n, n)):
+            with pytest.raises(ValueError):
+                call()
+    with pytest.raises(ValueError):
+        st.evict([20, 20], recent=2 ** 32)
+    st.check()
+    assert st.read_state() == ([L0, 30], [1, 2])
+    st.close()
