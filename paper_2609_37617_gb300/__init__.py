@@ -603,35 +603,52 @@ class State:
             raise ValueError(f"{name} must name {self.batch} requests")
         return _int32s(values, name)
 
+    def _address(self, t, name, dtype, least):
+        """Device address of a contiguous tensor of `least` elements or more on the caches' device
+        (None: NULL)."""
+        if t is None:
+            return None
+        if str(t.dtype) != dtype:
+            raise TypeError(f"{name} must be a tensor of {dtype}")
+        if t.get_device() != self._caches[0].get_device():
+            raise ValueError(f"{name} must be on the caches' device")
+        if not t.is_contiguous() or t.numel() < least:
+            raise ValueError(f"{name} must be contiguous, of {least} elements")
+        return t.data_ptr()
+
     def verify_tree(self, candidates, parents, k, n_accepted, correction, greedy=None, logits=None,
                     path=None, stream=0):
         """as2d_verify_tree: device int32 candidates and parents, packed."""
-        counts = self._counts(k, "k")
-        out = make_verify_out(n_accepted.data_ptr(), correction.data_ptr(),
-                              greedy.data_ptr() if greedy is not None else 0,
-                              logits.data_ptr() if logits is not None else 0)
+        counts, total = self._counts(k, "k"), sum(k)
+        rows, i32, at = total + self.batch, "torch.int32", self._address
+        out = make_verify_out(at(n_accepted, "n_accepted", i32, self.batch),
+                              at(correction, "correction", i32, self.batch), at(greedy, "greedy", i32, rows) or 0,
+                              at(logits, "logits", "torch.float32", rows * self.model.cfg.vocab) or 0)
         some = candidates is not None and candidates.numel()
         _check(_lib.as2d_verify_tree(
-            self.handle, candidates.data_ptr() if some else None, parents.data_ptr() if some else None,
-            counts, ctypes.byref(out), path.data_ptr() if path is not None else None, stream),
-            "as2d_verify_tree")
+            self.handle, at(candidates if some else None, "candidates", i32, total),
+            at(parents if some else None, "parents", i32, total), counts, ctypes.byref(out),
+            at(path, "path", i32, self.batch * AS2D_MAX_K), stream), "as2d_verify_tree")
 
     def verify_sampled(self, candidates, k, u, temperature, probs, n_accepted, correction,
                        draft_probs=None, greedy=None, stream=0):
         """as2d_verify_sampled: u [rows] and probs [rows, vocab] device float."""
-        counts = self._counts(k, "k")
-        out = make_verify_out(n_accepted.data_ptr(), correction.data_ptr(),
-                              greedy.data_ptr() if greedy is not None else 0)
+        counts, total, vocab = self._counts(k, "k"), sum(k), self.model.cfg.vocab
+        rows, i32, f32, at = total + self.batch, "torch.int32", "torch.float32", self._address
+        out = make_verify_out(at(n_accepted, "n_accepted", i32, self.batch),
+                              at(correction, "correction", i32, self.batch), at(greedy, "greedy", i32, rows) or 0)
         some = candidates is not None and candidates.numel()
         _check(_lib.as2d_verify_sampled(
-            self.handle, candidates.data_ptr() if some else None, counts,
-            draft_probs.data_ptr() if draft_probs is not None and some else None, u.data_ptr(),
-            temperature, ctypes.byref(out), probs.data_ptr(), stream), "as2d_verify_sampled")
+            self.handle, at(candidates if some else None, "candidates", i32, total), counts,
+            at(draft_probs if some else None, "draft_probs", f32, total * vocab), at(u, "u", f32, rows),
+            temperature, ctypes.byref(out), at(probs, "probs", f32, rows * vocab), stream), "as2d_verify_sampled")
 
     def track_weights(self, weights):
         """as2d_kv_track_weights: a device float tensor (kept alive here) or None."""
+        caches = self._caches[0]
         _check(_lib.as2d_kv_track_weights(
-            self.handle, weights.data_ptr() if weights is not None else None), "as2d_kv_track_weights")
+            self.handle, self._address(weights, "weights", "torch.float32", caches.numel() // self.model.cfg.head_dim)),
+            "as2d_kv_track_weights")
         self._weights = weights
 
     def evict(self, keep, recent=0, stream=0):

@@ -703,3 +703,40 @@ def test_counts_of_a_state(pair):
     st.check()
     assert st.read_state() == ([L0, 30], [1, 2])
     st.close()
+
+
+def test_tensors_of_a_state(pair):
+    """Tensors of another type, device or layout, or too few elements, are refused before the call."""
+    st, V = pair.state([L0, 30], CAP, [1, 2]), pair.cfg.vocab
+    z = lambda *s, t=torch.int32, d="cuda": torch.zeros(s, dtype=t, device=d)  # noqa: E731
+    f = torch.float32
+
+    def tree(**kw):
+        a = dict(candidates=z(3), parents=z(3), k=[2, 1], n_accepted=z(2), correction=z(2), greedy=z(5),
+                 logits=z(5, V, t=f), path=z(2, 16))
+        a.update(kw)
+        st.verify_tree(**a)
+
+    def sampled(**kw):
+        a = dict(candidates=z(3), k=[2, 1], u=z(5, t=f), temperature=1.0, probs=z(5, V, t=f), n_accepted=z(2),
+                 correction=z(2), draft_probs=z(3, V, t=f), greedy=z(5))
+        a.update(kw)
+        st.verify_sampled(**a)
+    both = [("candidates", 3), ("n_accepted", 2), ("correction", 2), ("greedy", 5)]
+    for call, names in ((tree, both + [("parents", 3), ("path", 32)]), (sampled, both)):
+        for name, n in names:
+            for bad in (z(n - 1), z(n, d="cpu"), z(n, t=torch.int64), z(2 * n)[::2]):
+                with pytest.raises((ValueError, TypeError), match=name):
+                    call(**{name: bad})
+    for call, names in ((tree, [("logits", 5 * V)]), (sampled, [("u", 5), ("probs", 5 * V), ("draft_probs", 3 * V)]),
+                        (lambda weights: st.track_weights(weights), [("weights", st.kc[..., 0].numel())])):
+        for name, n in names:
+            for bad in (z(n - 1, t=f), z(n, t=f, d="cpu"), z(n, t=torch.float64), z(n, t=torch.bfloat16), z(2 * n, t=f)[::2]):
+                with pytest.raises((ValueError, TypeError), match=name):
+                    call(**{name: bad})
+    st.check()
+    assert st.read_state() == ([L0, 30], [1, 2])
+    tree()
+    sampled()
+    st.check()
+    st.close()
