@@ -997,3 +997,40 @@ def test_integers_beyond_32_bits(lib):
     assert x.kv_len.tolist() == [40] and (w == 0).all() and n.tolist() == [-7, -7]
     with pytest.raises(lib.AS2DError):  # (what 32 bits hold goes on to the library's own checks)
         cache.tree_attention(x.q, x.kv_len, x.rows, layer=1)
+
+
+def test_captured_on_torchs_current_stream(lib):
+    """The step captured as torch captures its own work, results made in the graph's memory among
+    it; replayed, and everything given back afterwards."""
+    args = together_inputs(8)
+    x, w, logits, cand, ks, u, keep = args
+    inputs = (x.k, x.v, x.kv_len, w)
+    first = [t.clone() for t in inputs]
+    cache = lib.Cache(x.k, x.v)
+
+    def step():
+        lse = torch.empty(x.q.shape[:2], device="cuda")
+        out = cache.tree_attention(x.q, x.kv_len, x.rows, x.visible, lse=lse)
+        cache.attention_weights(x.q, lse, w, x.kv_len, x.rows, x.visible)
+        cache.evict(w, x.kv_len, keep, recent=4)
+        p = lib.token_probs(logits, 0.9)
+        n, tok = (torch.empty(len(ks), dtype=torch.int32, device="cuda") for _ in range(2))
+        lib.accept_sampled(p, cand, ks, u, n, tok)
+        return out, lse, p, n, tok
+    want = [t.clone() for t in step() + inputs]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        made = step()
+    for _ in range(3):
+        for t, f in zip(inputs, first):
+            t.copy_(f)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(made + inputs, want))
+    torch.cuda.synchronize()
+    del made, graph, cache
+    torch.cuda.empty_cache()
+    again = lib.Cache(x.k, x.v)
+    for t, f in zip(inputs, first):
+        t.copy_(f)
+    assert torch.equal(again.tree_attention(x.q, x.kv_len, x.rows, x.visible), want[0])

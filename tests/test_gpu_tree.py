@@ -740,3 +740,25 @@ def test_tensors_of_a_state(pair):
     sampled()
     st.check()
     st.close()
+
+
+def test_sampled_drops_a_bad_token(pair):
+    """A candidate outside the vocabulary drops its request, its tracked weights as they were;
+    the other goes on by the rule."""
+    import paper_2609_37617_gb300 as lib
+    cfg = pair.cfg
+    for bad in (cfg.vocab, -1, 2 ** 31 - 1):
+        st = pair.state([L0, 50], CAP, [1, 2])
+        w0 = torch.rand(st.kc.shape[:4], device="cuda")
+        w = w0.clone()
+        st.track_weights(w)
+        probs, u = torch.empty((5, cfg.vocab), device="cuda"), torch.full((5,), 0.5, device="cuda")
+        n, corr = (torch.zeros(2, dtype=torch.int32, device="cuda") for _ in range(2))
+        st.verify_sampled(ints([5, bad, 9]), [2, 1], u, 0.5, probs, n, corr)
+        with pytest.raises(lib.AS2DError, match="vocab"):
+            st.check()
+        want = ref.accept(probs[3:].double().cpu().numpy(), None, [9], [1], [0.5, 0.5])
+        assert n.tolist() == [-1] + want[0] and corr.tolist() == [-1] + want[1]
+        assert st.read_state() == ([L0, 51 + want[0][0]], [1, want[1][0]])
+        assert torch.equal(w[:, 0], w0[:, 0]) and not torch.equal(w[:, 1, :, :50], w0[:, 1, :, :50])
+        st.close()
