@@ -102,31 +102,27 @@ __device__ __forceinline__ void add_weights(const uint32_t (&v)[16], uint64_t c2
   }
 }
 
-// The weight of one key of 32-bit queries q0 .. q0 + n - 1 of a head, that came out as NaN: if the key
-// holds infinities (and no NaN) once more in 32-bit arithmetic, as in hi and lo parts a score
-// of -inf may be NaN.
+// The weight of one key of 32-bit queries q0 .. q0 + n - 1 of a head, that came out as NaN, by a whole warp:
+// if the key holds infinities (and no NaN) once more in 32-bit arithmetic, as in hi and lo
+// parts a score of -inf may be NaN.
 template <int D>
 __device__ __forceinline__ float weight_of(const TreeArgs& a, const Unit& it, int q0, int n, int key, const float* lse,
-                                           const uint2* seen, uint32_t need, bool upper) {
+                                           const uint2* seen, uint32_t need, bool upper, int lane) {
   const bf16* k = a.k + (((size_t)it.b * a.nkv + it.g) * a.cap + key) * D;
+  if (!infinite_key<D>(k, lane)) return NAN;
   const int G = a.nq / a.nkv;
-  bool inf = false, none = true;
-#pragma unroll 1
-  for (int d = 0; d < D; ++d) {
-    const float y = fabsf(__bfloat162float(k[d]));
-    inf = inf || y == INFINITY;
-    none = none && y == y;
-  }
-  if (!inf || !none) return NAN;
   float sum = 0.f;
 #pragma unroll 1
-  for (int q = 0; q < n; ++q) {
+  for (int q = lane; q < n; q += 32) {
     const uint32_t w = upper ? seen[q].y : seen[q].x;
     if ((w & need) != need) continue;
     const int i = divide_group(a, q0 + q);
     const float* x = (const float*)a.q + (it.r0 + i) * a.q_stride + (int64_t)(it.g * G + (q0 + q - i * G)) * D;
     sum += ex2(fmaf(exact_product<D>(x, k), a.scale_log2, lse[q]));
   }
+  __syncwarp();
+#pragma unroll 1
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
   return sum;
 }
 
@@ -372,9 +368,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(&s_empty[buf]);
           float more = sums.x + sums.y;
-          if (F32 && ok && live && more != more) more = weight_of<D>(a, s.it, qt * 128, n, key, lse, seen, need, upper);
+          if (F32)
+            for (unsigned left = __ballot_sync(~0u, ok && live && more != more); left; left &= left - 1) {
+              const int of = __ffs(left) - 1;
+              const float y = weight_of<D>(a, s.it, qt * 128, n, __shfl_sync(~0u, key, of), lse, seen,
+                                           __shfl_sync(~0u, need, of), __shfl_sync(~0u, (int)upper, of), lane);
+              if (lane == of) more = y;
+            }
           if (live && ok) w[key] = before + more;
-          __syncwarp();
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&e_empty[pass & 1]);

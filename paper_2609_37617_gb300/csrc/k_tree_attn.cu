@@ -202,14 +202,7 @@ __device__ __forceinline__ float mend_weights(uint32_t ts, bool mine, const floa
     for (uint32_t left = __reduce_or_sync(~0u, nan); left; left &= left - 1) {
       const int e = __ffs(left) - 1;
       const bf16* key = k + (size_t)(x + e) * D;
-      bool inf = false, none = true;  // infinities, no NaN
-#pragma unroll
-      for (int d = 0; d < D; d += 32) {
-        const float y = fabsf(__bfloat162float(key[d + lane]));
-        inf = inf || y == INFINITY;
-        none = none && y == y;
-      }
-      if (!__any_sync(~0u, inf) || !__all_sync(~0u, none)) continue;
+      if (!infinite_key<D>(key, lane)) continue;
       if (((nan >> e) & 1) && exact_product<D>(q, key) * c < ref - 160.f) gone |= 1u << e;
       __syncwarp();
     }

@@ -60,6 +60,19 @@ __device__ __forceinline__ void hi_lo(float a, float b, uint32_t& h, uint32_t& l
   l = pack2(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xFFFF0000u));
 }
 
+// Whether a key holds infinities and no NaN, by a whole warp.
+template <int D>
+__device__ __forceinline__ bool infinite_key(const bf16* k, int lane) {
+  bool inf = false, none = true;
+#pragma unroll
+  for (int d = 0; d < D; d += 32) {
+    const float y = fabsf(__bfloat162float(k[d + lane]));
+    inf = inf || y == INFINITY;
+    none = none && y == y;
+  }
+  return __any_sync(~0u, inf) && __all_sync(~0u, none);
+}
+
 // A 32-bit query's product with a key, in 32-bit arithmetic.
 template <int D>
 __device__ __forceinline__ float exact_product(const float* q, const bf16* k) {
