@@ -577,7 +577,9 @@ as2d_status as2d_tree_attention_workspace(const as2d_cache* cache, int64_t* byte
      out = sum_t p_t v_t,  p = softmax over the visible t of scale q k_t,
    and, unless lse is NULL, lse = ln sum_t e^(scale q k_t).  out: device [sum
    rows][n_q][head_dim] of q_type, 16-byte aligned; lse: device float [sum
-   rows][n_q].  Scores, maxima and sums are held in 32 bits.  A row that sees
+   rows][n_q].  Scores, maxima and sums are held in 32 bits; 32-bit queries and the
+   weights p enter the products as two bf16 parts, to 2^-17 of each (as the
+   operands of this library's projections do).  A row that sees
    nothing gets out = 0 and lse = -inf.  What a row does not see does not reach
    its result, whatever it holds (NaN and infinities among it).  What it sees
    does as the formula has it: an infinite value makes its dim that infinity
@@ -644,7 +646,8 @@ as2d_status as2d_token_probs(const float* logits, int32_t n_rows, int32_t vocab,
    does not.  The token after them is drawn, by u_k, from max(p_n - q_n, 0) if n <
    k (without draft_probs: p_n without candidate n) and from p_k otherwise: the
    lowest v at which the sum of the weights up to v exceeds u_k times their total
-   (sums to some 48 bits).  With u uniform the tokens follow the target's
+   (sums to some 48 bits where the total is 2^-100 or more; a total beyond 32-bit
+   range gives token -1).  With u uniform the tokens follow the target's
    distribution.  Weights need not sum to 1; negative, infinite
    and NaN ones count as 0.  If max(p_n -
    q_n, 0) is 0 throughout the token is drawn from p_n; if that is too, token

@@ -18,9 +18,9 @@
 // 14-17 take the tiles in turn.  More than 128 queries: one pass over the CTA's
 // tiles for each 128 (the keys then come from L2).
 //
-// Bound by memory: each key is read once (16 ragged requests, 64 MB: 21.2 us, of
+// Bound by memory: each key is read once (16 ragged requests, 64 MB: 21.5 us, of
 // which 10 at 6 TB/s in the loop, 4 until the first product, 2 for each turn), for few
-// entries by latency (9 rows over 814 entries of two kv heads: 8.3 us).
+// entries by latency (9 rows over 814 entries of two kv heads: 8.0 to 9.2 us).
 #include <type_traits>
 
 #include "ops.h"

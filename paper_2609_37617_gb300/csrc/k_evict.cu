@@ -6,7 +6,9 @@
 // counted in shared memory), then the entries that stay, in
 // order: those above it, those equal to it from the lowest position up to the
 // number wanted, the latest `recent`.  It writes their old positions and moves
-// their weights.  The weights stay in registers over all passes.
+// their weights.  Each thread reads its weights once and holds them over all passes: in
+// registers up to a capacity of 16384 (16 a thread), mostly in local memory beyond (64 a
+// thread of 64 registers: 880 bytes of stack, not timed).
 // evict_move_kernel, one CTA per unit, cache and 128 bytes of an entry: entry j comes
 // from position at[j] >= j.  Tiles of entries in order, a tile read wholly before
 // it is written: what its writes cover, [j0, j0 + T), no later tile reads, as
@@ -52,7 +54,7 @@ __device__ __forceinline__ int warp_prefix(int v, int* s) {
 }
 
 // T threads, E entries of a thread (a warp's are consecutive, 32 at a time), which
-// stay in registers.
+// it holds.
 template <int T, int E>
 __global__ void __launch_bounds__(T) evict_select_kernel(const __grid_constant__ EvictArgs a) {
   constexpr int W = T / 32, B = kBins / T;  // warps, bins of a thread
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const __grid_constant__
     n += __popc(__ballot_sync(~0u, yes));
   }
   int j = warp_prefix<W>(n, s_w), first = keep;
-  // (every weight is in a register by now: their places can be written)
+  // (every weight has been read by now: their places can be written)
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     const bool yes = (stay[i / 32] >> (i % 32)) & 1;
@@ -221,8 +223,8 @@ void cache_evict_carve(EvictArgs& a, int64_t units, void* workspace) {
 
 cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, cudaStream_t st) {
   const unsigned units = (unsigned)(a.n_layers * a.batch * a.nkv);
-  // (an eviction of 200 entries of the tiny decoder takes 17.0 us with 1024 threads,
-  // 13.5 with 256: fewer warps wait for one another)
+  // (an eviction of 200 entries of the tiny decoder took 17.0 us with 1024 threads and
+  // 13.5 with 256 on one machine: fewer warps wait for one another.  14.4 to 18.3 over machines.)
   const cudaError_t e =
       a.cap <= 4096    ? launch_pdl(evict_select_kernel<256, 16>, dim3(units), dim3(256), 0, st, 1, a)
       : a.cap <= 16384 ? launch_pdl(evict_select_kernel<1024, 16>, dim3(units), dim3(1024), 0, st, 1, a)

@@ -30,7 +30,7 @@ __device__ __forceinline__ float ex2(float x) {
 // bytes.
 
 // Bound by latency for few rows (9 of 152064 values 5.2 us), by memory for many (145:
-// 35.3 us, 5.0 TB/s).
+// 35.4 us, 5.0 TB/s).
 //
 // Threads, values a thread holds, CTAs per SM.  145 rows of 152064 values, us: 512 /
 // 40 / 2 39, 256 / 40 / 4 42, 256 / 48 / 3 41, 128 / 40 / 8 45, 1024 / 24 / 1 55
@@ -217,8 +217,9 @@ __global__ void __launch_bounds__(kProbs, kProbsCtas) probs_rows_kernel(const fl
 // the border lies between finds the token in its chunk.  All of it in pairs of
 // floats: in 64 bits, at this card's rate and latency for them, the additions of
 // one request took 9 of 22 us.  Bound by latency for a few requests (three
-// dependent round trips to memory: one 7.0 us), by how many clusters of 16 run at
-// once for more (16 with draft 15.0 us; with 12, 10 and 9 CTAs 14.1, 17.7 and 14.4).
+// dependent round trips to memory: one without draft 7.0 us).  What bounds more of them has
+// not been found: 16 with draft take 15.0 us with 16 CTAs each, of which 14 clusters run at
+// once, and 14.1, 17.7 and 14.4 with 12, 10 and 9, of which all run.
 
 // a + b = s + e exactly.
 __device__ __forceinline__ void two_sum(float a, float b, float& s, float& e) {

@@ -37,11 +37,18 @@
 // of |q| |k|), 16-bit ones are exact.
 //
 // Bound by memory for the rows of a chain or a small tree (a key and value are
-// read once: 16 ragged requests, 126 MB, 38.7 us; in the loop 5.3 TB/s of a copy's
+// read once: 16 ragged requests, 126 MB, 39.3 us; in the loop 5.3 TB/s of a copy's
 // 6.8, the rest is start, turns and join), by the products and what stands
 // between them for more than 128 queries to a kv head (64 rows of seven over 15128
-// entries 29.6 us, the tensor pipe 3/4 busy in the loop), by the latency of one
-// chain of launch, load, products for few entries (9 rows over 1564: 9.5 us).
+// entries 29.5 us, the tensor pipe 3/4 busy in the loop), by the latency of one
+// chain of launch, load, products for few entries (one row over 1564: 9 to 10.7 us).
+//
+// What is not finite.  NaN scores pass the maxima by and reach the sums, so a row that sees NaN
+// is NaN in out and lse.  Parts of bf16 products take infinities apart (hi inf + lo inf with lo
+// negative or 0): a NaN in a tile's sum, and an accumulator that is not finite, make the
+// warp look at the keys or values once more (mend_weights, not_finite_values), at 1.8 % of the
+// ragged requests' time and none of the tree's where all is finite; an infinite value in
+// 15128 entries costs 64 rows of 32-bit queries some 90 us, NaN everywhere some 100.
 #include <algorithm>
 #include <cfloat>
 

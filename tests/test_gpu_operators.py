@@ -1034,3 +1034,16 @@ def test_captured_on_torchs_current_stream(lib):
     for t, f in zip(inputs, first):
         t.copy_(f)
     assert torch.equal(again.tree_attention(x.q, x.kv_len, x.rows, x.visible), want[0])
+
+
+def test_accept_largest_and_smallest_weights(lib):
+    """Weights whose total 32 bits do not hold give no token; the smallest ones do."""
+    p = np.zeros((1, 4000), dtype=np.float32)
+    p[0, [5, 9, 3990]] = 3e38
+    assert run_accept(lib, p, None, [], [0], [0.5]) == ([0], [-1])
+    p[0, [9, 3990]] = 0.0
+    assert run_accept(lib, p, None, [], [0], [0.5]) == ([0], [5])
+    p[0, 5] = 0.0
+    p[0, [3, 3990]] = 1e-44
+    for u, want in ((0.0, 3), (0.25, 3), (0.75, 3990), (1 - 2.0 ** -24, 3990)):
+        assert run_accept(lib, p, None, [], [0], [u]) == ([0], [want])
