@@ -579,6 +579,7 @@ class State:
         self.model = model
         self.batch = len(kv_len)
         self._caches = (k_cache, v_cache)
+        self._places = model.cfg.n_layers * self.batch * model.cfg.n_kv_heads * capacity
         st, h = as2d_kv_init_prefilled(model.handle, self.batch, kv_len, capacity,
                                        k_cache.data_ptr(), v_cache.data_ptr(), roots)
         _check(st, "as2d_kv_init_prefilled")
@@ -645,10 +646,8 @@ class State:
 
     def track_weights(self, weights):
         """as2d_kv_track_weights: a device float tensor (kept alive here) or None."""
-        caches = self._caches[0]
         _check(_lib.as2d_kv_track_weights(
-            self.handle, self._address(weights, "weights", "torch.float32", caches.numel() // self.model.cfg.head_dim)),
-            "as2d_kv_track_weights")
+            self.handle, self._address(weights, "weights", "torch.float32", self._places)), "as2d_kv_track_weights")
         self._weights = weights
 
     def evict(self, keep, recent=0, stream=0):
@@ -795,16 +794,16 @@ class Cache:
         self._current_stream = _stream_reader(torch)
         self._made_on = self._current_stream(device)
 
-    def _device(self):
+    def _enter(self, stream):
+        """(device, torch's current stream, the call's stream) of a call."""
         device = self._current()
         if device != self._on:
             raise ValueError("the cache must be on the current CUDA device")
-        return device
-
-    def _used_here(self):
-        """Tells torch's allocator of a use of the workspace on torch's current stream."""
-        import torch
-        self._workspace.record_stream(torch.cuda.current_stream(self._on))
+        current = self._current_stream(device)
+        if stream is None and current != self._made_on:
+            import torch  # torch's allocator is told of a use on another stream than the workspace's own
+            self._workspace.record_stream(torch.cuda.current_stream(device))
+        return device, current, current if stream is None else stream
 
     def _counts(self, values, name):
         if len(values) != self.shape[1]:
@@ -840,12 +839,7 @@ class Cache:
     def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
                        lse=None, error_bits=None, stream=None):
         """as2d_tree_attention; returns out (made like q unless given)."""
-        device = self._device()
-        current = self._current_stream(device)
-        if stream is None:
-            stream = current
-            if stream != self._made_on:
-                self._used_here()
+        device, current, stream = self._enter(stream)
         r = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
         shape = q.shape
         if out is None:
@@ -863,12 +857,7 @@ class Cache:
     def attention_weights(self, q, lse, weights, kv_len, rows, visible=None, layer=0, scale=None,
                           max_len=0, error_bits=None, stream=None):
         """as2d_attention_weights: adds to weights in place."""
-        device = self._device()
-        current = self._current_stream(device)
-        if stream is None:
-            stream = current
-            if stream != self._made_on:
-                self._used_here()
+        device, current, stream = self._enter(stream)
         r = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
         st = _lib.as2d_attention_weights(
             self._ref, layer, ctypes.byref(r), _address(lse, "lse", device, self._f32, q.shape[:2]),
@@ -880,16 +869,12 @@ class Cache:
 
     def evict(self, weights, kv_len, keep, recent=0, stream=None):
         """as2d_cache_evict: cuts the cache, weights and kv_len in place."""
-        device = self._device()
-        current = self._current_stream(device)
-        if stream is None:
-            stream = current
-            if stream != self._made_on:
-                self._used_here()
+        device, _, stream = self._enter(stream)
         st = _lib.as2d_cache_evict(
             self._ref, _address(weights, "weights", device, self._f32, self.shape[:4]),
             _address(kv_len, "kv_len", device, self._i32, self._per_request),
-            self._counts(keep, "keep"), _int32s((recent,), "recent")[0], self._workspace.data_ptr(), self._workspace.numel(), stream)
+            self._counts(keep, "keep"), _int32s((recent,), "recent")[0], self._workspace.data_ptr(),
+            self._workspace.numel(), stream)
         if st:
             _check(st, "as2d_cache_evict")
 
