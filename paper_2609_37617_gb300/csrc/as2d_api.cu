@@ -981,11 +981,10 @@ extern "C" as2d_status as2d_kv_evict(as2d_kv* kh, const int32_t* keep, int32_t r
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
   const bool eager = cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone;
   for (int b = 0; b < s.batch; ++b) {
-    const int64_t left = s.len_upper[b] > keep[b] ? keep[b] : s.len_upper[b];
-    if (eager)
-      s.len_upper[b] = s.floor_upper[b] = left;  // (the floor is keep[b], or what it was: no more than the length)
-    else if (keep[b] > s.floor_captured[b])
-      s.floor_captured[b] = keep[b];
+    // (the floor becomes keep[b], or stays what it was: no more than a length that keep[b] holds; it
+    // stays where the bound is no more than keep[b])
+    if (eager && s.len_upper[b] > keep[b]) s.len_upper[b] = s.floor_upper[b] = keep[b];
+    if (!eager && keep[b] > s.floor_captured[b]) s.floor_captured[b] = keep[b];
   }
   return AS2D_OK;
 }

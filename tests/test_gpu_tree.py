@@ -762,3 +762,19 @@ def test_sampled_drops_a_bad_token(pair):
         assert st.read_state() == ([L0, 51 + want[0][0]], [1, want[1][0]])
         assert torch.equal(w[:, 0], w0[:, 0]) and not torch.equal(w[:, 1, :, :50], w0[:, 1, :, :50])
         st.close()
+
+
+def test_a_rollback_after_an_eviction_of_nothing(pair):
+    """An eviction that is to keep more than there is sets no floor: the host's bound follows a
+    rollback below it, so that the capacity is there to be used again."""
+    cfg = pair.cfg
+    st = pair.state([L0], CAP, [5])
+    st.track_weights(torch.zeros(st.kc.shape[:4], device="cuda"))
+    st.evict([240], recent=4)
+    st.track_weights(None)
+    st.rollback([10], [7])
+    for _ in range(14):  # 14 calls of 17 rows at most: 248 places, where 56 are left behind L0
+        run_gpu_block(st, cfg, [[1] * 16], want_logits=False)
+    st.check()
+    assert 24 <= st.read_state()[0][0] <= 248
+    st.close()
