@@ -13,7 +13,7 @@ A cache in 4 bits holds for each 16 consecutive dims of an entry a scale s of on
 byte and 16 whole numbers c in -7 .. 7, and stands for s c.  The scale byte has five
 bits of exponent (bias 15, the lowest for subnormals) and three of fraction, and is
 that of the number nearest to a seventh of the largest magnitude of the 16, at most
-9216, ties to the even one; c is the whole number nearest to x / s, ties to the even
+896, ties to the even one; c is the whole number nearest to x / s, ties to the even
 one, and 0 where s is.  Codes are c + 8: of 8 dims in a 32-bit word, dim 2e is in
 bits 4e .. 4e + 3 and dim 2e + 1 in bits 4e + 16 .. 4e + 19.
 """
@@ -269,7 +269,7 @@ def _pack(x):
     t = blocks.abs().amax(-1) / torch.full((), 7.0, dtype=torch.float64, device=x.device)
     low = torch.full_like(t, -14)
     e = torch.where(t > 0, torch.maximum((torch.frexp(t).exponent - 1).double(), low), low)
-    s = torch.minimum(torch.round(t * torch.exp2(3 - e)) * torch.exp2(e - 3), torch.full_like(t, 9216.0))
+    s = torch.minimum(torch.round(t * torch.exp2(3 - e)) * torch.exp2(e - 3), torch.full_like(t, 896.0))
     c = torch.round(blocks / torch.where(s > 0, s, torch.ones_like(s))[..., None]).clamp_(-7, 7)
     c = torch.where((s > 0)[..., None], c, torch.zeros_like(c)).long().reshape(*x.shape[:-1], -1, 4, 2) + 8
     # four dims of a word's lower half, its even ones, then the odd ones
@@ -282,7 +282,7 @@ def _unpack(codes, scales):
     """The values that codes and scale bytes stand for, in 32 bits."""
     c = torch.stack((codes & 15, codes >> 4), -1).int().reshape(*codes.shape[:-1], -1, 2, 4) - 8
     c = c.transpose(-1, -2).reshape(*codes.shape[:-1], -1, 16)
-    s = (scales.to(torch.int16) << 7).view(torch.float16).float().clamp(max=9216.0)
+    s = (scales.to(torch.int16) << 7).view(torch.float16).float().clamp(max=896.0)
     return (c.float() * s[..., None]).flatten(-2)
 
 
@@ -384,7 +384,7 @@ def _cost(case):
 
 def _scale_table():
     """The value of each scale byte that is written, by the byte."""
-    byte = torch.arange(0xE2, device="cuda")
+    byte = torch.arange(0xC7, device="cuda")
     e, f = (byte >> 3).double(), (byte & 7).double()
     return torch.where(e > 0, torch.exp2(e - 15) * (1 + f / 8), torch.exp2(torch.full_like(f, -14)) * f / 8)
 
