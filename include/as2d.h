@@ -62,6 +62,8 @@ typedef int32_t as2d_status;
                                     its request                               */
 #define AS2D_DEVERR_NO_TOKEN 32  /* a row's probabilities gave no token (NaN
                                     logits, or none above -inf)               */
+#define AS2D_DEVERR_NOT_FINITE 64 /* NaN or an infinity was to be written into a
+                                    cache of 4 bits                           */
 
 /* Largest number of candidates per request in one call (the budget b of
    App. A.2; physical width K = k + 1 <= 17). */
@@ -659,6 +661,120 @@ as2d_status as2d_accept_sampled(const float* probs, const float* draft_probs,
                                 const int32_t* candidates, const int32_t* k, int32_t batch,
                                 int32_t vocab, const float* u, int32_t* n_accepted,
                                 int32_t* token, void* stream);
+
+/* ---- Between a projection and its attention ------------------------------------
+   The rows of a projection normed, rotated and appended to a cache; a cache held in
+   4 bits, written as rows are appended or from a cache in bf16, read back, and
+   attended to; attention of whole prompts.  As the operators above in all that
+   concerns streams, captures, workspaces and addresses. */
+
+/* A caller's cache in 4 bits, sizes as of as2d_cache.  k, v: device bytes
+   [n_layers][batch][n_kv][capacity][head_dim / 2], 16-byte aligned; k_scale, v_scale:
+   device bytes [n_layers][batch][n_kv][capacity][head_dim / 16], 8-byte aligned.
+     Each 16 consecutive dims of an entry share a scale s and stand for s (c - 8),
+   c their codes 0 .. 15.  A scale byte x has the 16-bit float x 2^7 as bits (five bits
+   of exponent, three of fraction), at most 896: greater ones, whatever their bits,
+   count as that.  Of 8 consecutive dims in a 32-bit little-endian word, dim 2e has
+   bits 4e .. 4e + 3 and dim 2e + 1 bits 4e + 16 .. 4e + 19.  So every value that a
+   cache can hold is finite and exact in bf16 and in 16-bit floats.
+     What writes: s is the nearest scale to a seventh of the largest magnitude of
+   the 16, ties to the even byte; c - 8 is the whole number nearest to x / s within
+   -7 .. 7, ties to the even one, and 0 where s is 0; both as in exact arithmetic.  A
+   value is off by at most s / 2, where s is neither capped nor below 2^-14.  NaN is written
+   as 0 and an infinity as the largest magnitude of its sign that the 16 can have
+   (s = 896). */
+typedef struct as2d_cache4 {
+  uint8_t *k, *k_scale, *v, *v_scale;
+  int32_t n_layers, batch, n_kv, capacity, head_dim;
+} as2d_cache4;
+
+/* Rows of a projection.  Request b has rows[b] >= 0 of them, packed request by
+   request, which become the entries [kv_len[b], kv_len[b] + rows[b]) of its cache.
+   q: device [sum rows][n_q][head_dim] of `type`, k and v: [sum rows][n_kv][head_dim];
+   row r at element r q_stride (k_stride, v_stride), so that they may be parts of
+   one tensor; addresses and strides in bytes are multiples of 16.
+   q_norm, k_norm: device float [head_dim] or NULL: each head of a row is divided by
+   its root mean square (mean of squares + eps; eps >= 0) and multiplied by these gains.
+   rotary: dims 0 .. rotary - 1 of each head of q and k are rotated by position, dim j
+   with dim j + rotary / 2 by the angle position theta^(-2j / rotary); a multiple of 16
+   of at most head_dim, 0 for none.  theta > 0.  positions: device int32 [sum
+   rows], or NULL: kv_len[b] + i for row i.  rows: host int32 [batch]; kv_len: device
+   int32 [batch]. */
+typedef struct as2d_new_rows {
+  const void *q, *k, *v;
+  int32_t type, n_q;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t* kv_len;
+  const int32_t* rows;
+  const int32_t* positions;
+  const float *q_norm, *k_norm;
+  float eps, theta;
+  int32_t rotary;
+} as2d_new_rows;
+
+/* Finish rows and append them to one layer of a cache: q_out (device [sum
+   rows][n_q][head_dim] of `type`, 16-byte aligned) gets the queries, normed and
+   rotated, the cache the keys, normed and rotated, and the values as they are.
+   Computed in 32 bits, angles exactly reduced for every position, and rounded once.
+   kv_len stays as it is.  A request whose kv_len[b] is negative or leaves no room
+   for its rows in the capacity is skipped: its cache and its rows of q_out stay as they
+   were and AS2D_DEVERR_CAPACITY is ORed into error_bits (device int32 [1] or
+   NULL).  q_out may not overlap q, k or v.  At most 2^24 rows. */
+as2d_status as2d_cache_append(const as2d_cache* cache, int32_t layer, const as2d_new_rows* rows,
+                              void* q_out, int32_t* error_bits, void* stream);
+
+/* The same into a cache in 4 bits: keys are rounded once, from their exact value.
+   AS2D_DEVERR_NOT_FINITE is ORed into error_bits where a key or value is NaN or
+   infinite. */
+as2d_status as2d_cache4_append(const as2d_cache4* cache, int32_t layer, const as2d_new_rows* rows,
+                               void* q_out, int32_t* error_bits, void* stream);
+
+/* Write entries [start[b], end[b]) of each request of a cache in bf16 into the
+   same places of one in 4 bits (as2d_cache4_write; flags AS2D_DEVERR_NOT_FINITE), or back
+   (as2d_cache4_read, exactly).  The caches have the same sizes but for the
+   capacities.  layer: one, or -1 for all.  start (NULL: 0), end: device int32
+   [batch].  A request with start[b] >= end[b] has nothing to do; one with start[b] < 0 or
+   end[b] past either capacity is skipped and flagged AS2D_DEVERR_CAPACITY.
+   max_entries: host bound of end[b] - start[b], by which the launch is sized (0: the
+   smaller capacity); results do not depend on it.  error_bits: device int32 [1] or
+   NULL. */
+as2d_status as2d_cache4_write(const as2d_cache4* to, const as2d_cache* from, int32_t layer,
+                              const int32_t* start, const int32_t* end, int32_t max_entries,
+                              int32_t* error_bits, void* stream);
+as2d_status as2d_cache4_read(const as2d_cache4* from, const as2d_cache* to, int32_t layer,
+                             const int32_t* start, const int32_t* end, int32_t max_entries,
+                             int32_t* error_bits, void* stream);
+
+/* Bytes of as2d_cache4_attention's workspace on the current device, whatever the
+   call. */
+as2d_status as2d_cache4_attention_workspace(const as2d_cache4* cache, int64_t* bytes);
+
+/* as2d_tree_attention over a cache in 4 bits, which holds the entries of the rows
+   too.  Queries enter the products in 16-bit floats with a power of two of their own,
+   32-bit ones as two parts (to 2^-22 of a query's largest dim, or nearer), and so do the
+   weights p (to 2^-11 for bf16 queries, 2^-22 for 32-bit ones).  What a row does not
+   see does not reach its result.  A query that is not finite, or a score of +inf, makes its
+   row NaN in out and lse. */
+as2d_status as2d_cache4_attention(const as2d_cache4* cache, int32_t layer,
+                                  const as2d_tree_rows* rows, void* out, float* lse,
+                                  void* workspace, int64_t workspace_bytes,
+                                  int32_t* error_bits, void* stream);
+
+/* Bytes of as2d_prompt_attention's workspace on the current device, whatever the
+   call. */
+as2d_status as2d_prompt_attention_workspace(const as2d_cache* cache, int64_t* bytes);
+
+/* Causal attention of whole prompts over one layer of a cache: as as2d_tree_attention
+   with rows[b] up to the capacity, row i of request b seeing the entries 0 ..
+   kv_len[b] + i; visible is NULL.  bf16 queries (others: AS2D_ERR_UNSUPPORTED); the
+   weights p enter the products in bf16, their sum in 32 bits.  What a row does not see does
+   not reach its result, whatever it holds; a value that it sees and that is not
+   finite makes its dim not finite, and NaN or +inf among its scores the row NaN in out
+   and lse.  At most 2^24 rows. */
+as2d_status as2d_prompt_attention(const as2d_cache* cache, int32_t layer,
+                                  const as2d_tree_rows* rows, void* out, float* lse,
+                                  void* workspace, int64_t workspace_bytes,
+                                  int32_t* error_bits, void* stream);
 
 /* ---- The same on a verification state ------------------------------------------ */
 

@@ -32,6 +32,7 @@ AS2D_DEVERR_TIMEOUT = 4
 AS2D_DEVERR_CAPACITY = 8
 AS2D_DEVERR_BAD_TREE = 16
 AS2D_DEVERR_NO_TOKEN = 32
+AS2D_DEVERR_NOT_FINITE = 64
 AS2D_CBUF_BATCH = 8
 CBUF_MODES = {0: "normal", 1: "realign", 2: "alone"}
 AS2D_MAX_K = 16
@@ -54,7 +55,9 @@ EXPORTED = ("as2d_model_load", "as2d_kv_init_prefilled", "as2d_verify_block",
             "as2d_tree_attention_workspace", "as2d_tree_attention", "as2d_attention_weights",
             "as2d_cache_evict_workspace", "as2d_cache_evict", "as2d_token_probs",
             "as2d_accept_sampled", "as2d_verify_tree", "as2d_verify_sampled",
-            "as2d_kv_track_weights", "as2d_kv_evict")
+            "as2d_kv_track_weights", "as2d_kv_evict", "as2d_cache_append", "as2d_cache4_append",
+            "as2d_cache4_write", "as2d_cache4_read", "as2d_cache4_attention_workspace",
+            "as2d_cache4_attention", "as2d_prompt_attention_workspace", "as2d_prompt_attention")
 KERNEL_CLASSES = {"qkv": 0, "attention": 1, "o": 2, "gate_up": 3, "down": 4,
                   "lm_head": 5, "other": 6}
 
@@ -95,6 +98,21 @@ class as2d_tree_rows(ctypes.Structure):
                 ("q_stride", ctypes.c_int64), ("kv_len", ctypes.c_void_p),
                 ("max_len", ctypes.c_int32), ("rows", ctypes.c_void_p),
                 ("visible", ctypes.c_void_p), ("scale", ctypes.c_float)]
+
+
+class as2d_cache4(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "k_scale", "v", "v_scale")] + \
+               [(n, ctypes.c_int32) for n in ("n_layers", "batch", "n_kv", "capacity", "head_dim")]
+
+
+class as2d_new_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("type", ctypes.c_int32), ("n_q", ctypes.c_int32), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("kv_len", ctypes.c_void_p), ("rows", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("q_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float), ("theta", ctypes.c_float),
+                ("rotary", ctypes.c_int32)]
 
 
 class as2d_session_spec(ctypes.Structure):
@@ -189,6 +207,15 @@ _lib.as2d_tree_attention.argtypes = [_CACHE, _S, _ROWS, _P, _P, _P, _I64, _P, _P
 _lib.as2d_attention_weights.argtypes = [_CACHE, _S, _ROWS, _P, _P, _P, _P]
 _lib.as2d_cache_evict_workspace.argtypes = [_CACHE, ctypes.POINTER(_I64)]
 _lib.as2d_cache_evict.argtypes = [_CACHE, _P, _P, _P, _S, _P, _I64, _P]
+_CACHE4, _NEW = ctypes.POINTER(as2d_cache4), ctypes.POINTER(as2d_new_rows)
+_lib.as2d_cache_append.argtypes = [_CACHE, _S, _NEW, _P, _P, _P]
+_lib.as2d_cache4_append.argtypes = [_CACHE4, _S, _NEW, _P, _P, _P]
+_lib.as2d_cache4_write.argtypes = [_CACHE4, _CACHE, _S, _P, _P, _S, _P, _P]
+_lib.as2d_cache4_read.argtypes = [_CACHE4, _CACHE, _S, _P, _P, _S, _P, _P]
+_lib.as2d_cache4_attention_workspace.argtypes = [_CACHE4, ctypes.POINTER(_I64)]
+_lib.as2d_cache4_attention.argtypes = [_CACHE4, _S, _ROWS, _P, _P, _P, _I64, _P, _P]
+_lib.as2d_prompt_attention_workspace.argtypes = [_CACHE, ctypes.POINTER(_I64)]
+_lib.as2d_prompt_attention.argtypes = [_CACHE, _S, _ROWS, _P, _P, _P, _I64, _P, _P]
 _lib.as2d_token_probs.argtypes = [_P, _S, _S, ctypes.c_float, _P, _P]
 _lib.as2d_accept_sampled.argtypes = [_P, _P, _P, _P, _S, _S, _P, _P, _P, _P]
 _lib.as2d_verify_tree.argtypes = [_P, _P, _P, _P, ctypes.POINTER(as2d_verify_out), _P, _P]
@@ -199,7 +226,9 @@ _lib.as2d_kv_evict.argtypes = [_P, _P, _S, _P]
 for _n in ("as2d_verify_tree", "as2d_verify_sampled", "as2d_kv_track_weights", "as2d_kv_evict",
            "as2d_tree_attention_workspace", "as2d_tree_attention", "as2d_attention_weights",
            "as2d_cache_evict_workspace", "as2d_cache_evict", "as2d_token_probs",
-           "as2d_accept_sampled"):
+           "as2d_accept_sampled", "as2d_cache_append", "as2d_cache4_append", "as2d_cache4_write",
+           "as2d_cache4_read", "as2d_cache4_attention_workspace", "as2d_cache4_attention",
+           "as2d_prompt_attention_workspace", "as2d_prompt_attention"):
     getattr(_lib, _n).restype = _S
 _lib.as2d_last_error.argtypes = []
 _lib.as2d_last_error.restype = ctypes.c_char_p
@@ -761,36 +790,22 @@ def _address(t, name, device, dtype, shape):
     return _tensor(t, name, device, (dtype,), shape)
 
 
-class Cache:
-    """A key/value cache of the caller's (two bf16 tensors [n_layers][batch][n_kv]
-    [capacity][head_dim], kept alive here) with the workspace of the operators
-    on it; see include/as2d.h, "Operators on caches and logits".  Calls on one
-    Cache share the workspace, so calls that may overlap on the GPU (several
-    streams, captured graphs) need a Cache each.  A Cache outlives the captured
-    graphs that hold its calls, and calls enqueued on a stream that was given by
-    its handle; those on torch's current stream may still run when it goes."""
+class _CacheCalls:
+    """What the caches below share: checks of a call's arguments, the workspace and its stream."""
 
-    def __init__(self, k, v):
+    def _set_up(self, c, shape, device, k):
         import torch
+        self._c, self.shape, self._on = c, shape, device
         self._current = torch.cuda.current_device
-        device = self._on = self._current()
-        kp = _tensor(k, "k", device, (torch.bfloat16,))
-        if k.dim() != 5:
-            raise ValueError("k must have shape [n_layers, batch, n_kv, capacity, head_dim]")
-        vp = _tensor(v, "v", device, (torch.bfloat16,), k.shape)
-        self.k, self.v, self.shape = k, v, tuple(k.shape)
-        self._c = as2d_cache(kp, vp, *self.shape)
         self._ref = ctypes.byref(self._c)
-        self._per_request = self.shape[1:2]
+        self._per_request = shape[1:2]
         self._bf16, self._f32, self._i32, self._i64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
         self._mask = (torch.int64, torch.uint64)
-        need = _I64()
-        _check(_lib.as2d_tree_attention_workspace(self._ref, ctypes.byref(need)),
-               "as2d_tree_attention_workspace")
-        most = need.value
-        _check(_lib.as2d_cache_evict_workspace(self._ref, ctypes.byref(need)),
-               "as2d_cache_evict_workspace")
-        self._workspace = torch.empty(max(most, need.value), dtype=torch.uint8, device=k.device)
+        most, need = 0, _I64()
+        for name in self._WORKSPACES:
+            _check(getattr(_lib, name)(self._ref, ctypes.byref(need)), name)
+            most = max(most, need.value)
+        self._workspace = torch.empty(most, dtype=torch.uint8, device=k.device)
         self._current_stream = _stream_reader(torch)
         self._made_on = self._current_stream(device)
 
@@ -836,23 +851,103 @@ class Cache:
         r.keep = host_rows  # alive as long as the descriptor
         return r
 
-    def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
-                       lse=None, error_bits=None, stream=None):
-        """as2d_tree_attention; returns out (made like q unless given)."""
+    def _attention(self, name, q, kv_len, rows, visible, scale, layer, max_len, out, lse, error_bits, stream):
         device, current, stream = self._enter(stream)
         r = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
         shape = q.shape
         if out is None:
             out = q.new_empty(shape) if stream == current else _new_on(stream, device, q, shape)
-        st = _lib.as2d_tree_attention(
+        st = getattr(_lib, name)(
             self._ref, layer, ctypes.byref(r), _address(out, "out", device, q.dtype, shape),
             None if lse is None else _address(lse, "lse", device, self._f32, shape[:2]),
             self._workspace.data_ptr(), self._workspace.numel(),
             None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)),
             stream)
         if st:
-            _check(st, "as2d_tree_attention")
+            _check(st, name)
         return out
+
+    def _append(self, name, q, k, v, kv_len, rows, layer, positions, q_norm, k_norm, eps, theta, rotary,
+                out, error_bits, stream):
+        device, current, stream = self._enter(stream)
+        n_kv, d = self.shape[2], self.shape[4]
+        if abs(layer) >> 31:
+            raise ValueError("layer must be of 32 bits")
+        dtype, shape = q.dtype, q.shape
+        n_q = shape[1] if len(shape) == 3 else 0
+        at = [_tensor(q, "q", device, (self._bf16, self._f32), None, False)]
+        if n_q == 0 or shape[2] != d:
+            raise ValueError(f"q must be [rows, n_q, {d}]")
+        n = shape[0]
+        for t, its_name in ((k, "k"), (v, "v")):
+            at.append(_tensor(t, its_name, device, (dtype,), (n, n_kv, d), False))
+        for t, its_name in ((q, "q"), (k, "k"), (v, "v")):
+            if t.stride()[1:] != (d, 1):
+                raise ValueError(f"{its_name} must have contiguous rows")
+        host_rows = self._counts(rows, "rows")
+        if n != sum(rows):
+            raise ValueError("q must have as many rows as the requests together")
+        gains = [None if t is None else _address(t, its_name, device, self._f32, (d,))
+                 for t, its_name in ((q_norm, "q_norm"), (k_norm, "k_norm"))]
+        rotary = d if rotary is None else _int32s((rotary,), "rotary")[0]
+        # (the stride of a single row is not looked at)
+        strides = [t.stride(0) if n > 1 else t.shape[1] * d for t in (q, k, v)]
+        r = as2d_new_rows(
+            *at, AS2D_TYPE_BF16 if dtype is self._bf16 else AS2D_TYPE_F32, n_q, *strides,
+            _address(kv_len, "kv_len", device, self._i32, self._per_request), ctypes.addressof(host_rows),
+            None if positions is None else _address(positions, "positions", device, self._i32, (n,)),
+            *gains, eps, theta, rotary)
+        if out is None:
+            out = q.new_empty(shape) if stream == current else _new_on(stream, device, q, shape)
+        st = getattr(_lib, name)(
+            self._ref, layer, ctypes.byref(r), _address(out, "out", device, dtype, shape),
+            None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)), stream)
+        if st:
+            _check(st, name)
+        return out
+
+
+class Cache(_CacheCalls):
+    """A key/value cache of the caller's (two bf16 tensors [n_layers][batch][n_kv]
+    [capacity][head_dim], kept alive here) with the workspace of the operators
+    on it; see include/as2d.h, "Operators on caches and logits".  Calls on one
+    Cache share the workspace, so calls that may overlap on the GPU (several
+    streams, captured graphs) need a Cache each.  A Cache outlives the captured
+    graphs that hold its calls, and calls enqueued on a stream that was given by
+    its handle; those on torch's current stream may still run when it goes."""
+
+    _WORKSPACES = ("as2d_tree_attention_workspace", "as2d_cache_evict_workspace",
+                   "as2d_prompt_attention_workspace")
+
+    def __init__(self, k, v):
+        import torch
+        device = torch.cuda.current_device()
+        kp = _tensor(k, "k", device, (torch.bfloat16,))
+        if k.dim() != 5:
+            raise ValueError("k must have shape [n_layers, batch, n_kv, capacity, head_dim]")
+        vp = _tensor(v, "v", device, (torch.bfloat16,), k.shape)
+        self.k, self.v = k, v
+        self._set_up(as2d_cache(kp, vp, *k.shape), tuple(k.shape), device, k)
+
+    def append(self, q, k, v, kv_len, rows, layer=0, positions=None, q_norm=None, k_norm=None, eps=1e-6,
+               theta=1e6, rotary=None, out=None, error_bits=None, stream=None):
+        """as2d_cache_append: q [rows, n_q, head_dim], k and v [rows, n_kv, head_dim]
+        (parts of one tensor, if need be); rotary: the rotated dims (head_dim unless
+        given).  Returns out, the queries (made like q unless given)."""
+        return self._append("as2d_cache_append", q, k, v, kv_len, rows, layer, positions, q_norm, k_norm,
+                            eps, theta, rotary, out, error_bits, stream)
+
+    def prompt_attention(self, q, kv_len, rows, layer=0, scale=None, max_len=0, out=None, lse=None,
+                         error_bits=None, stream=None):
+        """as2d_prompt_attention; returns out (made like q unless given)."""
+        return self._attention("as2d_prompt_attention", q, kv_len, rows, None, scale, layer, max_len, out, lse,
+                               error_bits, stream)
+
+    def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
+                       lse=None, error_bits=None, stream=None):
+        """as2d_tree_attention; returns out (made like q unless given)."""
+        return self._attention("as2d_tree_attention", q, kv_len, rows, visible, scale, layer, max_len, out, lse,
+                               error_bits, stream)
 
     def attention_weights(self, q, lse, weights, kv_len, rows, visible=None, layer=0, scale=None,
                           max_len=0, error_bits=None, stream=None):
@@ -877,6 +972,65 @@ class Cache:
             self._workspace.numel(), stream)
         if st:
             _check(st, "as2d_cache_evict")
+
+
+class Cache4(_CacheCalls):
+    """A key/value cache of the caller's in 4 bits (uint8 tensors k and v [n_layers][batch]
+    [n_kv][capacity][head_dim / 2], k_scale and v_scale [..][head_dim / 16], kept alive
+    here; as2d_cache4 in include/as2d.h has the format).  As Cache in what concerns
+    streams and the workspace."""
+
+    _WORKSPACES = ("as2d_cache4_attention_workspace",)
+
+    def __init__(self, k, k_scale, v, v_scale):
+        import torch
+        device, u8 = torch.cuda.current_device(), (torch.uint8,)
+        at = [_tensor(k, "k", device, u8)]
+        if k.dim() != 5:
+            raise ValueError("k must have shape [n_layers, batch, n_kv, capacity, head_dim / 2]")
+        d = 2 * k.shape[4]
+        scales = (*k.shape[:4], d // 16)
+        for t, name, shape in ((k_scale, "k_scale", scales), (v, "v", k.shape), (v_scale, "v_scale", scales)):
+            at.append(_tensor(t, name, device, u8, shape))
+        self.k, self.k_scale, self.v, self.v_scale = k, k_scale, v, v_scale
+        shape = (*k.shape[:4], d)
+        self._set_up(as2d_cache4(*at, *shape), shape, device, k)
+
+    def append(self, q, k, v, kv_len, rows, layer=0, positions=None, q_norm=None, k_norm=None, eps=1e-6,
+               theta=1e6, rotary=None, out=None, error_bits=None, stream=None):
+        """as2d_cache4_append; arguments as Cache.append."""
+        return self._append("as2d_cache4_append", q, k, v, kv_len, rows, layer, positions, q_norm, k_norm,
+                            eps, theta, rotary, out, error_bits, stream)
+
+    def _convert(self, name, cache, end, start, layer, max_entries, error_bits, stream):
+        device, _, stream = self._enter(stream)
+        if not isinstance(cache, Cache):
+            raise TypeError("cache must be a Cache")
+        if cache._on != device:
+            raise ValueError("both caches must be on the current CUDA device")
+        layer, max_entries = _int32s((-1 if layer is None else layer, max_entries), "layer and max_entries")
+        st = getattr(_lib, name)(
+            self._ref, cache._ref, layer,
+            None if start is None else _address(start, "start", device, self._i32, self._per_request),
+            _address(end, "end", device, self._i32, self._per_request), max_entries,
+            None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)), stream)
+        if st:
+            _check(st, name)
+
+    def write(self, cache, end, start=None, layer=None, max_entries=0, error_bits=None, stream=None):
+        """as2d_cache4_write: entries [start, end) (int32 [batch], start 0 unless given) of
+        a Cache into this one; every layer unless one is given."""
+        self._convert("as2d_cache4_write", cache, end, start, layer, max_entries, error_bits, stream)
+
+    def read(self, cache, end, start=None, layer=None, max_entries=0, error_bits=None, stream=None):
+        """as2d_cache4_read: entries [start, end) of this cache into a Cache."""
+        self._convert("as2d_cache4_read", cache, end, start, layer, max_entries, error_bits, stream)
+
+    def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
+                       lse=None, error_bits=None, stream=None):
+        """as2d_cache4_attention; returns out (made like q unless given)."""
+        return self._attention("as2d_cache4_attention", q, kv_len, rows, visible, scale, layer, max_len, out,
+                               lse, error_bits, stream)
 
 
 def token_probs(logits, temperature, out=None, stream=None):

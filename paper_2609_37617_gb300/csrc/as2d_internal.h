@@ -64,6 +64,7 @@ enum : int32_t {
   kErrCapacity = AS2D_DEVERR_CAPACITY,
   kErrBadTree = AS2D_DEVERR_BAD_TREE,
   kErrNoToken = AS2D_DEVERR_NO_TOKEN,
+  kErrNotFinite = AS2D_DEVERR_NOT_FINITE,
 };
 
 // Whether a request of device-side length `len` has room for `rows` more

@@ -1,0 +1,555 @@
+// k_attn4.cu -- attention of a tree of drafted tokens over a cache in 4 bits
+// (as2d_cache4_attention).
+//
+// With s_t = scale q k_t over the entries that a row sees (as k_tree_attn.cu):
+//   m = max s_t, l = sum e^(s_t - m), out = sum e^(s_t - m) v_t / l, lse = m + ln l.
+#include <algorithm>
+
+#include "cache4.cuh"
+#include "ptx_sm100.cuh"
+#include "tree_dev.cuh"
+
+namespace as2d {
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+// P may grow to 2^kLazy of its reference before sums are rescaled; a reference stands for 2^kUp
+// (the weights, at most 2^(kLazy + kUp), use the range of 16-bit floats).
+constexpr float kLazy = 8.f, kUp = 7.f;
+
+enum Mode : int { kShares = 0, kWhole = 1 };
+
+struct Work {
+  float2* o;   // [2 CTAs][pairs of dims][32 lanes]
+  float2* ml;  // [2 CTAs][queries] (reference base 2, sum)
+};
+
+template <int D, int NT, bool F32>
+struct Shape {
+  static constexpr int Q = 8 * NT;                         // queries of a tile
+  static constexpr int CODES = 16 * D / 2, SCALES = D;     // bytes of a warp's 16 keys (or values)
+  static constexpr int STAGE = 2 * (CODES + SCALES);
+  static constexpr int NST = NT == 1 && !F32 ? 5 : 8;
+  static constexpr int RING = kWarps * NST * STAGE;
+  static constexpr int PAIRS = D / 16 * NT * 2;            // of dims, a lane
+  static constexpr int PARTS = kWarps * (PAIRS * 32 * 8 + Q * 8);
+  static constexpr int SMEM = RING > PARTS ? RING : PARTS;
+};
+
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {  // 8 x 8 of 16 bits
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t halves(float a, float b) {
+  const __half2 t = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ uint32_t as_u32(__half2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+
+template <int N>
+__device__ __forceinline__ void cp_async(void* dst, const void* src) {
+  if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(dst)), "l"(__cvta_generic_to_global(src)) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(ptx::smem_u32(dst)), "l"(__cvta_generic_to_global(src)), "n"(N) : "memory");
+}
+
+// A value's 16-byte pieces: those that lanes of one g read together (rows 4t) lie in other banks.
+__device__ __forceinline__ int value_off(int off, int row) { return off ^ (((row >> 2) & 3) << 5); }
+
+// A warp's 16 keys and values from entry p on into a stage; entries from `end` on are
+// copies of the last one (and masked).
+template <int D>
+__device__ __forceinline__ void load_slice(const Tree4Args& a, size_t head, int p, int end, int lane, uint8_t* to) {
+  constexpr int ROW = D / 2, PIECES = ROW / 16, CODES = 16 * ROW, S = D / 16;
+#pragma unroll
+  for (int i = 0; i < PIECES / 2; ++i) {
+    const int x = lane + 32 * i, row = x / PIECES, off = row * ROW + x % PIECES * 16;
+    const size_t at = (head + min(p + row, end - 1)) * ROW + x % PIECES * 16;
+    cp_async<16>(to + off, a.k + at);
+    cp_async<16>(to + CODES + value_off(off, row), a.v + at);
+  }
+  const int row = lane & 15;
+  const size_t at = (head + min(p + row, end - 1)) * S;
+  cp_async<S>(to + 2 * CODES + lane * S, (lane < 16 ? a.ks : a.vs) + at);
+}
+
+// A query tile's operands: lane (g, t) has dims D / 4 t .. of query 8 nt + g, as halves times a
+// power of two of the query's own, which brings its largest dim to 2^14 .. 2^15; back: what scores
+// are to be multiplied by, of queries 8 nt + 2 t and + 1.
+template <int D, int NT, bool F32>
+__device__ __forceinline__ void load_queries4(const TreeArgs& a, const Unit& it, int lane, uint32_t (&hi)[NT][D / 8],
+                                              uint32_t (&lo)[F32 ? NT : 1][D / 8], float (&back)[NT][2]) {
+  const int g = lane >> 2, t = lane & 3, G = a.nq / a.nkv, n = it.rows * G;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int q = it.qt * 8 * NT + 8 * nt + g;
+    float x[D / 4];
+#pragma unroll
+    for (int e = 0; e < D / 4; ++e) x[e] = 0.f;
+    if (q < n) {
+      const int i = divide_group(a, q), h = it.g * G + (q - i * G);
+      const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + D / 4 * t;
+      if constexpr (F32) {
+#pragma unroll
+        for (int e = 0; e < D / 4; e += 4) {
+          const float4 v = *reinterpret_cast<const float4*>((const float*)a.q + at + e);
+          x[e] = v.x, x[e + 1] = v.y, x[e + 2] = v.z, x[e + 3] = v.w;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < D / 4; e += 8) {
+          const uint4 v = *reinterpret_cast<const uint4*>((const bf16*)a.q + at + e);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            x[e + 2 * f] = __uint_as_float(w[f] << 16);
+            x[e + 2 * f + 1] = __uint_as_float(w[f] & 0xFFFF0000u);
+          }
+        }
+      }
+    }
+    float most = 0.f, zero = 0.f;  // 0 times every dim: NaN if one is not finite
+#pragma unroll
+    for (int e = 0; e < D / 4; ++e) {
+      most = fmaxf(most, fabsf(x[e]));
+      zero = fmaf(x[e], 0.f, zero);
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+      zero += __shfl_xor_sync(~0u, zero, o);
+    }
+    // 2^up in two factors, as up may be 163
+    const int up = most > 0.f && zero == 0.f ? 14 - ilogbf(most) : 0;
+    const int u0 = up / 2, u1 = up - u0;
+    const float f0 = __uint_as_float((uint32_t)(127 + u0) << 23), f1 = __uint_as_float((uint32_t)(127 + u1) << 23);
+#pragma unroll
+    for (int e = 0; e < D / 8; ++e) {
+      const float y0 = x[2 * e] * f0 * f1 + zero, y1 = x[2 * e + 1] * f0 * f1 + zero;
+      hi[nt][e] = halves(y0, y1);
+      if constexpr (F32) {
+        const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&hi[nt][e]));
+        lo[nt][e] = halves(y0 - r.x, y1 - r.y);
+      }
+    }
+    const float b = fminf(a.scale_log2 * __uint_as_float((uint32_t)(127 - u0) << 23) *
+                              __uint_as_float((uint32_t)(127 - u1) << 23), 3.4e38f);
+    back[nt][0] = __shfl_sync(~0u, b, 8 * t);
+    back[nt][1] = __shfl_sync(~0u, b, 8 * t + 4);
+  }
+}
+
+// What a warp has of its queries: maxima (references, base 2) and sums of queries 8 nt + 2 t and + 1 (a
+// lane's keys), and its dims of the accumulator.
+template <int D, int NT>
+struct Sums {
+  float m[NT][2], l[NT][2];
+  float o[NT][D / 16][4];
+};
+
+// 16 keys of a stage, from entry p on.
+template <int D, int NT, bool F32>
+__device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const uint8_t* st, int p, int lane,
+                                       const uint32_t (&qh)[NT][D / 8], const uint32_t (&ql)[F32 ? NT : 1][D / 8],
+                                       const float (&back)[NT][2], Sums<D, NT>& x) {
+  constexpr int ROW = D / 2, CODES = 16 * ROW, S = D / 16;
+  const int g = lane >> 2, t = lane & 3;
+  // ---- scores: the rows g and g + 8 of the product are keys k0 and k0 + 2 of the 16 ----
+  const int k0 = 4 * (g >> 1) + (g & 1);
+  float s[NT][4];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+  uint32_t w[2][D / 32], sb[2];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const uint8_t* row = st + (k0 + 2 * r) * ROW + t * (ROW / 4);
+    const uint8_t* sc = st + 2 * CODES + (k0 + 2 * r) * S;
+    if constexpr (D == 128) {
+      const uint4 v = *reinterpret_cast<const uint4*>(row);
+      w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
+      sb[r] = *reinterpret_cast<const uint16_t*>(sc + 2 * t);
+    } else {
+      const uint2 v = *reinterpret_cast<const uint2*>(row);
+      w[r][0] = v.x, w[r][1] = v.y;
+      sb[r] = sc[t];
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < D / 64; ++b) {  // 16 dims of a lane, a scale
+    __half2 sc[2], sh[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      sc[r] = scale_pair(((sb[r] >> (8 * b)) & 255u) * 0x10001u);
+      sh[r] = scale_shift(sc[r]);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      __half2 v0[4], v1[4];
+      decode_word(w[0][2 * b + c], sc[0], sh[0], v0);
+      decode_word(w[1][2 * b + c], sc[1], sh[1], v1);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t f[4] = {as_u32(v0[2 * k]), as_u32(v1[2 * k]), as_u32(v0[2 * k + 1]), as_u32(v1[2 * k + 1])};
+        const int at = 8 * b + 4 * c + 2 * k;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma16(s[nt], f, qh[nt][at], qh[nt][at + 1]);
+          if constexpr (F32) mma16(s[nt], f, ql[nt][at], ql[nt][at + 1]);
+        }
+      }
+    }
+  }
+  // ---- weights ----
+  // (s[.][2 r + e]: key k0 + 2 r, query 8 nt + 2 t + e)
+  bool grow = false;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[nt][e] *= back[nt][e & 1];
+  if (p + 16 > it.L) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int q = it.qt * 8 * NT + 8 * nt + 2 * t + e, i = min(divide_group(a, q), it.rows - 1);
+        const uint64_t vis = visible_rows(a, it.r0 + i, i, it.rows);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int rel = p + k0 + 2 * r - it.L;
+          if (rel >= 0 && (rel >= it.rows || !((vis >> rel) & 1))) s[nt][2 * r + e] = -INFINITY;
+        }
+      }
+  }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) grow = grow || fmaxf(s[nt][e], s[nt][2 + e]) > x.m[nt][e] + kLazy;
+  if (__any_sync(~0u, grow)) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float most = fmaxf(s[nt][e], s[nt][2 + e]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+        const float m = x.m[nt][e];
+        if (most > m + kLazy) {
+          const float f = m == -INFINITY ? 0.f : ex2(m - most);
+          x.m[nt][e] = most;
+          x.l[nt][e] *= f;
+#pragma unroll
+          for (int mt = 0; mt < D / 16; ++mt) {
+            x.o[nt][mt][e] *= f;
+            x.o[nt][mt][2 + e] *= f;
+          }
+        }
+      }
+  }
+  uint32_t ph[NT][2], pl[F32 ? NT : 1][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float w4[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float m = x.m[nt][e & 1];
+      w4[e] = ex2(s[nt][e] - ((m == -INFINITY ? 0.f : m) - kUp));
+    }
+    x.l[nt][0] += w4[0] + w4[2];
+    x.l[nt][1] += w4[1] + w4[3];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const uint32_t h = halves(w4[2 * r], w4[2 * r + 1]);
+      ph[nt][r] = transposed(h);
+      if constexpr (F32) {
+        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        pl[nt][r] = transposed(halves(w4[2 * r] - y.x, w4[2 * r + 1] - y.y));
+      }
+    }
+  }
+  // ---- accumulators: rows g and g + 8 of the products are dims D / 8 g + 2 mt and + 1 ----
+  uint32_t vw[4][D / 64], vb[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = 4 * t + r;
+    const uint8_t* at = st + CODES + value_off(row * ROW + g * (D / 16), row);
+    if constexpr (D == 128) {
+      const uint2 v = *reinterpret_cast<const uint2*>(at);
+      vw[r][0] = v.x, vw[r][1] = v.y;
+    } else {
+      vw[r][0] = *reinterpret_cast<const uint32_t*>(at);
+    }
+    vb[r] = st[2 * CODES + 16 * S + row * S + (D == 128 ? g : g >> 1)];
+  }
+  const __half2 s0 = scale_pair(vb[0] | vb[1] << 16), s1 = scale_pair(vb[2] | vb[3] << 16);
+  const __half2 h0 = scale_shift(s0), h1 = scale_shift(s1);
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    __half2 v[4][4];  // keys 0 and 1: even dims, odd dims; keys 2 and 3
+    decode_word(__byte_perm(vw[0][c], vw[1][c], 0x5410), s0, h0, v[0]);
+    decode_word(__byte_perm(vw[0][c], vw[1][c], 0x7632), s0, h0, v[1]);
+    decode_word(__byte_perm(vw[2][c], vw[3][c], 0x5410), s1, h1, v[2]);
+    decode_word(__byte_perm(vw[2][c], vw[3][c], 0x7632), s1, h1, v[3]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t f[4] = {as_u32(v[0][e]), as_u32(v[1][e]), as_u32(v[2][e]), as_u32(v[3][e])};
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        mma16(x.o[nt][4 * c + e], f, ph[nt][0], ph[nt][1]);
+        if constexpr (F32) mma16(x.o[nt][4 * c + e], f, pl[nt][0], pl[nt][1]);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ float part_weight(float m, float M) {
+  return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
+}
+
+// Two dims of a query: 32-bit or bf16.
+template <bool F32>
+__device__ __forceinline__ void write_pair(const TreeArgs& a, float2 x, size_t at) {
+  if constexpr (F32)
+    *reinterpret_cast<float2*>((float*)a.out + at) = x;
+  else
+    *reinterpret_cast<uint32_t*>((bf16*)a.out + at) = pack2(x.x, x.y);
+}
+
+// Result of a lane's pair of dims (as Sums): its query of the tile and first dim.
+template <int D>
+__device__ __forceinline__ void place_of(int pair, int lane, int& query, int& dim) {
+  const int e = pair & 1, mt = (pair >> 1) % (D / 16), nt = (pair >> 1) / (D / 16);
+  query = 8 * nt + 2 * (lane & 3) + e;
+  dim = (lane >> 2) * (D / 8) + 2 * mt;
+}
+
+template <int D, int NT, bool F32>
+__global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
+    attn4_kernel(const __grid_constant__ Tree4Args a4, Work ws, int mode, int turn) {
+  using S = Shape<D, NT, F32>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ UnitPlan s_plan;
+  __shared__ First s_first;
+  const TreeArgs& a = a4.t;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint8_t* ring = smem + warp * S::NST * S::STAGE;
+  float2* s_o = reinterpret_cast<float2*>(smem);                                  // [warp][pair][lane]
+  float2* s_ml = reinterpret_cast<float2*>(smem + kWarps * S::PAIRS * 32 * 8);    // [warp][query]
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  Unit it;
+  int u1 = 0;
+  if (mode == kWhole) {
+    it.b = blockIdx.z, it.g = blockIdx.y, it.qt = blockIdx.x;
+    it.r0 = a.rm.start[it.b];
+    it.rows = a.rm.start[it.b + 1] - it.r0;
+    it.L = a.len[it.b];
+    const bool some = it.qt * S::Q < it.rows * (a.nq / a.nkv), fits = rows_fit(it.L, it.rows, a.cap);
+    if (some && !fits && tid == 0 && a.err) atomicOr(a.err, kErrCapacity);
+    it.tiles = some && fits ? (it.L + it.rows + 127) / 128 : 0;
+    it.t0 = 0;
+    it.t1 = it.tiles;
+    if (it.tiles == 0) return;
+  } else {
+    if (warp == 0) {
+      make_plan(a, S::Q, turn, lane, s_plan, blockIdx.x == 0);
+      first_item(s_plan, a, blockIdx.x, gridDim.x, lane, s_first);
+    }
+    __syncthreads();
+    it = s_first.it, u1 = s_first.u1;
+    if (it.rows == 0) return;
+  }
+  const int G = a.nq / a.nkv;
+  for (bool more = true; more;) {
+    const int end = it.L + it.rows, n = it.t1 - it.t0;
+    const size_t head = ((size_t)it.b * a.nkv + it.g) * a.cap;
+    auto load = [&](int k) {
+      if (k < n) load_slice<D>(a4, head, (it.t0 + k) * 128 + 16 * warp, end, lane, ring + k % S::NST * S::STAGE);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll 1
+    for (int k = 0; k < S::NST - 1; ++k) load(k);
+    uint32_t qh[NT][D / 8], ql[F32 ? NT : 1][D / 8];
+    float back[NT][2];
+    load_queries4<D, NT, F32>(a, it, lane, qh, ql, back);
+    Sums<D, NT> x;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      x.m[nt][0] = x.m[nt][1] = -INFINITY;
+      x.l[nt][0] = x.l[nt][1] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.o[nt][mt][e] = 0.f;
+    }
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::NST - 2) : "memory");
+      __syncwarp();
+      const int p = (it.t0 + k) * 128 + 16 * warp;
+      if (p < end) attend<D, NT, F32>(a, it, ring + k % S::NST * S::STAGE, p, lane, qh, ql, back, x);
+      __syncwarp();
+      load(k + S::NST - 1);
+    }
+    // ---- the warps' parts, over the rings ----
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) x.l[nt][e] += __shfl_xor_sync(~0u, x.l[nt][e], o);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int mt = 0; mt < D / 16; ++mt)
+          s_o[(warp * S::PAIRS + (nt * (D / 16) + mt) * 2 + e) * 32 + lane] = make_float2(x.o[nt][mt][e], x.o[nt][mt][2 + e]);
+        if (lane < 4) s_ml[warp * S::Q + 8 * nt + 2 * lane + e] = make_float2(x.m[nt][e], x.l[nt][e]);
+      }
+    __syncthreads();
+    const bool done = it.t0 == 0 && it.t1 == it.tiles;
+    const size_t part = (size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1);
+    for (int j = tid; j < S::PAIRS * 32; j += kThreads) {
+      int query, dim;
+      place_of<D>(j / 32, lane, query, dim);
+      const int q = it.qt * S::Q + query;
+      if (q >= it.rows * G) continue;
+      float M = -INFINITY, l = 0.f;
+      float2 o = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_ml[w * S::Q + query].x);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 ml = s_ml[w * S::Q + query], v = s_o[w * S::PAIRS * 32 + j];
+        const float f = part_weight(ml.x, M);
+        l = fmaf(ml.y, f, l);  // (a NaN stays)
+        o.x = fmaf(v.x, f, o.x);
+        o.y = fmaf(v.y, f, o.y);
+      }
+      if (done) {
+        const int i = divide_group(a, q), h = it.g * G + (q - i * G);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        write_pair<F32>(a, l == l ? make_float2(o.x * inv, o.y * inv) : make_float2(l, l), ((size_t)(it.r0 + i) * a.nq + h) * D + dim);
+        if (dim == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M - kUp, l);
+      } else {
+        ws.o[part * S::PAIRS * 32 + j] = o;
+        if (dim == 0) ws.ml[part * S::Q + query] = make_float2(M, l);
+      }
+    }
+    more = false;
+    if (mode == kShares) {
+      int u = it.next;
+      more = next_item(s_plan, a, u, u1, it);
+    }
+    __syncthreads();
+  }
+}
+
+// The parts of items cut between CTAs, joined in CTA order: a block for an item.
+template <int D, int NT, bool F32>
+__global__ void __launch_bounds__(kThreads) join4_kernel(const __grid_constant__ TreeArgs a, Work ws, int ctas, int turn) {
+  using S = Shape<D, NT, F32>;
+  __shared__ UnitPlan plan;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int b = blockIdx.z, g = blockIdx.y, qt = blockIdx.x;
+  const int r0 = a.rm.start[b], rows = a.rm.start[b + 1] - r0, G = a.nq / a.nkv;
+  ptx::griddep_launch_dependents();
+  if (qt * S::Q < rows * G) {
+    if (tid < 32) make_plan(a, S::Q, turn, lane, plan, false);
+    __syncthreads();
+  }
+  ptx::griddep_wait();
+  if (qt * S::Q >= rows * G) return;
+  const int tiles = plan.tiles[b];
+  const int first = plan.unit[b] + (g * plan.qts[b] + qt) * (tiles + turn) + turn;
+  const int c0 = tiles > 0 ? unit_owner(plan, first, ctas) : 0;
+  const int n = tiles > 0 ? unit_owner(plan, first + tiles - 1, ctas) - c0 + 1 : 0;
+  if (n <= 1) return;  // skipped, or written by its CTA
+  auto part = [&](int k) { return (size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0); };
+  for (int j = tid; j < S::PAIRS * 32; j += kThreads) {
+    int query, dim;
+    place_of<D>(j / 32, lane, query, dim);
+    const int q = qt * S::Q + query;
+    if (q >= rows * G) continue;
+    float M = -INFINITY, l = 0.f;
+    float2 o = make_float2(0.f, 0.f);
+    for (int k = 0; k < n; ++k) M = fmaxf(M, __ldcg(&ws.ml[part(k) * S::Q + query]).x);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const float2 ml = __ldcg(&ws.ml[part(k) * S::Q + query]), v = __ldcg(&ws.o[part(k) * S::PAIRS * 32 + j]);
+      const float f = part_weight(ml.x, M);
+      l = fmaf(ml.y, f, l);
+      o.x = fmaf(v.x, f, o.x);
+      o.y = fmaf(v.y, f, o.y);
+    }
+    const int i = divide_group(a, q), h = g * G + (q - i * G);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    write_pair<F32>(a, l == l ? make_float2(o.x * inv, o.y * inv) : make_float2(l, l), ((size_t)(r0 + i) * a.nq + h) * D + dim);
+    if (dim == 0 && a.lse) a.lse[(size_t)(r0 + i) * a.nq + h] = row_lse(M - kUp, l);
+  }
+}
+
+// Items of at most this many tiles are each done by one CTA.
+constexpr int kWholeTiles = 2;
+
+template <int D, int NT, bool F32>
+cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sms, cudaStream_t st) {
+  using S = Shape<D, NT, F32>;
+  static PerDevice opted;
+  const cudaError_t e = opt_in(opted, attn4_kernel<D, NT, F32>, S::SMEM);
+  if (e != cudaSuccess) return e;
+  const TreeArgs& a = a4.t;
+  const int G = a.nq / a.nkv;
+  int64_t items = 0;
+  int most = 0;
+  for (int b = 0; b < a.rm.batch; ++b) {
+    const int rows = a.rm.start[b + 1] - a.rm.start[b];
+    most = std::max(most, rows);
+    items += (int64_t)(rows * G + S::Q - 1) / S::Q * a.nkv;
+  }
+  const int64_t tiles = (max_keys + 127) / 128, units = items * tiles;
+  const dim3 each((most * G + S::Q - 1) / S::Q, a.nkv, a.rm.batch);
+  if (tiles <= kWholeTiles)
+    return launch_pdl(attn4_kernel<D, NT, F32>, each, dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kWhole, 0);
+  const int ctas = (int)std::min<int64_t>(units, 2 * sms), turn = 0;
+  const cudaError_t f = launch_pdl(attn4_kernel<D, NT, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kShares, turn);
+  if (f != cudaSuccess) return f;
+  return launch_pdl(join4_kernel<D, NT, F32>, each, dim3(kThreads), 0, st, 1, a, ws, ctas, turn);
+}
+
+template <int D>
+cudaError_t launch_d(const Tree4Args& a, void* workspace, int64_t max_keys, cudaStream_t st) {
+  const int sms = device_sms();
+  Work ws;
+  ws.o = (float2*)workspace;
+  ws.ml = ws.o + (size_t)2 * sms * 2 * 16 * D / 2;
+  int most = 0;
+  for (int b = 0; b < a.t.rm.batch; ++b) most = std::max(most, a.t.rm.start[b + 1] - a.t.rm.start[b]);
+  if (most * (a.t.nq / a.t.nkv) <= 8)
+    return a.t.q_f32 ? launch<D, 1, true>(a, ws, max_keys, sms, st) : launch<D, 1, false>(a, ws, max_keys, sms, st);
+  return a.t.q_f32 ? launch<D, 2, true>(a, ws, max_keys, sms, st) : launch<D, 2, false>(a, ws, max_keys, sms, st);
+}
+
+}  // namespace
+
+size_t attention4_workspace(int head_dim) {
+  return (size_t)device_sms() * 2 * 2 * 16 * (head_dim * 4 + 8);
+}
+
+cudaError_t launch_attention4(const Tree4Args& a, int head_dim, int64_t max_keys, void* workspace, cudaStream_t st) {
+  return head_dim == 128 ? launch_d<128>(a, workspace, max_keys, st) : launch_d<64>(a, workspace, max_keys, st);
+}
+
+}  // namespace as2d

@@ -112,6 +112,39 @@ struct SampledArgs {
   int32_t *n_out, *token_out;
 };
 
+// Rows of a projection for one layer of a cache, in bf16 or in 4 bits (as2d_new_rows).
+struct AppendArgs {
+  RowMap rm;
+  const int32_t* len;       // device [batch]
+  const int32_t* positions; // device [rows], or null: len + i
+  int cap, nq, nkv;
+  const void *q, *k, *v;    // [rows][heads][d], rows strides apart
+  int64_t q_stride, k_stride, v_stride;
+  void* q_out;              // [rows][nq][d]
+  const float *q_norm, *k_norm;  // [d], nullable
+  float eps;
+  int half;                 // half of the rotated dims
+  uint64_t turn[64];        // 2^64 times the turns a position makes, by dim of the first half
+  bf16 *ck, *cv;            // the layer's [batch][nkv][cap][d]
+  uint8_t *ck4, *cks, *cv4, *cvs;  // or, in 4 bits, codes and scales
+  int32_t* err;             // error bits, nullable
+};
+
+struct Pack4Args {
+  bf16 *k, *v;              // [units][cap][d]
+  uint8_t *k4, *ks, *v4, *vs;  // [units][cap4][..]
+  const int32_t *start, *end;  // device [batch]; start nullable
+  int batch, nkv, cap, cap4;
+  int64_t units;            // (layers batch nkv)
+  int32_t* err;
+};
+
+// As TreeArgs of an attention over a cache in 4 bits (k and v unused).
+struct Tree4Args {
+  TreeArgs t;
+  const uint8_t *k, *ks, *v, *vs;  // the layer's
+};
+
 // SMs of the current device; (request, kv head, tile of 128 queries) items of a call.
 int device_sms();
 int64_t tree_items(const TreeArgs& a);
@@ -126,5 +159,12 @@ void cache_evict_carve(EvictArgs& a, int64_t units, void* workspace);
 cudaError_t launch_token_probs(const float* logits, int rows, int vocab, float temperature, float* probs,
                                cudaStream_t st);
 cudaError_t launch_accept_sampled(const SampledArgs& a, cudaStream_t st);
+cudaError_t launch_append(const AppendArgs& a, int head_dim, bool f32, cudaStream_t st);
+cudaError_t launch_pack4(const Pack4Args& a, int head_dim, bool write, int max_entries, cudaStream_t st);
+cudaError_t launch_attention4(const Tree4Args& a, int head_dim, int64_t max_keys, void* workspace, cudaStream_t st);
+size_t attention4_workspace(int head_dim);
+cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
+                                    cudaStream_t st);
+size_t prompt_attention_workspace(int head_dim);
 
 }  // namespace as2d

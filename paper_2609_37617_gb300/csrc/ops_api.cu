@@ -35,9 +35,10 @@ as2d_status check_cache(const as2d_cache* c, bool data) {
 }
 
 // Checks of the rows of a call, and its arguments but for outputs.  max_keys:
-// the most entries a request can have by the host's bound.
+// the most entries a request can have by the host's bound; limit: the most rows of
+// a request; tile: the fewest queries of an item.
 as2d_status check_rows(const as2d_cache* c, int32_t layer, const as2d_tree_rows* r, TreeArgs& a,
-                       int64_t& max_keys) {
+                       int64_t& max_keys, int32_t limit = kMaxTree, int tile = 64) {
   as2d_status st = check_cache(c, true);
   if (st != AS2D_OK) return st;
   if (layer < 0 || layer >= c->n_layers) return invalid("layer outside [0, n_layers)");
@@ -52,7 +53,8 @@ as2d_status check_rows(const as2d_cache* c, int32_t layer, const as2d_tree_rows*
   a.rm.start[0] = 0;
   int most = 0;
   for (int b = 0; b < c->batch; ++b) {
-    if (r->rows[b] < 0 || r->rows[b] > kMaxTree) return invalid("rows must be in [0, AS2D_MAX_TREE]");
+    if (r->rows[b] < 0 || r->rows[b] > limit)
+      return invalid(limit == kMaxTree ? "rows must be in [0, AS2D_MAX_TREE]" : "rows must be >= 0");
     if (r->rows[b] > c->capacity) return report_error(AS2D_ERR_CAPACITY, "more rows than the capacity");
     a.rm.start[b + 1] = a.rm.start[b] + r->rows[b];
     if (r->rows[b] > most) most = r->rows[b];
@@ -82,9 +84,120 @@ as2d_status check_rows(const as2d_cache* c, int32_t layer, const as2d_tree_rows*
   if (max_keys > c->capacity) max_keys = c->capacity;
   // units of work (tiles, and up to eight for each turn), counted in 32 bits on the device
   const int64_t tiles = (c->capacity + 127) / 128 + 8, G = r->n_q / c->n_kv;
-  if ((a.rm.rows * G / 64 + c->batch) * c->n_kv * tiles > 0x7fffffff)
+  if ((a.rm.rows * G / tile + c->batch) * c->n_kv * tiles > 0x7fffffff)
     return report_error(AS2D_ERR_UNSUPPORTED, "too many heads, rows and positions");
   return AS2D_OK;
+}
+
+// A cache in 4 bits, as one in bf16 of the same sizes.
+as2d_status check_cache4(const as2d_cache4* c, bool data, as2d_cache& sizes) {
+  if (!c) return invalid("cache is NULL");
+  sizes = {c->k, c->v, c->n_layers, c->batch, c->n_kv, c->capacity, c->head_dim};
+  const as2d_status st = check_cache(&sizes, data);
+  if (st != AS2D_OK) return st;
+  if (data && (!c->k_scale || !c->v_scale)) return invalid("a scale pointer is NULL");
+  if (data && (!aligned(c->k_scale, 8) || !aligned(c->v_scale, 8))) return invalid("scales must be 8-byte aligned");
+  return AS2D_OK;
+}
+
+// Checks of the rows of a projection and q_out, for a cache of these sizes.
+as2d_status check_new_rows(const as2d_cache* c, int32_t layer, const as2d_new_rows* r, const void* q_out,
+                           const int32_t* error_bits, AppendArgs& a) {
+  if (layer < 0 || layer >= c->n_layers) return invalid("layer outside [0, n_layers)");
+  if (!r || !r->kv_len || !r->rows) return invalid("rows, its kv_len and its rows are required");
+  if (r->type != AS2D_TYPE_BF16 && r->type != AS2D_TYPE_F32) return invalid("type is no AS2D_TYPE_*");
+  if (r->n_q < 1) return invalid("n_q must be positive");
+  if (r->n_q > 65535) return report_error(AS2D_ERR_UNSUPPORTED, "too many query heads");
+  const int d = c->head_dim;
+  if (r->rotary < 0 || r->rotary > d || r->rotary % 16 != 0)
+    return invalid("rotary must be a multiple of 16 in [0, head_dim]");
+  if (r->rotary > 0 && (!(r->theta > 0.f) || !std::isfinite(r->theta))) return invalid("theta must be finite and > 0");
+  if ((r->q_norm || r->k_norm) && (!(r->eps >= 0.f) || !std::isfinite(r->eps)))
+    return invalid("eps must be finite and >= 0");
+  a.rm.batch = c->batch;
+  a.rm.start[0] = 0;
+  int64_t total = 0;
+  for (int b = 0; b < c->batch; ++b) {
+    if (r->rows[b] < 0) return invalid("rows must be >= 0");
+    if (r->rows[b] > c->capacity) return report_error(AS2D_ERR_CAPACITY, "more rows than the capacity");
+    total += r->rows[b];
+    a.rm.start[b + 1] = (int32_t)total;
+  }
+  a.rm.rows = (int32_t)total;
+  if (total > (1 << 24)) return report_error(AS2D_ERR_UNSUPPORTED, "more than 2^24 rows");
+  if (total > 0 && (!r->q || !r->k || !r->v || !q_out)) return invalid("q, k, v and q_out are required");
+  const int64_t size = r->type == AS2D_TYPE_F32 ? 4 : 2;
+  if (r->q_stride < (int64_t)r->n_q * d || r->k_stride < (int64_t)c->n_kv * d || r->v_stride < (int64_t)c->n_kv * d)
+    return invalid("a row's stride is less than its heads");
+  for (int64_t stride : {r->q_stride, r->k_stride, r->v_stride})
+    if (stride > INT64_MAX / (8 << 24) || stride * size % 16 != 0)
+      return invalid("strides in bytes must be multiples of 16");
+  for (const void* p : {r->q, r->k, r->v, q_out, (const void*)r->q_norm, (const void*)r->k_norm})
+    if (!aligned(p, 16)) return invalid("q, k, v, q_out and gains must be 16-byte aligned");
+  for (const void* p : {(const void*)r->kv_len, (const void*)r->positions, (const void*)error_bits})
+    if (!aligned(p, 4)) return invalid("kv_len, positions and error_bits must be 4-byte aligned");
+  a.len = r->kv_len;
+  a.positions = r->positions;
+  a.cap = c->capacity;
+  a.nq = r->n_q;
+  a.nkv = c->n_kv;
+  a.q = r->q;
+  a.k = r->k;
+  a.v = r->v;
+  a.q_stride = r->q_stride;
+  a.k_stride = r->k_stride;
+  a.v_stride = r->v_stride;
+  a.q_out = const_cast<void*>(q_out);
+  a.q_norm = r->q_norm;
+  a.k_norm = r->k_norm;
+  a.eps = r->eps;
+  a.half = r->rotary / 2;
+  a.err = const_cast<int32_t*>(error_bits);
+  // theta^(-2j / rotary) / 2 pi of a turn modulo 1, in 2^-64 of one: a product of the powers
+  // for the bits of j, each rounded once
+  double power[6], f[64];
+  for (int i = 0; (1 << i) < a.half; ++i) power[i] = std::pow((double)r->theta, -(double)(1 << i) / a.half);
+  for (int j = 0; j < a.half; ++j) {
+    f[j] = j == 0 ? 1.0 : f[j & (j - 1)] * power[__builtin_ctz(j)];
+    const double turns = f[j] * 0.15915494309189533577;
+    a.turn[j] = (uint64_t)std::ldexp(turns - std::floor(turns), 64);
+  }
+  return AS2D_OK;
+}
+
+// What as2d_cache4_write and as2d_cache4_read are given.
+as2d_status pack4(const as2d_cache4* c4, const as2d_cache* c, int32_t layer, const int32_t* start, const int32_t* end,
+                  int32_t max_entries, int32_t* error_bits, bool write, void* stream, const char* what) {
+  as2d_cache sizes;
+  as2d_status st = check_cache4(c4, true, sizes);
+  if (st == AS2D_OK) st = check_cache(c, true);
+  if (st != AS2D_OK) return st;
+  if (c->n_layers != c4->n_layers || c->batch != c4->batch || c->n_kv != c4->n_kv || c->head_dim != c4->head_dim)
+    return invalid("the caches' sizes differ in more than the capacity");
+  if (layer < -1 || layer >= c->n_layers) return invalid("layer outside [-1, n_layers)");
+  if (!end) return invalid("end is required");
+  if (!aligned(start, 4) || !aligned(end, 4) || !aligned(error_bits, 4))
+    return invalid("start, end and error_bits must be 4-byte aligned");
+  const int32_t most = c->capacity < c4->capacity ? c->capacity : c4->capacity;
+  if (max_entries < 0 || max_entries > most) return invalid("max_entries outside [0, capacity]");
+  const int64_t of_layer = (int64_t)c->batch * c->n_kv, first = layer > 0 ? layer * of_layer : 0;
+  const int d = c->head_dim;
+  Pack4Args a{};
+  a.k = (bf16*)c->k + first * c->capacity * d;
+  a.v = (bf16*)c->v + first * c->capacity * d;
+  a.k4 = c4->k + first * c4->capacity * (d / 2);
+  a.v4 = c4->v + first * c4->capacity * (d / 2);
+  a.ks = c4->k_scale + first * c4->capacity * (d / 16);
+  a.vs = c4->v_scale + first * c4->capacity * (d / 16);
+  a.start = start;
+  a.end = end;
+  a.batch = c->batch;
+  a.nkv = c->n_kv;
+  a.cap = c->capacity;
+  a.cap4 = c4->capacity;
+  a.units = layer >= 0 ? of_layer : of_layer * c->n_layers;
+  a.err = error_bits;
+  return launched(launch_pack4(a, d, write, max_entries > 0 ? max_entries : most, (cudaStream_t)stream), what);
 }
 
 as2d_status check_workspace(const void* workspace, int64_t bytes, size_t need) {
@@ -225,4 +338,124 @@ extern "C" as2d_status as2d_accept_sampled(const float* probs, const float* draf
   a.n_out = n_accepted;
   a.token_out = token;
   return launched(launch_accept_sampled(a, (cudaStream_t)stream), "as2d_accept_sampled");
+}
+
+extern "C" as2d_status as2d_cache_append(const as2d_cache* cache, int32_t layer, const as2d_new_rows* rows,
+                                         void* q_out, int32_t* error_bits, void* stream) {
+  clear_error();
+  as2d_status st = check_cache(cache, true);
+  if (st != AS2D_OK) return st;
+  AppendArgs a{};
+  st = check_new_rows(cache, layer, rows, q_out, error_bits, a);
+  if (st != AS2D_OK || a.rm.rows == 0) return st;
+  const size_t at = (size_t)layer * cache->batch * cache->n_kv * cache->capacity * cache->head_dim;
+  a.ck = (bf16*)cache->k + at;
+  a.cv = (bf16*)cache->v + at;
+  return launched(launch_append(a, cache->head_dim, rows->type == AS2D_TYPE_F32, (cudaStream_t)stream),
+                  "as2d_cache_append");
+}
+
+extern "C" as2d_status as2d_cache4_append(const as2d_cache4* cache, int32_t layer, const as2d_new_rows* rows,
+                                          void* q_out, int32_t* error_bits, void* stream) {
+  clear_error();
+  as2d_cache sizes;
+  as2d_status st = check_cache4(cache, true, sizes);
+  if (st != AS2D_OK) return st;
+  AppendArgs a{};
+  st = check_new_rows(&sizes, layer, rows, q_out, error_bits, a);
+  if (st != AS2D_OK || a.rm.rows == 0) return st;
+  const size_t at = (size_t)layer * cache->batch * cache->n_kv * cache->capacity;
+  a.ck4 = cache->k + at * (cache->head_dim / 2);
+  a.cv4 = cache->v + at * (cache->head_dim / 2);
+  a.cks = cache->k_scale + at * (cache->head_dim / 16);
+  a.cvs = cache->v_scale + at * (cache->head_dim / 16);
+  return launched(launch_append(a, cache->head_dim, rows->type == AS2D_TYPE_F32, (cudaStream_t)stream),
+                  "as2d_cache4_append");
+}
+
+extern "C" as2d_status as2d_cache4_write(const as2d_cache4* to, const as2d_cache* from, int32_t layer,
+                                         const int32_t* start, const int32_t* end, int32_t max_entries,
+                                         int32_t* error_bits, void* stream) {
+  clear_error();
+  return pack4(to, from, layer, start, end, max_entries, error_bits, true, stream, "as2d_cache4_write");
+}
+
+extern "C" as2d_status as2d_cache4_read(const as2d_cache4* from, const as2d_cache* to, int32_t layer,
+                                        const int32_t* start, const int32_t* end, int32_t max_entries,
+                                        int32_t* error_bits, void* stream) {
+  clear_error();
+  return pack4(from, to, layer, start, end, max_entries, error_bits, false, stream, "as2d_cache4_read");
+}
+
+extern "C" as2d_status as2d_cache4_attention_workspace(const as2d_cache4* cache, int64_t* bytes) {
+  clear_error();
+  as2d_cache sizes;
+  const as2d_status st = check_cache4(cache, false, sizes);
+  if (st != AS2D_OK) return st;
+  if (!bytes) return invalid("bytes is NULL");
+  *bytes = (int64_t)attention4_workspace(cache->head_dim);
+  return AS2D_OK;
+}
+
+extern "C" as2d_status as2d_cache4_attention(const as2d_cache4* cache, int32_t layer, const as2d_tree_rows* rows,
+                                             void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                                             int32_t* error_bits, void* stream) {
+  clear_error();
+  as2d_cache sizes;
+  as2d_status st = check_cache4(cache, true, sizes);
+  if (st != AS2D_OK) return st;
+  Tree4Args a{};
+  int64_t max_keys = 0;
+  st = check_rows(&sizes, layer, rows, a.t, max_keys, kMaxTree, 8);
+  if (st != AS2D_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, attention4_workspace(cache->head_dim));
+  if (st != AS2D_OK) return st;
+  if (a.t.rm.rows == 0) return AS2D_OK;
+  if (!out || !aligned(out, 16)) return invalid("out must be 16-byte aligned");
+  if (!aligned(lse, 4) || !aligned(error_bits, 4)) return invalid("lse and error_bits must be 4-byte aligned");
+  const size_t at = (size_t)layer * cache->batch * cache->n_kv * cache->capacity;
+  a.k = cache->k + at * (cache->head_dim / 2);
+  a.v = cache->v + at * (cache->head_dim / 2);
+  a.ks = cache->k_scale + at * (cache->head_dim / 16);
+  a.vs = cache->v_scale + at * (cache->head_dim / 16);
+  a.t.k = a.t.v = nullptr;
+  a.t.out = out;
+  a.t.lse = lse;
+  a.t.err = error_bits;
+  return launched(launch_attention4(a, cache->head_dim, max_keys, workspace, (cudaStream_t)stream),
+                  "as2d_cache4_attention");
+}
+
+extern "C" as2d_status as2d_prompt_attention_workspace(const as2d_cache* cache, int64_t* bytes) {
+  clear_error();
+  const as2d_status st = check_cache(cache, false);
+  if (st != AS2D_OK) return st;
+  if (!bytes) return invalid("bytes is NULL");
+  *bytes = (int64_t)prompt_attention_workspace(cache->head_dim);
+  return AS2D_OK;
+}
+
+extern "C" as2d_status as2d_prompt_attention(const as2d_cache* cache, int32_t layer, const as2d_tree_rows* rows,
+                                             void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                                             int32_t* error_bits, void* stream) {
+  clear_error();
+  as2d_status st = check_cache(cache, true);
+  if (st != AS2D_OK) return st;
+  TreeArgs a{};
+  int64_t max_keys = 0;
+  st = check_rows(cache, layer, rows, a, max_keys, INT32_MAX, 256);
+  if (st != AS2D_OK) return st;
+  if (a.q_f32) return report_error(AS2D_ERR_UNSUPPORTED, "prompt attention takes bf16 queries");
+  if (a.visible) return invalid("visible must be NULL: prompts are causal");
+  if (a.rm.rows > (1 << 24)) return report_error(AS2D_ERR_UNSUPPORTED, "more than 2^24 rows");
+  st = check_workspace(workspace, workspace_bytes, prompt_attention_workspace(cache->head_dim));
+  if (st != AS2D_OK) return st;
+  if (a.rm.rows == 0) return AS2D_OK;
+  if (!out || !aligned(out, 16)) return invalid("out must be 16-byte aligned");
+  if (!aligned(lse, 4) || !aligned(error_bits, 4)) return invalid("lse and error_bits must be 4-byte aligned");
+  a.out = out;
+  a.lse = lse;
+  a.err = error_bits;
+  return launched(launch_prompt_attention(a, cache->head_dim, max_keys, workspace, (cudaStream_t)stream),
+                  "as2d_prompt_attention");
 }
