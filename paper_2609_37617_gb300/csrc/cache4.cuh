@@ -30,19 +30,34 @@ __device__ __forceinline__ float scale_of(T t, T& units) {
 }
 __device__ __forceinline__ uint8_t scale_byte(float s) { return (uint8_t)(__half_as_ushort(__float2half_rn(s)) >> 7); }
 
-// The codes of 8 values in a word.
-__device__ __forceinline__ uint32_t code_word(const int (&c)[8]) {
-  uint32_t w = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    w |= (uint32_t)(c[2 * e] + 8) << (4 * e) | (uint32_t)(c[2 * e + 1] + 8) << (16 + 4 * e);
-  return w;
+// ---- coding ---------------------------------------------------------------------
+//
+// Exact values of 8 significant bits (bf16) need no division: x / s with s of four bits,
+// and a largest magnitude over 7 in steps of scales, are on the border of two whole numbers or
+// at least 2^-10 from it where they are over 0.4, so that a product with the reciprocal (off by 2^-20), rounded
+// to 2^-12, is on the border just where they are.  (on_grid(x, f): x f so rounded, for |x f| <= 16.)
+__device__ __forceinline__ float on_grid(float x, float f) { return fmaf(x, f, 2304.f) - 2304.f; }
+
+__device__ __forceinline__ float reciprocal(float s) { return s > 0.f ? __fdividef(1.f, s) : 0.f; }
+
+// The scale of exact bf16 values whose largest magnitude is `most`.
+__device__ __forceinline__ float exact_scale(float most) {
+  const float t = most * (1.f / 7.f);
+  const int e = min(max((int)(__float_as_uint(t) >> 23), 127 - 14), 127 + 9);
+  const float steps = fminf(most, 7168.f) * __uint_as_float((uint32_t)(2 * 127 + 3 - e) << 23);  // of 1/7
+  return fminf(rintf(fminf(on_grid(steps, 1.f / 7.f), 16.f)) * __uint_as_float((uint32_t)(e - 3) << 23), kMaxScale4);
 }
 
-// c = x / s to the nearest, ties to even.  The quotient of 8 significant bits by four is
-// never so near to a border that its rounding to 32 bits would cross it.
-__device__ __forceinline__ int code_of(float x, float s) {
-  return s > 0.f ? (int)rintf(fminf(fmaxf(__fdiv_rn(x, s), -7.f), 7.f)) : 0;
+// A whole number of a code, rounded from q, as the bits of 1.5 2^23 + 8 + it: the code in the lowest.
+__device__ __forceinline__ uint32_t code_bits(float q) {
+  return __float_as_uint(fminf(fmaxf(q, -7.f), 7.f) + 12582920.f);
+}
+// The word of 8 codes.
+__device__ __forceinline__ uint32_t code_word(const uint32_t (&c)[8]) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 3; e >= 0; --e) w = w * 16 + __byte_perm(c[2 * e], c[2 * e + 1], 0x5410);
+  return w;
 }
 
 // ---- decoding -------------------------------------------------------------------

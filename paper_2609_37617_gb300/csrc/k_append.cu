@@ -25,17 +25,33 @@
 namespace as2d {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kMostRows = 4;
+// How far a finished value may be from its exact one, over |y_j| + |y_j'| of its pair: the mean
+// square, its root, the division and two products add 11 roundings of 2^-24, sine and cosine (one
+// step, and an angle rounded to 2^-25 of a half turn) 4, the rotation 2.
+constexpr float kOff = 1.5e-6f;
 
+// 8 dims as they are in memory.
 template <bool F32>
-__device__ __forceinline__ void load8(const void* base, int64_t at, float (&x)[8]) {
+struct Raw {
+  uint4 w[F32 ? 2 : 1];
+};
+template <bool F32>
+__device__ __forceinline__ void load8(const void* base, int64_t at, Raw<F32>& x) {
+  const uint4* p = reinterpret_cast<const uint4*>((const char*)base + at * (F32 ? 4 : 2));
+  x.w[0] = __ldcs(p);
+  if constexpr (F32) x.w[1] = __ldcs(p + 1);
+}
+template <bool F32>
+__device__ __forceinline__ void floats(const Raw<F32>& r, float (&x)[8]) {
+  const uint4 a = r.w[0];
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
   if constexpr (F32) {
-    const float4* p = reinterpret_cast<const float4*>((const float*)base + at);
-    const float4 a = __ldcs(p), b = __ldcs(p + 1);
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    const uint4 b = r.w[1];
+    const uint32_t v[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]), x[4 + e] = __uint_as_float(v[e]);
   } else {
-    const uint4 a = __ldcs(reinterpret_cast<const uint4*>((const bf16*)base + at));
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       x[2 * e] = __uint_as_float(w[e] << 16);
@@ -58,115 +74,159 @@ __device__ __forceinline__ void store8(float* to, const float (&y)[8]) {
   reinterpret_cast<float4*>(to)[1] = make_float4(y[4], y[5], y[6], y[7]);
 }
 
-// 8 dims of a head in 64 bits, as the 32-bit code below.
+// Those of 8 dims of a head that `which` has bits for, in 64 bits.  By whole warps, whose heads
+// may be keys and values: every thread takes part in the shuffles.
 template <int D>
-__device__ __noinline__ void finish_exactly(const AppendArgs& a, const float (&x)[8], const float* gain, int position,
-                                            int c, double (&y)[8]) {
+__device__ __noinline__ void finish_exactly(const AppendArgs& a, const float (&x)[8], const float* gain, bool turn,
+                                            int position, int c, uint32_t which, double (&y)[8]) {
   constexpr int C = D / 8;
-  // (heads with gains and heads without share a warp: every thread takes part in the shuffles)
   double ss = 0.0;
   for (int e = 0; e < 8; ++e) ss = fma((double)x[e], (double)x[e], ss);
   for (int o = C / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
   const double f = 1.0 / sqrt(ss / D + (double)a.eps);
-  for (int e = 0; e < 8; ++e) y[e] = gain ? (double)x[e] * f * (double)gain[8 * c + e] : (double)x[e];
   const int h = a.half, d0 = 8 * c, other = d0 < h ? c + h / 8 : c - h / 8;
   const int from = (threadIdx.x & 31 & ~(C - 1)) | (other & (C - 1));
+#pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const double z = __shfl_sync(~0u, y[e], from);
-    if (d0 < 2 * h) {
+    if (!((which >> e) & 1)) continue;  // (the same in every thread)
+    double v = gain ? (double)x[e] * f * (double)gain[8 * c + e] : (double)x[e];
+    const double z = __shfl_sync(~0u, v, from);
+    if (turn && d0 < 2 * h) {
       const int j = (d0 < h ? d0 : d0 - h) + e;
       double sn, cs;
       sincospi((double)(int64_t)((uint64_t)(int64_t)position * a.turn[j]) * 0x1p-63, &sn, &cs);
-      y[e] = d0 < h ? y[e] * cs - z * sn : y[e] * cs + z * sn;
+      v = d0 < h ? v * cs - z * sn : v * cs + z * sn;
     }
     __syncwarp();
+    y[e] = v;
   }
 }
 
-// 8 dims into 4 bits.  off: how far each may be from its exact value (0: it is exact);
-// returns whether a code or the scale is that near to a border.
-template <typename T>
-__device__ __forceinline__ bool quantise(const T (&y)[8], const float (&off)[8], uint32_t& codes, uint8_t& scale,
-                                         bool& odd) {
-  T most = 0;
-  float far = 0.f;
+// What 8 dims become in 4 bits.
+struct Coded {
+  float s;
+  uint32_t c[8];  // code_bits
+};
+
+// off: how far each of the values may be from its exact one (0: it is exact, of bf16).  Returns
+// bits of the dims whose code, and 2^8 if the scale, is that near to a border.
+__device__ __forceinline__ uint32_t code8(const float (&y)[8], const float (&off)[8], Coded& to, bool& odd) {
+  float most = 0.f, far = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const T m = fabs(y[e]);
-    most = m > most ? m : most;  // (NaN is passed by)
-    odd = odd || !(m <= (T)3.4028235e38f);
+    most = fmaxf(most, fabsf(y[e]));
+    odd = odd || !(fabsf(y[e]) <= 3.4028235e38f);
     far = fmaxf(far, off[e]);
   }
-  const T there = __shfl_xor_sync(~0u, most, 1);
-  most = there > most ? there : most;
+  most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
   far = fmaxf(far, __shfl_xor_sync(~0u, far, 1));
-  T units;
-  const T seventh = most / (T)7;
-  const float s = scale_of(seventh, units);
-  bool near = far > 0.f && fabs(fabs(units - rint(units)) - (T)0.5) * (seventh / (units > 0 ? units : (T)1)) <=
-                               (T)(far + 2e-7f * (float)seventh);
-  int c[8];
-  const float inv = s > 0.f ? 1.f / s : 0.f;
+  const float t = most * (1.f / 7.f);
+  float steps;
+  const float s = scale_of(t, steps), exact = exact_scale(most), inv_step = steps > 0.f ? steps / t : 0.f;
+  uint32_t near = far > 0.f && fabsf(fabsf(steps - rintf(steps)) - 0.5f) <= (far + 2.5e-7f * t) * inv_step ? 256u : 0u;
+  to.s = far > 0.f ? s : exact;
+  const float inv = reciprocal(to.s);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    if constexpr (sizeof(T) == 4) {
-      const float q = s > 0.f ? __fdiv_rn(y[e], s) : 0.f;
-      near = near || (off[e] > 0.f && fabsf(fabsf(q - rintf(q)) - 0.5f) <= off[e] * inv + 2e-6f);
-      c[e] = (int)rintf(fminf(fmaxf(q, -7.f), 7.f));
-    } else {
-      const double q = s > 0.f ? y[e] / (double)s : 0.0;
-      c[e] = (int)rint(fmin(fmax(q, -7.0), 7.0));
-    }
-    if (y[e] != y[e]) c[e] = 0;
+    const float q = y[e] * inv;
+    if (off[e] > 0.f && fabsf(fabsf(q - rintf(q)) - 0.5f) <= fmaf(off[e], inv, 4e-6f)) near |= 1u << e;
+    to.c[e] = code_bits(off[e] > 0.f ? q : on_grid(y[e], inv));
   }
-  codes = code_word(c);
-  scale = scale_byte(s);
+  if (odd)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (y[e] != y[e]) to.c[e] = code_bits(0.f);
   return near;
 }
 
-// A block: R rows (grid-stride).  A unit is a head of a row, 8 dims a thread.
-template <int D, bool F32, bool FOUR>
+// The same of exact values: with bit 2^8 of `which` all of it, else those codes that it has bits for.
+__device__ __noinline__ void code8_exactly(const double (&y)[8], uint32_t which, Coded& to) {
+  if (which & 256u) {
+    double most = 0.0, steps;
+    for (int e = 0; e < 8; ++e) most = fmax(most, fabs(y[e]));
+    most = fmax(most, __shfl_xor_sync(~0u, most, 1));
+    to.s = scale_of(most / 7.0, steps);
+  }
+  for (int e = 0; e < 8; ++e)
+    if ((which >> e) & 1) {
+      const double q = to.s > 0.f ? y[e] / (double)to.s : 0.0;
+      to.c[e] = code_bits(y[e] == y[e] ? (float)rint(fmin(fmax(q, -7.0), 7.0)) : 0.f);
+    }
+}
+
+// What a thread has of one head of a row of a block.
+struct Place {
+  int i, head;   // row of the block, head of the row: queries, keys, values
+  bool live;     // there is such a head
+  bool isq, isv;
+  int hh;        // head among its kind
+};
+
+// A block: R rows, U heads at once a thread.
+template <int D, bool F32, bool FOUR, int U>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs a, int R) {
   constexpr int C = D / 8, G = kThreads / C;  // threads of a head, heads at once
-  __shared__ float2 s_turn[8][64];
-  __shared__ int s_req[8], s_at[8], s_pos[8];
+  __shared__ float2 s_turn[kMostRows][64];
+  __shared__ int s_req[kMostRows], s_at[kMostRows], s_pos[kMostRows];
   const int tid = threadIdx.x, c = tid % C, H = a.nq + 2 * a.nkv;
+  const int r0 = blockIdx.x * R, n = min(R, a.rm.rows - r0), units = n * H;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
+  auto place = [&](int u) {
+    Place p;
+    p.live = u < units;
+    p.i = p.live ? u / H : 0;
+    p.head = p.live ? u - p.i * H : 0;
+    p.isq = p.head < a.nq, p.isv = p.head >= a.nq + a.nkv;
+    p.hh = p.isq ? p.head : p.head - a.nq - (p.isv ? a.nkv : 0);
+    return p;
+  };
+  Raw<F32> raw[U];
+  auto load = [&](int u0) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const Place p = place(u0 + k * G + tid / C);
+      const int64_t stride = p.isq ? a.q_stride : p.isv ? a.v_stride : a.k_stride;
+      if (p.live) load8(p.isq ? a.q : p.isv ? a.v : a.k, (r0 + p.i) * stride + p.hh * D + 8 * c, raw[k]);
+    }
+  };
+  load(0);
+  if (tid < n) {
+    const int r = r0 + tid, b = row_request(a.rm, r), L = a.len[b], rows = a.rm.start[b + 1] - a.rm.start[b];
+    const int i = r - a.rm.start[b];
+    const bool fits = rows_fit(L, rows, a.cap);
+    if (!fits && i == 0 && a.err) atomicOr(a.err, kErrCapacity);
+    s_req[tid] = b;
+    s_at[tid] = fits ? L + i : -1;
+    s_pos[tid] = a.positions ? a.positions[r] : fits ? L + i : 0;
+  }
+  __syncthreads();
+  for (int t = tid; t < n * a.half; t += kThreads) {
+    const int i = t / a.half, j = t - i * a.half;
+    const uint64_t turns = (uint64_t)(int64_t)s_pos[i] * a.turn[j];
+    float2 v;
+    sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &v.y, &v.x);
+    s_turn[i][j] = v;
+  }
+  __syncthreads();
   bool odd = false;
-  for (int r0 = blockIdx.x * R; r0 < a.rm.rows; r0 += gridDim.x * R) {
-    const int n = min(R, a.rm.rows - r0);
-    if (tid < n) {
-      const int r = r0 + tid, b = row_request(a.rm, r), L = a.len[b], rows = a.rm.start[b + 1] - a.rm.start[b];
-      const int i = r - a.rm.start[b];
-      const bool fits = rows_fit(L, rows, a.cap);
-      if (!fits && i == 0 && a.err) atomicOr(a.err, kErrCapacity);
-      s_req[tid] = b;
-      s_at[tid] = fits ? L + i : -1;
-      s_pos[tid] = a.positions ? a.positions[r] : fits ? L + i : 0;
-    }
-    __syncthreads();
-    for (int t = tid; t < n * a.half; t += kThreads) {
-      const int i = t / a.half, j = t - i * a.half;
-      const uint64_t turns = (uint64_t)(int64_t)s_pos[i] * a.turn[j];
-      float2 v;
-      sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &v.y, &v.x);
-      s_turn[i][j] = v;
-    }
-    __syncthreads();
-    const int units = n * H;
-    for (int u0 = 0; u0 < units; u0 += G) {
-      const int u = u0 + tid / C, i = u / H, head = u - i * H;
+  const int h = a.half, d0 = 8 * c, other = d0 < h ? c + h / 8 : c - h / 8;
+  const int from = (tid & 31 & ~(C - 1)) | (other & (C - 1));
+  for (int u0 = 0; u0 < units; u0 += U * G) {
+    if (u0 > 0) load(u0);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (u0 + k * G >= units) break;
       // (threads past the last unit take part in the shuffles)
-      const bool live = u < units && s_at[min(i, n - 1)] >= 0;
-      const bool isq = head < a.nq, isv = head >= a.nq + a.nkv;
-      const int hh = isq ? head : head - a.nq - (isv ? a.nkv : 0), r = r0 + i;
-      float x[8] = {};
-      if (live)
-        load8<F32>(isq ? a.q : isv ? a.v : a.k, r * (isq ? a.q_stride : isv ? a.v_stride : a.k_stride) + hh * D + 8 * c, x);
-      const float* gain = isq ? a.q_norm : isv ? nullptr : a.k_norm;
-      float y[8];
-      float ss = 0.f;
+      const Place p = place(u0 + k * G + tid / C);
+      const bool live = p.live && s_at[p.i] >= 0;
+      const float* gain = p.isq ? a.q_norm : p.isv ? nullptr : a.k_norm;
+      float y[8], off[8];  // off: how far a value is from the exact one, at most (4 bits)
+      float ss = 0.f, x[8];
+      floats<F32>(raw[k], x);
+      if (!p.live)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
 #pragma unroll
@@ -181,67 +241,60 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = x[e];
       }
-      // how far a value is from the exact one, at most (4 bits)
-      float off[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) off[e] = gain || F32 ? 1e-6f * fabsf(y[e]) : 0.f;
-      const int h = a.half, d0 = 8 * c, other = d0 < h ? c + h / 8 : c - h / 8;
-      const int from = (tid & 31 & ~(C - 1)) | (other & (C - 1));
-      const bool turned = !isv && d0 < 2 * h;
+      for (int e = 0; e < 8; ++e) off[e] = gain || F32 ? kOff * fabsf(y[e]) : 0.f;
       if (h > 0) {
+        const bool turned = !p.isv && d0 < 2 * h;
+        const float2* turn = s_turn[p.i] + (d0 < h ? d0 : d0 - h);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float z = __shfl_sync(~0u, y[e], from);
           if (turned) {
-            const float2 t = s_turn[min(i, n - 1)][(d0 < h ? d0 : d0 - h) + e];
-            if (FOUR) off[e] = 1e-6f * (fabsf(y[e]) + fabsf(z));
+            const float2 t = turn[e];
+            if (FOUR) off[e] = kOff * (fabsf(y[e]) + fabsf(z));
             y[e] = d0 < h ? y[e] * t.x - z * t.y : y[e] * t.x + z * t.y;
           }
         }
       }
       if (FOUR) {
-        uint32_t codes;
-        uint8_t scale;
+        Coded to;
         bool strange = false;
-        bool near = quantise(y, off, codes, scale, strange);
-        if (__any_sync(~0u, near && live && !isq)) {
+        const bool mine = live && !p.isq;
+        const uint32_t near = code8(y, off, to, strange);
+        uint32_t which = __reduce_or_sync(~0u, mine ? near : 0u);
+        if (which) {
+          if (which & 256u) which = 511u;
           double z[8];
-          finish_exactly<D>(a, x, gain, s_pos[min(i, n - 1)], c, z);
-          if (isv)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = x[e];
-          bool ignore = false;
-          quantise(z, off, codes, scale, ignore);
+          finish_exactly<D>(a, x, gain, !p.isv, s_pos[p.i], c, which, z);
+          code8_exactly(z, which, to);
         }
-        if (live && !isq) {
+        if (mine) {
           odd = odd || strange;
-          const size_t at = (((size_t)s_req[i] * a.nkv + hh) * a.cap + s_at[i]) * C + c;
-          reinterpret_cast<uint32_t*>(isv ? a.cv4 : a.ck4)[at] = codes;
-          if (c % 2 == 0) (isv ? a.cvs : a.cks)[at / 2] = scale;
+          const size_t at = (((size_t)s_req[p.i] * a.nkv + p.hh) * a.cap + s_at[p.i]) * C + c;
+          reinterpret_cast<uint32_t*>(p.isv ? a.cv4 : a.ck4)[at] = code_word(to.c);
+          if (c % 2 == 0) (p.isv ? a.cvs : a.cks)[at / 2] = scale_byte(to.s);
         }
-      } else if (live && !isq) {
-        store8((isv ? a.cv : a.ck) + (((size_t)s_req[i] * a.nkv + hh) * a.cap + s_at[i]) * D + 8 * c, y);
+      } else if (live && !p.isq) {
+        store8((p.isv ? a.cv : a.ck) + (((size_t)s_req[p.i] * a.nkv + p.hh) * a.cap + s_at[p.i]) * D + 8 * c, y);
       }
-      if (live && isq) {
-        const size_t at = ((size_t)r * a.nq + hh) * D + 8 * c;
+      if (live && p.isq) {
+        const size_t at = ((size_t)(r0 + p.i) * a.nq + p.hh) * D + 8 * c;
         if constexpr (F32)
           store8((float*)a.q_out + at, y);
         else
           store8((bf16*)a.q_out + at, y);
       }
     }
-    __syncthreads();
   }
   if (FOUR && __any_sync(~0u, odd) && (tid & 31) == 0 && a.err) atomicOr(a.err, kErrNotFinite);
 }
 
 template <int D, bool F32>
 cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
-  const int sms = device_sms();
-  const int R = a.rm.rows <= 4 * sms ? 1 : 4;
-  const int64_t blocks = std::min<int64_t>((a.rm.rows + R - 1) / R, 64 * sms);
-  return launch_pdl(a.ck4 ? append_kernel<D, F32, true> : append_kernel<D, F32, false>, dim3((unsigned)blocks),
-                    dim3(kThreads), 0, st, 1, a, R);
+  constexpr int U = F32 ? 2 : 3;
+  const int R = a.rm.rows <= 4 * device_sms() ? 1 : kMostRows;
+  return launch_pdl(a.ck4 ? append_kernel<D, F32, true, U> : append_kernel<D, F32, false, U>,
+                    dim3((a.rm.rows + R - 1) / R), dim3(kThreads), 0, st, 1, a, R);
 }
 
 }  // namespace

@@ -24,6 +24,15 @@ struct Work {
   float2* ml;  // [2 CTAs][queries] (reference base 2, sum)
 };
 
+// A query tile's operands: as halves times a power of two of the query's own, which brings its
+// largest dim to 2^14 .. 2^15, in the order of the product's fragments (lane 4 g + t has dims D / 4
+// t .. of query 8 nt + g); back: what scores are to be multiplied by.
+template <int D, int NT, bool F32>
+struct QueryTile {
+  uint4 hi[NT][D / 32][32], lo[F32 ? NT : 1][F32 ? D / 32 : 1][32];
+  float back[8 * NT];
+};
+
 template <int D, int NT, bool F32>
 struct Shape {
   static constexpr int Q = 8 * NT;                         // queries of a tile
@@ -32,19 +41,19 @@ struct Shape {
   static constexpr int NST = NT == 1 && !F32 ? 5 : 8;
   static constexpr int RING = kWarps * NST * STAGE;
   static constexpr int PAIRS = D / 16 * NT * 2;            // of dims, a lane
-  static constexpr int PARTS = kWarps * (PAIRS * 32 * 8 + Q * 8);
-  static constexpr int SMEM = RING > PARTS ? RING : PARTS;
+  static constexpr int PARTS = kWarps * PAIRS * 32 * 8;
+  static constexpr int AREA = RING > PARTS ? RING : PARTS;
+  static constexpr int SMEM = AREA + sizeof(QueryTile<D, NT, F32>);
 };
 
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {  // 8 x 8 of 16 bits
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 __device__ __forceinline__ uint32_t halves(float a, float b) {
@@ -69,81 +78,74 @@ __device__ __forceinline__ int value_off(int off, int row) { return off ^ (((row
 template <int D>
 __device__ __forceinline__ void load_slice(const Tree4Args& a, size_t head, int p, int end, int lane, uint8_t* to) {
   constexpr int ROW = D / 2, PIECES = ROW / 16, CODES = 16 * ROW, S = D / 16;
+  const int last = end - 1 - p;  // of the slice
+  const size_t at = head + p;
+  const uint8_t *k = a.k + at * ROW, *v = a.v + at * ROW;
 #pragma unroll
   for (int i = 0; i < PIECES / 2; ++i) {
-    const int x = lane + 32 * i, row = x / PIECES, off = row * ROW + x % PIECES * 16;
-    const size_t at = (head + min(p + row, end - 1)) * ROW + x % PIECES * 16;
-    cp_async<16>(to + off, a.k + at);
-    cp_async<16>(to + CODES + value_off(off, row), a.v + at);
+    const int x = lane + 32 * i, row = x / PIECES, off = x % PIECES * 16;
+    const int from = min(row, last) * ROW + off;
+    cp_async<16>(to + row * ROW + off, k + from);
+    cp_async<16>(to + CODES + value_off(row * ROW + off, row), v + from);
   }
-  const int row = lane & 15;
-  const size_t at = (head + min(p + row, end - 1)) * S;
-  cp_async<S>(to + 2 * CODES + lane * S, (lane < 16 ? a.ks : a.vs) + at);
+  cp_async<S>(to + 2 * CODES + lane * S, (lane < 16 ? a.ks : a.vs) + at * S + min(lane & 15, last) * S);
 }
 
-// A query tile's operands: lane (g, t) has dims D / 4 t .. of query 8 nt + g, as halves times a
-// power of two of the query's own, which brings its largest dim to 2^14 .. 2^15; back: what scores
-// are to be multiplied by, of queries 8 nt + 2 t and + 1.
+// By the whole block.
 template <int D, int NT, bool F32>
-__device__ __forceinline__ void load_queries4(const TreeArgs& a, const Unit& it, int lane, uint32_t (&hi)[NT][D / 8],
-                                              uint32_t (&lo)[F32 ? NT : 1][D / 8], float (&back)[NT][2]) {
-  const int g = lane >> 2, t = lane & 3, G = a.nq / a.nkv, n = it.rows * G;
+__device__ __forceinline__ void load_queries4(const TreeArgs& a, const Unit& it, int warp, int lane,
+                                              QueryTile<D, NT, F32>& to) {
+  constexpr int N = D / 32;  // dims of a lane
+  const int G = a.nq / a.nkv;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int q = it.qt * 8 * NT + 8 * nt + g;
-    float x[D / 4];
-#pragma unroll
-    for (int e = 0; e < D / 4; ++e) x[e] = 0.f;
-    if (q < n) {
+    const int q = it.qt * 8 * NT + 8 * nt + warp;
+    float x[N] = {};
+    if (q < it.rows * G) {
       const int i = divide_group(a, q), h = it.g * G + (q - i * G);
-      const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + D / 4 * t;
+      const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + N * lane;
       if constexpr (F32) {
 #pragma unroll
-        for (int e = 0; e < D / 4; e += 4) {
-          const float4 v = *reinterpret_cast<const float4*>((const float*)a.q + at + e);
-          x[e] = v.x, x[e + 1] = v.y, x[e + 2] = v.z, x[e + 3] = v.w;
+        for (int e = 0; e < N; e += 2) {
+          const float2 v = *reinterpret_cast<const float2*>((const float*)a.q + at + e);
+          x[e] = v.x, x[e + 1] = v.y;
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < D / 4; e += 8) {
-          const uint4 v = *reinterpret_cast<const uint4*>((const bf16*)a.q + at + e);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            x[e + 2 * f] = __uint_as_float(w[f] << 16);
-            x[e + 2 * f + 1] = __uint_as_float(w[f] & 0xFFFF0000u);
-          }
+        for (int e = 0; e < N; e += 2) {
+          const uint32_t w = *reinterpret_cast<const uint32_t*>((const bf16*)a.q + at + e);
+          x[e] = __uint_as_float(w << 16);
+          x[e + 1] = __uint_as_float(w & 0xFFFF0000u);
         }
       }
     }
     float most = 0.f, zero = 0.f;  // 0 times every dim: NaN if one is not finite
 #pragma unroll
-    for (int e = 0; e < D / 4; ++e) {
+    for (int e = 0; e < N; ++e) {
       most = fmaxf(most, fabsf(x[e]));
       zero = fmaf(x[e], 0.f, zero);
     }
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-      zero += __shfl_xor_sync(~0u, zero, o);
-    }
+    for (int o = 1; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+    if (__any_sync(~0u, zero != zero)) zero = __uint_as_float(0x7FFFFFFFu);
     // 2^up in two factors, as up may be 163
     const int up = most > 0.f && zero == 0.f ? 14 - ilogbf(most) : 0;
     const int u0 = up / 2, u1 = up - u0;
     const float f0 = __uint_as_float((uint32_t)(127 + u0) << 23), f1 = __uint_as_float((uint32_t)(127 + u1) << 23);
+    const int t = lane >> 3, e0 = lane * N % (D / 4) / 2;  // of the lane that has these dims, its pair
 #pragma unroll
-    for (int e = 0; e < D / 8; ++e) {
+    for (int e = 0; e < N / 2; ++e) {
       const float y0 = x[2 * e] * f0 * f1 + zero, y1 = x[2 * e + 1] * f0 * f1 + zero;
-      hi[nt][e] = halves(y0, y1);
+      const uint32_t h = halves(y0, y1);
+      reinterpret_cast<uint32_t*>(&to.hi[nt][(e0 + e) / 4][4 * warp + t])[(e0 + e) % 4] = h;
       if constexpr (F32) {
-        const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&hi[nt][e]));
-        lo[nt][e] = halves(y0 - r.x, y1 - r.y);
+        const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        reinterpret_cast<uint32_t*>(&to.lo[nt][(e0 + e) / 4][4 * warp + t])[(e0 + e) % 4] = halves(y0 - r.x, y1 - r.y);
       }
     }
-    const float b = fminf(a.scale_log2 * __uint_as_float((uint32_t)(127 - u0) << 23) *
-                              __uint_as_float((uint32_t)(127 - u1) << 23), 3.4e38f);
-    back[nt][0] = __shfl_sync(~0u, b, 8 * t);
-    back[nt][1] = __shfl_sync(~0u, b, 8 * t + 4);
+    if (lane == 0)
+      to.back[8 * nt + warp] = fminf(a.scale_log2 * __uint_as_float((uint32_t)(127 - u0) << 23) *
+                                         __uint_as_float((uint32_t)(127 - u1) << 23), 3.4e38f);
   }
 }
 
@@ -164,11 +166,11 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
   const int g = lane >> 2, t = lane & 3;
   // ---- scores: the rows g and g + 8 of the product are keys k0 and k0 + 2 of the 16 ----
   const int k0 = 4 * (g >> 1) + (g & 1);
-  float s[NT][4];
+  float s[NT][4], s2[NT][4];  // (two chains of products)
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+    for (int e = 0; e < 4; ++e) s[nt][e] = s2[nt][e] = 0.f;
   uint32_t w[2][D / 32], sb[2];
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
@@ -203,8 +205,8 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
         const int at = 8 * b + 4 * c + 2 * k;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          mma16(s[nt], f, qh[nt][at], qh[nt][at + 1]);
-          if constexpr (F32) mma16(s[nt], f, ql[nt][at], ql[nt][at + 1]);
+          mma16(k ? s2[nt] : s[nt], f, qh[nt][at], qh[nt][at + 1]);
+          if constexpr (F32) mma16(k ? s[nt] : s2[nt], f, ql[nt][at], ql[nt][at + 1]);
         }
       }
     }
@@ -215,7 +217,7 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[nt][e] *= back[nt][e & 1];
+    for (int e = 0; e < 4; ++e) s[nt][e] = (s[nt][e] + s2[nt][e]) * back[nt][e & 1];
   if (p + 16 > it.L) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -343,7 +345,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint8_t* ring = smem + warp * S::NST * S::STAGE;
   float2* s_o = reinterpret_cast<float2*>(smem);                                  // [warp][pair][lane]
-  float2* s_ml = reinterpret_cast<float2*>(smem + kWarps * S::PAIRS * 32 * 8);    // [warp][query]
+  auto& s_q = *reinterpret_cast<QueryTile<D, NT, F32>*>(smem + S::AREA);
+  __shared__ float s_m[kWarps][S::Q], s_l[kWarps][S::Q];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   Unit it;
@@ -378,9 +381,24 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
     };
 #pragma unroll 1
     for (int k = 0; k < S::NST - 1; ++k) load(k);
+    load_queries4<D, NT, F32>(a, it, warp, lane, s_q);
+    __syncthreads();
     uint32_t qh[NT][D / 8], ql[F32 ? NT : 1][D / 8];
     float back[NT][2];
-    load_queries4<D, NT, F32>(a, it, lane, qh, ql, back);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) {
+        const uint4 h = s_q.hi[nt][e][lane];
+        qh[nt][4 * e] = h.x, qh[nt][4 * e + 1] = h.y, qh[nt][4 * e + 2] = h.z, qh[nt][4 * e + 3] = h.w;
+        if constexpr (F32) {
+          const uint4 l = s_q.lo[nt][e][lane];
+          ql[nt][4 * e] = l.x, ql[nt][4 * e + 1] = l.y, ql[nt][4 * e + 2] = l.z, ql[nt][4 * e + 3] = l.w;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) back[nt][e] = s_q.back[8 * nt + 2 * (lane & 3) + e];
+    }
     Sums<D, NT> x;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -400,23 +418,30 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
       __syncwarp();
       load(k + S::NST - 1);
     }
-    // ---- the warps' parts, over the rings ----
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) x.l[nt][e] += __shfl_xor_sync(~0u, x.l[nt][e], o);
+    // ---- the warps' parts, brought to one reference, over the rings ----
     asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (lane < 4)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) s_m[warp][8 * nt + 2 * lane + e] = x.m[nt][e];
     __syncthreads();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
+        const int query = 8 * nt + 2 * (lane & 3) + e;
+        float M = -INFINITY, l = x.l[nt][e];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w][query]);
+        const float f = part_weight(x.m[nt][e], M);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(~0u, l, o);
+        if (lane < 4) s_l[warp][query] = l * f;  // (a NaN stays)
 #pragma unroll
         for (int mt = 0; mt < D / 16; ++mt)
-          s_o[(warp * S::PAIRS + (nt * (D / 16) + mt) * 2 + e) * 32 + lane] = make_float2(x.o[nt][mt][e], x.o[nt][mt][2 + e]);
-        if (lane < 4) s_ml[warp * S::Q + 8 * nt + 2 * lane + e] = make_float2(x.m[nt][e], x.l[nt][e]);
+          s_o[(warp * S::PAIRS + (nt * (D / 16) + mt) * 2 + e) * 32 + lane] =
+              make_float2(x.o[nt][mt][e] * f, x.o[nt][mt][2 + e] * f);
       }
     __syncthreads();
     const bool done = it.t0 == 0 && it.t1 == it.tiles;
@@ -426,22 +451,23 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
       place_of<D>(j / 32, lane, query, dim);
       const int q = it.qt * S::Q + query;
       if (q >= it.rows * G) continue;
-      float M = -INFINITY, l = 0.f;
+      float l = 0.f;
       float2 o = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_ml[w * S::Q + query].x);
-#pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float2 ml = s_ml[w * S::Q + query], v = s_o[w * S::PAIRS * 32 + j];
-        const float f = part_weight(ml.x, M);
-        l = fmaf(ml.y, f, l);  // (a NaN stays)
-        o.x = fmaf(v.x, f, o.x);
-        o.y = fmaf(v.y, f, o.y);
+        const float2 v = s_o[w * S::PAIRS * 32 + j];
+        l += s_l[w][query];
+        o.x += v.x;
+        o.y += v.y;
       }
+      float M = -INFINITY;
+      if (!done || dim == 0)
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w][query]);
       if (done) {
         const int i = divide_group(a, q), h = it.g * G + (q - i * G);
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        write_pair<F32>(a, l == l ? make_float2(o.x * inv, o.y * inv) : make_float2(l, l), ((size_t)(it.r0 + i) * a.nq + h) * D + dim);
+        write_pair<F32>(a, make_float2(o.x * inv, o.y * inv), ((size_t)(it.r0 + i) * a.nq + h) * D + dim);
         if (dim == 0 && a.lse) a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M - kUp, l);
       } else {
         ws.o[part * S::PAIRS * 32 + j] = o;
@@ -457,48 +483,79 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
   }
 }
 
-// The parts of items cut between CTAs, joined in CTA order: a block for an item.
+// The parts of items cut between CTAs, joined in CTA order.  A lane has two dims of a query,
+// `split` warps of a block share an item's parts of 32 such, a block has 8 / split times 32.
 template <int D, int NT, bool F32>
-__global__ void __launch_bounds__(kThreads) join4_kernel(const __grid_constant__ TreeArgs a, Work ws, int ctas, int turn) {
+__global__ void __launch_bounds__(kThreads) join4_kernel(const __grid_constant__ TreeArgs a, Work ws, int ctas, int turn, int split) {
   using S = Shape<D, NT, F32>;
   __shared__ UnitPlan plan;
-  const int tid = threadIdx.x, lane = tid & 31;
-  const int b = blockIdx.z, g = blockIdx.y, qt = blockIdx.x;
+  __shared__ float2 s_o[kWarps][32], s_ml[kWarps][32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, each = S::PAIRS * split / kWarps;
+  const int b = blockIdx.z, g = blockIdx.y, qt = blockIdx.x / each;
+  const int pair = blockIdx.x % each * (kWarps / split) + warp / split, first_part = warp % split;
   const int r0 = a.rm.start[b], rows = a.rm.start[b + 1] - r0, G = a.nq / a.nkv;
   ptx::griddep_launch_dependents();
-  if (qt * S::Q < rows * G) {
-    if (tid < 32) make_plan(a, S::Q, turn, lane, plan, false);
-    __syncthreads();
-  }
-  ptx::griddep_wait();
-  if (qt * S::Q >= rows * G) return;
-  const int tiles = plan.tiles[b];
-  const int first = plan.unit[b] + (g * plan.qts[b] + qt) * (tiles + turn) + turn;
+  const bool some = qt * S::Q < rows * G;
+  if (some && tid < 32) make_plan(a, S::Q, turn, lane, plan, false);
+  __syncthreads();
+  const int tiles = some ? plan.tiles[b] : 0;
+  const int first = some ? plan.unit[b] + (g * plan.qts[b] + qt) * (tiles + turn) + turn : 0;
   const int c0 = tiles > 0 ? unit_owner(plan, first, ctas) : 0;
   const int n = tiles > 0 ? unit_owner(plan, first + tiles - 1, ctas) - c0 + 1 : 0;
+  ptx::griddep_wait();
   if (n <= 1) return;  // skipped, or written by its CTA
   auto part = [&](int k) { return (size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0); };
-  for (int j = tid; j < S::PAIRS * 32; j += kThreads) {
-    int query, dim;
-    place_of<D>(j / 32, lane, query, dim);
-    const int q = qt * S::Q + query;
-    if (q >= rows * G) continue;
-    float M = -INFINITY, l = 0.f;
-    float2 o = make_float2(0.f, 0.f);
-    for (int k = 0; k < n; ++k) M = fmaxf(M, __ldcg(&ws.ml[part(k) * S::Q + query]).x);
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) {
-      const float2 ml = __ldcg(&ws.ml[part(k) * S::Q + query]), v = __ldcg(&ws.o[part(k) * S::PAIRS * 32 + j]);
+  int query, dim;
+  place_of<D>(pair, lane, query, dim);
+  const int q = qt * S::Q + query;
+  float M = -INFINITY, l = 0.f;
+  float2 o = make_float2(0.f, 0.f);
+  constexpr int U = 5;  // parts in flight
+  for (int k0 = first_part; k0 < n; k0 += U * split) {
+    float2 ml[U], v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * split;
+      ml[u] = make_float2(-INFINITY, 0.f);
+      v[u] = make_float2(0.f, 0.f);
+      if (k < n && q < rows * G) {
+        ml[u] = __ldcg(&ws.ml[part(k) * S::Q + query]);
+        v[u] = __ldcg(&ws.o[(part(k) * S::PAIRS + pair) * 32 + lane]);
+      }
+    }
+    const float before = M;
+#pragma unroll
+    for (int u = 0; u < U; ++u) M = fmaxf(M, ml[u].x);
+    const float w = part_weight(before, M);
+    l *= w, o.x *= w, o.y *= w;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = part_weight(ml[u].x, M);
+      l = fmaf(ml[u].y, f, l);
+      o.x = fmaf(v[u].x, f, o.x);
+      o.y = fmaf(v[u].y, f, o.y);
+    }
+  }
+  if (split > 1) {
+    s_o[warp][lane] = o;
+    s_ml[warp][lane] = make_float2(M, l);
+    __syncthreads();
+    if (first_part > 0) return;
+    for (int w = 1; w < split; ++w) M = fmaxf(M, s_ml[warp + w][lane].x);
+    l = 0.f, o = make_float2(0.f, 0.f);
+    for (int w = 0; w < split; ++w) {
+      const float2 ml = s_ml[warp + w][lane], v = s_o[warp + w][lane];
       const float f = part_weight(ml.x, M);
       l = fmaf(ml.y, f, l);
       o.x = fmaf(v.x, f, o.x);
       o.y = fmaf(v.y, f, o.y);
     }
-    const int i = divide_group(a, q), h = g * G + (q - i * G);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    write_pair<F32>(a, l == l ? make_float2(o.x * inv, o.y * inv) : make_float2(l, l), ((size_t)(r0 + i) * a.nq + h) * D + dim);
-    if (dim == 0 && a.lse) a.lse[(size_t)(r0 + i) * a.nq + h] = row_lse(M - kUp, l);
   }
+  if (q >= rows * G) return;
+  const int i = divide_group(a, q), h = g * G + (q - i * G);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  write_pair<F32>(a, make_float2(o.x * inv, o.y * inv), ((size_t)(r0 + i) * a.nq + h) * D + dim);
+  if (dim == 0 && a.lse) a.lse[(size_t)(r0 + i) * a.nq + h] = row_lse(M - kUp, l);
 }
 
 // Items of at most this many tiles are each done by one CTA.
@@ -526,7 +583,10 @@ cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sm
   const int ctas = (int)std::min<int64_t>(units, 2 * sms), turn = 0;
   const cudaError_t f = launch_pdl(attn4_kernel<D, NT, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kShares, turn);
   if (f != cudaSuccess) return f;
-  return launch_pdl(join4_kernel<D, NT, F32>, each, dim3(kThreads), 0, st, 1, a, ws, ctas, turn);
+  const int64_t parts = ctas / std::max<int64_t>(items, 1);
+  const int split = parts > 20 ? 8 : parts > 10 ? 4 : parts > 5 ? 2 : 1;
+  const dim3 joins(each.x * (S::PAIRS * split / kWarps), each.y, each.z);
+  return launch_pdl(join4_kernel<D, NT, F32>, joins, dim3(kThreads), 0, st, 1, a, ws, ctas, turn, split);
 }
 
 template <int D>

@@ -2,7 +2,6 @@
 // (as2d_cache4_write, as2d_cache4_read).
 //
 // A thread has 8 dims: 16 bytes of bf16, a word of codes; two threads share a scale.
-// bf16 values and scales of four bits decide every code exactly in 32 bits (code_of).
 // Bound by memory: 2.56 bytes a value.
 #include <algorithm>
 
@@ -28,11 +27,14 @@ __device__ __forceinline__ void write8(uint4 v, uint32_t& codes, uint8_t& scale,
     odd = odd || !(fabsf(x[e]) <= 3.4028235e38f);
   }
   most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-  float units;
-  const float s = scale_of(__fdiv_rn(most, 7.f), units);
-  int c[8];
+  const float s = exact_scale(most), inv = reciprocal(s);
+  uint32_t c[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) c[e] = x[e] != x[e] ? 0 : code_of(x[e], s);
+  for (int e = 0; e < 8; ++e) c[e] = code_bits(on_grid(x[e], inv));
+  if (odd)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (x[e] != x[e]) c[e] = code_bits(0.f);
   codes = code_word(c);
   scale = scale_byte(s);
 }
