@@ -696,7 +696,7 @@ typedef struct as2d_cache4 {
    q_norm, k_norm: device float [head_dim] or NULL: each head of a row is divided by
    its root mean square (mean of squares + eps; eps >= 0) and multiplied by these gains.
    rotary: dims 0 .. rotary - 1 of each head of q and k are rotated by position, dim j
-   with dim j + rotary / 2 by the angle position theta^(-2j / rotary); a multiple of 16
+   with dim j + rotary / 2 by the angle position theta^(-2j / rotary); a multiple of 32
    of at most head_dim, 0 for none.  theta > 0.  positions: device int32 [sum
    rows], or NULL: kv_len[b] + i for row i.  rows: host int32 [batch]; kv_len: device
    int32 [batch]. */

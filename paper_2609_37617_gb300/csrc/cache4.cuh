@@ -62,22 +62,27 @@ __device__ __forceinline__ uint32_t code_word(const uint32_t (&c)[8]) {
 
 // ---- decoding -------------------------------------------------------------------
 //
-// (64 + n) s - 72 s = (n - 8) s in one fused multiply-add of two halves: the
-// significand of 64 + n holds the code n in bits 4 .. 7.
+// A code n over the significand of a half whose exponent gives its place the value 1: 64 + n in bits
+// 4 .. 7, of which one fused multiply-add makes (64 + n) s - 72 s = (n - 8) s; and 1024 + n in bits 0
+// .. 3, less 1032 first (1032 s is no half).  So a word's eight codes take one shift and four
+// logic operations, the rest runs where products do.  All steps are exact.
 
-// s of a scale byte, twice, and -72 s.
-__device__ __forceinline__ __half2 scale_pair(uint32_t bytes) {  // two bytes, 16 bits apart
-  const uint32_t b = (bytes & 0x00FF00FFu) << 7;
+// s of two scale bytes (16 bits apart), and -72 s.
+__device__ __forceinline__ __half2 scale_pair(uint32_t bytes) {
+  const uint32_t b = bytes * 128u;
   return __hmin2(*reinterpret_cast<const __half2*>(&b), __float2half2_rn(kMaxScale4));
 }
 __device__ __forceinline__ __half2 scale_shift(__half2 s) { return __hmul2(s, __float2half2_rn(-72.f)); }
 
 // The four pairs of codes in a word (each 16 bits apart): pair e is at bits 4e.
 __device__ __forceinline__ void decode_word(uint32_t w, __half2 s, __half2 shift, __half2 (&v)[4]) {
-  const uint32_t m = 0x00F000F0u, one = 0x54005400u;
-  const uint32_t x[4] = {((w << 4) & m) | one, (w & m) | one, ((w >> 4) & m) | one, ((w >> 8) & m) | one};
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = __hfma2(*reinterpret_cast<const __half2*>(&x[e]), s, shift);
+  for (int e = 0; e < 4; e += 2) {
+    const uint32_t u = e ? w >> 8 : w;
+    const uint32_t x = (u & 0x000F000Fu) | 0x64006400u, y = (u & 0x00F000F0u) | 0x54005400u;
+    v[e] = __hmul2(__hadd2(*reinterpret_cast<const __half2*>(&x), __float2half2_rn(-1032.f)), s);
+    v[e + 1] = __hfma2(*reinterpret_cast<const __half2*>(&y), s, shift);
+  }
 }
 
 }  // namespace as2d

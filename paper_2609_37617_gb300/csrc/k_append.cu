@@ -6,18 +6,17 @@
 // Queries go out, keys and values into the cache at the request's length, in bf16 or in 4
 // bits.
 //
-// A thread has 8 dims of a head (16 bytes of bf16; a word of codes), D / 8 threads a head;
-// sums of squares and the other halves of the rotation go through shuffles.  Angles: a
-// position times 2^64 turns of its frequency, modulo 2^64, is the angle in turns whatever the
-// position, to 2^-64 of a turn and the frequency's own rounding; a row's sines and
-// cosines are computed once, in shared memory.
+// A thread has 8 dims of a head, D / 8 threads a head: four and those that they are paired with
+// in the rotation, so that only sums of squares, and the largest magnitudes of 16 dims, go through
+// shuffles.  Angles: a position times 2^64 turns of its frequency, modulo 2^64, is the angle in
+// turns whatever the position, to 2^-64 of a turn and the frequency's own rounding.
 //
 // Codes are those of the exact values: a value or a scale that 32-bit arithmetic finds nearer to
 // the border of two codes than its error (some 2e-6 of them) has its head computed once more in
 // 64 bits.
 //
 // Bound by memory: each value is read and written once.
-#include <cmath>
+#include <algorithm>
 
 #include "cache4.cuh"
 #include "ptx_sm100.cuh"
@@ -25,112 +24,127 @@
 namespace as2d {
 namespace {
 
-constexpr int kThreads = 256, kMostRows = 4;
+constexpr int kThreads = 256;
+constexpr int kAtOnce = 3;  // heads of a thread whose loads are on their way together
 // How far a finished value may be from its exact one, over |y_j| + |y_j'| of its pair: the mean
 // square, its root, the division and two products add 11 roundings of 2^-24, sine and cosine (one
 // step, and an angle rounded to 2^-25 of a half turn) 4, the rotation 2.
 constexpr float kOff = 1.5e-6f;
 
-// 8 dims as they are in memory.
+// Four dims as they are in memory.
 template <bool F32>
 struct Raw {
-  uint4 w[F32 ? 2 : 1];
+  uint32_t w[F32 ? 4 : 2];
 };
 template <bool F32>
-__device__ __forceinline__ void load8(const void* base, int64_t at, Raw<F32>& x) {
-  const uint4* p = reinterpret_cast<const uint4*>((const char*)base + at * (F32 ? 4 : 2));
-  x.w[0] = __ldcs(p);
-  if constexpr (F32) x.w[1] = __ldcs(p + 1);
+__device__ __forceinline__ void load4(const void* base, int64_t at, Raw<F32>& x) {
+  if constexpr (F32) {
+    const uint4 v = __ldcs(reinterpret_cast<const uint4*>((const float*)base + at));
+    x.w[0] = v.x, x.w[1] = v.y, x.w[2] = v.z, x.w[3] = v.w;
+  } else {
+    const uint2 v = __ldcs(reinterpret_cast<const uint2*>((const bf16*)base + at));
+    x.w[0] = v.x, x.w[1] = v.y;
+  }
 }
 template <bool F32>
-__device__ __forceinline__ void floats(const Raw<F32>& r, float (&x)[8]) {
-  const uint4 a = r.w[0];
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-  if constexpr (F32) {
-    const uint4 b = r.w[1];
-    const uint32_t v[4] = {b.x, b.y, b.z, b.w};
+__device__ __forceinline__ void floats(const Raw<F32>& r, float* x) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]), x[4 + e] = __uint_as_float(v[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = __uint_as_float(w[e] << 16);
-      x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-    }
-  }
+  for (int e = 0; e < 4; ++e)
+    x[e] = __uint_as_float(F32 ? r.w[F32 ? e : 0] : e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
+}
+__device__ __forceinline__ void store4(bf16* to, const float* y) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(y[0], y[1]), b = __floats2bfloat162_rn(y[2], y[3]);
+  *reinterpret_cast<uint2*>(to) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+__device__ __forceinline__ void store4(float* to, const float* y) {
+  *reinterpret_cast<float4*>(to) = make_float4(y[0], y[1], y[2], y[3]);
 }
 
-__device__ __forceinline__ void store8(bf16* to, const float (&y)[8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const __nv_bfloat162 t = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
-    w[e] = *reinterpret_cast<const uint32_t*>(&t);
-  }
-  *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void store8(float* to, const float (&y)[8]) {
-  reinterpret_cast<float4*>(to)[0] = make_float4(y[0], y[1], y[2], y[3]);
-  reinterpret_cast<float4*>(to)[1] = make_float4(y[4], y[5], y[6], y[7]);
+// The two fours of dims that thread c of a head has: 4 c of the rotated dims' first half and those they
+// are paired with; behind the rotated dims eight side by side.
+struct Dims {
+  int a, b;
+  bool pair;
+};
+__device__ __forceinline__ Dims dims_of(int c, int half) {
+  if (4 * c < half) return {4 * c, half + 4 * c, true};
+  const int d = 8 * c;  // (2 half + 8 (c - half / 4))
+  return {d, d + 4, false};
 }
 
-// Those of 8 dims of a head that `which` has bits for, in 64 bits.  By whole warps, whose heads
-// may be keys and values: every thread takes part in the shuffles.
+__device__ __forceinline__ uint64_t turns_of(const AppendArgs& a, int position, int j) {
+  return (uint64_t)(int64_t)position * a.turn[j];
+}
+
+// Those of a head's dims (y[0 .. 3] at d.a, y[4 .. 7] at d.b) that `which` has bits for, in 64
+// bits.  By whole warps, whose heads may be keys and values: every thread takes part in the shuffles.
 template <int D>
 __device__ __noinline__ void finish_exactly(const AppendArgs& a, const float (&x)[8], const float* gain, bool turn,
-                                            int position, int c, uint32_t which, double (&y)[8]) {
-  constexpr int C = D / 8;
+                                            int position, Dims d, uint32_t which, double (&y)[8]) {
   double ss = 0.0;
   for (int e = 0; e < 8; ++e) ss = fma((double)x[e], (double)x[e], ss);
-  for (int o = C / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
+  for (int o = D / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
   const double f = 1.0 / sqrt(ss / D + (double)a.eps);
-  const int h = a.half, d0 = 8 * c, other = d0 < h ? c + h / 8 : c - h / 8;
-  const int from = (threadIdx.x & 31 & ~(C - 1)) | (other & (C - 1));
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (!((which >> e) & 1)) continue;  // (the same in every thread)
-    double v = gain ? (double)x[e] * f * (double)gain[8 * c + e] : (double)x[e];
-    const double z = __shfl_sync(~0u, v, from);
-    if (turn && d0 < 2 * h) {
-      const int j = (d0 < h ? d0 : d0 - h) + e;
+  for (int e = 0; e < 4; ++e) {
+    if (!((which >> e | which >> (4 + e)) & 1)) continue;
+    double u = x[e], v = x[4 + e];
+    if (gain) u *= f * (double)gain[d.a + e], v *= f * (double)gain[d.b + e];
+    if (turn && d.pair) {
       double sn, cs;
-      sincospi((double)(int64_t)((uint64_t)(int64_t)position * a.turn[j]) * 0x1p-63, &sn, &cs);
-      v = d0 < h ? v * cs - z * sn : v * cs + z * sn;
+      sincospi((double)(int64_t)turns_of(a, position, d.a + e) * 0x1p-63, &sn, &cs);
+      const double w = u * cs - v * sn;
+      v = v * cs + u * sn;
+      u = w;
     }
-    __syncwarp();
-    y[e] = v;
+    y[e] = u, y[4 + e] = v;
   }
 }
 
-// What 8 dims become in 4 bits.
+// What 8 dims (two fours) become in 4 bits.
 struct Coded {
-  float s;
+  float s[2];
   uint32_t c[8];  // code_bits
 };
 
+// The larger of a head's two fours' numbers with the other fours of their 16 dims.
+template <typename T>
+__device__ __forceinline__ void over_blocks(T& u, T& v, bool pair) {
+  const T u1 = __shfl_xor_sync(~0u, u, 1), v1 = __shfl_xor_sync(~0u, v, 1);
+  u = u1 > u ? u1 : u, v = v1 > v ? v1 : v;
+  const T u2 = __shfl_xor_sync(~0u, u, 2), v2 = __shfl_xor_sync(~0u, v, 2);
+  if (pair)
+    u = u2 > u ? u2 : u, v = v2 > v ? v2 : v;
+  else
+    u = v = v > u ? v : u;
+}
+
 // off: how far each of the values may be from its exact one (0: it is exact, of bf16).  Returns
-// bits of the dims whose code, and 2^8 if the scale, is that near to a border.
-__device__ __forceinline__ uint32_t code8(const float (&y)[8], const float (&off)[8], Coded& to, bool& odd) {
-  float most = 0.f, far = 0.f;
+// bits of the dims whose code, and 2^8 if a scale, is that near to a border.
+__device__ __forceinline__ uint32_t code8(const float (&y)[8], const float (&off)[8], bool pair, Coded& to, bool& odd) {
+  float most[2] = {0.f, 0.f}, far[2] = {0.f, 0.f};
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    most = fmaxf(most, fabsf(y[e]));
+    most[e / 4] = fmaxf(most[e / 4], fabsf(y[e]));
     odd = odd || !(fabsf(y[e]) <= 3.4028235e38f);
-    far = fmaxf(far, off[e]);
+    far[e / 4] = fmaxf(far[e / 4], off[e]);
   }
-  most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-  far = fmaxf(far, __shfl_xor_sync(~0u, far, 1));
-  const float t = most * (1.f / 7.f);
-  float steps;
-  const float s = scale_of(t, steps), exact = exact_scale(most), inv_step = steps > 0.f ? steps / t : 0.f;
-  uint32_t near = far > 0.f && fabsf(fabsf(steps - rintf(steps)) - 0.5f) <= (far + 2.5e-7f * t) * inv_step ? 256u : 0u;
-  to.s = far > 0.f ? s : exact;
-  const float inv = reciprocal(to.s);
+  over_blocks(most[0], most[1], pair);
+  over_blocks(far[0], far[1], pair);
+  uint32_t near = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float q = y[e] * inv;
-    if (off[e] > 0.f && fabsf(fabsf(q - rintf(q)) - 0.5f) <= fmaf(off[e], inv, 4e-6f)) near |= 1u << e;
-    to.c[e] = code_bits(off[e] > 0.f ? q : on_grid(y[e], inv));
+  for (int k = 0; k < 2; ++k) {
+    const float t = most[k] * (1.f / 7.f);
+    float steps;
+    const float s = scale_of(t, steps), exact = exact_scale(most[k]), inv_step = steps > 0.f ? __fdividef(steps, t) : 0.f;
+    if (far[k] > 0.f && fabsf(fabsf(steps - rintf(steps)) - 0.5f) <= (far[k] + 2.5e-7f * t) * inv_step * 1.001f) near |= 256u;
+    to.s[k] = far[k] > 0.f ? s : exact;
+    const float inv = reciprocal(to.s[k]);
+#pragma unroll
+    for (int e = 4 * k; e < 4 * k + 4; ++e) {
+      const float q = y[e] * inv;
+      if (off[e] > 0.f && fabsf(fabsf(q - rintf(q)) - 0.5f) <= fmaf(off[e], inv, 4e-6f)) near |= 1u << e;
+      to.c[e] = code_bits(off[e] > 0.f ? q : on_grid(y[e], inv));
+    }
   }
   if (odd)
 #pragma unroll
@@ -140,149 +154,160 @@ __device__ __forceinline__ uint32_t code8(const float (&y)[8], const float (&off
 }
 
 // The same of exact values: with bit 2^8 of `which` all of it, else those codes that it has bits for.
-__device__ __noinline__ void code8_exactly(const double (&y)[8], uint32_t which, Coded& to) {
+__device__ __noinline__ void code8_exactly(const double (&y)[8], uint32_t which, bool pair, Coded& to) {
   if (which & 256u) {
-    double most = 0.0, steps;
-    for (int e = 0; e < 8; ++e) most = fmax(most, fabs(y[e]));
-    most = fmax(most, __shfl_xor_sync(~0u, most, 1));
-    to.s = scale_of(most / 7.0, steps);
+    double most[2] = {0.0, 0.0}, steps;
+    for (int e = 0; e < 8; ++e) most[e / 4] = fmax(most[e / 4], fabs(y[e]));
+    over_blocks(most[0], most[1], pair);
+    for (int k = 0; k < 2; ++k) to.s[k] = scale_of(most[k] / 7.0, steps);
   }
   for (int e = 0; e < 8; ++e)
     if ((which >> e) & 1) {
-      const double q = to.s > 0.f ? y[e] / (double)to.s : 0.0;
+      const double s = to.s[e / 4], q = s > 0.0 ? y[e] / s : 0.0;
       to.c[e] = code_bits(y[e] == y[e] ? (float)rint(fmin(fmax(q, -7.0), 7.0)) : 0.f);
     }
 }
 
-// What a thread has of one head of a row of a block.
-struct Place {
-  int i, head;   // row of the block, head of the row: queries, keys, values
-  bool live;     // there is such a head
-  bool isq, isv;
-  int hh;        // head among its kind
-};
+// Four codes, as the even four of a word.
+__device__ __forceinline__ uint32_t half_word(const uint32_t* c) {
+  return __byte_perm(c[0], c[1], 0x5410) | __byte_perm(c[2], c[3], 0x5410) << 4;
+}
 
-// A block: R rows, U heads at once a thread.
-template <int D, bool F32, bool FOUR, int U>
-__global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs a, int R) {
-  constexpr int C = D / 8, G = kThreads / C;  // threads of a head, heads at once
-  __shared__ float2 s_turn[kMostRows][64];
-  __shared__ int s_req[kMostRows], s_at[kMostRows], s_pos[kMostRows];
-  const int tid = threadIdx.x, c = tid % C, H = a.nq + 2 * a.nkv;
-  const int r0 = blockIdx.x * R, n = min(R, a.rm.rows - r0), units = n * H;
+// `per` groups of C threads to a row, each its heads in turn (a row's sines and cosines, and the
+// gains, stay in registers).
+template <int D, bool F32, bool FOUR>
+__global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs a, int per) {
+  constexpr int C = D / 8, G = kThreads / C;  // threads of a head, groups of them
+  const int tid = threadIdx.x, c = tid % C, group = tid / C;
+  const int H = a.nq + 2 * a.nkv, r = blockIdx.x * (G / per) + group / per, h0 = group % per;
+  const Dims d = dims_of(c, a.half);
+  const bool row_live = r < a.rm.rows;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  auto place = [&](int u) {
-    Place p;
-    p.live = u < units;
-    p.i = p.live ? u / H : 0;
-    p.head = p.live ? u - p.i * H : 0;
-    p.isq = p.head < a.nq, p.isv = p.head >= a.nq + a.nkv;
-    p.hh = p.isq ? p.head : p.head - a.nq - (p.isv ? a.nkv : 0);
-    return p;
-  };
-  Raw<F32> raw[U];
-  auto load = [&](int u0) {
+  Raw<F32> raw[kAtOnce][2];
+  auto load = [&](int h) {
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const Place p = place(u0 + k * G + tid / C);
-      const int64_t stride = p.isq ? a.q_stride : p.isv ? a.v_stride : a.k_stride;
-      if (p.live) load8(p.isq ? a.q : p.isv ? a.v : a.k, (r0 + p.i) * stride + p.hh * D + 8 * c, raw[k]);
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int head = h + k * per;
+      const bool isq = head < a.nq, isv = head >= a.nq + a.nkv;
+      const void* from = isq ? a.q : isv ? a.v : a.k;
+      const int64_t at = r * (isq ? a.q_stride : isv ? a.v_stride : a.k_stride) +
+                         (isq ? head : isv ? head - a.nq - a.nkv : head - a.nq) * D;
+#pragma unroll
+      for (int e = 0; e < (F32 ? 4 : 2); ++e) raw[k][0].w[e] = raw[k][1].w[e] = 0;
+      if (row_live && head < H) {
+        load4(from, at + d.a, raw[k][0]);
+        load4(from, at + d.b, raw[k][1]);
+      }
     }
   };
-  load(0);
-  if (tid < n) {
-    const int r = r0 + tid, b = row_request(a.rm, r), L = a.len[b], rows = a.rm.start[b + 1] - a.rm.start[b];
-    const int i = r - a.rm.start[b];
-    const bool fits = rows_fit(L, rows, a.cap);
-    if (!fits && i == 0 && a.err) atomicOr(a.err, kErrCapacity);
-    s_req[tid] = b;
-    s_at[tid] = fits ? L + i : -1;
-    s_pos[tid] = a.positions ? a.positions[r] : fits ? L + i : 0;
+  load(h0);
+  // the gains of these dims, queries' and keys'
+  float gain[2][8];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float* g = k ? a.k_norm : a.q_norm;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) gain[k][e] = 1.f;
+    if (g) {
+      const float4 u = *reinterpret_cast<const float4*>(g + d.a), v = *reinterpret_cast<const float4*>(g + d.b);
+      gain[k][0] = u.x, gain[k][1] = u.y, gain[k][2] = u.z, gain[k][3] = u.w;
+      gain[k][4] = v.x, gain[k][5] = v.y, gain[k][6] = v.z, gain[k][7] = v.w;
+    }
   }
-  __syncthreads();
-  for (int t = tid; t < n * a.half; t += kThreads) {
-    const int i = t / a.half, j = t - i * a.half;
-    const uint64_t turns = (uint64_t)(int64_t)s_pos[i] * a.turn[j];
-    float2 v;
-    sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &v.y, &v.x);
-    s_turn[i][j] = v;
+  int b = 0, at = -1, position = 0;
+  if (row_live) {
+    b = row_request(a.rm, r);
+    const int L = a.len[b], i = r - a.rm.start[b];
+    const bool fits = rows_fit(L, a.rm.start[b + 1] - a.rm.start[b], a.cap);
+    if (!fits && i == 0 && h0 == 0 && c == 0 && a.err) atomicOr(a.err, kErrCapacity);
+    at = fits ? L + i : -1;
+    position = a.positions ? a.positions[r] : fits ? L + i : 0;
   }
-  __syncthreads();
+  float sn[4], cs[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    sn[e] = 0.f, cs[e] = 1.f;
+    if (d.pair) sincospif((float)(int32_t)(turns_of(a, position, d.a + e) >> 32) * 0x1p-31f, &sn[e], &cs[e]);
+  }
   bool odd = false;
-  const int h = a.half, d0 = 8 * c, other = d0 < h ? c + h / 8 : c - h / 8;
-  const int from = (tid & 31 & ~(C - 1)) | (other & (C - 1));
-  for (int u0 = 0; u0 < units; u0 += U * G) {
-    if (u0 > 0) load(u0);
+  const int rounds = (H + per - 1) / per;
+#pragma unroll 1
+  for (int t0 = 0; t0 < rounds; t0 += kAtOnce) {
+    if (t0 > 0) load(h0 + t0 * per);
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      if (u0 + k * G >= units) break;
-      // (threads past the last unit take part in the shuffles)
-      const Place p = place(u0 + k * G + tid / C);
-      const bool live = p.live && s_at[p.i] >= 0;
-      const float* gain = p.isq ? a.q_norm : p.isv ? nullptr : a.k_norm;
-      float y[8], off[8];  // off: how far a value is from the exact one, at most (4 bits)
-      float ss = 0.f, x[8];
-      floats<F32>(raw[k], x);
-      if (!p.live)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (t0 + k >= rounds) break;
+      // (threads past the last head take part in the shuffles)
+      const int head = h0 + (t0 + k) * per;
+      const bool live = at >= 0 && head < H, isq = head < a.nq, isv = head >= a.nq + a.nkv;
+      const int hh = isq ? head : head - a.nq - (isv ? a.nkv : 0);
+      const bool norm = isq ? a.q_norm != nullptr : !isv && a.k_norm != nullptr;
+      float x[8], y[8], off[8];  // off: how far a value is from the exact one, at most (4 bits)
+      floats<F32>(raw[k][0], x);
+      floats<F32>(raw[k][1], x + 4);
+      float ss = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
 #pragma unroll
       for (int o = C / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
-      if (gain) {
-        const float f = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-        const float4 g0 = reinterpret_cast<const float4*>(gain)[2 * c], g1 = reinterpret_cast<const float4*>(gain)[2 * c + 1];
-        const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+      const float f = norm ? 1.f / sqrtf(ss * (1.f / D) + a.eps) : 1.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = x[e] * f * g[e];
-      } else {
+      for (int e = 0; e < 8; ++e) y[e] = norm ? x[e] * f * (isq ? gain[0][e] : gain[1][e]) : x[e];
+      const bool turned = d.pair && !isv;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = x[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) off[e] = gain || F32 ? kOff * fabsf(y[e]) : 0.f;
-      if (h > 0) {
-        const bool turned = !p.isv && d0 < 2 * h;
-        const float2* turn = s_turn[p.i] + (d0 < h ? d0 : d0 - h);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float z = __shfl_sync(~0u, y[e], from);
-          if (turned) {
-            const float2 t = turn[e];
-            if (FOUR) off[e] = kOff * (fabsf(y[e]) + fabsf(z));
-            y[e] = d0 < h ? y[e] * t.x - z * t.y : y[e] * t.x + z * t.y;
-          }
+      for (int e = 0; e < 4; ++e) {
+        const float u = y[e], v = y[4 + e];
+        if (FOUR) {
+          off[e] = norm || F32 ? kOff * fabsf(u) : 0.f;
+          off[4 + e] = norm || F32 ? kOff * fabsf(v) : 0.f;
+          if (turned) off[e] = off[4 + e] = kOff * (fabsf(u) + fabsf(v));
         }
+        y[e] = turned ? u * cs[e] - v * sn[e] : u;
+        y[4 + e] = turned ? v * cs[e] + u * sn[e] : v;
       }
       if (FOUR) {
         Coded to;
         bool strange = false;
-        const bool mine = live && !p.isq;
-        const uint32_t near = code8(y, off, to, strange);
+        const bool mine = live && !isq;
+        const uint32_t near = code8(y, off, d.pair, to, strange);
         uint32_t which = __reduce_or_sync(~0u, mine ? near : 0u);
         if (which) {
           if (which & 256u) which = 511u;
           double z[8];
-          finish_exactly<D>(a, x, gain, !p.isv, s_pos[p.i], c, which, z);
-          code8_exactly(z, which, to);
+          finish_exactly<D>(a, x, norm ? (isq ? a.q_norm : a.k_norm) : nullptr, !isv, position, d, which, z);
+          code8_exactly(z, which, d.pair, to);
         }
+        // the words of codes: of paired fours a thread writes the one of its even or odd neighbours
+        const uint32_t wa = half_word(to.c), wb = half_word(to.c + 4);
+        const uint32_t there = __shfl_xor_sync(~0u, c & 1 ? wa : wb, 1);
+        const uint32_t word = !d.pair ? wa | wb << 8 : c & 1 ? there | wb << 8 : wa | there << 8;
+        const int word_at = !d.pair ? d.a / 8 : c & 1 ? (d.b - 4) / 8 : d.a / 8;
         if (mine) {
           odd = odd || strange;
-          const size_t at = (((size_t)s_req[p.i] * a.nkv + p.hh) * a.cap + s_at[p.i]) * C + c;
-          reinterpret_cast<uint32_t*>(p.isv ? a.cv4 : a.ck4)[at] = code_word(to.c);
-          if (c % 2 == 0) (p.isv ? a.cvs : a.cks)[at / 2] = scale_byte(to.s);
+          const size_t entry = ((size_t)b * a.nkv + hh) * a.cap + at;
+          reinterpret_cast<uint32_t*>(isv ? a.cv4 : a.ck4)[entry * C + word_at] = word;
+          uint8_t* scales = (isv ? a.cvs : a.cks) + entry * (D / 16);
+          if (d.pair) {
+            if (c % 4 < 2) scales[(c % 4 ? d.b : d.a) / 16] = scale_byte(to.s[c % 4]);
+          } else if (c % 2 == 0) {
+            scales[d.a / 16] = scale_byte(to.s[0]);
+          }
         }
-      } else if (live && !p.isq) {
-        store8((p.isv ? a.cv : a.ck) + (((size_t)s_req[p.i] * a.nkv + p.hh) * a.cap + s_at[p.i]) * D + 8 * c, y);
+      } else if (live && !isq) {
+        bf16* to = (isv ? a.cv : a.ck) + (((size_t)b * a.nkv + hh) * a.cap + at) * D;
+        store4(to + d.a, y);
+        store4(to + d.b, y + 4);
       }
-      if (live && p.isq) {
-        const size_t at = ((size_t)(r0 + p.i) * a.nq + p.hh) * D + 8 * c;
-        if constexpr (F32)
-          store8((float*)a.q_out + at, y);
-        else
-          store8((bf16*)a.q_out + at, y);
+      if (live && isq) {
+        const size_t to = ((size_t)r * a.nq + hh) * D;
+        if constexpr (F32) {
+          store4((float*)a.q_out + to + d.a, y);
+          store4((float*)a.q_out + to + d.b, y + 4);
+        } else {
+          store4((bf16*)a.q_out + to + d.a, y);
+          store4((bf16*)a.q_out + to + d.b, y + 4);
+        }
       }
     }
   }
@@ -291,10 +316,14 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
 
 template <int D, bool F32>
 cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
-  constexpr int U = F32 ? 2 : 3;
-  const int R = a.rm.rows <= 4 * device_sms() ? 1 : kMostRows;
-  return launch_pdl(a.ck4 ? append_kernel<D, F32, true, U> : append_kernel<D, F32, false, U>,
-                    dim3((a.rm.rows + R - 1) / R), dim3(kThreads), 0, st, 1, a, R);
+  constexpr int G = kThreads / (D / 8);
+  // few rows: as many threads to one as there are heads; many: four groups, whose sines, cosines and
+  // gains serve all their heads
+  const int H = a.nq + 2 * a.nkv;
+  int per = 4;
+  while (per < G && per < H && (int64_t)a.rm.rows * per / G < 2 * device_sms()) per *= 2;
+  return launch_pdl(a.ck4 ? append_kernel<D, F32, true> : append_kernel<D, F32, false>,
+                    dim3((a.rm.rows + G / per - 1) / (G / per)), dim3(kThreads), 0, st, 1, a, per);
 }
 
 }  // namespace

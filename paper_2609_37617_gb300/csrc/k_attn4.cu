@@ -38,7 +38,8 @@ struct Shape {
   static constexpr int Q = 8 * NT;                         // queries of a tile
   static constexpr int CODES = 16 * D / 2, SCALES = D;     // bytes of a warp's 16 keys (or values)
   static constexpr int STAGE = 2 * (CODES + SCALES);
-  static constexpr int NST = NT == 1 && !F32 ? 5 : 8;
+  static constexpr int Z = NT == 1 ? 2 : 1;                // slices together
+  static constexpr int NST = 10;
   static constexpr int RING = kWarps * NST * STAGE;
   static constexpr int PAIRS = D / 16 * NT * 2;            // of dims, a lane
   static constexpr int PARTS = kWarps * PAIRS * 32 * 8;
@@ -157,16 +158,16 @@ struct Sums {
   float o[NT][D / 16][4];
 };
 
-// 16 keys of a stage, from entry p on.
+// Scores of 16 keys of a stage: s[nt][2 r + e] of key k0 + 2 r and query 8 nt + 2 t + e.
 template <int D, int NT, bool F32>
-__device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const uint8_t* st, int p, int lane,
-                                       const uint32_t (&qh)[NT][D / 8], const uint32_t (&ql)[F32 ? NT : 1][D / 8],
-                                       const float (&back)[NT][2], Sums<D, NT>& x) {
+__device__ __forceinline__ void scores(const uint8_t* st, int lane, const uint32_t (&qh)[NT][D / 8],
+                                       const uint32_t (&ql)[F32 ? NT : 1][D / 8], const float (&back)[NT][2],
+                                       float (&s)[NT][4]) {
   constexpr int ROW = D / 2, CODES = 16 * ROW, S = D / 16;
   const int g = lane >> 2, t = lane & 3;
-  // ---- scores: the rows g and g + 8 of the product are keys k0 and k0 + 2 of the 16 ----
+  // the rows g and g + 8 of the product are keys k0 and k0 + 2 of the 16
   const int k0 = 4 * (g >> 1) + (g & 1);
-  float s[NT][4], s2[NT][4];  // (two chains of products)
+  float s2[NT][4];  // (two chains of products)
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -191,7 +192,7 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
     __half2 sc[2], sh[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      sc[r] = scale_pair(((sb[r] >> (8 * b)) & 255u) * 0x10001u);
+      sc[r] = scale_pair(__byte_perm(sb[r], 0, b ? 0x4141 : 0x4040));
       sh[r] = scale_shift(sc[r]);
     }
 #pragma unroll
@@ -211,53 +212,34 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
       }
     }
   }
-  // ---- weights ----
-  // (s[.][2 r + e]: key k0 + 2 r, query 8 nt + 2 t + e)
-  bool grow = false;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[nt][e] = (s[nt][e] + s2[nt][e]) * back[nt][e & 1];
-  if (p + 16 > it.L) {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int q = it.qt * 8 * NT + 8 * nt + 2 * t + e, i = min(divide_group(a, q), it.rows - 1);
-        const uint64_t vis = visible_rows(a, it.r0 + i, i, it.rows);
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int rel = p + k0 + 2 * r - it.L;
-          if (rel >= 0 && (rel >= it.rows || !((vis >> rel) & 1))) s[nt][2 * r + e] = -INFINITY;
-        }
-      }
-  }
+}
+
+// What is not seen of 16 keys from entry p on (and all from `stop` on) gets a score of -inf.
+template <int NT>
+__device__ __forceinline__ void mask_slice(const TreeArgs& a, const Unit& it, int p, int stop, int lane, float (&s)[NT][4]) {
+  const int g = lane >> 2, t = lane & 3, k0 = 4 * (g >> 1) + (g & 1);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) grow = grow || fmaxf(s[nt][e], s[nt][2 + e]) > x.m[nt][e] + kLazy;
-  if (__any_sync(~0u, grow)) {
+    for (int e = 0; e < 2; ++e) {
+      const int q = it.qt * 8 * NT + 8 * nt + 2 * t + e, i = min(divide_group(a, q), it.rows - 1);
+      const uint64_t vis = visible_rows(a, it.r0 + i, i, it.rows);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float most = fmaxf(s[nt][e], s[nt][2 + e]);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-        const float m = x.m[nt][e];
-        if (most > m + kLazy) {
-          const float f = m == -INFINITY ? 0.f : ex2(m - most);
-          x.m[nt][e] = most;
-          x.l[nt][e] *= f;
-#pragma unroll
-          for (int mt = 0; mt < D / 16; ++mt) {
-            x.o[nt][mt][e] *= f;
-            x.o[nt][mt][2 + e] *= f;
-          }
-        }
+      for (int r = 0; r < 2; ++r) {
+        const int at = p + k0 + 2 * r, rel = at - it.L;
+        if (at >= stop || (rel >= 0 && !((vis >> rel) & 1))) s[nt][2 * r + e] = -INFINITY;
       }
-  }
-  uint32_t ph[NT][2], pl[F32 ? NT : 1][2];
+    }
+}
+
+// The weights of a slice's scores, as operands of its second product, and their sums.
+template <int D, int NT, bool F32>
+__device__ __forceinline__ void weights_of(const float (&s)[NT][4], Sums<D, NT>& x, uint32_t (&ph)[NT][2],
+                                           uint32_t (&pl)[F32 ? NT : 1][2]) {
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     float w4[4];
@@ -278,7 +260,14 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
       }
     }
   }
-  // ---- accumulators: rows g and g + 8 of the products are dims D / 8 g + 2 mt and + 1 ----
+}
+
+// A slice's values into the accumulators: rows g and g + 8 of the products are dims D / 8 g + 2 mt and + 1.
+template <int D, int NT, bool F32>
+__device__ __forceinline__ void add_values(const uint8_t* st, int lane, const uint32_t (&ph)[NT][2],
+                                           const uint32_t (&pl)[F32 ? NT : 1][2], Sums<D, NT>& x) {
+  constexpr int ROW = D / 2, CODES = 16 * ROW, S = D / 16;
+  const int g = lane >> 2, t = lane & 3;
   uint32_t vw[4][D / 64], vb[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -313,6 +302,57 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
   }
 }
 
+// Z slices of 16 keys together: entries p + 128 z .. of stages st[z], those from `stop` on masked.
+template <int D, int NT, bool F32, int Z>
+__device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const uint8_t* const (&st)[Z], int p, int stop,
+                                       int lane, const uint32_t (&qh)[NT][D / 8],
+                                       const uint32_t (&ql)[F32 ? NT : 1][D / 8], const float (&back)[NT][2],
+                                       Sums<D, NT>& x) {
+  float s[Z][NT][4];
+#pragma unroll
+  for (int z = 0; z < Z; ++z) scores<D, NT, F32>(st[z], lane, qh, ql, back, s[z]);
+#pragma unroll
+  for (int z = 0; z < Z; ++z)
+    if (p + 128 * z + 16 > min(it.L, stop)) mask_slice<NT>(a, it, p + 128 * z, stop, lane, s[z]);
+  float most[NT][2];
+  bool grow = false;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      most[nt][e] = fmaxf(s[0][nt][e], s[0][nt][2 + e]);
+#pragma unroll
+      for (int z = 1; z < Z; ++z) most[nt][e] = max3(most[nt][e], s[z][nt][e], s[z][nt][2 + e]);
+      grow = grow || most[nt][e] > x.m[nt][e] + kLazy;
+    }
+  if (__any_sync(~0u, grow)) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float now = most[nt][e];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) now = fmaxf(now, __shfl_xor_sync(~0u, now, o));
+        const float m = x.m[nt][e];
+        if (now > m + kLazy) {
+          const float f = m == -INFINITY ? 0.f : ex2(m - now);
+          x.m[nt][e] = now;
+          x.l[nt][e] *= f;
+#pragma unroll
+          for (int mt = 0; mt < D / 16; ++mt) {
+            x.o[nt][mt][e] *= f;
+            x.o[nt][mt][2 + e] *= f;
+          }
+        }
+      }
+  }
+  uint32_t ph[Z][NT][2], pl[Z][F32 ? NT : 1][2];
+#pragma unroll
+  for (int z = 0; z < Z; ++z) weights_of<D, NT, F32>(s[z], x, ph[z], pl[z]);
+#pragma unroll
+  for (int z = 0; z < Z; ++z) add_values<D, NT, F32>(st[z], lane, ph[z], pl[z], x);
+}
+
 __device__ __forceinline__ float part_weight(float m, float M) {
   return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
 }
@@ -335,7 +375,7 @@ __device__ __forceinline__ void place_of(int pair, int lane, int& query, int& di
 }
 
 template <int D, int NT, bool F32>
-__global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, 1)
     attn4_kernel(const __grid_constant__ Tree4Args a4, Work ws, int mode, int turn) {
   using S = Shape<D, NT, F32>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -380,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll 1
-    for (int k = 0; k < S::NST - 1; ++k) load(k);
+    for (int k = 0; k < S::NST - S::Z; ++k) load(k);
     load_queries4<D, NT, F32>(a, it, warp, lane, s_q);
     __syncthreads();
     uint32_t qh[NT][D / 8], ql[F32 ? NT : 1][D / 8];
@@ -410,13 +450,17 @@ __global__ void __launch_bounds__(kThreads, NT == 1 && !F32 ? 2 : 1)
         for (int e = 0; e < 4; ++e) x.o[nt][mt][e] = 0.f;
     }
 #pragma unroll 1
-    for (int k = 0; k < n; ++k) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::NST - 2) : "memory");
+    for (int k = 0; k < n; k += S::Z) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::NST - 2 * S::Z) : "memory");
       __syncwarp();
       const int p = (it.t0 + k) * 128 + 16 * warp;
-      if (p < end) attend<D, NT, F32>(a, it, ring + k % S::NST * S::STAGE, p, lane, qh, ql, back, x);
+      const uint8_t* st[S::Z];
+#pragma unroll
+      for (int z = 0; z < S::Z; ++z) st[z] = ring + (k + z) % S::NST * S::STAGE;
+      if (p < end) attend<D, NT, F32, S::Z>(a, it, st, p, min(end, it.t1 * 128), lane, qh, ql, back, x);
       __syncwarp();
-      load(k + S::NST - 1);
+#pragma unroll
+      for (int z = 0; z < S::Z; ++z) load(k + S::NST - S::Z + z);
     }
     // ---- the warps' parts, brought to one reference, over the rings ----
     asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -580,7 +624,7 @@ cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sm
   const dim3 each((most * G + S::Q - 1) / S::Q, a.nkv, a.rm.batch);
   if (tiles <= kWholeTiles)
     return launch_pdl(attn4_kernel<D, NT, F32>, each, dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kWhole, 0);
-  const int ctas = (int)std::min<int64_t>(units, 2 * sms), turn = 0;
+  const int ctas = (int)std::min<int64_t>(units, sms), turn = 0;
   const cudaError_t f = launch_pdl(attn4_kernel<D, NT, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kShares, turn);
   if (f != cudaSuccess) return f;
   const int64_t parts = ctas / std::max<int64_t>(items, 1);
@@ -594,7 +638,7 @@ cudaError_t launch_d(const Tree4Args& a, void* workspace, int64_t max_keys, cuda
   const int sms = device_sms();
   Work ws;
   ws.o = (float2*)workspace;
-  ws.ml = ws.o + (size_t)2 * sms * 2 * 16 * D / 2;
+  ws.ml = ws.o + (size_t)sms * 2 * 16 * D / 2;
   int most = 0;
   for (int b = 0; b < a.t.rm.batch; ++b) most = std::max(most, a.t.rm.start[b + 1] - a.t.rm.start[b]);
   if (most * (a.t.nq / a.t.nkv) <= 8)
@@ -605,7 +649,7 @@ cudaError_t launch_d(const Tree4Args& a, void* workspace, int64_t max_keys, cuda
 }  // namespace
 
 size_t attention4_workspace(int head_dim) {
-  return (size_t)device_sms() * 2 * 2 * 16 * (head_dim * 4 + 8);
+  return (size_t)device_sms() * 2 * 16 * (head_dim * 4 + 8);
 }
 
 cudaError_t launch_attention4(const Tree4Args& a, int head_dim, int64_t max_keys, void* workspace, cudaStream_t st) {

@@ -109,8 +109,8 @@ as2d_status check_new_rows(const as2d_cache* c, int32_t layer, const as2d_new_ro
   if (r->n_q < 1) return invalid("n_q must be positive");
   if (r->n_q > 65535) return report_error(AS2D_ERR_UNSUPPORTED, "too many query heads");
   const int d = c->head_dim;
-  if (r->rotary < 0 || r->rotary > d || r->rotary % 16 != 0)
-    return invalid("rotary must be a multiple of 16 in [0, head_dim]");
+  if (r->rotary < 0 || r->rotary > d || r->rotary % 32 != 0)
+    return invalid("rotary must be a multiple of 32 in [0, head_dim]");
   if (r->rotary > 0 && (!(r->theta > 0.f) || !std::isfinite(r->theta))) return invalid("theta must be finite and > 0");
   if ((r->q_norm || r->k_norm) && (!(r->eps >= 0.f) || !std::isfinite(r->eps)))
     return invalid("eps must be finite and >= 0");

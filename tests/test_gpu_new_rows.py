@@ -76,7 +76,7 @@ def check_queries(x, out, want):
 @pytest.mark.parametrize("lens,rows", SETS)
 @pytest.mark.parametrize("norm,part", [(True, 1.0), (False, 0.5), (True, 0)])
 def test_append(lib, heads, lens, rows, dtype, norm, part):
-    x = Rows(heads, lens, rows, dtype, norm, int(part * heads[2]) // 16 * 16)
+    x = Rows(heads, lens, rows, dtype, norm, int(part * heads[2]) // 32 * 32)
     k, v = (torch.full(x.shape, 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
     out = lib.Cache(k, v).append(x.q, x.k, x.v, x.kv_len, rows, layer=1, **x.call)
     torch.cuda.synchronize()
@@ -96,7 +96,7 @@ def test_append(lib, heads, lens, rows, dtype, norm, part):
 @pytest.mark.parametrize("norm,part", [(True, 1.0), (False, 0.5), (False, 0)])
 def test_append4(lib, heads, lens, rows, dtype, norm, part):
     """Codes and scales are those of the exact values, every one of them."""
-    x = Rows(heads, lens, rows, dtype, norm, int(part * heads[2]) // 16 * 16, seed=len(rows))
+    x = Rows(heads, lens, rows, dtype, norm, int(part * heads[2]) // 32 * 32, seed=len(rows))
     c4 = x.packed()
     err = ints([0])
     out = lib.Cache4(*c4).append(x.q, x.k, x.v, x.kv_len, rows, layer=1, error_bits=err, **x.call)

@@ -102,7 +102,7 @@ BAD_NEW = [(dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(q=A
            (dict(q_stride=36 * 128 + 4), -1), (dict(v_stride=2 ** 62), -1), (dict(kv_len=None), -1),
            (dict(kv_len=A + 2), -1), (dict(rows=None), -1), (dict(positions=A + 1), -1), (dict(q_norm=A + 4), -1),
            (dict(k_norm=A + 8), -1), (dict(q_norm=A, eps=-1.0), -1), (dict(k_norm=A, eps=float("nan")), -1),
-           (dict(theta=0.0), -1), (dict(theta=float("inf")), -1), (dict(rotary=-16), -1), (dict(rotary=8), -1),
+           (dict(theta=0.0), -1), (dict(theta=float("inf")), -1), (dict(rotary=-16), -1), (dict(rotary=16), -1),
            (dict(rotary=144), -1)]
 
 
