@@ -17,6 +17,13 @@ constexpr int kWarps = 8, kThreads = 32 * kWarps;
 // (the weights, at most 2^(kLazy + kUp), use the range of 16-bit floats).
 constexpr float kLazy = 8.f, kUp = 7.f;
 
+// Queries of the partial results of an SM's CTAs: two of 8, or one of 16, two parts each.
+constexpr int kParts = 2 * 16;
+
+// What turning to another item costs a CTA, in tiles: its queries, the joining of its warps. us with 0 /
+// 3 / 5 / 8: 16 requests of one row 26.4 / 21.1 / 22.0 / 22.6.
+constexpr int kTurn = 4;
+
 enum Mode : int { kShares = 0, kWhole = 1 };
 
 struct Work {
@@ -38,8 +45,8 @@ struct Shape {
   static constexpr int Q = 8 * NT;                         // queries of a tile
   static constexpr int CODES = 16 * D / 2, SCALES = D;     // bytes of a warp's 16 keys (or values)
   static constexpr int STAGE = 2 * (CODES + SCALES);
-  static constexpr int Z = NT == 1 ? 2 : 1;                // slices together
-  static constexpr int NST = 10;
+  static constexpr int CTAS = NT == 1 ? 2 : 1;             // of an SM
+  static constexpr int NST = CTAS == 2 ? 5 : 10;
   static constexpr int RING = kWarps * NST * STAGE;
   static constexpr int PAIRS = D / 16 * NT * 2;            // of dims, a lane
   static constexpr int PARTS = kWarps * PAIRS * 32 * 8;
@@ -218,7 +225,7 @@ __device__ __forceinline__ void scores(const uint8_t* st, int lane, const uint32
     for (int e = 0; e < 4; ++e) s[nt][e] = (s[nt][e] + s2[nt][e]) * back[nt][e & 1];
 }
 
-// What is not seen of 16 keys from entry p on (and all from `stop` on) gets a score of -inf.
+// What is not seen of 16 keys from entry p on (`stop`: the request's end) gets a score of -inf.
 template <int NT>
 __device__ __forceinline__ void mask_slice(const TreeArgs& a, const Unit& it, int p, int stop, int lane, float (&s)[NT][4]) {
   const int g = lane >> 2, t = lane & 3, k0 = 4 * (g >> 1) + (g & 1);
@@ -302,27 +309,21 @@ __device__ __forceinline__ void add_values(const uint8_t* st, int lane, const ui
   }
 }
 
-// Z slices of 16 keys together: entries p + 128 z .. of stages st[z], those from `stop` on masked.
-template <int D, int NT, bool F32, int Z>
-__device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const uint8_t* const (&st)[Z], int p, int stop,
-                                       int lane, const uint32_t (&qh)[NT][D / 8],
+// 16 keys of a stage: entries p .. of the item.
+template <int D, int NT, bool F32>
+__device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const uint8_t* st, int p, int stop, int lane, const uint32_t (&qh)[NT][D / 8],
                                        const uint32_t (&ql)[F32 ? NT : 1][D / 8], const float (&back)[NT][2],
                                        Sums<D, NT>& x) {
-  float s[Z][NT][4];
-#pragma unroll
-  for (int z = 0; z < Z; ++z) scores<D, NT, F32>(st[z], lane, qh, ql, back, s[z]);
-#pragma unroll
-  for (int z = 0; z < Z; ++z)
-    if (p + 128 * z + 16 > min(it.L, stop)) mask_slice<NT>(a, it, p + 128 * z, stop, lane, s[z]);
+  float s[NT][4];
+  scores<D, NT, F32>(st, lane, qh, ql, back, s);
+  if (p + 16 > it.L) mask_slice<NT>(a, it, p, stop, lane, s);
   float most[NT][2];
   bool grow = false;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      most[nt][e] = fmaxf(s[0][nt][e], s[0][nt][2 + e]);
-#pragma unroll
-      for (int z = 1; z < Z; ++z) most[nt][e] = max3(most[nt][e], s[z][nt][e], s[z][nt][2 + e]);
+      most[nt][e] = fmaxf(s[nt][e], s[nt][2 + e]);
       grow = grow || most[nt][e] > x.m[nt][e] + kLazy;
     }
   if (__any_sync(~0u, grow)) {
@@ -346,15 +347,9 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
         }
       }
   }
-  uint32_t ph[Z][NT][2], pl[Z][F32 ? NT : 1][2];
-#pragma unroll
-  for (int z = 0; z < Z; ++z) weights_of<D, NT, F32>(s[z], x, ph[z], pl[z]);
-#pragma unroll
-  for (int z = 0; z < Z; ++z) add_values<D, NT, F32>(st[z], lane, ph[z], pl[z], x);
-}
-
-__device__ __forceinline__ float part_weight(float m, float M) {
-  return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
+  uint32_t ph[NT][2], pl[F32 ? NT : 1][2];
+  weights_of<D, NT, F32>(s, x, ph, pl);
+  add_values<D, NT, F32>(st, lane, ph, pl, x);
 }
 
 // Two dims of a query: 32-bit or bf16.
@@ -375,7 +370,7 @@ __device__ __forceinline__ void place_of(int pair, int lane, int& query, int& di
 }
 
 template <int D, int NT, bool F32>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
     attn4_kernel(const __grid_constant__ Tree4Args a4, Work ws, int mode, int turn) {
   using S = Shape<D, NT, F32>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -420,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll 1
-    for (int k = 0; k < S::NST - S::Z; ++k) load(k);
+    for (int k = 0; k < S::NST - 1; ++k) load(k);
     load_queries4<D, NT, F32>(a, it, warp, lane, s_q);
     __syncthreads();
     uint32_t qh[NT][D / 8], ql[F32 ? NT : 1][D / 8];
@@ -450,17 +445,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int e = 0; e < 4; ++e) x.o[nt][mt][e] = 0.f;
     }
 #pragma unroll 1
-    for (int k = 0; k < n; k += S::Z) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(S::NST - 2 * S::Z) : "memory");
+    for (int k = 0; k < n; ++k) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S::NST - 2) : "memory");
       __syncwarp();
       const int p = (it.t0 + k) * 128 + 16 * warp;
-      const uint8_t* st[S::Z];
-#pragma unroll
-      for (int z = 0; z < S::Z; ++z) st[z] = ring + (k + z) % S::NST * S::STAGE;
-      if (p < end) attend<D, NT, F32, S::Z>(a, it, st, p, min(end, it.t1 * 128), lane, qh, ql, back, x);
+      if (p < end) attend<D, NT, F32>(a, it, ring + k % S::NST * S::STAGE, p, end, lane, qh, ql, back, x);
       __syncwarp();
-#pragma unroll
-      for (int z = 0; z < S::Z; ++z) load(k + S::NST - S::Z + z);
+      load(k + S::NST - 1);
     }
     // ---- the warps' parts, brought to one reference, over the rings ----
     asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -624,7 +615,7 @@ cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sm
   const dim3 each((most * G + S::Q - 1) / S::Q, a.nkv, a.rm.batch);
   if (tiles <= kWholeTiles)
     return launch_pdl(attn4_kernel<D, NT, F32>, each, dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kWhole, 0);
-  const int ctas = (int)std::min<int64_t>(units, sms), turn = 0;
+  const int ctas = (int)std::min<int64_t>(units, (int64_t)S::CTAS * sms), turn = units > S::CTAS * sms ? kTurn : 0;
   const cudaError_t f = launch_pdl(attn4_kernel<D, NT, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kShares, turn);
   if (f != cudaSuccess) return f;
   const int64_t parts = ctas / std::max<int64_t>(items, 1);
@@ -633,15 +624,20 @@ cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sm
   return launch_pdl(join4_kernel<D, NT, F32>, joins, dim3(kThreads), 0, st, 1, a, ws, ctas, turn, split);
 }
 
+// Requests of more queries to a kv head go to k_attn4_wide.cu.
+constexpr int kMostNarrow = 16;
+
 template <int D>
 cudaError_t launch_d(const Tree4Args& a, void* workspace, int64_t max_keys, cudaStream_t st) {
   const int sms = device_sms();
   Work ws;
   ws.o = (float2*)workspace;
-  ws.ml = ws.o + (size_t)sms * 2 * 16 * D / 2;
+  ws.ml = ws.o + (size_t)sms * kParts * D / 2;
   int most = 0;
   for (int b = 0; b < a.t.rm.batch; ++b) most = std::max(most, a.t.rm.start[b + 1] - a.t.rm.start[b]);
-  if (most * (a.t.nq / a.t.nkv) <= 8)
+  const int queries = most * (a.t.nq / a.t.nkv);
+  if (queries > kMostNarrow) return launch_attention4_wide(a, D, max_keys, workspace, st);
+  if (queries <= 8)
     return a.t.q_f32 ? launch<D, 1, true>(a, ws, max_keys, sms, st) : launch<D, 1, false>(a, ws, max_keys, sms, st);
   return a.t.q_f32 ? launch<D, 2, true>(a, ws, max_keys, sms, st) : launch<D, 2, false>(a, ws, max_keys, sms, st);
 }
@@ -649,7 +645,7 @@ cudaError_t launch_d(const Tree4Args& a, void* workspace, int64_t max_keys, cuda
 }  // namespace
 
 size_t attention4_workspace(int head_dim) {
-  return (size_t)device_sms() * 2 * 16 * (head_dim * 4 + 8);
+  return std::max((size_t)device_sms() * kParts * (head_dim * 4 + 8), tree_attention_workspace(head_dim));
 }
 
 cudaError_t launch_attention4(const Tree4Args& a, int head_dim, int64_t max_keys, void* workspace, cudaStream_t st) {

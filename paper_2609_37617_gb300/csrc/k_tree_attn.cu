@@ -76,13 +76,6 @@ enum Mode : int {
 };
 constexpr int kRanks = 8;
 
-struct TreeWork {
-  float4* o;   // [2 CTAs][D / 4][128] partial accumulators, four dims of a query
-               // together: slot 0 an item that began in an earlier CTA, slot 1 one
-               // that began in this
-  float2* ml;  // [2 CTAs][128] (maximum base 2, sum)
-};
-
 template <int D, bool F32>
 struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;            // one K or V tile
@@ -92,12 +85,6 @@ struct Shape {
       1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16 + 2 * sizeof(Unit);
   static_assert(SMEM + sizeof(UnitPlan) + sizeof(First) <= 232448, "shared memory of one CTA");
 };
-
-// The weight of a part (maximum m) beside a maximum M: 0 where the part holds
-// nothing that the row sees.
-__device__ __forceinline__ float part_weight(float m, float M) {
-  return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
-}
 
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= FLT_MAX; }
 
@@ -126,20 +113,6 @@ __device__ __forceinline__ void dsmem_st(uint32_t addr, float v) {
 }
 __device__ __forceinline__ void dsmem_st2(uint32_t addr, float2 v) {
   asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
-}
-
-// Which of keys [p0, p0 + 32) a row sees.
-__device__ __forceinline__ uint32_t key_bits(int p0, int L, uint64_t vis) {
-  const int off = L - p0;  // prefix entries in the word
-  if (off >= 32) return ~0u;
-  if (off >= 0) return ((1u << off) - 1) | (uint32_t)(vis << off);
-  return off > -64 ? (uint32_t)(vis >> -off) : 0u;
-}
-
-__device__ __forceinline__ void mask_scores(uint32_t (&v)[32], uint32_t bits) {
-#pragma unroll
-  for (int e = 0; e < 32; ++e)
-    if (!((bits >> e) & 1)) v[e] = 0xFF800000u;  // -inf
 }
 
 // A value tile that holds entries from L on, before it is multiplied: entries
@@ -868,6 +841,17 @@ __global__ void __launch_bounds__(32 * kCombineWarps, U == 12 ? 2 : U == 8 ? 3 :
   if (quad == 0 && a.lse) a.lse[(size_t)(r0 + i) * a.nq + h] = row_lse(M, l);
 }
 
+template <int D, bool F32>
+cudaError_t launch_join(const TreeArgs& a, const TreeWork& ws, int most_rows, int ctas, int turn, int sms,
+                        cudaStream_t st) {
+  const dim3 join((most_rows * (a.nq / a.nkv) + 127) / 128 * 4 * (D / 4 / kCombineWarps), a.nkv, a.rm.batch);
+  const int64_t joins = (int64_t)join.x * join.y * join.z;
+  return launch_pdl(joins <= 2 * sms   ? tree_combine_kernel<D, F32, 12>
+                    : joins <= 3 * sms ? tree_combine_kernel<D, F32, 8>
+                                       : tree_combine_kernel<D, F32, 4>,
+                    join, dim3(32 * kCombineWarps), 0, st, 1, a, ws, ctas, turn);
+}
+
 // Items of at most this many key tiles are each done by one CTA.  us, in one CTA /
 // by clusters: four items of two tiles 6.7 / 6.9, of three 8.2 / 7.2.
 constexpr int kWholeTiles = 2;
@@ -905,13 +889,8 @@ cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs&
   e = launch_pdl(tree_attn_kernel<D, F32, false>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, tk, tv, a, ws,
                  (int)kShares, turn);
   if (e != cudaSuccess) return e;
-  const dim3 join(direct.x * 4 * (D / 4 / kCombineWarps), direct.y, direct.z);
   ++launches;
-  const int64_t joins = (int64_t)join.x * join.y * join.z;
-  return launch_pdl(joins <= 2 * sms   ? tree_combine_kernel<D, F32, 12>
-                    : joins <= 3 * sms ? tree_combine_kernel<D, F32, 8>
-                                       : tree_combine_kernel<D, F32, 4>,
-                    join, dim3(32 * kCombineWarps), 0, st, 1, a, ws, ctas, turn);
+  return launch_join<D, F32>(a, ws, most_rows, ctas, turn, sms, st);
 }
 
 }  // namespace
@@ -936,6 +915,24 @@ int64_t tree_items(const TreeArgs& a) {
   return items;
 }
 
+TreeWork tree_work(void* workspace, int head_dim) {
+  TreeWork ws;
+  ws.o = (float4*)workspace;
+  ws.ml = (float2*)(ws.o + (size_t)device_sms() * 2 * 128 * head_dim / 4);
+  return ws;
+}
+
+cudaError_t launch_tree_join(const TreeArgs& a, int head_dim, const TreeWork& ws, int ctas, int turn, cudaStream_t st) {
+  const int sms = device_sms();
+  int most = 0;
+  for (int b = 0; b < a.rm.batch; ++b) most = std::max(most, a.rm.start[b + 1] - a.rm.start[b]);
+  if (head_dim == 128)
+    return a.q_f32 ? launch_join<128, true>(a, ws, most, ctas, turn, sms, st)
+                   : launch_join<128, false>(a, ws, most, ctas, turn, sms, st);
+  return a.q_f32 ? launch_join<64, true>(a, ws, most, ctas, turn, sms, st)
+                 : launch_join<64, false>(a, ws, most, ctas, turn, sms, st);
+}
+
 size_t tree_attention_workspace(int head_dim) {
   return (size_t)device_sms() * 2 * 128 * (head_dim * 4 + 8);
 }
@@ -947,9 +944,7 @@ cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_k
   const int64_t items = tree_items(a);
   int most = 0;  // rows of a request
   for (int b = 0; b < a.rm.batch; ++b) most = std::max(most, a.rm.start[b + 1] - a.rm.start[b]);
-  TreeWork ws;
-  ws.o = (float4*)workspace;
-  ws.ml = (float2*)(ws.o + (size_t)sms * 2 * 128 * head_dim / 4);
+  const TreeWork ws = tree_work(workspace, head_dim);
   CUtensorMap tk, tv;
   if (!encode_cache_map(&tk, a.k, head_dim, a.cap, (int64_t)a.rm.batch * a.nkv) ||
       !encode_cache_map(&tv, a.v, head_dim, a.cap, (int64_t)a.rm.batch * a.nkv))

@@ -112,6 +112,14 @@ struct SampledArgs {
   int32_t *n_out, *token_out;
 };
 
+// Partial results of items of 128 queries that are cut between CTAs.
+struct TreeWork {
+  float4* o;   // [2 CTAs][D / 4][128] partial accumulators, four dims of a query
+               // together: slot 0 an item that began in an earlier CTA, slot 1 one
+               // that began in this
+  float2* ml;  // [2 CTAs][128] (maximum base 2, sum)
+};
+
 // Rows of a projection for one layer of a cache, in bf16 or in 4 bits (as2d_new_rows).
 struct AppendArgs {
   RowMap rm;
@@ -152,6 +160,9 @@ int64_t tree_items(const TreeArgs& a);
 cudaError_t launch_tree_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
                                   cudaStream_t st, int64_t* launches = nullptr);
 size_t tree_attention_workspace(int head_dim);
+TreeWork tree_work(void* workspace, int head_dim);
+// The parts of items that `ctas` CTAs left by even shares of their units (make_plan), joined.
+cudaError_t launch_tree_join(const TreeArgs& a, int head_dim, const TreeWork& ws, int ctas, int turn, cudaStream_t st);
 cudaError_t launch_attention_weights(const WeightArgs& a, int head_dim, int64_t max_keys, cudaStream_t st);
 cudaError_t launch_cache_evict(const EvictArgs& a, int head_dim, cudaStream_t st);
 size_t cache_evict_workspace(int64_t units, int cap);
@@ -162,6 +173,7 @@ cudaError_t launch_accept_sampled(const SampledArgs& a, cudaStream_t st);
 cudaError_t launch_append(const AppendArgs& a, int head_dim, bool f32, cudaStream_t st);
 cudaError_t launch_pack4(const Pack4Args& a, int head_dim, bool write, int max_entries, cudaStream_t st);
 cudaError_t launch_attention4(const Tree4Args& a, int head_dim, int64_t max_keys, void* workspace, cudaStream_t st);
+cudaError_t launch_attention4_wide(const Tree4Args& a, int head_dim, int64_t max_keys, void* workspace, cudaStream_t st);
 size_t attention4_workspace(int head_dim);
 cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
                                     cudaStream_t st);

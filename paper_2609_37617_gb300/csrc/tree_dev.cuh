@@ -96,6 +96,26 @@ __device__ __forceinline__ uint64_t visible_rows(const TreeArgs& a, int r, int i
   return (a.visible ? a.visible[r] : ~0ull >> (63 - i)) & all;
 }
 
+// Which of keys [p0, p0 + 32) a row sees.
+__device__ __forceinline__ uint32_t key_bits(int p0, int L, uint64_t vis) {
+  const int off = L - p0;  // prefix entries in the word
+  if (off >= 32) return ~0u;
+  if (off >= 0) return ((1u << off) - 1) | (uint32_t)(vis << off);
+  return off > -64 ? (uint32_t)(vis >> -off) : 0u;
+}
+
+__device__ __forceinline__ void mask_scores(uint32_t (&v)[32], uint32_t bits) {
+#pragma unroll
+  for (int e = 0; e < 32; ++e)
+    if (!((bits >> e) & 1)) v[e] = 0xFF800000u;  // -inf
+}
+
+// The weight of a part (maximum m) beside a maximum M: 0 where the part holds
+// nothing that the row sees.
+__device__ __forceinline__ float part_weight(float m, float M) {
+  return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
+}
+
 // The ring's next stage and its parity, as slot | parity << 8.
 struct Stage {
   uint32_t x = 0;
