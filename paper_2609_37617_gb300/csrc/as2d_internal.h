@@ -331,6 +331,10 @@ size_t attn_qimg_bytes(int head_dim);
 // map the attention kernel loads key/value tiles through.
 bool encode_cache_map(CUtensorMap* map, const void* cache, int head_dim, int capacity,
                       int64_t heads);
+// Rows [n_rows][heads][head_dim] bf16, `stride` elements apart, in boxes of 64 dims of
+// some heads of some rows.
+bool encode_rows_map(CUtensorMap* map, const void* rows, int head_dim, int heads, int64_t n_rows,
+                     int64_t stride, int box_heads, int box_rows);
 // With q32 only the QKV projection is finished: keys and values appended, rotated
 // queries to q32 ([rows][nq][d]).
 cudaError_t launch_attention_split(const RowMap& m, const Model& md, KvState& kv, int layer,

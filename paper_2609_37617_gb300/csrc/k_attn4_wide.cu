@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const unsigned long long limit = a.timeout_ns;
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok && !ptx::mbar_spin(bar, parity, limit)) {
+    if (ok && !ptx::mbar_sleep(bar, parity, limit)) {
       ok = false;
       if (a.err) atomicOr(a.err, kErrTimeout);
     }

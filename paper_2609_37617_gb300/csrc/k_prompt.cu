@@ -5,19 +5,26 @@
 //   m = max s_t, l = sum e^(s_t - m), out = sum e^(s_t - m) v_t / l, lse = m + ln l.
 //
 // The G = n_q / n_kv query heads of a kv head, for all rows of a request, form one
-// query matrix of rows G queries (row by row, so that 256 queries stand for few rows and
-// little of a tile on the diagonal is masked), cut into pairs of query tiles of 128
-// (the MMA's M).  An item is one (request, kv head, pair); a CTA takes it through its key
-// tiles of 128.
+// query matrix (row by row, so that 256 queries stand for few rows and little of a tile on
+// the diagonal is masked), cut into pairs of query tiles of 128 (the MMA's M): as many whole rows
+// as fit 256 queries (of more than 256 heads: 256 of a row).  An item is one (request, kv head,
+// pair); a CTA takes it through its key tiles of 128.  One CTA per SM takes the items in turn,
+// those of most key tiles first, back and forth over the CTAs (by the lengths on the device: eight
+// prompts of 1 to 2029 rows take 102 us in the order of their rows, 90 so).
 //
 // Per CTA (12 warps, TMEM full: two score buffers, two accumulators):
 //   warp 0     loads key and value tiles by TMA through a ring of shared-memory stages;
 //   warp 1     issues the products: S = Q K^T, O += P V (P from TMEM) of the two query
 //              tiles in turn, so that one's products run under the other's softmax;
-//   warps 2-3  prepare the value tiles that hold entries not every row sees;
-//   warps 4-7 and 8-11 a query tile each, a query a thread: S from TMEM, mask, running
-//              maximum, P = 2^(S - m) back into TMEM in bf16 over S; O is rescaled only where
-//              the maximum grew by more than 2^8.
+//   warps 2-3  prepare the value tiles that hold entries not every row sees, and have the next
+//              item's queries brought in (TMA) when the last scores of this one are there;
+//   warps 4-11 four to a query tile, a query a thread: S from TMEM, mask, P = 2^(S - m) back into
+//              TMEM in bf16 over S.  The next item's scores are computed while an item's
+//              results are written.
+// m is not looked for: a tile's weights are computed with the reference there is, and only where
+// their sum passes 2^kMost (or there is none yet) is the tile's maximum taken for the new one, the accumulator
+// rescaled and the weights computed again.  That keeps the chain from scores to weights, which the
+// products of one query tile wait for while the other's run, at one exponential a score.
 // P in one bf16 part: each weight is off by at most 2^-8 of itself, as the result's own
 // rounding is; the sums l are of the weights in 32 bits.
 #include <algorithm>
@@ -31,22 +38,109 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int kMaxTails = 3;  // key tiles that not all rows of 256 queries see whole
-// P may grow to 2^kLazy before the accumulator is rescaled.
-constexpr float kLazy = 8.f;
+// The sum of a tile's 128 weights that makes its maximum the reference.
+constexpr float kMost = 8192.f;
 
-// The items of a call, longest first: requests by their rows, of a request its last rows first.
-struct Items {
-  int first[kMaxBatch + 1];   // items before the n-th request of the order
-  uint8_t request[kMaxBatch];
+// How queries are cut into items.
+struct Cut {
+  int rows_each, chunks;  // whole rows of an item, or items of a row
+};
+
+struct Item {
+  int b, g, r0, L;
+  int i_min, h0, nq;  // row and head (of the group) of its first query, queries
+  int end, from;      // entries that some row sees; from the first that not every row does
+  int cnt, tail0;     // key tiles (0: there are no more items); the first that holds such entries
 };
 
 template <int D>
 struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;  // one K or V tile, and one query tile
   static constexpr int NST = D == 64 ? 8 : 5;
-  static constexpr uint32_t SMEM = 1024 + (2 + NST) * STAGE + (3 * NST + 8 + kMaxTails) * 8 + 4 * kMaxTails * 4 + 16;
+  static constexpr uint32_t SMEM =
+      (2 + NST) * STAGE + (3 * NST + 11 + kMaxTails) * 8 + 4 * kMaxTails * 4 + 2 * sizeof(Item) + 16;
   static_assert(SMEM <= 232448, "shared memory of one CTA");
 };
+
+// The n-th item of this CTA, by a whole warp: the items of all requests in the order of their key
+// tiles, most first, go over the CTAs back and forth.  (tiles 0: there are no more.  Not inlined:
+// two roles run it, once an item.)  A request's k-th item has (end of its last row + 127) / 128 tiles,
+// so that those with at least T need no list to be counted.
+static __device__ __noinline__ Item item_at(const TreeArgs& a, Cut cut, int n, int lane) {
+  const int ctas = gridDim.x, G = a.nq / a.nkv;
+  const int64_t at = (int64_t)n * ctas + (n & 1 ? ctas - 1 - (int)blockIdx.x : (int)blockIdx.x);
+  int L[2], rows[2], items[2], most = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int b = 32 * h + lane;
+    L[h] = rows[h] = items[h] = 0;
+    if (b < a.rm.batch) {
+      const int r = a.rm.start[b + 1] - a.rm.start[b], len = a.len[b];
+      if (rows_fit(len, r, a.cap)) {
+        L[h] = len, rows[h] = r;
+        items[h] = cut.chunks > 1 ? r * cut.chunks : (r + cut.rows_each - 1) / cut.rows_each;
+        if (r > 0) most = max(most, (len + r + 127) / 128);
+      }
+    }
+  }
+  most = __reduce_max_sync(~0u, most);
+  // of a request, the first item with at least T tiles
+  auto first = [&](int h, int T) {
+    const int x = (T - 1) * 128 - L[h];  // rows that end before
+    return x >= rows[h] ? items[h] : x <= 0 ? 0 : cut.chunks > 1 ? x * cut.chunks : x / cut.rows_each;
+  };
+  auto count = [&](int T) {
+    return (int64_t)a.nkv * __reduce_add_sync(~0u, items[0] - first(0, T) + items[1] - first(1, T));
+  };
+  Item it;
+  it.cnt = 0;
+  if (most == 0 || count(1) <= at) return it;
+  int T = 1, hi = most;  // the most tiles that the item has
+  while (T < hi) {
+    const int mid = (T + hi + 1) >> 1;
+    if (count(mid) > at)
+      T = mid;
+    else
+      hi = mid - 1;
+  }
+  const int in = (int)(at - count(T + 1)), x = in / a.nkv;  // among those with T tiles
+  it.g = in - x * a.nkv;
+  int before = 0, b = -1, item = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int from = first(h, T), mine = first(h, T + 1) - from;
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(~0u, sum, o);
+      if (lane >= o) sum += y;
+    }
+    const uint32_t past = __ballot_sync(~0u, before + sum > x);
+    if (b < 0 && past) {
+      const int l = __ffs(past) - 1;
+      b = 32 * h + l;
+      item = __shfl_sync(~0u, from + x - before - (sum - mine), l);
+      it.L = __shfl_sync(~0u, L[h], l);
+    }
+    before += __shfl_sync(~0u, sum, 31);
+  }
+  it.b = b;
+  it.r0 = a.rm.start[b];
+  if (cut.chunks > 1) {
+    it.i_min = item / cut.chunks;
+    it.h0 = item % cut.chunks * 256;
+    it.nq = min(256, G - it.h0);
+  } else {
+    it.i_min = item * cut.rows_each;
+    it.h0 = 0;
+    it.nq = min(cut.rows_each, a.rm.start[b + 1] - it.r0 - it.i_min) * G;
+  }
+  it.end = it.L + it.i_min + divide_group(a, it.h0 + it.nq - 1) + 1;
+  it.from = it.L + it.i_min + 1;
+  it.cnt = T;
+  it.tail0 = it.from / 128;
+  return it;
+}
 
 // Of a value tile the entries from `from` on, which not every row of the item sees: values
 // that are not finite become 0 and their rows are noted in bad (bit: entry - from0); entries
@@ -82,26 +176,28 @@ __device__ __forceinline__ void clean_tile(uint8_t* v, int p0, int from, int end
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
-    prompt_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                  const __grid_constant__ TreeArgs a, const __grid_constant__ Items items) {
+    prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                  const __grid_constant__ CUtensorMap tmV,
+                  const __grid_constant__ TreeArgs a, const Cut cut) {
   using S = Shape<D>;
   constexpr int NST = S::NST, NR = D / 64;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* sm = reinterpret_cast<uint8_t*>(
-      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  extern __shared__ __align__(1024) uint8_t sm[];  // (the kernel has no other shared memory)
   uint8_t* qimg = sm;
   uint8_t* ring = sm + 2 * S::STAGE;
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + NST * S::STAGE);
   uint64_t* empty = full + NST;
   uint64_t* tail_full = empty + NST;  // in full's place for value tiles that clean_tile prepares
   uint64_t* q_full = tail_full + NST;
-  uint64_t* s_full = q_full + 1;  // [2]
-  uint64_t* p_full = s_full + 2;  // [2]
-  uint64_t* o_full = p_full + 2;  // [2]
-  uint64_t* drain = o_full + 2;
-  uint64_t* v_clean = drain + 1;  // [kMaxTails]
+  uint64_t* q_empty = q_full + 1;
+  uint64_t* s_full = q_empty + 1;   // [2]
+  uint64_t* p_full = s_full + 2;    // [2]
+  uint64_t* o_full = p_full + 2;    // [2]
+  uint64_t* o_empty = o_full + 2;
+  uint64_t* drain = o_empty + 1;
+  uint64_t* v_clean = drain + 1;    // [kMaxTails]
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(v_clean + kMaxTails);  // [4 kMaxTails]
-  uint32_t* tslot = s_bad + 4 * kMaxTails;
+  Item* s_item = reinterpret_cast<Item*>(s_bad + 4 * kMaxTails);       // [2] the items of this parity
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(s_item + 2);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -110,73 +206,45 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(&empty[i], 1);
       ptx::mbar_init(&tail_full[i], 1);
     }
-    ptx::mbar_init(q_full, (kThreads - 64) / 32);
+    ptx::mbar_init(q_full, 1);
+    ptx::mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&s_full[i], 1);
       ptx::mbar_init(&p_full[i], 4);
       ptx::mbar_init(&o_full[i], 1);
     }
+    ptx::mbar_init(o_empty, 8);
     ptx::mbar_init(drain, 1);
     for (int i = 0; i < kMaxTails; ++i) ptx::mbar_init(&v_clean[i], 64);
     ptx::fence_mbar_init();
   }
-  if (tid >= 64 && tid < 64 + 4 * kMaxTails) s_bad[tid - 64] = 0;
   if (warp == 1) ptx::tmem_alloc(tslot, 512);
   if (warp == 0 && lane == 0) {
+    ptx::prefetch_tmap(&tmQ);
     ptx::prefetch_tmap(&tmK);
     ptx::prefetch_tmap(&tmV);
   }
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  // the item
-  int lo = 0, hi = a.rm.batch - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (items.first[mid] <= (int)blockIdx.x)
-      lo = mid;
-    else
-      hi = mid - 1;
+  Item it;  // of the two roles that look for the items
+  if (warp == 0 || warp == 2) it = item_at(a, cut, 0, lane);
+  if (tid == 64) s_item[0] = it;
+  if (warp == 3 && blockIdx.x == 0) {
+    bool over = false;
+    for (int b = lane; b < a.rm.batch; b += 32)
+      over = over || !rows_fit(a.len[b], a.rm.start[b + 1] - a.rm.start[b], a.cap);
+    if (__any_sync(~0u, over) && lane == 0 && a.err) atomicOr(a.err, kErrCapacity);
   }
-  const int b = items.request[lo], r0 = a.rm.start[b], rows = a.rm.start[b + 1] - r0;
-  const int G = a.nq / a.nkv, queries = rows * G;
-  const int in = blockIdx.x - items.first[lo], pairs = (queries + 255) / 256;
-  const int g = in % a.nkv, pair = pairs - 1 - in / a.nkv;
-  const int q0 = pair * 256, nq = min(256, queries - q0);
-  const int i_min = q0 / G, h0 = q0 - i_min * G;  // row and head of the first query
-  const int i_max = i_min + divide_group(a, h0 + nq - 1);
-  const int len = a.len[b];
-  const bool fits = rows_fit(len, rows, a.cap);
-  const int L = fits ? len : 0;
-  if (!fits && tid == 0 && a.err) atomicOr(a.err, kErrCapacity);
-  const int end = L + i_max + 1;                // entries that some row sees
-  const int cnt = fits ? (end + 127) / 128 : 0;  // key tiles
-  const int from = L + i_min + 1;               // entries that not every row sees
-  const int tail0 = from / 128;                 // the first tile that holds some
-  const bool two = nq > 128;
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *tslot;
-  if (warp >= 2 && cnt > 0) {
-    // the queries, every copy on its way at once
-    constexpr int C = D / 8;
-    const bf16* from_q = (const bf16*)a.q + (r0 + i_min) * a.q_stride + (int64_t)g * G * D;
-#pragma unroll 4
-    for (int x = tid - 64; x < nq * C; x += kThreads - 64) {
-      const int r = x / C, cc = x % C, i = divide_group(a, h0 + r), h = h0 + r - i * G;
-      ptx::cp_async16(qimg + (r >> 7) * S::STAGE + chunk_off(r & 127, cc), from_q + i * a.q_stride + h * D + 8 * cc);
-    }
-    ptx::cp_async_wait_all();
-    ptx::fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) ptx::mbar_arrive(q_full);
-  }
   // every wait is bounded; a role that gives up flags the call and waits for
   // nothing more, so that all of them come to the end
   const unsigned long long limit = a.timeout_ns;
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok && !ptx::mbar_spin(bar, parity, limit)) {
+    if (ok && !ptx::mbar_sleep(bar, parity, limit)) {
       ok = false;
       if (a.err) atomicOr(a.err, kErrTimeout);
     }
@@ -184,213 +252,337 @@ __global__ void __launch_bounds__(kThreads, 1)
   };
 
   if (warp == 0) {
-    if (lane == 0) {
-      const uint64_t pol = ptx::policy_evict_last();
-      const int z = b * a.nkv + g;
-      uint32_t n = 0, tail = 0;  // slots whose last tile is on tail_full
-      for (int t = 0; t < cnt && ok; ++t)
+    const uint64_t pol = ptx::policy_evict_last();
+    uint32_t n = 0, tail = 0, turn = 0;  // slots whose last tile is on tail_full, its parity
+    auto load = [&](int from, int to) {  // by one thread
+      const int z = it.b * a.nkv + it.g;
+      for (int t = from; t < to && ok; ++t)
         for (int kv = 0; kv < 2; ++kv, ++n) {
           const uint32_t s = n % NST, bit = 1u << s;
           if (n >= NST && !wait(&empty[s], (n / NST - 1) & 1)) break;
           uint64_t* bar = &full[s];
           tail &= ~bit;
-          if (kv && t >= tail0) {
+          if (kv && t >= it.tail0) {
             ptx::mbar_arrive(bar);  // (this tile's phase of it)
             bar = &tail_full[s];
             tail |= bit;
+            turn ^= bit;
           }
           ptx::mbar_arrive_expect_tx(bar, S::STAGE);
 #pragma unroll
           for (int h = 0; h < NR; ++h)
             ptx::tma_load_3d(ring + s * S::STAGE + h * kRegion, kv ? &tmV : &tmK, bar, 64 * h, t * 128, z, pol);
         }
-      // no copy is in flight when the CTA ends
+    };
+    for (int round = 1; it.cnt > 0; ++round) {
+      // (the next item is looked for while this one's first tiles are on their way)
+      if (lane == 0) load(0, min(it.cnt, 2));
+      __syncwarp();
+      const Item next = item_at(a, cut, round, lane);
+      if (lane == 0) load(2, it.cnt);
+      ok = __all_sync(~0u, ok);
+      it = next;
+      if (!ok) break;
+    }
+    // no copy is in flight when the CTA ends
+    if (lane == 0)
       for (uint32_t i = n > NST ? n - NST : 0; i < n; ++i) {
         const uint32_t s = i % NST;
         if ((tail >> s) & 1)
-          ptx::mbar_wait(&tail_full[s], 0, ptx::kDrainNs);
+          ptx::mbar_wait(&tail_full[s], ((turn >> s) & 1) ^ 1, ptx::kDrainNs);
         else
           ptx::mbar_wait(&full[s], (i / NST) & 1, ptx::kDrainNs);
       }
-    }
   } else if (warp == 1) {
     // the whole warp, for operands in uniform registers; one thread issues
     const uint32_t lead = ptx::elect_one(), tm = __shfl_sync(~0u, tmem, 0);
     auto whole = [&](bool) { return ok = __all_sync(~0u, ok); };
     constexpr uint32_t IDESC1 = ptx::idesc_bf16_f32(128, 128);
     constexpr uint32_t IDESC2 = ptx::idesc_bf16_f32(128, D, true);
-    const uint32_t q_lo = ptx::desc_lo(ptx::smem_u32(qimg), 16u);
+    // (shuffled, so that the compiler knows them to be the same in all threads and has a
+    // product's descriptors computed in uniform registers: 20 cycles a product, not 44)
+    auto uniform = [](uint32_t x) { return __shfl_sync(~0u, x, 0); };
+    const uint32_t q_lo = uniform(ptx::desc_lo(ptx::smem_u32(qimg), 16u));
     Stage at;
-    auto scores = [&](int t, uint32_t k) {
-      const uint32_t kt = ptx::desc_lo(ptx::smem_u32(ring + Stage::slot(k) * S::STAGE), 16u);
+    uint32_t p_turn = 0, c_turn = 0;  // parities of p_full and v_clean
+    auto stage_of = [&](uint32_t x) { return ptx::smem_u32(ring + Stage::slot(x) * S::STAGE); };
+    auto scores = [&](int t, uint32_t kt) {
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-        const uint32_t to = ((kk >> 2) * kRegion + 32u * (kk & 3)) >> 4;
-        ptx::mma_bf16_lo(lead, tm + 128 * t, q_lo + t * (S::STAGE >> 4) + to, kt + to, IDESC1, kk > 0 ? 1u : 0u);
-      }
+      for (int kk = 0; kk < D / 16; ++kk)
+        ptx::mma_bf16_lo(lead, tm + 128 * t, q_lo + (((kk >> 2) * 2 * kRegion + t * kRegion + 32u * (kk & 3)) >> 4),
+                         kt + (((kk >> 2) * kRegion + 32u * (kk & 3)) >> 4), IDESC1, kk > 0 ? 1u : 0u);
       ptx::mma_commit_if(lead, &s_full[t]);
     };
-    if (cnt > 0 && whole(wait(q_full, 0))) {
+    for (uint32_t n = 0; ok; ++n) {
+      if (n == 0 && s_item[0].cnt == 0) break;
+      if (!whole(wait(q_full, n & 1))) break;
+      const int cnt = __shfl_sync(~0u, s_item[n & 1].cnt, 0), tail0 = __shfl_sync(~0u, s_item[n & 1].tail0, 0);
+      const bool two = __shfl_sync(~0u, s_item[n & 1].nq, 0) > 128;
+      if (cnt == 0) break;
       uint32_t k = at.next<NST>(), v = at.next<NST>();
-      if (whole(wait(&full[Stage::slot(k)], Stage::parity(k)))) {
-        ptx::tc_fence_after();
-        scores(0, k);
-        if (two) scores(1, k);
-        ptx::mma_commit_if(lead, &empty[Stage::slot(k)]);
-      }
+      if (!whole(wait(&full[Stage::slot(k)], Stage::parity(k)))) break;
+      // (products run in the order of their issue: scores come after the products that
+      // read weights in their place)
+      ptx::tc_fence_after();
+      const uint32_t first = uniform(ptx::desc_lo(stage_of(k), 16u));
+      scores(0, first);
+      if (two) scores(1, first);
+      ptx::mma_commit_if(lead, &empty[Stage::slot(k)]);
+      if (cnt == 1) ptx::mma_commit_if(lead, q_empty);
       for (int j = 0; j < cnt && ok; ++j) {
         const int tail = j - tail0;
-        if (!whole(tail < 0 ? wait(&full[Stage::slot(v)], Stage::parity(v)) : wait(&v_clean[tail], 0))) break;
-        const uint32_t vt = ptx::desc_lo(ptx::smem_u32(ring + Stage::slot(v) * S::STAGE), kRegion);
+        const bool more = j + 1 < cnt;
         const uint32_t v_now = v;
-        k = at.next<NST>();
-        v = at.next<NST>();
-#pragma unroll 1
-        for (int t = 0; t < (two ? 2 : 1); ++t) {
-          if (!whole(wait(&p_full[t], j & 1))) break;
-          ptx::tc_fence_after();
+        if (more) k = at.next<NST>(), v = at.next<NST>();
+        // the values, the first tile's weights and the next keys: their first looks overlap
+        uint64_t* v_bar = tail < 0 ? &full[Stage::slot(v_now)] : &v_clean[tail];
+        const uint32_t v_parity = tail < 0 ? Stage::parity(v_now) : (c_turn >> tail) & 1;
+        const bool v_there = ptx::mbar_try_wait(v_bar, v_parity), p_there = ptx::mbar_try_wait(&p_full[0], p_turn & 1);
+        const bool k_there = !more || ptx::mbar_try_wait(&full[Stage::slot(k)], Stage::parity(k));
+        if (!v_there) wait(v_bar, v_parity);
+        if (!p_there) wait(&p_full[0], p_turn & 1);
+        if (!k_there) wait(&full[Stage::slot(k)], Stage::parity(k));
+        if (j == 0 && n > 0) wait(o_empty, (n - 1) & 1);
+        if (!whole(ok)) break;
+        if (tail >= 0) c_turn ^= 1u << tail;
+        p_turn ^= two ? 3u : 1u;
+        ptx::tc_fence_after();
+        const uint32_t vt = uniform(ptx::desc_lo(stage_of(v_now), kRegion)), kt = uniform(ptx::desc_lo(stage_of(k), 16u));
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (t == 1) {
+            if (!two) break;
+            if (!whole(wait(&p_full[1], ((p_turn >> 1) & 1) ^ 1))) break;
+            ptx::tc_fence_after();
+          }
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)
             ptx::mma_bf16_ta_lo(lead, tm + 256 + 128 * t, tm + 128 * t + 8u * kk, vt + 128u * kk, IDESC2,
                                 j > 0 || kk > 0 ? 1u : 0u);
-          if (t == (two ? 1 : 0)) ptx::mma_commit_if(lead, &empty[Stage::slot(v_now)]);
-          if (j + 1 == cnt) {
+          if (more)
+            scores(t, kt);
+          else
             ptx::mma_commit_if(lead, &o_full[t]);
-          } else {
-            // (products run in the order of their issue: these scores come after the
-            // product that reads the weights in their place)
-            if (t == 0 && !whole(wait(&full[Stage::slot(k)], Stage::parity(k)))) break;
-            ptx::tc_fence_after();
-            scores(t, k);
-            if (t == (two ? 1 : 0)) ptx::mma_commit_if(lead, &empty[Stage::slot(k)]);
-          }
         }
+        // (what was loaded is let go when all products up to here are done)
+        ptx::mma_commit_if(lead, &empty[Stage::slot(v_now)]);
+        if (more) ptx::mma_commit_if(lead, &empty[Stage::slot(k)]);
+        if (j + 2 == cnt) ptx::mma_commit_if(lead, q_empty);
       }
     }
     // no product is running when TMEM is freed
     ptx::mma_commit_if(lead, drain);
     ptx::mbar_wait(drain, 0, ptx::kDrainNs);
   } else if (warp < 4) {
-    for (int t = tail0; t < cnt; ++t) {
-      const uint32_t s = (2 * t + 1) % NST;
-      if (!wait(&tail_full[s], 0)) break;
-      clean_tile<D>(ring + s * S::STAGE, t * 128, from, end, from, tid - 64, s_bad);
-      ptx::fence_proxy_async_smem();
-      ptx::mbar_arrive(&v_clean[t - tail0]);
+    const int t64 = tid - 64;
+    uint32_t tiles = 0, turn = 0;
+    auto load_queries = [&](const Item& it) {  // by one thread
+      const int heads = min(256, a.nq / a.nkv);
+      ptx::mbar_arrive_expect_tx(q_full, NR * 128 * heads * cut.rows_each);
+#pragma unroll
+      for (int h = 0; h < NR; ++h)
+        ptx::tma_load_3d(qimg + 2 * h * kRegion, &tmQ, q_full, 64 * h, it.g * (a.nq / a.nkv) + it.h0, it.r0 + it.i_min,
+                         ptx::policy_evict_first());
+    };
+    if (t64 == 0 && s_item[0].cnt > 0) load_queries(s_item[0]);
+    uint32_t loaded = 1;
+    for (uint32_t n = 0;; ++n) {
+      it = s_item[n & 1];
+      if (it.cnt == 0) break;
+      // the results of the item before are read: so are its description and what was noted for it
+      if (n > 0) wait(o_empty, (n - 1) & 1);
+      if (warp == 2) {
+        const Item next = item_at(a, cut, n + 1, lane);
+        if (lane == 0) s_item[(n + 1) & 1] = next;
+      }
+      if (t64 < 4 * kMaxTails) s_bad[t64] = 0;
+      ptx::named_bar_sync(9, 64);
+      for (int t = it.tail0; t < it.cnt; ++t) {
+        const uint32_t s = (2 * (tiles + t) + 1) % NST;
+        const bool here = wait(&tail_full[s], (turn >> s) & 1);
+        turn ^= 1u << s;
+        if (!here) continue;  // (nor is this one let go)
+        clean_tile<D>(ring + s * S::STAGE, t * 128, it.from, it.end, it.from, t64, s_bad);
+        ptx::fence_proxy_async_smem();
+        ptx::mbar_arrive(&v_clean[t - it.tail0]);
+      }
+      tiles += it.cnt;
+      // the next item's queries, when this one's have been read
+      if (t64 == 0 && wait(q_empty, n & 1)) {
+        if (s_item[(n + 1) & 1].cnt > 0) {
+          load_queries(s_item[(n + 1) & 1]);
+          ++loaded;
+        } else {
+          ptx::mbar_arrive(q_full);
+        }
+      }
     }
-  } else if (cnt > 0 && (two || warp < 8)) {
-    const int t = (warp - 4) >> 2, quad = warp & 3, row = 32 * quad + lane;
+    // no copy is in flight when the CTA ends (q_empty says so of those that were waited for)
+    if (t64 == 0 && tiles > 0 && !ok) ptx::mbar_wait(q_full, (loaded - 1) & 1, ptx::kDrainNs);
+  } else {
+    const int quad = warp & 3, t = (warp - 4) >> 2, row = 32 * quad + lane;
     const uint32_t tl = tmem + ((uint32_t)(32 * quad) << 16);
     const uint32_t ts = tl + 128 * t, to = tl + 256 + 128 * t;
-    const bool live = 128 * t + row < nq;
-    const int q = h0 + min(128 * t + row, nq - 1), of = divide_group(a, q), i = i_min + of, h = g * G + (q - of * G);
+    const int G = a.nq / a.nkv;
     const float c = a.scale_log2;
-    float m = -INFINITY, l = 0.f;
-#pragma unroll 1
-    for (int j = 0; j < cnt; ++j) {
-      wait(&s_full[t], j & 1);
+    uint32_t ns = 0, mine_items = 0, c_turn = 0;
+    for (uint32_t n = 0;; ++n) {
+      if (n == 0 && s_item[0].cnt == 0) break;
+      wait(q_full, n & 1);
       ok = __all_sync(~0u, ok);
-      ptx::tc_fence_after();
-      uint32_t v[128];
-#pragma unroll
-      for (int x = 0; x < 128; x += 32) ptx::tmem_ld32(ts + x, v + x);
-      ptx::tmem_ld_wait();
-      const int seen = L + i + 1 - j * 128;  // entries of the tile that the row sees
-      if (j >= tail0) {
-#pragma unroll
-        for (int e = 0; e < 128; ++e)
-          if (e >= seen) v[e] = 0xFF800000u;  // -inf
-      }
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int e = 0; e < 128; e += 8)
-#pragma unroll
-        for (int f = 0; f < 4; ++f)
-          mx[f] = max3(mx[f], __uint_as_float(v[e + 2 * f]), __uint_as_float(v[e + 2 * f + 1]));
-      const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-      // (NaN scores pass the maximum by, and reach the sums)
-      const bool grow = mt > m + kLazy;
-      if (__any_sync(~0u, grow)) {
-        const float m_new = grow ? mt : m;
-        const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
-        l = grow ? l * f : l;
-        if (j > 0) {
+      const int cnt = s_item[n & 1].cnt;
+      if (!ok || cnt == 0) break;
+      const int tail0 = s_item[n & 1].tail0, nq = s_item[n & 1].nq;
+      const bool some = nq > 128 * t;  // the tile has queries
+      // the last entry that the row sees
+      const int last = s_item[n & 1].L + s_item[n & 1].i_min + divide_group(a, s_item[n & 1].h0 + min(128 * t + row, nq - 1));
+      // (a row that is no query's has what was in its place before, of no consequence)
+      const bool live = 128 * t + row < nq;
+      float m = live ? -INFINITY : 0.f, l = 0.f;
+      bool fresh = __any_sync(~0u, live);  // a row has no reference yet
+      if (some) {
 #pragma unroll 1
-          for (int x = 0; x < D; x += 16) {
-            uint32_t o[16];
-            ptx::tmem_ld16(to + x, o);
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = grow ? __float_as_uint(__uint_as_float(o[e]) * f) : o[e];
-            ptx::tmem_st16(to + x, o);
-          }
-        }
-        m = m_new;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      const uint64_t c2 = as2d::two(c, c), ref2 = as2d::two(-ref, -ref);
-      uint64_t ls[2] = {0, 0};
-#pragma unroll
-      for (int x = 0; x < 128; x += 32) {
-        uint32_t p[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float2 y = of_two(fma2(as2d::two(__uint_as_float(v[x + 2 * e]), __uint_as_float(v[x + 2 * e + 1])), c2, ref2));
-          const uint64_t w = as2d::two(ex2(y.x), ex2(y.y));
-          ls[e & 1] = add2(ls[e & 1], w);
-          const float2 f = of_two(w);
-          p[e] = pack2(f.x, f.y);
-        }
-        ptx::tmem_st16(ts + x / 2, p);
-      }
-      const float2 sums = of_two(add2(ls[0], ls[1]));
-      l += sums.x + sums.y;
-      ptx::tmem_st_wait();
-      ptx::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&p_full[t]);
-    }
-    wait(&o_full[t], 0);
-    for (int x = 0; x < cnt - tail0; ++x) wait(&v_clean[x], 0);
-    ok = __all_sync(~0u, ok);
-    ptx::tc_fence_after();
-    if (ok) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      bf16* out = (bf16*)a.out + ((size_t)(r0 + i) * a.nq + h) * D;
-      uint32_t any = 0;
-      for (int x = 0; x < 4 * kMaxTails; ++x) any |= s_bad[x];
+        for (int j = 0; j < cnt; ++j, ++ns) {
+          wait(&s_full[t], ns & 1);
+          __syncwarp();
+          ptx::tc_fence_after();
+          const bool tail = j >= tail0;
+          const int seen = last + 1 - j * 128;  // entries of the tile that the row sees
+          uint32_t p[64];
+          float sum;
+          bool need = m == -INFINITY, again = fresh;
 #pragma unroll 1
-      for (int d0 = 0; d0 < D; d0 += 16) {
-        uint32_t o[16];
-        ptx::tmem_ld16(to + d0, o);
-        ptx::tmem_ld_wait();
-        if (any) {
-          // values that are not finite in entries that not every row sees: added where they are seen
-          for (int x = 0; x < 4 * kMaxTails; ++x)
-            for (uint32_t left = s_bad[x]; left; left &= left - 1) {
-              const int e = from + 32 * x + __ffs(left) - 1;
-              if (e > L + i) continue;
-              const bf16* v = a.v + (((size_t)b * a.nkv + g) * a.cap + e) * D + d0;
+          for (;;) {
+            if (again) {
+              float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll 1
+              for (int x = 0; x < 128; x += 32) {
+                uint32_t v[32];
+                ptx::tmem_ld32(ts + x, v);
+                ptx::tmem_ld_wait();
 #pragma unroll
-              for (int y = 0; y < 16; ++y) {
-                const float z = __bfloat162float(v[y]);
-                if (!(fabsf(z) <= 3.4e38f)) o[y] = __float_as_uint(__uint_as_float(o[y]) + z);
+                for (int e = 0; e < 32; ++e)
+                  if (!tail || x + e < seen) mx[e & 1] = fmaxf(mx[e & 1], __uint_as_float(v[e]));
+              }
+              // (NaN scores pass the maximum by, and reach the sums)
+              const float mt = fmaxf(mx[0], mx[1]) * c;
+              // (a row whose sum is fine keeps its reference: what another row sees changes nothing for it)
+              const bool grow = need && mt > m;
+              const float m_new = grow ? mt : m, f = m == -INFINITY ? 0.f : ex2(m - m_new);
+              l = grow ? l * f : l;
+              if (j > 0) {
+#pragma unroll 1
+                for (int x = 0; x < D; x += 16) {
+                  uint32_t o[16];
+                  ptx::tmem_ld16(to + x, o);
+                  ptx::tmem_ld_wait();
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) o[e] = grow ? __float_as_uint(__uint_as_float(o[e]) * f) : o[e];
+                  ptx::tmem_st16(to + x, o);
+                }
+              }
+              m = m_new;
+              fresh = __any_sync(~0u, m == -INFINITY);
+            }
+            const float ref = m == -INFINITY ? 0.f : m;
+            const uint64_t c2 = as2d::two(c, c), ref2 = as2d::two(-ref, -ref);
+            uint64_t ls[2] = {0, 0};
+            uint32_t v[2][32];
+            ptx::tmem_ld32(ts, v[0]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              ptx::tmem_ld_wait();
+              if (x < 3) ptx::tmem_ld32(ts + 32 * (x + 1), v[(x + 1) & 1]);
+              uint32_t(&u)[32] = v[x & 1];
+              if (tail) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  if (32 * x + e >= seen) u[e] = 0xFF800000u;  // -inf
+              }
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float2 y = of_two(fma2(as2d::two(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1])), c2, ref2));
+                const uint64_t w = as2d::two(ex2(y.x), ex2(y.y));
+                ls[e & 1] = add2(ls[e & 1], w);
+                const float2 f = of_two(w);
+                p[16 * x + e] = pack2(f.x, f.y);
               }
             }
+            const float2 sums = of_two(add2(ls[0], ls[1]));
+            sum = sums.x + sums.y;
+            need = live && !(sum <= kMost);
+            if (again || !__any_sync(~0u, need)) break;
+            again = true;
+          }
+#pragma unroll
+          for (int x = 0; x < 64; x += 16) ptx::tmem_st16(ts + x, p + x);
+          l += sum;
+          ptx::tmem_st_wait();
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&p_full[t]);
           __syncwarp();
         }
-        if (live) {
-          uint32_t p[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = pack2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
-          reinterpret_cast<uint4*>(out + d0)[0] = make_uint4(p[0], p[1], p[2], p[3]);
-          reinterpret_cast<uint4*>(out + d0)[1] = make_uint4(p[4], p[5], p[6], p[7]);
-        }
-        __syncwarp();
+        // ---- the item's end ----
+        wait(&o_full[t], mine_items & 1);
+        ++mine_items;
+      } else {
+        wait(&o_full[0], n & 1);  // (not an item ahead of the others)
       }
-      if (live && a.lse) a.lse[(size_t)(r0 + i) * a.nq + h] = row_lse(m, l);
+      for (int x = 0; x < cnt - tail0; ++x) {
+        if (some) wait(&v_clean[x], (c_turn >> x) & 1);
+        c_turn ^= 1u << x;
+      }
+      ok = __all_sync(~0u, ok);
+      ptx::tc_fence_after();
+      if (some && ok) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        it = s_item[n & 1];
+        const int q = it.h0 + min(128 * t + row, nq - 1), of = divide_group(a, q), h = it.g * G + (q - of * G);
+        const size_t at = (size_t)(it.r0 + it.i_min + of) * a.nq + h;
+        bf16* out = (bf16*)a.out + at * D;
+        uint32_t any = 0;
+        if (cnt > tail0)
+          for (int x = 0; x < 4 * kMaxTails; ++x) any |= s_bad[x];
+#pragma unroll 1
+        for (int d0 = 0; d0 < D; d0 += 32) {
+          uint32_t o[32];
+          ptx::tmem_ld32(to + d0, o);
+          ptx::tmem_ld_wait();
+          if (any) {
+            // values that are not finite in entries that not every row sees: added where they are seen
+            for (int x = 0; x < 4 * kMaxTails; ++x)
+              for (uint32_t left = s_bad[x]; left; left &= left - 1) {
+                const int e = it.from + 32 * x + __ffs(left) - 1;
+                if (e > last) continue;
+                const bf16* u = a.v + (((size_t)it.b * a.nkv + it.g) * a.cap + e) * D + d0;
+#pragma unroll
+                for (int y = 0; y < 32; ++y) {
+                  const float z = __bfloat162float(u[y]);
+                  if (!(fabsf(z) <= 3.4e38f)) o[y] = __float_as_uint(__uint_as_float(o[y]) + z);
+                }
+              }
+            __syncwarp();
+          }
+          if (live) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 16) {
+              uint32_t w[8];
+#pragma unroll
+              for (int y = 0; y < 8; ++y)
+                w[y] = pack2(__uint_as_float(o[e + 2 * y]) * inv, __uint_as_float(o[e + 2 * y + 1]) * inv);
+              ptx::store_8(out + d0 + e, w);
+            }
+          }
+          __syncwarp();
+        }
+        if (live && a.lse) a.lse[at] = row_lse(m, l);
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(o_empty);
+      __syncwarp();
     }
-    ptx::tc_fence_before();
   }
   __syncthreads();
   if (warp == 1) {
@@ -400,36 +592,30 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 template <int D>
-cudaError_t launch(const CUtensorMap& tk, const CUtensorMap& tv, const TreeArgs& a, const Items& items, int64_t n,
-                   cudaStream_t st) {
+cudaError_t launch(const TreeArgs& a, Cut cut, int64_t n, cudaStream_t st) {
   static PerDevice opted;
   const cudaError_t e = opt_in(opted, prompt_kernel<D>, Shape<D>::SMEM);
   if (e != cudaSuccess) return e;
-  return launch_pdl(prompt_kernel<D>, dim3((unsigned)n), dim3(kThreads), Shape<D>::SMEM, st, 1, tk, tv, a, items);
+  CUtensorMap tq, tk, tv;
+  const int64_t heads = (int64_t)a.rm.batch * a.nkv;
+  if (!encode_rows_map(&tq, a.q, D, a.nq, a.rm.rows, a.q_stride, std::min(256, a.nq / a.nkv), cut.rows_each) ||
+      !encode_cache_map(&tk, a.k, D, a.cap, heads) || !encode_cache_map(&tv, a.v, D, a.cap, heads))
+    return cudaErrorInvalidValue;
+  return launch_pdl(prompt_kernel<D>, dim3((unsigned)std::min<int64_t>(n, device_sms())), dim3(kThreads), Shape<D>::SMEM,
+                    st, 1, tq, tk, tv, a, cut);
 }
 
 }  // namespace
 
-size_t prompt_attention_workspace(int) { return 256; }
-
-cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
-                                    cudaStream_t st) {
-  Items items = {};
-  const int G = a.nq / a.nkv, batch = a.rm.batch;
-  auto rows = [&](int b) { return a.rm.start[b + 1] - a.rm.start[b]; };
-  for (int b = 0; b < batch; ++b) items.request[b] = (uint8_t)b;
-  std::stable_sort(items.request, items.request + batch, [&](uint8_t x, uint8_t y) { return rows(x) > rows(y); });
+cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, cudaStream_t st) {
+  const int G = a.nq / a.nkv;
+  const Cut cut = {std::max(1, 256 / G), (G + 255) / 256};
   int64_t n = 0;
-  for (int k = 0; k < batch; ++k) {
-    items.first[k] = (int)n;
-    n += ((int64_t)rows(items.request[k]) * G + 255) / 256 * a.nkv;
+  for (int b = 0; b < a.rm.batch; ++b) {
+    const int64_t r = a.rm.start[b + 1] - a.rm.start[b];
+    n += (cut.chunks > 1 ? r * cut.chunks : (r + cut.rows_each - 1) / cut.rows_each) * a.nkv;
   }
-  items.first[batch] = (int)n;
-  CUtensorMap tk, tv;
-  if (!encode_cache_map(&tk, a.k, head_dim, a.cap, (int64_t)batch * a.nkv) ||
-      !encode_cache_map(&tv, a.v, head_dim, a.cap, (int64_t)batch * a.nkv))
-    return cudaErrorInvalidValue;
-  return head_dim == 128 ? launch<128>(tk, tv, a, items, n, st) : launch<64>(tk, tv, a, items, n, st);
+  return head_dim == 128 ? launch<128>(a, cut, n, st) : launch<64>(a, cut, n, st);
 }
 
 }  // namespace as2d

@@ -88,10 +88,43 @@ __device__ __forceinline__ bool mbar_spin(uint64_t* bar, uint32_t parity, uint64
   }
 }
 
+// As mbar_wait, for warps beside which others compute: the thread is suspended until the phase
+// completes, for up to kSuspendNs at a time (tries that return at once are instructions of the
+// queue that exponentials go through too).
+constexpr uint32_t kSuspendNs = 100000;
+__device__ __forceinline__ bool mbar_sleep(uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
+  uint64_t t0 = 0;
+  for (uint32_t i = 0;; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs)
+        : "memory");
+    if (ok) return true;
+    if ((i & 15u) == 15u) {
+      const uint64_t t = globaltimer_ns();
+      if (t0 == 0)
+        t0 = t;
+      else if (t - t0 >= limit_ns)
+        return false;
+    }
+  }
+}
+
 // Limit of the waits by which a CTA drains its own outstanding bulk copies
 // and tensor-core products before it exits: never shortened, so that no copy
 // or product is still outstanding when a CTA ends.
 constexpr uint64_t kDrainNs = 2000000000ull;
+
+// 32 bytes to a 32-byte aligned address in one store.
+__device__ __forceinline__ void store_8(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(__cvta_generic_to_global(p)), "r"(v[0]),
+               "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
 
 // ---- TMA ------------------------------------------------------------------------
 
