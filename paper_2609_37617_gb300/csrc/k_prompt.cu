@@ -44,13 +44,23 @@ constexpr float kMost = 8192.f;
 // How queries are cut into items.
 struct Cut {
   int rows_each, chunks;  // whole rows of an item, or items of a row
+  int parts;              // of an item's key tiles; more than one where there are fewer items than SMs
+};
+// Partial results of an item's parts; at most kSlots an SM, of parts of kPartTiles tiles at least (but
+// for requests shorter than the host's bound).
+constexpr int kSlots = 2, kPartTiles = 4;
+struct Parts {
+  float4* o;   // [slot][D / 4][256], four dims of a query together; slot: item parts + part
+  float2* ml;  // [slot][256] (reference base 2, sum)
 };
 
 struct Item {
   int b, g, r0, L;
   int i_min, h0, nq;  // row and head (of the group) of its first query, queries
   int end, from;      // entries that some row sees; from the first that not every row does
-  int cnt, tail0;     // key tiles (0: there are no more items); the first that holds such entries
+  int t0, cnt;        // key tiles: the first, how many (0: there are no more items)
+  int tail0;          // the first that holds such entries, from t0
+  int slot;           // of its partial results
 };
 
 template <int D>
@@ -62,13 +72,11 @@ struct Shape {
   static_assert(SMEM <= 232448, "shared memory of one CTA");
 };
 
-// The n-th item of this CTA, by a whole warp: the items of all requests in the order of their key
-// tiles, most first, go over the CTAs back and forth.  (tiles 0: there are no more.  Not inlined:
-// two roles run it, once an item.)  A request's k-th item has (end of its last row + 127) / 128 tiles,
+// An item of all requests' in the order of their key tiles, most first, by a whole warp.  (No
+// tiles: there are no more.  Not inlined: two roles run it, once an item.)  A request's k-th item has (end of its last row + 127) / 128 tiles,
 // so that those with at least T need no list to be counted.
-static __device__ __noinline__ Item item_at(const TreeArgs& a, Cut cut, int n, int lane) {
-  const int ctas = gridDim.x, G = a.nq / a.nkv;
-  const int64_t at = (int64_t)n * ctas + (n & 1 ? ctas - 1 - (int)blockIdx.x : (int)blockIdx.x);
+static __device__ __noinline__ Item item_at(const TreeArgs& a, Cut cut, int64_t at, int lane) {
+  const int G = a.nq / a.nkv;
   int L[2], rows[2], items[2], most = 0;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -137,9 +145,29 @@ static __device__ __noinline__ Item item_at(const TreeArgs& a, Cut cut, int n, i
   }
   it.end = it.L + it.i_min + divide_group(a, it.h0 + it.nq - 1) + 1;
   it.from = it.L + it.i_min + 1;
+  it.t0 = 0;
   it.cnt = T;
   it.tail0 = it.from / 128;
   return it;
+}
+
+// The n-th item, or part of one, of this CTA: back and forth over the CTAs; of parts, those without tiles
+// are passed by (n: the one after it).
+__device__ __forceinline__ Item item_of_cta(const TreeArgs& a, Cut cut, int& n, int lane, const Parts& parts) {
+  const int ctas = gridDim.x, c = blockIdx.x;
+  for (;;) {
+    const int64_t at = (int64_t)n * ctas + (n & 1 ? ctas - 1 - c : c);
+    ++n;
+    Item it = item_at(a, cut, at / cut.parts, lane);
+    if (cut.parts == 1 || it.cnt == 0) return it;
+    const int T = it.cnt, part = (int)(at % cut.parts);
+    it.slot = (int)at;
+    it.t0 = T * part / cut.parts;
+    it.cnt = T * (part + 1) / cut.parts - it.t0;
+    it.tail0 -= it.t0;
+    if (it.cnt > 0) return it;
+    for (int r = lane; r < 256; r += 32) parts.ml[at * 256 + r] = make_float2(-INFINITY, 0.f);
+  }
 }
 
 // Of a value tile the entries from `from` on, which not every row of the item sees: values
@@ -178,7 +206,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     prompt_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                   const __grid_constant__ CUtensorMap tmV,
-                  const __grid_constant__ TreeArgs a, const Cut cut) {
+                  const __grid_constant__ TreeArgs a, const Cut cut, const Parts parts) {
   using S = Shape<D>;
   constexpr int NST = S::NST, NR = D / 64;
   extern __shared__ __align__(1024) uint8_t sm[];  // (the kernel has no other shared memory)
@@ -227,7 +255,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   Item it;  // of the two roles that look for the items
-  if (warp == 0 || warp == 2) it = item_at(a, cut, 0, lane);
+  int next_item = 0;
+  if (warp == 0 || warp == 2) it = item_of_cta(a, cut, next_item, lane, parts);
   if (tid == 64) s_item[0] = it;
   if (warp == 3 && blockIdx.x == 0) {
     bool over = false;
@@ -271,14 +300,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::mbar_arrive_expect_tx(bar, S::STAGE);
 #pragma unroll
           for (int h = 0; h < NR; ++h)
-            ptx::tma_load_3d(ring + s * S::STAGE + h * kRegion, kv ? &tmV : &tmK, bar, 64 * h, t * 128, z, pol);
+            ptx::tma_load_3d(ring + s * S::STAGE + h * kRegion, kv ? &tmV : &tmK, bar, 64 * h, (it.t0 + t) * 128, z, pol);
         }
     };
-    for (int round = 1; it.cnt > 0; ++round) {
+    while (it.cnt > 0) {
       // (the next item is looked for while this one's first tiles are on their way)
       if (lane == 0) load(0, min(it.cnt, 2));
       __syncwarp();
-      const Item next = item_at(a, cut, round, lane);
+      const Item next = item_of_cta(a, cut, next_item, lane, parts);
       if (lane == 0) load(2, it.cnt);
       ok = __all_sync(~0u, ok);
       it = next;
@@ -392,17 +421,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       // the results of the item before are read: so are its description and what was noted for it
       if (n > 0) wait(o_empty, (n - 1) & 1);
       if (warp == 2) {
-        const Item next = item_at(a, cut, n + 1, lane);
+        const Item next = item_of_cta(a, cut, next_item, lane, parts);
         if (lane == 0) s_item[(n + 1) & 1] = next;
       }
       if (t64 < 4 * kMaxTails) s_bad[t64] = 0;
       ptx::named_bar_sync(9, 64);
-      for (int t = it.tail0; t < it.cnt; ++t) {
+      for (int t = max(it.tail0, 0); t < it.cnt; ++t) {
         const uint32_t s = (2 * (tiles + t) + 1) % NST;
         const bool here = wait(&tail_full[s], (turn >> s) & 1);
         turn ^= 1u << s;
         if (!here) continue;  // (nor is this one let go)
-        clean_tile<D>(ring + s * S::STAGE, t * 128, it.from, it.end, it.from, t64, s_bad);
+        clean_tile<D>(ring + s * S::STAGE, (it.t0 + t) * 128, it.from, it.end, it.from, t64, s_bad);
         ptx::fence_proxy_async_smem();
         ptx::mbar_arrive(&v_clean[t - it.tail0]);
       }
@@ -432,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = __all_sync(~0u, ok);
       const int cnt = s_item[n & 1].cnt;
       if (!ok || cnt == 0) break;
-      const int tail0 = s_item[n & 1].tail0, nq = s_item[n & 1].nq;
+      const int tail0 = s_item[n & 1].tail0, nq = s_item[n & 1].nq, t0 = s_item[n & 1].t0;
       const bool some = nq > 128 * t;  // the tile has queries
       // the last entry that the row sees
       const int last = s_item[n & 1].L + s_item[n & 1].i_min + divide_group(a, s_item[n & 1].h0 + min(128 * t + row, nq - 1));
@@ -447,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           ptx::tc_fence_after();
           const bool tail = j >= tail0;
-          const int seen = last + 1 - j * 128;  // entries of the tile that the row sees
+          const int seen = last + 1 - (t0 + j) * 128;  // entries of the tile that the row sees
           uint32_t p[64];
           float sum;
           bool need = m == -INFINITY, again = fresh;
@@ -529,7 +558,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else {
         wait(&o_full[0], n & 1);  // (not an item ahead of the others)
       }
-      for (int x = 0; x < cnt - tail0; ++x) {
+      for (int x = max(-tail0, 0); x < cnt - tail0; ++x) {
         if (some) wait(&v_clean[x], (c_turn >> x) & 1);
         c_turn ^= 1u << x;
       }
@@ -564,7 +593,13 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             __syncwarp();
           }
-          if (live) {
+          if (live && cut.parts > 1) {
+            float4* to_part = parts.o + ((size_t)it.slot * (D / 4) + d0 / 4) * 256 + 128 * t + row;
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              to_part[e / 4 * 256] = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]),
+                                                 __uint_as_float(o[e + 3]));
+          } else if (live) {
 #pragma unroll
             for (int e = 0; e < 32; e += 16) {
               uint32_t w[8];
@@ -576,7 +611,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           __syncwarp();
         }
-        if (live && a.lse) a.lse[at] = row_lse(m, l);
+        if (live && cut.parts > 1)
+          parts.ml[(size_t)it.slot * 256 + 128 * t + row] = make_float2(m, l);
+        else if (live && a.lse)
+          a.lse[at] = row_lse(m, l);
       }
       ptx::tc_fence_before();
       __syncwarp();
@@ -591,31 +629,115 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+// The parts of items joined, in the order of their tiles: a block for 32 queries of an item, a lane to a
+// query.
+constexpr int kJoinWarps = 8;
 template <int D>
-cudaError_t launch(const TreeArgs& a, Cut cut, int64_t n, cudaStream_t st) {
+__global__ void __launch_bounds__(32 * kJoinWarps)
+    prompt_join_kernel(const __grid_constant__ TreeArgs a, const Cut cut, const Parts parts) {
+  __shared__ Item s_item;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockIdx.x / 8, row = blockIdx.x % 8 * 32 + lane;
+  ptx::griddep_launch_dependents();
+  // (the lengths before the wait: the kernel before lets this one start after its own, and writes none)
+  if (warp == 0) {
+    const Item it = item_at(a, cut, n, lane);
+    if (lane == 0) s_item = it;
+  }
+  __syncthreads();
+  ptx::griddep_wait();
+  if (s_item.cnt == 0 || row >= s_item.nq) return;
+  const int G = a.nq / a.nkv;
+  const int q = s_item.h0 + row, of = divide_group(a, q), h = s_item.g * G + (q - of * G);
+  const size_t at = (size_t)(s_item.r0 + s_item.i_min + of) * a.nq + h;
+  constexpr int Z = D / 4 / kJoinWarps, U = 4;  // of a lane; parts in flight
+  float M = -INFINITY, l = 0.f;
+  float4 o[Z];
+#pragma unroll
+  for (int z = 0; z < Z; ++z) o[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = 0; k0 < cut.parts; k0 += U) {
+    float2 ml[U];
+    float4 v[U][Z];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t slot = n * cut.parts + min(k0 + u, cut.parts - 1);
+      ml[u] = __ldcg(&parts.ml[slot * 256 + row]);
+      if (k0 + u >= cut.parts) ml[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int z = 0; z < Z; ++z) v[u][z] = __ldcg(&parts.o[(slot * (D / 4) + warp * Z + z) * 256 + row]);
+    }
+    const float before = M;
+#pragma unroll
+    for (int u = 0; u < U; ++u) M = fmaxf(M, ml[u].x);
+    const float w = part_weight(before, M);
+    // (what a part has that is not finite stays, whatever its weight; one without tiles has nothing)
+    auto weighted = [](float x, float f) { return is_finite(x) ? x * f : x; };
+    l *= w;  // (a NaN stays)
+#pragma unroll
+    for (int z = 0; z < Z; ++z)
+      o[z] = make_float4(weighted(o[z].x, w), weighted(o[z].y, w), weighted(o[z].z, w), weighted(o[z].w, w));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = part_weight(ml[u].x, M);
+      l = fmaf(ml[u].y, f, l);
+      if (ml[u].x == -INFINITY && ml[u].y == 0.f) continue;
+#pragma unroll
+      for (int z = 0; z < Z; ++z) {
+        o[z].x += weighted(v[u][z].x, f);
+        o[z].y += weighted(v[u][z].y, f);
+        o[z].z += weighted(v[u][z].z, f);
+        o[z].w += weighted(v[u][z].w, f);
+      }
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  bf16* out = (bf16*)a.out + at * D + warp * Z * 4;
+#pragma unroll
+  for (int z = 0; z < Z; ++z)
+    *reinterpret_cast<uint2*>(out + 4 * z) =
+        make_uint2(pack2(o[z].x * inv, o[z].y * inv), pack2(o[z].z * inv, o[z].w * inv));
+  if (warp == 0 && a.lse) a.lse[at] = row_lse(M, l);
+}
+
+template <int D>
+cudaError_t launch(const TreeArgs& a, Cut cut, int64_t n, void* workspace, cudaStream_t st) {
   static PerDevice opted;
-  const cudaError_t e = opt_in(opted, prompt_kernel<D>, Shape<D>::SMEM);
+  cudaError_t e = opt_in(opted, prompt_kernel<D>, Shape<D>::SMEM);
   if (e != cudaSuccess) return e;
   CUtensorMap tq, tk, tv;
   const int64_t heads = (int64_t)a.rm.batch * a.nkv;
   if (!encode_rows_map(&tq, a.q, D, a.nq, a.rm.rows, a.q_stride, std::min(256, a.nq / a.nkv), cut.rows_each) ||
       !encode_cache_map(&tk, a.k, D, a.cap, heads) || !encode_cache_map(&tv, a.v, D, a.cap, heads))
     return cudaErrorInvalidValue;
-  return launch_pdl(prompt_kernel<D>, dim3((unsigned)std::min<int64_t>(n, device_sms())), dim3(kThreads), Shape<D>::SMEM,
-                    st, 1, tq, tk, tv, a, cut);
+  Parts parts;
+  parts.o = (float4*)workspace;
+  parts.ml = (float2*)(parts.o + (size_t)kSlots * device_sms() * 256 * D / 4);
+  e = launch_pdl(prompt_kernel<D>, dim3((unsigned)std::min<int64_t>(n * cut.parts, device_sms())), dim3(kThreads),
+                 Shape<D>::SMEM, st, 1, tq, tk, tv, a, cut, parts);
+  if (e != cudaSuccess || cut.parts == 1) return e;
+  return launch_pdl(prompt_join_kernel<D>, dim3((unsigned)n * 8), dim3(32 * kJoinWarps), 0, st, 1, a, cut, parts);
 }
 
 }  // namespace
 
-cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, cudaStream_t st) {
-  const int G = a.nq / a.nkv;
-  const Cut cut = {std::max(1, 256 / G), (G + 255) / 256};
+size_t prompt_attention_workspace(int head_dim) {
+  return (size_t)kSlots * device_sms() * 256 * (head_dim * 4 + 8);
+}
+
+cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
+                                    cudaStream_t st) {
+  const int G = a.nq / a.nkv, sms = device_sms();
+  Cut cut = {std::max(1, 256 / G), (G + 255) / 256, 1};
   int64_t n = 0;
   for (int b = 0; b < a.rm.batch; ++b) {
     const int64_t r = a.rm.start[b + 1] - a.rm.start[b];
     n += (cut.chunks > 1 ? r * cut.chunks : (r + cut.rows_each - 1) / cut.rows_each) * a.nkv;
   }
-  return head_dim == 128 ? launch<128>(a, cut, n, st) : launch<64>(a, cut, n, st);
+  // Few items of many tiles: one part a CTA, or where that is less than two, parts for two
+  // rounds.  us, 28 query and 4 kv heads, 128 rows after 15000 / 4000 / 1000 entries: whole 189 / 60 / 24, parts of
+  // four tiles at least 42 / 26 / 22, of eight 42 / 29 / 24.
+  const int64_t tiles = (max_keys + 127) / 128;
+  if (n <= sms) cut.parts = (int)std::max<int64_t>(1, std::min<int64_t>((2 * n <= sms ? 1 : kSlots) * sms / n, tiles / kPartTiles));
+  return head_dim == 128 ? launch<128>(a, cut, n, workspace, st) : launch<64>(a, cut, n, workspace, st);
 }
 
 }  // namespace as2d

@@ -86,8 +86,6 @@ struct Shape {
   static_assert(SMEM + sizeof(UnitPlan) + sizeof(First) <= 232448, "shared memory of one CTA");
 };
 
-__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= FLT_MAX; }
-
 // An accumulator of weight w; infinities and NaN as they are, as no weight of the
 // formula is 0.
 __device__ __forceinline__ float weighted(float x, float w) { return is_finite(x) ? x * w : x; }

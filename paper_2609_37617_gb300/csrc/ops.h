@@ -175,6 +175,8 @@ cudaError_t launch_pack4(const Pack4Args& a, int head_dim, bool write, int max_e
 cudaError_t launch_attention4(const Tree4Args& a, int head_dim, int64_t max_keys, void* workspace, cudaStream_t st);
 cudaError_t launch_attention4_wide(const Tree4Args& a, int head_dim, int64_t max_keys, void* workspace, cudaStream_t st);
 size_t attention4_workspace(int head_dim);
-cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, cudaStream_t st);
+cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
+                                    cudaStream_t st);
+size_t prompt_attention_workspace(int head_dim);
 
 }  // namespace as2d

@@ -431,7 +431,7 @@ extern "C" as2d_status as2d_prompt_attention_workspace(const as2d_cache* cache, 
   const as2d_status st = check_cache(cache, false);
   if (st != AS2D_OK) return st;
   if (!bytes) return invalid("bytes is NULL");
-  *bytes = 256;
+  *bytes = (int64_t)prompt_attention_workspace(cache->head_dim);
   return AS2D_OK;
 }
 
@@ -448,7 +448,7 @@ extern "C" as2d_status as2d_prompt_attention(const as2d_cache* cache, int32_t la
   if (a.q_f32) return report_error(AS2D_ERR_UNSUPPORTED, "prompt attention takes bf16 queries");
   if (a.visible) return invalid("visible must be NULL: prompts are causal");
   if (a.rm.rows > (1 << 24)) return report_error(AS2D_ERR_UNSUPPORTED, "more than 2^24 rows");
-  st = check_workspace(workspace, workspace_bytes, 256);
+  st = check_workspace(workspace, workspace_bytes, prompt_attention_workspace(cache->head_dim));
   if (st != AS2D_OK) return st;
   if (a.rm.rows == 0) return AS2D_OK;
   if (!out || !aligned(out, 32)) return invalid("out must be 32-byte aligned");
@@ -456,6 +456,6 @@ extern "C" as2d_status as2d_prompt_attention(const as2d_cache* cache, int32_t la
   a.out = out;
   a.lse = lse;
   a.err = error_bits;
-  return launched(launch_prompt_attention(a, cache->head_dim, (cudaStream_t)stream),
+  return launched(launch_prompt_attention(a, cache->head_dim, max_keys, workspace, (cudaStream_t)stream),
                   "as2d_prompt_attention");
 }

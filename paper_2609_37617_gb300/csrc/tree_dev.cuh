@@ -3,6 +3,8 @@
 // k_attn_weights.cu).
 #pragma once
 
+#include <cfloat>
+
 #include "ptx_sm100.cuh"
 #include "tree_plan.cuh"
 
@@ -115,6 +117,8 @@ __device__ __forceinline__ void mask_scores(uint32_t (&v)[32], uint32_t bits) {
 __device__ __forceinline__ float part_weight(float m, float M) {
   return m == -INFINITY ? 0.f : (m == M ? 1.f : ex2(m - M));
 }
+
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= FLT_MAX; }
 
 // The ring's next stage and its parity, as slot | parity << 8.
 struct Stage {

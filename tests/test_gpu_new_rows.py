@@ -486,6 +486,29 @@ def test_prompt_long(lib):
     check(x, *prompt(lib, x), p_rel=P_REL)
 
 
+@pytest.mark.parametrize("heads", [(28, 4, 128), (4, 2, 64), (16, 1, 128)])
+@pytest.mark.parametrize("lens,rows", [([5000], [1]), ([5000], [30]), ([15128], [70]), ([3000, 10, 0], [40, 3, 1]),
+                                       ([2000], [200]), ([9000, 64], [5, 127])])
+def test_prompt_few_rows_after_many(lib, heads, lens, rows):
+    """Items cut along their keys and joined; short requests beside long ones."""
+    x = Prompt(heads, lens, rows, seed=sum(rows))
+    base, base_lse = prompt(lib, x)
+    check(x, base, base_lse, p_rel=P_REL)
+    check(x, *prompt(lib, x, max_len=max(lens)), p_rel=P_REL)
+    check(x, *prompt(lib, x, max_len=1), p_rel=P_REL)
+    # a value that is not finite among the rows' own: of the first row's entry, and of the last's
+    for at in (lens[0], lens[0] + rows[0] - 1):
+        kept = x.v[0, 0, 0, at, 7].clone()
+        x.v[0, 0, 0, at, 7] = math.nan
+        out, lse = prompt(lib, x)
+        first, G = at - lens[0], heads[0] // heads[1]
+        assert torch.equal(lse, base_lse) and torch.equal(out[:first], base[:first])
+        assert torch.isnan(out[first:rows[0], :G, 7]).all() and torch.equal(out[rows[0]:], base[rows[0]:])
+        rest = [e for e in range(heads[2]) if e != 7]
+        assert torch.equal(out[..., rest], base[..., rest])
+        x.v[0, 0, 0, at, 7] = kept
+
+
 def test_prompt_many_heads(lib):
     x = Prompt((1024, 1, 64), [100], [90])  # more than 2^16 queries
     check(x, *prompt(lib, x), p_rel=P_REL)
