@@ -48,9 +48,18 @@ __device__ __forceinline__ float exact_scale(float most) {
   return fminf(rintf(fminf(on_grid(steps, 1.f / 7.f), 16.f)) * __uint_as_float((uint32_t)(e - 3) << 23), kMaxScale4);
 }
 
-// A whole number of a code, rounded from q, as the bits of 1.5 2^23 + 8 + it: the code in the lowest.
-__device__ __forceinline__ uint32_t code_bits(float q) {
-  return __float_as_uint(fminf(fmaxf(q, -7.f), 7.f) + 12582920.f);
+// The code of x / s, s = 1 / inv, as the lowest bits of the result, for exact values: the product on
+// the grid, then rounded to a whole number by an addition whose sum's last place is 1.  With
+// |x inv| < 7.5 (scales of 2^-14 and more that are not capped); clamped: for all.
+__device__ __forceinline__ uint32_t code_bits(float x, float inv) {
+  return __float_as_uint(fmaf(x, inv, 2304.f) + (12582912.f + 8.f - 2304.f));
+}
+__device__ __forceinline__ uint32_t code_bits_clamped(float x, float inv) {
+  return __float_as_uint(fminf(fmaxf(on_grid(x, inv), -7.f), 7.f) + (12582912.f + 8.f));
+}
+// The same of values that are not exact, rounded where they are.
+__device__ __forceinline__ uint32_t code_bits_near(float q) {
+  return __float_as_uint(fminf(fmaxf(q, -7.f), 7.f) + (12582912.f + 8.f));
 }
 // The word of 8 codes.
 __device__ __forceinline__ uint32_t code_word(const uint32_t (&c)[8]) {

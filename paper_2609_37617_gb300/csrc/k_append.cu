@@ -17,6 +17,7 @@
 //
 // Bound by memory: each value is read and written once.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache4.cuh"
 #include "ptx_sm100.cuh"
@@ -26,9 +27,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kAtOnce = 3;  // heads of a thread whose loads are on their way together
-// How far a finished value may be from its exact one, over |y_j| + |y_j'| of its pair: the mean
-// square, its root, the division and two products add 11 roundings of 2^-24, sine and cosine (one
-// step, and an angle rounded to 2^-25 of a half turn) 4, the rotation 2.
+// How far a finished value may be from its exact one, over |y_j| + |y_j'| of its pair: the mean square
+// adds 6 roundings of 2^-24 to its root, rsqrtf 4, two products 2, sine and cosine (one step, and an
+// angle rounded to 2^-25 of a half turn) 4, the rotation 2.
 constexpr float kOff = 1.5e-6f;
 
 // Four dims as they are in memory.
@@ -76,22 +77,57 @@ __device__ __forceinline__ uint64_t turns_of(const AppendArgs& a, int position, 
   return (uint64_t)(int64_t)position * a.turn[j];
 }
 
+// Sine and cosine of an angle given in 2^-64 turns, to some 2^-50: the nearest eighth of a turn, and
+// the Taylor series of what is left (at most pi / 8; its next terms are below 2^-55).  64-bit operations are
+// slow here (one warp's take some 64 cycles), and the library's sincospi has several times as many.
+__device__ __forceinline__ void turn_exactly(uint64_t turns, double& sn, double& cs) {
+  const uint64_t eighth = (turns + (1ull << 60)) >> 61;
+  const double t = (double)(int64_t)(turns - (eighth << 61)) * (6.283185307179586477 * 0x1p-64), t2 = t * t;
+  double s = 1. / 6227020800., c = 1. / 479001600.;
+  s = fma(s, t2, -1. / 39916800.);
+  c = fma(c, t2, -1. / 3628800.);
+  s = fma(s, t2, 1. / 362880.);
+  c = fma(c, t2, 1. / 40320.);
+  s = fma(s, t2, -1. / 5040.);
+  c = fma(c, t2, -1. / 720.);
+  s = fma(s, t2, 1. / 120.);
+  c = fma(c, t2, 1. / 24.);
+  s = fma(s, t2, -1. / 6.);
+  c = fma(c, t2, -0.5);
+  s = fma(s * t2, t, t);
+  c = fma(c, t2, 1.);
+  if (eighth & 1) {  // by an eighth of a turn
+    const double u = (c - s) * 0.70710678118654752440;
+    s = (c + s) * 0.70710678118654752440;
+    c = u;
+  }
+  const uint32_t quarter = (uint32_t)(eighth >> 1) & 3u;
+  sn = quarter & 1 ? c : s;
+  cs = quarter & 1 ? -s : c;
+  if (quarter & 2) sn = -sn, cs = -cs;
+}
+
 // Those of a head's dims (y[0 .. 3] at d.a, y[4 .. 7] at d.b) that `which` has bits for, in 64
 // bits.  By whole warps, whose heads may be keys and values: every thread takes part in the shuffles.
 template <int D>
 __device__ __noinline__ void finish_exactly(const AppendArgs& a, const float (&x)[8], const float* gain, bool turn,
                                             int position, Dims d, uint32_t which, double (&y)[8]) {
-  double ss = 0.0;
-  for (int e = 0; e < 8; ++e) ss = fma((double)x[e], (double)x[e], ss);
-  for (int o = D / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
-  const double f = 1.0 / sqrt(ss / D + (double)a.eps);
+  double f = 1.0;
+  if (__any_sync(~0u, gain != nullptr)) {
+    double ss = 0.0;
+    for (int e = 0; e < 8; ++e) ss = fma((double)x[e], (double)x[e], ss);
+    for (int o = D / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
+    // 1 / sqrt(v): r (1 + e / 2 + 3 e^2 / 8), e = 1 - v r^2 of the 32-bit root, off by e^3
+    const double v = fma(ss, 1.0 / D, (double)a.eps), r = (double)rsqrtf((float)v), e = fma(-v * r, r, 1.0);
+    f = v > 0.0 && (float)v < INFINITY && (float)v > 1e-37f ? fma(r * e, fma(0.375, e, 0.5), r) : 1.0 / sqrt(v);
+  }
   for (int e = 0; e < 4; ++e) {
     if (!((which >> e | which >> (4 + e)) & 1)) continue;
     double u = x[e], v = x[4 + e];
     if (gain) u *= f * (double)gain[d.a + e], v *= f * (double)gain[d.b + e];
     if (turn && d.pair) {
       double sn, cs;
-      sincospi((double)(int64_t)turns_of(a, position, d.a + e) * 0x1p-63, &sn, &cs);
+      turn_exactly(turns_of(a, position, d.a + e), sn, cs);
       const double w = u * cs - v * sn;
       v = v * cs + u * sn;
       u = w;
@@ -143,13 +179,13 @@ __device__ __forceinline__ uint32_t code8(const float (&y)[8], const float (&off
     for (int e = 4 * k; e < 4 * k + 4; ++e) {
       const float q = y[e] * inv;
       if (off[e] > 0.f && fabsf(fabsf(q - rintf(q)) - 0.5f) <= fmaf(off[e], inv, 4e-6f)) near |= 1u << e;
-      to.c[e] = code_bits(off[e] > 0.f ? q : on_grid(y[e], inv));
+      to.c[e] = off[e] > 0.f ? code_bits_near(q) : code_bits_clamped(y[e], inv);
     }
   }
   if (odd)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (y[e] != y[e]) to.c[e] = code_bits(0.f);
+      if (y[e] != y[e]) to.c[e] = code_bits_near(0.f);
   return near;
 }
 
@@ -163,8 +199,21 @@ __device__ __noinline__ void code8_exactly(const double (&y)[8], uint32_t which,
   }
   for (int e = 0; e < 8; ++e)
     if ((which >> e) & 1) {
-      const double s = to.s[e / 4], q = s > 0.0 ? y[e] / s : 0.0;
-      to.c[e] = code_bits(y[e] == y[e] ? (float)rint(fmin(fmax(q, -7.0), 7.0)) : 0.f);
+      // which of the two whole numbers around it is nearer: their border times s is exact, and the
+      // quotient in 32 bits is within 1e-4 of the right one
+      const double s = to.s[e / 4], m = fabs(y[e]);
+      if (!(m <= 3.4e38)) {
+        to.c[e] = code_bits_near(m == m ? copysignf(7.f, (float)y[e]) : 0.f);
+      } else if (s == 0.0) {
+        to.c[e] = code_bits_near(0.f);
+      } else {
+        const float low = fminf(floorf((float)m * reciprocal((float)s) - 1e-4f), 7.f);
+        const double over = m - ((double)low + 0.5) * s;
+        const float up = low + (over > 0.0 || (over == 0.0 && ((int)low & 1)) ? 1.f : 0.f);
+        const double more = m - ((double)up + 0.5) * s;  // (low may have been one too low)
+        const float c = up + (more > 0.0 || (more == 0.0 && ((int)up & 1)) ? 1.f : 0.f);
+        to.c[e] = code_bits_near(copysignf(c, (float)y[e]));
+      }
     }
 }
 
@@ -179,29 +228,30 @@ template <int D, bool F32, bool FOUR>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs a, int per) {
   constexpr int C = D / 8, G = kThreads / C;  // threads of a head, groups of them
   const int tid = threadIdx.x, c = tid % C, group = tid / C;
-  const int H = a.nq + 2 * a.nkv, r = blockIdx.x * (G / per) + group / per, h0 = group % per;
+  const int r = blockIdx.x * (G / per) + group / per, h0 = group % per;
   const Dims d = dims_of(c, a.half);
   const bool row_live = r < a.rm.rows;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  Raw<F32> raw[kAtOnce][2];
-  auto load = [&](int h) {
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int head = h + k * per;
-      const bool isq = head < a.nq, isv = head >= a.nq + a.nkv;
-      const void* from = isq ? a.q : isv ? a.v : a.k;
-      const int64_t at = r * (isq ? a.q_stride : isv ? a.v_stride : a.k_stride) +
-                         (isq ? head : isv ? head - a.nq - a.nkv : head - a.nq) * D;
-#pragma unroll
-      for (int e = 0; e < (F32 ? 4 : 2); ++e) raw[k][0].w[e] = raw[k][1].w[e] = 0;
-      if (row_live && head < H) {
-        load4(from, at + d.a, raw[k][0]);
-        load4(from, at + d.b, raw[k][1]);
-      }
-    }
+  // a row's queries, keys and values, and the first of this group's heads of each
+  const int64_t row = row_live ? r : 0;
+  const int heads[3] = {a.nq, a.nkv, a.nkv};
+  const int64_t from[3] = {row * a.q_stride, row * a.k_stride, row * a.v_stride};
+  const void* const base[3] = {a.q, a.k, a.v};
+  auto load = [&](auto kind, int head, Raw<F32>(&raw)[2]) {
+    constexpr int K = decltype(kind)::value;
+    const int h = min(head, heads[K] - 1);  // (one that is no head's is not used)
+    load4(base[K], from[K] + h * D + d.a, raw[0]);
+    load4(base[K], from[K] + h * D + d.b, raw[1]);
   };
-  load(h0);
+  using Q = std::integral_constant<int, 0>;
+  using Key = std::integral_constant<int, 1>;
+  using Value = std::integral_constant<int, 2>;
+  Raw<F32> raw_k[2], raw_v[2], raw_q[kAtOnce][2];
+  load(Key(), h0, raw_k);
+  load(Value(), h0, raw_v);
+#pragma unroll
+  for (int k = 0; k < kAtOnce; ++k) load(Q(), h0 + k * per, raw_q[k]);
   // the gains of these dims, queries' and keys'
   float gain[2][8];
 #pragma unroll
@@ -231,76 +281,43 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     if (d.pair) sincospif((float)(int32_t)(turns_of(a, position, d.a + e) >> 32) * 0x1p-31f, &sn[e], &cs[e]);
   }
   bool odd = false;
-  const int rounds = (H + per - 1) / per;
-#pragma unroll 1
-  for (int t0 = 0; t0 < rounds; t0 += kAtOnce) {
-    if (t0 > 0) load(h0 + t0 * per);
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      if (t0 + k >= rounds) break;
-      // (threads past the last head take part in the shuffles)
-      const int head = h0 + (t0 + k) * per;
-      const bool live = at >= 0 && head < H, isq = head < a.nq, isv = head >= a.nq + a.nkv;
-      const int hh = isq ? head : head - a.nq - (isv ? a.nkv : 0);
-      const bool norm = isq ? a.q_norm != nullptr : !isv && a.k_norm != nullptr;
-      float x[8], y[8], off[8];  // off: how far a value is from the exact one, at most (4 bits)
-      floats<F32>(raw[k][0], x);
-      floats<F32>(raw[k][1], x + 4);
+  // One head of a row (threads whose head there is not take part in the shuffles).
+  auto finish = [&](auto kind, const Raw<F32>(&raw)[2], int head) {
+    constexpr int K = decltype(kind)::value;
+    const bool live = at >= 0 && head < heads[K];
+    const float* norm = K == 0 ? a.q_norm : K == 1 ? a.k_norm : nullptr;
+    float x[8], y[8], off[8];  // off: how far a value is from the exact one, at most (4 bits)
+    floats<F32>(raw[0], x);
+    floats<F32>(raw[1], x + 4);
+    if (K < 2 && norm) {
       float ss = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
 #pragma unroll
       for (int o = C / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
-      const float f = norm ? 1.f / sqrtf(ss * (1.f / D) + a.eps) : 1.f;
+      const float f = rsqrtf(fmaf(ss, 1.f / D, a.eps));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = norm ? x[e] * f * (isq ? gain[0][e] : gain[1][e]) : x[e];
-      const bool turned = d.pair && !isv;
+      for (int e = 0; e < 8; ++e) y[e] = x[e] * f * gain[K & 1][e];
+    } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float u = y[e], v = y[4 + e];
-        if (FOUR) {
-          off[e] = norm || F32 ? kOff * fabsf(u) : 0.f;
-          off[4 + e] = norm || F32 ? kOff * fabsf(v) : 0.f;
-          if (turned) off[e] = off[4 + e] = kOff * (fabsf(u) + fabsf(v));
-        }
-        y[e] = turned ? u * cs[e] - v * sn[e] : u;
-        y[4 + e] = turned ? v * cs[e] + u * sn[e] : v;
+      for (int e = 0; e < 8; ++e) y[e] = x[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float u = y[e], v = y[4 + e];
+      if (FOUR && K > 0) {
+        off[e] = norm || F32 ? kOff * fabsf(u) : 0.f;
+        off[4 + e] = norm || F32 ? kOff * fabsf(v) : 0.f;
+        if (K == 1 && d.pair) off[e] = off[4 + e] = kOff * (fabsf(u) + fabsf(v));
       }
-      if (FOUR) {
-        Coded to;
-        bool strange = false;
-        const bool mine = live && !isq;
-        const uint32_t near = code8(y, off, d.pair, to, strange);
-        uint32_t which = __reduce_or_sync(~0u, mine ? near : 0u);
-        if (which) {
-          if (which & 256u) which = 511u;
-          double z[8];
-          finish_exactly<D>(a, x, norm ? (isq ? a.q_norm : a.k_norm) : nullptr, !isv, position, d, which, z);
-          code8_exactly(z, which, d.pair, to);
-        }
-        // the words of codes: of paired fours a thread writes the one of its even or odd neighbours
-        const uint32_t wa = half_word(to.c), wb = half_word(to.c + 4);
-        const uint32_t there = __shfl_xor_sync(~0u, c & 1 ? wa : wb, 1);
-        const uint32_t word = !d.pair ? wa | wb << 8 : c & 1 ? there | wb << 8 : wa | there << 8;
-        const int word_at = !d.pair ? d.a / 8 : c & 1 ? (d.b - 4) / 8 : d.a / 8;
-        if (mine) {
-          odd = odd || strange;
-          const size_t entry = ((size_t)b * a.nkv + hh) * a.cap + at;
-          reinterpret_cast<uint32_t*>(isv ? a.cv4 : a.ck4)[entry * C + word_at] = word;
-          uint8_t* scales = (isv ? a.cvs : a.cks) + entry * (D / 16);
-          if (d.pair) {
-            if (c % 4 < 2) scales[(c % 4 ? d.b : d.a) / 16] = scale_byte(to.s[c % 4]);
-          } else if (c % 2 == 0) {
-            scales[d.a / 16] = scale_byte(to.s[0]);
-          }
-        }
-      } else if (live && !isq) {
-        bf16* to = (isv ? a.cv : a.ck) + (((size_t)b * a.nkv + hh) * a.cap + at) * D;
-        store4(to + d.a, y);
-        store4(to + d.b, y + 4);
+      if (K < 2 && d.pair) {
+        y[e] = u * cs[e] - v * sn[e];
+        y[4 + e] = v * cs[e] + u * sn[e];
       }
-      if (live && isq) {
-        const size_t to = ((size_t)r * a.nq + hh) * D;
+    }
+    if (K == 0) {
+      if (live) {
+        const size_t to = ((size_t)r * a.nq + head) * D;
         if constexpr (F32) {
           store4((float*)a.q_out + to + d.a, y);
           store4((float*)a.q_out + to + d.b, y + 4);
@@ -309,7 +326,56 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
           store4((bf16*)a.q_out + to + d.b, y + 4);
         }
       }
+    } else if (FOUR) {
+      Coded to;
+      bool strange = false;
+      const uint32_t near = code8(y, off, d.pair, to, strange);
+      uint32_t which = __reduce_or_sync(~0u, live ? near : 0u);
+      if (which) {
+        if (which & 256u) which = 511u;
+        double z[8];
+        finish_exactly<D>(a, x, norm, K == 1, position, d, which, z);
+        code8_exactly(z, which, d.pair, to);
+      }
+      // the words of codes: of paired fours a thread writes the one of its even or odd neighbours
+      const uint32_t wa = half_word(to.c), wb = half_word(to.c + 4);
+      const uint32_t there = __shfl_xor_sync(~0u, c & 1 ? wa : wb, 1);
+      const uint32_t word = !d.pair ? wa | wb << 8 : c & 1 ? there | wb << 8 : wa | there << 8;
+      const int word_at = !d.pair ? d.a / 8 : c & 1 ? (d.b - 4) / 8 : d.a / 8;
+      if (live) {
+        odd = odd || strange;
+        const size_t entry = ((size_t)b * a.nkv + head) * a.cap + at;
+        reinterpret_cast<uint32_t*>(K == 2 ? a.cv4 : a.ck4)[entry * C + word_at] = word;
+        uint8_t* scales = (K == 2 ? a.cvs : a.cks) + entry * (D / 16);
+        if (d.pair) {
+          if (c % 4 < 2) scales[(c % 4 ? d.b : d.a) / 16] = scale_byte(to.s[c % 4]);
+        } else if (c % 2 == 0) {
+          scales[d.a / 16] = scale_byte(to.s[0]);
+        }
+      }
+    } else if (live) {
+      bf16* to = (K == 2 ? a.cv : a.ck) + (((size_t)b * a.nkv + head) * a.cap + at) * D;
+      store4(to + d.a, y);
+      store4(to + d.b, y + 4);
     }
+  };
+  // (the rounds are those of a whole block)
+#pragma unroll 1
+  for (int t0 = 0; t0 < a.nkv; t0 += per) {
+    if (t0 > 0) load(Key(), t0 + h0, raw_k), load(Value(), t0 + h0, raw_v);
+    finish(Key(), raw_k, t0 + h0);
+    finish(Value(), raw_v, t0 + h0);
+  }
+#pragma unroll 1
+  for (int t0 = 0; t0 < a.nq; t0 += kAtOnce * per) {
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int t = t0 + k * per;
+      if (t0 > 0) load(Q(), t + h0, raw_q[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (t0 + k * per < a.nq) finish(Q(), raw_q[k], t0 + k * per + h0);
   }
   if (FOUR && __any_sync(~0u, odd) && (tid & 31) == 0 && a.err) atomicOr(a.err, kErrNotFinite);
 }
@@ -319,9 +385,8 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
   constexpr int G = kThreads / (D / 8);
   // few rows: as many threads to one as there are heads; many: four groups, whose sines, cosines and
   // gains serve all their heads
-  const int H = a.nq + 2 * a.nkv;
   int per = 4;
-  while (per < G && per < H && (int64_t)a.rm.rows * per / G < 2 * device_sms()) per *= 2;
+  while (per < G && per < a.nq && (int64_t)a.rm.rows * per / G < 2 * device_sms()) per *= 2;
   return launch_pdl(a.ck4 ? append_kernel<D, F32, true> : append_kernel<D, F32, false>,
                     dim3((a.rm.rows + G / per - 1) / (G / per)), dim3(kThreads), 0, st, 1, a, per);
 }

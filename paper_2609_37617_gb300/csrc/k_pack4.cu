@@ -13,28 +13,44 @@ namespace {
 
 constexpr int kThreads = 256, kAtOnce = 4;
 
+// The largest magnitude of the 16 is found on pairs of bf16 as whole numbers, of which NaN and
+// infinities are the largest.
 __device__ __forceinline__ void write8(uint4 v, uint32_t& codes, uint8_t& scale, bool& odd) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  float x[8], most = 0.f;
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) top = __vmaxu2(top, w[e] & 0x7FFF7FFFu);
+  top = __vmaxu2(top, __shfl_xor_sync(~0u, top, 1));
+  const uint32_t most = max(top & 0xFFFFu, top >> 16);
+  float x[8];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[2 * e] = __uint_as_float(w[e] << 16);
     x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    most = fmaxf(most, fabsf(x[e]));
-    odd = odd || !(fabsf(x[e]) <= 3.4028235e38f);
-  }
-  most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-  const float s = exact_scale(most), inv = reciprocal(s);
+  const float s = exact_scale(__uint_as_float(most << 16)), inv = reciprocal(s);
   uint32_t c[8];
+  if (s >= 6.103515625e-5f && s < kMaxScale4) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) c[e] = code_bits(on_grid(x[e], inv));
-  if (odd)
+    for (int e = 0; e < 8; ++e) c[e] = code_bits(x[e], inv);
+  } else if (most < 0x7F80u) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (x[e] != x[e]) c[e] = code_bits(0.f);
+    for (int e = 0; e < 8; ++e) c[e] = code_bits_clamped(x[e], inv);
+  } else {
+    // (the largest number is not the largest magnitude where there is NaN; an infinity has the largest scale)
+    odd = true;
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[e]));
+    const uint32_t pair = 3u << (threadIdx.x & 30);
+    m = fmaxf(m, __shfl_xor_sync(pair, m, 1));
+    const float t = exact_scale(m), f = reciprocal(t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = code_bits_clamped(x[e] == x[e] ? x[e] : 0.f, f);
+    codes = code_word(c);
+    scale = scale_byte(t);
+    return;
+  }
   codes = code_word(c);
   scale = scale_byte(s);
 }
