@@ -8,6 +8,7 @@ loudly if libas2d.so has not been built: there is no fallback path.
 """
 import ctypes
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libas2d.so")
@@ -201,13 +202,14 @@ _lib.as2d_cpu_decoder_free.restype = None
 for _n in ("as2d_cpu_decoder_create", "as2d_cpu_decoder_step", "as2d_cpu_decoder_logits",
            "as2d_cpu_decoder_reset"):
     getattr(_lib, _n).restype = _S
-_CACHE, _ROWS, _I64 = ctypes.POINTER(as2d_cache), ctypes.POINTER(as2d_tree_rows), ctypes.c_int64
+# (rows are described by their structure, or by its bytes)
+_CACHE, _ROWS, _I64 = ctypes.POINTER(as2d_cache), _P, ctypes.c_int64
 _lib.as2d_tree_attention_workspace.argtypes = [_CACHE, ctypes.POINTER(_I64)]
 _lib.as2d_tree_attention.argtypes = [_CACHE, _S, _ROWS, _P, _P, _P, _I64, _P, _P]
 _lib.as2d_attention_weights.argtypes = [_CACHE, _S, _ROWS, _P, _P, _P, _P]
 _lib.as2d_cache_evict_workspace.argtypes = [_CACHE, ctypes.POINTER(_I64)]
 _lib.as2d_cache_evict.argtypes = [_CACHE, _P, _P, _P, _S, _P, _I64, _P]
-_CACHE4, _NEW = ctypes.POINTER(as2d_cache4), ctypes.POINTER(as2d_new_rows)
+_CACHE4, _NEW = ctypes.POINTER(as2d_cache4), _P
 _lib.as2d_cache_append.argtypes = [_CACHE, _S, _NEW, _P, _P, _P]
 _lib.as2d_cache4_append.argtypes = [_CACHE4, _S, _NEW, _P, _P, _P]
 _lib.as2d_cache4_write.argtypes = [_CACHE4, _CACHE, _S, _P, _P, _S, _P, _P]
@@ -790,6 +792,25 @@ def _address(t, name, device, dtype, shape):
     return _tensor(t, name, device, (dtype,), shape)
 
 
+def _packer(structure, layout):
+    """A function that gives the bytes of a structure's fields, in a third of the time that the
+    structure itself takes; what it refuses is left to that (numbers beyond 32 bits, errors)."""
+    packer = struct.Struct(layout)
+    assert packer.size == ctypes.sizeof(structure)
+    pack = packer.pack
+
+    def fields(*values):
+        try:
+            return pack(*values)
+        except (struct.error, OverflowError):
+            return bytes(structure(*values))
+    return fields
+
+
+_TREE_ROWS = _packer(as2d_tree_rows, "@PiiqPiPPf4x")
+_NEW_ROWS = _packer(as2d_new_rows, "@PPPiiqqqPPPPPffi4x")
+
+
 class _CacheCalls:
     """What the caches below share: checks of a call's arguments, the workspace and its stream."""
 
@@ -798,7 +819,7 @@ class _CacheCalls:
         self._c, self.shape, self._on = c, shape, device
         self._current = torch.cuda.current_device
         self._ref = ctypes.byref(self._c)
-        self._per_request = shape[1:2]
+        self._per_request, self._counts_type = shape[1:2], ctypes.c_int32 * shape[1]
         self._bf16, self._f32, self._i32, self._i64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
         self._mask = (torch.int64, torch.uint64)
         most, need = 0, _I64()
@@ -823,7 +844,10 @@ class _CacheCalls:
     def _counts(self, values, name):
         if len(values) != self.shape[1]:
             raise ValueError(f"{name} must name {self.shape[1]} requests")
-        return _int32s(values, name)
+        array = self._counts_type(*values)
+        if array[:] != (values if type(values) is list else list(values)):
+            raise ValueError(f"{name} must be of 32 bits")
+        return array
 
     def _rows(self, device, q, kv_len, rows, visible, scale, layer, max_len):
         d = self.shape[4]
@@ -843,22 +867,21 @@ class _CacheCalls:
                 visible = _address(visible, "visible", device, self._i64, shape[:1])
             else:
                 visible = _tensor(visible, "visible", device, self._mask, shape[:1])
-        r = as2d_tree_rows(
+        r = _TREE_ROWS(
             at, AS2D_TYPE_BF16 if q.dtype is self._bf16 else AS2D_TYPE_F32, n_q,
             q.stride(0) if n > 1 else n_q * d,  # (the stride of a single row is not looked at)
             _address(kv_len, "kv_len", device, self._i32, self._per_request), max_len,
-            ctypes.addressof(host_rows), visible, d ** -0.5 if scale is None else scale)
-        r.keep = host_rows  # alive as long as the descriptor
-        return r
+            ctypes.addressof(host_rows), visible or 0, d ** -0.5 if scale is None else scale)
+        return r, host_rows  # (which the descriptor points to)
 
     def _attention(self, name, q, kv_len, rows, visible, scale, layer, max_len, out, lse, error_bits, stream):
         device, current, stream = self._enter(stream)
-        r = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
+        r, keep = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
         shape = q.shape
         if out is None:
             out = q.new_empty(shape) if stream == current else _new_on(stream, device, q, shape)
         st = getattr(_lib, name)(
-            self._ref, layer, ctypes.byref(r), _address(out, "out", device, q.dtype, shape),
+            self._ref, layer, r, _address(out, "out", device, q.dtype, shape),
             None if lse is None else _address(lse, "lse", device, self._f32, shape[:2]),
             self._workspace.data_ptr(), self._workspace.numel(),
             None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)),
@@ -867,40 +890,53 @@ class _CacheCalls:
             _check(st, name)
         return out
 
+    def _check_new_rows(self, device, q, k, v):
+        """What is wrong with the rows of an append."""
+        n_kv, d = self.shape[2], self.shape[4]
+        _tensor(q, "q", device, (self._bf16, self._f32), None, False)
+        if q.dim() != 3 or q.shape[1] == 0 or q.shape[2] != d:
+            raise ValueError(f"q must be [rows, n_q, {d}]")
+        for t, name in ((k, "k"), (v, "v")):
+            _tensor(t, name, device, (q.dtype,), (q.shape[0], n_kv, d), False)
+        raise ValueError("the rows of q, k and v must be contiguous")
+
     def _append(self, name, q, k, v, kv_len, rows, layer, positions, q_norm, k_norm, eps, theta, rotary,
                 out, error_bits, stream):
         device, current, stream = self._enter(stream)
-        n_kv, d = self.shape[2], self.shape[4]
-        if abs(layer) >> 31:
-            raise ValueError("layer must be of 32 bits")
-        dtype, shape = q.dtype, q.shape
-        n_q = shape[1] if len(shape) == 3 else 0
-        at = [_tensor(q, "q", device, (self._bf16, self._f32), None, False)]
-        if n_q == 0 or shape[2] != d:
-            raise ValueError(f"q must be [rows, n_q, {d}]")
-        n = shape[0]
-        for t, its_name in ((k, "k"), (v, "v")):
-            at.append(_tensor(t, its_name, device, (dtype,), (n, n_kv, d), False))
-        for t, its_name in ((q, "q"), (k, "k"), (v, "v")):
-            if t.stride()[1:] != (d, 1):
-                raise ValueError(f"{its_name} must have contiguous rows")
+        d = self.shape[4]
+        # the common case in one expression, as a small call's time is the host's
+        try:
+            dtype, shape = q.dtype, q.shape
+            n, n_q, _ = shape
+            new = (n, self.shape[2], d)
+            of_q, of_k, of_v = q.stride(), k.stride(), v.stride()
+            good = (k.dtype is dtype and v.dtype is dtype and (dtype is self._bf16 or dtype is self._f32) and
+                    n_q > 0 and shape[2] == d and k.shape == new and v.shape == new and
+                    of_q[1] == of_k[1] == of_v[1] == d and of_q[2] == of_k[2] == of_v[2] == 1 and
+                    q.get_device() == device and k.get_device() == device and v.get_device() == device)
+        except (AttributeError, ValueError, IndexError):
+            good = False
+        if not good:
+            self._check_new_rows(device, q, k, v)
         host_rows = self._counts(rows, "rows")
         if n != sum(rows):
             raise ValueError("q must have as many rows as the requests together")
-        gains = [None if t is None else _address(t, its_name, device, self._f32, (d,))
-                 for t, its_name in ((q_norm, "q_norm"), (k_norm, "k_norm"))]
-        rotary = d if rotary is None else _int32s((rotary,), "rotary")[0]
-        # (the stride of a single row is not looked at)
-        strides = [t.stride(0) if n > 1 else t.shape[1] * d for t in (q, k, v)]
-        r = as2d_new_rows(
-            *at, AS2D_TYPE_BF16 if dtype is self._bf16 else AS2D_TYPE_F32, n_q, *strides,
-            _address(kv_len, "kv_len", device, self._i32, self._per_request), ctypes.addressof(host_rows),
-            None if positions is None else _address(positions, "positions", device, self._i32, (n,)),
-            *gains, eps, theta, rotary)
+        if n == 1:  # (the stride of a single row is not looked at)
+            of_q, of_k, of_v = (n_q * d,), (new[1] * d,), (new[1] * d,)
+        rotary = d if rotary is None else rotary
+        if layer.bit_length() > 31 or rotary.bit_length() > 31:
+            raise ValueError("layer and rotary must be of 32 bits")
+        r = _NEW_ROWS(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), AS2D_TYPE_BF16 if dtype is self._bf16 else AS2D_TYPE_F32, n_q,
+            of_q[0], of_k[0], of_v[0], _address(kv_len, "kv_len", device, self._i32, self._per_request),
+            ctypes.addressof(host_rows),
+            0 if positions is None else _address(positions, "positions", device, self._i32, (n,)),
+            0 if q_norm is None else _address(q_norm, "q_norm", device, self._f32, (d,)),
+            0 if k_norm is None else _address(k_norm, "k_norm", device, self._f32, (d,)), eps, theta, rotary)
         if out is None:
             out = q.new_empty(shape) if stream == current else _new_on(stream, device, q, shape)
         st = getattr(_lib, name)(
-            self._ref, layer, ctypes.byref(r), _address(out, "out", device, dtype, shape),
+            self._ref, layer, r, _address(out, "out", device, dtype, shape),
             None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)), stream)
         if st:
             _check(st, name)
@@ -953,9 +989,9 @@ class Cache(_CacheCalls):
                           max_len=0, error_bits=None, stream=None):
         """as2d_attention_weights: adds to weights in place."""
         device, current, stream = self._enter(stream)
-        r = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
+        r, keep = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
         st = _lib.as2d_attention_weights(
-            self._ref, layer, ctypes.byref(r), _address(lse, "lse", device, self._f32, q.shape[:2]),
+            self._ref, layer, r, _address(lse, "lse", device, self._f32, q.shape[:2]),
             _address(weights, "weights", device, self._f32, self.shape[:4]),
             None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)),
             stream)
@@ -1008,7 +1044,9 @@ class Cache4(_CacheCalls):
             raise TypeError("cache must be a Cache")
         if cache._on != device:
             raise ValueError("both caches must be on the current CUDA device")
-        layer, max_entries = _int32s((-1 if layer is None else layer, max_entries), "layer and max_entries")
+        layer = -1 if layer is None else layer
+        if layer.bit_length() > 31 or max_entries.bit_length() > 31:
+            raise ValueError("layer and max_entries must be of 32 bits")
         st = getattr(_lib, name)(
             self._ref, cache._ref, layer,
             None if start is None else _address(start, "start", device, self._i32, self._per_request),
