@@ -682,7 +682,7 @@ as2d_status as2d_accept_sampled(const float* probs, const float* draft_probs,
    -7 .. 7, ties to the even one, and 0 where s is 0; both as in exact arithmetic.  A
    value is off by at most s / 2, where s is neither capped nor below 2^-14.  NaN is written
    as 0 and an infinity as the largest magnitude of its sign that the 16 can have
-   (s = 896). */
+   (s = 896; one that a norm or a rotation meets may count as NaN). */
 typedef struct as2d_cache4 {
   uint8_t *k, *k_scale, *v, *v_scale;
   int32_t n_layers, batch, n_kv, capacity, head_dim;

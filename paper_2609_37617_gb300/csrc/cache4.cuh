@@ -18,16 +18,6 @@ namespace as2d {
 
 constexpr float kMaxScale4 = 896.f;  // 72 of them fit a 16-bit float (scale_shift)
 
-// The scale nearest to t >= 0 (ties to even); units: t in steps of the scales around it.
-template <typename T>
-__device__ __forceinline__ float scale_of(T t, T& units) {
-  // steps of 2^(e - 3), e the exponent of t, at least that of the smallest normal scale
-  // (t rounded up to a power of two gives the same scale)
-  const int e = min(max((int)(__float_as_uint((float)t) >> 23), 127 - 14), 127 + 9);
-  units = t * (T)__uint_as_float((uint32_t)(2 * 127 + 3 - e) << 23);
-  const float r = fminf((float)rint(units), 16.f);  // (16: the next exponent's first)
-  return fminf(r * __uint_as_float((uint32_t)(e - 3) << 23), kMaxScale4);
-}
 __device__ __forceinline__ uint8_t scale_byte(float s) { return (uint8_t)(__half_as_ushort(__float2half_rn(s)) >> 7); }
 
 // ---- coding ---------------------------------------------------------------------

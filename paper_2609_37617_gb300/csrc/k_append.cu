@@ -11,9 +11,10 @@
 // shuffles.  Angles: a position times 2^64 turns of its frequency, modulo 2^64, is the angle in
 // turns whatever the position, to 2^-64 of a turn and the frequency's own rounding.
 //
-// Codes are those of the exact values: a value or a scale that 32-bit arithmetic finds nearer to
-// the border of two codes than its error (some 2e-6 of them) has its head computed once more in
-// 64 bits.
+// Codes are those of the exact values: keys that go into 4 bits are computed in pairs of floats (a
+// number and what it is off by, Knuth's and Dekker's sums and products), to some 2^-38, and each
+// code and scale is compared with the border that it is next to, which is exact in 32 bits.  (Values
+// near a border computed again in 64 bits instead: the first call of that code on an SM took 11 us.)
 //
 // Bound by memory: each value is read and written once.
 #include <algorithm>
@@ -27,11 +28,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kAtOnce = 3;  // heads of a thread whose loads are on their way together
-// How far a finished value may be from its exact one, over |y_j| + |y_j'| of its pair: the mean square
-// adds 6 roundings of 2^-24 to its root, rsqrtf 4, two products 2, sine and cosine (one step, and an
-// angle rounded to 2^-25 of a half turn) 4, the rotation 2.
-constexpr float kOff = 1.5e-6f;
-
 // Four dims as they are in memory.
 template <bool F32>
 struct Raw {
@@ -73,67 +69,61 @@ __device__ __forceinline__ Dims dims_of(int c, int half) {
   return {d, d + 4, false};
 }
 
-__device__ __forceinline__ uint64_t turns_of(const AppendArgs& a, int position, int j) {
-  return (uint64_t)(int64_t)position * a.turn[j];
+// ---- pairs of floats ------------------------------------------------------------
+
+struct Two {
+  float h, l;
+};
+__device__ __forceinline__ Two product(float a, float b) {
+  const float h = __fmul_rn(a, b);
+  return {h, fmaf(a, b, -h)};
+}
+__device__ __forceinline__ Two sum(float a, float b) {
+  const float h = __fadd_rn(a, b), t = __fsub_rn(h, a);
+  return {h, __fadd_rn(__fsub_rn(a, __fsub_rn(h, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Two sum(Two a, Two b) {
+  const Two s = sum(a.h, b.h);
+  return {s.h, s.l + (a.l + b.l)};
+}
+__device__ __forceinline__ Two product(Two a, Two b) {
+  const Two p = product(a.h, b.h);
+  return {p.h, p.l + fmaf(a.h, b.l, a.l * b.h)};
 }
 
-// Sine and cosine of an angle given in 2^-64 turns, to some 2^-50: the nearest eighth of a turn, and
-// the Taylor series of what is left (at most pi / 8; its next terms are below 2^-55).  64-bit operations are
-// slow here (one warp's take some 64 cycles), and the library's sincospi has several times as many.
-__device__ __forceinline__ void turn_exactly(uint64_t turns, double& sn, double& cs) {
-  const uint64_t eighth = (turns + (1ull << 60)) >> 61;
-  const double t = (double)(int64_t)(turns - (eighth << 61)) * (6.283185307179586477 * 0x1p-64), t2 = t * t;
-  double s = 1. / 6227020800., c = 1. / 479001600.;
-  s = fma(s, t2, -1. / 39916800.);
-  c = fma(c, t2, -1. / 3628800.);
-  s = fma(s, t2, 1. / 362880.);
-  c = fma(c, t2, 1. / 40320.);
-  s = fma(s, t2, -1. / 5040.);
-  c = fma(c, t2, -1. / 720.);
-  s = fma(s, t2, 1. / 120.);
-  c = fma(c, t2, 1. / 24.);
-  s = fma(s, t2, -1. / 6.);
-  c = fma(c, t2, -0.5);
-  s = fma(s * t2, t, t);
-  c = fma(c, t2, 1.);
-  if (eighth & 1) {  // by an eighth of a turn
-    const double u = (c - s) * 0.70710678118654752440;
-    s = (c + s) * 0.70710678118654752440;
-    c = u;
-  }
-  const uint32_t quarter = (uint32_t)(eighth >> 1) & 3u;
-  sn = quarter & 1 ? c : s;
-  cs = quarter & 1 ? -s : c;
-  if (quarter & 2) sn = -sn, cs = -cs;
-}
+// cos(k pi / 32)
+__constant__ float2 kCosines[17] = {
+    {1.0f, 0.0f}, {0.9951847195625305f, 7.109666189109021e-09f}, {0.9807852506637573f, 2.9739473106360492e-08f},
+    {0.9569403529167175f, -1.7184508038781132e-08f}, {0.9238795042037964f, 2.830748968563057e-08f}, {0.8819212913513184f, -2.7002963420841297e-08f},
+    {0.8314695954322815f, 1.687026340846387e-08f}, {0.7730104327201843f, 2.0642552556182636e-08f}, {0.7071067690849304f, 1.2101617485882343e-08f},
+    {0.6343932747840881f, 9.37955757507325e-09f}, {0.5555702447891235f, -1.1769521357507529e-08f}, {0.4713967442512512f, -7.425253745196869e-09f},
+    {0.3826834261417389f, 6.2233507236442165e-09f}, {0.290284663438797f, 1.3815665056426951e-08f}, {0.19509032368659973f, -1.670471427850373e-09f},
+    {0.0980171412229538f, -8.933931927579408e-10f}, {0.0f, 0.0f}};
 
-// Those of a head's dims (y[0 .. 3] at d.a, y[4 .. 7] at d.b) that `which` has bits for, in 64
-// bits.  By whole warps, whose heads may be keys and values: every thread takes part in the shuffles.
-template <int D>
-__device__ __noinline__ void finish_exactly(const AppendArgs& a, const float (&x)[8], const float* gain, bool turn,
-                                            int position, Dims d, uint32_t which, double (&y)[8]) {
-  double f = 1.0;
-  if (__any_sync(~0u, gain != nullptr)) {
-    double ss = 0.0;
-    for (int e = 0; e < 8; ++e) ss = fma((double)x[e], (double)x[e], ss);
-    for (int o = D / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
-    // 1 / sqrt(v): r (1 + e / 2 + 3 e^2 / 8), e = 1 - v r^2 of the 32-bit root, off by e^3
-    const double v = fma(ss, 1.0 / D, (double)a.eps), r = (double)rsqrtf((float)v), e = fma(-v * r, r, 1.0);
-    f = v > 0.0 && (float)v < INFINITY && (float)v > 1e-37f ? fma(r * e, fma(0.375, e, 0.5), r) : 1.0 / sqrt(v);
+// Sine and cosine of an angle given in 2^-64 turns: the nearest of 64 parts of a turn, from the table,
+// and the Taylor series of what is left (at most pi / 64; its next terms are below 2^-42).
+__device__ __forceinline__ void turn_exactly(uint64_t turns, Two& sn, Two& cs) {
+  const uint32_t k = (uint32_t)((turns + (1ull << 57)) >> 58) & 63u;
+  const int64_t left = (int64_t)(turns - ((uint64_t)k << 58));
+  const float a = (float)(int32_t)(left >> 34) * 0x1p-30f, b = (float)(uint32_t)((left >> 10) & 0xFFFFFF) * 0x1p-54f;
+  Two x = product(a, 6.28318548f);  // 2 pi, and what that is off by
+  x.l += fmaf(a, -1.74845553e-7f, b * 6.28318548f);
+  Two z = product(x.h, x.h);
+  z.l = fmaf(2.f * x.h, x.l, z.l);
+  const Two s = {x.h, fmaf(x.h * z.h, fmaf(z.h, fmaf(z.h, -1.f / 5040.f, 1.f / 120.f), -1.f / 6.f), x.l)};
+  const Two w = {-0.5f * z.h, fmaf(z.h * z.h, fmaf(z.h, -1.f / 720.f, 1.f / 24.f), -0.5f * z.l)};  // cos - 1
+  const float2 u = kCosines[k & 15], v = kCosines[16 - (k & 15)];
+  Two C = {u.x, u.y}, S = {v.x, v.y};
+  if (k & 16) {
+    const Two t = C;
+    C = {-S.h, -S.l};
+    S = t;
   }
-  for (int e = 0; e < 4; ++e) {
-    if (!((which >> e | which >> (4 + e)) & 1)) continue;
-    double u = x[e], v = x[4 + e];
-    if (gain) u *= f * (double)gain[d.a + e], v *= f * (double)gain[d.b + e];
-    if (turn && d.pair) {
-      double sn, cs;
-      turn_exactly(turns_of(a, position, d.a + e), sn, cs);
-      const double w = u * cs - v * sn;
-      v = v * cs + u * sn;
-      u = w;
-    }
-    y[e] = u, y[4 + e] = v;
-  }
+  if (k & 32) C = {-C.h, -C.l}, S = {-S.h, -S.l};
+  const Two Ss = product(S, s), Cs = product(C, s);
+  const Two c = sum(C, sum(product(C, w), Two{-Ss.h, -Ss.l})), t = sum(S, sum(product(S, w), Cs));
+  cs = sum(c.h, c.l);  // (the first parts the nearest)
+  sn = sum(t.h, t.l);
 }
 
 // What 8 dims (two fours) become in 4 bits.
@@ -143,78 +133,63 @@ struct Coded {
 };
 
 // The larger of a head's two fours' numbers with the other fours of their 16 dims.
-template <typename T>
-__device__ __forceinline__ void over_blocks(T& u, T& v, bool pair) {
-  const T u1 = __shfl_xor_sync(~0u, u, 1), v1 = __shfl_xor_sync(~0u, v, 1);
-  u = u1 > u ? u1 : u, v = v1 > v ? v1 : v;
-  const T u2 = __shfl_xor_sync(~0u, u, 2), v2 = __shfl_xor_sync(~0u, v, 2);
+__device__ __forceinline__ void over_blocks(float& u, float& v, bool pair) {
+  u = fmaxf(u, __shfl_xor_sync(~0u, u, 1)), v = fmaxf(v, __shfl_xor_sync(~0u, v, 1));
+  const float u2 = __shfl_xor_sync(~0u, u, 2), v2 = __shfl_xor_sync(~0u, v, 2);
   if (pair)
-    u = u2 > u ? u2 : u, v = v2 > v ? v2 : v;
+    u = fmaxf(u, u2), v = fmaxf(v, v2);
   else
-    u = v = v > u ? v : u;
+    u = v = fmaxf(u, v);
 }
 
-// off: how far each of the values may be from its exact one (0: it is exact, of bf16).  Returns
-// bits of the dims whose code, and 2^8 if a scale, is that near to a border.
-__device__ __forceinline__ uint32_t code8(const float (&y)[8], const float (&off)[8], bool pair, Coded& to, bool& odd) {
-  float most[2] = {0.f, 0.f}, far[2] = {0.f, 0.f};
+// Exact values of bf16.
+__device__ __forceinline__ void code8(const float (&y)[8], bool pair, Coded& to) {
+  float most[2] = {0.f, 0.f};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    most[e / 4] = fmaxf(most[e / 4], fabsf(y[e]));
-    odd = odd || !(fabsf(y[e]) <= 3.4028235e38f);
-    far[e / 4] = fmaxf(far[e / 4], off[e]);
-  }
+  for (int e = 0; e < 8; ++e) most[e / 4] = fmaxf(most[e / 4], fabsf(y[e]));
   over_blocks(most[0], most[1], pair);
-  over_blocks(far[0], far[1], pair);
-  uint32_t near = 0;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const float t = most[k] * (1.f / 7.f);
-    float steps;
-    const float s = scale_of(t, steps), exact = exact_scale(most[k]), inv_step = steps > 0.f ? __fdividef(steps, t) : 0.f;
-    if (far[k] > 0.f && fabsf(fabsf(steps - rintf(steps)) - 0.5f) <= (far[k] + 2.5e-7f * t) * inv_step * 1.001f) near |= 256u;
-    to.s[k] = far[k] > 0.f ? s : exact;
+    to.s[k] = exact_scale(most[k]);
     const float inv = reciprocal(to.s[k]);
 #pragma unroll
-    for (int e = 4 * k; e < 4 * k + 4; ++e) {
-      const float q = y[e] * inv;
-      if (off[e] > 0.f && fabsf(fabsf(q - rintf(q)) - 0.5f) <= fmaf(off[e], inv, 4e-6f)) near |= 1u << e;
-      to.c[e] = off[e] > 0.f ? code_bits_near(q) : code_bits_clamped(y[e], inv);
-    }
+    for (int e = 4 * k; e < 4 * k + 4; ++e) to.c[e] = code_bits_clamped(y[e], inv);
   }
-  if (odd)
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (y[e] != y[e]) to.c[e] = code_bits_near(0.f);
-  return near;
 }
 
-// The same of exact values: with bit 2^8 of `which` all of it, else those codes that it has bits for.
-__device__ __noinline__ void code8_exactly(const double (&y)[8], uint32_t which, bool pair, Coded& to) {
-  if (which & 256u) {
-    double most[2] = {0.0, 0.0}, steps;
-    for (int e = 0; e < 8; ++e) most[e / 4] = fmax(most[e / 4], fabs(y[e]));
-    over_blocks(most[0], most[1], pair);
-    for (int k = 0; k < 2; ++k) to.s[k] = scale_of(most[k] / 7.0, steps);
-  }
+// A whole number n next to (x.h + x.l) / s, 0 if s is, made the nearest one (ties to even).
+__device__ __forceinline__ float nearest(float n, Two x, float s) {
+  // (n s, its difference from x.h and that one's from the border, where it is near, are exact)
+  const float d = fmaf(-n, s, x.h), past = (fabsf(d) - 0.5f * s) + (d < 0.f ? -x.l : x.l);
+  const bool other = past > 0.f || (past == 0.f && ((int)n & 1));
+  return other && s > 0.f ? n + copysignf(1.f, d) : n;
+}
+
+// Values as pairs of floats (their first parts the nearest to them).
+__device__ __forceinline__ void code8(const Two (&y)[8], bool pair, Coded& to) {
+  float most[2] = {0.f, 0.f}, rest[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most[e / 4] = fmaxf(most[e / 4], fabsf(y[e].h));
+  over_blocks(most[0], most[1], pair);
+#pragma unroll
   for (int e = 0; e < 8; ++e)
-    if ((which >> e) & 1) {
-      // which of the two whole numbers around it is nearer: their border times s is exact, and the
-      // quotient in 32 bits is within 1e-4 of the right one
-      const double s = to.s[e / 4], m = fabs(y[e]);
-      if (!(m <= 3.4e38)) {
-        to.c[e] = code_bits_near(m == m ? copysignf(7.f, (float)y[e]) : 0.f);
-      } else if (s == 0.0) {
-        to.c[e] = code_bits_near(0.f);
-      } else {
-        const float low = fminf(floorf((float)m * reciprocal((float)s) - 1e-4f), 7.f);
-        const double over = m - ((double)low + 0.5) * s;
-        const float up = low + (over > 0.0 || (over == 0.0 && ((int)low & 1)) ? 1.f : 0.f);
-        const double more = m - ((double)up + 0.5) * s;  // (low may have been one too low)
-        const float c = up + (more > 0.0 || (more == 0.0 && ((int)up & 1)) ? 1.f : 0.f);
-        to.c[e] = code_bits_near(copysignf(c, (float)y[e]));
-      }
+    if (fabsf(y[e].h) == most[e / 4]) rest[e / 4] = fmaxf(rest[e / 4], y[e].h < 0.f ? -y[e].l : y[e].l);
+  over_blocks(rest[0], rest[1], pair);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    // the scale: a seventh in steps of those around it
+    const int e = min(max((int)(__float_as_uint(most[k] * (1.f / 7.f)) >> 23), 127 - 14), 127 + 9);
+    const float step = __uint_as_float((uint32_t)(e - 3) << 23), big = fminf(most[k], 7168.f);
+    const float n = rintf(big * (1.f / 7.f) * __uint_as_float((uint32_t)(2 * 127 + 3 - e) << 23));
+    const float s = fminf(fminf(nearest(n, {big, most[k] < 7168.f ? rest[k] : 0.f}, 7.f * step), 16.f) * step, kMaxScale4);
+    to.s[k] = s;
+    const float inv = reciprocal(s);
+#pragma unroll
+    for (int f = 4 * k; f < 4 * k + 4; ++f) {
+      const float c = rintf(fminf(fmaxf(y[f].h * inv, -7.f), 7.f));
+      to.c[f] = code_bits_near(nearest(c, y[f], s));
     }
+  }
 }
 
 // Four codes, as the even four of a word.
@@ -274,11 +249,19 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     at = fits ? L + i : -1;
     position = a.positions ? a.positions[r] : fits ? L + i : 0;
   }
-  float sn[4], cs[4];
+  float sn[4], cs[4], sn_l[4], cs_l[4];  // (the second parts for keys in 4 bits)
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    sn[e] = 0.f, cs[e] = 1.f;
-    if (d.pair) sincospif((float)(int32_t)(turns_of(a, position, d.a + e) >> 32) * 0x1p-31f, &sn[e], &cs[e]);
+    sn[e] = sn_l[e] = cs_l[e] = 0.f, cs[e] = 1.f;
+    if (!d.pair) continue;
+    const uint64_t turns = (uint64_t)(int64_t)position * a.turn[d.a + e];
+    if constexpr (FOUR) {
+      Two s, c;
+      turn_exactly(turns, s, c);
+      sn[e] = s.h, sn_l[e] = s.l, cs[e] = c.h, cs_l[e] = c.l;
+    } else {
+      sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &sn[e], &cs[e]);
+    }
   }
   bool odd = false;
   // One head of a row (threads whose head there is not take part in the shuffles).
@@ -286,34 +269,58 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
     constexpr int K = decltype(kind)::value;
     const bool live = at >= 0 && head < heads[K];
     const float* norm = K == 0 ? a.q_norm : K == 1 ? a.k_norm : nullptr;
-    float x[8], y[8], off[8];  // off: how far a value is from the exact one, at most (4 bits)
+    float x[8], y[8];
+    Two z[8];  // (keys in 4 bits)
     floats<F32>(raw[0], x);
     floats<F32>(raw[1], x + 4);
-    if (K < 2 && norm) {
-      float ss = 0.f;
+    if constexpr (FOUR && K == 1) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+      for (int e = 0; e < 8; ++e) z[e] = {x[e], 0.f};
+      if (norm) {
+        Two ss = {0.f, 0.f};
 #pragma unroll
-      for (int o = C / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
-      const float f = rsqrtf(fmaf(ss, 1.f / D, a.eps));
+        for (int e = 0; e < 8; ++e) ss = sum(ss, product(x[e], x[e]));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[e] * f * gain[K & 1][e];
+        for (int o = C / 2; o > 0; o >>= 1) ss = sum(ss, Two{__shfl_xor_sync(~0u, ss.h, o), __shfl_xor_sync(~0u, ss.l, o)});
+        // f = 1 / sqrt(v): r (1 + e / 2 + 3 e^2 / 8), e = 1 - v r^2 of the approximate root r
+        const Two v = sum(Two{ss.h * (1.f / D), ss.l * (1.f / D)}, Two{a.eps, 0.f});
+        const float r = rsqrtf(v.h);
+        const Two p = product(v, product(r, r));
+        const float err = (1.f - p.h) - p.l;
+        const Two f = {r, r * err * fmaf(0.375f, err, 0.5f)};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = product(product(x[e], gain[1][e]), f);
+      }
+      if (d.pair)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const Two u = z[e], v = z[4 + e], s = {sn[e], sn_l[e]}, c = {cs[e], cs_l[e]}, ns = {-sn[e], -sn_l[e]};
+          z[e] = sum(product(u, c), product(v, ns));
+          z[4 + e] = sum(product(v, c), product(u, s));
+        }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = sum(z[e].h, z[e].l);
     } else {
+      if (K < 2 && norm) {
+        float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[e];
-    }
+        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float u = y[e], v = y[4 + e];
-      if (FOUR && K > 0) {
-        off[e] = norm || F32 ? kOff * fabsf(u) : 0.f;
-        off[4 + e] = norm || F32 ? kOff * fabsf(v) : 0.f;
-        if (K == 1 && d.pair) off[e] = off[4 + e] = kOff * (fabsf(u) + fabsf(v));
+        for (int o = C / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(~0u, ss, o);
+        const float f = rsqrtf(fmaf(ss, 1.f / D, a.eps));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = x[e] * f * gain[K & 1][e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = x[e];
       }
-      if (K < 2 && d.pair) {
-        y[e] = u * cs[e] - v * sn[e];
-        y[4 + e] = v * cs[e] + u * sn[e];
-      }
+      if (K < 2 && d.pair)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float u = y[e], v = y[4 + e];
+          y[e] = u * cs[e] - v * sn[e];
+          y[4 + e] = v * cs[e] + u * sn[e];
+        }
     }
     if (K == 0) {
       if (live) {
@@ -327,16 +334,25 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
         }
       }
     } else if (FOUR) {
+      // (NaN counts as 0, an infinity as more than the largest scale)
       Coded to;
       bool strange = false;
-      const uint32_t near = code8(y, off, d.pair, to, strange);
-      uint32_t which = __reduce_or_sync(~0u, live ? near : 0u);
-      if (which) {
-        if (which & 256u) which = 511u;
-        double z[8];
-        finish_exactly<D>(a, x, norm, K == 1, position, d, which, z);
-        code8_exactly(z, which, d.pair, to);
+      if constexpr (K == 2) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          strange = strange || !(fabsf(y[e]) <= 3.4028235e38f);
+          if (!(y[e] == y[e])) y[e] = 0.f;
+          z[e] = {y[e], 0.f};
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!(fabsf(z[e].h) <= 3.4028235e38f)) strange = true, z[e] = {z[e].h == z[e].h ? z[e].h : 0.f, 0.f};
       }
+      if constexpr (K == 2 && !F32)
+        code8(y, d.pair, to);
+      else
+        code8(z, d.pair, to);
       // the words of codes: of paired fours a thread writes the one of its even or odd neighbours
       const uint32_t wa = half_word(to.c), wb = half_word(to.c + 4);
       const uint32_t there = __shfl_xor_sync(~0u, c & 1 ? wa : wb, 1);
