@@ -200,7 +200,7 @@ __device__ __forceinline__ uint32_t half_word(const uint32_t* c) {
 // `per` groups of C threads to a row, each its heads in turn (a row's sines and cosines, and the
 // gains, stay in registers).
 template <int D, bool F32, bool FOUR>
-__global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs a, int per) {
+__global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_constant__ AppendArgs a, int per) {
   constexpr int C = D / 8, G = kThreads / C;  // threads of a head, groups of them
   const int tid = threadIdx.x, c = tid % C, group = tid / C;
   const int r = blockIdx.x * (G / per) + group / per, h0 = group % per;
@@ -399,9 +399,9 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
 template <int D, bool F32>
 cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
   constexpr int G = kThreads / (D / 8);
-  // few rows: as many threads to one as there are heads; many: four groups, whose sines, cosines and
-  // gains serve all their heads
-  int per = 4;
+  // few rows: as many threads to one as there are heads; many: two groups, whose sines, cosines and
+  // gains serve all their heads (7564 rows, us with 2 / 4 / 8: 30.7 / 31.7 / 41)
+  int per = 2;
   while (per < G && per < a.nq && (int64_t)a.rm.rows * per / G < 2 * device_sms()) per *= 2;
   return launch_pdl(a.ck4 ? append_kernel<D, F32, true> : append_kernel<D, F32, false>,
                     dim3((a.rm.rows + G / per - 1) / (G / per)), dim3(kThreads), 0, st, 1, a, per);
