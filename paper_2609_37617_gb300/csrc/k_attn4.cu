@@ -24,7 +24,8 @@ constexpr int kParts = 2 * 16;
 // 3 / 5 / 8: 16 requests of one row 26.4 / 21.1 / 22.0 / 22.6.
 constexpr int kTurn = 4;
 
-enum Mode : int { kShares = 0, kWhole = 1 };
+// How the items go over the CTAs: even shares of all units, or the same number of CTAs to each item.
+enum Mode : int { kShares = 0, kDirect = 1 };
 
 struct Work {
   float2* o;   // [2 CTAs][pairs of dims][32 lanes]
@@ -371,7 +372,7 @@ __device__ __forceinline__ void place_of(int pair, int lane, int& query, int& di
 
 template <int D, int NT, bool F32>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
-    attn4_kernel(const __grid_constant__ Tree4Args a4, Work ws, int mode, int turn) {
+    attn4_kernel(const __grid_constant__ Tree4Args a4, Work ws, int mode, int turn) {  // (kDirect: turn CTAs to an item)
   using S = Shape<D, NT, F32>;
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ UnitPlan s_plan;
@@ -386,17 +387,22 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
   ptx::griddep_launch_dependents();
   Unit it;
   int u1 = 0;
-  if (mode == kWhole) {
-    it.b = blockIdx.z, it.g = blockIdx.y, it.qt = blockIdx.x;
+  const size_t block = ((size_t)blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+  if (mode == kDirect) {
+    const int p = blockIdx.x % turn;
+    it.b = blockIdx.z, it.g = blockIdx.y, it.qt = blockIdx.x / turn;
     it.r0 = a.rm.start[it.b];
     it.rows = a.rm.start[it.b + 1] - it.r0;
     it.L = a.len[it.b];
     const bool some = it.qt * S::Q < it.rows * (a.nq / a.nkv), fits = rows_fit(it.L, it.rows, a.cap);
     if (some && !fits && tid == 0 && a.err) atomicOr(a.err, kErrCapacity);
     it.tiles = some && fits ? (it.L + it.rows + 127) / 128 : 0;
-    it.t0 = 0;
-    it.t1 = it.tiles;
-    if (it.tiles == 0) return;
+    it.t0 = it.tiles * p / turn;
+    it.t1 = it.tiles * (p + 1) / turn;
+    if (it.t0 == it.t1) {  // (a part of fewer tiles than parts)
+      if (turn > 1 && tid < S::Q) ws.ml[block * S::Q + tid] = make_float2(-INFINITY, 0.f);
+      return;
+    }
   } else {
     if (warp == 0) {
       make_plan(a, S::Q, turn, lane, s_plan, blockIdx.x == 0);
@@ -479,8 +485,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
               make_float2(x.o[nt][mt][e] * f, x.o[nt][mt][2 + e] * f);
       }
     __syncthreads();
-    const bool done = it.t0 == 0 && it.t1 == it.tiles;
-    const size_t part = (size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1);
+    const bool done = mode == kDirect ? turn == 1 : it.t0 == 0 && it.t1 == it.tiles;
+    const size_t part = mode == kDirect ? block : (size_t)blockIdx.x * 2 + (it.t0 > 0 ? 0 : 1);
     for (int j = tid; j < S::PAIRS * 32; j += kThreads) {
       int query, dim;
       place_of<D>(j / 32, lane, query, dim);
@@ -521,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
 // The parts of items cut between CTAs, joined in CTA order.  A lane has two dims of a query,
 // `split` warps of a block share an item's parts of 32 such, a block has 8 / split times 32.
 template <int D, int NT, bool F32>
-__global__ void __launch_bounds__(kThreads) join4_kernel(const __grid_constant__ TreeArgs a, Work ws, int ctas, int turn, int split) {
+__global__ void __launch_bounds__(kThreads) join4_kernel(const __grid_constant__ TreeArgs a, Work ws, int mode, int ctas, int turn, int split) {
   using S = Shape<D, NT, F32>;
   __shared__ UnitPlan plan;
   __shared__ float2 s_o[kWarps][32], s_ml[kWarps][32];
@@ -531,15 +537,25 @@ __global__ void __launch_bounds__(kThreads) join4_kernel(const __grid_constant__
   const int r0 = a.rm.start[b], rows = a.rm.start[b + 1] - r0, G = a.nq / a.nkv;
   ptx::griddep_launch_dependents();
   const bool some = qt * S::Q < rows * G;
-  if (some && tid < 32) make_plan(a, S::Q, turn, lane, plan, false);
-  __syncthreads();
-  const int tiles = some ? plan.tiles[b] : 0;
-  const int first = some ? plan.unit[b] + (g * plan.qts[b] + qt) * (tiles + turn) + turn : 0;
-  const int c0 = tiles > 0 ? unit_owner(plan, first, ctas) : 0;
-  const int n = tiles > 0 ? unit_owner(plan, first + tiles - 1, ctas) - c0 + 1 : 0;
+  int n = 0;  // parts
+  size_t first_slot = 0;
+  if (mode == kDirect) {
+    n = some && rows_fit(a.len[b], rows, a.cap) ? turn : 0;
+    first_slot = (((size_t)b * gridDim.y + g) * (gridDim.x / each) + qt) * turn;
+  } else {
+    if (some && tid < 32) make_plan(a, S::Q, turn, lane, plan, false);
+    __syncthreads();
+    const int tiles = some ? plan.tiles[b] : 0;
+    if (tiles > 0) {
+      const int first = plan.unit[b] + (g * plan.qts[b] + qt) * (tiles + turn) + turn;
+      const int c0 = unit_owner(plan, first, ctas);
+      n = unit_owner(plan, first + tiles - 1, ctas) - c0 + 1;
+      first_slot = (size_t)c0 * 2;
+    }
+  }
   ptx::griddep_wait();
   if (n <= 1) return;  // skipped, or written by its CTA
-  auto part = [&](int k) { return (size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0); };
+  auto part = [&](int k) { return mode == kDirect ? first_slot + k : first_slot + 2 * k + (k == 0 ? 1 : 0); };
   int query, dim;
   place_of<D>(pair, lane, query, dim);
   const int q = qt * S::Q + query;
@@ -567,8 +583,10 @@ __global__ void __launch_bounds__(kThreads) join4_kernel(const __grid_constant__
     for (int u = 0; u < U; ++u) {
       const float f = part_weight(ml[u].x, M);
       l = fmaf(ml[u].y, f, l);
-      o.x = fmaf(v[u].x, f, o.x);
-      o.y = fmaf(v[u].y, f, o.y);
+      if (ml[u].x != -INFINITY) {  // (a part without tiles has written no more)
+        o.x = fmaf(v[u].x, f, o.x);
+        o.y = fmaf(v[u].y, f, o.y);
+      }
     }
   }
   if (split > 1) {
@@ -614,14 +632,28 @@ cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sm
   const int64_t tiles = (max_keys + 127) / 128, units = items * tiles;
   const dim3 each((most * G + S::Q - 1) / S::Q, a.nkv, a.rm.batch);
   if (tiles <= kWholeTiles)
-    return launch_pdl(attn4_kernel<D, NT, F32>, each, dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kWhole, 0);
-  const int ctas = (int)std::min<int64_t>(units, (int64_t)S::CTAS * sms), turn = units > S::CTAS * sms ? kTurn : 0;
-  const cudaError_t f = launch_pdl(attn4_kernel<D, NT, F32>, dim3(ctas), dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kShares, turn);
+    return launch_pdl(attn4_kernel<D, NT, F32>, each, dim3(kThreads), S::SMEM, st, 1, a4, ws, (int)kDirect, 1);
+  int mode = kShares, ctas = (int)std::min<int64_t>(units, (int64_t)S::CTAS * sms);
+  int turn = units > S::CTAS * sms ? kTurn : 0;
+  int64_t parts = ctas / std::max<int64_t>(items, 1);
+  // One request: the same number of CTAs to each of its items, without a plan: four fifths of the SMs, or
+  // two to an SM where each would have more than eight tiles.  us, one row of 28 / 4 heads over 300 / 1564 / 8000 / 15128 / 60000 entries:
+  // by even shares 6.5 / 7.0 / 9.5 / 12.8 / 17.5; 20 CTAs to an item 5.6 / 6.3 / 8.8 / 10.4 / 24.0,
+  // 30 5.6 / 6.3 / 8.3 / 9.1 / 18.1, 38 (every SM has one, or some two and some none) 5.7 / 6.3 / 9.2 / 11.4 / -, 76 5.7 /
+  // 6.3 / 8.9 / 10.4 / 17.2.
+  if (a.rm.batch == 1 && 2 * items <= sms) {
+    mode = kDirect;
+    parts = std::max<int64_t>(1, 4 * sms / 5 / items);
+    if (tiles > 8 * parts) parts = S::CTAS * sms / items;
+    parts = std::min(parts, tiles);
+    turn = (int)parts;
+  }
+  const cudaError_t f = launch_pdl(attn4_kernel<D, NT, F32>, mode == kDirect ? dim3(each.x * turn, each.y, each.z) : dim3(ctas),
+                                   dim3(kThreads), S::SMEM, st, 1, a4, ws, mode, turn);
   if (f != cudaSuccess) return f;
-  const int64_t parts = ctas / std::max<int64_t>(items, 1);
   const int split = parts > 20 ? 8 : parts > 10 ? 4 : parts > 5 ? 2 : 1;
   const dim3 joins(each.x * (S::PAIRS * split / kWarps), each.y, each.z);
-  return launch_pdl(join4_kernel<D, NT, F32>, joins, dim3(kThreads), 0, st, 1, a, ws, ctas, turn, split);
+  return launch_pdl(join4_kernel<D, NT, F32>, joins, dim3(kThreads), 0, st, 1, a, ws, mode, ctas, turn, split);
 }
 
 // Requests of more queries to a kv head go to k_attn4_wide.cu.
