@@ -766,7 +766,7 @@ as2d_status as2d_prompt_attention_workspace(const as2d_cache* cache, int64_t* by
 
 /* Causal attention of whole prompts over one layer of a cache: as as2d_tree_attention
    with rows[b] up to the capacity, row i of request b seeing the entries 0 ..
-   kv_len[b] + i; visible is NULL.  bf16 queries (others: AS2D_ERR_UNSUPPORTED); the
+   kv_len[b] + i; visible is NULL, out 32-byte aligned.  bf16 queries (others: AS2D_ERR_UNSUPPORTED); the
    weights p enter the products in bf16, their sum in 32 bits.  What a row does not see does
    not reach its result, whatever it holds; a value that it sees and that is not
    finite makes its dim not finite, and NaN or +inf among its scores the row NaN in out

@@ -2,6 +2,9 @@
 rows appended to caches in bf16 and in 4 bits, caches packed and read back, attention over
 caches in 4 bits and of whole prompts, and a run of them together."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -411,21 +414,23 @@ def test_attention4_skips(lib):
 def test_attention4_queries_of_any_size(lib, q_type):
     """Queries far from 1, with the scale that brings their scores back; scores far apart;
     zeros; queries that are not finite."""
-    for size in (2.0 ** -100, 2.0 ** -20, 2.0 ** 20, 2.0 ** 100):
-        x = Inputs((4, 2, 64), [400], [5], trees.chain_masks([5]), q_type, spread=size)
-        x.scale = 0.125 / size
+    for heads, lens in (((4, 2, 64), [400]), ((28, 4, 128), [400]), ((28, 4, 128), [5000, 4000])):  # few, many queries
+        rows = [5] * len(lens)
+        for size in (2.0 ** -100, 2.0 ** -20, 2.0 ** 20, 2.0 ** 100):
+            x = Inputs(heads, lens, rows, trees.chain_masks(rows), q_type, spread=size)
+            x.scale = 0.125 / size
+            check(x, *attend4(lib, x))
+        x = Inputs(heads, lens, rows, trees.chain_masks(rows), q_type, spread=60.0)
         check(x, *attend4(lib, x))
-    x = Inputs((4, 2, 64), [400], [5], trees.chain_masks([5]), q_type, spread=60.0)
-    check(x, *attend4(lib, x))
-    x.q[1] = 0
-    check(x, *attend4(lib, x))
-    base, base_lse = attend4(lib, x)
-    for value in (math.nan, math.inf):
-        x.q[2, 3, 7] = value
-        out, lse = attend4(lib, x)
-        assert torch.isnan(out[2, 3]).all() and torch.isnan(lse[2, 3])
-        out[2, 3], lse[2, 3] = base[2, 3], base_lse[2, 3]
-        assert torch.equal(out, base) and torch.equal(lse, base_lse)
+        x.q[1] = 0
+        check(x, *attend4(lib, x))
+        base, base_lse = attend4(lib, x)
+        for value in (math.nan, math.inf):
+            x.q[2, 3, 7] = value
+            out, lse = attend4(lib, x)
+            assert torch.isnan(out[2, 3]).all() and torch.isnan(lse[2, 3])
+            out[2, 3], lse[2, 3] = base[2, 3], base_lse[2, 3]
+            assert torch.equal(out, base) and torch.equal(lse, base_lse)
 
 
 # ---- prompts ---------------------------------------------------------------------
@@ -563,6 +568,53 @@ def test_prompt_skips(lib):
         assert (out[:60] == 3).all() and (lse[:60] == 3).all() and torch.equal(out[60:], base[60:])
 
 
+@pytest.mark.parametrize("lens,rows", [([50], [200]), ([0], [1500]), ([6000], [40])])
+def test_prompt_queries_and_keys_not_finite(lib, lens, rows):
+    """A query that is not finite makes its row NaN and no other; a key that holds infinities gives
+    a score of either sign: a weight of 0, or NaN."""
+    x = Prompt((28, 4, 128), lens, rows)
+    base, base_lse = prompt(lib, x)
+    at, kept = (rows[0] // 3, 9), x.q[rows[0] // 3, 9, 100].clone()
+    for value in (math.nan, math.inf):
+        x.q[at[0], at[1], 100] = value
+        out, lse = prompt(lib, x)
+        assert torch.isnan(out[at]).all() and torch.isnan(lse[at])
+        out[at], lse[at] = base[at], base_lse[at]
+        assert torch.equal(out, base) and torch.equal(lse, base_lse)
+    x.q[at[0], at[1], 100] = kept
+    x.k[0, 0, 1, 3, 64] = math.inf
+    out, lse = prompt(lib, x)
+    sees = torch.arange(rows[0], device="cuda") + lens[0] >= 3
+    gone = (x.q[:, 7:14, 64] < 0) & sees[:, None]  # a score of -inf: as if the entry were not there
+    # (entry 3 is the only one that is -inf: what is left is the softmax of the others)
+    bad = (x.q[:, 7:14, 64] > 0) & sees[:, None]
+    assert torch.isnan(out[:, 7:14][bad]).all() and torch.isnan(lse[:, 7:14][bad]).all()
+    assert torch.isfinite(out[:, 7:14][gone]).all() and (lse[:, 7:14][gone] <= base_lse[:, 7:14][gone] + 1e-4).all()
+    rest = [h for h in range(28) if not 7 <= h < 14]
+    assert torch.equal(out[:, rest], base[:, rest])
+
+
+def test_prompt_references_that_jump(lib):
+    """Scores that grow along the keys, by little and by much, so that a row's reference has to follow;
+    that fall; and whose first tiles are far below the others."""
+    for steps in ((0.02,), (1.0,), (-0.5,), (0.0, 300.0, 0.0)):
+        x = Prompt((28, 4, 128), [0], [1300])
+        n, at = 1300 // len(steps), 0.0
+        level = torch.empty(1300, device="cuda")
+        for i, s in enumerate(steps):
+            if len(steps) > 1:
+                level[i * n:] = at = at + s
+            else:
+                level = torch.arange(1300, device="cuda") * s
+        # one dim of the queries is 1, that of the keys the level: the scores move with it
+        x.q[..., 5] = 1.0
+        x.k[0, 0, :, :1300, 5] = level.bfloat16()
+        x.scale = 1.0
+        x.q[..., :5] *= 0.1
+        x.q[..., 6:] *= 0.1
+        check(x, *prompt(lib, x), p_rel=P_REL)
+
+
 def test_prompt_extreme_scores(lib):
     x = Prompt((4, 2, 64), [50], [200], spread=60.0)
     check(x, *prompt(lib, x), p_rel=P_REL)
@@ -646,6 +698,77 @@ def test_captured_and_on_other_streams(lib):
     other.synchronize()
     for a, b in zip(again, own):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+FIRST_USE = """
+import torch
+import paper_2609_37617_gb300 as lib
+g = torch.Generator(device="cuda").manual_seed(0)
+k, v = (torch.randn((1, 2, 4, 900, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+c4 = [torch.zeros((1, 2, 4, 900, w), dtype=torch.uint8, device="cuda") for w in (64, 8, 64, 8)]
+x = torch.randn((7, 36, 128), generator=g, device="cuda").bfloat16()
+q, kn, vn = x.split([28, 4, 4], 1)
+n = torch.tensor([600, 300], dtype=torch.int32, device="cuda")
+cache, cache4 = lib.Cache(k, v), lib.Cache4(*c4)
+def calls():
+    cache4.write(cache, n)
+    a = cache.append(q, kn, vn, n, [4, 3])
+    b = cache4.append(q, kn, vn, n, [4, 3])
+    return [a, b, cache.prompt_attention(a, n, [4, 3]), cache4.tree_attention(b, n, [4, 3]),
+            cache4.tree_attention(b[:2].contiguous(), n, [1, 1])]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = calls()
+graph.replay()
+torch.cuda.synchronize()
+for a, b in zip([t.clone() for t in got], calls()):
+    torch.cuda.synchronize()
+    assert torch.equal(a, b) and a.abs().sum() > 0
+"""
+
+
+def test_first_use_under_capture(lib):
+    """Kernels' attributes and the device's properties are found out on first use, also where
+    that is captured."""
+    subprocess.run([sys.executable, "-c", FIRST_USE], check=True, timeout=120,
+                   cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+
+def test_binding_refusals(lib):
+    x = Rows((4, 2, 64), [3, 9], [5, 4], torch.bfloat16, layers=1)
+    k, v = (torch.zeros(x.shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cache, c4 = lib.Cache(k, v), x.packed()
+    cache4 = lib.Cache4(*c4)
+    good = dict(q=x.q, k=x.k, v=x.v, kv_len=x.kv_len, rows=x.rows)
+    for c in (cache, cache4):
+        c.append(**good)
+        for change, error in ((dict(q=x.q.cpu()), ValueError), (dict(k=x.k.float()), TypeError), (dict(q=x.q.half()), TypeError),
+                              (dict(v=x.v[:8]), ValueError), (dict(k=x.k[:, :1]), ValueError), (dict(q=None), TypeError),
+                              (dict(q=x.q[..., :32]), ValueError), (dict(v=x.v.transpose(1, 2).contiguous().transpose(1, 2)), ValueError),
+                              (dict(rows=[5, 5]), ValueError), (dict(rows=[9]), ValueError), (dict(rows=[2 ** 32 + 5, 4 - 2 ** 32]), ValueError),
+                              (dict(kv_len=x.kv_len.long()), TypeError), (dict(kv_len=x.kv_len[:1]), ValueError),
+                              (dict(layer=2 ** 32), ValueError), (dict(layer=1), lib.AS2DError), (dict(rotary=2 ** 32), ValueError),
+                              (dict(rotary=16), lib.AS2DError), (dict(q_norm=x.gains[0][:32]), ValueError),
+                              (dict(k_norm=x.gains[1].double()), TypeError), (dict(positions=x.place[:3]), ValueError),
+                              (dict(out=torch.empty_like(x.q, dtype=torch.float32)), TypeError),
+                              (dict(theta=-1.0), lib.AS2DError), (dict(eps=math.nan, q_norm=x.gains[0]), lib.AS2DError)):
+            with pytest.raises(error):
+                c.append(**dict(good, **change))
+    for change, error in ((dict(cache=c4), TypeError), (dict(end=x.kv_len.long()), TypeError), (dict(start=x.kv_len[:1]), ValueError),
+                          (dict(layer=1), lib.AS2DError), (dict(max_entries=2 ** 31), ValueError), (dict(max_entries=-1), lib.AS2DError)):
+        for f in (cache4.write, cache4.read):
+            with pytest.raises(error):
+                f(**dict(dict(cache=cache, end=x.kv_len), **change))
+    for bad in ((c4[0], c4[1], c4[2], c4[1][..., :1]), (c4[0].int(), *c4[1:]), (c4[0][0], *c4[1:]), (c4[0].cpu(), *c4[1:])):
+        with pytest.raises((TypeError, ValueError)):
+            lib.Cache4(*bad)
+    with pytest.raises(lib.AS2DError):
+        cache.prompt_attention(x.q.float().contiguous(), x.kv_len, x.rows)
+    out = torch.empty(9 * 4 * 64 + 8, dtype=torch.bfloat16, device="cuda")[8:].view(9, 4, 64)  # 16 bytes off
+    with pytest.raises(lib.AS2DError):
+        cache.prompt_attention(x.q.contiguous(), x.kv_len, x.rows, out=out)
+    torch.cuda.synchronize()
 
 
 def test_results_repeat(lib):
