@@ -656,19 +656,33 @@ cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sm
   return launch_pdl(join4_kernel<D, NT, F32>, joins, dim3(kThreads), 0, st, 1, a, ws, mode, ctas, turn, split);
 }
 
-// Requests of more queries to a kv head go to k_attn4_wide.cu.
-constexpr int kMostNarrow = 16;
+// Calls of more queries to a kv head than this, and of more units (16 queries, 128 keys) to an SM than
+// kUnits (kOneRequest, of one request, whose items have CTAs of their own), go to k_attn4_wide.cu, which takes
+// 128 queries for the reading of 16.  us on the device here / there, 28 / 4 heads of 128, queries in bf16:
+//   14 queries over 1564 / 15128 entries (96 / 476 units)             8.0 / 10.6,  11.7 / 19.4
+//   16 requests of 14 over 376 .. 7426 (2000)                         23.7 / 36.0
+//   63 queries over 100 / 1500 / 8000 / 30000 (16 / 192 / 1008 / 3760)  6.6 / 9.7,  9.8 / 11.6,  15.1 / 15.8,  31.6 / 25.4
+//   252 over 100 / 1500 / 8000 (64 / 768 / 4032)                      7.4 / 13.7,  13.3 / 15.3,  35.5 / 21.3
+//   2 requests of 21 / 42 over 2000 (256 / 384)                       11.6 / 12.3,  12.9 / 13.3
+//   4 requests of 42 over 300 / 2000 (144 / 768)                      10.7 / 11.3,  16.1 / 14.6
+//   16 requests of 21 / 42 over 500 (512 / 768)                       15.3 / 16.6,  20.3 / 17.3
+constexpr int kMostNarrow = 16, kUnits = 2, kOneRequest = 8;
 
 template <int D>
 cudaError_t launch_d(const Tree4Args& a, void* workspace, int64_t max_keys, cudaStream_t st) {
-  const int sms = device_sms();
+  const int sms = device_sms(), G = a.t.nq / a.t.nkv;
   Work ws;
   ws.o = (float2*)workspace;
   ws.ml = ws.o + (size_t)sms * kParts * D / 2;
-  int most = 0;
-  for (int b = 0; b < a.t.rm.batch; ++b) most = std::max(most, a.t.rm.start[b + 1] - a.t.rm.start[b]);
-  const int queries = most * (a.t.nq / a.t.nkv);
-  if (queries > kMostNarrow) return launch_attention4_wide(a, D, max_keys, workspace, st);
+  int64_t queries = 0, items = 0;
+  for (int b = 0; b < a.t.rm.batch; ++b) {
+    const int64_t n = (int64_t)(a.t.rm.start[b + 1] - a.t.rm.start[b]) * G;
+    queries = std::max(queries, n);
+    items += (n + 15) / 16 * a.t.nkv;
+  }
+  const bool own = a.t.rm.batch == 1 && 2 * items <= sms;
+  if (queries > kMostNarrow && items * ((max_keys + 127) / 128) > (own ? kOneRequest : kUnits) * sms)
+    return launch_attention4_wide(a, D, max_keys, workspace, st);
   if (queries <= 8)
     return a.t.q_f32 ? launch<D, 1, true>(a, ws, max_keys, sms, st) : launch<D, 1, false>(a, ws, max_keys, sms, st);
   return a.t.q_f32 ? launch<D, 2, true>(a, ws, max_keys, sms, st) : launch<D, 2, false>(a, ws, max_keys, sms, st);

@@ -331,6 +331,59 @@ def test_attention4_sizes(lib, heads, length, rows, q_type):
     check(x, *attend4(lib, x))
 
 
+class Roomy(Inputs):
+    """The same in a cache of 65536 entries: with no bound of the lengths, many queries are
+    taken together whatever the lengths are."""
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        for i, c in enumerate(self.c4):
+            self.c4[i] = torch.full((*c.shape[:3], 65536, c.shape[4]), 0xFF, dtype=torch.uint8, device="cuda")
+            self.c4[i][:, :, :, :c.shape[3]] = c
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("heads", [(28, 4, 128), (8, 8, 64), (48, 2, 128)])
+@pytest.mark.parametrize("length", [0, 1, 63, 127, 128, 129, 1000])
+@pytest.mark.parametrize("rows", [5, 19, 64])
+def test_attention4_sizes_in_a_large_cache(lib, heads, length, rows, q_type):
+    rows = max(rows, 17 * heads[1] // heads[0] + 1)
+    masks = trees.tree_masks([rows], np.random.default_rng(length + rows))
+    x = Roomy(heads, [length], [rows], masks, q_type, seed=length)
+    many = attend4(lib, x)
+    check(x, *many)
+    check(x, *attend4(lib, x, max_len=max(length, 1)))
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+def test_attention4_in_a_large_cache(lib, q_type):
+    """Masks, skips and what is not finite where many queries are taken together."""
+    masks = [[0, 0b1, 0b11110, 0b11111, (2 ** 64 - 1) ^ 0b11111, 2 ** 64 - 1]]
+    for length in (0, 130):
+        x = Roomy((28, 4, 128), [length], [6], masks, q_type)
+        base, base_lse = attend4(lib, x)
+        check(x, base, base_lse)
+        for c in x.c4:
+            c[0, 0, :, length + 1] = 0xFE
+        out, lse = attend4(lib, x)
+        for i in (0, 1, 4):
+            assert torch.equal(out[i], base[i]) and torch.equal(lse[i], base_lse[i])
+    x = Roomy((28, 4, 128), [400], [5], trees.chain_masks([5]), q_type, spread=60.0)
+    base, base_lse = attend4(lib, x)
+    check(x, base, base_lse)
+    for value in (math.nan, math.inf):
+        x.q[2, 3, 7] = value
+        out, lse = attend4(lib, x)
+        assert torch.isnan(out[2, 3]).all() and torch.isnan(lse[2, 3])
+        out[2, 3], lse[2, 3] = base[2, 3], base_lse[2, 3]
+        assert torch.equal(out, base) and torch.equal(lse, base_lse)
+    for bad in (65532, -1, 2 ** 31 - 1, -2 ** 31):
+        x.kv_len.fill_(bad)
+        out, lse, err = torch.full_like(x.q, 3.0).contiguous(), torch.full((5, 28), 3.0, device="cuda"), ints([0])
+        lib.Cache4(*x.c4).tree_attention(x.q, x.kv_len, x.rows, out=out, lse=lse, error_bits=err)
+        assert err.item() == lib.AS2D_DEVERR_CAPACITY and (out == 3).all() and (lse == 3).all()
+
+
 @pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("heads", [(4, 2, 64), (28, 4, 128)])
 @pytest.mark.parametrize("most", [1, 2, 64])
