@@ -32,6 +32,7 @@ struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;
   static constexpr uint32_t Q = (F32 ? 2 : 1) * STAGE;
   static constexpr int NST = 4;
+  static_assert(128u * D * (F32 ? 4 : 2) <= NST * STAGE, "queries in the ring");
   static constexpr uint32_t SMEM = 1024 + Q + NST * STAGE + 128 * 4 + 2 * 128 * 8 + (2 * NST + 6) * 8 + 16;
   static_assert(SMEM + sizeof(UnitPlan) + sizeof(First) + sizeof(Unit) <= 232448, "shared memory of one CTA");
 };
@@ -74,54 +75,77 @@ __device__ __forceinline__ void put_piece(uint8_t* img, int row, int part, const
   }
 }
 
-// A query of an item into the operand image(s), by a warp: halves times a power of two that brings
-// its largest dim to 2^14 .. 2^15; returns what its scores are to be multiplied by.
+// Query n of warp w of 12: four and four.
+__device__ __forceinline__ int query_of(int w, int n) { return 48 * (n >> 2) + 4 * w + (n & 3); }
+
+// A warp's queries of an item as they are in memory, into shared memory.
 template <int D, bool F32>
-__device__ __forceinline__ float put_query(const TreeArgs& a, const Unit& it, int row, int lane, uint8_t* img) {
-  constexpr int N = D / 32;  // dims of a lane
-  const int G = a.nq / a.nkv, q = it.qt * 128 + row, i = divide_group(a, q), h = it.g * G + (q - i * G);
-  const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D + N * lane;
-  float x[N];
+__device__ __forceinline__ void stage_queries(const TreeArgs& a, const Unit& it, int w, int end, int lane, uint8_t* to) {
+  constexpr int ROW = D * (F32 ? 4 : 2), PIECES = ROW / 16;
+  const int G = a.nq / a.nkv;
+#pragma unroll 1
+  for (int x = lane, row; (row = query_of(w, x / PIECES)) < end; x += 32) {
+    const int q = it.qt * 128 + row, i = divide_group(a, q), h = it.g * G + (q - i * G);
+    const int64_t at = (it.r0 + i) * a.q_stride + (int64_t)h * D;
+    ptx::cp_async16(to + row * ROW + x % PIECES * 16, (const uint8_t*)a.q + at * (F32 ? 4 : 2) + x % PIECES * 16);
+  }
+  ptx::cp_async_wait_all();
+  __syncwarp();
+}
+
+// Four queries (of which those below `end` are there) into the operand image(s), by a warp, eight
+// lanes to a query: halves times a power of two that brings the largest dim to 2^14 .. 2^15, and
+// what its scores are to be multiplied by.
+template <int D, bool F32>
+__device__ __forceinline__ void put_queries(const TreeArgs& a, const uint8_t* staged, int row, int end, int lane, uint8_t* img, float* back) {
+  constexpr int N = F32 ? 4 : 8, PIECES = D / N / 8;  // dims of a piece of 16 bytes, a lane's pieces
+  const int c = lane & 7;
+  float x[PIECES][N];
 #pragma unroll
-  for (int e = 0; e < N; e += 2) {
-    if constexpr (F32) {
-      const float2 v = *reinterpret_cast<const float2*>((const float*)a.q + at + e);
-      x[e] = v.x, x[e + 1] = v.y;
-    } else {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>((const bf16*)a.q + at + e);
-      x[e] = __uint_as_float(w << 16);
-      x[e + 1] = __uint_as_float(w & 0xFFFF0000u);
-    }
+  for (int p = 0; p < PIECES; ++p) {
+    const uint4 v = reinterpret_cast<const uint4*>(staged + row * D * (F32 ? 4 : 2))[c + 8 * p];
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      x[p][e] = __uint_as_float(F32 ? w[e % 4] : e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
   }
   float most = 0.f, zero = 0.f;  // 0 times every dim: NaN if one is not finite
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    most = fmaxf(most, fabsf(x[e]));
-    zero = fmaf(x[e], 0.f, zero);
-  }
+  for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-  if (__any_sync(~0u, zero != zero)) zero = __uint_as_float(0x7FFFFFFFu);
+    for (int e = 0; e < N; ++e) {
+      most = fmaxf(most, fabsf(x[p][e]));
+      zero = fmaf(x[p][e], 0.f, zero);
+    }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+  if ((__ballot_sync(~0u, zero != zero) >> (lane & 24)) & 0xFFu) zero = __uint_as_float(0x7FFFFFFFu);
+  if (row >= end) return;
   // 2^up in two factors, as up may be 163
   const int up = most > 0.f && zero == 0.f ? 14 - ilogbf(most) : 0;
   const int u0 = up / 2, u1 = up - u0;
   const float f0 = __uint_as_float((uint32_t)(127 + u0) << 23), f1 = __uint_as_float((uint32_t)(127 + u1) << 23);
-  uint32_t hi[N / 2], lo[N / 2];
 #pragma unroll
-  for (int e = 0; e < N / 2; ++e) {
-    const float y0 = x[2 * e] * f0 * f1 + zero, y1 = x[2 * e + 1] * f0 * f1 + zero;
-    hi[e] = halves(y0, y1);
-    const float2 r = floats_of(hi[e]);
-    lo[e] = halves(y0 - r.x, y1 - r.y);
-  }
-  uint8_t* to = img + chunk_off(row, lane * N / 8) + lane * N % 8 * 2;
+  for (int p = 0; p < PIECES; ++p) {
+    uint32_t hi[N / 2], lo[N / 2];
 #pragma unroll
-  for (int e = 0; e < N / 2; ++e) {
-    reinterpret_cast<uint32_t*>(to)[e] = hi[e];
-    if (F32) reinterpret_cast<uint32_t*>(to + 128 * D * 2)[e] = lo[e];
+    for (int e = 0; e < N / 2; ++e) {
+      const float y0 = x[p][2 * e] * f0 * f1 + zero, y1 = x[p][2 * e + 1] * f0 * f1 + zero;
+      hi[e] = halves(y0, y1);
+      const float2 r = floats_of(hi[e]);
+      lo[e] = halves(y0 - r.x, y1 - r.y);
+    }
+    const int dim = (c + 8 * p) * N;
+    uint8_t* to = img + chunk_off(row, dim / 8) + dim % 8 * 2;
+    if constexpr (F32) {
+      *reinterpret_cast<uint2*>(to) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(to + 128 * D * 2) = make_uint2(lo[0], lo[1]);
+    } else {
+      *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    }
   }
   const float b = a.scale_log2 * __uint_as_float((uint32_t)(127 - u0) << 23) * __uint_as_float((uint32_t)(127 - u1) << 23);
-  return fminf(fmaxf(b, 1e-37f), 3.4e38f);  // (0 or infinity times a score of none: NaN)
+  if (c == 0) back[row] = fminf(fmaxf(b, 1e-37f), 3.4e38f);  // (0 or infinity times a score of none: NaN)
 }
 
 template <bool F32>
@@ -219,12 +243,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     };
     if (warp >= 8 && warp < 12) fetch(0);
-    if (warp < 12)
+    // (all of a warp's queries on their way together, by the ring, which is empty)
+    if (warp < 12) {
+      const int last = min(queries, 128);
+      stage_queries<D, F32>(a, it, warp, last, lane, ring);
 #pragma unroll 1
-      for (int row = warp; row < min(queries, 128); row += 12) {
-        const float b = put_query<D, F32>(a, it, row, lane, qimg);
-        if (lane == 0) s_back[row] = b;
-      }
+      for (int k = 0; query_of(warp, k) < last; k += 4) put_queries<D, F32>(a, ring, query_of(warp, k + lane / 8), last, lane, qimg, s_back);
+    }
     ptx::fence_proxy_async_smem();
     if (warp == 12 && lane == 0) {  // the item after this one
       Unit then;
