@@ -3,6 +3,25 @@
 //
 // With s_t = scale q k_t over the entries that a row sees (as k_tree_attn.cu):
 //   m = max s_t, l = sum e^(s_t - m), out = sum e^(s_t - m) v_t / l, lse = m + ln l.
+//
+// The G = n_q / n_kv query heads of a kv head, for all rows of a request, form one query matrix,
+// cut into tiles of 8 or 16; a unit is such a tile and 128 keys.  Units are spread over
+// one or two CTAs per SM in even shares, or one request's items over the same number of CTAs each, and the
+// parts joined by join4_kernel.  (Many queries: k_attn4_wide.cu.)
+//
+// Per CTA: eight warps, 16 keys of a tile each, with a ring of copies of their own and no barrier between
+// them until the item's end.  The keys are the rows of the product (S^T = K Q^T, out^T = V^T P^T), so
+// that 8 queries fill its columns: on tcgen05 a tile of 128 rows would be 7 of one token's queries, and codes
+// would go through shared memory twice.  Codes become 16-bit floats in registers, exactly, on their way into
+// mma.sync.  Queries are 16-bit floats times a power of two of their own: bf16 ones exactly (but for dims below 2^-31 of
+// the largest), 32-bit ones in two parts, to 2^-22.  Weights beside bf16 queries are one 16-bit
+// float, off by at most 2^-11 where the result's own rounding is off by 2^-8, beside 32-bit ones two.
+//
+// Bound, one row of 28 / 4 heads of 128 (floor: the cache's 4.5 bits a value, read once): over 15128 entries (1.3 us)
+// by latency, 9.1 us on the device, of which one over 200 takes 5.1.  Over 60000 (5.1) 17.1, and 16 requests over
+// 376 .. 7495 (5.2) 20: 0.75 us a tile on an SM whether it has one CTA or two.  Of the issue slots 52 % are used
+// while it runs, of the pipe for whole numbers some 45 %: the 90 operations on bits and 96 on pairs of halves that decode a
+// warp's 16 keys and values.  (Addresses kept in registers from tile to tile: 1 % less.)
 #include <algorithm>
 
 #include "cache4.cuh"
@@ -611,7 +630,8 @@ __global__ void __launch_bounds__(kThreads) join4_kernel(const __grid_constant__
   if (dim == 0 && a.lse) a.lse[(size_t)(r0 + i) * a.nq + h] = row_lse(M - kUp, l);
 }
 
-// Items of at most this many tiles are each done by one CTA.
+// Items of at most this many tiles are each done by one CTA (us, one row of 28 / 4 heads over 200 entries, with 1 / 2: 5.7 / 5.1;
+// over 300, three tiles by three CTAs and joined: 5.6).
 constexpr int kWholeTiles = 2;
 
 template <int D, int NT, bool F32>
@@ -656,17 +676,19 @@ cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sm
   return launch_pdl(join4_kernel<D, NT, F32>, joins, dim3(kThreads), 0, st, 1, a, ws, mode, ctas, turn, split);
 }
 
-// Calls of more queries to a kv head than this, and of more units (16 queries, 128 keys) to an SM than
-// kUnits (kOneRequest, of one request, whose items have CTAs of their own), go to k_attn4_wide.cu, which takes
-// 128 queries for the reading of 16.  us on the device here / there, 28 / 4 heads of 128, queries in bf16:
-//   14 queries over 1564 / 15128 entries (96 / 476 units)             8.0 / 10.6,  11.7 / 19.4
-//   16 requests of 14 over 376 .. 7426 (2000)                         23.7 / 36.0
-//   63 queries over 100 / 1500 / 8000 / 30000 (16 / 192 / 1008 / 3760)  6.6 / 9.7,  9.8 / 11.6,  15.1 / 15.8,  31.6 / 25.4
-//   252 over 100 / 1500 / 8000 (64 / 768 / 4032)                      7.4 / 13.7,  13.3 / 15.3,  35.5 / 21.3
-//   2 requests of 21 / 42 over 2000 (256 / 384)                       11.6 / 12.3,  12.9 / 13.3
-//   4 requests of 42 over 300 / 2000 (144 / 768)                      10.7 / 11.3,  16.1 / 14.6
-//   16 requests of 21 / 42 over 500 (512 / 768)                       15.3 / 16.6,  20.3 / 17.3
-constexpr int kMostNarrow = 16, kUnits = 2, kOneRequest = 8;
+// Calls of more queries to a kv head than kMostNarrow and of more units (16 queries, 128 keys) than so many to an SM
+// go to k_attn4_wide.cu, which takes 128 queries for the reading of 16 but starts later: kOwn if it is one request, whose items
+// have CTAs of their own; kWhole if items are done whole; else kUnits.  us on the device here / there (units to
+// an SM), 28 / 4 heads of 128, queries in bf16:
+//   one request  14 queries over 1564 / 15128   (0.6) 8.0 / 10.6   (3.1) 11.7 / 19.4
+//                63 over 100 / 1500 / 8000      (0.1) 6.6 / 8.1    (1.3) 9.8 / 10.2    (6.6) 15.0 / 14.4
+//                252 over 100 / 1500 / 4000     (0.4) 7.5 / 10.9   (5.1) 13.3 / 12.5   (13) 22.0 / 15.4
+//                21 over 4000 / 15128           (1.7) 10.6 / 13.4  (6.3) 15.1 / 19.3
+//   items whole  2 requests of 252, 16 of 21 over 200   (1.7) 7.5 / 11.7   (1.7) 7.7 / 11.5
+//   others       4 of 28 / 63 over 300          (0.6) 8.9 / 10.0   (1.3) 11.2 / 10.7
+//                4 of 84 over 600, 2000         (3.2) 13.2 / 11.3  (10) 21.6 / 14.5
+// Up to kMostNarrow queries a key tile is read once here too: 16 requests of 14 over 376 .. 7426 23.7 / 36.0.
+constexpr int kMostNarrow = 16, kOwn = 8, kWhole = 2, kUnits = 1;
 
 template <int D>
 cudaError_t launch_d(const Tree4Args& a, void* workspace, int64_t max_keys, cudaStream_t st) {
@@ -680,8 +702,9 @@ cudaError_t launch_d(const Tree4Args& a, void* workspace, int64_t max_keys, cuda
     queries = std::max(queries, n);
     items += (n + 15) / 16 * a.t.nkv;
   }
-  const bool own = a.t.rm.batch == 1 && 2 * items <= sms;
-  if (queries > kMostNarrow && items * ((max_keys + 127) / 128) > (own ? kOneRequest : kUnits) * sms)
+  const int64_t tiles = (max_keys + 127) / 128;
+  const int most = a.t.rm.batch == 1 && 2 * items <= sms ? kOwn : tiles <= kWholeTiles ? kWhole : kUnits;
+  if (queries > kMostNarrow && items * tiles > (int64_t)most * sms)
     return launch_attention4_wide(a, D, max_keys, workspace, st);
   if (queries <= 8)
     return a.t.q_f32 ? launch<D, 1, true>(a, ws, max_keys, sms, st) : launch<D, 1, false>(a, ws, max_keys, sms, st);
