@@ -1,19 +1,28 @@
 // k_attn4_wide.cu -- attention of a tree of drafted tokens over a cache in 4 bits, for
 // requests of many queries to a kv head (as2d_cache4_attention; k_attn4.cu has few).
 //
+// With s_t = scale q k_t over the entries that a row sees: m = max s_t, l = sum e^(s_t - m),
+// out = sum e^(s_t - m) v_t / l, lse = m + ln l.
+//
 // The units (query tile of 128, 128-key tile) are spread over one CTA per SM and joined as
 // those of k_tree_attn.cu.  Codes become 16-bit floats, exactly, on their way into shared
 // memory, and the products run on tcgen05 with 16-bit floats: a query with a power of two of its own
 // (two parts of 32-bit ones), weights up to 2^15 (two parts beside 32-bit queries).
 //
-// Per CTA (13 warps, TMEM full: two score buffers, two accumulators):
+// Per CTA (16 warps, TMEM full: two score buffers, two accumulators):
 //   warps 0-7   two sets of four that take the item's key tiles in turn, a query a thread: S from
 //               TMEM, mask, running maximum, P = 2^(S - m + 7) back into TMEM over S; each
 //               set has its own accumulator, maximum and sum;
-//   warps 8-11  codes and scales from memory, a tile ahead in registers, into the operand images;
-//   warp 12     issues the products.
+//   warps 8-14  codes and scales from memory, a quarter of a tile ahead in registers, into the operand images;
+//   warp 15     issues the products.
 // Every value that codes stand for is finite, so that what a row does not see needs no care
 // beyond a weight of 0.
+//
+// Bound by the tiles' coming: a tile (128 keys and values, 18 KB) takes an SM 1.6 us beside bf16 queries, 1.9 beside 32-bit
+// ones, whose products alone are 1.1; memory would bring one in 0.4.  448 queries of 28 / 4 heads of 128 over 60000
+// entries, us on the device with 5 / 6 / 7 loading warps: bf16 97.6 / 86.6 / 84.3, 32-bit 109 / 100.5 / 99.1 (four, each
+// with a quarter of every tile and the next tile's in registers: 85.6 / 105.8).  A sixteenth of a tile at a time, with
+// a fence each: 133 / 145.  16 requests of 3 to 17 rows over 376 .. 7495, 32-bit: 37.9.
 #include <algorithm>
 
 #include "cache4.cuh"
@@ -23,9 +32,11 @@
 namespace as2d {
 namespace {
 
-constexpr int kThreads = 416, kLoaders = 128;
+constexpr int kThreads = 512, kLoaders = 7, kIssuer = 15;  // warps 8 .. 14 load, kIssuer issues
 constexpr float kLazy = 8.f, kUp = 7.f;
-constexpr int kTurn = 5;
+// What turning to another item costs a CTA, in tiles.  us with 2 / 3 / 5: 16 requests of 126 32-bit queries over 500 entries
+// 18.5 / 20.0 / 23.3, over 4000 42.6 / 40.8 / 42.0, the ragged ones 41.2 / 37.9 / 38.9.
+constexpr int kTurn = 3;
 
 template <int D, bool F32>
 struct Shape {
@@ -75,8 +86,8 @@ __device__ __forceinline__ void put_piece(uint8_t* img, int row, int part, const
   }
 }
 
-// Query n of warp w of 12: four and four.
-__device__ __forceinline__ int query_of(int w, int n) { return 48 * (n >> 2) + 4 * w + (n & 3); }
+// Query n of warp w: four and four.
+__device__ __forceinline__ int query_of(int w, int n) { return kThreads / 8 * (n >> 2) + 4 * w + (n & 3); }
 
 // A warp's queries of an item as they are in memory, into shared memory.
 template <int D, bool F32>
@@ -169,7 +180,7 @@ template <int D, bool F32>
 __global__ void __launch_bounds__(kThreads, 1)
     wide4_kernel(const __grid_constant__ Tree4Args a4, TreeWork ws, int turn) {
   using S = Shape<D, F32>;
-  constexpr int NST = S::NST, PARTS = D / 32, MINE = 128 * PARTS / kLoaders;  // pieces of a row; of a loader and tile
+  constexpr int NST = S::NST, PARTS = D / 32, MINE = PARTS;  // pieces of a row; a lane's of a quarter of a tile (of keys or values)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -191,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < NST; ++i) {
-      ptx::mbar_init(&full[i], kLoaders / 32);
+      ptx::mbar_init(&full[i], 4);
       ptx::mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -202,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::mbar_init(drain, 1);
     ptx::fence_mbar_init();
   }
-  if (warp == 12) ptx::tmem_alloc(tslot, 512);
+  if (warp == kIssuer) ptx::tmem_alloc(tslot, 512);
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   if (warp == 0) {
@@ -232,33 +243,34 @@ __global__ void __launch_bounds__(kThreads, 1)
   while (more) {
     const int cnt = it.t1 - it.t0, end = it.L + it.rows, queries = it.rows * G - it.qt * 128;
     const size_t head = ((size_t)it.b * a.nkv + it.g) * a.cap;
-    const int ld = tid - 256;  // loader
-    Piece next[2][MINE];
-    auto fetch = [&](int j) {
+    // Quarters of the item's tiles, of keys and of values in turn, go round the loaders.  (Seven to four: a warp's next
+    // quarter is at most two tiles of the ring on, so that the wait for the stage's last use is never for a phase
+    // before the one that runs.)
+    const int quarters = 8 * cnt;
+    Piece next[MINE];
+    auto fetch = [&](int g) {
+      const uint8_t *codes = g & 4 ? a4.v : a4.k, *scales = g & 4 ? a4.vs : a4.ks;
 #pragma unroll
       for (int x = 0; x < MINE; ++x) {
-        const int piece = ld + x * kLoaders, row = min((it.t0 + j) * 128 + piece / PARTS, end - 1);
-        load_piece<D>(a4.k, a4.ks, head + row, piece % PARTS, next[0][x]);
-        load_piece<D>(a4.v, a4.vs, head + row, piece % PARTS, next[1][x]);
+        const int piece = (g & 3) * 32 * MINE + x * 32 + lane, row = min((it.t0 + g / 8) * 128 + piece / PARTS, end - 1);
+        load_piece<D>(codes, scales, head + row, piece % PARTS, next[x]);
       }
     };
-    if (warp >= 8 && warp < 12) fetch(0);
+    if (warp >= 8 && warp < kIssuer && warp - 8 < quarters) fetch(warp - 8);
     // (all of a warp's queries on their way together, by the ring, which is empty)
-    if (warp < 12) {
-      const int last = min(queries, 128);
-      stage_queries<D, F32>(a, it, warp, last, lane, ring);
+    const int last = min(queries, 128);
+    stage_queries<D, F32>(a, it, warp, last, lane, ring);
 #pragma unroll 1
-      for (int k = 0; query_of(warp, k) < last; k += 4) put_queries<D, F32>(a, ring, query_of(warp, k + lane / 8), last, lane, qimg, s_back);
-    }
+    for (int k = 0; query_of(warp, k) < last; k += 4) put_queries<D, F32>(a, ring, query_of(warp, k + lane / 8), last, lane, qimg, s_back);
     ptx::fence_proxy_async_smem();
-    if (warp == 12 && lane == 0) {  // the item after this one
+    if (warp == kIssuer && lane == 0) {  // the item after this one
       Unit then;
       int u = it.next;
       if (!next_item(s_plan, a, u, u1, then)) then.rows = 0;
       s_next = then;
     }
     __syncthreads();
-    if (warp == 12) {
+    if (warp == kIssuer) {
       // the whole warp, for operands in uniform registers; one thread issues
       const uint32_t lead = ptx::elect_one(), tm = __shfl_sync(~0u, tmem, 0);
       auto whole = [&](bool) { return ok = __all_sync(~0u, ok); };
@@ -304,24 +316,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     } else if (warp >= 8) {
 #pragma unroll 1
-      for (int j = 0; j < cnt; ++j) {
+      for (int g = warp - 8; g < quarters; g += kLoaders) {
+        const uint32_t m = n + g / 4, s = m % NST;
+        if (m >= NST) wait(&empty[s], (m / NST - 1) & 1);
+        ok = __all_sync(~0u, ok);
+        if (ok) {
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t m = n + 2 * j + kv, s = m % NST;
-          if (m >= NST) wait(&empty[s], (m / NST - 1) & 1);
-          ok = __all_sync(~0u, ok);
-          if (ok) {
-#pragma unroll
-            for (int x = 0; x < MINE; ++x) {
-              const int piece = ld + x * kLoaders;
-              put_piece<D>(ring + s * S::STAGE, piece / PARTS, piece % PARTS, next[kv][x]);
-            }
+          for (int x = 0; x < MINE; ++x) {
+            const int piece = (g & 3) * 32 * MINE + x * 32 + lane;
+            put_piece<D>(ring + s * S::STAGE, piece / PARTS, piece % PARTS, next[x]);
           }
-          ptx::fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(&full[s]);
         }
-        if (j + 1 < cnt) fetch(j + 1);
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&full[s]);
+        if (g + kLoaders < quarters) fetch(g + kLoaders);
       }
     } else {
       const int set = warp >> 2, quad = warp & 3, row = 32 * quad + lane;  // query of the tile, TMEM lane
@@ -472,13 +481,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     it = then;
     more = it.rows > 0;
   }
-  if (warp == 12) {
+  if (warp == kIssuer) {
     // no product is running when TMEM is freed
     ptx::mma_commit_if(ptx::elect_one(), drain);
     ptx::mbar_wait(drain, 0, ptx::kDrainNs);
   }
   __syncthreads();
-  if (warp == 12) ptx::tmem_dealloc(tmem, 512);
+  if (warp == kIssuer) ptx::tmem_dealloc(tmem, 512);
 }
 
 template <int D, bool F32>
