@@ -16,7 +16,9 @@
 // code and scale is compared with the border that it is next to, which is exact in 32 bits.  (Values
 // near a border computed again in 64 bits instead: the first call of that code on an SM took 11 us.)
 //
-// Bound by memory: each value is read and written once.
+// Bound by memory: each value is read and written once.  7564 rows of 28 / 4 heads of 128, in bf16 (floor 20.5 us): 30.5,
+// of which a launch and the last blocks' end are some 5; 145 rows into 4 bits and read back (0.45) 10.3 on the device,
+// two launches' latency.
 #include <algorithm>
 #include <type_traits>
 

@@ -680,14 +680,14 @@ cudaError_t launch(const Tree4Args& a4, const Work& ws, int64_t max_keys, int sm
 // go to k_attn4_wide.cu, which takes 128 queries for the reading of 16 but starts later: kOwn if it is one request, whose items
 // have CTAs of their own; kWhole if items are done whole; else kUnits.  us on the device here / there (units to
 // an SM), 28 / 4 heads of 128, queries in bf16:
-//   one request  14 queries over 1564 / 15128   (0.6) 8.0 / 10.6   (3.1) 11.7 / 19.4
-//                63 over 100 / 1500 / 8000      (0.1) 6.6 / 8.1    (1.3) 9.8 / 10.2    (6.6) 15.0 / 14.4
-//                252 over 100 / 1500 / 4000     (0.4) 7.5 / 10.9   (5.1) 13.3 / 12.5   (13) 22.0 / 15.4
-//                21 over 4000 / 15128           (1.7) 10.6 / 13.4  (6.3) 15.1 / 19.3
-//   items whole  2 requests of 252, 16 of 21 over 200   (1.7) 7.5 / 11.7   (1.7) 7.7 / 11.5
-//   others       4 of 28 / 63 over 300          (0.6) 8.9 / 10.0   (1.3) 11.2 / 10.7
-//                4 of 84 over 600, 2000         (3.2) 13.2 / 11.3  (10) 21.6 / 14.5
-// Up to kMostNarrow queries a key tile is read once here too: 16 requests of 14 over 376 .. 7426 23.7 / 36.0.
+//   one request  14 queries over 1564 / 15128   (0.3) 8.0 / 10.1   (3.1) 11.7 / 18.6
+//                63 over 100 / 1500 / 8000      (0.1) 6.6 / 8.1    (1.3) 9.8 / 10.0    (6.6) 15.1 / 14.8
+//                252 over 100 / 1500 / 4000     (0.8) 7.4 / 10.8   (5.1) 13.3 / 11.9   (13) 22.0 / 16.0
+//                21 over 4000 / 15128           (1.7) 10.6 / 12.9  (6.3) 15.1 / 18.9
+//   items whole  2 requests of 252, 16 of 21 over 200   (1.7) 7.5 / 11.6   (1.7) 7.7 / 11.1
+//   others       4 of 28 / 63 over 300          (0.6) 8.8 / 9.8    (1.3) 11.2 / 10.6
+//                4 of 84 over 600 / 2000        (3.2) 13.2 / 11.1  (10) 21.6 / 12.5
+// Up to kMostNarrow queries a key tile is read once here too: 16 requests of 14 over 376 .. 7426 23.7 / 32.5.
 constexpr int kMostNarrow = 16, kOwn = 8, kWhole = 2, kUnits = 1;
 
 template <int D>

@@ -2,7 +2,8 @@
 // (as2d_cache4_write, as2d_cache4_read).
 //
 // A thread has 8 dims: 16 bytes of bf16, a word of codes; two threads share a scale.
-// Bound by memory: 2.56 bytes a value.
+// Bound by memory: 2 + 0.5625 bytes a value.  28 layers of 15128 entries, written and read back (4 kv heads of 128:
+// floor 327 us): 356, 6.2 TB/s.
 #include <algorithm>
 
 #include "cache4.cuh"
@@ -11,7 +12,10 @@
 namespace as2d {
 namespace {
 
+// Pieces of a thread on their way together, and blocks to an SM in all, at most: us, the 15128 entries, with 2 / 4 / 8
+// pieces 366 / 358 / 377, with 16 / 64 / 256 blocks 364 / 358 / 385.
 constexpr int kThreads = 256, kAtOnce = 4;
+constexpr int64_t kBlocks = 64;
 
 // The largest magnitude of the 16 is found on pairs of bf16 as whole numbers, of which NaN and
 // infinities are the largest.
@@ -131,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) pack4_kernel(const __grid_constant__
 cudaError_t launch_pack4(const Pack4Args& a, int head_dim, bool write, int max_entries, cudaStream_t st) {
   const int64_t pieces = (int64_t)max_entries * (head_dim / 8), each = kThreads * kAtOnce;
   const int64_t units = std::min<int64_t>(a.units, 65535);
-  const int64_t x = std::max<int64_t>(1, std::min<int64_t>((pieces + each - 1) / each, (64ll * device_sms() + units - 1) / units));
+  const int64_t x = std::max<int64_t>(1, std::min<int64_t>((pieces + each - 1) / each, (kBlocks * device_sms() + units - 1) / units));
   auto* kernel = head_dim == 128 ? (write ? pack4_kernel<128, true> : pack4_kernel<128, false>)
                                  : (write ? pack4_kernel<64, true> : pack4_kernel<64, false>);
   return launch_pdl(kernel, dim3((unsigned)x, (unsigned)units, 2), dim3(kThreads), 0, st, 1, a);
