@@ -16,8 +16,9 @@
 //   warp 0     loads key and value tiles by TMA through a ring of shared-memory stages;
 //   warp 1     issues the products: S = Q K^T, O += P V (P from TMEM) of the two query
 //              tiles in turn, so that one's products run under the other's softmax;
-//   warps 2-3  prepare the value tiles that hold entries not every row sees, and have the next
-//              item's queries brought in (TMA) when the last scores of this one are there;
+//   warp 2     looks for the next item while this one runs, and has its queries brought in (TMA) when the
+//              last scores of this one are there;
+//   warp 3     prepares the value tiles that hold entries not every row sees;
 //   warps 4-11 four to a query tile, a query a thread: S from TMEM, mask, P = 2^(S - m) back into
 //              TMEM in bf16 over S.  The next item's scores are computed while an item's
 //              results are written.
@@ -27,7 +28,9 @@
 // products of one query tile wait for while the other's run, at one exponential a score.
 // Bound by the tensor cores and the chain between them.  7564 rows of 28 / 4 heads of 128 (floor 212 us): 300 to 308, the
 // tensor pipe 57 to 60 % busy; a key tile's four products read shared memory for as many cycles as they compute. Sixteen
-// softmax warps, which have to agree on a reference: 315 and more.
+// softmax warps, which have to agree on a reference: 315 and more; a quarter of the exponentials by
+// polynomials: 363.  Clocks of an item (cycles): 2970 a key tile, of which the softmax of a query tile is 1900 and its two
+// products 1024; at its end 1300 until the results are there and 3700 to write them.
 // P in one bf16 part: each weight is off by at most 2^-8 of itself, as the result's own
 // rounding is; the sums l are of the weights in 32 bits.
 #include <algorithm>
@@ -41,6 +44,8 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr int kMaxTails = 3;  // key tiles that not all rows of 256 queries see whole
+// Items that are described at a time (a power of two): the one whose results are written, the one before and the one after.
+constexpr int kItems = 4;
 // The sum of a tile's 128 weights that makes its maximum the reference.
 constexpr float kMost = 8192.f;
 
@@ -71,7 +76,7 @@ struct Shape {
   static constexpr uint32_t STAGE = 128 * D * 2;  // one K or V tile, and one query tile
   static constexpr int NST = D == 64 ? 8 : 5;
   static constexpr uint32_t SMEM =
-      (2 + NST) * STAGE + (3 * NST + 11 + kMaxTails) * 8 + 4 * kMaxTails * 4 + 2 * sizeof(Item) + 16;
+      (2 + NST) * STAGE + (3 * NST + 10 + 2 * kMaxTails) * 8 + 8 * kMaxTails * 4 + kItems * sizeof(Item) + 16;
   static_assert(SMEM <= 232448, "shared memory of one CTA");
 };
 
@@ -173,20 +178,45 @@ __device__ __forceinline__ Item item_of_cta(const TreeArgs& a, Cut cut, int& n, 
   }
 }
 
+// Whether a value tile has values that are not finite in rows z .. e - 1, by a warp: 0 times one is NaN, and
+// stays in the sum.
+template <int D>
+__device__ __forceinline__ bool not_finite(const uint8_t* v, int z, int e, int lane) {
+  const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+  __nv_bfloat162 s[4] = {zero, zero, zero, zero};
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h) {
+    const uint8_t* end = v + h * kRegion + e * 128;
+#pragma unroll 4
+    for (const uint8_t* at = v + h * kRegion + z * 128 + lane * 16; at < end; at += 512) {
+      const uint4 x = *reinterpret_cast<const uint4*>(at);
+      s[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.x), zero, s[0]);
+      s[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.y), zero, s[1]);
+      s[2] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.z), zero, s[2]);
+      s[3] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.w), zero, s[3]);
+    }
+  }
+  const float2 t = __bfloat1622float2(__hadd2(__hadd2(s[0], s[1]), __hadd2(s[2], s[3])));
+  return __any_sync(~0u, t.x != 0.f || t.y != 0.f);  // (true of NaN)
+}
+
 // Of a value tile the entries from `from` on, which not every row of the item sees: values
 // that are not finite become 0 and their rows are noted in bad (bit: entry - from0); entries
-// from `end` on become 0.
+// from `end` on become 0, if any of both are not finite.  By a warp; of most tiles it is a look (by
+// two warps, value by value, one prompt of 36 rows took 11.2 us, not 10.0, 16 of 100 20.4, not 18.6).
 template <int D>
-__device__ __forceinline__ void clean_tile(uint8_t* v, int p0, int from, int end, int from0, int tid, uint32_t* bad) {
+static __device__ __noinline__ void clean_tile(uint8_t* v, int p0, int from, int end, int from0, int lane, uint32_t* bad) {
   constexpr int C = D / 8;
   const int z = max(from - p0, 0), e0 = min(max(end - p0, z), 128);
+  if (!not_finite<D>(v, z, 128, lane)) return;
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h)
+#pragma unroll 8
+    for (int x = e0 * 128 + lane * 16; x < kRegion; x += 512) *reinterpret_cast<uint4*>(v + h * kRegion + x) = make_uint4(0, 0, 0, 0);
+  if (!not_finite<D>(v, z, e0, lane)) return;
 #pragma unroll 1
-  for (int c = z * C + tid; c < 128 * C; c += 64) {
+  for (int c = z * C + lane; c < e0 * C; c += 32) {
     uint4* at = reinterpret_cast<uint4*>(v + chunk_off(c / C, c % C));
-    if (c >= e0 * C) {
-      *at = make_uint4(0, 0, 0, 0);
-      continue;
-    }
     uint4 x = *at;
     uint32_t* w = reinterpret_cast<uint32_t*>(&x);
     // an exponent of ones, and no other, carries into its value's sign bit
@@ -225,10 +255,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* o_full = p_full + 2;    // [2]
   uint64_t* o_empty = o_full + 2;
   uint64_t* drain = o_empty + 1;
-  uint64_t* v_clean = drain + 1;    // [kMaxTails]
-  uint32_t* s_bad = reinterpret_cast<uint32_t*>(v_clean + kMaxTails);  // [4 kMaxTails]
-  Item* s_item = reinterpret_cast<Item*>(s_bad + 4 * kMaxTails);       // [2] the items of this parity
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(s_item + 2);
+  uint64_t* v_clean = drain + 1;    // [2][kMaxTails] of items of this parity
+  uint32_t* s_bad = reinterpret_cast<uint32_t*>(v_clean + 2 * kMaxTails);  // [2][4 kMaxTails]
+  Item* s_item = reinterpret_cast<Item*>(s_bad + 8 * kMaxTails);           // [kItems]
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(s_item + kItems);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -238,7 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       ptx::mbar_init(&tail_full[i], 1);
     }
     ptx::mbar_init(q_full, 1);
-    ptx::mbar_init(q_empty, 1);
+    // (all that look at q_full let go of an item's queries, so that none of them is an item behind)
+    ptx::mbar_init(q_empty, 10);
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&s_full[i], 1);
       ptx::mbar_init(&p_full[i], 4);
@@ -246,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     ptx::mbar_init(o_empty, 8);
     ptx::mbar_init(drain, 1);
-    for (int i = 0; i < kMaxTails; ++i) ptx::mbar_init(&v_clean[i], 64);
+    for (int i = 0; i < 2 * kMaxTails; ++i) ptx::mbar_init(&v_clean[i], 32);
     ptx::fence_mbar_init();
   }
   if (warp == 1) ptx::tmem_alloc(tslot, 512);
@@ -348,8 +379,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (uint32_t n = 0; ok; ++n) {
       if (n == 0 && s_item[0].cnt == 0) break;
       if (!whole(wait(q_full, n & 1))) break;
-      const int cnt = __shfl_sync(~0u, s_item[n & 1].cnt, 0), tail0 = __shfl_sync(~0u, s_item[n & 1].tail0, 0);
-      const bool two = __shfl_sync(~0u, s_item[n & 1].nq, 0) > 128;
+      const int cnt = __shfl_sync(~0u, s_item[n % kItems].cnt, 0), tail0 = __shfl_sync(~0u, s_item[n % kItems].tail0, 0);
+      const bool two = __shfl_sync(~0u, s_item[n % kItems].nq, 0) > 128;
       if (cnt == 0) break;
       uint32_t k = at.next<NST>(), v = at.next<NST>();
       if (!whole(wait(&full[Stage::slot(k)], Stage::parity(k)))) break;
@@ -367,8 +398,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t v_now = v;
         if (more) k = at.next<NST>(), v = at.next<NST>();
         // the values, the first tile's weights and the next keys: their first looks overlap
-        uint64_t* v_bar = tail < 0 ? &full[Stage::slot(v_now)] : &v_clean[tail];
-        const uint32_t v_parity = tail < 0 ? Stage::parity(v_now) : (c_turn >> tail) & 1;
+        const int tail_bar = (n & 1) * kMaxTails + tail;
+        uint64_t* v_bar = tail < 0 ? &full[Stage::slot(v_now)] : &v_clean[tail_bar];
+        const uint32_t v_parity = tail < 0 ? Stage::parity(v_now) : (c_turn >> tail_bar) & 1;
         const bool v_there = ptx::mbar_try_wait(v_bar, v_parity), p_there = ptx::mbar_try_wait(&p_full[0], p_turn & 1);
         const bool k_there = !more || ptx::mbar_try_wait(&full[Stage::slot(k)], Stage::parity(k));
         if (!v_there) wait(v_bar, v_parity);
@@ -376,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!k_there) wait(&full[Stage::slot(k)], Stage::parity(k));
         if (j == 0 && n > 0) wait(o_empty, (n - 1) & 1);
         if (!whole(ok)) break;
-        if (tail >= 0) c_turn ^= 1u << tail;
+        if (tail >= 0) c_turn ^= 1u << tail_bar;
         p_turn ^= two ? 3u : 1u;
         ptx::tc_fence_after();
         const uint32_t vt = uniform(ptx::desc_lo(stage_of(v_now), kRegion)), kt = uniform(ptx::desc_lo(stage_of(k), 16u));
@@ -405,9 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // no product is running when TMEM is freed
     ptx::mma_commit_if(lead, drain);
     ptx::mbar_wait(drain, 0, ptx::kDrainNs);
-  } else if (warp < 4) {
-    const int t64 = tid - 64;
-    uint32_t tiles = 0, turn = 0;
+  } else if (warp == 2) {
     auto load_queries = [&](const Item& it) {  // by one thread
       const int heads = min(256, a.nq / a.nkv);
       ptx::mbar_arrive_expect_tx(q_full, NR * 128 * heads * cut.rows_each);
@@ -416,41 +446,50 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::tma_load_3d(qimg + 2 * h * kRegion, &tmQ, q_full, 64 * h, it.g * (a.nq / a.nkv) + it.h0, it.r0 + it.i_min,
                          ptx::policy_evict_first());
     };
-    if (t64 == 0 && s_item[0].cnt > 0) load_queries(s_item[0]);
-    uint32_t loaded = 1;
-    for (uint32_t n = 0;; ++n) {
-      it = s_item[n & 1];
-      if (it.cnt == 0) break;
-      // the results of the item before are read: so are its description and what was noted for it
-      if (n > 0) wait(o_empty, (n - 1) & 1);
-      if (warp == 2) {
-        const Item next = item_of_cta(a, cut, next_item, lane, parts);
-        if (lane == 0) s_item[(n + 1) & 1] = next;
+    if (lane == 0 && it.cnt > 0) load_queries(it);
+    uint32_t n = 0;  // items whose queries are on their way, or were
+    while (it.cnt > 0) {
+      it = item_of_cta(a, cut, next_item, lane, parts);
+      // this item's queries, when the last one's have been read.  (Its results are not written yet, but those of the one
+      // before are: who writes them has let go of the last one's queries.)
+      if (lane == 0 && wait(q_empty, n & 1)) {
+        s_item[(n + 1) % kItems] = it;
+        if (it.cnt > 0)
+          load_queries(it);
+        else
+          ptx::mbar_arrive(q_full);
       }
-      if (t64 < 4 * kMaxTails) s_bad[t64] = 0;
-      ptx::named_bar_sync(9, 64);
+      ok = __all_sync(~0u, ok);
+      if (!ok) break;
+      ++n;
+    }
+    // no copy is in flight when the CTA ends (q_empty says so of those that were waited for)
+    if (lane == 0 && !ok) ptx::mbar_wait(q_full, n & 1, ptx::kDrainNs);
+  } else if (warp == 3) {
+    uint32_t tiles = 0, turn = 0;
+    for (uint32_t n = 0; ok; ++n) {
+      if (n == 0 && s_item[0].cnt == 0) break;
+      wait(q_full, n & 1);
+      ok = __all_sync(~0u, ok);
+      it = s_item[n % kItems];
+      if (!ok || it.cnt == 0) break;
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(q_empty);
+      // (what was noted for the item before the last has been read)
+      uint32_t* bad = s_bad + (n & 1) * 4 * kMaxTails;
+      if (lane < 4 * kMaxTails) bad[lane] = 0;
+      __syncwarp();
       for (int t = max(it.tail0, 0); t < it.cnt; ++t) {
         const uint32_t s = (2 * (tiles + t) + 1) % NST;
         const bool here = wait(&tail_full[s], (turn >> s) & 1);
         turn ^= 1u << s;
         if (!here) continue;  // (nor is this one let go)
-        clean_tile<D>(ring + s * S::STAGE, (it.t0 + t) * 128, it.from, it.end, it.from, t64, s_bad);
+        clean_tile<D>(ring + s * S::STAGE, (it.t0 + t) * 128, it.from, it.end, it.from, lane, bad);
         ptx::fence_proxy_async_smem();
-        ptx::mbar_arrive(&v_clean[t - it.tail0]);
+        ptx::mbar_arrive(&v_clean[(n & 1) * kMaxTails + t - it.tail0]);
       }
       tiles += it.cnt;
-      // the next item's queries, when this one's have been read
-      if (t64 == 0 && wait(q_empty, n & 1)) {
-        if (s_item[(n + 1) & 1].cnt > 0) {
-          load_queries(s_item[(n + 1) & 1]);
-          ++loaded;
-        } else {
-          ptx::mbar_arrive(q_full);
-        }
-      }
     }
-    // no copy is in flight when the CTA ends (q_empty says so of those that were waited for)
-    if (t64 == 0 && tiles > 0 && !ok) ptx::mbar_wait(q_full, (loaded - 1) & 1, ptx::kDrainNs);
   } else {
     const int quad = warp & 3, t = (warp - 4) >> 2, row = 32 * quad + lane;
     const uint32_t tl = tmem + ((uint32_t)(32 * quad) << 16);
@@ -462,14 +501,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (n == 0 && s_item[0].cnt == 0) break;
       wait(q_full, n & 1);
       ok = __all_sync(~0u, ok);
-      const int cnt = s_item[n & 1].cnt;
+      const int cnt = s_item[n % kItems].cnt;
       if (!ok || cnt == 0) break;
-      const int tail0 = s_item[n & 1].tail0, nq = s_item[n & 1].nq, t0 = s_item[n & 1].t0;
+      const int tail0 = s_item[n % kItems].tail0, nq = s_item[n % kItems].nq, t0 = s_item[n % kItems].t0;
+      const int of_parity = n & 1;
       const bool some = nq > 128 * t;  // the tile has queries
       // the last entry that the row sees
-      const int last = s_item[n & 1].L + s_item[n & 1].i_min + divide_group(a, s_item[n & 1].h0 + min(128 * t + row, nq - 1));
+      const int last = s_item[n % kItems].L + s_item[n % kItems].i_min + divide_group(a, s_item[n % kItems].h0 + min(128 * t + row, nq - 1));
       // (a row that is no query's has what was in its place before, of no consequence)
       const bool live = 128 * t + row < nq;
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(q_empty);
       float m = live ? -INFINITY : 0.f, l = 0.f;
       bool fresh = __any_sync(~0u, live);  // a row has no reference yet
       if (some) {
@@ -562,20 +604,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         wait(&o_full[0], n & 1);  // (not an item ahead of the others)
       }
       for (int x = max(-tail0, 0); x < cnt - tail0; ++x) {
-        if (some) wait(&v_clean[x], (c_turn >> x) & 1);
-        c_turn ^= 1u << x;
+        const int bar = of_parity * kMaxTails + x;
+        if (some) wait(&v_clean[bar], (c_turn >> bar) & 1);
+        c_turn ^= 1u << bar;
       }
       ok = __all_sync(~0u, ok);
       ptx::tc_fence_after();
       if (some && ok) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        it = s_item[n & 1];
+        it = s_item[n % kItems];
         const int q = it.h0 + min(128 * t + row, nq - 1), of = divide_group(a, q), h = it.g * G + (q - of * G);
         const size_t at = (size_t)(it.r0 + it.i_min + of) * a.nq + h;
         bf16* out = (bf16*)a.out + at * D;
+        const uint32_t* bad = s_bad + of_parity * 4 * kMaxTails;
         uint32_t any = 0;
         if (cnt > tail0)
-          for (int x = 0; x < 4 * kMaxTails; ++x) any |= s_bad[x];
+          for (int x = 0; x < 4 * kMaxTails; ++x) any |= bad[x];
 #pragma unroll 1
         for (int d0 = 0; d0 < D; d0 += 32) {
           uint32_t o[32];
@@ -584,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (any) {
             // values that are not finite in entries that not every row sees: added where they are seen
             for (int x = 0; x < 4 * kMaxTails; ++x)
-              for (uint32_t left = s_bad[x]; left; left &= left - 1) {
+              for (uint32_t left = bad[x]; left; left &= left - 1) {
                 const int e = it.from + 32 * x + __ffs(left) - 1;
                 if (e > last) continue;
                 const bf16* u = a.v + (((size_t)it.b * a.nkv + it.g) * a.cap + e) * D + d0;
