@@ -754,7 +754,8 @@ as2d_status as2d_cache4_attention_workspace(const as2d_cache4* cache, int64_t* b
    32-bit ones as two parts (to 2^-22 of a query's largest dim, or nearer), and so do the
    weights p (to 2^-11 for bf16 queries, 2^-22 for 32-bit ones).  What a row does not
    see does not reach its result.  A query that is not finite, or a score of +inf, makes its
-   row NaN in out and lse. */
+   row NaN in out and lse.  What another max_len or other rows change is the order of sums
+   and what the weights are relative to before they are rounded. */
 as2d_status as2d_cache4_attention(const as2d_cache4* cache, int32_t layer,
                                   const as2d_tree_rows* rows, void* out, float* lse,
                                   void* workspace, int64_t workspace_bytes,
@@ -767,7 +768,8 @@ as2d_status as2d_prompt_attention_workspace(const as2d_cache* cache, int64_t* by
 /* Causal attention of whole prompts over one layer of a cache: as as2d_tree_attention
    with rows[b] up to the capacity, row i of request b seeing the entries 0 ..
    kv_len[b] + i; visible is NULL, out 32-byte aligned.  bf16 queries (others: AS2D_ERR_UNSUPPORTED); the
-   weights p enter the products in bf16, their sum in 32 bits.  What a row does not see does
+   weights p enter the products in bf16 (relative to what max_len and the other rows of the
+   call may change), their sum in 32 bits.  What a row does not see does
    not reach its result, whatever it holds; a value that it sees and that is not
    finite makes its dim not finite, and NaN or +inf among its scores the row NaN in out
    and lse.  At most 2^24 rows. */
