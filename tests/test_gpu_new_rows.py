@@ -537,6 +537,23 @@ def test_prompt_packed(lib, heads):
         check(x, *prompt(lib, x, layer=1, max_len=most), layer=1, p_rel=P_REL)
 
 
+@pytest.mark.parametrize("behind", [0.0, 1.0, math.nan])
+@pytest.mark.parametrize("heads", [(28, 4, 128), (8, 8, 64)])
+def test_prompt_many_short(lib, heads, behind):
+    """64 requests of a tile or two each, several to a CTA, with anything behind their entries."""
+    rng = np.random.default_rng(9)
+    lens = [int(t) for t in rng.integers(0, 200, 64) * rng.integers(0, 2, 64)]
+    rows = [int(t) for t in rng.integers(0, 90, 64)]
+    x = Prompt(heads, lens, rows)
+    for b, (n, r) in enumerate(zip(lens, rows)):
+        x.k[:, b, :, n + r:] = x.v[:, b, :, n + r:] = behind
+    out, lse = prompt(lib, x)
+    check(x, out, lse, p_rel=P_REL)
+    for most in (0, 1, 199):
+        again = prompt(lib, x, max_len=most)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
 def test_prompt_long(lib):
     x = Prompt((28, 4, 128), [0], [5000])
     check(x, *prompt(lib, x), p_rel=P_REL)
