@@ -10,7 +10,7 @@
 // as fit 256 queries (of more than 256 heads: 256 of a row).  An item is one (request, kv head,
 // pair); a CTA takes it through its key tiles of 128.  One CTA per SM takes the items in turn,
 // those of most key tiles first, back and forth over the CTAs (by the lengths on the device: eight
-// prompts of 1 to 2029 rows take 102 us in the order of their rows, 90 so).
+// prompts of 1 to 2029 rows take 102 us in the order of their rows, 87 so).
 //
 // Per CTA (12 warps, TMEM full: two score buffers, two accumulators):
 //   warp 0     loads key and value tiles by TMA through a ring of shared-memory stages;
@@ -53,6 +53,7 @@ constexpr float kMost = 8192.f;
 struct Cut {
   int rows_each, chunks;  // whole rows of an item, or items of a row
   int parts;              // of an item's key tiles; more than one where there are fewer items than SMs
+  int last;               // the round over the CTAs that has fewer items, or parts of them, than CTAs; -1: none
 };
 // Partial results of an item's parts; at most kSlots an SM, of parts of kPartTiles tiles at least (but
 // for requests shorter than the host's bound).
@@ -81,9 +82,9 @@ struct Shape {
 };
 
 // An item of all requests' in the order of their key tiles, most first, by a whole warp.  (No
-// tiles: there are no more.  Not inlined: two roles run it, once an item.)  A request's k-th item has (end of its last row + 127) / 128 tiles,
+// tiles: there are no more.)  A request's k-th item has (end of its last row + 127) / 128 tiles,
 // so that those with at least T need no list to be counted.
-static __device__ __noinline__ Item item_at(const TreeArgs& a, Cut cut, int64_t at, int lane) {
+__device__ __forceinline__ Item item_at(const TreeArgs& a, Cut cut, int64_t at, int lane) {
   const int G = a.nq / a.nkv;
   int L[2], rows[2], items[2], most = 0;
 #pragma unroll
@@ -159,12 +160,14 @@ static __device__ __noinline__ Item item_at(const TreeArgs& a, Cut cut, int64_t 
   return it;
 }
 
-// The n-th item, or part of one, of this CTA: back and forth over the CTAs; of parts, those without tiles
-// are passed by (n: the one after it).
-__device__ __forceinline__ Item item_of_cta(const TreeArgs& a, Cut cut, int& n, int lane, const Parts& parts) {
+// The n-th item, or part of one, of this CTA: back and forth over the CTAs, and the last ones, which not all CTAs have,
+// to those whose first was shortest (tiles, and 2.6 for each item, of the busiest CTA with the eight prompts: 47 without
+// that, 45 so, of 42.6 on average); of parts, those without tiles are passed by (n: the one after it).  Not inlined: two
+// roles run it, once an item.
+static __device__ __noinline__ Item item_of_cta(const TreeArgs& a, Cut cut, int& n, int lane, const Parts& parts) {
   const int ctas = gridDim.x, c = blockIdx.x;
   for (;;) {
-    const int64_t at = (int64_t)n * ctas + (n & 1 ? ctas - 1 - c : c);
+    const int64_t at = (int64_t)n * ctas + ((n & 1) || n == cut.last ? ctas - 1 - c : c);
     ++n;
     Item it = item_at(a, cut, at / cut.parts, lane);
     if (cut.parts == 1 || it.cnt == 0) return it;
@@ -773,7 +776,7 @@ size_t prompt_attention_workspace(int head_dim) {
 cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, int64_t max_keys, void* workspace,
                                     cudaStream_t st) {
   const int G = a.nq / a.nkv, sms = device_sms();
-  Cut cut = {std::max(1, 256 / G), (G + 255) / 256, 1};
+  Cut cut = {std::max(1, 256 / G), (G + 255) / 256, 1, -1};
   int64_t n = 0;
   for (int b = 0; b < a.rm.batch; ++b) {
     const int64_t r = a.rm.start[b + 1] - a.rm.start[b];
@@ -784,6 +787,8 @@ cudaError_t launch_prompt_attention(const TreeArgs& a, int head_dim, int64_t max
   // four tiles at least 42 / 26 / 22, of eight 42 / 29 / 24.
   const int64_t tiles = (max_keys + 127) / 128;
   if (n <= sms) cut.parts = (int)std::max<int64_t>(1, std::min<int64_t>((2 * n <= sms ? 1 : kSlots) * sms / n, tiles / kPartTiles));
+  const int64_t all = n * cut.parts, ctas = std::min<int64_t>(all, sms);
+  if (all % ctas != 0) cut.last = (int)(all / ctas);
   return head_dim == 128 ? launch<128>(a, cut, n, workspace, st) : launch<64>(a, cut, n, workspace, st);
 }
 
