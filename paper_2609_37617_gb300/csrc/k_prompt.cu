@@ -10,7 +10,7 @@
 // as fit 256 queries (of more than 256 heads: 256 of a row).  An item is one (request, kv head,
 // pair); a CTA takes it through its key tiles of 128.  One CTA per SM takes the items in turn,
 // those of most key tiles first, back and forth over the CTAs (by the lengths on the device: eight
-// prompts of 1 to 2029 rows take 102 us in the order of their rows, 87 so).
+// prompts of 1 to 2029 rows take 102 us in the order of their rows, 90 so).
 //
 // Per CTA (12 warps, TMEM full: two score buffers, two accumulators):
 //   warp 0     loads key and value tiles by TMA through a ring of shared-memory stages;
