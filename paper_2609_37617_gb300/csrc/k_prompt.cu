@@ -527,7 +527,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int seen = last + 1 - (t0 + j) * 128;  // entries of the tile that the row sees
           uint32_t p[64];
           float sum;
-          bool need = m == -INFINITY, again = fresh;
+          // looked: the row's reference may have been moved, and is what this tile gives
+          bool need = m == -INFINITY, again = fresh, looked = false;
 #pragma unroll 1
           for (;;) {
             if (again) {
@@ -559,6 +560,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
               }
               m = m_new;
+              looked = looked || need;
               fresh = __any_sync(~0u, m == -INFINITY);
             }
             const float ref = m == -INFINITY ? 0.f : m;
@@ -587,8 +589,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             const float2 sums = of_two(add2(ls[0], ls[1]));
             sum = sums.x + sums.y;
-            need = live && !(sum <= kMost);
-            if (again || !__any_sync(~0u, need)) break;
+            // (a pass for rows without a reference, of which NaN rows are never rid, was none for the others)
+            need = live && !looked && !(sum <= kMost);
+            if (!__any_sync(~0u, need)) break;
             again = true;
           }
 #pragma unroll
