@@ -48,6 +48,8 @@ constexpr int kMaxTails = 3;  // key tiles that not all rows of 256 queries see 
 constexpr int kItems = 4;
 // The sum of a tile's 128 weights that makes its maximum the reference.
 constexpr float kMost = 8192.f;
+// References from here on (base 2) are rounded by 32 and more (exponent_of); below, weights stay within 2^45.
+constexpr float kFar = 1073741824.f;
 
 // How queries are cut into items.
 struct Cut {
@@ -515,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool live = 128 * t + row < nq;
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(q_empty);
-      float m = live ? -INFINITY : 0.f, l = 0.f;
+      float ref = live ? -INFINITY : 0.f, l = 0.f;  // the reference, a score
       bool fresh = __any_sync(~0u, live);  // a row has no reference yet
       if (some) {
 #pragma unroll 1
@@ -528,6 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t p[64];
           float sum;
           // looked: the row's reference may have been moved, and is what this tile gives
+          float m = __fmul_rn(ref, c);
           bool need = m == -INFINITY, again = fresh, looked = false;
 #pragma unroll 1
           for (;;) {
@@ -543,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                   if (!tail || x + e < seen) mx[e & 1] = fmaxf(mx[e & 1], __uint_as_float(v[e]));
               }
               // (NaN scores pass the maximum by, and reach the sums)
-              const float mt = fmaxf(mx[0], mx[1]) * c;
+              const float top = fmaxf(mx[0], mx[1]), mt = __fmul_rn(top, c);
               // (a row whose sum is fine keeps its reference: what another row sees changes nothing for it)
               const bool grow = need && mt > m;
               const float m_new = grow ? mt : m, f = m == -INFINITY ? 0.f : ex2(m - m_new);
@@ -560,11 +563,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
               }
               m = m_new;
+              ref = grow ? top : ref;
               looked = looked || need;
               fresh = __any_sync(~0u, m == -INFINITY);
             }
-            const float ref = m == -INFINITY ? 0.f : m;
-            const uint64_t c2 = as2d::two(c, c), ref2 = as2d::two(-ref, -ref);
+            const Exponent x2 = exponent_of(ref, m, c, kFar);
+            const uint64_t c2 = as2d::two(x2.by, x2.by), ref2 = as2d::two(-x2.at, -x2.at);
             uint64_t ls[2] = {0, 0};
             uint32_t v[2][32];
             ptx::tmem_ld32(ts, v[0]);
@@ -617,7 +621,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = __all_sync(~0u, ok);
       ptx::tc_fence_after();
       if (some && ok) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float m = __fmul_rn(ref, c), inv = l == 0.f ? 0.f : 1.f / l;
         it = s_item[n % kItems];
         const int q = it.h0 + min(128 * t + row, nq - 1), of = divide_group(a, q), h = it.g * G + (q - of * G);
         const size_t at = (size_t)(it.r0 + it.i_min + of) * a.nq + h;

@@ -82,3 +82,66 @@ def test_prompt_references_jump_after_nothing(lib, lens, rows):
     assert torch.isnan(out[i, h]).all() and torch.isnan(lse[i, h])
     out[i, h], lse[i, h] = base[i, h], base_lse[i, h]
     assert same(out, base) and same(lse, base_lse)
+
+
+# ---- scores far from 1, and beyond 32 bits -----------------------------------------
+
+SIZES = (2.0 ** 18, 2.0 ** 24, 2.0 ** 28, 2.0 ** 34, 2.0 ** 60, 2.0 ** 120)
+
+
+def check_far(x, out, lse, p_rel):
+    """Where one score of a row is so far above the others that no rounding of sums (d products, each
+    addition off by 2^-23 of their magnitudes) can change that, the row is that entry's value, to its weight's
+    rounding p_rel."""
+    r0 = clear = 0
+    for b, r in enumerate(x.rows):
+        if not r:
+            continue
+        q, k, v, seen = x.request(b)
+        G = q.shape[1] // k.shape[0]
+        half_step = torch.finfo(out.dtype).eps / 2
+        for h in range(q.shape[1]):
+            s = (q[:, h] @ k[h // G].T * x.scale).masked_fill(~seen.to(q.device), -math.inf)
+            off = (q[:, h].abs() @ k[h // G].abs().T * x.scale).amax(-1) * q.shape[2] * 2.0 ** -22
+            top, at = s.topk(2, -1)
+            got, got_lse = out[r0:r0 + r, h].double(), lse[r0:r0 + r, h].double()
+            assert torch.isfinite(got).all() and torch.isfinite(got_lse).all()
+            assert ((got_lse - top[:, 0]).abs() <= off + math.log(s.shape[1])).all()
+            # (the others' weights together below 2^-30)
+            won = top[:, 0] - top[:, 1] > 2 * off + 21 + math.log(s.shape[1])
+            want = v[h // G][at[:, 0]]
+            over = (got - want).abs() - want.abs() * (half_step * (1 + 2.0 ** -6) + p_rel) - v.abs().max() * 2.0 ** -20
+            assert not won.any() or over[won].max() <= 0, float(over[won].max())
+            clear += int(won.sum())
+        r0 += r
+    assert clear * 2 > sum(x.rows) * q.shape[1]
+
+
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("lens,rows", [(0, 700), (6000, 40)])
+def test_prompt_scores_far(lib, lens, rows, size):
+    x = rows_of.Prompt((28, 4, 128), [lens], [rows])
+    x.scale = size
+    check_far(x, *rows_of.prompt(lib, x), rows_of.P_REL)
+
+
+@pytest.mark.parametrize("lens,rows", [(0, 1300), (300, 200), (6000, 40)])
+def test_prompt_scores_beyond_32_bits(lib, lens, rows):
+    """Finite queries and keys whose product is finite and whose score is not: +inf makes the row NaN, -inf
+    is a weight of 0; in the first key tile and in a later one."""
+    for at in (3, lens + rows // 2 - 20):
+        x = rows_of.Prompt((28, 4, 128), [lens], [rows])
+        x.scale = 2.0
+        x.k[0, 0, :, at, 7] = 2.0 ** 64
+        base, base_lse = rows_of.prompt(lib, x)
+        assert torch.isfinite(base).all() and torch.isfinite(base_lse).all()
+        i, h = rows - 1, 9
+        x.q[i, h] = 0
+        x.q[i, h, 7] = 2.0 ** 63
+        out, lse = rows_of.prompt(lib, x)
+        assert torch.isnan(out[i, h]).all() and torch.isnan(lse[i, h])
+        out[i, h], lse[i, h] = base[i, h], base_lse[i, h]
+        assert same(out, base) and same(lse, base_lse)
+        x.q[i, h, 7] = -2.0 ** 63
+        out, lse = rows_of.prompt(lib, x)
+        assert torch.isfinite(out[i, h]).all() and torch.isfinite(lse[i, h])
