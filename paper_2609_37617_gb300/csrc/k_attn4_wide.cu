@@ -34,6 +34,8 @@ namespace {
 
 constexpr int kThreads = 512, kLoaders = 7, kIssuer = 15;  // warps 8 .. 14 load, kIssuer issues
 constexpr float kLazy = 8.f, kUp = 7.f;
+// References from here on (base 2) are rounded by 1 and more (exponent_of); below, weights stay within 2^15.5.
+constexpr float kFar = 16777216.f;
 // What turning to another item costs a CTA, in tiles.  us with 2 / 3 / 5: 16 requests of 126 32-bit queries over 500 entries
 // 18.5 / 20.0 / 23.3, over 4000 42.6 / 40.8 / 42.0, the ragged ones 41.2 / 37.9 / 38.9.
 constexpr int kTurn = 3;
@@ -341,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int q = it.qt * 128 + row, i = divide_group(a, q), h = it.g * G + (q - i * G);
       uint64_t vis = 0;
       if (live && it.t1 > it.L / 128) vis = visible_rows(a, it.r0 + i, i, it.rows);
-      float m = -INFINITY, l = 0.f;
+      float ref = -INFINITY, l = 0.f;  // the reference, a score
 #pragma unroll 1
       for (int j = set; j < cnt; j += 2, ++turns) {
         wait(&s_full[set], turns & 1);
@@ -371,9 +373,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           if (tail) ptx::tmem_st_wait();
-          const float mt = fmaxf(mx[0], mx[1]) * c;
-          // (NaN scores pass the maximum by, and reach the sums)
-          const bool grow = mt > m + kLazy;
+          const float top = fmaxf(mx[0], mx[1]), mt = __fmul_rn(top, c);
+          float m = __fmul_rn(ref, c);
+          // (NaN scores pass the maximum by, and reach the sums; beside a far reference nothing greater is left)
+          const bool grow = mt > m + kLazy || (fmaxf(fabsf(m), fabsf(mt)) >= kFar && mt > -INFINITY && top > ref);
           if (__any_sync(~0u, grow)) {
             const float m_new = grow ? mt : m, f = m == -INFINITY ? 0.f : ex2(m - m_new);
             l = grow ? l * f : l;
@@ -389,9 +392,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
             m = m_new;
+            ref = grow ? top : ref;
           }
-          const float ref = (m == -INFINITY ? 0.f : m) - kUp;
-          const uint64_t c2 = two(c, c), ref2 = two(-ref, -ref);
+          const Exponent x2 = exponent_of(ref, m, c, kFar);
+          const float at = x2.at - kUp;
+          const uint64_t c2 = two(x2.by, x2.by), ref2 = two(-at, -at);
           uint64_t ls[2] = {0, 0};
           // P: of each 16 keys the weights' first parts, then the second ones
 #pragma unroll 1
@@ -433,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       wait(o_full, items & 1);
       ok = __all_sync(~0u, ok);
       ptx::tc_fence_after();
-      s_ml[set * 128 + row] = make_float2(m, l);
+      s_ml[set * 128 + row] = make_float2(__fmul_rn(ref, c), l);
       ptx::named_bar_sync(1, 256);
       const float m0 = s_ml[row].x, m1 = s_ml[128 + row].x;
       const float M = fmaxf(m0, m1), w0 = part_weight(m0, M), w1 = part_weight(m1, M);
@@ -464,11 +469,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
         if (live && set == 0) {
-          const float ref = M - kUp;  // (what the sums are relative to)
+          const float to_sum = M - kUp;  // (what the sums are relative to)
           if (!done)
-            ws.ml[part * 128 + row] = make_float2(ref, lt);
+            ws.ml[part * 128 + row] = make_float2(to_sum, lt);
           else if (a.lse)
-            a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(ref, lt);
+            a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(to_sum, lt);
         }
       }
       ptx::tc_fence_before();

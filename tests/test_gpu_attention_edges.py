@@ -145,3 +145,34 @@ def test_prompt_scores_beyond_32_bits(lib, lens, rows):
         x.q[i, h, 7] = -2.0 ** 63
         out, lse = rows_of.prompt(lib, x)
         assert torch.isfinite(out[i, h]).all() and torch.isfinite(lse[i, h])
+
+
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+def test_attention4_scores_far(lib, q_type, size):
+    """Few queries together, many (in a large cache), and many cut between CTAs."""
+    for kind, lens, rows in ((rows_of.Inputs, [400], [5]), (rows_of.Roomy, [400], [19]),
+                             (rows_of.Inputs, [5000, 40], [64, 3])):
+        x = kind((28, 4, 128), lens, rows, trees.chain_masks(rows), q_type)
+        x.scale = size
+        check_far(x, *rows_of.attend4(lib, x), 2.0 ** -11)
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("heads,length,large", [((4, 2, 64), 400, False), ((28, 4, 128), 400, False),
+                                                ((28, 4, 128), 400, True), ((8, 8, 64), 400, True)])
+def test_attention4_scores_beyond_32_bits(lib, heads, length, large, q_type):
+    """Over a cache in 4 bits a finite query with scores of +inf gives NaN, whether few queries are taken
+    together or (in a large cache) many."""
+    rows = 19 if large else 5
+    x = (rows_of.Roomy if large else rows_of.Inputs)(heads, [length], [rows], trees.chain_masks([rows]), q_type)
+    x.scale = 1.0
+    base, base_lse = rows_of.attend4(lib, x)
+    i, h = rows - 2, 3
+    for at in (0, 3):  # (3: four times as large as other dims)
+        x.q[i, h] = 0
+        x.q[i, h, at] = 1.5 * 2.0 ** 127
+        out, lse = rows_of.attend4(lib, x)
+        assert torch.isnan(out[i, h]).all() and torch.isnan(lse[i, h])
+        out[i, h], lse[i, h] = base[i, h], base_lse[i, h]
+        assert same(out, base) and same(lse, base_lse)
