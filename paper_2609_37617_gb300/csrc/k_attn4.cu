@@ -32,8 +32,9 @@ namespace as2d {
 namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
-// P may grow to 2^kLazy of its reference before sums are rescaled; a reference stands for 2^kUp
-// (the weights, at most 2^(kLazy + kUp), use the range of 16-bit floats).
+// P may grow to less than 2^kLazy of its reference before sums are rescaled; a reference stands for 2^kUp
+// (the weights, less than 2^(kLazy + kUp), use the range of 16-bit floats; where a score's last place is 2 or 4
+// that is 2^14 or less beside a reference for 2^8, as scores of 2^kLazy more do not stay).
 constexpr float kLazy = 8.f, kUp = 7.f;
 
 // Queries of the partial results of an SM's CTAs: two of 8, or one of 16, two parts each.
@@ -344,7 +345,7 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       most[nt][e] = fmaxf(s[nt][e], s[nt][2 + e]);
-      grow = grow || most[nt][e] > x.m[nt][e] + kLazy;
+      grow = grow || most[nt][e] - x.m[nt][e] >= kLazy;
     }
   if (__any_sync(~0u, grow)) {
 #pragma unroll
@@ -355,7 +356,7 @@ __device__ __forceinline__ void attend(const TreeArgs& a, const Unit& it, const 
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) now = fmaxf(now, __shfl_xor_sync(~0u, now, o));
         const float m = x.m[nt][e];
-        if (now > m + kLazy) {
+        if (now - m >= kLazy) {
           const float f = m == -INFINITY ? 0.f : ex2(m - now);
           x.m[nt][e] = now;
           x.l[nt][e] *= f;

@@ -176,3 +176,30 @@ def test_attention4_scores_beyond_32_bits(lib, heads, length, large, q_type):
         assert torch.isnan(out[i, h]).all() and torch.isnan(lse[i, h])
         out[i, h], lse[i, h] = base[i, h], base_lse[i, h]
         assert same(out, base) and same(lse, base_lse)
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("heads,rows,large", [((4, 2, 64), 1, False), ((4, 2, 64), 5, False), ((28, 4, 128), 19, True)])
+@pytest.mark.parametrize("level", [0, 2 ** 10, 2 ** 24])
+def test_attention4_weights_at_their_limit(lib, heads, rows, large, q_type, level):
+    """Scores (base 2, exact) that rise by just 8 from one key tile to the next, which a weight's range has
+    room for: beside references that are rounded too."""
+    n = 200
+    x = (rows_of.Roomy if large else rows_of.Inputs)(heads, [n], [rows], trees.chain_masks([rows]), q_type)
+    k = torch.zeros((n + rows, heads[2]), dtype=torch.float64, device="cuda")
+    k[:, 0] = k[:, 16] = k[128:, 32] = 4.0
+    k[:, 1] = k[:, 17] = k[:, 33] = 7.0  # (the scales: 1)
+    for c, packed in zip(x.c4[:2], ref.pack(k)):
+        c[0, 0, :, :n + rows] = packed
+    x.q.zero_()
+    x.q[..., 0], x.q[..., 16], x.q[..., 32] = level / 4, 16.0, 2.0
+    x.scale = math.log(2.0)
+    out, lse = rows_of.attend4(lib, x)
+    half_step = torch.finfo(q_type).eps / 2
+    _, _, v, seen = x.request(0)
+    w = torch.where(torch.arange(n + rows, device="cuda") < 128, 1.0, 256.0).double() * seen.to("cuda")
+    want = torch.einsum("it,gtd->igd", w / w.sum(-1, keepdim=True), v).repeat_interleave(heads[0] // heads[1], 1)
+    # (a weight's rounding; the scale's base 2 is 1 to 2^-23, of scores that differ by 8)
+    assert ((out.double() - want).abs() <= want.abs() * half_step * (1 + 2.0 ** -6) + v.abs().max() * 2.0 ** -10).all()
+    want_lse = (level + 64 + w.sum(-1).log2()) * math.log(2.0)
+    assert ((lse.double() - want_lse[:, None]).abs() <= want_lse[:, None] * 2.0 ** -21 + 2.0 ** -12).all()
