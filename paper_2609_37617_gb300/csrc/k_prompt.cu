@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               // (NaN scores pass the maximum by, and reach the sums)
               const float top = fmaxf(mx[0], mx[1]), mt = __fmul_rn(top, c);
               // (a row whose sum is fine keeps its reference: what another row sees changes nothing for it)
-              const bool grow = need && mt > m;
+              const bool grow = need && top > ref && mt > -INFINITY;
               const float m_new = grow ? mt : m, f = m == -INFINITY ? 0.f : ex2(m - m_new);
               l = grow ? l * f : l;
               if (j > 0) {

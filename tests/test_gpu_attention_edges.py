@@ -147,6 +147,40 @@ def test_prompt_scores_beyond_32_bits(lib, lens, rows):
         assert torch.isfinite(out[i, h]).all() and torch.isfinite(lse[i, h])
 
 
+def next_to_each_other(x, n):
+    """Scores 3 2^60 + j 2^38, and from the second key tile on the next one in 32 bits, with a j at which the
+    scale (1, in base 2) rounds both to the same number.  (Sums of products no larger than half of
+    them, so that none of their bits are cut off.)"""
+    c = torch.tensor(1.0) * 1.4426950408889634
+    j = next(j for j in range(128) if len({float(torch.tensor(3 * 2.0 ** 60 + i * 2.0 ** 38) * c) for i in (j, j + 1)}) == 1)
+    x.q.zero_()
+    x.q[..., :4], x.q[..., 4:6] = 1.5 * 2.0 ** 29, 2.0 ** 18
+    k = x.k[0, 0, :, :n]
+    k.zero_()
+    k[..., :4], k[..., 4], k[:, 128:, 5] = 2.0 ** 30, j * 2.0 ** 20, 2.0 ** 20
+
+
+def check_next_to_each_other(x, out, lse):
+    """Results are means of what the rows see, whichever of the two scores' entries they are of."""
+    _, _, v, seen = x.request(0)
+    G = out.shape[1] // v.shape[0]
+    for g in range(v.shape[0]):
+        for i in range(len(out)):
+            values = v[g][seen[i].to(v.device)]
+            low, high = values.amin(0), values.amax(0)
+            got, room = out[i, g * G:(g + 1) * G].double(), 2.0 ** -7 * values.abs().amax(0)
+            assert ((got >= low - room) & (got <= high + room)).all()
+    assert ((lse.double() / (3 * 2.0 ** 60) - 1).abs() < 2.0 ** -15).all()
+
+
+@pytest.mark.parametrize("lens,rows", [(0, 300), (6000, 40)])
+def test_prompt_scores_next_to_each_other(lib, lens, rows):
+    x = rows_of.Prompt((28, 4, 128), [lens], [rows])
+    next_to_each_other(x, lens + rows)
+    x.scale = 1.0
+    check_next_to_each_other(x, *rows_of.prompt(lib, x))
+
+
 @pytest.mark.parametrize("size", SIZES)
 @pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
 def test_attention4_scores_far(lib, q_type, size):
