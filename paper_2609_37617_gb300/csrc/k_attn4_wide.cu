@@ -34,8 +34,9 @@ namespace {
 
 constexpr int kThreads = 512, kLoaders = 7, kIssuer = 15;  // warps 8 .. 14 load, kIssuer issues
 constexpr float kLazy = 8.f, kUp = 7.f;
-// References from here on (base 2) are rounded by 1 and more (exponent_of); below, weights stay within 2^15.5.
-constexpr float kFar = 16777216.f;
+// References from here on (base 2) are rounded by a half and more (exponent_of), as they are less kUp; below, weights
+// stay within 2^15.75.
+constexpr float kFar = 8388608.f;
 // What turning to another item costs a CTA, in tiles.  us with 2 / 3 / 5: 16 requests of 126 32-bit queries over 500 entries
 // 18.5 / 20.0 / 23.3, over 4000 42.6 / 40.8 / 42.0, the ragged ones 41.2 / 37.9 / 38.9.
 constexpr int kTurn = 3;
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       wait(o_full, items & 1);
       ok = __all_sync(~0u, ok);
       ptx::tc_fence_after();
-      s_ml[set * 128 + row] = make_float2(__fmul_rn(ref, c), l);
+      s_ml[set * 128 + row] = make_float2(__fmul_rn(ref, c) - kUp, l);  // (what the sum is relative to)
       ptx::named_bar_sync(1, 256);
       const float m0 = s_ml[row].x, m1 = s_ml[128 + row].x;
       const float M = fmaxf(m0, m1), w0 = part_weight(m0, M), w1 = part_weight(m1, M);
@@ -469,11 +470,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
         if (live && set == 0) {
-          const float to_sum = M - kUp;  // (what the sums are relative to)
           if (!done)
-            ws.ml[part * 128 + row] = make_float2(to_sum, lt);
+            ws.ml[part * 128 + row] = make_float2(M, lt);
           else if (a.lse)
-            a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(to_sum, lt);
+            a.lse[(size_t)(it.r0 + i) * a.nq + h] = row_lse(M, lt);
         }
       }
       ptx::tc_fence_before();

@@ -213,27 +213,31 @@ def test_attention4_scores_beyond_32_bits(lib, heads, length, large, q_type):
 
 
 @pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("heads,rows,large", [((4, 2, 64), 1, False), ((4, 2, 64), 5, False), ((28, 4, 128), 19, True)])
-@pytest.mark.parametrize("level", [0, 2 ** 10, 2 ** 24])
-def test_attention4_weights_at_their_limit(lib, heads, rows, large, q_type, level):
-    """Scores (base 2, exact) that rise by just 8 from one key tile to the next, which a weight's range has
-    room for: beside references that are rounded too."""
-    n = 200
-    x = (rows_of.Roomy if large else rows_of.Inputs)(heads, [n], [rows], trees.chain_masks([rows]), q_type)
-    k = torch.zeros((n + rows, heads[2]), dtype=torch.float64, device="cuda")
-    k[:, 0] = k[:, 16] = k[128:, 32] = 4.0
+@pytest.mark.parametrize("heads,lens,rows,jump", [((4, 2, 64), [200], [1], 128), ((4, 2, 64), [200], [5], 128),
+                                                  ((28, 4, 128), [900] * 16, [19] * 16, 512)])
+@pytest.mark.parametrize("level,more", [(0, 64), (2 ** 10, 64), (2 ** 24, 64), (-2 ** 24, 4)])
+def test_attention4_weights_at_their_limit(lib, heads, lens, rows, jump, q_type, level, more):
+    """Scores (base 2, exact) that rise by just 8 from one of a warp's key tiles to a later one, which a
+    weight's range has room for: beside references that are rounded too.  Few queries together, and many."""
+    x = rows_of.Inputs(heads, lens, rows, trees.chain_masks(rows), q_type)
+    n = lens[0] + rows[0]
+    k = torch.zeros((n, heads[2]), dtype=torch.float64, device="cuda")
+    k[:, 0] = k[:, 16] = k[jump:, 32] = 4.0
     k[:, 1] = k[:, 17] = k[:, 33] = 7.0  # (the scales: 1)
     for c, packed in zip(x.c4[:2], ref.pack(k)):
-        c[0, 0, :, :n + rows] = packed
+        c[0, :, :, :n] = packed
     x.q.zero_()
-    x.q[..., 0], x.q[..., 16], x.q[..., 32] = level / 4, 16.0, 2.0
+    x.q[..., 0], x.q[..., 16], x.q[..., 32] = level / 4, more / 4, 2.0
     x.scale = math.log(2.0)
     out, lse = rows_of.attend4(lib, x)
     half_step = torch.finfo(q_type).eps / 2
-    _, _, v, seen = x.request(0)
-    w = torch.where(torch.arange(n + rows, device="cuda") < 128, 1.0, 256.0).double() * seen.to("cuda")
-    want = torch.einsum("it,gtd->igd", w / w.sum(-1, keepdim=True), v).repeat_interleave(heads[0] // heads[1], 1)
-    # (a weight's rounding; the scale's base 2 is 1 to 2^-23, of scores that differ by 8)
-    assert ((out.double() - want).abs() <= want.abs() * half_step * (1 + 2.0 ** -6) + v.abs().max() * 2.0 ** -10).all()
-    want_lse = (level + 64 + w.sum(-1).log2()) * math.log(2.0)
-    assert ((lse.double() - want_lse[:, None]).abs() <= want_lse[:, None] * 2.0 ** -21 + 2.0 ** -12).all()
+    for b in range(len(lens)):
+        sl = slice(x.starts[b], x.starts[b + 1])
+        _, _, v, seen = x.request(b)
+        w = torch.where(torch.arange(n, device="cuda") < jump, 1.0, 256.0).double() * seen.to("cuda")
+        want = torch.einsum("it,gtd->igd", w / w.sum(-1, keepdim=True), v).repeat_interleave(heads[0] // heads[1], 1)
+        # (a weight's rounding; the scale's base 2 is 1 to 2^-23, of scores that differ by 8)
+        room = want.abs() * half_step * (1 + 2.0 ** -6) + v.abs().max() * 2.0 ** -10
+        assert ((out[sl].double() - want).abs() <= room).all()
+        want_lse = (level + more + w.sum(-1).log2()) * math.log(2.0)
+        assert ((lse[sl].double() - want_lse[:, None]).abs() <= want_lse[:, None].abs() * 2.0 ** -21 + 2.0 ** -12).all()
