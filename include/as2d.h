@@ -586,7 +586,8 @@ as2d_status as2d_tree_attention_workspace(const as2d_cache* cache, int64_t* byte
    its result, whatever it holds (NaN and infinities among it).  What it sees
    does as the formula has it: an infinite value makes its dim that infinity
    (values of both: NaN), a score of -inf is a weight of 0, and NaN or a score of +inf
-   makes the row NaN in out and lse.
+   makes the row NaN in out and lse (scores are held as multiples of ln 2 too: beyond
+   32 bits so, they are infinite).
    A request whose kv_len[b] is negative or leaves no room for its rows in the
    capacity is skipped: its rows of out and lse stay as they were and
    AS2D_DEVERR_CAPACITY is ORed into error_bits (device int32 [1], set to 0 by

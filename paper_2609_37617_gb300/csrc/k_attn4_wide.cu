@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             m = m_new;
             ref = grow ? top : ref;
           }
-          const Exponent x2 = exponent_of(ref, m, c, kFar);
+          const Exponent x2 = exponent_of([&] { return ref; }, m, c, kFar);
           const float at = x2.at - kUp;
           const uint64_t c2 = two(x2.by, x2.by), ref2 = two(-at, -at);
           uint64_t ls[2] = {0, 0};

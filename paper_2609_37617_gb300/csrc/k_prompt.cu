@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               looked = looked || need;
               fresh = __any_sync(~0u, m == -INFINITY);
             }
-            const Exponent x2 = exponent_of(ref, m, c, kFar);
+            const Exponent x2 = exponent_of([&] { return ref; }, m, c, kFar);
             const uint64_t c2 = as2d::two(x2.by, x2.by), ref2 = as2d::two(-x2.at, -x2.at);
             uint64_t ls[2] = {0, 0};
             uint32_t v[2][32];

@@ -67,6 +67,8 @@ constexpr int kThreads = 640;
 constexpr int kTurn = 5;
 // P may grow to 2^kLazy before the accumulator is rescaled.
 constexpr float kLazy = 8.f;
+// References from here on (base 2) are rounded by 32 and more (exponent_of); below, weights stay within 2^41.
+constexpr float kFar = 1073741824.f;
 
 // How the items go over the CTAs.
 enum Mode : int {
@@ -82,7 +84,7 @@ struct Shape {
   static constexpr uint32_t Q = (F32 ? 2 : 1) * 128 * D * 2;  // hi (and lo) image
   static constexpr int NST = D == 64 ? 8 : F32 ? 4 : 5;
   static constexpr uint32_t SMEM =
-      1024 + Q + NST * STAGE + 4 * 128 * 8 + 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16 + 2 * sizeof(Unit);
+      1024 + Q + NST * STAGE + 4 * 128 * 8 + 2 * 4 * 128 * 4 + (3 * NST + 12) * 8 + 8 + 16 + 2 * sizeof(Unit);
   static_assert(SMEM + sizeof(UnitPlan) + sizeof(First) <= 232448, "shared memory of one CTA");
 };
 
@@ -261,7 +263,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   float2* recv_ml = reinterpret_cast<float2*>(recv + kRanks * kQuads * 128);  // [rank][128]
   float2* s_ml = reinterpret_cast<float2*>(ring + NST * S::STAGE);  // [4 groups][128] (maximum, sum)
   float* s_mx = reinterpret_cast<float*>(s_ml + 4 * 128);           // [4 groups][128] a tile's maxima
-  uint64_t* full = reinterpret_cast<uint64_t*>(s_mx + 4 * 128);
+  float* s_ref = s_mx + 4 * 128;                                    // [4 groups][128] the scores that references are of
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_ref + 4 * 128);
   uint64_t* empty = full + NST;
   uint64_t* tail_full = empty + NST;  // in full's place for value tiles that clean_tile prepares
   uint64_t* q_full = tail_full + NST;
@@ -557,7 +560,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float mine = fmaxf(mx[0], mx[1]);
           s_mx[group * 128 + row] = mine;
           ptx::named_bar_sync(3 + 4 * set + quad, 64);
-          const float mt = fmaxf(mine, s_mx[(group ^ 2) * 128 + row]) * c;
+          const float top = fmaxf(mine, s_mx[(group ^ 2) * 128 + row]), mt = top * c;
           // (NaN scores pass the maximum by, and reach the sums)
           const bool grow = mt > m + kLazy || (m == -INFINITY && mt > m);
           if (__any_sync(~0u, grow)) {
@@ -576,9 +579,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
             m = m_new;
+            if (grow) s_ref[group * 128 + row] = top;
           }
-          const float ref = m == -INFINITY ? 0.f : m;
-          const uint64_t c2 = two(c, c), ref2 = two(-ref, -ref), less = two(-1.f, -1.f);
+          // (a greater score that did not move m has the same product with c)
+          const Exponent x2 = exponent_of([&] { return fmaxf(s_ref[group * 128 + row], top); }, m, c, kFar);
+          const uint64_t c2 = two(x2.by, x2.by), ref2 = two(-x2.at, -x2.at), less = two(-1.f, -1.f);
           uint64_t ls[2] = {0, 0};
           // P: of each 16 keys the hi parts, then the lo parts, in the place of
           // their scores (which are read a second time: they do not fit the
@@ -608,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             place(i, h);
             more = mend_weights<D>(ts, live && more != more,
                                    (const float*)a.q + (it.r0 + i) * a.q_stride + (int64_t)h * D,
-                                   a.k + (((size_t)it.b * a.nkv + it.g) * a.cap + p0) * D, c, ref, more);
+                                   a.k + (((size_t)it.b * a.nkv + it.g) * a.cap + p0) * D, c, m == -INFINITY ? 0.f : m, more);
           }
           l += more;
           ptx::tmem_st_wait();

@@ -122,15 +122,16 @@ __device__ __forceinline__ float part_weight(float m, float M) {
 // rounded product of c and the reference r (a score; m -inf: none), as long as m is off by little.  From
 // `far` on its rounding would be a factor of 2 and more of every weight, up to infinity, so r is multiplied by
 // c's power of two, exactly: there scores next to each other in 32 bits are as far apart as a row's largest and
-// nothing.  NaN for m = +inf, a score of more than 32 bits.
+// nothing.  NaN for m = +inf, a score of more than 32 bits.  (r(): called where it is needed.)
 struct Exponent {
   float by, at;
 };
-__device__ __forceinline__ Exponent exponent_of(float r, float m, float c, float far) {
+template <typename R>
+__device__ __forceinline__ Exponent exponent_of(R r, float m, float c, float far) {
   Exponent x = {c, m == -INFINITY ? 0.f : m};
   if (fabsf(x.at) >= far) {
     x.by = __uint_as_float(__float_as_uint(c) & 0x7F800000u);
-    x.at = m == INFINITY ? NAN : __fmul_rn(r, x.by);
+    x.at = m == INFINITY ? NAN : __fmul_rn(r(), x.by);
   }
   return x;
 }

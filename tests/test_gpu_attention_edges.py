@@ -241,3 +241,43 @@ def test_attention4_weights_at_their_limit(lib, heads, lens, rows, jump, q_type,
         assert ((out[sl].double() - want).abs() <= room).all()
         want_lse = (level + more + w.sum(-1).log2()) * math.log(2.0)
         assert ((lse[sl].double() - want_lse[:, None]).abs() <= want_lse[:, None].abs() * 2.0 ** -21 + 2.0 ** -12).all()
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("size", SIZES)
+def test_tree_attention_scores_far(lib, size, q_type):
+    """The same over a cache in bf16: items done whole, by clusters and by even shares.  (32-bit queries
+    enter the products to 2^-17 of themselves.)"""
+    for lens, rows in (([200], [5]), ([3000], [5]), ([5000, 40], [64, 3])):
+        x = operators.Inputs((28, 4, 128), lens, rows, trees.chain_masks(rows), q_type)
+        x.scale = size
+        check_far(x, *operators.run_attention(lib, x, scale=size), 2.0 ** -16)
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("length", [300, 3000])
+def test_tree_attention_scores_next_to_each_other(lib, length, q_type):
+    x = operators.Inputs((28, 4, 128), [length], [5], trees.chain_masks([5]), q_type)
+    next_to_each_other(x, length + 5)
+    check_next_to_each_other(x, *operators.run_attention(lib, x, scale=1.0))
+
+
+@pytest.mark.parametrize("q_type", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("length", [200, 3000, 15128])
+def test_tree_attention_scores_beyond_32_bits(lib, length, q_type):
+    """The same over a cache in bf16: items done whole, by clusters and by even shares."""
+    lens, rows = ([length], [5]) if length < 15128 else ([length, 40], [64, 3])
+    x = operators.Inputs((28, 4, 128), lens, rows, trees.chain_masks(rows), q_type)
+    for at in (3, length + 1):
+        kept = x.k[0, 0, :, at, 7].clone()
+        x.k[0, 0, :, at, 7] = 2.0 ** 64
+        x.q[3, 9] = 1.0
+        base, base_lse = operators.run_attention(lib, x, scale=2.0)
+        assert torch.isfinite(base).all() and torch.isfinite(base_lse).all()
+        x.q[3, 9] = 0
+        x.q[3, 9, 7] = 2.0 ** 63
+        out, lse = operators.run_attention(lib, x, scale=2.0)
+        assert torch.isnan(out[3, 9]).all() and torch.isnan(lse[3, 9])
+        out[3, 9], lse[3, 9] = base[3, 9], base_lse[3, 9]
+        assert same(out, base) and same(lse, base_lse)
+        x.k[0, 0, :, at, 7] = kept
