@@ -299,8 +299,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 64) s_item[0] = it;
   if (warp == 3 && blockIdx.x == 0) {
     bool over = false;
-    for (int b = lane; b < a.rm.batch; b += 32)
-      over = over || !rows_fit(a.len[b], a.rm.start[b + 1] - a.rm.start[b], a.cap);
+    for (int b = lane; b < a.rm.batch; b += 32) {
+      const int rows = a.rm.start[b + 1] - a.rm.start[b];
+      over = over || (rows > 0 && !rows_fit(a.len[b], rows, a.cap));
+    }
     if (__any_sync(~0u, over) && lane == 0 && a.err) atomicOr(a.err, kErrCapacity);
   }
   ptx::tc_fence_before();

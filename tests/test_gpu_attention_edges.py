@@ -281,3 +281,26 @@ def test_tree_attention_scores_beyond_32_bits(lib, length, q_type):
         out[3, 9], lse[3, 9] = base[3, 9], base_lse[3, 9]
         assert same(out, base) and same(lse, base_lse)
         x.k[0, 0, :, at, 7] = kept
+
+
+# ---- requests without rows --------------------------------------------------------
+
+@pytest.mark.parametrize("bad", [-1, 2 ** 31 - 1, -2 ** 31])
+def test_lengths_of_requests_without_rows(lib, bad):
+    """The length of a request that has no rows in a call is not looked at: nothing is flagged."""
+    x = rows_of.Prompt((4, 2, 64), [100, 20, 7], [60, 0, 5])
+    base, base_lse = rows_of.prompt(lib, x)
+    t = rows_of.Inputs((4, 2, 64), [100, 20, 7], [6, 0, 5], trees.chain_masks([6, 0, 5]))
+    base4, base4_lse = rows_of.attend4(lib, t)
+    x.kv_len[1] = t.kv_len[1] = bad
+    err = rows_of.ints([0])
+    out, lse = rows_of.prompt(lib, x, error_bits=err)
+    assert err.item() == 0 and same(out, base) and same(lse, base_lse)
+    out, lse = rows_of.attend4(lib, t, error_bits=err)
+    assert err.item() == 0 and same(out, base4) and same(lse, base4_lse)
+    cache = lib.Cache(x.k, x.v)
+    cache.tree_attention(x.q[:11].contiguous(), x.kv_len, [6, 0, 5], error_bits=err)
+    new = torch.randn((11, 8, 64), device="cuda").bfloat16()
+    cache.append(new[:, :4], new[:, 4:6], new[:, 6:], x.kv_len, [6, 0, 5], error_bits=err)
+    lib.Cache4(*t.c4).append(new[:, :4], new[:, 4:6], new[:, 6:], t.kv_len, [6, 0, 5], error_bits=err)
+    assert err.item() == 0
