@@ -488,9 +488,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       for (int t = max(it.tail0, 0); t < it.cnt; ++t) {
         const uint32_t s = (2 * (tiles + t) + 1) % NST;
-        const bool here = wait(&tail_full[s], (turn >> s) & 1);
+        // (what follows is done by the whole warp, or by none of it; nor is a tile let go that did not come)
+        ok = __all_sync(~0u, wait(&tail_full[s], (turn >> s) & 1));
         turn ^= 1u << s;
-        if (!here) continue;  // (nor is this one let go)
+        if (!ok) break;
         clean_tile<D>(ring + s * S::STAGE, (it.t0 + t) * 128, it.from, it.end, it.from, lane, bad);
         ptx::fence_proxy_async_smem();
         ptx::mbar_arrive(&v_clean[(n & 1) * kMaxTails + t - it.tail0]);
