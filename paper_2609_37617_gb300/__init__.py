@@ -874,16 +874,18 @@ class _CacheCalls:
             ctypes.addressof(host_rows), visible or 0, d ** -0.5 if scale is None else scale)
         return r, host_rows  # (which the descriptor points to)
 
-    def _attention(self, name, q, kv_len, rows, visible, scale, layer, max_len, out, lse, error_bits, stream):
+    def _attention(self, name, q, kv_len, rows, visible, scale, layer, max_len, out, lse, error_bits, stream,
+                   space=None):
         device, current, stream = self._enter(stream)
         r, keep = self._rows(device, q, kv_len, rows, visible, scale, layer, max_len)
         shape = q.shape
         if out is None:
             out = q.new_empty(shape) if stream == current else _new_on(stream, device, q, shape)
+        workspace = self._workspace if space is None else space(device, current, stream)
         st = getattr(_lib, name)(
             self._ref, layer, r, _address(out, "out", device, q.dtype, shape),
             None if lse is None else _address(lse, "lse", device, self._f32, shape[:2]),
-            self._workspace.data_ptr(), self._workspace.numel(),
+            workspace.data_ptr(), workspace.numel(),
             None if error_bits is None else _tensor(error_bits, "error_bits", device, (self._i32,)),
             stream)
         if st:
@@ -946,14 +948,14 @@ class _CacheCalls:
 class Cache(_CacheCalls):
     """A key/value cache of the caller's (two bf16 tensors [n_layers][batch][n_kv]
     [capacity][head_dim], kept alive here) with the workspace of the operators
-    on it; see include/as2d.h, "Operators on caches and logits".  Calls on one
+    on it (prompts have one of their own, made with the first of them); see
+    include/as2d.h, "Operators on caches and logits".  Calls on one
     Cache share the workspace, so calls that may overlap on the GPU (several
     streams, captured graphs) need a Cache each.  A Cache outlives the captured
     graphs that hold its calls, and calls enqueued on a stream that was given by
     its handle; those on torch's current stream may still run when it goes."""
 
-    _WORKSPACES = ("as2d_tree_attention_workspace", "as2d_cache_evict_workspace",
-                   "as2d_prompt_attention_workspace")
+    _WORKSPACES = ("as2d_tree_attention_workspace", "as2d_cache_evict_workspace")
 
     def __init__(self, k, v):
         import torch
@@ -964,6 +966,20 @@ class Cache(_CacheCalls):
         vp = _tensor(v, "v", device, (torch.bfloat16,), k.shape)
         self.k, self.v = k, v
         self._set_up(as2d_cache(kp, vp, *k.shape), tuple(k.shape), device, k)
+        self._prompts = None
+
+    def _of_prompts(self, device, current, stream):
+        """The prompts' workspace, twice the others': made with the first prompt, as its result would be."""
+        if self._prompts is None:
+            need = _I64()
+            _check(_lib.as2d_prompt_attention_workspace(self._ref, ctypes.byref(need)), "as2d_prompt_attention_workspace")
+            like, shape = self._workspace, (need.value,)
+            self._prompts = like.new_empty(shape) if stream == current else _new_on(stream, device, like, shape)
+            self._prompts_on = stream
+        elif stream == current != self._prompts_on:
+            import torch
+            self._prompts.record_stream(torch.cuda.current_stream(device))
+        return self._prompts
 
     def append(self, q, k, v, kv_len, rows, layer=0, positions=None, q_norm=None, k_norm=None, eps=1e-6,
                theta=1e6, rotary=None, out=None, error_bits=None, stream=None):
@@ -977,7 +993,7 @@ class Cache(_CacheCalls):
                          error_bits=None, stream=None):
         """as2d_prompt_attention; returns out (made like q unless given)."""
         return self._attention("as2d_prompt_attention", q, kv_len, rows, None, scale, layer, max_len, out, lse,
-                               error_bits, stream)
+                               error_bits, stream, self._of_prompts)
 
     def tree_attention(self, q, kv_len, rows, visible=None, layer=0, scale=None, max_len=0, out=None,
                        lse=None, error_bits=None, stream=None):
