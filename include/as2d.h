@@ -716,7 +716,9 @@ typedef struct as2d_new_rows {
 /* Finish rows and append them to one layer of a cache: q_out (device [sum
    rows][n_q][head_dim] of `type`, 16-byte aligned) gets the queries, normed and
    rotated, the cache the keys, normed and rotated, and the values as they are.
-   Computed in 32 bits, angles exactly reduced for every position, and rounded once.
+   Computed in 32 bits (of a head that is normed, the squares too: beyond their range it
+   is not what the formula says), angles exactly reduced for every position, and rounded
+   once.
    kv_len stays as it is.  A request whose kv_len[b] is negative or leaves no room
    for its rows in the capacity is skipped: its cache and its rows of q_out stay as they
    were and AS2D_DEVERR_CAPACITY is ORed into error_bits (device int32 [1] or

@@ -16,9 +16,11 @@
 // code and scale is compared with the border that it is next to, which is exact in 32 bits.  (Values
 // near a border computed again in 64 bits instead: the first call of that code on an SM took 11 us.)
 //
-// Bound by memory: each value is read and written once.  7564 rows of 28 / 4 heads of 128, in bf16 (floor 20.5 us): 30.5,
-// of which a launch and the last blocks' end are some 5; 145 rows into 4 bits and read back (0.45) 10.3 on the device,
-// two launches' latency.
+// Each value is read and written once.  7564 rows of 28 / 4 heads of 128, us (floor): bf16 30.7 (20.5), 32-bit 50 (39), into
+// 4 bits 51 (19) and 75 (37).  That is 4.5 and 5.3 TB/s, not what memory has: a batch of heads is loaded when the one before
+// is stored, so that a load's time shows four times a row; in 4 bits it is the keys' arithmetic.  Few rows: a chain of
+// norm, turn and codes.  145 rows (0.4) 4.2 on the device, into 4 bits 9.3: a fourth of a row's groups do its keys and values,
+// the others go through the same code with nothing to write.
 #include <algorithm>
 #include <type_traits>
 

@@ -19,7 +19,7 @@
 //
 // Bound, one row of 28 / 4 heads of 128 (floor: the cache's 4.5 bits a value, read once): over 15128 entries (1.3 us)
 // by latency, 9.1 us on the device, of which one over 200 takes 5.1.  Over 60000 (5.1) 17.1, and 16 requests over
-// 376 .. 7495 (5.2) 20: 0.75 us a tile on an SM whether it has one CTA or two.  Of the issue slots 52 % are used
+// 376 .. 7495 (5.2) 20.2: 0.75 us a tile on an SM whether it has one CTA or two.  Of the issue slots 52 % are used
 // while it runs, of the pipe for whole numbers some 45 %: the 90 operations on bits and 96 on pairs of halves that decode a
 // warp's 16 keys and values.  (Addresses kept in registers from tile to tile: 1 % less.)
 #include <algorithm>
@@ -40,8 +40,9 @@ constexpr float kLazy = 8.f, kUp = 7.f;
 // Queries of the partial results of an SM's CTAs: two of 8, or one of 16, two parts each.
 constexpr int kParts = 2 * 16;
 
-// What turning to another item costs a CTA, in tiles: its queries, the joining of its warps. us with 0 /
-// 3 / 5 / 8: 16 requests of one row 26.4 / 21.1 / 22.0 / 22.6.
+// What turning to another item costs a CTA, in tiles: its queries, the joining of its warps. us on the device with
+// 3 / 4 / 5 / 8: 16 requests of one row over 376 .. 7495 entries 19.2 / 20.2 / 20.5 / 21.4, over 4000 19.3 / 19.9 /
+// 19.7 / 20.0, 64 over 2000 30.3 / 30.4 / 30.4 / 30.5; with none the first 26 where 3 gave 21.
 constexpr int kTurn = 4;
 
 // How the items go over the CTAs: even shares of all units, or the same number of CTAs to each item.

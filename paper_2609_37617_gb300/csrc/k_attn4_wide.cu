@@ -18,7 +18,7 @@
 // Every value that codes stand for is finite, so that what a row does not see needs no care
 // beyond a weight of 0.
 //
-// Bound by the tiles' coming: a tile (128 keys and values, 18 KB) takes an SM 1.6 us beside bf16 queries, 1.9 beside 32-bit
+// Bound by the tiles' coming: a tile (128 keys and values, 18 KB) takes an SM 1.5 us beside bf16 queries, 1.8 beside 32-bit
 // ones, whose products alone are 1.1; memory would bring one in 0.4.  448 queries of 28 / 4 heads of 128 over 60000
 // entries, us on the device with 5 / 6 / 7 loading warps: bf16 97.6 / 86.6 / 84.3, 32-bit 109 / 100.5 / 99.1 (four, each
 // with a quarter of every tile and the next tile's in registers: 85.6 / 105.8).  A sixteenth of a tile at a time, with
@@ -37,8 +37,8 @@ constexpr float kLazy = 8.f, kUp = 7.f;
 // References from here on (base 2) are rounded by a half and more (exponent_of), as they are less kUp; below, weights
 // stay within 2^15.75.
 constexpr float kFar = 8388608.f;
-// What turning to another item costs a CTA, in tiles.  us with 2 / 3 / 5: 16 requests of 126 32-bit queries over 500 entries
-// 18.5 / 20.0 / 23.3, over 4000 42.6 / 40.8 / 42.0, the ragged ones 41.2 / 37.9 / 38.9.
+// What turning to another item costs a CTA, in tiles.  us on the device with 2 / 3 / 4 / 5: 16 requests of 126 32-bit queries
+// over 500 entries 18.6 / 20.1 / 20.6 / 23.7, over 4000 43.2 / 41.2 / 42.7 / 43.0, the ragged ones 41.4 / 37.9 / 38.3 / 39.4.
 constexpr int kTurn = 3;
 
 template <int D, bool F32>

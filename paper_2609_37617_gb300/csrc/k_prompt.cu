@@ -10,7 +10,7 @@
 // as fit 256 queries (of more than 256 heads: 256 of a row).  An item is one (request, kv head,
 // pair); a CTA takes it through its key tiles of 128.  One CTA per SM takes the items in turn,
 // those of most key tiles first, back and forth over the CTAs (by the lengths on the device: eight
-// prompts of 1 to 2029 rows take 102 us in the order of their rows, 90 so).
+// prompts of 1 to 2029 rows took 102 us in the order of their rows where they took 90 so; 84 now).
 //
 // Per CTA (12 warps, TMEM full: two score buffers, two accumulators):
 //   warp 0     loads key and value tiles by TMA through a ring of shared-memory stages;
@@ -26,8 +26,8 @@
 // their sum passes kMost (or there is none yet) is the tile's maximum taken for the new one, the accumulator
 // rescaled and the weights computed again.  That keeps the chain from scores to weights, which the
 // products of one query tile wait for while the other's run, at one exponential a score.
-// Bound by the tensor cores and the chain between them.  7564 rows of 28 / 4 heads of 128 (floor 212 us): 300 to 308, the
-// tensor pipe 57 to 60 % busy; a key tile's four products read shared memory for as many cycles as they compute. Sixteen
+// Bound by the tensor cores and the chain between them.  7564 rows of 28 / 4 heads of 128 (floor 212 us): 304 to 309, the
+// tensor pipe 60 % busy; a key tile's four products read shared memory for as many cycles as they compute. Sixteen
 // softmax warps, which have to agree on a reference: 315 and more; a quarter of the exponentials by
 // polynomials: 363.  Clocks of an item (cycles): 2970 a key tile, of which the softmax of a query tile is 1900 and its two
 // products 1024; at its end 1300 until the results are there and 3700 to write them.
