@@ -1,6 +1,6 @@
 """Bounded waits of the kernels whose roles go on as whole warps: a wait's outcome is each lane's own, and
-lanes that it sent different ways would not meet again at the next warp-wide instruction.  Found in the
-source, as no run may make such waits run out."""
+lanes that it sent different ways would not meet again at the next warp-wide instruction.  Looked for in the
+source: a run has no way to let a wait give up for some lanes of a warp and not for others."""
 import os
 import re
 
